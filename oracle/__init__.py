@@ -16,6 +16,8 @@ Modules
   layers        Sec. 4: convolution, affine and pooling, both as the plain
                 (sequential) definition and as the paper's distributed
                 algorithms; the point-wise / loss glue of the Sec. 5 network.
+  blocks        beyond the paper: the operators of gated recurrent blocks
+                (norm, 8-bit numbers, recurrence, AdamW), whole tensors.
 
 Parity pins: every function here is checked in tests/ (run with -m "not gpu")
 against values the paper prints (App. B.1 examples, App. C table), against
