@@ -402,6 +402,144 @@ int distdl_dot_static(const void* const a_dev[], const void* const b_dev[], cons
                       distdl_dtype dtype, double* result_dev, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Operators of gated recurrent blocks and of their training step, on the same
+ * partitions: features or time are split over workers by the balanced split,
+ * a worker's array is dense and row-major.  The conventions at the top hold,
+ * with these differences: pointer arrays of up to 16 workers (8 for the norm)
+ * travel with the launch, so a call with arrays that a plan has not seen
+ * neither copies a table nor fails while its stream is being captured (the
+ * update of many arrays does both, as the other layers do); scratch is still
+ * allocated by a plan's first call on a stream.
+ *
+ * 8-BIT NUMBERS.  A code is e4m3 (no infinities, largest 448); a block of 128
+ * consecutive numbers of a row shares a scale 2^(byte - 127), one byte
+ * (e8m0): the smallest power of two for which no magnitude of the block
+ * exceeds 448 codes, at least 2^-126.  A row's last block may be short.  A NaN
+ * is a NaN code and leaves the rest of its block alone; a block that holds an
+ * infinity gets the byte 255 and stands for NaN throughout.  Scales of a
+ * matrix [rows][cols] in blocks of rows lie as [ceil(cols / 128)][rows]: the
+ * scales of a product's rows for one block are one run.  In tiles of
+ * 128 x 128 they lie as [ceil(rows / 128)][ceil(cols / 128)].
+ *
+ * quant8: every x_dev[i], rows[i] x cols[i] of `dtype`, to codes q and scales
+ *   s of its rows, and codes qt [cols][rows] and scales st of the rows of its
+ *   transpose; either pair may be NULL.  tiles != 0: one scale for each tile
+ *   of 128 x 128, the same in both orders.  Outputs must not overlap inputs.
+ * ---------------------------------------------------------------------- */
+int distdl_quant8(const void* const x_dev[], const int64_t rows[], const int64_t cols[], int n_arrays, int tiles,
+                  void* const q_dev[], void* const s_dev[], void* const qt_dev[], void* const st_dev[],
+                  distdl_dtype dtype, void* stream);
+
+/* Partitioned layer without bias on 8-bit operands; worker (i, j) of the
+ * weights has id i*P_fi + j as in the affine layer.  Sums are fp32; y and dx
+ * have the plan's dtype (rounded once, nearest even), dW is fp32.
+ *
+ * fwd:   y_i [n_b][fo_i] = sum_j x_j W_ij^T, x_j in blocks of rows, W_ij
+ *        [fo_i][fi_j] in tiles
+ * bwd_x: dx_j [n_b][fi_j] = sum_i dy_i W_ij, dy_i in blocks of rows, wt_ij
+ *        [fi_j][fo_i] (the transpose) in tiles
+ * bwd_w: dW_ij [fo_i][fi_j] = dy_i^T x_j, from dyt_i [fo_i][n_b] and xt_j
+ *        [fi_j][n_b] in blocks of rows (that is, along the batch)
+ * Each is what distdl_quant8 writes.  Outputs must not overlap inputs. */
+typedef struct distdl_linear8_plan distdl_linear8_plan;
+int distdl_linear8_plan_create(distdl_linear8_plan** out, int64_t n_b, int64_t n_fi, int64_t n_fo, int P_fo,
+                               int P_fi, distdl_dtype dtype);
+int distdl_linear8_plan_destroy(distdl_linear8_plan* plan);
+int distdl_linear8_fwd(distdl_linear8_plan* plan, const void* const xq_dev[], const void* const xs_dev[],
+                       const void* const wq_dev[], const void* const ws_dev[], void* const y_dev[], void* stream);
+int distdl_linear8_bwd_x(distdl_linear8_plan* plan, const void* const dyq_dev[], const void* const dys_dev[],
+                         const void* const wtq_dev[], const void* const wts_dev[], void* const dx_dev[],
+                         void* stream);
+int distdl_linear8_bwd_w(distdl_linear8_plan* plan, const void* const dytq_dev[], const void* const dyts_dev[],
+                         const void* const xtq_dev[], const void* const xts_dev[], float* const dw_dev[],
+                         void* stream);
+
+/* Root-mean-square norm of rows whose n_f features P workers share; x_j is
+ * [rows][f_j], g_j [f_j] fp32.  The sum over features is the all-reduce of
+ * the workers' sums.
+ *
+ * fwd: s = x + r (r_dev may be NULL: s = x);  rstd = 1 / sqrt(mean(s^2) + eps);
+ *      y = s rstd g.  Any of the outputs s, y, codes q with scales qs, and
+ *      rstd [rows] may be NULL, not all.  y and q are made from the unrounded
+ *      s.  s may lie on x or r, y on x or r where s is NULL or lies elsewhere.
+ * bwd: from s, g, rstd, dy and dsum (the gradient that reaches s beside the
+ *      norm; may be NULL): dx = dsum + rstd (dy g - n mean(dy g n)) with
+ *      n = s rstd, the gradient of both x and r, and dg = sum over rows of
+ *      dy n, in fp32 and in a fixed order.  dx may lie on dy, dsum or s.
+ * rows may be 0 (dg is 0 then). */
+typedef struct distdl_rmsnorm_plan distdl_rmsnorm_plan;
+int distdl_rmsnorm_plan_create(distdl_rmsnorm_plan** out, int64_t rows, int64_t n_f, int P, double eps,
+                               distdl_dtype dtype);
+int distdl_rmsnorm_plan_destroy(distdl_rmsnorm_plan* plan);
+int distdl_rmsnorm_fwd(distdl_rmsnorm_plan* plan, const void* const x_dev[], const void* const r_dev[],
+                       const float* const g_dev[], void* const s_dev[], void* const y_dev[], void* const q_dev[],
+                       void* const qs_dev[], float* rstd_dev, void* stream);
+int distdl_rmsnorm_bwd(distdl_rmsnorm_plan* plan, const void* const s_dev[], const float* const g_dev[],
+                       const float* rstd_dev, const void* const dy_dev[], const void* const dsum_dev[],
+                       void* const dx_dev[], float* const dg_dev[], void* stream);
+
+/* Gated linear recurrence over T steps that P workers share; a worker's
+ * arrays are [n_b][T_p][n_c] of the plan's dtype, states [n_b][n_c] are fp32.
+ *   GIVEN    h_t = a_t h_{t-1} + x_t
+ *   SIGMOID  h_t = s_t h_{t-1} + (1 - s_t) x_t,  s_t = 1 / (1 + exp(-a_t))
+ * fwd: h of all steps and, if not NULL, the last state hT.  h0 NULL: zeros.
+ *   lengths [n_b] (int32, NULL: all T; values are cut to 0 .. T): steps from
+ *   a sequence's length on are not read, their h is 0, and hT is the state
+ *   at its end, h0 for an empty sequence.  h may lie on a or x.
+ * bwd: from a, x (not read with given gates; may be NULL), the h that fwd
+ *   wrote, dh and dhT (NULL: zeros): da, dx and, if not NULL, dh0.  Steps
+ *   from a sequence's length on get zeros.  da may lie on a, dx on x or dh.
+ * step: one token for each row: state_dev[slots[row]] is read and
+ *   overwritten, h is the new state in the tensor's type.  slots NULL: row i has
+ *   state i.  A row whose slot is not in 0 .. n_slots - 1 is idle: its h is 0
+ *   and no state changes.  Slots of one call must differ. */
+typedef enum { DISTDL_GATE_GIVEN = 0, DISTDL_GATE_SIGMOID = 1 } distdl_gate;
+typedef struct distdl_scan_plan distdl_scan_plan;
+int distdl_scan_plan_create(distdl_scan_plan** out, int64_t n_b, int64_t T, int64_t n_c, int P, distdl_gate gate,
+                            distdl_dtype dtype);
+int distdl_scan_plan_destroy(distdl_scan_plan* plan);
+int distdl_scan_fwd(distdl_scan_plan* plan, const void* const a_dev[], const void* const x_dev[],
+                    const float* h0_dev, const int32_t* lengths_dev, void* const h_dev[], float* hT_dev,
+                    void* stream);
+int distdl_scan_bwd(distdl_scan_plan* plan, const void* const a_dev[], const void* const x_dev[],
+                    const void* const h_dev[], const float* h0_dev, const int32_t* lengths_dev,
+                    const void* const dh_dev[], const float* dhT_dev, void* const da_dev[], void* const dx_dev[],
+                    float* dh0_dev, void* stream);
+int distdl_scan_step(const void* a_dev, const void* x_dev, float* state_dev, int64_t n_slots,
+                     const int32_t* slots_dev, void* h_dev, int64_t rows, int64_t n_c, distdl_gate gate,
+                     distdl_dtype dtype, void* stream);
+
+/* AdamW over many arrays at once: count[i] weights p (fp32) each, gradients g
+ * of g_dtype, first and second moments, in one launch.
+ *   g' = g * *gscale_dev (NULL: 1);  m = beta1 m + (1 - beta1) g';
+ *   v = beta2 v + (1 - beta2) g'^2;
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * with t = *step_dev if that is not NULL (what a recorded step needs), else
+ * step, from 1 on.  copy_dev, or any copy_dev[i], may be NULL: else p
+ * rounded to bf16 goes there.
+ * states8 = 0: m and v are fp32.  states8 = 1: m and sqrt(v) are 8-bit
+ * numbers in blocks of 128 of an array, scales ms and vs (ceil(count / 128)
+ * bytes), rounded up or down at random so that a moving average keeps its
+ * mean; a positive sqrt(v) stays positive.  The random bits are a function of
+ * seed, t and the number's place; equal calls give equal bits.  Codes and
+ * scales that are all zero are the start.  p is made from the unrounded
+ * moments.  Counts may be 0.  Arrays of a call must not overlap. */
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;
+  int64_t step;
+  const int64_t* step_dev;
+  const float* gscale_dev;
+  uint32_t seed;
+} distdl_adamw_args;
+typedef struct distdl_adamw_plan distdl_adamw_plan;
+int distdl_adamw_plan_create(distdl_adamw_plan** out, const int64_t count[], int n_arrays, distdl_dtype g_dtype,
+                             int states8);
+int distdl_adamw_plan_destroy(distdl_adamw_plan* plan);
+int distdl_adamw_step(distdl_adamw_plan* plan, void* const p_dev[], const void* const g_dev[], void* const m_dev[],
+                      void* const v_dev[], void* const ms_dev[], void* const vs_dev[], void* const copy_dev[],
+                      const distdl_adamw_args* args, void* stream);
+
+/* ------------------------------------------------------------------------
  * Measurement support.  plan_stats: cell counts behind the algorithmic-bytes
  * figures of the halo kernels, summed over all workers and per sample and
  * channel: out[0] halo cells (in-domain, non-owned), out[1] zero-padding

@@ -80,6 +80,24 @@ _SIGS = {
     "distdl_affine_plan_destroy": [_vp],
     "distdl_affine_fwd": [_vp, _pp, _pp, _pp, _pp, _vp],
     "distdl_affine_bwd": [_vp, _pp, _pp, _pp, _pp, _pp, _pp, _vp],
+    "distdl_quant8": [_pp, _p64, _p64, _i, _i, _pp, _pp, _pp, _pp, _i, _vp],
+    "distdl_linear8_plan_create": [C.POINTER(_vp), _i64, _i64, _i64, _i, _i, _i],
+    "distdl_linear8_plan_destroy": [_vp],
+    "distdl_linear8_fwd": [_vp, _pp, _pp, _pp, _pp, _pp, _vp],
+    "distdl_linear8_bwd_x": [_vp, _pp, _pp, _pp, _pp, _pp, _vp],
+    "distdl_linear8_bwd_w": [_vp, _pp, _pp, _pp, _pp, _pp, _vp],
+    "distdl_rmsnorm_plan_create": [C.POINTER(_vp), _i64, _i64, _i, C.c_double, _i],
+    "distdl_rmsnorm_plan_destroy": [_vp],
+    "distdl_rmsnorm_fwd": [_vp, _pp, _pp, _pp, _pp, _pp, _pp, _pp, _vp, _vp],
+    "distdl_rmsnorm_bwd": [_vp, _pp, _pp, _vp, _pp, _pp, _pp, _pp, _vp],
+    "distdl_scan_plan_create": [C.POINTER(_vp), _i64, _i64, _i64, _i, _i, _i],
+    "distdl_scan_plan_destroy": [_vp],
+    "distdl_scan_fwd": [_vp, _pp, _pp, _vp, _vp, _pp, _vp, _vp],
+    "distdl_scan_bwd": [_vp, _pp, _pp, _pp, _vp, _vp, _pp, _vp, _pp, _pp, _vp, _vp],
+    "distdl_scan_step": [_vp, _vp, _vp, _i64, _vp, _vp, _i64, _i64, _i, _i, _vp],
+    "distdl_adamw_plan_create": [C.POINTER(_vp), _p64, _i, _i, _i],
+    "distdl_adamw_plan_destroy": [_vp],
+    "distdl_adamw_step": [_vp, _pp, _pp, _pp, _pp, _pp, _pp, _pp, _vp, _vp],
     "distdl_dot": [_pp, _pp, _p64, _i, _i, _vp, _vp],
     "distdl_dot_static": [_pp, _pp, _p64, _i, _i, _vp, _vp],
     "distdl_relu_fwd": [_pp, _pp, _p64, _i, _vp],
@@ -447,6 +465,209 @@ def distdl_affine_fwd(plan, x, W, b, y):
 def distdl_affine_bwd(plan, x, W, dy, dx, dW, db):
     _check(lib.distdl_affine_bwd(plan.handle, _ptrs(x), _ptrs(W), _ptrs(dy), _ptrs(dx), _ptrs(dW),
                                  None if db is None else _ptrs(db), _stream()))
+
+
+# ---- operators of gated recurrent blocks -----------------------------------
+# Their kernels trust the extents that a plan was made for, so the tensors are held against it here: type, elements, layout, device.
+
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+_SCALES = (torch.float8_e8m0fnu, torch.uint8)
+BLOCK8 = 128
+
+
+def _blocks8(n):
+    return -(-n // BLOCK8)
+
+
+def _split(n, parts):
+    return [n // parts + (r < n % parts) for r in range(parts)]
+
+
+def _one(what, t, kinds, numel):
+    """The address of a dense device tensor of `numel` elements of one of `kinds`."""
+    if t.dtype not in kinds or t.numel() != numel or not t.is_contiguous() or not t.is_cuda:
+        raise DistdlError(ERR_INVALID_ARG, f"{what}: a {'' if t.is_contiguous() else 'strided '}{t.dtype} tensor of shape {tuple(t.shape)} "
+                                           f"on {t.device}, where {numel} dense elements of {' or '.join(map(str, kinds))} on a GPU are wanted")
+    return t.data_ptr()
+
+
+def _many(what, ts, kinds, numels):
+    """The host array of their addresses; None stays NULL."""
+    if ts is None:
+        return None
+    if len(ts) != len(numels):
+        raise DistdlError(ERR_INVALID_ARG, f"{what}: {len(ts)} tensors, {len(numels)} are wanted")
+    return (C.c_void_p * len(ts))(*[_one(what, t, kinds, n) for t, n in zip(ts, numels)])
+
+
+def _maybe(what, t, kinds, numel):
+    return None if t is None else _one(what, t, kinds, numel)
+
+
+class _Handle:
+    """Owner of a plan's handle; destroy: the library's call that ends it."""
+
+    def __init__(self, handle, destroy, **what):
+        self.handle, self._destroy = handle, destroy
+        self.__dict__.update(what)
+
+    def destroy(self):
+        if self.handle:
+            self._destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+_F32 = (torch.float32,)
+
+
+def distdl_quant8(x, q, s, qt, st, tiles=False):
+    """x: 2-D tensors.  Codes q and scales s in blocks of their rows, qt and st in blocks of the rows of their transposes; either pair
+    may be None.  tiles: one scale for each 128 x 128."""
+    rows, cols = [], []
+    for t in x:
+        if t.dim() != 2:
+            raise DistdlError(ERR_INVALID_ARG, f"quant8: a tensor of shape {tuple(t.shape)}, where two dimensions are wanted")
+        rows.append(t.shape[0])
+        cols.append(t.shape[1])
+    numels = [r * c for r, c in zip(rows, cols)]
+    n = len(numels)
+    if n == 0:
+        raise DistdlError(ERR_INVALID_ARG, "quant8: no tensors")
+    one = [_blocks8(c) * (_blocks8(r) if tiles else r) for r, c in zip(rows, cols)]
+    other = [_blocks8(r) * (_blocks8(c) if tiles else c) for r, c in zip(rows, cols)]
+    kind = x[0].dtype
+    _check(lib.distdl_quant8(_many("x", x, (kind,), numels), (C.c_int64 * n)(*rows), (C.c_int64 * n)(*cols), n, int(tiles),
+                             _many("q", q, _CODES, numels), _many("s", s, _SCALES, one), _many("qt", qt, _CODES, numels),
+                             _many("st", st, _SCALES, other), _dtype_code(kind), _stream()))
+
+
+def distdl_linear8_plan_create(n_b, n_fi, n_fo, P_fo, P_fi, dtype=torch.bfloat16):
+    h = C.c_void_p()
+    _check(lib.distdl_linear8_plan_create(C.byref(h), n_b, n_fi, n_fo, P_fo, P_fi, _dtype_code(dtype)))
+    fo, fi = _split(n_fo, P_fo), _split(n_fi, P_fi)
+    kind = _F32 if _dtype_code(dtype) == DISTDL_F32 else (torch.bfloat16,)
+    return _Handle(h, lib.distdl_linear8_plan_destroy, kind=kind,
+                   nx=[n_b * n for n in fi], nxs=[n_b * _blocks8(n) for n in fi], ny=[n_b * n for n in fo], nys=[n_b * _blocks8(n) for n in fo],
+                   nw=[m * n for m in fo for n in fi], nws=[_blocks8(m) * _blocks8(n) for m in fo for n in fi],
+                   nxts=[_blocks8(n_b) * n for n in fi], nyts=[_blocks8(n_b) * n for n in fo])
+
+
+def distdl_linear8_fwd(plan, xq, xs, wq, ws, y):
+    _check(lib.distdl_linear8_fwd(plan.handle, _many("xq", xq, _CODES, plan.nx), _many("xs", xs, _SCALES, plan.nxs),
+                                  _many("wq", wq, _CODES, plan.nw), _many("ws", ws, _SCALES, plan.nws), _many("y", y, plan.kind, plan.ny),
+                                  _stream()))
+
+
+def distdl_linear8_bwd_x(plan, dyq, dys, wtq, wts, dx):
+    _check(lib.distdl_linear8_bwd_x(plan.handle, _many("dyq", dyq, _CODES, plan.ny), _many("dys", dys, _SCALES, plan.nys),
+                                    _many("wtq", wtq, _CODES, plan.nw), _many("wts", wts, _SCALES, plan.nws),
+                                    _many("dx", dx, plan.kind, plan.nx), _stream()))
+
+
+def distdl_linear8_bwd_w(plan, dytq, dyts, xtq, xts, dw):
+    _check(lib.distdl_linear8_bwd_w(plan.handle, _many("dytq", dytq, _CODES, plan.ny), _many("dyts", dyts, _SCALES, plan.nyts),
+                                    _many("xtq", xtq, _CODES, plan.nx), _many("xts", xts, _SCALES, plan.nxts),
+                                    _many("dw", dw, _F32, plan.nw), _stream()))
+
+
+def distdl_rmsnorm_plan_create(rows, n_f, P, eps, dtype=torch.bfloat16):
+    h = C.c_void_p()
+    _check(lib.distdl_rmsnorm_plan_create(C.byref(h), rows, n_f, P, eps, _dtype_code(dtype)))
+    f = _split(n_f, P)
+    kind = _F32 if _dtype_code(dtype) == DISTDL_F32 else (torch.bfloat16,)
+    return _Handle(h, lib.distdl_rmsnorm_plan_destroy, kind=kind, f=f, rows=rows, n=[rows * n for n in f], ns=[rows * _blocks8(n) for n in f])
+
+
+def distdl_rmsnorm_fwd(plan, x, r, g, s, y, q, qs, rstd):
+    """r, and any of the outputs s, y, (q, qs), rstd, may be None."""
+    _check(lib.distdl_rmsnorm_fwd(plan.handle, _many("x", x, plan.kind, plan.n), _many("r", r, plan.kind, plan.n), _many("g", g, _F32, plan.f),
+                                  _many("s", s, plan.kind, plan.n), _many("y", y, plan.kind, plan.n), _many("q", q, _CODES, plan.n),
+                                  _many("qs", qs, _SCALES, plan.ns), _maybe("rstd", rstd, _F32, plan.rows), _stream()))
+
+
+def distdl_rmsnorm_bwd(plan, s, g, rstd, dy, dsum, dx, dg):
+    """dsum may be None."""
+    _check(lib.distdl_rmsnorm_bwd(plan.handle, _many("s", s, plan.kind, plan.n), _many("g", g, _F32, plan.f), _one("rstd", rstd, _F32, plan.rows),
+                                  _many("dy", dy, plan.kind, plan.n), _many("dsum", dsum, plan.kind, plan.n),
+                                  _many("dx", dx, plan.kind, plan.n), _many("dg", dg, _F32, plan.f), _stream()))
+
+
+GATE_GIVEN, GATE_SIGMOID = 0, 1
+_GATES = {"given": GATE_GIVEN, "sigmoid": GATE_SIGMOID, GATE_GIVEN: GATE_GIVEN, GATE_SIGMOID: GATE_SIGMOID}
+
+
+def _gate_code(gate):
+    if gate not in _GATES:
+        raise DistdlError(ERR_UNSUPPORTED, f"gate {gate}")
+    return _GATES[gate]
+
+
+def distdl_scan_plan_create(n_b, T, n_c, P, gate, dtype=torch.bfloat16):
+    """gate: "given" or "sigmoid"."""
+    h = C.c_void_p()
+    _check(lib.distdl_scan_plan_create(C.byref(h), n_b, T, n_c, P, _gate_code(gate), _dtype_code(dtype)))
+    kind = _F32 if _dtype_code(dtype) == DISTDL_F32 else (torch.bfloat16,)
+    return _Handle(h, lib.distdl_scan_plan_destroy, kind=kind, n=[n_b * t * n_c for t in _split(T, P)], state=n_b * n_c, n_b=n_b)
+
+
+def distdl_scan_fwd(plan, a, x, h0, lengths, h, hT):
+    """h0, lengths and hT may be None."""
+    _check(lib.distdl_scan_fwd(plan.handle, _many("a", a, plan.kind, plan.n), _many("x", x, plan.kind, plan.n), _maybe("h0", h0, _F32, plan.state),
+                               _maybe("lengths", lengths, (torch.int32,), plan.n_b), _many("h", h, plan.kind, plan.n),
+                               _maybe("hT", hT, _F32, plan.state), _stream()))
+
+
+def distdl_scan_bwd(plan, a, x, h, h0, lengths, dh, dhT, da, dx, dh0):
+    """h0, lengths, dhT and dh0 may be None, and x with given gates."""
+    _check(lib.distdl_scan_bwd(plan.handle, _many("a", a, plan.kind, plan.n), _many("x", x, plan.kind, plan.n), _many("h", h, plan.kind, plan.n),
+                               _maybe("h0", h0, _F32, plan.state), _maybe("lengths", lengths, (torch.int32,), plan.n_b),
+                               _many("dh", dh, plan.kind, plan.n), _maybe("dhT", dhT, _F32, plan.state), _many("da", da, plan.kind, plan.n),
+                               _many("dx", dx, plan.kind, plan.n), _maybe("dh0", dh0, _F32, plan.state), _stream()))
+
+
+def distdl_scan_step(a, x, state, slots, h, gate):
+    """a, x, h: [rows, n_c]; state: fp32 [n_slots, n_c]; slots: int32 [rows], or None for state i of row i."""
+    if a.dim() != 2 or state.dim() != 2 or state.shape[1] != a.shape[1]:
+        raise DistdlError(ERR_INVALID_ARG, f"scan_step: gates of shape {tuple(a.shape)}, states of shape {tuple(state.shape)}")
+    kind, n = (a.dtype,), a.numel()
+    _check(lib.distdl_scan_step(_one("a", a, kind, n), _one("x", x, kind, n), _one("state", state, _F32, state.numel()), state.shape[0],
+                                _maybe("slots", slots, (torch.int32,), a.shape[0]), _one("h", h, kind, n), a.shape[0], a.shape[1],
+                                _gate_code(gate), _dtype_code(a.dtype), _stream()))
+
+
+class AdamwArgs(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+                ("step", C.c_int64), ("step_dev", C.c_void_p), ("gscale_dev", C.c_void_p), ("seed", C.c_uint32)]
+
+
+def distdl_adamw_plan_create(counts, g_dtype=torch.float32, states8=False):
+    counts = [int(n) for n in counts]
+    h = C.c_void_p()
+    _check(lib.distdl_adamw_plan_create(C.byref(h), _arr(C.c_int64, counts), len(counts), _dtype_code(g_dtype), int(states8)))
+    return _Handle(h, lib.distdl_adamw_plan_destroy, counts=counts, blocks=[_blocks8(n) for n in counts],
+                   g_kind=_F32 if _dtype_code(g_dtype) == DISTDL_F32 else (torch.bfloat16,), state_kind=_CODES if states8 else _F32, states8=states8)
+
+
+def distdl_adamw_step(plan, p, g, m, v, ms=None, vs=None, p16=None, *, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, step=0, seed=0,
+                      step_dev=None, gscale=None):
+    """Updates p, m and v (8-bit states: the codes m of the first moment and v of the second's root, and their scales) in place, and
+    writes the bf16 copies p16 if given.  step_dev: int64 on the device, in the place of step.  gscale: one fp32 number on the device."""
+    if plan.states8 and (ms is None or vs is None):
+        raise DistdlError(ERR_NULL, "adamw_step: 8-bit moments need their scales")
+    args = AdamwArgs(lr, beta1, beta2, eps, weight_decay, step, _maybe("step_dev", step_dev, (torch.int64,), 1),
+                     _maybe("gscale", gscale, _F32, 1), seed & 0xFFFFFFFF)
+    n = plan.counts
+    scales = plan.states8
+    _check(lib.distdl_adamw_step(plan.handle, _many("p", p, _F32, n), _many("g", g, plan.g_kind, n), _many("m", m, plan.state_kind, n),
+                                 _many("v", v, plan.state_kind, n), _many("ms", ms, _SCALES, plan.blocks) if scales else None,
+                                 _many("vs", vs, _SCALES, plan.blocks) if scales else None, _many("p16", p16, (torch.bfloat16,), n),
+                                 C.byref(args), _stream()))
 
 
 def _numels(ts):

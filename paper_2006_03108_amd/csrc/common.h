@@ -26,6 +26,16 @@ int set_error(int code, const char* fmt, ...);
       return ::distdl::set_error(DISTDL_ERR_HIP, "%s failed: %s", #expr, hipGetErrorString(e__)); \
   } while (0)
 
+// What an entry point does, with a C++ exception (there is no other than a failed allocation) as an error code.
+template <class F>
+inline int guarded(F f) {
+  try {
+    return f();
+  } catch (...) {
+    return set_error(DISTDL_ERR_NOMEM, "out of host memory");
+  }
+}
+
 inline size_t dtype_size(distdl_dtype t) { return t == DISTDL_F32 ? 4 : 2; }
 
 // Estimated times (us) of what the host and the device take for the same call: the longer one, and more where they are alike.

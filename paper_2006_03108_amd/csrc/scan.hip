@@ -1,0 +1,622 @@
+// Gated linear recurrence over time that P workers share, its adjoint, and the step of single tokens.
+//
+//   given gates      h_t = a_t h_{t-1} + x_t
+//   sigmoid gates    h_t = a_t h_{t-1} + (1 - a_t) x_t,  a_t = 1 / (1 + exp(-g_t))
+//   adjoint          d_t = dh_t + b_{t+1},  b_t = a_t d_t,  b_len = dhT,  dh_0 = b_0;  du_t = d_t,  da_t = d_t h_{t-1}
+//
+// Each channel is a chain of its own; along time the steps are affine maps, which compose: (A, B) after (A', B') is
+// (A A', A B' + B).  So a workgroup of eight waves takes a tile of steps, L to a wave, and 64 V channels: each wave composes its steps,
+// the eight maps meet in LDS, and each wave then runs its steps from the state in front of it, all from registers.  Where
+// sequences and channels are too few for that to fill the card, time is cut into segments as well: a first launch composes each
+// segment's map, the second starts every segment from the maps before it (time is read twice there, once from HBM).
+// The workers' boundaries are those of arrays only: a state passes them as it passes tiles.
+#include <algorithm>
+
+#include "block8.h"
+#include "common.h"
+#include "profile.h"
+
+namespace distdl {
+
+constexpr int kScanInline = 16;  // workers whose pointers travel with the launch; more are in a table
+constexpr int kScanWaves = 8;
+constexpr int kScanV = 2;        // channels of a lane
+constexpr int kScanCols = 64 * kScanV;
+
+struct ScanWorker {
+  const void *a, *x, *h, *dh;  // h: input of the adjoint
+  void *o0, *o1;               // forward: h; adjoint: da, dx
+};
+
+struct ScanArgs {
+  ScanWorker w[kScanInline];
+  const ScanWorker* more;
+  int64_t T, n_c;
+  int64_t part, extra;   // worker p has part + (p < extra) steps
+  int32_t P, n_b, groups, segments;
+  int64_t seg_steps;
+  const int32_t* lengths;
+  const float *h0, *end;  // end: dhT of the adjoint
+  float *hT;              // forward: hT; adjoint: dh0
+  float* maps;            // [n_b][segments][2][n_c]
+};
+
+__device__ __forceinline__ const ScanWorker& scan_worker(const ScanArgs& s, int p) { return s.more ? s.more[p] : s.w[p]; }
+
+struct ScanSpan {  // the worker that holds step t, and its steps
+  int p;
+  int64_t lo, hi;
+};
+__device__ __forceinline__ ScanSpan scan_span(const ScanArgs& s, int64_t t) {
+  const int64_t wide = s.extra * (s.part + 1);
+  ScanSpan r;
+  if (t < wide) {
+    r.p = (int)(t / (s.part + 1));
+    r.lo = r.p * (s.part + 1);
+    r.hi = r.lo + s.part + 1;
+  } else {
+    r.p = (int)(s.extra + (t - wide) / s.part);
+    r.lo = wide + (r.p - s.extra) * s.part;
+    r.hi = r.lo + s.part;
+  }
+  return r;
+}
+
+// Two channels of one step: n of them exist.
+__device__ __forceinline__ u32x2 scan_load(const float* p, int n) {
+  if (n >= 2) return *(const u32x2_any*)p;
+  return u32x2{n > 0 ? __float_as_uint(*p) : 0u, 0u};
+}
+typedef uint32_t u32_any __attribute__((aligned(1)));
+__device__ __forceinline__ uint32_t scan_load(const uint16_t* p, int n) {
+  if (n >= 2) return *(const u32_any*)p;
+  return n > 0 ? (uint32_t)*p : 0u;
+}
+__device__ __forceinline__ void scan_values(u32x2 r, float* v) {
+  v[0] = __uint_as_float(r[0]);
+  v[1] = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ void scan_values(uint32_t r, float* v) {
+  v[0] = bf16_lo(r);
+  v[1] = bf16_hi(r);
+}
+__device__ __forceinline__ void scan_store(float* p, const float* v, int n) {
+  if (n >= 2) *(u32x2_any*)p = u32x2{__float_as_uint(v[0]), __float_as_uint(v[1])};
+  else if (n > 0) *p = v[0];
+}
+__device__ __forceinline__ void scan_store(uint16_t* p, const float* v, int n) {
+  if (n >= 2) *(u32_any*)p = to_bf16(v[0]) | to_bf16(v[1]) << 16;
+  else if (n > 0) *p = (uint16_t)to_bf16(v[0]);
+}
+template <class E>
+struct ScanRaw;
+template <>
+struct ScanRaw<float> {
+  typedef u32x2 type;
+};
+template <>
+struct ScanRaw<uint16_t> {
+  typedef uint32_t type;
+};
+
+// a and 1 - a.  Through exp(-|g|), which neither overflows nor loses 1 - a where a is near one.
+template <int GATE>
+__device__ __forceinline__ void scan_gate(float g, float& a, float& rest) {
+  if constexpr (GATE == DISTDL_GATE_GIVEN) {
+    a = g;
+    rest = 1.f;
+  } else {
+    const float e = __expf(-fabsf(g)), r = __builtin_amdgcn_rcpf(1.f + e);
+    a = g >= 0.f ? r : e * r;
+    rest = g >= 0.f ? e * r : r;
+  }
+}
+
+struct ScanPlace {
+  int group, seg, b, c, n;  // n: channels of this lane
+  int64_t len, lo, hi;      // steps of the sequence; of the segment
+};
+__device__ __forceinline__ ScanPlace scan_place(const ScanArgs& s) {
+  ScanPlace r;
+  uint32_t at = blockIdx.x;
+  r.group = at % s.groups;
+  at /= s.groups;
+  r.b = at % s.n_b;
+  r.seg = at / s.n_b;
+  r.c = r.group * kScanCols + (threadIdx.x & 63) * kScanV;
+  r.n = (int)max((int64_t)0, min((int64_t)kScanV, s.n_c - r.c));
+  r.len = s.lengths ? max((int64_t)0, min(s.T, (int64_t)s.lengths[r.b])) : s.T;
+  r.lo = r.seg * s.seg_steps;
+  r.hi = min(s.T, r.lo + s.seg_steps);
+  return r;
+}
+
+// The maps of all waves, each behind the one before it: `mine` is the state in front of this wave's steps, `state` that behind the tile.
+__device__ __forceinline__ void scan_meet(float (*lds)[2][kScanCols], const float* A, const float* B, float* state, float* mine) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v) {
+    lds[wave][0][v * 64 + lane] = A[v];
+    lds[wave][1][v * 64 + lane] = B[v];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kScanWaves; ++w) {
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) {
+      if (w == wave) mine[v] = state[v];
+      state[v] = fmaf(lds[w][0][v * 64 + lane], state[v], lds[w][1][v * 64 + lane]);
+    }
+  }
+}
+
+// The state in front of a segment: that of the sequence through the maps of the segments before (behind) it.
+template <bool BACK>
+__device__ __forceinline__ void scan_start(const ScanArgs& s, const ScanPlace& at, float* state) {
+  const float* from = BACK ? s.end : s.h0;
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v) state[v] = from && v < at.n ? from[at.b * s.n_c + at.c + v] : 0.f;
+  const int n = BACK ? s.segments - 1 - at.seg : at.seg;
+  for (int i = 0; i < n; ++i) {
+    const float* m = s.maps + ((int64_t)at.b * s.segments + (BACK ? s.segments - 1 - i : i)) * 2 * s.n_c + at.c;
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v)
+      if (v < at.n) state[v] = fmaf(m[v], state[v], m[s.n_c + v]);
+  }
+}
+
+// A segment's map: a wave composes an eighth of the steps, the eighths meet at the end.
+template <class E, int GATE, bool BACK>
+__global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
+  constexpr int L = 16;
+  __shared__ float lds[kScanWaves][2][kScanCols];
+  const ScanPlace at = scan_place(s);
+  const int wave = BACK ? kScanWaves - 1 - (threadIdx.x >> 6) : threadIdx.x >> 6;
+  const int64_t hi = min(at.hi, at.len), each = (max((int64_t)0, hi - at.lo) + kScanWaves - 1) / kScanWaves;
+  const int64_t from = min(hi, at.lo + wave * each), to = min(hi, from + each);
+  typedef typename ScanRaw<E>::type Raw;
+  float A[kScanV], B[kScanV];
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v) {
+    A[v] = 1.f;
+    B[v] = 0.f;
+  }
+  for (int64_t done = 0; done < to - from;) {
+    // the next run of at most L steps of one worker, forwards or backwards
+    const int64_t t = BACK ? to - 1 - done : from + done;
+    const ScanSpan sp = scan_span(s, t);
+    const int cnt = (int)min((int64_t)L, BACK ? t + 1 - max(from, sp.lo) : min(to, sp.hi) - t);
+    const ScanWorker& w = scan_worker(s, sp.p);
+    const int64_t row = (int64_t)at.b * (sp.hi - sp.lo) + (t - sp.lo);
+    Raw ra[L], rx[L];
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (i < cnt) {
+        const int64_t o = (row + (BACK ? -i : i)) * s.n_c + at.c;
+        ra[i] = scan_load((const E*)w.a + o, at.n);
+        rx[i] = scan_load((const E*)(BACK ? w.dh : w.x) + o, at.n);
+      }
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (i < cnt) {
+        float g[kScanV], x[kScanV];
+        scan_values(ra[i], g);
+        scan_values(rx[i], x);
+#pragma unroll
+        for (int v = 0; v < kScanV; ++v) {
+          float a, rest;
+          scan_gate<GATE>(g[v], a, rest);
+          A[v] *= a;
+          B[v] = BACK ? a * (B[v] + x[v]) : fmaf(a, B[v], rest * x[v]);
+        }
+      }
+    done += cnt;
+  }
+  float state[kScanV] = {}, mine[kScanV], all[kScanV];
+  scan_meet(lds, A, B, state, mine);  // B of the whole: the map of zero
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v) {
+    all[v] = 1.f;
+    for (int w = 0; w < kScanWaves; ++w) all[v] *= lds[w][0][v * 64 + lane];
+  }
+  if (threadIdx.x < 64) {
+    float* m = s.maps + ((int64_t)at.b * s.segments + at.seg) * 2 * s.n_c + at.c;
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v)
+      if (v < at.n) {
+        m[v] = all[v];
+        m[s.n_c + v] = state[v];
+      }
+  }
+}
+
+template <class E, int GATE>
+__global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
+  constexpr int L = 16;
+  __shared__ float lds[2][kScanWaves][2][kScanCols];
+  const ScanPlace at = scan_place(s);
+  const int wave = threadIdx.x >> 6;
+  typedef typename ScanRaw<E>::type Raw;
+  float state[kScanV];
+  scan_start<false>(s, at, state);
+  int turn = 0;
+  for (int64_t t0 = at.lo; t0 < at.hi; turn ^= 1) {
+    const ScanSpan sp = scan_span(s, t0);
+    const ScanWorker& w = scan_worker(s, sp.p);
+    const int64_t t1 = min(min(at.hi, sp.hi), t0 + kScanWaves * L), mine0 = t0 + wave * L;
+    const int cnt = (int)max((int64_t)0, min((int64_t)L, t1 - mine0)), live = (int)max((int64_t)0, min((int64_t)cnt, at.len - mine0));
+    const int64_t row = ((int64_t)at.b * (sp.hi - sp.lo) + (mine0 - sp.lo)) * s.n_c + at.c;
+    Raw ra[L], rx[L];
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (i < live) {
+        ra[i] = scan_load((const E*)w.a + row + i * s.n_c, at.n);
+        rx[i] = scan_load((const E*)w.x + row + i * s.n_c, at.n);
+      }
+    float a[L][kScanV], u[L][kScanV], A[kScanV], B[kScanV];
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) {
+      A[v] = 1.f;
+      B[v] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (i < live) {
+        float g[kScanV], x[kScanV];
+        scan_values(ra[i], g);
+        scan_values(rx[i], x);
+#pragma unroll
+        for (int v = 0; v < kScanV; ++v) {
+          float rest;
+          scan_gate<GATE>(g[v], a[i][v], rest);
+          u[i][v] = rest * x[v];
+          A[v] *= a[i][v];
+          B[v] = fmaf(a[i][v], B[v], u[i][v]);
+        }
+      }
+    float h[kScanV];
+    scan_meet(lds[turn], A, B, state, h);
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (i < cnt) {
+        float out[kScanV];
+#pragma unroll
+        for (int v = 0; v < kScanV; ++v) {
+          if (i < live) h[v] = fmaf(a[i][v], h[v], u[i][v]);
+          out[v] = i < live ? h[v] : 0.f;
+        }
+        scan_store((E*)w.o0 + row + i * s.n_c, out, at.n);
+      }
+    t0 = t1;
+  }
+  if (s.hT && at.hi == s.T && wave == 0) {
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v)
+      if (v < at.n) s.hT[at.b * s.n_c + at.c + v] = state[v];
+  }
+}
+
+// Backwards in time: wave 0 has a tile's last steps, and step i of a wave is the i-th from its end.
+template <class E, int GATE>
+__global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
+  constexpr int L = 8;
+  __shared__ float lds[2][kScanWaves][2][kScanCols];
+  const ScanPlace at = scan_place(s);
+  const int wave = threadIdx.x >> 6;
+  typedef typename ScanRaw<E>::type Raw;
+  float state[kScanV];
+  scan_start<true>(s, at, state);
+  int turn = 0;
+  for (int64_t t1 = at.hi; t1 > at.lo; turn ^= 1) {
+    const ScanSpan sp = scan_span(s, t1 - 1);
+    const ScanWorker& w = scan_worker(s, sp.p);
+    const int64_t t0 = max(max(at.lo, sp.lo), t1 - kScanWaves * L), last = t1 - 1 - wave * L;  // step i: last - i
+    const int cnt = (int)max((int64_t)0, min((int64_t)L, last + 1 - t0));
+    const int skip = (int)max((int64_t)0, min((int64_t)cnt, last + 1 - at.len));  // steps behind the sequence's end come first
+    const int64_t row = ((int64_t)at.b * (sp.hi - sp.lo) + (last - sp.lo)) * s.n_c + at.c;
+    Raw ra[L], rx[L], rd[L], rh[L];
+    float first[kScanV];  // the state in front of step 0, in 32 bits
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (i >= skip && i < cnt) {
+        const int64_t o = row - i * s.n_c;
+        ra[i] = scan_load((const E*)w.a + o, at.n);
+        rd[i] = scan_load((const E*)w.dh + o, at.n);
+        if (GATE != DISTDL_GATE_GIVEN) rx[i] = scan_load((const E*)w.x + o, at.n);
+        const int64_t t = last - i;
+        if (t > sp.lo) {
+          rh[i] = scan_load((const E*)w.h + o - s.n_c, at.n);
+        } else if (t > 0) {  // the last state of the worker before
+          const ScanSpan b = scan_span(s, t - 1);
+          rh[i] = scan_load((const E*)scan_worker(s, b.p).h + ((int64_t)at.b * (b.hi - b.lo) + (b.hi - b.lo - 1)) * s.n_c + at.c, at.n);
+        } else {
+#pragma unroll
+          for (int v = 0; v < kScanV; ++v) first[v] = s.h0 && v < at.n ? s.h0[at.b * s.n_c + at.c + v] : 0.f;
+        }
+      }
+    float a[L][kScanV], rest[L][kScanV], A[kScanV], B[kScanV];
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) {
+      A[v] = 1.f;
+      B[v] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (i >= skip && i < cnt) {
+        float g[kScanV], d[kScanV];
+        scan_values(ra[i], g);
+        scan_values(rd[i], d);
+#pragma unroll
+        for (int v = 0; v < kScanV; ++v) {
+          scan_gate<GATE>(g[v], a[i][v], rest[i][v]);
+          A[v] *= a[i][v];
+          B[v] = a[i][v] * (B[v] + d[v]);
+        }
+      }
+    float back[kScanV];
+    scan_meet(lds[turn], A, B, state, back);
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (i < cnt) {
+        float da[kScanV] = {}, dx[kScanV] = {};
+        if (i >= skip) {
+          float d[kScanV], x[kScanV] = {}, before[kScanV];
+          scan_values(rd[i], d);
+          if (GATE != DISTDL_GATE_GIVEN) scan_values(rx[i], x);
+          if (last - i > 0) scan_values(rh[i], before);
+#pragma unroll
+          for (int v = 0; v < kScanV; ++v) {
+            if (last - i == 0) before[v] = first[v];
+            d[v] += back[v];
+            back[v] = a[i][v] * d[v];
+            da[v] = GATE == DISTDL_GATE_GIVEN ? d[v] * before[v] : d[v] * (before[v] - x[v]) * (a[i][v] * rest[i][v]);
+            dx[v] = d[v] * rest[i][v];
+          }
+        }
+        const int64_t o = row - i * s.n_c;
+        scan_store((E*)w.o0 + o, da, at.n);
+        scan_store((E*)w.o1 + o, dx, at.n);
+      }
+    t1 = t0;
+  }
+  if (s.hT && at.lo == 0 && wave == 0) {
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v)
+      if (v < at.n) s.hT[at.b * s.n_c + at.c + v] = state[v];
+  }
+}
+
+// One token of each row: its state lies at row slots[row] of the pool.  A row without a slot of the pool is idle.
+template <class E, int GATE>
+__global__ __launch_bounds__(256) void scan_step_kernel(const E* __restrict__ a, const E* __restrict__ x, float* __restrict__ state,
+                                                        const int32_t* __restrict__ slots, E* __restrict__ h, int64_t n_slots,
+                                                        int64_t n_c) {
+  const int64_t row = blockIdx.y, c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * kScanV;
+  if (c >= n_c) return;
+  const int n = (int)min((int64_t)kScanV, n_c - c);
+  const int64_t slot = slots ? slots[row] : row, o = row * n_c + c;
+  float out[kScanV] = {};
+  if (slot >= 0 && slot < n_slots) {
+    float g[kScanV], u[kScanV], old[kScanV];
+    float* const at = state + slot * n_c + c;
+    scan_values(scan_load(a + o, n), g);
+    scan_values(scan_load(x + o, n), u);
+    scan_values(scan_load(at, n), old);
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) {
+      float f, rest;
+      scan_gate<GATE>(g[v], f, rest);
+      out[v] = fmaf(f, old[v], rest * u[v]);
+    }
+    scan_store(at, out, n);
+  }
+  scan_store(h + o, out, n);
+}
+
+}  // namespace distdl
+
+struct distdl_scan_plan {
+  int64_t n_b = 0, T = 0, n_c = 0;
+  int P = 1, gate = 0;
+  distdl_dtype dtype = DISTDL_F32;
+  int groups = 1, segments = 1;
+  int64_t seg_steps = 0;
+  distdl::DevArray<distdl::ScanWorker> table;
+  distdl::StreamScratch maps;
+};
+
+namespace distdl {
+
+static int scan_check(const void* v, size_t size, const char* what, int j) {
+  if (!v) return set_error(DISTDL_ERR_NULL, "scan: %s[%d] is null", what, j);
+  if ((uintptr_t)v % size) return set_error(DISTDL_ERR_INVALID_ARG, "scan: %s[%d] is not aligned to its elements", what, j);
+  return DISTDL_OK;
+}
+
+static int scan_args(distdl_scan_plan* p, const std::vector<ScanWorker>& w, hipStream_t st, ScanArgs* s) {
+  s->more = nullptr;
+  s->T = p->T;
+  s->n_c = p->n_c;
+  s->part = p->T / p->P;
+  s->extra = p->T % p->P;
+  s->P = p->P;
+  s->n_b = (int32_t)p->n_b;
+  s->groups = p->groups;
+  s->segments = p->segments;
+  s->seg_steps = p->seg_steps;
+  int rc = DISTDL_OK;
+  if (p->P <= kScanInline) {
+    std::copy(w.begin(), w.end(), s->w);
+  } else {
+    if ((rc = p->table.upload(w, st))) return rc;
+    s->more = p->table.dev;
+  }
+  s->maps = nullptr;
+  if (p->segments > 1) rc = p->maps.get((size_t)p->n_b * p->segments * 2 * p->n_c, st, &s->maps);
+  return rc;
+}
+
+template <class E, int GATE>
+static void launch_scan(const ScanArgs& s, bool back, hipStream_t st) {
+  const dim3 grid((unsigned)((int64_t)s.groups * s.n_b * s.segments)), block(64 * kScanWaves);
+  if (s.segments > 1) {
+    if (back) hipLaunchKernelGGL((scan_map_kernel<E, GATE, true>), grid, block, 0, st, s);
+    else hipLaunchKernelGGL((scan_map_kernel<E, GATE, false>), grid, block, 0, st, s);
+  }
+  if (back) hipLaunchKernelGGL((scan_bwd_kernel<E, GATE>), grid, block, 0, st, s);
+  else hipLaunchKernelGGL((scan_fwd_kernel<E, GATE>), grid, block, 0, st, s);
+}
+
+template <class F>
+static void scan_kind(distdl_dtype dtype, int gate, F f) {
+  typedef std::integral_constant<int, DISTDL_GATE_GIVEN> Given;
+  typedef std::integral_constant<int, DISTDL_GATE_SIGMOID> Sigmoid;
+  if (dtype == DISTDL_F32) {
+    if (gate == DISTDL_GATE_GIVEN) f(float(), Given());
+    else f(float(), Sigmoid());
+  } else {
+    if (gate == DISTDL_GATE_GIVEN) f(uint16_t(), Given());
+    else f(uint16_t(), Sigmoid());
+  }
+}
+
+}  // namespace distdl
+
+using namespace distdl;
+
+extern "C" {
+
+int distdl_scan_plan_create(distdl_scan_plan** out, int64_t n_b, int64_t T, int64_t n_c, int P, distdl_gate gate, distdl_dtype dtype) {
+  if (!out) return set_error(DISTDL_ERR_NULL, "scan_plan_create: null argument");
+  *out = nullptr;
+  if (n_b < 1 || T < 1 || n_c < 1 || P < 1) return set_error(DISTDL_ERR_INVALID_ARG, "scan_plan_create: sizes must be >= 1");
+  if (gate != DISTDL_GATE_GIVEN && gate != DISTDL_GATE_SIGMOID) return set_error(DISTDL_ERR_UNSUPPORTED, "unknown gate");
+  if (dtype != DISTDL_F32 && dtype != DISTDL_BF16) return set_error(DISTDL_ERR_UNSUPPORTED, "unknown dtype");
+  if (T < P) return set_error(DISTDL_ERR_EMPTY_PARTITION, "scan: %lld steps over %d workers", (long long)T, P);
+  const int64_t groups = (n_c + kScanCols - 1) / kScanCols;
+  if (T >= int64_t(1) << 31 || n_c >= int64_t(1) << 30 || n_b >= int64_t(1) << 22 || groups * n_b >= int64_t(1) << 22)
+    return set_error(DISTDL_ERR_UNSUPPORTED, "scan: problem too large");
+  return guarded([&]() -> int {
+    std::unique_ptr<distdl_scan_plan> p(new distdl_scan_plan());
+    p->n_b = n_b;
+    p->T = T;
+    p->n_c = n_c;
+    p->P = P;
+    p->gate = gate;
+    p->dtype = dtype;
+    p->groups = (int)groups;
+    // Two workgroups for each of the 256 compute units; a segment has at least four tiles of the forward pass.
+    const int64_t tile = 16 * kScanWaves, want = (512 + groups * n_b - 1) / (groups * n_b);
+    const int64_t most = std::max<int64_t>(1, T / (4 * tile)), segments = std::min(want, most);
+    p->seg_steps = (((T + segments - 1) / segments) + tile - 1) / tile * tile;
+    p->segments = (int)((T + p->seg_steps - 1) / p->seg_steps);
+    *out = p.release();
+    return DISTDL_OK;
+  });
+}
+
+int distdl_scan_plan_destroy(distdl_scan_plan* p) {
+  if (!p) return DISTDL_OK;
+  p->table.release();
+  p->maps.release();
+  delete p;
+  return DISTDL_OK;
+}
+
+int distdl_scan_fwd(distdl_scan_plan* p, const void* const a_dev[], const void* const x_dev[], const float* h0_dev,
+                    const int32_t* lengths_dev, void* const h_dev[], float* hT_dev, void* stream) {
+  if (!p || !a_dev || !x_dev || !h_dev) return set_error(DISTDL_ERR_NULL, "scan_fwd: null argument");
+  if ((uintptr_t)h0_dev % 4 || (uintptr_t)lengths_dev % 4 || (uintptr_t)hT_dev % 4)
+    return set_error(DISTDL_ERR_INVALID_ARG, "scan_fwd: h0, lengths or hT is not aligned to its elements");
+  return guarded([&]() -> int {
+    const size_t size = dtype_size(p->dtype);
+    std::vector<ScanWorker> w((size_t)p->P);
+    int rc;
+    for (int j = 0; j < p->P; ++j) {
+      if ((rc = scan_check(a_dev[j], size, "a", j)) || (rc = scan_check(x_dev[j], size, "x", j)) || (rc = scan_check(h_dev[j], size, "h", j)))
+        return rc;
+      w[j] = ScanWorker{a_dev[j], x_dev[j], nullptr, nullptr, h_dev[j], nullptr};
+    }
+    hipStream_t st_ = (hipStream_t)stream;
+    ScanArgs s;
+    if ((rc = scan_args(p, w, st_, &s))) return rc;
+    s.lengths = lengths_dev;
+    s.h0 = h0_dev;
+    s.end = nullptr;
+    s.hT = hT_dev;
+    {
+      ProfScope prof("scan_fwd", st_);
+      scan_kind(p->dtype, p->gate, [&](auto e, auto gate) { launch_scan<decltype(e), decltype(gate)::value>(s, false, st_); });
+    }
+    DISTDL_HIP_TRY(hipGetLastError());
+    return DISTDL_OK;
+  });
+}
+
+int distdl_scan_bwd(distdl_scan_plan* p, const void* const a_dev[], const void* const x_dev[], const void* const h_dev[],
+                    const float* h0_dev, const int32_t* lengths_dev, const void* const dh_dev[], const float* dhT_dev,
+                    void* const da_dev[], void* const dx_dev[], float* dh0_dev, void* stream) {
+  if (!p || !a_dev || !h_dev || !dh_dev || !da_dev || !dx_dev) return set_error(DISTDL_ERR_NULL, "scan_bwd: null argument");
+  if (!x_dev && p->gate != DISTDL_GATE_GIVEN) return set_error(DISTDL_ERR_NULL, "scan_bwd: sigmoid gates need x");
+  if ((uintptr_t)h0_dev % 4 || (uintptr_t)lengths_dev % 4 || (uintptr_t)dhT_dev % 4 || (uintptr_t)dh0_dev % 4)
+    return set_error(DISTDL_ERR_INVALID_ARG, "scan_bwd: h0, lengths, dhT or dh0 is not aligned to its elements");
+  return guarded([&]() -> int {
+    const size_t size = dtype_size(p->dtype);
+    std::vector<ScanWorker> w((size_t)p->P);
+    int rc;
+    for (int j = 0; j < p->P; ++j) {
+      if ((rc = scan_check(a_dev[j], size, "a", j)) || (p->gate != DISTDL_GATE_GIVEN && (rc = scan_check(x_dev[j], size, "x", j))) ||
+          (rc = scan_check(h_dev[j], size, "h", j)) || (rc = scan_check(dh_dev[j], size, "dh", j)) ||
+          (rc = scan_check(da_dev[j], size, "da", j)) || (rc = scan_check(dx_dev[j], size, "dx", j)))
+        return rc;
+      w[j] = ScanWorker{a_dev[j], x_dev ? x_dev[j] : nullptr, h_dev[j], dh_dev[j], da_dev[j], dx_dev[j]};
+    }
+    hipStream_t st_ = (hipStream_t)stream;
+    ScanArgs s;
+    if ((rc = scan_args(p, w, st_, &s))) return rc;
+    s.lengths = lengths_dev;
+    s.h0 = h0_dev;
+    s.end = dhT_dev;
+    s.hT = dh0_dev;
+    {
+      ProfScope prof("scan_bwd", st_);
+      scan_kind(p->dtype, p->gate, [&](auto e, auto gate) { launch_scan<decltype(e), decltype(gate)::value>(s, true, st_); });
+    }
+    DISTDL_HIP_TRY(hipGetLastError());
+    return DISTDL_OK;
+  });
+}
+
+int distdl_scan_step(const void* a_dev, const void* x_dev, float* state_dev, int64_t n_slots, const int32_t* slots_dev, void* h_dev,
+                     int64_t rows, int64_t n_c, distdl_gate gate, distdl_dtype dtype, void* stream) {
+  if (rows < 0 || n_c < 1 || n_slots < 0) return set_error(DISTDL_ERR_INVALID_ARG, "scan_step: %lld rows of %lld channels, %lld slots",
+                                                           (long long)rows, (long long)n_c, (long long)n_slots);
+  if (gate != DISTDL_GATE_GIVEN && gate != DISTDL_GATE_SIGMOID) return set_error(DISTDL_ERR_UNSUPPORTED, "unknown gate");
+  if (dtype != DISTDL_F32 && dtype != DISTDL_BF16) return set_error(DISTDL_ERR_UNSUPPORTED, "unknown dtype");
+  if (rows == 0) return DISTDL_OK;
+  if (!a_dev || !x_dev || !h_dev || (!state_dev && n_slots > 0)) return set_error(DISTDL_ERR_NULL, "scan_step: null argument");
+  if (!slots_dev && n_slots < rows) return set_error(DISTDL_ERR_INVALID_ARG, "scan_step: %lld states for %lld rows", (long long)n_slots, (long long)rows);
+  if (rows > int64_t(65535) * 65535 || n_c >= int64_t(1) << 30) return set_error(DISTDL_ERR_UNSUPPORTED, "scan_step: problem too large");
+  const size_t size = dtype_size(dtype);
+  if ((uintptr_t)a_dev % size || (uintptr_t)x_dev % size || (uintptr_t)h_dev % size || (uintptr_t)state_dev % 4 || (uintptr_t)slots_dev % 4)
+    return set_error(DISTDL_ERR_INVALID_ARG, "scan_step: an array is not aligned to its elements");
+  hipStream_t st_ = (hipStream_t)stream;
+  {
+    ProfScope prof("scan_step", st_);
+    const int64_t wide = (n_c + 256 * kScanV - 1) / (256 * kScanV);
+    for (int64_t row0 = 0; row0 < rows; row0 += 65535) {  // (one launch for any batch that a decoder has)
+      const int64_t n = std::min<int64_t>(65535, rows - row0);
+      scan_kind(dtype, gate, [&](auto e, auto g) {
+        typedef decltype(e) E;
+        hipLaunchKernelGGL((scan_step_kernel<E, decltype(g)::value>), dim3((unsigned)wide, (unsigned)n), dim3(256), 0, st_,
+                           (const E*)a_dev + row0 * n_c, (const E*)x_dev + row0 * n_c, state_dev + (slots_dev ? 0 : row0 * n_c),
+                           slots_dev ? slots_dev + row0 : nullptr, (E*)h_dev + row0 * n_c, slots_dev ? n_slots : n_slots - row0, n_c);
+      });
+    }
+  }
+  DISTDL_HIP_TRY(hipGetLastError());
+  return DISTDL_OK;
+}
+
+}  // extern "C"

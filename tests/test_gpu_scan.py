@@ -1,0 +1,247 @@
+"""Gated linear recurrence on the GPU against the fp64 oracle.
+
+Tolerances follow the recurrence itself.  A step rounds its products and sum, and a sigmoid gate is off by a few units of 2^-24
+(exponential, sum, reciprocal: 2 each at most, and |g| of the exponent's argument); what a step adds is carried on by the factors.
+With b_t = f_t b_{t-1} + 16 units (f_t |h_{t-1}| + |u_t|), the order of composition included (each map's factor has one rounding a
+step, which multiplies the state that it carries), every h is within b of the oracle's.  The same for the adjoint's chain; its
+products add 16 units of their terms.  bf16 results (8 bits, numbers 2^-7 apart) have 2^-8 besides."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2006_03108_amd as dd
+from gpu_util import require_gpu
+from oracle import blocks
+
+pytestmark = pytest.mark.gpu
+UNIT = 2.0 ** -24
+KINDS = {"f32": (torch.float32, UNIT), "bf16": (torch.bfloat16, 2.0 ** -8)}
+
+
+def cut(x, P):
+    sizes = [x.shape[1] // P + (r < x.shape[1] % P) for r in range(P)]
+    return [t.contiguous() for t in x.split(sizes, 1)]
+
+
+def wide(ts):
+    return torch.cat([t.float() for t in ts], 1).cpu().double().numpy()
+
+
+def host(t):
+    return t.cpu().double().numpy()
+
+
+def within(got, want, tol, what):
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} off, the first at {np.argwhere(bad)[0]}: {got[bad][0]} for {want[bad][0]}, tol {tol[bad][0]}"
+
+
+def make(n, T, C, P, dtype, sigmoid, ragged, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    t = KINDS[dtype][0]
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    a = 2 + 2 * rnd(n, T, C)
+    a = (a if sigmoid else torch.sigmoid(a)).to(t)
+    lengths = None
+    if ragged:
+        lengths = torch.randint(0, T + 1, (n,), generator=g, device="cuda", dtype=torch.int32)
+        lengths[0] = 0
+        lengths[-1] = T
+    return dict(a=cut(a, P), x=cut(rnd(n, T, C).to(t), P), dh=cut(rnd(n, T, C).to(t), P), h0=rnd(n, C), dhT=rnd(n, C), lengths=lengths)
+
+
+def check(n, T, C, P, dtype, sigmoid, ragged, seed=0):
+    d = make(n, T, C, P, dtype, sigmoid, ragged, seed)
+    kind, half = KINDS[dtype]
+    new = lambda: [torch.full_like(t, 7.0) for t in d["x"]]  # noqa: E731
+    plan = dd.distdl_scan_plan_create(n, T, C, P, "sigmoid" if sigmoid else "given", kind)
+    h, hT = new(), torch.empty(n, C, device="cuda")
+    dd.distdl_scan_fwd(plan, d["a"], d["x"], d["h0"], d["lengths"], h, hT)
+    a, x, h0, dh, dhT = wide(d["a"]), wide(d["x"]), host(d["h0"]), wide(d["dh"]), host(d["dhT"])
+    ends = np.full(n, T) if d["lengths"] is None else d["lengths"].cpu().numpy()
+    wh, wT = blocks.scan_forward(a, x, h0, ends, sigmoid)
+    f, u = blocks.gates(a, x, sigmoid)
+    grown = 16 * UNIT * (np.abs(f) * np.abs(np.concatenate([h0[:, None], wh[:, :-1]], 1)) + np.abs(u))
+    tol, tolT = blocks.scan_forward(np.abs(f), grown, UNIT * np.abs(h0), ends, False)
+    within(wide(h), wh, tol + half * np.abs(wh), "h")
+    within(host(hT), wT, tolT + UNIT * np.abs(wT), "hT")
+    # the adjoint reads the states that the forward pass wrote
+    hw = wide(h)
+    da, dx, dh0 = new(), new(), torch.empty(n, C, device="cuda")
+    dd.distdl_scan_bwd(plan, d["a"], d["x"] if sigmoid else None, h, d["h0"], d["lengths"], d["dh"], d["dhT"], da, dx, dh0)
+    wa, wx, w0 = blocks.scan_adjoint(a, x, hw, h0, ends, dh, dhT, sigmoid)
+    # sizes of the chain's gradients, and its error: d_t = dh_t + b, b = f d
+    _, size, _ = blocks.scan_adjoint(np.abs(f), x, hw, h0, ends, np.abs(dh), np.abs(dhT), False)
+    _, err, err0 = blocks.scan_adjoint(np.abs(f), x, hw, h0, ends, 16 * UNIT * size, 16 * UNIT * np.abs(dhT), False)
+    before = np.abs(np.concatenate([h0[:, None], hw[:, :-1]], 1))
+    slope = before if not sigmoid else (before + np.abs(x)) * f * (1 - f)
+    rest = 1.0 if not sigmoid else 1 - f
+    within(wide(da), wa, (err + 16 * UNIT * size) * slope + half * np.abs(wa), "da")
+    within(wide(dx), wx, (err + 16 * UNIT * size) * rest + half * np.abs(wx), "dx")
+    within(host(dh0), w0, err0 + 16 * UNIT * np.abs(w0) + 1e-30, "dh0")
+
+
+SIZES = [(1, 1, 1, 1), (2, 1, 130, 1), (3, 2, 5, 2), (2, 17, 64, 3), (1, 128, 129, 1), (3, 129, 33, 4), (2, 300, 257, 20), (1, 1100, 128, 1),
+         (1, 2049, 70, 3), (2, 5000, 3, 1), (9, 700, 12, 2)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sigmoid", [False, True], ids=["given", "sigmoid"])
+@pytest.mark.parametrize("n,T,C,P", SIZES)
+def test_forward_and_adjoint(n, T, C, P, dtype, sigmoid):
+    require_gpu()
+    check(n, T, C, P, dtype, sigmoid, ragged=False)
+
+
+@pytest.mark.parametrize("sigmoid", [False, True], ids=["given", "sigmoid"])
+@pytest.mark.parametrize("n,T,C,P", [(5, 1, 9, 1), (4, 40, 65, 3), (6, 300, 20, 2), (3, 3001, 17, 2), (8, 1500, 150, 1)])
+def test_ragged(n, T, C, P, sigmoid):
+    require_gpu()
+    for dtype in ("f32", "bf16"):
+        check(n, T, C, P, dtype, sigmoid, ragged=True, seed=3)
+
+
+def test_many_channels_in_one_segment():
+    require_gpu()
+    check(3, 140, 70000, 1, "bf16", True, ragged=True, seed=5)
+
+
+def test_defaults_and_lengths_outside():
+    """No h0, lengths, dhT: zeros and whole sequences; lengths below zero and beyond T are cut."""
+    require_gpu()
+    n, T, C = 3, 50, 20
+    d = make(n, T, C, 1, "f32", True, False)
+    plan = dd.distdl_scan_plan_create(n, T, C, 1, "sigmoid", torch.float32)
+    new = lambda: [torch.empty_like(t) for t in d["x"]]  # noqa: E731
+    zero, h, g = torch.zeros(n, C, device="cuda"), [new(), new()], [(new(), new()) for _ in range(2)]
+    all_of = torch.full((n,), T + 9, dtype=torch.int32, device="cuda")
+    dd.distdl_scan_fwd(plan, d["a"], d["x"], None, None, h[0], None)
+    dd.distdl_scan_fwd(plan, d["a"], d["x"], zero, all_of, h[1], None)
+    assert torch.equal(h[0][0], h[1][0])
+    dd.distdl_scan_bwd(plan, d["a"], d["x"], h[0], None, None, d["dh"], None, *g[0], None)
+    dd.distdl_scan_bwd(plan, d["a"], d["x"], h[0], zero, all_of, d["dh"], zero, *g[1], None)
+    assert torch.equal(g[0][0][0], g[1][0][0]) and torch.equal(g[0][1][0], g[1][1][0])
+    none = torch.full((n,), -4, dtype=torch.int32, device="cuda")
+    hT = torch.empty(n, C, device="cuda")
+    dd.distdl_scan_fwd(plan, d["a"], d["x"], d["h0"], none, h[1], hT)
+    assert not h[1][0].any() and torch.equal(hT, d["h0"])
+
+
+@pytest.mark.parametrize("T", [40, 2500])
+def test_masked_steps_are_not_read(T):
+    """NaN and infinities behind a sequence's end, and gates of large size within it, leave finite results."""
+    require_gpu()
+    n, C = 3, 40
+    d = make(n, T, C, 2, "f32", True, False)
+    lengths = torch.tensor([T, T // 3, 0], dtype=torch.int32, device="cuda")
+    at = 0
+    for a, x, dh in zip(d["a"], d["x"], d["dh"]):
+        behind = torch.arange(at, at + a.shape[1], device="cuda")[None, :, None] >= lengths[:, None, None]
+        at += a.shape[1]
+        for t, v in ((a, float("nan")), (x, float("inf")), (dh, float("nan"))):
+            t.masked_fill_(behind, v)
+        a[:, 0].clamp_(min=80.0)
+        a[:, 1].clamp_(max=-200.0)
+    plan = dd.distdl_scan_plan_create(n, T, C, 2, "sigmoid", torch.float32)
+    new = lambda: [torch.empty_like(t) for t in d["x"]]  # noqa: E731
+    h, da, dx, hT, dh0 = new(), new(), new(), torch.empty(n, C, device="cuda"), torch.empty(n, C, device="cuda")
+    dd.distdl_scan_fwd(plan, d["a"], d["x"], d["h0"], lengths, h, hT)
+    dd.distdl_scan_bwd(plan, d["a"], d["x"], h, d["h0"], lengths, d["dh"], d["dhT"], da, dx, dh0)
+    for t in h + da + dx + [hT, dh0]:
+        assert torch.isfinite(t).all()
+    assert torch.equal(hT[2], d["h0"][2]) and torch.equal(dh0[2], d["dhT"][2])
+
+
+def test_adjoint_is_the_difference_of_the_forward():
+    """Along a direction, f32, step 2^-6: second differences are of order 2^-12 of the slope, rounding 2^-17."""
+    require_gpu()
+    n, T, C, P = 2, 60, 30, 3
+    d, v = make(n, T, C, P, "f32", True, True), make(n, T, C, P, "f32", True, False, seed=9)
+    plan = dd.distdl_scan_plan_create(n, T, C, P, "sigmoid", torch.float32)
+    new = lambda: [torch.empty_like(t) for t in d["x"]]  # noqa: E731
+    h, hT = new(), torch.empty(n, C, device="cuda")
+    move = lambda k, s: [p + s * q for p, q in zip(d[k], v[k])]  # noqa: E731
+
+    def f(s):
+        dd.distdl_scan_fwd(plan, move("a", s), move("x", s), d["h0"] + s * v["h0"], d["lengths"], h, hT)
+        return (wide(h) * wide(d["dh"])).sum() + (host(hT) * host(d["dhT"])).sum()
+
+    slope = 32 * (f(1 / 64) - f(-1 / 64))
+    f(0.0)
+    da, dx, dh0 = new(), new(), torch.empty(n, C, device="cuda")
+    dd.distdl_scan_bwd(plan, d["a"], d["x"], h, d["h0"], d["lengths"], d["dh"], d["dhT"], da, dx, dh0)
+    parts = [wide(da) * wide(v["a"]), wide(dx) * wide(v["x"]), host(dh0) * host(v["h0"])]
+    assert abs(sum(p.sum() for p in parts) - slope) <= 2e-3 * np.sqrt(sum((p ** 2).sum() for p in parts))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sigmoid", [False, True], ids=["given", "sigmoid"])
+@pytest.mark.parametrize("rows,C", [(1, 1), (3, 7), (5, 600), (2, 4097), (700, 4)])
+def test_step(rows, C, sigmoid, dtype):
+    require_gpu()
+    kind, half = KINDS[dtype]
+    d = make(rows, 1, C, 1, dtype, sigmoid, False, seed=4)
+    a, x = d["a"][0].view(rows, C), d["x"][0].view(rows, C)
+    pool = torch.randn(rows + 3, C, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    slots = torch.randperm(rows + 3, generator=torch.Generator().manual_seed(2))[:rows].int()
+    slots[0] = -1
+    if rows > 2:
+        slots[2] = rows + 3  # behind the pool
+    before, h = pool.clone(), torch.full_like(x, 7.0)
+    dd.distdl_scan_step(a, x, pool, slots.cuda(), h, "sigmoid" if sigmoid else "given")
+    f, u = blocks.gates(host(a.float()), host(x.float()), sigmoid)
+    want = host(before)
+    for i, s in enumerate(slots.tolist()):
+        if 0 <= s < rows + 3:
+            new = f[i] * want[s] + u[i]
+            tol = 16 * UNIT * (np.abs(f[i] * want[s]) + np.abs(u[i]))
+            within(host(pool)[s], new, tol, "state")
+            within(host(h.float())[i], new, tol + half * np.abs(new), "h")
+            want[s] = host(pool)[s]
+        else:
+            assert not h[i].any()
+    assert np.array_equal(host(pool), want), "idle slots stay"
+    # without slots, row i has state i, and steps one after the other are the scan
+    state, T = d["h0"].clone(), 5
+    s = make(rows, T, C, 1, dtype, sigmoid, False, seed=8)
+    plan = dd.distdl_scan_plan_create(rows, T, C, 1, "sigmoid" if sigmoid else "given", kind)
+    hs, hT = torch.empty_like(s["x"][0]), torch.empty(rows, C, device="cuda")
+    dd.distdl_scan_fwd(plan, s["a"], s["x"], d["h0"], None, [hs], hT)
+    for t in range(T):
+        dd.distdl_scan_step(s["a"][0][:, t].contiguous(), s["x"][0][:, t].contiguous(), state, None, h, "sigmoid" if sigmoid else "given")
+        assert (h.float() - hs[:, t].float()).abs().max() <= (2 * half + 64 * UNIT) * hs.float().abs().max() + 1e-6
+    assert (state - hT).abs().max() <= 128 * UNIT * max(1.0, float(hT.abs().max()))
+
+
+def test_in_place_streams_and_graph():
+    require_gpu()
+    n, T, C, P = 2, 1300, 40, 2
+    d = make(n, T, C, P, "bf16", True, True)
+    plan = dd.distdl_scan_plan_create(n, T, C, P, "sigmoid", torch.bfloat16)
+    new = lambda: [torch.empty_like(t) for t in d["x"]]  # noqa: E731
+    h, da, dx = new(), new(), new()
+    dd.distdl_scan_fwd(plan, d["a"], d["x"], d["h0"], d["lengths"], h, None)
+    dd.distdl_scan_bwd(plan, d["a"], d["x"], h, d["h0"], d["lengths"], d["dh"], d["dhT"], da, dx, None)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    place = [t.clone() for t in d["x"]]
+    torch.cuda.synchronize()
+    h2, da2, dx2 = place, [t.clone() for t in d["a"]], [t.clone() for t in d["dh"]]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        dd.distdl_scan_fwd(plan, d["a"], place, d["h0"], d["lengths"], h2, None)
+        dd.distdl_scan_bwd(plan, da2, d["x"], h2, d["h0"], d["lengths"], dx2, d["dhT"], da2, dx2, None)
+    stream.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(h + da + dx, h2 + da2 + dx2))
+    graph = torch.cuda.CUDAGraph()
+    out, oa, ox = new(), new(), new()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        dd.distdl_scan_fwd(plan, d["a"], d["x"], d["h0"], d["lengths"], out, None)
+        dd.distdl_scan_bwd(plan, d["a"], d["x"], out, d["h0"], d["lengths"], d["dh"], d["dhT"], oa, ox, None)
+    for _ in range(4):
+        for t in out + oa + ox:
+            t.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(h + da + dx, out + oa + ox))
