@@ -88,6 +88,17 @@ __device__ __forceinline__ void scan_store(uint16_t* p, const float* v, int n) {
   if (n >= 2) *(u32_any*)p = to_bf16(v[0]) | to_bf16(v[1]) << 16;
   else if (n > 0) *p = (uint16_t)to_bf16(v[0]);
 }
+// Steps of one worker's array as a wave reads and writes them: a uniform pointer to the group's first channel of a step, the lane's
+// channels behind it.  ALL: every lane has both channels.
+template <bool ALL, class E>
+__device__ __forceinline__ auto scan_at(const E* row, int lane, int n) {
+  return scan_load(row + lane * kScanV, ALL ? kScanV : n);
+}
+template <bool ALL, class E>
+__device__ __forceinline__ void scan_put(E* row, int lane, const float* v, int n) {
+  scan_store(row + lane * kScanV, v, ALL ? kScanV : n);
+}
+
 template <class E>
 struct ScanRaw;
 template <>
@@ -112,8 +123,12 @@ __device__ __forceinline__ void scan_gate(float g, float& a, float& rest) {
   }
 }
 
+// (the compiler does not know that it is the same in all lanes, and would make every branch on it one of lanes)
+__device__ __forceinline__ int scan_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
 struct ScanPlace {
-  int group, seg, b, c, n;  // n: channels of this lane
+  int group, seg, b, c, n;  // c: first channel of the group; n: channels of this lane
+  bool all;                 // every lane has both
   int64_t len, lo, hi;      // steps of the sequence; of the segment
 };
 __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& s) {
@@ -123,8 +138,9 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& s) {
   at /= s.groups;
   r.b = at % s.n_b;
   r.seg = at / s.n_b;
-  r.c = r.group * kScanCols + (threadIdx.x & 63) * kScanV;
-  r.n = (int)max((int64_t)0, min((int64_t)kScanV, s.n_c - r.c));
+  r.c = r.group * kScanCols;
+  r.n = (int)max((int64_t)0, min((int64_t)kScanV, s.n_c - r.c - (int)(threadIdx.x & 63) * kScanV));
+  r.all = s.n_c - r.c >= kScanCols;
   r.len = s.lengths ? max((int64_t)0, min(s.T, (int64_t)s.lengths[r.b])) : s.T;
   r.lo = r.seg * s.seg_steps;
   r.hi = min(s.T, r.lo + s.seg_steps);
@@ -133,7 +149,7 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& s) {
 
 // The maps of all waves, each behind the one before it: `mine` is the state in front of this wave's steps, `state` that behind the tile.
 __device__ __forceinline__ void scan_meet(float (*lds)[2][kScanCols], const float* A, const float* B, float* state, float* mine) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int wave = scan_wave(), lane = threadIdx.x & 63;
 #pragma unroll
   for (int v = 0; v < kScanV; ++v) {
     lds[wave][0][v * 64 + lane] = A[v];
@@ -154,11 +170,12 @@ __device__ __forceinline__ void scan_meet(float (*lds)[2][kScanCols], const floa
 template <bool BACK>
 __device__ __forceinline__ void scan_start(const ScanArgs& s, const ScanPlace& at, float* state) {
   const float* from = BACK ? s.end : s.h0;
+  const int c = at.c + (threadIdx.x & 63) * kScanV;
 #pragma unroll
-  for (int v = 0; v < kScanV; ++v) state[v] = from && v < at.n ? from[at.b * s.n_c + at.c + v] : 0.f;
+  for (int v = 0; v < kScanV; ++v) state[v] = from && v < at.n ? from[at.b * s.n_c + c + v] : 0.f;
   const int n = BACK ? s.segments - 1 - at.seg : at.seg;
   for (int i = 0; i < n; ++i) {
-    const float* m = s.maps + ((int64_t)at.b * s.segments + (BACK ? s.segments - 1 - i : i)) * 2 * s.n_c + at.c;
+    const float* m = s.maps + ((int64_t)at.b * s.segments + (BACK ? s.segments - 1 - i : i)) * 2 * s.n_c + c;
 #pragma unroll
     for (int v = 0; v < kScanV; ++v)
       if (v < at.n) state[v] = fmaf(m[v], state[v], m[s.n_c + v]);
@@ -171,7 +188,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
   constexpr int L = 16;
   __shared__ float lds[kScanWaves][2][kScanCols];
   const ScanPlace at = scan_place(s);
-  const int wave = BACK ? kScanWaves - 1 - (threadIdx.x >> 6) : threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = BACK ? kScanWaves - 1 - scan_wave() : scan_wave();
   const int64_t hi = min(at.hi, at.len), each = (max((int64_t)0, hi - at.lo) + kScanWaves - 1) / kScanWaves;
   const int64_t from = min(hi, at.lo + wave * each), to = min(hi, from + each);
   typedef typename ScanRaw<E>::type Raw;
@@ -187,41 +204,51 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
     const ScanSpan sp = scan_span(s, t);
     const int cnt = (int)min((int64_t)L, BACK ? t + 1 - max(from, sp.lo) : min(to, sp.hi) - t);
     const ScanWorker& w = scan_worker(s, sp.p);
-    const int64_t row = (int64_t)at.b * (sp.hi - sp.lo) + (t - sp.lo);
+    const int64_t row = ((int64_t)at.b * (sp.hi - sp.lo) + (t - sp.lo)) * s.n_c + at.c, hop = BACK ? -s.n_c : s.n_c;
+    const E *pa = (const E*)w.a + row, *px = (const E*)(BACK ? w.dh : w.x) + row;
     Raw ra[L], rx[L];
+    auto compose = [&](int i) {
+      float g[kScanV], x[kScanV];
+      scan_values(ra[i], g);
+      scan_values(rx[i], x);
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-      if (i < cnt) {
-        const int64_t o = (row + (BACK ? -i : i)) * s.n_c + at.c;
-        ra[i] = scan_load((const E*)w.a + o, at.n);
-        rx[i] = scan_load((const E*)(BACK ? w.dh : w.x) + o, at.n);
+      for (int v = 0; v < kScanV; ++v) {
+        float a, rest;
+        scan_gate<GATE>(g[v], a, rest);
+        A[v] *= a;
+        B[v] = BACK ? a * (B[v] + x[v]) : fmaf(a, B[v], rest * x[v]);
+      }
+    };
+    if (cnt == L && at.all) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        ra[i] = scan_at<true>(pa + i * hop, lane, 0);
+        rx[i] = scan_at<true>(px + i * hop, lane, 0);
       }
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-      if (i < cnt) {
-        float g[kScanV], x[kScanV];
-        scan_values(ra[i], g);
-        scan_values(rx[i], x);
+      for (int i = 0; i < L; ++i) compose(i);
+    } else {
 #pragma unroll
-        for (int v = 0; v < kScanV; ++v) {
-          float a, rest;
-          scan_gate<GATE>(g[v], a, rest);
-          A[v] *= a;
-          B[v] = BACK ? a * (B[v] + x[v]) : fmaf(a, B[v], rest * x[v]);
+      for (int i = 0; i < L; ++i)
+        if (i < cnt) {
+          ra[i] = scan_at<false>(pa + i * hop, lane, at.n);
+          rx[i] = scan_at<false>(px + i * hop, lane, at.n);
         }
-      }
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (i < cnt) compose(i);
+    }
     done += cnt;
   }
   float state[kScanV] = {}, mine[kScanV], all[kScanV];
   scan_meet(lds, A, B, state, mine);  // B of the whole: the map of zero
-  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int v = 0; v < kScanV; ++v) {
     all[v] = 1.f;
     for (int w = 0; w < kScanWaves; ++w) all[v] *= lds[w][0][v * 64 + lane];
   }
-  if (threadIdx.x < 64) {
-    float* m = s.maps + ((int64_t)at.b * s.segments + at.seg) * 2 * s.n_c + at.c;
+  if (scan_wave() == 0) {
+    float* m = s.maps + ((int64_t)at.b * s.segments + at.seg) * 2 * s.n_c + at.c + lane * kScanV;
 #pragma unroll
     for (int v = 0; v < kScanV; ++v)
       if (v < at.n) {
@@ -231,12 +258,21 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
   }
 }
 
+// hT, or dh0 of the adjoint
+__device__ __forceinline__ void scan_finish(const ScanArgs& s, const ScanPlace& at, const float* state) {
+  if (!s.hT || scan_wave() != 0) return;
+  float* to = s.hT + at.b * s.n_c + at.c + (threadIdx.x & 63) * kScanV;
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v)
+    if (v < at.n) to[v] = state[v];
+}
+
 template <class E, int GATE>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
   constexpr int L = 16;
   __shared__ float lds[2][kScanWaves][2][kScanCols];
   const ScanPlace at = scan_place(s);
-  const int wave = threadIdx.x >> 6;
+  const int wave = scan_wave(), lane = threadIdx.x & 63;
   typedef typename ScanRaw<E>::type Raw;
   float state[kScanV];
   scan_start<false>(s, at, state);
@@ -247,63 +283,81 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
     const int64_t t1 = min(min(at.hi, sp.hi), t0 + kScanWaves * L), mine0 = t0 + wave * L;
     const int cnt = (int)max((int64_t)0, min((int64_t)L, t1 - mine0)), live = (int)max((int64_t)0, min((int64_t)cnt, at.len - mine0));
     const int64_t row = ((int64_t)at.b * (sp.hi - sp.lo) + (mine0 - sp.lo)) * s.n_c + at.c;
+    const E *pa = (const E*)w.a + row, *px = (const E*)w.x + row;
+    E* const po = (E*)w.o0 + row;
+    const bool full = live == L && at.all;
     Raw ra[L], rx[L];
-#pragma unroll
-    for (int i = 0; i < L; ++i)
-      if (i < live) {
-        ra[i] = scan_load((const E*)w.a + row + i * s.n_c, at.n);
-        rx[i] = scan_load((const E*)w.x + row + i * s.n_c, at.n);
-      }
-    float a[L][kScanV], u[L][kScanV], A[kScanV], B[kScanV];
+    float a[L][kScanV], u[L][kScanV], A[kScanV], B[kScanV], h[kScanV];
 #pragma unroll
     for (int v = 0; v < kScanV; ++v) {
       A[v] = 1.f;
       B[v] = 0.f;
     }
+    auto compose = [&](int i) {
+      float g[kScanV], x[kScanV];
+      scan_values(ra[i], g);
+      scan_values(rx[i], x);
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-      if (i < live) {
-        float g[kScanV], x[kScanV];
-        scan_values(ra[i], g);
-        scan_values(rx[i], x);
-#pragma unroll
-        for (int v = 0; v < kScanV; ++v) {
-          float rest;
-          scan_gate<GATE>(g[v], a[i][v], rest);
-          u[i][v] = rest * x[v];
-          A[v] *= a[i][v];
-          B[v] = fmaf(a[i][v], B[v], u[i][v]);
-        }
+      for (int v = 0; v < kScanV; ++v) {
+        float rest;
+        scan_gate<GATE>(g[v], a[i][v], rest);
+        u[i][v] = rest * x[v];
+        A[v] *= a[i][v];
+        B[v] = fmaf(a[i][v], B[v], u[i][v]);
       }
-    float h[kScanV];
+    };
+    if (full) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        ra[i] = scan_at<true>(pa + i * s.n_c, lane, 0);
+        rx[i] = scan_at<true>(px + i * s.n_c, lane, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < L; ++i) compose(i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (i < live) {
+          ra[i] = scan_at<false>(pa + i * s.n_c, lane, at.n);
+          rx[i] = scan_at<false>(px + i * s.n_c, lane, at.n);
+        }
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (i < live) compose(i);
+    }
     scan_meet(lds[turn], A, B, state, h);
+    if (full) {
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-      if (i < cnt) {
-        float out[kScanV];
+      for (int i = 0; i < L; ++i) {
 #pragma unroll
-        for (int v = 0; v < kScanV; ++v) {
-          if (i < live) h[v] = fmaf(a[i][v], h[v], u[i][v]);
-          out[v] = i < live ? h[v] : 0.f;
-        }
-        scan_store((E*)w.o0 + row + i * s.n_c, out, at.n);
+        for (int v = 0; v < kScanV; ++v) h[v] = fmaf(a[i][v], h[v], u[i][v]);
+        scan_put<true>(po + i * s.n_c, lane, h, 0);
       }
+    } else {
+      const float none[kScanV] = {};
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (i < live) {
+#pragma unroll
+          for (int v = 0; v < kScanV; ++v) h[v] = fmaf(a[i][v], h[v], u[i][v]);
+          scan_put<false>(po + i * s.n_c, lane, h, at.n);
+        } else if (i < cnt) {
+          scan_put<false>(po + i * s.n_c, lane, none, at.n);
+        }
+    }
     t0 = t1;
   }
-  if (s.hT && at.hi == s.T && wave == 0) {
-#pragma unroll
-    for (int v = 0; v < kScanV; ++v)
-      if (v < at.n) s.hT[at.b * s.n_c + at.c + v] = state[v];
-  }
+  if (at.hi == s.T) scan_finish(s, at, state);
 }
 
 // Backwards in time: wave 0 has a tile's last steps, and step i of a wave is the i-th from its end.
 template <class E, int GATE>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
   constexpr int L = 8;
+  constexpr bool X = GATE != DISTDL_GATE_GIVEN;
   __shared__ float lds[2][kScanWaves][2][kScanCols];
   const ScanPlace at = scan_place(s);
-  const int wave = threadIdx.x >> 6;
+  const int wave = scan_wave(), lane = threadIdx.x & 63;
   typedef typename ScanRaw<E>::type Raw;
   float state[kScanV];
   scan_start<true>(s, at, state);
@@ -315,76 +369,100 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
     const int cnt = (int)max((int64_t)0, min((int64_t)L, last + 1 - t0));
     const int skip = (int)max((int64_t)0, min((int64_t)cnt, last + 1 - at.len));  // steps behind the sequence's end come first
     const int64_t row = ((int64_t)at.b * (sp.hi - sp.lo) + (last - sp.lo)) * s.n_c + at.c;
+    const E *pa = (const E*)w.a + row, *px = X ? (const E*)w.x + row : nullptr, *ph = (const E*)w.h + row - s.n_c, *pd = (const E*)w.dh + row;
+    E *const o0 = (E*)w.o0 + row, *const o1 = (E*)w.o1 + row;
+    const bool full = cnt == L && skip == 0 && at.all && last - L + 1 > sp.lo;  // and the state before each step is this worker's
     Raw ra[L], rx[L], rd[L], rh[L];
-    float first[kScanV];  // the state in front of step 0, in 32 bits
-#pragma unroll
-    for (int i = 0; i < L; ++i)
-      if (i >= skip && i < cnt) {
-        const int64_t o = row - i * s.n_c;
-        ra[i] = scan_load((const E*)w.a + o, at.n);
-        rd[i] = scan_load((const E*)w.dh + o, at.n);
-        if (GATE != DISTDL_GATE_GIVEN) rx[i] = scan_load((const E*)w.x + o, at.n);
-        const int64_t t = last - i;
-        if (t > sp.lo) {
-          rh[i] = scan_load((const E*)w.h + o - s.n_c, at.n);
-        } else if (t > 0) {  // the last state of the worker before
-          const ScanSpan b = scan_span(s, t - 1);
-          rh[i] = scan_load((const E*)scan_worker(s, b.p).h + ((int64_t)at.b * (b.hi - b.lo) + (b.hi - b.lo - 1)) * s.n_c + at.c, at.n);
-        } else {
-#pragma unroll
-          for (int v = 0; v < kScanV; ++v) first[v] = s.h0 && v < at.n ? s.h0[at.b * s.n_c + at.c + v] : 0.f;
-        }
-      }
-    float a[L][kScanV], rest[L][kScanV], A[kScanV], B[kScanV];
+    float first[kScanV] = {};  // the state in front of step 0, in 32 bits
+    float a[L][kScanV], rest[L][kScanV], A[kScanV], B[kScanV], back[kScanV];
 #pragma unroll
     for (int v = 0; v < kScanV; ++v) {
       A[v] = 1.f;
       B[v] = 0.f;
     }
+    auto compose = [&](int i) {
+      float g[kScanV], d[kScanV];
+      scan_values(ra[i], g);
+      scan_values(rd[i], d);
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-      if (i >= skip && i < cnt) {
-        float g[kScanV], d[kScanV];
-        scan_values(ra[i], g);
-        scan_values(rd[i], d);
-#pragma unroll
-        for (int v = 0; v < kScanV; ++v) {
-          scan_gate<GATE>(g[v], a[i][v], rest[i][v]);
-          A[v] *= a[i][v];
-          B[v] = a[i][v] * (B[v] + d[v]);
-        }
+      for (int v = 0; v < kScanV; ++v) {
+        scan_gate<GATE>(g[v], a[i][v], rest[i][v]);
+        A[v] *= a[i][v];
+        B[v] = a[i][v] * (B[v] + d[v]);
       }
-    float back[kScanV];
-    scan_meet(lds[turn], A, B, state, back);
+    };
+    auto gradient = [&](int i, bool zero, float* da, float* dx) {
+      float d[kScanV], x[kScanV] = {}, before[kScanV];
+      scan_values(rd[i], d);
+      if (X) scan_values(rx[i], x);
+      scan_values(rh[i], before);
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-      if (i < cnt) {
-        float da[kScanV] = {}, dx[kScanV] = {};
-        if (i >= skip) {
-          float d[kScanV], x[kScanV] = {}, before[kScanV];
-          scan_values(rd[i], d);
-          if (GATE != DISTDL_GATE_GIVEN) scan_values(rx[i], x);
-          if (last - i > 0) scan_values(rh[i], before);
+      for (int v = 0; v < kScanV; ++v) {
+        if (zero) before[v] = first[v];
+        d[v] += back[v];
+        back[v] = a[i][v] * d[v];
+        da[v] = X ? d[v] * (before[v] - x[v]) * (a[i][v] * rest[i][v]) : d[v] * before[v];
+        dx[v] = d[v] * rest[i][v];
+      }
+    };
+    if (full) {
 #pragma unroll
-          for (int v = 0; v < kScanV; ++v) {
-            if (last - i == 0) before[v] = first[v];
-            d[v] += back[v];
-            back[v] = a[i][v] * d[v];
-            da[v] = GATE == DISTDL_GATE_GIVEN ? d[v] * before[v] : d[v] * (before[v] - x[v]) * (a[i][v] * rest[i][v]);
-            dx[v] = d[v] * rest[i][v];
+      for (int i = 0; i < L; ++i) {
+        ra[i] = scan_at<true>(pa - i * s.n_c, lane, 0);
+        rd[i] = scan_at<true>(pd - i * s.n_c, lane, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        rh[i] = scan_at<true>(ph - i * s.n_c, lane, 0);
+        if (X) rx[i] = scan_at<true>(px - i * s.n_c, lane, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < L; ++i) compose(i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (i >= skip && i < cnt) {
+          ra[i] = scan_at<false>(pa - i * s.n_c, lane, at.n);
+          rd[i] = scan_at<false>(pd - i * s.n_c, lane, at.n);
+          if (X) rx[i] = scan_at<false>(px - i * s.n_c, lane, at.n);
+          const int64_t t = last - i;
+          if (t > sp.lo) {
+            rh[i] = scan_at<false>(ph - i * s.n_c, lane, at.n);
+          } else if (t > 0) {  // the last state of the worker before
+            const ScanSpan b = scan_span(s, t - 1);
+            rh[i] = scan_at<false>((const E*)scan_worker(s, b.p).h + ((int64_t)at.b * (b.hi - b.lo) + (b.hi - b.lo - 1)) * s.n_c + at.c, lane, at.n);
+          } else {
+            rh[i] = Raw{};
+#pragma unroll
+            for (int v = 0; v < kScanV; ++v) first[v] = s.h0 && v < at.n ? s.h0[at.b * s.n_c + at.c + lane * kScanV + v] : 0.f;
           }
         }
-        const int64_t o = row - i * s.n_c;
-        scan_store((E*)w.o0 + o, da, at.n);
-        scan_store((E*)w.o1 + o, dx, at.n);
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (i >= skip && i < cnt) compose(i);
+    }
+    scan_meet(lds[turn], A, B, state, back);
+    if (full) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        float da[kScanV], dx[kScanV];
+        gradient(i, false, da, dx);
+        scan_put<true>(o0 - i * s.n_c, lane, da, 0);
+        scan_put<true>(o1 - i * s.n_c, lane, dx, 0);
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (i < cnt) {
+          float da[kScanV] = {}, dx[kScanV] = {};
+          if (i >= skip) gradient(i, last - i == 0, da, dx);
+          scan_put<false>(o0 - i * s.n_c, lane, da, at.n);
+          scan_put<false>(o1 - i * s.n_c, lane, dx, at.n);
+        }
+    }
     t1 = t0;
   }
-  if (s.hT && at.lo == 0 && wave == 0) {
-#pragma unroll
-    for (int v = 0; v < kScanV; ++v)
-      if (v < at.n) s.hT[at.b * s.n_c + at.c + v] = state[v];
-  }
+  if (at.lo == 0) scan_finish(s, at, state);
 }
 
 // One token of each row: its state lies at row slots[row] of the pool.  A row without a slot of the pool is idle.
