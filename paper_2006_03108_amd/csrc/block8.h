@@ -52,11 +52,13 @@ typedef u32x2 u32x2_any __attribute__((aligned(1)));
 
 __device__ __forceinline__ float bf16_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
-__device__ __forceinline__ uint32_t to_bf16(float v) {  // nearest even, NaNs stay NaN
-  uint32_t u = __float_as_uint(v);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return (u >> 16) | 0x40u;
-  return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
+// Nearest even, NaNs stay NaN: one instruction for two
+__device__ __forceinline__ uint32_t to_bf16(float lo, float hi) {
+  typedef __bf16 pair_bf16 __attribute__((ext_vector_type(2)));
+  typedef float pair_f32 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(pair_f32{lo, hi}, pair_bf16));
 }
+__device__ __forceinline__ uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
 
 // The raw bits of eight elements: those below `n` of them, zeros for the rest.
 template <class T>
@@ -125,12 +127,12 @@ __device__ __forceinline__ void store8(uint16_t* p, const float* v, int n) {
   if (n >= 8) {
     u32x4 a;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = to_bf16(v[2 * i]) | to_bf16(v[2 * i + 1]) << 16;
+    for (int i = 0; i < 4; ++i) a[i] = to_bf16(v[2 * i], v[2 * i + 1]);
     *(u32x4_any*)p = a;
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = (uint16_t)to_bf16(v[i]);
+      if (i < n) p[i] = to_bf16(v[i]);
   }
 }
 // Eight codes
@@ -150,6 +152,13 @@ __device__ __forceinline__ u32x2 load8_codes(const uint8_t* p, int n) {
   for (int i = 0; i < 8; ++i)
     if (i < n) c[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
   return c;
+}
+
+// Workgroups go to the eight XCDs in turn; this numbers them so that neighbours meet in one XCD, and so in one L2: the lines that two of
+// them share (rows that are no multiple of 128 bytes) are put together there instead of being written in parts.
+__device__ __forceinline__ uint32_t xcd_order(uint32_t block, uint32_t blocks) {
+  const uint32_t x = block & 7, each = blocks >> 3, left = blocks & 7;
+  return x * each + min(x, left) + (block >> 3);
 }
 
 // ---- reductions over lanes ------------------------------------------------

@@ -62,53 +62,68 @@ __device__ __forceinline__ ScanSpan scan_span(const ScanArgs& s, int64_t t) {
   return r;
 }
 
-// Two channels of one step: n of them exist.
-__device__ __forceinline__ u32x2 scan_load(const float* p, int n) {
-  if (n >= 2) return *(const u32x2_any*)p;
-  return u32x2{n > 0 ? __float_as_uint(*p) : 0u, 0u};
-}
-typedef uint32_t u32_any __attribute__((aligned(1)));
-__device__ __forceinline__ uint32_t scan_load(const uint16_t* p, int n) {
-  if (n >= 2) return *(const u32_any*)p;
-  return n > 0 ? (uint32_t)*p : 0u;
-}
-__device__ __forceinline__ void scan_values(u32x2 r, float* v) {
-  v[0] = __uint_as_float(r[0]);
-  v[1] = __uint_as_float(r[1]);
-}
-__device__ __forceinline__ void scan_values(uint32_t r, float* v) {
-  v[0] = bf16_lo(r);
-  v[1] = bf16_hi(r);
-}
-__device__ __forceinline__ void scan_store(float* p, const float* v, int n) {
-  if (n >= 2) *(u32x2_any*)p = u32x2{__float_as_uint(v[0]), __float_as_uint(v[1])};
-  else if (n > 0) *p = v[0];
-}
-__device__ __forceinline__ void scan_store(uint16_t* p, const float* v, int n) {
-  if (n >= 2) *(u32_any*)p = to_bf16(v[0]) | to_bf16(v[1]) << 16;
-  else if (n > 0) *p = (uint16_t)to_bf16(v[0]);
-}
-// Steps of one worker's array as a wave reads and writes them: a uniform pointer to the group's first channel of a step, the lane's
-// channels behind it.  ALL: every lane has both channels.
-template <bool ALL, class E>
-__device__ __forceinline__ auto scan_at(const E* row, int lane, int n) {
-  return scan_load(row + lane * kScanV, ALL ? kScanV : n);
-}
-template <bool ALL, class E>
-__device__ __forceinline__ void scan_put(E* row, int lane, const float* v, int n) {
-  scan_store(row + lane * kScanV, v, ALL ? kScanV : n);
-}
-
-template <class E>
-struct ScanRaw;
-template <>
-struct ScanRaw<float> {
-  typedef u32x2 type;
+// The two channels of a lane in one step: neighbours in one access of twice the size (PAIR), where every row starts at a multiple of that, and
+// otherwise 64 apart in two, each at its natural alignment.  Measured, 7 x 2049 steps of fp32, adjoint: 1024 channels in pairs 92 us;
+// 1001 and 1002 channels in pairs that straddle 203 and 163 us.  n: how many of the two exist.
+template <class E, bool PAIR>
+struct ScanRaw {
+  u32x2 v;
+  __device__ __forceinline__ void load(const E* row, int lane, int n) {
+    v[0] = n > 0 ? bits(row[lane]) : 0u;
+    v[1] = n > 1 ? bits(row[lane + 64]) : 0u;
+  }
+  __device__ __forceinline__ void values(float* f) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) f[i] = __uint_as_float(sizeof(E) == 4 ? v[i] : v[i] << 16);
+  }
+  static __device__ __forceinline__ uint32_t bits(float x) { return __float_as_uint(x); }
+  static __device__ __forceinline__ uint32_t bits(uint16_t x) { return x; }
 };
 template <>
-struct ScanRaw<uint16_t> {
-  typedef uint32_t type;
+struct ScanRaw<float, true> {
+  u32x2 v;
+  __device__ __forceinline__ void load(const float* row, int lane, int n) {
+    if (n > 1) v = *(const u32x2*)(row + lane * 2);
+    else v = u32x2{n > 0 ? __float_as_uint(row[lane * 2]) : 0u, 0u};
+  }
+  __device__ __forceinline__ void values(float* f) const {
+    f[0] = __uint_as_float(v[0]);
+    f[1] = __uint_as_float(v[1]);
+  }
 };
+template <>
+struct ScanRaw<uint16_t, true> {
+  uint32_t v;
+  __device__ __forceinline__ void load(const uint16_t* row, int lane, int n) {
+    if (n > 1) v = *(const uint32_t*)(row + lane * 2);
+    else v = n > 0 ? row[lane * 2] : 0u;
+  }
+  __device__ __forceinline__ void values(float* f) const {
+    f[0] = bf16_lo(v);
+    f[1] = bf16_hi(v);
+  }
+};
+template <bool PAIR>
+__device__ __forceinline__ void scan_put(float* row, int lane, const float* v, int n) {
+  if (PAIR && n > 1) {
+    *(u32x2*)(row + lane * 2) = u32x2{__float_as_uint(v[0]), __float_as_uint(v[1])};
+  } else {
+    if (n > 0) row[PAIR ? lane * 2 : lane] = v[0];
+    if (n > 1) row[lane + 64] = v[1];
+  }
+}
+template <bool PAIR>
+__device__ __forceinline__ void scan_put(uint16_t* row, int lane, const float* v, int n) {
+  if (PAIR && n > 1) {
+    *(uint32_t*)(row + lane * 2) = to_bf16(v[0], v[1]);
+  } else {
+    if (n > 0) row[PAIR ? lane * 2 : lane] = to_bf16(v[0]);
+    if (n > 1) row[lane + 64] = to_bf16(v[1]);
+  }
+}
+// Channel v of a lane, from the group's first
+template <bool PAIR>
+__device__ __forceinline__ int scan_channel(int lane, int v) { return PAIR ? lane * 2 + v : lane + 64 * v; }
 
 // a and 1 - a.  Through exp(-|g|), which neither overflows nor loses 1 - a where a is near one.
 template <int GATE>
@@ -131,16 +146,20 @@ struct ScanPlace {
   bool all;                 // every lane has both
   int64_t len, lo, hi;      // steps of the sequence; of the segment
 };
-__device__ __forceinline__ ScanPlace scan_place(const ScanArgs& s) {
+template <bool PAIR>
+__device__ __forceinline__ ScanPlace scan_place(const ScanArgs& s, bool reversed) {
   ScanPlace r;
-  uint32_t at = blockIdx.x;
+  uint32_t at = xcd_order(blockIdx.x, gridDim.x);
+  if (reversed) at = gridDim.x - 1 - at;
   r.group = at % s.groups;
   at /= s.groups;
   r.b = at % s.n_b;
   r.seg = at / s.n_b;
   r.c = r.group * kScanCols;
-  r.n = (int)max((int64_t)0, min((int64_t)kScanV, s.n_c - r.c - (int)(threadIdx.x & 63) * kScanV));
-  r.all = s.n_c - r.c >= kScanCols;
+  const int64_t left = s.n_c - r.c;
+  const int lane = threadIdx.x & 63;
+  r.n = (scan_channel<PAIR>(lane, 0) < left) + (scan_channel<PAIR>(lane, 1) < left);
+  r.all = left >= kScanCols;
   r.len = s.lengths ? max((int64_t)0, min(s.T, (int64_t)s.lengths[r.b])) : s.T;
   r.lo = r.seg * s.seg_steps;
   r.hi = min(s.T, r.lo + s.seg_steps);
@@ -166,32 +185,57 @@ __device__ __forceinline__ void scan_meet(float (*lds)[2][kScanCols], const floa
   }
 }
 
-// The state in front of a segment: that of the sequence through the maps of the segments before (behind) it.
-template <bool BACK>
-__device__ __forceinline__ void scan_start(const ScanArgs& s, const ScanPlace& at, float* state) {
+// The state in front of a segment: that of the sequence through the maps of the segments before (behind) it.  A wave composes an eighth of
+// them, eight loads at a time, and the eighths meet like the waves' steps.
+template <bool BACK, bool PAIR>
+__device__ __forceinline__ void scan_start(const ScanArgs& s, const ScanPlace& at, float (*lds)[2][kScanCols], float* state) {
   const float* from = BACK ? s.end : s.h0;
-  const int c = at.c + (threadIdx.x & 63) * kScanV;
+  const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int v = 0; v < kScanV; ++v) state[v] = from && v < at.n ? from[at.b * s.n_c + c + v] : 0.f;
+  for (int v = 0; v < kScanV; ++v) state[v] = from && v < at.n ? from[at.b * s.n_c + at.c + scan_channel<PAIR>(lane, v)] : 0.f;
   const int n = BACK ? s.segments - 1 - at.seg : at.seg;
-  for (int i = 0; i < n; ++i) {
-    const float* m = s.maps + ((int64_t)at.b * s.segments + (BACK ? s.segments - 1 - i : i)) * 2 * s.n_c + c;
+  if (n == 0) return;
+  const int each = (n + kScanWaves - 1) / kScanWaves, i0 = min(n, scan_wave() * each), i1 = min(n, i0 + each);
+  const int64_t hop = (BACK ? -2 : 2) * s.n_c;
+  const float* m = s.maps + ((int64_t)at.b * s.segments + (BACK ? s.segments - 1 - i0 : i0)) * 2 * s.n_c + at.c;
+  float A[kScanV], B[kScanV], mine[kScanV];
 #pragma unroll
-    for (int v = 0; v < kScanV; ++v)
-      if (v < at.n) state[v] = fmaf(m[v], state[v], m[s.n_c + v]);
+  for (int v = 0; v < kScanV; ++v) {
+    A[v] = 1.f;
+    B[v] = 0.f;
   }
+  for (int i = i0; i < i1; i += 8) {
+    float f[8][kScanV], u[8][kScanV];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int v = 0; v < kScanV; ++v) {
+        const bool is = i + k < i1 && v < at.n;
+        f[k][v] = is ? m[k * hop + scan_channel<PAIR>(lane, v)] : 1.f;
+        u[k][v] = is ? m[k * hop + s.n_c + scan_channel<PAIR>(lane, v)] : 0.f;
+      }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int v = 0; v < kScanV; ++v) {
+        A[v] *= f[k][v];
+        B[v] = fmaf(f[k][v], B[v], u[k][v]);
+      }
+    m += 8 * hop;
+  }
+  scan_meet(lds, A, B, state, mine);
 }
 
 // A segment's map: a wave composes an eighth of the steps, the eighths meet at the end.
-template <class E, int GATE, bool BACK>
+template <class E, int GATE, bool PAIR, bool BACK>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
   constexpr int L = 16;
   __shared__ float lds[kScanWaves][2][kScanCols];
-  const ScanPlace at = scan_place(s);
+  const ScanPlace at = scan_place<PAIR>(s, BACK);
   const int lane = threadIdx.x & 63, wave = BACK ? kScanWaves - 1 - scan_wave() : scan_wave();
   const int64_t hi = min(at.hi, at.len), each = (max((int64_t)0, hi - at.lo) + kScanWaves - 1) / kScanWaves;
   const int64_t from = min(hi, at.lo + wave * each), to = min(hi, from + each);
-  typedef typename ScanRaw<E>::type Raw;
+  typedef ScanRaw<E, PAIR> Raw;
   float A[kScanV], B[kScanV];
 #pragma unroll
   for (int v = 0; v < kScanV; ++v) {
@@ -209,8 +253,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
     Raw ra[L], rx[L];
     auto compose = [&](int i) {
       float g[kScanV], x[kScanV];
-      scan_values(ra[i], g);
-      scan_values(rx[i], x);
+      ra[i].values(g);
+      rx[i].values(x);
 #pragma unroll
       for (int v = 0; v < kScanV; ++v) {
         float a, rest;
@@ -222,8 +266,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
     if (cnt == L && at.all) {
 #pragma unroll
       for (int i = 0; i < L; ++i) {
-        ra[i] = scan_at<true>(pa + i * hop, lane, 0);
-        rx[i] = scan_at<true>(px + i * hop, lane, 0);
+        ra[i].load(pa + i * hop, lane, kScanV);
+        rx[i].load(px + i * hop, lane, kScanV);
       }
 #pragma unroll
       for (int i = 0; i < L; ++i) compose(i);
@@ -231,8 +275,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
 #pragma unroll
       for (int i = 0; i < L; ++i)
         if (i < cnt) {
-          ra[i] = scan_at<false>(pa + i * hop, lane, at.n);
-          rx[i] = scan_at<false>(px + i * hop, lane, at.n);
+          ra[i].load(pa + i * hop, lane, at.n);
+          rx[i].load(px + i * hop, lane, at.n);
         }
 #pragma unroll
       for (int i = 0; i < L; ++i)
@@ -248,34 +292,31 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
     for (int w = 0; w < kScanWaves; ++w) all[v] *= lds[w][0][v * 64 + lane];
   }
   if (scan_wave() == 0) {
-    float* m = s.maps + ((int64_t)at.b * s.segments + at.seg) * 2 * s.n_c + at.c + lane * kScanV;
-#pragma unroll
-    for (int v = 0; v < kScanV; ++v)
-      if (v < at.n) {
-        m[v] = all[v];
-        m[s.n_c + v] = state[v];
-      }
+    float* m = s.maps + ((int64_t)at.b * s.segments + at.seg) * 2 * s.n_c + at.c;
+    scan_put<PAIR>(m, lane, all, at.n);
+    scan_put<PAIR>(m + s.n_c, lane, state, at.n);
   }
 }
 
 // hT, or dh0 of the adjoint
+template <bool PAIR>
 __device__ __forceinline__ void scan_finish(const ScanArgs& s, const ScanPlace& at, const float* state) {
   if (!s.hT || scan_wave() != 0) return;
-  float* to = s.hT + at.b * s.n_c + at.c + (threadIdx.x & 63) * kScanV;
+  float* to = s.hT + at.b * s.n_c + at.c;
 #pragma unroll
   for (int v = 0; v < kScanV; ++v)
-    if (v < at.n) to[v] = state[v];
+    if (v < at.n) to[scan_channel<PAIR>(threadIdx.x & 63, v)] = state[v];
 }
 
-template <class E, int GATE>
+template <class E, int GATE, bool PAIR>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
   constexpr int L = 16;
   __shared__ float lds[2][kScanWaves][2][kScanCols];
-  const ScanPlace at = scan_place(s);
+  const ScanPlace at = scan_place<PAIR>(s, s.segments > 1);
   const int wave = scan_wave(), lane = threadIdx.x & 63;
-  typedef typename ScanRaw<E>::type Raw;
+  typedef ScanRaw<E, PAIR> Raw;
   float state[kScanV];
-  scan_start<false>(s, at, state);
+  scan_start<false, PAIR>(s, at, lds[1], state);
   int turn = 0;
   for (int64_t t0 = at.lo; t0 < at.hi; turn ^= 1) {
     const ScanSpan sp = scan_span(s, t0);
@@ -295,8 +336,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
     }
     auto compose = [&](int i) {
       float g[kScanV], x[kScanV];
-      scan_values(ra[i], g);
-      scan_values(rx[i], x);
+      ra[i].values(g);
+      rx[i].values(x);
 #pragma unroll
       for (int v = 0; v < kScanV; ++v) {
         float rest;
@@ -309,8 +350,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
     if (full) {
 #pragma unroll
       for (int i = 0; i < L; ++i) {
-        ra[i] = scan_at<true>(pa + i * s.n_c, lane, 0);
-        rx[i] = scan_at<true>(px + i * s.n_c, lane, 0);
+        ra[i].load(pa + i * s.n_c, lane, kScanV);
+        rx[i].load(px + i * s.n_c, lane, kScanV);
       }
 #pragma unroll
       for (int i = 0; i < L; ++i) compose(i);
@@ -318,8 +359,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
 #pragma unroll
       for (int i = 0; i < L; ++i)
         if (i < live) {
-          ra[i] = scan_at<false>(pa + i * s.n_c, lane, at.n);
-          rx[i] = scan_at<false>(px + i * s.n_c, lane, at.n);
+          ra[i].load(pa + i * s.n_c, lane, at.n);
+          rx[i].load(px + i * s.n_c, lane, at.n);
         }
 #pragma unroll
       for (int i = 0; i < L; ++i)
@@ -331,7 +372,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
       for (int i = 0; i < L; ++i) {
 #pragma unroll
         for (int v = 0; v < kScanV; ++v) h[v] = fmaf(a[i][v], h[v], u[i][v]);
-        scan_put<true>(po + i * s.n_c, lane, h, 0);
+        scan_put<PAIR>(po + i * s.n_c, lane, h, kScanV);
       }
     } else {
       const float none[kScanV] = {};
@@ -340,27 +381,27 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
         if (i < live) {
 #pragma unroll
           for (int v = 0; v < kScanV; ++v) h[v] = fmaf(a[i][v], h[v], u[i][v]);
-          scan_put<false>(po + i * s.n_c, lane, h, at.n);
+          scan_put<PAIR>(po + i * s.n_c, lane, h, at.n);
         } else if (i < cnt) {
-          scan_put<false>(po + i * s.n_c, lane, none, at.n);
+          scan_put<PAIR>(po + i * s.n_c, lane, none, at.n);
         }
     }
     t0 = t1;
   }
-  if (at.hi == s.T) scan_finish(s, at, state);
+  if (at.hi == s.T) scan_finish<PAIR>(s, at, state);
 }
 
 // Backwards in time: wave 0 has a tile's last steps, and step i of a wave is the i-th from its end.
-template <class E, int GATE>
+template <class E, int GATE, bool PAIR>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
   constexpr int L = 8;
   constexpr bool X = GATE != DISTDL_GATE_GIVEN;
   __shared__ float lds[2][kScanWaves][2][kScanCols];
-  const ScanPlace at = scan_place(s);
+  const ScanPlace at = scan_place<PAIR>(s, s.segments == 1);
   const int wave = scan_wave(), lane = threadIdx.x & 63;
-  typedef typename ScanRaw<E>::type Raw;
+  typedef ScanRaw<E, PAIR> Raw;
   float state[kScanV];
-  scan_start<true>(s, at, state);
+  scan_start<true, PAIR>(s, at, lds[1], state);
   int turn = 0;
   for (int64_t t1 = at.hi; t1 > at.lo; turn ^= 1) {
     const ScanSpan sp = scan_span(s, t1 - 1);
@@ -382,8 +423,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
     }
     auto compose = [&](int i) {
       float g[kScanV], d[kScanV];
-      scan_values(ra[i], g);
-      scan_values(rd[i], d);
+      ra[i].values(g);
+      rd[i].values(d);
 #pragma unroll
       for (int v = 0; v < kScanV; ++v) {
         scan_gate<GATE>(g[v], a[i][v], rest[i][v]);
@@ -393,9 +434,9 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
     };
     auto gradient = [&](int i, bool zero, float* da, float* dx) {
       float d[kScanV], x[kScanV] = {}, before[kScanV];
-      scan_values(rd[i], d);
-      if (X) scan_values(rx[i], x);
-      scan_values(rh[i], before);
+      rd[i].values(d);
+      if (X) rx[i].values(x);
+      rh[i].values(before);
 #pragma unroll
       for (int v = 0; v < kScanV; ++v) {
         if (zero) before[v] = first[v];
@@ -408,13 +449,13 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
     if (full) {
 #pragma unroll
       for (int i = 0; i < L; ++i) {
-        ra[i] = scan_at<true>(pa - i * s.n_c, lane, 0);
-        rd[i] = scan_at<true>(pd - i * s.n_c, lane, 0);
+        ra[i].load(pa - i * s.n_c, lane, kScanV);
+        rd[i].load(pd - i * s.n_c, lane, kScanV);
       }
 #pragma unroll
       for (int i = 0; i < L; ++i) {
-        rh[i] = scan_at<true>(ph - i * s.n_c, lane, 0);
-        if (X) rx[i] = scan_at<true>(px - i * s.n_c, lane, 0);
+        rh[i].load(ph - i * s.n_c, lane, kScanV);
+        if (X) rx[i].load(px - i * s.n_c, lane, kScanV);
       }
 #pragma unroll
       for (int i = 0; i < L; ++i) compose(i);
@@ -422,19 +463,19 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
 #pragma unroll
       for (int i = 0; i < L; ++i)
         if (i >= skip && i < cnt) {
-          ra[i] = scan_at<false>(pa - i * s.n_c, lane, at.n);
-          rd[i] = scan_at<false>(pd - i * s.n_c, lane, at.n);
-          if (X) rx[i] = scan_at<false>(px - i * s.n_c, lane, at.n);
+          ra[i].load(pa - i * s.n_c, lane, at.n);
+          rd[i].load(pd - i * s.n_c, lane, at.n);
+          if (X) rx[i].load(px - i * s.n_c, lane, at.n);
           const int64_t t = last - i;
           if (t > sp.lo) {
-            rh[i] = scan_at<false>(ph - i * s.n_c, lane, at.n);
+            rh[i].load(ph - i * s.n_c, lane, at.n);
           } else if (t > 0) {  // the last state of the worker before
             const ScanSpan b = scan_span(s, t - 1);
-            rh[i] = scan_at<false>((const E*)scan_worker(s, b.p).h + ((int64_t)at.b * (b.hi - b.lo) + (b.hi - b.lo - 1)) * s.n_c + at.c, lane, at.n);
+            rh[i].load((const E*)scan_worker(s, b.p).h + ((int64_t)at.b * (b.hi - b.lo) + (b.hi - b.lo - 1)) * s.n_c + at.c, lane, at.n);
           } else {
             rh[i] = Raw{};
 #pragma unroll
-            for (int v = 0; v < kScanV; ++v) first[v] = s.h0 && v < at.n ? s.h0[at.b * s.n_c + at.c + lane * kScanV + v] : 0.f;
+            for (int v = 0; v < kScanV; ++v) first[v] = s.h0 && v < at.n ? s.h0[at.b * s.n_c + at.c + scan_channel<PAIR>(lane, v)] : 0.f;
           }
         }
 #pragma unroll
@@ -447,8 +488,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
       for (int i = 0; i < L; ++i) {
         float da[kScanV], dx[kScanV];
         gradient(i, false, da, dx);
-        scan_put<true>(o0 - i * s.n_c, lane, da, 0);
-        scan_put<true>(o1 - i * s.n_c, lane, dx, 0);
+        scan_put<PAIR>(o0 - i * s.n_c, lane, da, kScanV);
+        scan_put<PAIR>(o1 - i * s.n_c, lane, dx, kScanV);
       }
     } else {
 #pragma unroll
@@ -456,13 +497,13 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
         if (i < cnt) {
           float da[kScanV] = {}, dx[kScanV] = {};
           if (i >= skip) gradient(i, last - i == 0, da, dx);
-          scan_put<false>(o0 - i * s.n_c, lane, da, at.n);
-          scan_put<false>(o1 - i * s.n_c, lane, dx, at.n);
+          scan_put<PAIR>(o0 - i * s.n_c, lane, da, at.n);
+          scan_put<PAIR>(o1 - i * s.n_c, lane, dx, at.n);
         }
     }
     t1 = t0;
   }
-  if (at.lo == 0) scan_finish(s, at, state);
+  if (at.lo == 0) scan_finish<PAIR>(s, at, state);
 }
 
 // One token of each row: its state lies at row slots[row] of the pool.  A row without a slot of the pool is idle.
@@ -470,26 +511,31 @@ template <class E, int GATE>
 __global__ __launch_bounds__(256) void scan_step_kernel(const E* __restrict__ a, const E* __restrict__ x, float* __restrict__ state,
                                                         const int32_t* __restrict__ slots, E* __restrict__ h, int64_t n_slots,
                                                         int64_t n_c) {
-  const int64_t row = blockIdx.y, c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * kScanV;
+  const int64_t row = blockIdx.y, c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (c >= n_c) return;
-  const int n = (int)min((int64_t)kScanV, n_c - c);
+  const int n = (int)min((int64_t)8, n_c - c);
   const int64_t slot = slots ? slots[row] : row, o = row * n_c + c;
-  float out[kScanV] = {};
+  float out[8] = {};
   if (slot >= 0 && slot < n_slots) {
-    float g[kScanV], u[kScanV], old[kScanV];
     float* const at = state + slot * n_c + c;
-    scan_values(scan_load(a + o, n), g);
-    scan_values(scan_load(x + o, n), u);
-    scan_values(scan_load(at, n), old);
+    Eight<E> ra, rx;
+    Eight<float> rs;
+    ra.load(a + o, n);
+    rx.load(x + o, n);
+    rs.load(at, n);
+    float g[8], u[8];
+    ra.values(g);
+    rx.values(u);
+    rs.values(out);
 #pragma unroll
-    for (int v = 0; v < kScanV; ++v) {
+    for (int v = 0; v < 8; ++v) {
       float f, rest;
       scan_gate<GATE>(g[v], f, rest);
-      out[v] = fmaf(f, old[v], rest * u[v]);
+      out[v] = fmaf(f, out[v], rest * u[v]);
     }
-    scan_store(at, out, n);
+    store8(at, out, n);
   }
-  scan_store(h + o, out, n);
+  store8(h + o, out, n);
 }
 
 }  // namespace distdl
@@ -535,15 +581,22 @@ static int scan_args(distdl_scan_plan* p, const std::vector<ScanWorker>& w, hipS
   return rc;
 }
 
-template <class E, int GATE>
+template <class E, int GATE, bool PAIR>
 static void launch_scan(const ScanArgs& s, bool back, hipStream_t st) {
   const dim3 grid((unsigned)((int64_t)s.groups * s.n_b * s.segments)), block(64 * kScanWaves);
   if (s.segments > 1) {
-    if (back) hipLaunchKernelGGL((scan_map_kernel<E, GATE, true>), grid, block, 0, st, s);
-    else hipLaunchKernelGGL((scan_map_kernel<E, GATE, false>), grid, block, 0, st, s);
+    if (back) hipLaunchKernelGGL((scan_map_kernel<E, GATE, PAIR, true>), grid, block, 0, st, s);
+    else hipLaunchKernelGGL((scan_map_kernel<E, GATE, PAIR, false>), grid, block, 0, st, s);
   }
-  if (back) hipLaunchKernelGGL((scan_bwd_kernel<E, GATE>), grid, block, 0, st, s);
-  else hipLaunchKernelGGL((scan_fwd_kernel<E, GATE>), grid, block, 0, st, s);
+  if (back) hipLaunchKernelGGL((scan_bwd_kernel<E, GATE, PAIR>), grid, block, 0, st, s);
+  else hipLaunchKernelGGL((scan_fwd_kernel<E, GATE, PAIR>), grid, block, 0, st, s);
+}
+
+// Whether every row of every array starts at a multiple of two elements.
+static bool scan_pairs(const distdl_scan_plan* p, const std::vector<ScanWorker>& w) {
+  uintptr_t bits = (uintptr_t)(p->n_c * (int64_t)dtype_size(p->dtype));
+  for (const ScanWorker& v : w) bits |= (uintptr_t)v.a | (uintptr_t)v.x | (uintptr_t)v.h | (uintptr_t)v.dh | (uintptr_t)v.o0 | (uintptr_t)v.o1;
+  return bits % (2 * dtype_size(p->dtype)) == 0;
 }
 
 template <class F>
@@ -584,9 +637,9 @@ int distdl_scan_plan_create(distdl_scan_plan** out, int64_t n_b, int64_t T, int6
     p->gate = gate;
     p->dtype = dtype;
     p->groups = (int)groups;
-    // Two workgroups for each of the 256 compute units; a segment has at least four tiles of the forward pass.
-    const int64_t tile = 16 * kScanWaves, want = (512 + groups * n_b - 1) / (groups * n_b);
-    const int64_t most = std::max<int64_t>(1, T / (4 * tile)), segments = std::min(want, most);
+    // Four workgroups for each of the 256 compute units; a segment has at least a tile of the forward pass.
+    const int64_t tile = 16 * kScanWaves, want = (1024 + groups * n_b - 1) / (groups * n_b);
+    const int64_t most = std::max<int64_t>(1, T / tile), segments = std::min(want, most);
     p->seg_steps = (((T + segments - 1) / segments) + tile - 1) / tile * tile;
     p->segments = (int)((T + p->seg_steps - 1) / p->seg_steps);
     *out = p.release();
@@ -625,7 +678,10 @@ int distdl_scan_fwd(distdl_scan_plan* p, const void* const a_dev[], const void* 
     s.hT = hT_dev;
     {
       ProfScope prof("scan_fwd", st_);
-      scan_kind(p->dtype, p->gate, [&](auto e, auto gate) { launch_scan<decltype(e), decltype(gate)::value>(s, false, st_); });
+      scan_kind(p->dtype, p->gate, [&](auto e, auto gate) {
+        if (scan_pairs(p, w)) launch_scan<decltype(e), decltype(gate)::value, true>(s, false, st_);
+        else launch_scan<decltype(e), decltype(gate)::value, false>(s, false, st_);
+      });
     }
     DISTDL_HIP_TRY(hipGetLastError());
     return DISTDL_OK;
@@ -659,7 +715,10 @@ int distdl_scan_bwd(distdl_scan_plan* p, const void* const a_dev[], const void* 
     s.hT = dh0_dev;
     {
       ProfScope prof("scan_bwd", st_);
-      scan_kind(p->dtype, p->gate, [&](auto e, auto gate) { launch_scan<decltype(e), decltype(gate)::value>(s, true, st_); });
+      scan_kind(p->dtype, p->gate, [&](auto e, auto gate) {
+        if (scan_pairs(p, w)) launch_scan<decltype(e), decltype(gate)::value, true>(s, true, st_);
+        else launch_scan<decltype(e), decltype(gate)::value, false>(s, true, st_);
+      });
     }
     DISTDL_HIP_TRY(hipGetLastError());
     return DISTDL_OK;
@@ -682,7 +741,7 @@ int distdl_scan_step(const void* a_dev, const void* x_dev, float* state_dev, int
   hipStream_t st_ = (hipStream_t)stream;
   {
     ProfScope prof("scan_step", st_);
-    const int64_t wide = (n_c + 256 * kScanV - 1) / (256 * kScanV);
+    const int64_t wide = (n_c + 2047) / 2048;
     for (int64_t row0 = 0; row0 < rows; row0 += 65535) {  // (one launch for any batch that a decoder has)
       const int64_t n = std::min<int64_t>(65535, rows - row0);
       scan_kind(dtype, gate, [&](auto e, auto g) {
