@@ -308,66 +308,82 @@ __device__ __forceinline__ void scan_finish(const ScanArgs& s, const ScanPlace& 
     if (v < at.n) to[scan_channel<PAIR>(threadIdx.x & 63, v)] = state[v];
 }
 
+// A wave's steps of one tile: `from` is the first (the last, backwards) of them.
+struct ScanTile {
+  int64_t next, from, row;  // where the tile after it starts; first step; its element in the worker's arrays
+  int64_t lo;               // the worker's first step
+  int p, cnt, live;         // worker; steps; those inside the sequence
+  bool full;                // all L steps and all channels
+};
+
 template <class E, int GATE, bool PAIR>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
-  constexpr int L = 16;
+  constexpr int L = 8;
   __shared__ float lds[2][kScanWaves][2][kScanCols];
   const ScanPlace at = scan_place<PAIR>(s, s.segments > 1);
   const int wave = scan_wave(), lane = threadIdx.x & 63;
   typedef ScanRaw<E, PAIR> Raw;
+  Raw ra[L], rx[L];
+  auto tile = [&](int64_t t0) {
+    ScanTile t;
+    const ScanSpan sp = scan_span(s, t0);
+    t.p = sp.p;
+    t.lo = sp.lo;
+    t.next = min(min(at.hi, sp.hi), t0 + kScanWaves * L);
+    t.from = t0 + wave * L;
+    t.cnt = (int)max((int64_t)0, min((int64_t)L, t.next - t.from));
+    t.live = (int)max((int64_t)0, min((int64_t)t.cnt, at.len - t.from));
+    t.row = ((int64_t)at.b * (sp.hi - sp.lo) + (t.from - sp.lo)) * s.n_c + at.c;
+    t.full = t.live == L && at.all;
+    const ScanWorker& w = scan_worker(s, t.p);
+    const E *pa = (const E*)w.a + t.row, *px = (const E*)w.x + t.row;
+    if (t.full) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        ra[i].load(pa + i * s.n_c, lane, kScanV);
+        rx[i].load(px + i * s.n_c, lane, kScanV);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (i < t.live) {
+          ra[i].load(pa + i * s.n_c, lane, at.n);
+          rx[i].load(px + i * s.n_c, lane, at.n);
+        }
+    }
+    return t;
+  };
+  ScanTile t = tile(at.lo);
   float state[kScanV];
   scan_start<false, PAIR>(s, at, lds[1], state);
-  int turn = 0;
-  for (int64_t t0 = at.lo; t0 < at.hi; turn ^= 1) {
-    const ScanSpan sp = scan_span(s, t0);
-    const ScanWorker& w = scan_worker(s, sp.p);
-    const int64_t t1 = min(min(at.hi, sp.hi), t0 + kScanWaves * L), mine0 = t0 + wave * L;
-    const int cnt = (int)max((int64_t)0, min((int64_t)L, t1 - mine0)), live = (int)max((int64_t)0, min((int64_t)cnt, at.len - mine0));
-    const int64_t row = ((int64_t)at.b * (sp.hi - sp.lo) + (mine0 - sp.lo)) * s.n_c + at.c;
-    const E *pa = (const E*)w.a + row, *px = (const E*)w.x + row;
-    E* const po = (E*)w.o0 + row;
-    const bool full = live == L && at.all;
-    Raw ra[L], rx[L];
+  for (int turn = 0;; turn ^= 1) {
     float a[L][kScanV], u[L][kScanV], A[kScanV], B[kScanV], h[kScanV];
 #pragma unroll
     for (int v = 0; v < kScanV; ++v) {
       A[v] = 1.f;
       B[v] = 0.f;
     }
-    auto compose = [&](int i) {
-      float g[kScanV], x[kScanV];
-      ra[i].values(g);
-      rx[i].values(x);
 #pragma unroll
-      for (int v = 0; v < kScanV; ++v) {
-        float rest;
-        scan_gate<GATE>(g[v], a[i][v], rest);
-        u[i][v] = rest * x[v];
-        A[v] *= a[i][v];
-        B[v] = fmaf(a[i][v], B[v], u[i][v]);
-      }
-    };
-    if (full) {
+    for (int i = 0; i < L; ++i)
+      if (i < t.live) {
+        float g[kScanV], x[kScanV];
+        ra[i].values(g);
+        rx[i].values(x);
 #pragma unroll
-      for (int i = 0; i < L; ++i) {
-        ra[i].load(pa + i * s.n_c, lane, kScanV);
-        rx[i].load(px + i * s.n_c, lane, kScanV);
-      }
-#pragma unroll
-      for (int i = 0; i < L; ++i) compose(i);
-    } else {
-#pragma unroll
-      for (int i = 0; i < L; ++i)
-        if (i < live) {
-          ra[i].load(pa + i * s.n_c, lane, at.n);
-          rx[i].load(px + i * s.n_c, lane, at.n);
+        for (int v = 0; v < kScanV; ++v) {
+          float rest;
+          scan_gate<GATE>(g[v], a[i][v], rest);
+          u[i][v] = rest * x[v];
+          A[v] *= a[i][v];
+          B[v] = fmaf(a[i][v], B[v], u[i][v]);
         }
-#pragma unroll
-      for (int i = 0; i < L; ++i)
-        if (i < live) compose(i);
-    }
+      }
+    const ScanTile now = t;
+    const bool more = now.next < at.hi;
+    if (more) t = tile(now.next);  // its loads are under way while this tile's waves meet and write
     scan_meet(lds[turn], A, B, state, h);
-    if (full) {
+    E* const po = (E*)scan_worker(s, now.p).o0 + now.row;
+    if (now.full) {
 #pragma unroll
       for (int i = 0; i < L; ++i) {
 #pragma unroll
@@ -378,15 +394,15 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
       const float none[kScanV] = {};
 #pragma unroll
       for (int i = 0; i < L; ++i)
-        if (i < live) {
+        if (i < now.live) {
 #pragma unroll
           for (int v = 0; v < kScanV; ++v) h[v] = fmaf(a[i][v], h[v], u[i][v]);
           scan_put<PAIR>(po + i * s.n_c, lane, h, at.n);
-        } else if (i < cnt) {
+        } else if (i < now.cnt) {
           scan_put<PAIR>(po + i * s.n_c, lane, none, at.n);
         }
     }
-    t0 = t1;
+    if (!more) break;
   }
   if (at.hi == s.T) scan_finish<PAIR>(s, at, state);
 }
@@ -394,114 +410,118 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
 // Backwards in time: wave 0 has a tile's last steps, and step i of a wave is the i-th from its end.
 template <class E, int GATE, bool PAIR>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
-  constexpr int L = 8;
+  constexpr int L = sizeof(ScanRaw<E, PAIR>) == 4 ? 8 : 4;  // what the registers hold beside the next tile's loads
   constexpr bool X = GATE != DISTDL_GATE_GIVEN;
   __shared__ float lds[2][kScanWaves][2][kScanCols];
   const ScanPlace at = scan_place<PAIR>(s, s.segments == 1);
   const int wave = scan_wave(), lane = threadIdx.x & 63;
   typedef ScanRaw<E, PAIR> Raw;
+  Raw ra[L], rx[L], rd[L], rh[L];
+  float first[kScanV] = {};  // the state in front of step 0, in 32 bits
+  auto tile = [&](int64_t t1) {
+    ScanTile t;
+    const ScanSpan sp = scan_span(s, t1 - 1);
+    t.p = sp.p;
+    t.lo = sp.lo;
+    t.next = max(max(at.lo, sp.lo), t1 - kScanWaves * L);
+    t.from = t1 - 1 - wave * L;  // step i: from - i
+    t.cnt = (int)max((int64_t)0, min((int64_t)L, t.from + 1 - t.next));
+    t.live = t.cnt - (int)max((int64_t)0, min((int64_t)t.cnt, t.from + 1 - at.len));  // (steps behind the sequence's end come first)
+    t.row = ((int64_t)at.b * (sp.hi - sp.lo) + (t.from - sp.lo)) * s.n_c + at.c;
+    t.full = t.live == L && at.all && t.from - L + 1 > sp.lo;  // and the state before each step is this worker's
+    const ScanWorker& w = scan_worker(s, t.p);
+    const E *pa = (const E*)w.a + t.row, *px = X ? (const E*)w.x + t.row : nullptr, *ph = (const E*)w.h + t.row - s.n_c, *pd = (const E*)w.dh + t.row;
+    if (t.full) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        ra[i].load(pa - i * s.n_c, lane, kScanV);
+        rd[i].load(pd - i * s.n_c, lane, kScanV);
+        rh[i].load(ph - i * s.n_c, lane, kScanV);
+        if (X) rx[i].load(px - i * s.n_c, lane, kScanV);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (i >= t.cnt - t.live && i < t.cnt) {
+          ra[i].load(pa - i * s.n_c, lane, at.n);
+          rd[i].load(pd - i * s.n_c, lane, at.n);
+          if (X) rx[i].load(px - i * s.n_c, lane, at.n);
+          const int64_t step = t.from - i;
+          if (step > t.lo) {
+            rh[i].load(ph - i * s.n_c, lane, at.n);
+          } else if (step > 0) {  // the last state of the worker before
+            const ScanSpan b = scan_span(s, step - 1);
+            rh[i].load((const E*)scan_worker(s, b.p).h + ((int64_t)at.b * (b.hi - b.lo) + (b.hi - b.lo - 1)) * s.n_c + at.c, lane, at.n);
+          } else {
+#pragma unroll
+            for (int v = 0; v < kScanV; ++v) first[v] = s.h0 && v < at.n ? s.h0[at.b * s.n_c + at.c + scan_channel<PAIR>(lane, v)] : 0.f;
+          }
+        }
+    }
+    return t;
+  };
+  ScanTile t = tile(at.hi);
   float state[kScanV];
   scan_start<true, PAIR>(s, at, lds[1], state);
-  int turn = 0;
-  for (int64_t t1 = at.hi; t1 > at.lo; turn ^= 1) {
-    const ScanSpan sp = scan_span(s, t1 - 1);
-    const ScanWorker& w = scan_worker(s, sp.p);
-    const int64_t t0 = max(max(at.lo, sp.lo), t1 - kScanWaves * L), last = t1 - 1 - wave * L;  // step i: last - i
-    const int cnt = (int)max((int64_t)0, min((int64_t)L, last + 1 - t0));
-    const int skip = (int)max((int64_t)0, min((int64_t)cnt, last + 1 - at.len));  // steps behind the sequence's end come first
-    const int64_t row = ((int64_t)at.b * (sp.hi - sp.lo) + (last - sp.lo)) * s.n_c + at.c;
-    const E *pa = (const E*)w.a + row, *px = X ? (const E*)w.x + row : nullptr, *ph = (const E*)w.h + row - s.n_c, *pd = (const E*)w.dh + row;
-    E *const o0 = (E*)w.o0 + row, *const o1 = (E*)w.o1 + row;
-    const bool full = cnt == L && skip == 0 && at.all && last - L + 1 > sp.lo;  // and the state before each step is this worker's
-    Raw ra[L], rx[L], rd[L], rh[L];
-    float first[kScanV] = {};  // the state in front of step 0, in 32 bits
-    float a[L][kScanV], rest[L][kScanV], A[kScanV], B[kScanV], back[kScanV];
+  for (int turn = 0;; turn ^= 1) {
+    // dx = d rest, da = d slope
+    float a[L][kScanV], d[L][kScanV], rest[L][kScanV], slope[L][kScanV], A[kScanV], B[kScanV], back[kScanV];
 #pragma unroll
     for (int v = 0; v < kScanV; ++v) {
       A[v] = 1.f;
       B[v] = 0.f;
     }
-    auto compose = [&](int i) {
-      float g[kScanV], d[kScanV];
-      ra[i].values(g);
-      rd[i].values(d);
 #pragma unroll
-      for (int v = 0; v < kScanV; ++v) {
-        scan_gate<GATE>(g[v], a[i][v], rest[i][v]);
-        A[v] *= a[i][v];
-        B[v] = a[i][v] * (B[v] + d[v]);
-      }
-    };
-    auto gradient = [&](int i, bool zero, float* da, float* dx) {
-      float d[kScanV], x[kScanV] = {}, before[kScanV];
-      rd[i].values(d);
-      if (X) rx[i].values(x);
-      rh[i].values(before);
+    for (int i = 0; i < L; ++i)
+      if (i >= t.cnt - t.live && i < t.cnt) {
+        float g[kScanV], x[kScanV] = {}, before[kScanV];
+        ra[i].values(g);
+        rd[i].values(d[i]);
+        if (X) rx[i].values(x);
+        rh[i].values(before);
 #pragma unroll
-      for (int v = 0; v < kScanV; ++v) {
-        if (zero) before[v] = first[v];
-        d[v] += back[v];
-        back[v] = a[i][v] * d[v];
-        da[v] = X ? d[v] * (before[v] - x[v]) * (a[i][v] * rest[i][v]) : d[v] * before[v];
-        dx[v] = d[v] * rest[i][v];
-      }
-    };
-    if (full) {
-#pragma unroll
-      for (int i = 0; i < L; ++i) {
-        ra[i].load(pa - i * s.n_c, lane, kScanV);
-        rd[i].load(pd - i * s.n_c, lane, kScanV);
-      }
-#pragma unroll
-      for (int i = 0; i < L; ++i) {
-        rh[i].load(ph - i * s.n_c, lane, kScanV);
-        if (X) rx[i].load(px - i * s.n_c, lane, kScanV);
-      }
-#pragma unroll
-      for (int i = 0; i < L; ++i) compose(i);
-    } else {
-#pragma unroll
-      for (int i = 0; i < L; ++i)
-        if (i >= skip && i < cnt) {
-          ra[i].load(pa - i * s.n_c, lane, at.n);
-          rd[i].load(pd - i * s.n_c, lane, at.n);
-          if (X) rx[i].load(px - i * s.n_c, lane, at.n);
-          const int64_t t = last - i;
-          if (t > sp.lo) {
-            rh[i].load(ph - i * s.n_c, lane, at.n);
-          } else if (t > 0) {  // the last state of the worker before
-            const ScanSpan b = scan_span(s, t - 1);
-            rh[i].load((const E*)scan_worker(s, b.p).h + ((int64_t)at.b * (b.hi - b.lo) + (b.hi - b.lo - 1)) * s.n_c + at.c, lane, at.n);
-          } else {
-            rh[i] = Raw{};
-#pragma unroll
-            for (int v = 0; v < kScanV; ++v) first[v] = s.h0 && v < at.n ? s.h0[at.b * s.n_c + at.c + scan_channel<PAIR>(lane, v)] : 0.f;
-          }
+        for (int v = 0; v < kScanV; ++v) {
+          if (t.from - i == 0) before[v] = first[v];
+          scan_gate<GATE>(g[v], a[i][v], rest[i][v]);
+          slope[i][v] = X ? (before[v] - x[v]) * (a[i][v] * rest[i][v]) : before[v];
+          A[v] *= a[i][v];
+          B[v] = a[i][v] * (B[v] + d[i][v]);
         }
-#pragma unroll
-      for (int i = 0; i < L; ++i)
-        if (i >= skip && i < cnt) compose(i);
-    }
+      }
+    const ScanTile now = t;
+    const bool more = now.next > at.lo;
+    if (more) t = tile(now.next);
     scan_meet(lds[turn], A, B, state, back);
-    if (full) {
+    const ScanWorker& w = scan_worker(s, now.p);
+    E *const o0 = (E*)w.o0 + now.row, *const o1 = (E*)w.o1 + now.row;
+    auto gradient = [&](int i, float* da, float* dx) {
+#pragma unroll
+      for (int v = 0; v < kScanV; ++v) {
+        const float all = d[i][v] + back[v];
+        back[v] = a[i][v] * all;
+        da[v] = all * slope[i][v];
+        dx[v] = all * rest[i][v];
+      }
+    };
+    if (now.full) {
 #pragma unroll
       for (int i = 0; i < L; ++i) {
         float da[kScanV], dx[kScanV];
-        gradient(i, false, da, dx);
+        gradient(i, da, dx);
         scan_put<PAIR>(o0 - i * s.n_c, lane, da, kScanV);
         scan_put<PAIR>(o1 - i * s.n_c, lane, dx, kScanV);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < L; ++i)
-        if (i < cnt) {
+        if (i < now.cnt) {
           float da[kScanV] = {}, dx[kScanV] = {};
-          if (i >= skip) gradient(i, last - i == 0, da, dx);
+          if (i >= now.cnt - now.live) gradient(i, da, dx);
           scan_put<PAIR>(o0 - i * s.n_c, lane, da, at.n);
           scan_put<PAIR>(o1 - i * s.n_c, lane, dx, at.n);
         }
     }
-    t1 = t0;
+    if (!more) break;
   }
   if (at.lo == 0) scan_finish<PAIR>(s, at, state);
 }
