@@ -11,8 +11,10 @@
 // segment's map, the second starts every segment from the maps before it (time is read twice there, once from HBM).
 // The workers' boundaries are those of arrays only: a state passes them as it passes tiles.
 #include <algorithm>
+#include <cstddef>
 
 #include "block8.h"
+#include "buffer.h"
 #include "common.h"
 #include "profile.h"
 
@@ -31,31 +33,36 @@ struct ScanWorker {
 struct ScanArgs {
   ScanWorker w[kScanInline];
   const ScanWorker* more;
-  int64_t T, n_c;
-  int64_t part, extra;   // worker p has part + (p < extra) steps
-  int32_t P, n_b, groups, segments;
-  int64_t seg_steps;
+  int64_t n_c;
+  int32_t T, part, extra;  // worker p has part + (p < extra) steps
+  int32_t P, n_b, groups, segments, seg_steps;
   const int32_t* lengths;
   const float *h0, *end;  // end: dhT of the adjoint
   float *hT;              // forward: hT; adjoint: dh0
   float* maps;            // [n_b][segments][2][n_c]
 };
 
-__device__ __forceinline__ const ScanWorker& scan_worker(const ScanArgs& s, int p) { return s.more ? s.more[p] : s.w[p]; }
+// Worker p's arrays, from the table or from the launch's own arguments (of which they are the first).  Read as constants, into scalar
+// registers: a vector load of them would wait for all data under way, and the compiler would take what it gives for different in each lane.
+__device__ __forceinline__ ScanWorker scan_worker(const ScanArgs& s, int p) {
+  static_assert(offsetof(ScanArgs, w) == 0, "the kernels' first argument starts with the workers");
+  typedef const __attribute__((address_space(4))) ScanWorker* Constant;
+  const Constant w = (s.more ? (Constant)(uint64_t)s.more : (Constant)__builtin_amdgcn_kernarg_segment_ptr()) + p;
+  return ScanWorker{w->a, w->x, w->h, w->dh, w->o0, w->o1};
+}
 
 struct ScanSpan {  // the worker that holds step t, and its steps
-  int p;
-  int64_t lo, hi;
+  int p, lo, hi;
 };
-__device__ __forceinline__ ScanSpan scan_span(const ScanArgs& s, int64_t t) {
-  const int64_t wide = s.extra * (s.part + 1);
+__device__ __forceinline__ ScanSpan scan_span(const ScanArgs& s, int t) {
+  const int wide = s.extra * (s.part + 1);
   ScanSpan r;
   if (t < wide) {
-    r.p = (int)(t / (s.part + 1));
+    r.p = (uint32_t)t / (uint32_t)(s.part + 1);
     r.lo = r.p * (s.part + 1);
     r.hi = r.lo + s.part + 1;
   } else {
-    r.p = (int)(s.extra + (t - wide) / s.part);
+    r.p = s.extra + (uint32_t)(t - wide) / (uint32_t)s.part;
     r.lo = wide + (r.p - s.extra) * s.part;
     r.hi = r.lo + s.part;
   }
@@ -64,27 +71,50 @@ __device__ __forceinline__ ScanSpan scan_span(const ScanArgs& s, int64_t t) {
 
 // The two channels of a lane in one step: neighbours in one access of twice the size (PAIR), where every row starts at a multiple of that, and
 // otherwise 64 apart in two, each at its natural alignment.  Measured, 7 x 2049 steps of fp32, adjoint: 1024 channels in pairs 92 us;
-// 1001 and 1002 channels in pairs that straddle 203 and 163 us.  n: how many of the two exist.
+// 1001 and 1002 channels in pairs that straddle 203 and 163 us.
+template <bool PAIR>
+__device__ __forceinline__ int scan_channel(int lane, int v) { return PAIR ? lane * 2 + v : lane + 64 * v; }
+
+// Steps of one array as a wave reads and writes them: a buffer from its group's first channel of some step on, whose byte offsets are
+// the lane's (the same for all steps; one that fails the check where the channel does not exist) and the step's (uniform).
+// So a step costs a scalar addition and no vector ones.
+struct ScanLane {
+  uint32_t off[2];
+  // nowhere, unless `is` (which is uniform)
+  __device__ __forceinline__ ScanLane where(bool is) const { return ScanLane{{is ? off[0] : kOob, is ? off[1] : kOob}}; }
+};
+template <class E, bool PAIR>
+__device__ __forceinline__ ScanLane scan_lane(int64_t left) {
+  ScanLane l;
+#pragma unroll
+  for (int v = 0; v < 2; ++v) {
+    const int c = scan_channel<PAIR>(threadIdx.x & 63, v);
+    l.off[v] = c < left ? c * (uint32_t)sizeof(E) : kOob;
+  }
+  return l;
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t scan_rows(const void* p) { return rsrc_of(p, kOob); }
+
 template <class E, bool PAIR>
 struct ScanRaw {
-  u32x2 v;
-  __device__ __forceinline__ void load(const E* row, int lane, int n) {
-    v[0] = n > 0 ? bits(row[lane]) : 0u;
-    v[1] = n > 1 ? bits(row[lane + 64]) : 0u;
+  uint32_t v[2];
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, const ScanLane& l, uint32_t step) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (sizeof(E) == 4) v[i] = __builtin_amdgcn_raw_buffer_load_b32(r, l.off[i], step, 0);
+      else v[i] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, l.off[i], step, 0);
+    }
   }
   __device__ __forceinline__ void values(float* f) const {
 #pragma unroll
     for (int i = 0; i < 2; ++i) f[i] = __uint_as_float(sizeof(E) == 4 ? v[i] : v[i] << 16);
   }
-  static __device__ __forceinline__ uint32_t bits(float x) { return __float_as_uint(x); }
-  static __device__ __forceinline__ uint32_t bits(uint16_t x) { return x; }
 };
 template <>
 struct ScanRaw<float, true> {
   u32x2 v;
-  __device__ __forceinline__ void load(const float* row, int lane, int n) {
-    if (n > 1) v = *(const u32x2*)(row + lane * 2);
-    else v = u32x2{n > 0 ? __float_as_uint(row[lane * 2]) : 0u, 0u};
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, const ScanLane& l, uint32_t step) {
+    v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, l.off[0], step, 0));
   }
   __device__ __forceinline__ void values(float* f) const {
     f[0] = __uint_as_float(v[0]);
@@ -94,36 +124,27 @@ struct ScanRaw<float, true> {
 template <>
 struct ScanRaw<uint16_t, true> {
   uint32_t v;
-  __device__ __forceinline__ void load(const uint16_t* row, int lane, int n) {
-    if (n > 1) v = *(const uint32_t*)(row + lane * 2);
-    else v = n > 0 ? row[lane * 2] : 0u;
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, const ScanLane& l, uint32_t step) {
+    v = __builtin_amdgcn_raw_buffer_load_b32(r, l.off[0], step, 0);
   }
   __device__ __forceinline__ void values(float* f) const {
     f[0] = bf16_lo(v);
     f[1] = bf16_hi(v);
   }
 };
-template <bool PAIR>
-__device__ __forceinline__ void scan_put(float* row, int lane, const float* v, int n) {
-  if (PAIR && n > 1) {
-    *(u32x2*)(row + lane * 2) = u32x2{__float_as_uint(v[0]), __float_as_uint(v[1])};
+template <class E, bool PAIR>
+__device__ __forceinline__ void scan_put(__amdgpu_buffer_rsrc_t r, const ScanLane& l, uint32_t step, const float* v) {
+  if constexpr (PAIR) {
+    if constexpr (sizeof(E) == 4) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(v[0]), __float_as_uint(v[1])}, r, l.off[0], step, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(to_bf16(v[0], v[1]), r, l.off[0], step, 0);
   } else {
-    if (n > 0) row[PAIR ? lane * 2 : lane] = v[0];
-    if (n > 1) row[lane + 64] = v[1];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (sizeof(E) == 4) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[i]), r, l.off[i], step, 0);
+      else __builtin_amdgcn_raw_buffer_store_b16(to_bf16(v[i]), r, l.off[i], step, 0);
+    }
   }
 }
-template <bool PAIR>
-__device__ __forceinline__ void scan_put(uint16_t* row, int lane, const float* v, int n) {
-  if (PAIR && n > 1) {
-    *(uint32_t*)(row + lane * 2) = to_bf16(v[0], v[1]);
-  } else {
-    if (n > 0) row[PAIR ? lane * 2 : lane] = to_bf16(v[0]);
-    if (n > 1) row[lane + 64] = to_bf16(v[1]);
-  }
-}
-// Channel v of a lane, from the group's first
-template <bool PAIR>
-__device__ __forceinline__ int scan_channel(int lane, int v) { return PAIR ? lane * 2 + v : lane + 64 * v; }
 
 // a and 1 - a.  Through exp(-|g|), which neither overflows nor loses 1 - a where a is near one.
 template <int GATE>
@@ -143,8 +164,7 @@ __device__ __forceinline__ int scan_wave() { return __builtin_amdgcn_readfirstla
 
 struct ScanPlace {
   int group, seg, b, c, n;  // c: first channel of the group; n: channels of this lane
-  bool all;                 // every lane has both
-  int64_t len, lo, hi;      // steps of the sequence; of the segment
+  int len, lo, hi;          // steps of the sequence; of the segment
 };
 template <bool PAIR>
 __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& s, bool reversed) {
@@ -159,10 +179,9 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& s, bool reversed
   const int64_t left = s.n_c - r.c;
   const int lane = threadIdx.x & 63;
   r.n = (scan_channel<PAIR>(lane, 0) < left) + (scan_channel<PAIR>(lane, 1) < left);
-  r.all = left >= kScanCols;
-  r.len = s.lengths ? max((int64_t)0, min(s.T, (int64_t)s.lengths[r.b])) : s.T;
+  r.len = s.lengths ? max(0, min(s.T, (int)__builtin_amdgcn_readfirstlane(s.lengths[r.b]))) : s.T;
   r.lo = r.seg * s.seg_steps;
-  r.hi = min(s.T, r.lo + s.seg_steps);
+  r.hi = s.T - r.lo < s.seg_steps ? s.T : r.lo + s.seg_steps;
   return r;
 }
 
@@ -229,60 +248,75 @@ __device__ __forceinline__ void scan_start(const ScanArgs& s, const ScanPlace& a
 // A segment's map: a wave composes an eighth of the steps, the eighths meet at the end.
 template <class E, int GATE, bool PAIR, bool BACK>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
-  constexpr int L = 16;
+  constexpr int L = 8;
   __shared__ float lds[kScanWaves][2][kScanCols];
   const ScanPlace at = scan_place<PAIR>(s, BACK);
   const int lane = threadIdx.x & 63, wave = BACK ? kScanWaves - 1 - scan_wave() : scan_wave();
-  const int64_t hi = min(at.hi, at.len), each = (max((int64_t)0, hi - at.lo) + kScanWaves - 1) / kScanWaves;
-  const int64_t from = min(hi, at.lo + wave * each), to = min(hi, from + each);
+  const int hi = min(at.hi, at.len), each = (max(0, hi - at.lo) + kScanWaves - 1) / kScanWaves;
+  const int from = min(hi, at.lo + wave * each), to = min(hi, from + each);
+  const ScanLane off = scan_lane<E, PAIR>(s.n_c - at.c);
+  const uint32_t hop = (uint32_t)(s.n_c * sizeof(E));
   typedef ScanRaw<E, PAIR> Raw;
+  Raw ra[2][L], rx[2][L];  // a run of at most L steps of one worker and the next one, forwards or backwards
+  const int steps = to - from;
+  auto load = [&](int done, Raw* a, Raw* x) {
+    const int t = BACK ? to - 1 - done : from + done;
+    const ScanSpan sp = scan_span(s, done < steps ? t : 0);
+    const int cnt = done < steps ? min(L, BACK ? t + 1 - max(from, sp.lo) : min(to, sp.hi) - t) : 0;
+    const ScanWorker w = scan_worker(s, sp.p);
+    const int64_t row = ((int64_t)at.b * (sp.hi - sp.lo) + (t - sp.lo) - (BACK ? cnt - 1 : 0)) * s.n_c + at.c;
+    const auto pa = scan_rows((const E*)w.a + row), px = scan_rows((const E*)(BACK ? w.dh : w.x) + row);
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const ScanLane o = off.where(i < cnt);
+      const uint32_t step = i < cnt ? (BACK ? cnt - 1 - i : i) * hop : 0;
+      a[i].load(pa, o, step);
+      x[i].load(px, o, step);
+    }
+    return cnt;
+  };
   float A[kScanV], B[kScanV];
 #pragma unroll
   for (int v = 0; v < kScanV; ++v) {
     A[v] = 1.f;
     B[v] = 0.f;
   }
-  for (int64_t done = 0; done < to - from;) {
-    // the next run of at most L steps of one worker, forwards or backwards
-    const int64_t t = BACK ? to - 1 - done : from + done;
-    const ScanSpan sp = scan_span(s, t);
-    const int cnt = (int)min((int64_t)L, BACK ? t + 1 - max(from, sp.lo) : min(to, sp.hi) - t);
-    const ScanWorker& w = scan_worker(s, sp.p);
-    const int64_t row = ((int64_t)at.b * (sp.hi - sp.lo) + (t - sp.lo)) * s.n_c + at.c, hop = BACK ? -s.n_c : s.n_c;
-    const E *pa = (const E*)w.a + row, *px = (const E*)(BACK ? w.dh : w.x) + row;
-    Raw ra[L], rx[L];
-    auto compose = [&](int i) {
+  auto compose = [&](const Raw* ar, const Raw* xr, int cnt) {
+    float a[L][kScanV], u[L][kScanV];
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
       float g[kScanV], x[kScanV];
-      ra[i].values(g);
-      rx[i].values(x);
+      ar[i].values(g);
+      xr[i].values(x);
 #pragma unroll
       for (int v = 0; v < kScanV; ++v) {
-        float a, rest;
-        scan_gate<GATE>(g[v], a, rest);
-        A[v] *= a;
-        B[v] = BACK ? a * (B[v] + x[v]) : fmaf(a, B[v], rest * x[v]);
+        float rest;
+        scan_gate<GATE>(g[v], a[i][v], rest);
+        u[i][v] = BACK ? x[v] : rest * x[v];
       }
-    };
-    if (cnt == L && at.all) {
-#pragma unroll
-      for (int i = 0; i < L; ++i) {
-        ra[i].load(pa + i * hop, lane, kScanV);
-        rx[i].load(px + i * hop, lane, kScanV);
-      }
-#pragma unroll
-      for (int i = 0; i < L; ++i) compose(i);
-    } else {
-#pragma unroll
-      for (int i = 0; i < L; ++i)
-        if (i < cnt) {
-          ra[i].load(pa + i * hop, lane, at.n);
-          rx[i].load(px + i * hop, lane, at.n);
-        }
-#pragma unroll
-      for (int i = 0; i < L; ++i)
-        if (i < cnt) compose(i);
     }
-    done += cnt;
+    if (cnt < L) {
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+#pragma unroll
+        for (int v = 0; v < kScanV; ++v) a[i][v] = i < cnt ? a[i][v] : 1.f;  // (and u is 0)
+    }
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int v = 0; v < kScanV; ++v) {
+        A[v] *= a[i][v];
+        B[v] = BACK ? a[i][v] * (B[v] + u[i][v]) : fmaf(a[i][v], B[v], u[i][v]);
+      }
+  };
+  int done = 0, c0 = load(0, ra[0], rx[0]);
+  while (c0 > 0) {
+    done += c0;
+    const int c1 = load(done, ra[1], rx[1]);
+    compose(ra[0], rx[0], c0);
+    done += c1;
+    c0 = load(done, ra[0], rx[0]);
+    compose(ra[1], rx[1], c1);
   }
   float state[kScanV] = {}, mine[kScanV], all[kScanV];
   scan_meet(lds, A, B, state, mine);  // B of the whole: the map of zero
@@ -293,8 +327,12 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
   }
   if (scan_wave() == 0) {
     float* m = s.maps + ((int64_t)at.b * s.segments + at.seg) * 2 * s.n_c + at.c;
-    scan_put<PAIR>(m, lane, all, at.n);
-    scan_put<PAIR>(m + s.n_c, lane, state, at.n);
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v)
+      if (v < at.n) {
+        m[scan_channel<PAIR>(lane, v)] = all[v];
+        m[s.n_c + scan_channel<PAIR>(lane, v)] = state[v];
+      }
   }
 }
 
@@ -308,12 +346,13 @@ __device__ __forceinline__ void scan_finish(const ScanArgs& s, const ScanPlace& 
     if (v < at.n) to[scan_channel<PAIR>(threadIdx.x & 63, v)] = state[v];
 }
 
-// A wave's steps of one tile: `from` is the first (the last, backwards) of them.
+// A wave's steps of one tile.  Both kernels run through a tile in straight lines: steps that are not there are loads and stores that fail
+// their check, so the next tile's loads are under way while this tile's waves meet and write (behind a branch the compiler
+// waits for them where the branches join).  Only the arithmetic knows whole tiles from others.
 struct ScanTile {
-  int64_t next, from, row;  // where the tile after it starts; first step; its element in the worker's arrays
-  int64_t lo;               // the worker's first step
-  int p, cnt, live;         // worker; steps; those inside the sequence
-  bool full;                // all L steps and all channels
+  int64_t row;          // element of its earliest step in the worker's arrays
+  int next, from, lo;   // where the tile after it starts; first step; the worker's first step
+  int p, cnt, live;     // worker; steps; those inside the sequence
 };
 
 template <class E, int GATE, bool PAIR>
@@ -321,87 +360,80 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
   constexpr int L = 8;
   __shared__ float lds[2][kScanWaves][2][kScanCols];
   const ScanPlace at = scan_place<PAIR>(s, s.segments > 1);
-  const int wave = scan_wave(), lane = threadIdx.x & 63;
-  typedef ScanRaw<E, PAIR> Raw;
-  Raw ra[L], rx[L];
-  auto tile = [&](int64_t t0) {
+  const int wave = scan_wave();
+  const ScanLane off = scan_lane<E, PAIR>(s.n_c - at.c);
+  const uint32_t hop = (uint32_t)(s.n_c * sizeof(E));
+  ScanRaw<E, PAIR> ra[L], rx[L];
+  auto tile = [&](int t0, bool is) {
     ScanTile t;
     const ScanSpan sp = scan_span(s, t0);
     t.p = sp.p;
     t.lo = sp.lo;
     t.next = min(min(at.hi, sp.hi), t0 + kScanWaves * L);
     t.from = t0 + wave * L;
-    t.cnt = (int)max((int64_t)0, min((int64_t)L, t.next - t.from));
-    t.live = (int)max((int64_t)0, min((int64_t)t.cnt, at.len - t.from));
+    t.cnt = is ? max(0, min(L, t.next - t.from)) : 0;
+    t.live = max(0, min(t.cnt, at.len - t.from));
     t.row = ((int64_t)at.b * (sp.hi - sp.lo) + (t.from - sp.lo)) * s.n_c + at.c;
-    t.full = t.live == L && at.all;
-    const ScanWorker& w = scan_worker(s, t.p);
-    const E *pa = (const E*)w.a + t.row, *px = (const E*)w.x + t.row;
-    if (t.full) {
+    const ScanWorker w = scan_worker(s, t.p);
+    const auto pa = scan_rows((const E*)w.a + t.row), px = scan_rows((const E*)w.x + t.row);
 #pragma unroll
-      for (int i = 0; i < L; ++i) {
-        ra[i].load(pa + i * s.n_c, lane, kScanV);
-        rx[i].load(px + i * s.n_c, lane, kScanV);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < L; ++i)
-        if (i < t.live) {
-          ra[i].load(pa + i * s.n_c, lane, at.n);
-          rx[i].load(px + i * s.n_c, lane, at.n);
-        }
+    for (int i = 0; i < L; ++i) {
+      const ScanLane o = off.where(i < t.live);
+      ra[i].load(pa, o, i * hop);
+      rx[i].load(px, o, i * hop);
     }
     return t;
   };
-  ScanTile t = tile(at.lo);
+  ScanTile t = tile(at.lo, true);
   float state[kScanV];
   scan_start<false, PAIR>(s, at, lds[1], state);
   for (int turn = 0;; turn ^= 1) {
     float a[L][kScanV], u[L][kScanV], A[kScanV], B[kScanV], h[kScanV];
 #pragma unroll
-    for (int v = 0; v < kScanV; ++v) {
-      A[v] = 1.f;
-      B[v] = 0.f;
+    for (int i = 0; i < L; ++i) {
+      float g[kScanV], x[kScanV];
+      ra[i].values(g);
+      rx[i].values(x);
+#pragma unroll
+      for (int v = 0; v < kScanV; ++v) {
+        float rest;
+        scan_gate<GATE>(g[v], a[i][v], rest);
+        u[i][v] = rest * x[v];  // (0 where there is no step)
+      }
     }
-#pragma unroll
-    for (int i = 0; i < L; ++i)
-      if (i < t.live) {
-        float g[kScanV], x[kScanV];
-        ra[i].values(g);
-        rx[i].values(x);
-#pragma unroll
-        for (int v = 0; v < kScanV; ++v) {
-          float rest;
-          scan_gate<GATE>(g[v], a[i][v], rest);
-          u[i][v] = rest * x[v];
-          A[v] *= a[i][v];
-          B[v] = fmaf(a[i][v], B[v], u[i][v]);
-        }
-      }
-    const ScanTile now = t;
-    const bool more = now.next < at.hi;
-    if (more) t = tile(now.next);  // its loads are under way while this tile's waves meet and write
-    scan_meet(lds[turn], A, B, state, h);
-    E* const po = (E*)scan_worker(s, now.p).o0 + now.row;
-    if (now.full) {
-#pragma unroll
-      for (int i = 0; i < L; ++i) {
-#pragma unroll
-        for (int v = 0; v < kScanV; ++v) h[v] = fmaf(a[i][v], h[v], u[i][v]);
-        scan_put<PAIR>(po + i * s.n_c, lane, h, kScanV);
-      }
-    } else {
-      const float none[kScanV] = {};
+    if (t.live < L) {
 #pragma unroll
       for (int i = 0; i < L; ++i)
-        if (i < now.live) {
 #pragma unroll
-          for (int v = 0; v < kScanV; ++v) h[v] = fmaf(a[i][v], h[v], u[i][v]);
-          scan_put<PAIR>(po + i * s.n_c, lane, h, at.n);
-        } else if (i < now.cnt) {
-          scan_put<PAIR>(po + i * s.n_c, lane, none, at.n);
-        }
+        for (int v = 0; v < kScanV; ++v) a[i][v] = i < t.live ? a[i][v] : 1.f;
     }
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) {
+      A[v] = a[0][v];
+      B[v] = u[0][v];
+#pragma unroll
+      for (int i = 1; i < L; ++i) {
+        A[v] *= a[i][v];
+        B[v] = fmaf(a[i][v], B[v], u[i][v]);
+      }
+    }
+    const ScanTile now = t;
+    const bool more = now.next < at.hi;
+    t = tile(more ? now.next : now.next - 1, more);
+    scan_meet(lds[turn], A, B, state, h);
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int v = 0; v < kScanV; ++v) u[i][v] = h[v] = fmaf(a[i][v], h[v], u[i][v]);
+    if (now.live < L) {
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+#pragma unroll
+        for (int v = 0; v < kScanV; ++v) u[i][v] = i < now.live ? u[i][v] : 0.f;
+    }
+    const auto po = scan_rows((E*)scan_worker(s, now.p).o0 + now.row);
+#pragma unroll
+    for (int i = 0; i < L; ++i) scan_put<E, PAIR>(po, off.where(i < now.cnt), i * hop, u[i]);
     if (!more) break;
   }
   if (at.hi == s.T) scan_finish<PAIR>(s, at, state);
@@ -415,86 +447,95 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
   __shared__ float lds[2][kScanWaves][2][kScanCols];
   const ScanPlace at = scan_place<PAIR>(s, s.segments == 1);
   const int wave = scan_wave(), lane = threadIdx.x & 63;
-  typedef ScanRaw<E, PAIR> Raw;
-  Raw ra[L], rx[L], rd[L], rh[L];
-  float first[kScanV] = {};  // the state in front of step 0, in 32 bits
-  auto tile = [&](int64_t t1) {
+  const ScanLane off = scan_lane<E, PAIR>(s.n_c - at.c);
+  const uint32_t hop = (uint32_t)(s.n_c * sizeof(E));
+  ScanRaw<E, PAIR> ra[L], rx[L], rd[L], rh[L], edge;  // edge: the state before a worker's first step, the last one of the worker before
+  auto tile = [&](int t1, bool is) {
     ScanTile t;
     const ScanSpan sp = scan_span(s, t1 - 1);
     t.p = sp.p;
     t.lo = sp.lo;
     t.next = max(max(at.lo, sp.lo), t1 - kScanWaves * L);
     t.from = t1 - 1 - wave * L;  // step i: from - i
-    t.cnt = (int)max((int64_t)0, min((int64_t)L, t.from + 1 - t.next));
-    t.live = t.cnt - (int)max((int64_t)0, min((int64_t)t.cnt, t.from + 1 - at.len));  // (steps behind the sequence's end come first)
-    t.row = ((int64_t)at.b * (sp.hi - sp.lo) + (t.from - sp.lo)) * s.n_c + at.c;
-    t.full = t.live == L && at.all && t.from - L + 1 > sp.lo;  // and the state before each step is this worker's
-    const ScanWorker& w = scan_worker(s, t.p);
-    const E *pa = (const E*)w.a + t.row, *px = X ? (const E*)w.x + t.row : nullptr, *ph = (const E*)w.h + t.row - s.n_c, *pd = (const E*)w.dh + t.row;
-    if (t.full) {
+    t.cnt = is ? max(0, min(L, t.from + 1 - t.next)) : 0;
+    t.live = t.cnt - max(0, min(t.cnt, t.from + 1 - at.len));  // (steps behind the sequence's end come first)
+    t.row = ((int64_t)at.b * (sp.hi - sp.lo) + (t.from - t.cnt + 1 - sp.lo)) * s.n_c + at.c;
+    const ScanWorker w = scan_worker(s, t.p);
+    const auto pa = scan_rows((const E*)w.a + t.row), pd = scan_rows((const E*)w.dh + t.row), ph = scan_rows((const E*)w.h + t.row - s.n_c);
+    const auto px = scan_rows((const E*)(X ? w.x : w.a) + t.row);
 #pragma unroll
-      for (int i = 0; i < L; ++i) {
-        ra[i].load(pa - i * s.n_c, lane, kScanV);
-        rd[i].load(pd - i * s.n_c, lane, kScanV);
-        rh[i].load(ph - i * s.n_c, lane, kScanV);
-        if (X) rx[i].load(px - i * s.n_c, lane, kScanV);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < L; ++i)
-        if (i >= t.cnt - t.live && i < t.cnt) {
-          ra[i].load(pa - i * s.n_c, lane, at.n);
-          rd[i].load(pd - i * s.n_c, lane, at.n);
-          if (X) rx[i].load(px - i * s.n_c, lane, at.n);
-          const int64_t step = t.from - i;
-          if (step > t.lo) {
-            rh[i].load(ph - i * s.n_c, lane, at.n);
-          } else if (step > 0) {  // the last state of the worker before
-            const ScanSpan b = scan_span(s, step - 1);
-            rh[i].load((const E*)scan_worker(s, b.p).h + ((int64_t)at.b * (b.hi - b.lo) + (b.hi - b.lo - 1)) * s.n_c + at.c, lane, at.n);
-          } else {
-#pragma unroll
-            for (int v = 0; v < kScanV; ++v) first[v] = s.h0 && v < at.n ? s.h0[at.b * s.n_c + at.c + scan_channel<PAIR>(lane, v)] : 0.f;
-          }
-        }
+    for (int i = 0; i < L; ++i) {
+      const bool in = i >= t.cnt - t.live && i < t.cnt;
+      const ScanLane o = off.where(in);
+      const uint32_t step = in ? (t.cnt - 1 - i) * hop : 0;
+      ra[i].load(pa, o, step);
+      rd[i].load(pd, o, step);
+      if (X) rx[i].load(px, o, step);
+      rh[i].load(ph, off.where(in && t.from - i > t.lo), step);
     }
+    const bool first = t.live > 0 && t.from - t.cnt + 1 == t.lo && t.lo > 0;
+    const ScanSpan b = scan_span(s, first ? t.lo - 1 : 0);
+    edge.load(scan_rows((const E*)scan_worker(s, b.p).h + ((int64_t)at.b * (b.hi - b.lo) + (b.hi - b.lo - 1)) * s.n_c + at.c), off.where(first), 0);
     return t;
   };
-  ScanTile t = tile(at.hi);
+  float start[kScanV];  // the state in front of step 0, in 32 bits
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v) start[v] = s.h0 && v < at.n ? s.h0[at.b * s.n_c + at.c + scan_channel<PAIR>(lane, v)] : 0.f;
+  ScanTile t = tile(at.hi, true);
   float state[kScanV];
   scan_start<true, PAIR>(s, at, lds[1], state);
   for (int turn = 0;; turn ^= 1) {
     // dx = d rest, da = d slope
     float a[L][kScanV], d[L][kScanV], rest[L][kScanV], slope[L][kScanV], A[kScanV], B[kScanV], back[kScanV];
+    float last[kScanV];
+    edge.values(last);
 #pragma unroll
-    for (int v = 0; v < kScanV; ++v) {
-      A[v] = 1.f;
-      B[v] = 0.f;
+    for (int v = 0; v < kScanV; ++v) last[v] = t.lo == 0 ? start[v] : last[v];
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      float g[kScanV], x[kScanV] = {}, before[kScanV];
+      ra[i].values(g);
+      rd[i].values(d[i]);
+      if (X) rx[i].values(x);
+      rh[i].values(before);
+#pragma unroll
+      for (int v = 0; v < kScanV; ++v) {
+        if (t.from - i == t.lo) before[v] = last[v];
+        scan_gate<GATE>(g[v], a[i][v], rest[i][v]);
+        slope[i][v] = X ? (before[v] - x[v]) * (a[i][v] * rest[i][v]) : before[v];
+      }
     }
+    if (t.live < L) {
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-      if (i >= t.cnt - t.live && i < t.cnt) {
-        float g[kScanV], x[kScanV] = {}, before[kScanV];
-        ra[i].values(g);
-        rd[i].values(d[i]);
-        if (X) rx[i].values(x);
-        rh[i].values(before);
+      for (int i = 0; i < L; ++i) {
+        const bool in = i >= t.cnt - t.live && i < t.cnt;
 #pragma unroll
         for (int v = 0; v < kScanV; ++v) {
-          if (t.from - i == 0) before[v] = first[v];
-          scan_gate<GATE>(g[v], a[i][v], rest[i][v]);
-          slope[i][v] = X ? (before[v] - x[v]) * (a[i][v] * rest[i][v]) : before[v];
-          A[v] *= a[i][v];
-          B[v] = a[i][v] * (B[v] + d[i][v]);
+          a[i][v] = in ? a[i][v] : 1.f;  // (d is 0 there)
+          rest[i][v] = in ? rest[i][v] : 0.f;
+          slope[i][v] = in ? slope[i][v] : 0.f;
         }
       }
+    }
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) {
+      A[v] = a[0][v];
+      B[v] = a[0][v] * d[0][v];
+#pragma unroll
+      for (int i = 1; i < L; ++i) {
+        A[v] *= a[i][v];
+        B[v] = a[i][v] * (B[v] + d[i][v]);
+      }
+    }
     const ScanTile now = t;
     const bool more = now.next > at.lo;
-    if (more) t = tile(now.next);
+    t = tile(more ? now.next : now.next + 1, more);
     scan_meet(lds[turn], A, B, state, back);
-    const ScanWorker& w = scan_worker(s, now.p);
-    E *const o0 = (E*)w.o0 + now.row, *const o1 = (E*)w.o1 + now.row;
-    auto gradient = [&](int i, float* da, float* dx) {
+    const ScanWorker w = scan_worker(s, now.p);
+    const auto o0 = scan_rows((E*)w.o0 + now.row), o1 = scan_rows((E*)w.o1 + now.row);
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      float da[kScanV], dx[kScanV];
 #pragma unroll
       for (int v = 0; v < kScanV; ++v) {
         const float all = d[i][v] + back[v];
@@ -502,24 +543,10 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
         da[v] = all * slope[i][v];
         dx[v] = all * rest[i][v];
       }
-    };
-    if (now.full) {
-#pragma unroll
-      for (int i = 0; i < L; ++i) {
-        float da[kScanV], dx[kScanV];
-        gradient(i, da, dx);
-        scan_put<PAIR>(o0 - i * s.n_c, lane, da, kScanV);
-        scan_put<PAIR>(o1 - i * s.n_c, lane, dx, kScanV);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < L; ++i)
-        if (i < now.cnt) {
-          float da[kScanV] = {}, dx[kScanV] = {};
-          if (i >= now.cnt - now.live) gradient(i, da, dx);
-          scan_put<PAIR>(o0 - i * s.n_c, lane, da, at.n);
-          scan_put<PAIR>(o1 - i * s.n_c, lane, dx, at.n);
-        }
+      const ScanLane o = off.where(i < now.cnt);
+      const uint32_t step = i < now.cnt ? (now.cnt - 1 - i) * hop : 0;
+      scan_put<E, PAIR>(o0, o, step, da);
+      scan_put<E, PAIR>(o1, o, step, dx);
     }
     if (!more) break;
   }
@@ -580,15 +607,15 @@ static int scan_check(const void* v, size_t size, const char* what, int j) {
 
 static int scan_args(distdl_scan_plan* p, const std::vector<ScanWorker>& w, hipStream_t st, ScanArgs* s) {
   s->more = nullptr;
-  s->T = p->T;
+  s->T = (int32_t)p->T;
   s->n_c = p->n_c;
-  s->part = p->T / p->P;
-  s->extra = p->T % p->P;
+  s->part = (int32_t)(p->T / p->P);
+  s->extra = (int32_t)(p->T % p->P);
   s->P = p->P;
   s->n_b = (int32_t)p->n_b;
   s->groups = p->groups;
   s->segments = p->segments;
-  s->seg_steps = p->seg_steps;
+  s->seg_steps = (int32_t)p->seg_steps;
   int rc = DISTDL_OK;
   if (p->P <= kScanInline) {
     std::copy(w.begin(), w.end(), s->w);
@@ -646,7 +673,8 @@ int distdl_scan_plan_create(distdl_scan_plan** out, int64_t n_b, int64_t T, int6
   if (dtype != DISTDL_F32 && dtype != DISTDL_BF16) return set_error(DISTDL_ERR_UNSUPPORTED, "unknown dtype");
   if (T < P) return set_error(DISTDL_ERR_EMPTY_PARTITION, "scan: %lld steps over %d workers", (long long)T, P);
   const int64_t groups = (n_c + kScanCols - 1) / kScanCols;
-  if (T >= int64_t(1) << 31 || n_c >= int64_t(1) << 30 || n_b >= int64_t(1) << 22 || groups * n_b >= int64_t(1) << 22)
+  if (T >= int64_t(1) << 30 || n_c >= int64_t(1) << 25 ||  // (a tile of one wave is addressed in 31 bits)
+       n_b >= int64_t(1) << 22 || groups * n_b >= int64_t(1) << 22)
     return set_error(DISTDL_ERR_UNSUPPORTED, "scan: problem too large");
   return guarded([&]() -> int {
     std::unique_ptr<distdl_scan_plan> p(new distdl_scan_plan());
