@@ -282,7 +282,6 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
     B[v] = 0.f;
   }
   auto compose = [&](const Raw* ar, const Raw* xr, int cnt) {
-    float a[L][kScanV], u[L][kScanV];
 #pragma unroll
     for (int i = 0; i < L; ++i) {
       float g[kScanV], x[kScanV];
@@ -290,24 +289,13 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
       xr[i].values(x);
 #pragma unroll
       for (int v = 0; v < kScanV; ++v) {
-        float rest;
-        scan_gate<GATE>(g[v], a[i][v], rest);
-        u[i][v] = BACK ? x[v] : rest * x[v];
+        float a, rest;
+        scan_gate<GATE>(g[v], a, rest);
+        a = i < cnt ? a : 1.f;  // (and x is 0)
+        A[v] *= a;
+        B[v] = BACK ? a * (B[v] + x[v]) : fmaf(a, B[v], rest * x[v]);
       }
     }
-    if (cnt < L) {
-#pragma unroll
-      for (int i = 0; i < L; ++i)
-#pragma unroll
-        for (int v = 0; v < kScanV; ++v) a[i][v] = i < cnt ? a[i][v] : 1.f;  // (and u is 0)
-    }
-#pragma unroll
-    for (int i = 0; i < L; ++i)
-#pragma unroll
-      for (int v = 0; v < kScanV; ++v) {
-        A[v] *= a[i][v];
-        B[v] = BACK ? a[i][v] * (B[v] + u[i][v]) : fmaf(a[i][v], B[v], u[i][v]);
-      }
   };
   int done = 0, c0 = load(0, ra[0], rx[0]);
   while (c0 > 0) {
