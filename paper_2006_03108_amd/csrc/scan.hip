@@ -146,16 +146,17 @@ __device__ __forceinline__ void scan_put(__amdgpu_buffer_rsrc_t r, const ScanLan
   }
 }
 
-// a and 1 - a.  Through exp(-|g|), which neither overflows nor loses 1 - a where a is near one.
+// a = 1 / (1 + e) and 1 - a = e / (1 + e) with e = exp(-g), which keeps 1 - a where a is near one.  e is held below 2^126, so that no
+// infinity meets a zero; the minimum is the one that keeps NaNs.
 template <int GATE>
 __device__ __forceinline__ void scan_gate(float g, float& a, float& rest) {
   if constexpr (GATE == DISTDL_GATE_GIVEN) {
     a = g;
     rest = 1.f;
   } else {
-    const float e = __expf(-fabsf(g)), r = __builtin_amdgcn_rcpf(1.f + e);
-    a = g >= 0.f ? r : e * r;
-    rest = g >= 0.f ? e * r : r;
+    const float e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(g * -1.4426950408889634f, 126.f));
+    a = __builtin_amdgcn_rcpf(1.f + e);
+    rest = e * a;
   }
 }
 
@@ -282,8 +283,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
     B[v] = 0.f;
   }
   auto compose = [&](const Raw* ar, const Raw* xr, int cnt) {
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
+    auto one = [&](int i, bool in) {
       float g[kScanV], x[kScanV];
       ar[i].values(g);
       xr[i].values(x);
@@ -291,10 +291,17 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
       for (int v = 0; v < kScanV; ++v) {
         float a, rest;
         scan_gate<GATE>(g[v], a, rest);
-        a = i < cnt ? a : 1.f;  // (and x is 0)
+        a = in ? a : 1.f;  // (and x is 0)
         A[v] *= a;
         B[v] = BACK ? a * (B[v] + x[v]) : fmaf(a, B[v], rest * x[v]);
       }
+    };
+    if (cnt == L) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) one(i, true);
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i) one(i, i < cnt);
     }
   };
   int done = 0, c0 = load(0, ra[0], rx[0]);
