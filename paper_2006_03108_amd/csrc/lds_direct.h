@@ -36,6 +36,17 @@ __device__ inline void load_to_lds(lds_u32x4 desc, uint32_t lds_addr, uint32_t v
                : "s"(lds_addr), "v"(voff), "s"(desc), "s"(soff)
                : "memory");
 }
+// The same for one byte per lane: it lands in the word at lds_addr + 4 L, zero-extended; an out-of-range lane writes zero.
+__device__ inline void load_byte_to_lds(lds_u32x4 desc, uint32_t lds_addr, uint32_t voff, uint32_t soff) {
+  lds_addr = __builtin_amdgcn_readfirstlane(lds_addr);
+  soff = __builtin_amdgcn_readfirstlane(soff);
+  desc = lds_u32x4{(uint32_t)__builtin_amdgcn_readfirstlane(desc[0]), (uint32_t)__builtin_amdgcn_readfirstlane(desc[1]),
+                   (uint32_t)__builtin_amdgcn_readfirstlane(desc[2]), (uint32_t)__builtin_amdgcn_readfirstlane(desc[3])};
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_ubyte %1, %2, %3 offen lds"
+               :
+               : "s"(lds_addr), "v"(voff), "s"(desc), "s"(soff)
+               : "memory");
+}
 __device__ inline uint32_t lds_address(const void* p) { return (uint32_t)(size_t)(lds_char_ptr)p; }
 
 // Workgroup barrier without the fences of __syncthreads(): those make the compiler wait for every outstanding

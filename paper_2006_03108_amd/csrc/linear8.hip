@@ -8,9 +8,12 @@
 // blocks start anew.  Codes times scales are exact in bf16 (one instruction for two), so bf16 matrix instructions
 // add exact products in fp32; measured, sums of 128 to 8192 products of N(0, 1) operands are 1e-8 to 3e-7 of their size off.
 #include <algorithm>
+#include <cstddef>
 
 #include "block8.h"
+#include "buffer.h"
 #include "common.h"
+#include "lds_direct.h"
 #include "profile.h"
 
 namespace distdl {
@@ -26,6 +29,7 @@ struct ProdOut {
   uint32_t tiles_m;     // workgroups along m
   int32_t seg0, segs;
 };
+static_assert(sizeof(ProdOut) == 32 && sizeof(ProdSeg) == 40, "read from the launch's arguments as they lie there");
 constexpr int kProdInline = 16;  // results and segments that travel with the launch; more are in a table
 struct ProdArgs {
   ProdOut out[kProdInline];
@@ -35,6 +39,7 @@ struct ProdArgs {
   int32_t n_out;
 };
 
+typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
@@ -52,6 +57,26 @@ __device__ __forceinline__ v8bf codes_to_bf16(uint32_t lo, uint32_t hi, float sc
   return u.v;
 }
 
+// A result and a worker's part of a sum, from the table or from the launch's own arguments, into scalar registers.
+typedef const __attribute__((address_space(4))) ProdOut* ProdOutPtr;
+typedef const __attribute__((address_space(4))) ProdSeg* ProdSegPtr;
+__device__ __forceinline__ ProdOut prod_out(const ProdArgs& a, int o) {
+  static_assert(offsetof(ProdArgs, out) == 0, "the kernels' first argument starts with the results");
+  const ProdOutPtr p = (a.more_out ? (ProdOutPtr)(uint64_t)a.more_out : (ProdOutPtr)__builtin_amdgcn_kernarg_segment_ptr()) + o;
+  return ProdOut{p->c, p->m, p->n, p->tile0, p->tiles_m, p->seg0, p->segs};
+}
+__device__ __forceinline__ ProdSeg prod_seg(const ProdArgs& a, int i) {
+  const ProdSegPtr p = (a.more_seg ? (ProdSegPtr)(uint64_t)a.more_seg
+                                   : (ProdSegPtr)((const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(ProdArgs, seg))) + i;
+  return ProdSeg{p->a, p->as, p->b, p->bs, p->k};
+}
+// The result that workgroup `block` belongs to
+__device__ __forceinline__ ProdOut prod_of(const ProdArgs& a, uint32_t block) {
+  int o = 0;
+  while (o + 1 < a.n_out && block >= prod_out(a, o + 1).tile0) ++o;
+  return prod_out(a, o);
+}
+
 // 16 codes, those from n on zero
 __device__ __forceinline__ u32x4 load16_codes(const uint8_t* p, int64_t n) {
   if (n >= 16) return *(const u32x4_any*)p;
@@ -62,21 +87,43 @@ __device__ __forceinline__ u32x4 load16_codes(const uint8_t* p, int64_t n) {
   return c;
 }
 
+// Four consecutive results of a row
+__device__ __forceinline__ void prod_store(float* c, int m, int n, int cols, v4f v) {
+  float* const to = c + (int64_t)m * cols + n;
+  typedef v4f v4f_any __attribute__((aligned(4)));
+  if (n + 3 < cols) {
+    *(v4f_any*)to = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (n + e < cols) to[e] = v[e];
+  }
+}
+__device__ __forceinline__ void prod_store(uint16_t* c, int m, int n, int cols, v4f v) {
+  uint16_t* const to = c + (int64_t)m * cols + n;
+  typedef u32x2 u32x2_two __attribute__((aligned(2)));
+  if (n + 3 < cols) {
+    *(u32x2_two*)to = u32x2{to_bf16(v[0], v[1]), to_bf16(v[2], v[3])};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (n + e < cols) to[e] = to_bf16(v[e]);
+  }
+}
+
 // Any sizes, strides of rows and alignment: 128 x 128 results a workgroup, 64 x 64 a wave, 128 k at a time through LDS.  The 16-byte
 // piece p of row r lies at piece p ^ (r & 7), so that the eight rows that lanes read together lie in different banks.
 template <class C, bool B_TILES>
 __global__ __launch_bounds__(256) void prod8_any_kernel(ProdArgs args) {
   __shared__ u32x4 lds[2][kBlock8][8];
-  int o = 0;
-  while (o + 1 < args.n_out && blockIdx.x >= (args.more_out ? args.more_out[o + 1].tile0 : args.out[o + 1].tile0)) ++o;
-  const ProdOut out = args.more_out ? args.more_out[o] : args.out[o];
+  const ProdOut out = prod_of(args, blockIdx.x);
   const uint32_t tile = blockIdx.x - out.tile0;
   const int m0 = (int)(tile % out.tiles_m) * 128, n0 = (int)(tile / out.tiles_m) * 128;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64, r16 = lane & 15, g = lane >> 4;
   v4f acc[4][4] = {};  // [n][m]: B's rows are the matrix instruction's rows, so that a lane holds four consecutive n of one m
   for (int sg = 0; sg < out.segs; ++sg) {
-    const ProdSeg seg = args.more_seg ? args.more_seg[out.seg0 + sg] : args.seg[out.seg0 + sg];
+    const ProdSeg seg = prod_seg(args, out.seg0 + sg);
     const int64_t blocks = (seg.k + kBlock8 - 1) / kBlock8;
     for (int64_t kb = 0; kb < blocks; ++kb) {
       u32x4 ra[4], rb[4];
@@ -132,13 +179,162 @@ __global__ __launch_bounds__(256) void prod8_any_kernel(ProdArgs args) {
     const int m = m0 + wm + i * 16 + r16;
     if (m >= out.m) continue;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int n = n0 + wn + j * 16 + g * 4;
-      C* const to = (C*)out.c + (int64_t)m * out.n + n;
+    for (int j = 0; j < 4; ++j) prod_store((C*)out.c, m, n0 + wn + j * 16 + g * 4, out.n, acc[j][i]);
+  }
+}
+
+// ---- rows of whole 16-byte pieces -------------------------------------------
+// TM x TN results a workgroup of WM x WN waves, 128 k a stage, ST stages in LDS.  Stages are filled by loads that go straight to LDS (no
+// registers, no instructions to store them) while earlier ones are multiplied; a stage costs one barrier.  A wave's load brings eight
+// rows of 128 bytes: lane L asks for piece (L & 7) ^ (L >> 3) of row L >> 3, so that row r's piece p lies at p ^ (r & 7) and the lanes
+// that read together find different banks.  Rows and pieces that are not there fail the check of their buffer and arrive as zeros.
+// The scales of the stage's rows come the same way, a byte to a word of LDS.
+// FP8: the codes' own matrix instruction, else bf16 ones on codes that are converted as they leave LDS.
+template <class C, bool B_TILES, bool FP8, int TM, int TN, int WM, int WN, int ST>
+__global__ __launch_bounds__(64 * WM * WN) void prod8_tile_kernel(ProdArgs args) {
+  constexpr int NW = WM * WN, MI = TM / WM / 16, NI = TN / WN / 16;
+  constexpr int kData = (TM + TN) * 128, kStage = kData + (TM + TN) * 4;
+  constexpr int kLoads = (TM + TN) / 8 / NW;                                            // a wave's loads of codes for a stage
+  constexpr int kScales = ((TM + TN) / 64 + NW - 1) / NW;                               // and of scales (some twice, where waves are many)
+  static_assert((TM + TN) / 8 % NW == 0 && TM % 64 == 0 && TN % 64 == 0, "whole loads");
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const uint32_t block = xcd_order(blockIdx.x, gridDim.x);
+  const ProdOut out = prod_of(args, block);
+  const uint32_t tile = block - out.tile0, tiles_n = ((uint32_t)out.n + TN - 1) / TN;
+  // eight rows of tiles are walked column by column: what an XCD works on at a time shares its operands in that XCD's L2
+  const uint32_t band = tile / (8 * tiles_n), in_band = tile - band * 8 * tiles_n, high = min(8u, out.tiles_m - band * 8);
+  const int m0 = (int)((band * 8 + in_band % high) * TM), n0 = (int)(in_band / high * TN);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave % WM * (TM / WM), wn = wave / WM * (TN / WN), r16 = lane & 15, g = lane >> 4;
+  const uint32_t lds0 = lds_address(lds);
+
+  // loads: which rows this lane asks for
+  const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+  int seg_i = 0;                       // the segment and its block that are loaded next
+  int kb_i = 0, blocks_i = 0, rest_i = 0;
+  lds_u32x4 ra, rb, rsa, rsb;
+  uint32_t voff[kLoads], soff_s[kScales], hop[kScales];
+  auto open = [&]() {                  // the buffers and offsets of segment seg_i
+    const ProdSeg seg = prod_seg(args, out.seg0 + seg_i);
+    const uint32_t k = (uint32_t)seg.k;
+    blocks_i = (int)((k + 127) / 128);
+    rest_i = (int)(k - (blocks_i - 1) * 128);
+    kb_i = 0;
+    ra = lds_direct_rsrc(seg.a + (int64_t)m0 * k, (uint32_t)min((int64_t)0x7fffffe0, (int64_t)(out.m - m0) * k));
+    rb = lds_direct_rsrc(seg.b + (int64_t)n0 * k, (uint32_t)min((int64_t)0x7fffffe0, (int64_t)(out.n - n0) * k));
+    rsa = lds_direct_rsrc(seg.as, (uint32_t)((int64_t)blocks_i * out.m));
+    rsb = lds_direct_rsrc(seg.bs, (uint32_t)((int64_t)blocks_i * (B_TILES ? (out.n + 127) >> 7 : out.n)));
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (n + e < out.n) st(to, e, acc[j][i][e]);
+    for (int i = 0; i < kLoads; ++i) {
+      const int l = wave * kLoads + i, row = l * 8 + (lane >> 3);
+      const bool is_a = l * 8 < TM;
+      const int r = is_a ? row : row - TM;
+      voff[i] = r < (is_a ? out.m - m0 : out.n - n0) ? (uint32_t)r * k + piece : kOob;
     }
+#pragma unroll
+    for (int i = 0; i < kScales; ++i) {
+      const int l = (wave * kScales + i) % ((TM + TN) / 64);
+      const bool is_a = l * 64 < TM;
+      const int r = is_a ? m0 + l * 64 + lane : n0 + l * 64 - TM + lane;
+      if (is_a) soff_s[i] = r < out.m ? r : kOob;
+      else soff_s[i] = r < out.n ? (B_TILES ? (uint32_t)(r >> 7) * blocks_i : r) : kOob;
+      hop[i] = is_a ? out.m : B_TILES ? 1 : out.n;
+    }
+  };
+  auto load = [&](int buffer) {        // the next block to `buffer`, if there is one
+    if (kb_i == blocks_i) {
+      ++seg_i;
+      open();
+    }
+    const bool last = kb_i == blocks_i - 1;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int l = wave * kLoads + i;
+      load_to_lds(l * 8 < TM ? ra : rb, lds0 + buffer * kStage + l * 1024, last && piece >= rest_i ? kOob : voff[i], kb_i * 128);
+    }
+#pragma unroll
+    for (int i = 0; i < kScales; ++i) {
+      const int l = (wave * kScales + i) % ((TM + TN) / 64);
+      load_byte_to_lds(l * 64 < TM ? rsa : rsb, lds0 + buffer * kStage + kData + l * 256, soff_s[i], kb_i * hop[i]);
+    }
+    ++kb_i;
+  };
+  int total = 0;
+  for (int i = 0; i < out.segs; ++i) total += (int)((prod_seg(args, out.seg0 + i).k + 127) / 128);
+
+  v4f acc[NI][MI] = {};  // B's rows are the matrix instruction's rows, so that a lane holds four consecutive n of one m
+  open();
+#pragma unroll
+  for (int i = 0; i < ST - 1; ++i)
+    if (i < total) load(i);
+  int buffer = 0;
+  for (int s = 0; s < total; ++s) {
+    if (total - 1 - s >= ST - 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((ST - 2) * (kLoads + kScales)) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds_barrier();  // this stage is there for all waves, and all have read the one before it
+    if (s + ST - 1 < total) load(buffer == 0 ? ST - 1 : buffer - 1);
+    const char* const at = lds + buffer * kStage;
+    const char* const at_a = at + (wm + r16) * 128;
+    const char* const at_b = at + (TM + wn + r16) * 128;
+    const int p0 = (g ^ (r16 & 7)) * 16, p1 = ((g + 4) ^ (r16 & 7)) * 16;
+    int sa[MI], sb[NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) sa[i] = *(const uint8_t*)(at + kData + (wm + i * 16 + r16) * 4);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) sb[j] = *(const uint8_t*)(at + kData + (TM + wn + j * 16 + r16) * 4);
+    if constexpr (FP8) {
+      auto both = [&](const char* p) {
+        const u32x4 lo = *(const u32x4*)(p + p0), hi = *(const u32x4*)(p + p1);
+        v8i f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f[i] = (int)lo[i];
+          f[i + 4] = (int)hi[i];
+        }
+        return f;
+      };
+      v8i fa[MI];
+#pragma unroll
+      for (int i = 0; i < MI; ++i) fa[i] = both(at_a + i * 2048);
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        const v8i fb = both(at_b + j * 2048);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+          acc[j][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, fa[i], acc[j][i], 0, 0, 0, sb[j], 0, sa[i]);
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        v8bf fa[MI][2];
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+          const u32x4 c = *(const u32x4*)(at_a + i * 2048 + (p ? p1 : p0));
+          const float f = scale_value(sa[i]);
+          fa[i][0] = codes_to_bf16(c[0], c[1], f);
+          fa[i][1] = codes_to_bf16(c[2], c[3], f);
+        }
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          const u32x4 c = *(const u32x4*)(at_b + j * 2048 + (p ? p1 : p0));
+          const float f = scale_value(sb[j]);
+          const v8bf b0 = codes_to_bf16(c[0], c[1], f), b1 = codes_to_bf16(c[2], c[3], f);
+#pragma unroll
+          for (int i = 0; i < MI; ++i) {
+            acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b0, fa[i][0], acc[j][i], 0, 0, 0);
+            acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b1, fa[i][1], acc[j][i], 0, 0, 0);
+          }
+        }
+      }
+    }
+    buffer = buffer == ST - 1 ? 0 : buffer + 1;
+  }
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int m = m0 + wm + i * 16 + r16;
+    if (m >= out.m) continue;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) prod_store((C*)out.c, m, n0 + wn + j * 16 + g * 4, out.n, acc[j][i]);
   }
 }
 
@@ -161,16 +357,47 @@ static int prod_check(const void* v, size_t size, const char* what, int j) {
   return DISTDL_OK;
 }
 
-static int launch_prod(distdl_linear8_plan* p, std::vector<ProdOut>& outs, const std::vector<ProdSeg>& segs, bool f32, bool b_tiles,
-                       const char* name, hipStream_t st) {
+// Tiles of TM x TN over all results: their first workgroups.  Returns the number of workgroups.
+static int64_t prod_tiles(std::vector<ProdOut>& outs, int TM, int TN) {
   int64_t tiles = 0;
   for (ProdOut& o : outs) {
-    o.tile0 = (uint32_t)tiles;
-    o.tiles_m = (uint32_t)((o.m + 127) / 128);
-    tiles += (int64_t)o.tiles_m * ((o.n + 127) / 128);
+    o.tile0 = (uint32_t)std::min<int64_t>(tiles, UINT32_MAX);
+    o.tiles_m = (uint32_t)((o.m + TM - 1) / TM);
+    tiles += (int64_t)o.tiles_m * ((o.n + TN - 1) / TN);
   }
-  if (tiles >= kMaxBlocks256) return set_error(DISTDL_ERR_UNSUPPORTED, "linear8: problem too large");
-  ProdArgs args;
+  return tiles;
+}
+
+// Whether rows are whole 16-byte pieces and all offsets within a tile fit 31 bits.
+static bool prod_pieces(const std::vector<ProdOut>& outs, const std::vector<ProdSeg>& segs) {
+  int64_t most = 0;
+  for (const ProdOut& o : outs) most = std::max<int64_t>(most, std::max(o.m, o.n));
+  for (const ProdSeg& g : segs)
+    if (((uintptr_t)g.a | (uintptr_t)g.b) % 16 || g.k % 16 || g.k > 1 << 22 || most * (g.k / 128 + 1) >= kOob) return false;
+  return true;
+}
+
+template <class C, bool B_TILES, bool FP8, int TM, int TN, int WM, int WN, int ST>
+static int launch_prod_tile(const ProdArgs& args, int64_t tiles, hipStream_t st) {
+  constexpr int bytes = ST * ((TM + TN) * 132);
+  static_assert(bytes <= 160 * 1024, "LDS of a compute unit");
+  const int rc = allow_large_lds<prod8_tile_kernel<C, B_TILES, FP8, TM, TN, WM, WN, ST>>();
+  if (rc) return rc;
+  hipLaunchKernelGGL((prod8_tile_kernel<C, B_TILES, FP8, TM, TN, WM, WN, ST>), dim3((unsigned)tiles), dim3(64 * WM * WN), bytes, st, args);
+  return DISTDL_OK;
+}
+
+template <class C, bool B_TILES>
+static int launch_prod_as(ProdArgs& args, std::vector<ProdOut>& outs, const std::vector<ProdSeg>& segs, distdl_linear8_plan* p, hipStream_t st) {
+  enum { kAny, kSmall, kLarge } kind = kAny;
+  int64_t tiles = 0;
+  if (prod_pieces(outs, segs)) {
+    // Large tiles need less of their operands from L2, and enough of them to keep the compute units busy.
+    tiles = prod_tiles(outs, 256, sizeof(C) == 2 ? 256 : 128);
+    kind = tiles >= 160 ? kLarge : kSmall;
+  }
+  if (kind != kLarge) tiles = kind == kSmall ? prod_tiles(outs, 64, 64) : prod_tiles(outs, 128, 128);
+  if (tiles >= kMaxBlocks256 / 2) return set_error(DISTDL_ERR_UNSUPPORTED, "linear8: problem too large");
   args.n_out = (int32_t)outs.size();
   args.more_out = nullptr;
   args.more_seg = nullptr;
@@ -183,17 +410,25 @@ static int launch_prod(distdl_linear8_plan* p, std::vector<ProdOut>& outs, const
     args.more_out = p->outs.dev;
     args.more_seg = p->segs.dev;
   }
+  if (kind == kLarge) {
+    if constexpr (sizeof(C) == 2) return launch_prod_tile<C, B_TILES, true, 256, 256, 2, 4, 2>(args, tiles, st);
+    else return launch_prod_tile<C, B_TILES, false, 256, 128, 4, 2, 3>(args, tiles, st);
+  }
+  if (kind == kSmall) return launch_prod_tile<C, B_TILES, false, 64, 64, 2, 2, 4>(args, tiles, st);
+  hipLaunchKernelGGL((prod8_any_kernel<C, B_TILES>), dim3((unsigned)tiles), dim3(256), 0, st, args);
+  return DISTDL_OK;
+}
+
+static int launch_prod(distdl_linear8_plan* p, std::vector<ProdOut>& outs, const std::vector<ProdSeg>& segs, bool f32, bool b_tiles,
+                       const char* name, hipStream_t st) {
+  ProdArgs args;
+  int rc;
   {
     ProfScope prof(name, st);
-    const dim3 grid((unsigned)tiles), block(256);
-    if (f32) {
-      if (b_tiles) hipLaunchKernelGGL((prod8_any_kernel<float, true>), grid, block, 0, st, args);
-      else hipLaunchKernelGGL((prod8_any_kernel<float, false>), grid, block, 0, st, args);
-    } else {
-      if (b_tiles) hipLaunchKernelGGL((prod8_any_kernel<uint16_t, true>), grid, block, 0, st, args);
-      else hipLaunchKernelGGL((prod8_any_kernel<uint16_t, false>), grid, block, 0, st, args);
-    }
+    if (f32) rc = b_tiles ? launch_prod_as<float, true>(args, outs, segs, p, st) : launch_prod_as<float, false>(args, outs, segs, p, st);
+    else rc = launch_prod_as<uint16_t, true>(args, outs, segs, p, st);
   }
+  if (rc) return rc;
   DISTDL_HIP_TRY(hipGetLastError());
   return DISTDL_OK;
 }
