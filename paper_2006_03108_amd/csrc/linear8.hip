@@ -183,6 +183,82 @@ __global__ __launch_bounds__(256) void prod8_any_kernel(ProdArgs args) {
   }
 }
 
+// Few rows of x (16 MI of them at most): reading the weights is all there is to do, once and as fast as memory gives them.  A workgroup takes 16
+// rows of the weights, its eight waves every eighth block of k; operands go from memory to registers, U blocks of them under way
+// at a time, and the waves' sums meet in LDS.  Rows of any length and alignment.
+template <class C, bool B_TILES, int MI, int U>
+__global__ __launch_bounds__(512) void prod8_rows_kernel(ProdArgs args) {
+  __shared__ v4f meet[8][MI][64];
+  const ProdOut out = prod_of(args, blockIdx.x);
+  const int n0 = (int)(blockIdx.x - out.tile0) * 16;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
+  // (rows that are not there are others' once more: what comes of them is not stored)
+  const int n = min(n0 + r16, out.n - 1);
+  int m[MI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) m[i] = min(i * 16 + r16, out.m - 1);
+  v4f acc[MI] = {};
+  for (int sg = 0; sg < out.segs; ++sg) {
+    const ProdSeg seg = prod_seg(args, out.seg0 + sg);
+    const int k = (int)seg.k, blocks = (k + 127) / 128;
+    const uint8_t *const b = seg.b + (int64_t)n * k + g * 16, *const bs = B_TILES ? seg.bs + (int64_t)(n >> 7) * blocks : seg.bs + n;
+    const uint8_t *a[MI], *as[MI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      a[i] = seg.a + (int64_t)m[i] * k + g * 16;
+      as[i] = seg.as + m[i];
+    }
+    for (int kb = wave; kb < blocks; kb += 8 * U) {
+      u32x4 fb[U][2], fa[U][MI][2];
+      int sb[U], sa[U][MI];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int at = kb + 8 * u;
+        if (at < blocks) {
+          auto piece = [&](const uint8_t* row, int p) {
+            const int64_t o = (int64_t)at * 128 + p * 64;
+            if (at < blocks - 1) return (u32x4) * (const u32x4_any*)(row + o);
+            return load16_codes(row + o, k - o - g * 16);
+          };
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            fb[u][p] = piece(b, p);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) fa[u][i][p] = piece(a[i], p);
+          }
+          sb[u] = bs[B_TILES ? (int64_t)at : (int64_t)at * out.n];
+#pragma unroll
+          for (int i = 0; i < MI; ++i) sa[u][i] = as[i][(int64_t)at * out.m];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (kb + 8 * u >= blocks) break;
+        const float f = scale_value(sb[u]);
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const v8bf b0 = codes_to_bf16(fb[u][p][0], fb[u][p][1], f), b1 = codes_to_bf16(fb[u][p][2], fb[u][p][3], f);
+#pragma unroll
+          for (int i = 0; i < MI; ++i) {
+            const float e = scale_value(sa[u][i]);
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b0, codes_to_bf16(fa[u][i][p][0], fa[u][i][p][1], e), acc[i], 0, 0, 0);
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b1, codes_to_bf16(fa[u][i][p][2], fa[u][i][p][3], e), acc[i], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MI; ++i) meet[wave][i][lane] = acc[i];
+  __syncthreads();
+  if (wave < MI) {
+    v4f sum = meet[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) sum += meet[w][wave][lane];
+    if (wave * 16 + r16 < out.m) prod_store((C*)out.c, wave * 16 + r16, n0 + g * 4, out.n, sum);
+  }
+}
+
 // ---- rows of whole 16-byte pieces -------------------------------------------
 // TM x TN results a workgroup of WM x WN waves, 128 k a stage, ST stages in LDS.  Stages are filled by loads that go straight to LDS (no
 // registers, no instructions to store them) while earlier ones are multiplied; a stage costs one barrier.  A wave's load brings eight
@@ -389,14 +465,19 @@ static int launch_prod_tile(const ProdArgs& args, int64_t tiles, hipStream_t st)
 
 template <class C, bool B_TILES>
 static int launch_prod_as(ProdArgs& args, std::vector<ProdOut>& outs, const std::vector<ProdSeg>& segs, distdl_linear8_plan* p, hipStream_t st) {
-  enum { kAny, kSmall, kLarge } kind = kAny;
-  int64_t tiles = 0;
-  if (prod_pieces(outs, segs)) {
+  enum { kAny, kRows, kSmall, kLarge } kind = kAny;
+  int64_t tiles = 0, rows = 0, longest = 0;
+  for (const ProdOut& o : outs) rows = std::max<int64_t>(rows, o.m);
+  for (const ProdSeg& g : segs) longest = std::max<int64_t>(longest, g.k);
+  if (rows <= 64 && longest < 1 << 30) {
+    kind = kRows;
+  } else if (prod_pieces(outs, segs)) {
     // Large tiles need less of their operands from L2, and enough of them to keep the compute units busy.
     tiles = prod_tiles(outs, 256, sizeof(C) == 2 ? 256 : 128);
     kind = tiles >= 160 ? kLarge : kSmall;
   }
-  if (kind != kLarge) tiles = kind == kSmall ? prod_tiles(outs, 64, 64) : prod_tiles(outs, 128, 128);
+  if (kind == kRows) tiles = prod_tiles(outs, 64, 16);
+  else if (kind != kLarge) tiles = kind == kSmall ? prod_tiles(outs, 64, 64) : prod_tiles(outs, 128, 128);
   if (tiles >= kMaxBlocks256 / 2) return set_error(DISTDL_ERR_UNSUPPORTED, "linear8: problem too large");
   args.n_out = (int32_t)outs.size();
   args.more_out = nullptr;
@@ -415,7 +496,11 @@ static int launch_prod_as(ProdArgs& args, std::vector<ProdOut>& outs, const std:
     else return launch_prod_tile<C, B_TILES, false, 256, 128, 4, 2, 3>(args, tiles, st);
   }
   if (kind == kSmall) return launch_prod_tile<C, B_TILES, false, 64, 64, 2, 2, 4>(args, tiles, st);
-  hipLaunchKernelGGL((prod8_any_kernel<C, B_TILES>), dim3((unsigned)tiles), dim3(256), 0, st, args);
+  const dim3 grid((unsigned)tiles);
+  if (kind == kAny) hipLaunchKernelGGL((prod8_any_kernel<C, B_TILES>), grid, dim3(256), 0, st, args);
+  else if (rows <= 16) hipLaunchKernelGGL((prod8_rows_kernel<C, B_TILES, 1, 4>), grid, dim3(512), 0, st, args);
+  else if (rows <= 32) hipLaunchKernelGGL((prod8_rows_kernel<C, B_TILES, 2, 2>), grid, dim3(512), 0, st, args);
+  else hipLaunchKernelGGL((prod8_rows_kernel<C, B_TILES, 4, 2>), grid, dim3(512), 0, st, args);
   return DISTDL_OK;
 }
 
