@@ -9,6 +9,7 @@
 // add exact products in fp32; measured, sums of 128 to 8192 products of N(0, 1) operands are 1e-8 to 3e-7 of their size off.
 #include <algorithm>
 #include <cstddef>
+#include <type_traits>
 
 #include "block8.h"
 #include "buffer.h"
@@ -77,14 +78,29 @@ __device__ __forceinline__ ProdOut prod_of(const ProdArgs& a, uint32_t block) {
   return prod_out(a, o);
 }
 
-// 16 codes, those from n on zero
-__device__ __forceinline__ u32x4 load16_codes(const uint8_t* p, int64_t n) {
-  if (n >= 16) return *(const u32x4_any*)p;
-  u32x4 c = {0u, 0u, 0u, 0u};
+// 16 codes from k on of a row of `n`, zeros behind its end: one load, of the row's last 16 where it would pass the end, and a shift.
+// WHOLE: they are all there.
+template <bool WHOLE>
+__device__ __forceinline__ u32x4 load16_codes(const uint8_t* row, int k, int n) {
+  if (WHOLE) return *(const u32x4_any*)(row + k);
+  if (n < 16) {  // (a row that holds no 16)
+    u32x4 c = {0u, 0u, 0u, 0u};
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (i < n) c[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
-  return c;
+    for (int i = 0; i < 16; ++i)
+      if (k + i < n) c[i >> 2] |= (uint32_t)row[k + i] << (8 * (i & 3));
+    return c;
+  }
+  const int from = min(k, n - 16), skip = min(k - from, 16) * 8;  // bits that are another piece's
+  const u32x4 c = *(const u32x4_any*)(row + from);
+  uint64_t lo = (uint64_t)c[1] << 32 | c[0], hi = (uint64_t)c[3] << 32 | c[2];
+  if (skip >= 64) {
+    lo = skip < 128 ? hi >> (skip - 64) : 0;
+    hi = 0;
+  } else if (skip > 0) {
+    lo = lo >> skip | hi << (64 - skip);
+    hi >>= skip;
+  }
+  return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
 
 // Four consecutive results of a row
@@ -124,16 +140,20 @@ __global__ __launch_bounds__(256) void prod8_any_kernel(ProdArgs args) {
   v4f acc[4][4] = {};  // [n][m]: B's rows are the matrix instruction's rows, so that a lane holds four consecutive n of one m
   for (int sg = 0; sg < out.segs; ++sg) {
     const ProdSeg seg = prod_seg(args, out.seg0 + sg);
-    const int64_t blocks = (seg.k + kBlock8 - 1) / kBlock8;
+    const int k = (int)seg.k, blocks = (k + kBlock8 - 1) / kBlock8;
     for (int64_t kb = 0; kb < blocks; ++kb) {
       u32x4 ra[4], rb[4];
+      auto fetch = [&](auto whole) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = i * 32 + (threadIdx.x >> 3), p = threadIdx.x & 7;
-        const int64_t k = kb * kBlock8 + p * 16;
-        ra[i] = load16_codes(seg.a + (m0 + r) * seg.k + k, m0 + r < out.m ? seg.k - k : 0);
-        rb[i] = load16_codes(seg.b + (n0 + r) * seg.k + k, n0 + r < out.n ? seg.k - k : 0);
-      }
+        for (int i = 0; i < 4; ++i) {
+          // (rows that are not there are the last one once more: what comes of them is not stored)
+          const int r = i * 32 + (threadIdx.x >> 3), at = (int)kb * kBlock8 + (threadIdx.x & 7) * 16;
+          ra[i] = load16_codes<decltype(whole)::value>(seg.a + (int64_t)min(m0 + r, out.m - 1) * k, at, k);
+          rb[i] = load16_codes<decltype(whole)::value>(seg.b + (int64_t)min(n0 + r, out.n - 1) * k, at, k);
+        }
+      };
+      if (kb < blocks - 1 || (k & 127) == 0) fetch(std::true_type());
+      else fetch(std::false_type());
       int sa[4], sb[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -198,52 +218,51 @@ __global__ __launch_bounds__(512) void prod8_rows_kernel(ProdArgs args) {
 #pragma unroll
   for (int i = 0; i < MI; ++i) m[i] = min(i * 16 + r16, out.m - 1);
   v4f acc[MI] = {};
-  for (int sg = 0; sg < out.segs; ++sg) {
-    const ProdSeg seg = prod_seg(args, out.seg0 + sg);
-    const int k = (int)seg.k, blocks = (k + 127) / 128;
-    const uint8_t *const b = seg.b + (int64_t)n * k + g * 16, *const bs = B_TILES ? seg.bs + (int64_t)(n >> 7) * blocks : seg.bs + n;
-    const uint8_t *a[MI], *as[MI];
+  int total = 0, sg = 0, base = 0;  // blocks of all segments; the segment at hand and its first block
+  for (int i = 0; i < out.segs; ++i) total += ((int)prod_seg(args, out.seg0 + i).k + 127) / 128;
+  ProdSeg seg = prod_seg(args, out.seg0);
+  int k = (int)seg.k, blocks = (k + 127) / 128;
+  for (int t0 = wave; t0 < total; t0 += 8 * U) {
+    u32x4 fb[U][2], fa[U][MI][2];
+    int sb[U], sa[U][MI];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      a[i] = seg.a + (int64_t)m[i] * k + g * 16;
-      as[i] = seg.as + m[i];
-    }
-    for (int kb = wave; kb < blocks; kb += 8 * U) {
-      u32x4 fb[U][2], fa[U][MI][2];
-      int sb[U], sa[U][MI];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int at = kb + 8 * u;
-        if (at < blocks) {
-          auto piece = [&](const uint8_t* row, int p) {
-            const int64_t o = (int64_t)at * 128 + p * 64;
-            if (at < blocks - 1) return (u32x4) * (const u32x4_any*)(row + o);
-            return load16_codes(row + o, k - o - g * 16);
-          };
-#pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            fb[u][p] = piece(b, p);
-#pragma unroll
-            for (int i = 0; i < MI; ++i) fa[u][i][p] = piece(a[i], p);
-          }
-          sb[u] = bs[B_TILES ? (int64_t)at : (int64_t)at * out.n];
-#pragma unroll
-          for (int i = 0; i < MI; ++i) sa[u][i] = as[i][(int64_t)at * out.m];
-        }
+    for (int u = 0; u < U; ++u) {
+      if (t0 + 8 * u >= total) break;
+      while (t0 + 8 * u - base >= blocks) {
+        base += blocks;
+        seg = prod_seg(args, out.seg0 + ++sg);
+        k = (int)seg.k;
+        blocks = (k + 127) / 128;
       }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (kb + 8 * u >= blocks) break;
-        const float f = scale_value(sb[u]);
+      const int kb = t0 + 8 * u - base;
+      const uint8_t* const b = seg.b + (int64_t)n * k;
+      auto fetch = [&](auto whole) {
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-          const v8bf b0 = codes_to_bf16(fb[u][p][0], fb[u][p][1], f), b1 = codes_to_bf16(fb[u][p][2], fb[u][p][3], f);
+          const int at = kb * 128 + p * 64 + g * 16;
+          fb[u][p] = load16_codes<decltype(whole)::value>(b, at, k);
 #pragma unroll
-          for (int i = 0; i < MI; ++i) {
-            const float e = scale_value(sa[u][i]);
-            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b0, codes_to_bf16(fa[u][i][p][0], fa[u][i][p][1], e), acc[i], 0, 0, 0);
-            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b1, codes_to_bf16(fa[u][i][p][2], fa[u][i][p][3], e), acc[i], 0, 0, 0);
-          }
+          for (int i = 0; i < MI; ++i) fa[u][i][p] = load16_codes<decltype(whole)::value>(seg.a + (int64_t)m[i] * k, at, k);
+        }
+      };
+      if (kb < blocks - 1 || (k & 127) == 0) fetch(std::true_type());
+      else fetch(std::false_type());
+      sb[u] = B_TILES ? seg.bs[(int64_t)(n >> 7) * blocks + kb] : seg.bs[(int64_t)kb * out.n + n];
+#pragma unroll
+      for (int i = 0; i < MI; ++i) sa[u][i] = seg.as[(int64_t)kb * out.m + m[i]];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (t0 + 8 * u >= total) break;
+      const float f = scale_value(sb[u]);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const v8bf b0 = codes_to_bf16(fb[u][p][0], fb[u][p][1], f), b1 = codes_to_bf16(fb[u][p][2], fb[u][p][3], f);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+          const float e = scale_value(sa[u][i]);
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b0, codes_to_bf16(fa[u][i][p][0], fa[u][i][p][1], e), acc[i], 0, 0, 0);
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b1, codes_to_bf16(fa[u][i][p][2], fa[u][i][p][3], e), acc[i], 0, 0, 0);
         }
       }
     }
@@ -466,10 +485,9 @@ static int launch_prod_tile(const ProdArgs& args, int64_t tiles, hipStream_t st)
 template <class C, bool B_TILES>
 static int launch_prod_as(ProdArgs& args, std::vector<ProdOut>& outs, const std::vector<ProdSeg>& segs, distdl_linear8_plan* p, hipStream_t st) {
   enum { kAny, kRows, kSmall, kLarge } kind = kAny;
-  int64_t tiles = 0, rows = 0, longest = 0;
+  int64_t tiles = 0, rows = 0;
   for (const ProdOut& o : outs) rows = std::max<int64_t>(rows, o.m);
-  for (const ProdSeg& g : segs) longest = std::max<int64_t>(longest, g.k);
-  if (rows <= 64 && longest < 1 << 30) {
+  if (rows <= 64) {
     kind = kRows;
   } else if (prod_pieces(outs, segs)) {
     // Large tiles need less of their operands from L2, and enough of them to keep the compute units busy.
