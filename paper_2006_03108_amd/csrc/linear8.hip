@@ -284,10 +284,13 @@ __global__ __launch_bounds__(512) void prod8_rows_kernel(ProdArgs args) {
 // rows of 128 bytes: lane L asks for piece (L & 7) ^ (L >> 3) of row L >> 3, so that row r's piece p lies at p ^ (r & 7) and the lanes
 // that read together find different banks.  Rows and pieces that are not there fail the check of their buffer and arrive as zeros.
 // The scales of the stage's rows come the same way, a byte to a word of LDS.
-// FP8: the codes' own matrix instruction, else bf16 ones on codes that are converted as they leave LDS.
-template <class C, bool B_TILES, bool FP8, int TM, int TN, int WM, int WN, int ST>
-__global__ __launch_bounds__(64 * WM * WN) void prod8_tile_kernel(ProdArgs args) {
-  constexpr int NW = WM * WN, MI = TM / WM / 16, NI = TN / WN / 16;
+// FP8: the codes' own matrix instruction, else bf16 ones on codes that are converted as they leave LDS.  WK = 2: two waves share a
+// part of the tile, each with half of a stage's k, and add up at the end: what a wave does in a stage is a chain
+// (barrier, LDS, conversion, four dependent products), and small tiles have a wave on each SIMD otherwise.
+template <class C, bool B_TILES, bool FP8, int TM, int TN, int WM, int WN, int WK, int ST>
+__global__ __launch_bounds__(64 * WM * WN * WK) void prod8_tile_kernel(ProdArgs args) {
+  static_assert(!FP8 || WK == 1, "an instruction takes a whole block of k");
+  constexpr int NW = WM * WN * WK, MI = TM / WM / 16, NI = TN / WN / 16;
   constexpr int kData = (TM + TN) * 128, kStage = kData + (TM + TN) * 4;
   constexpr int kLoads = (TM + TN) / 8 / NW;                                            // a wave's loads of codes for a stage
   constexpr int kScales = ((TM + TN) / 64 + NW - 1) / NW;                               // and of scales (some twice, where waves are many)
@@ -300,7 +303,7 @@ __global__ __launch_bounds__(64 * WM * WN) void prod8_tile_kernel(ProdArgs args)
   const uint32_t band = tile / (8 * tiles_n), in_band = tile - band * 8 * tiles_n, high = min(8u, out.tiles_m - band * 8);
   const int m0 = (int)((band * 8 + in_band % high) * TM), n0 = (int)(in_band / high * TN);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave % WM * (TM / WM), wn = wave / WM * (TN / WN), r16 = lane & 15, g = lane >> 4;
+  const int wm = wave % WM * (TM / WM), wn = wave / WM % WN * (TN / WN), wk = wave / (WM * WN), r16 = lane & 15, g = lane >> 4;
   const uint32_t lds0 = lds_address(lds);
 
   // loads: which rows this lane asks for
@@ -400,7 +403,8 @@ __global__ __launch_bounds__(64 * WM * WN) void prod8_tile_kernel(ProdArgs args)
       }
     } else {
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
+      for (int h = 0; h < 2 / WK; ++h) {
+        const int p = WK == 2 ? wk : h;
         v8bf fa[MI][2];
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
@@ -423,6 +427,23 @@ __global__ __launch_bounds__(64 * WM * WN) void prod8_tile_kernel(ProdArgs args)
       }
     }
     buffer = buffer == ST - 1 ? 0 : buffer + 1;
+  }
+  if constexpr (WK == 2) {
+    static_assert(TM * TN * 4 <= ST * kStage, "the sums of half the waves fit where the stages were");
+    v4f* const half = (v4f*)lds + (wave % (WM * WN)) * (NI * MI * 64) + lane;
+    lds_barrier();  // (no load is under way: the last stage was waited for)
+    if (wk == 1) {
+#pragma unroll
+      for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int i = 0; i < MI; ++i) half[(j * MI + i) * 64] = acc[j][i];
+    }
+    lds_barrier();
+    if (wk == 1) return;
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+      for (int i = 0; i < MI; ++i) acc[j][i] += half[(j * MI + i) * 64];
   }
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
@@ -472,30 +493,38 @@ static bool prod_pieces(const std::vector<ProdOut>& outs, const std::vector<Prod
   return true;
 }
 
-template <class C, bool B_TILES, bool FP8, int TM, int TN, int WM, int WN, int ST>
+template <class C, bool B_TILES, bool FP8, int TM, int TN, int WM, int WN, int WK, int ST>
 static int launch_prod_tile(const ProdArgs& args, int64_t tiles, hipStream_t st) {
   constexpr int bytes = ST * ((TM + TN) * 132);
   static_assert(bytes <= 160 * 1024, "LDS of a compute unit");
-  const int rc = allow_large_lds<prod8_tile_kernel<C, B_TILES, FP8, TM, TN, WM, WN, ST>>();
+  const int rc = allow_large_lds<prod8_tile_kernel<C, B_TILES, FP8, TM, TN, WM, WN, WK, ST>>();
   if (rc) return rc;
-  hipLaunchKernelGGL((prod8_tile_kernel<C, B_TILES, FP8, TM, TN, WM, WN, ST>), dim3((unsigned)tiles), dim3(64 * WM * WN), bytes, st, args);
+  hipLaunchKernelGGL((prod8_tile_kernel<C, B_TILES, FP8, TM, TN, WM, WN, WK, ST>), dim3((unsigned)tiles), dim3(64 * WM * WN * WK), bytes, st, args);
   return DISTDL_OK;
 }
 
 template <class C, bool B_TILES>
 static int launch_prod_as(ProdArgs& args, std::vector<ProdOut>& outs, const std::vector<ProdSeg>& segs, distdl_linear8_plan* p, hipStream_t st) {
-  enum { kAny, kRows, kSmall, kLarge } kind = kAny;
+  enum { kAny, kRows, kSmall, kMiddle, kLarge } kind = kAny;
   int64_t tiles = 0, rows = 0;
   for (const ProdOut& o : outs) rows = std::max<int64_t>(rows, o.m);
   if (rows <= 64) {
     kind = kRows;
   } else if (prod_pieces(outs, segs)) {
-    // Large tiles need less of their operands from L2, and enough of them to keep the compute units busy.
+    // Large tiles need less of their operands from L2, but there have to be enough of them to keep the compute units busy.
     tiles = prod_tiles(outs, 256, sizeof(C) == 2 ? 256 : 128);
-    kind = tiles >= 160 ? kLarge : kSmall;
+    kind = kLarge;
+    if (tiles < 160) {
+      tiles = prod_tiles(outs, 128, 128);
+      kind = kMiddle;
+    }
+    if (tiles < 128) {
+      tiles = prod_tiles(outs, 64, 64);
+      kind = kSmall;
+    }
   }
   if (kind == kRows) tiles = prod_tiles(outs, 64, 16);
-  else if (kind != kLarge) tiles = kind == kSmall ? prod_tiles(outs, 64, 64) : prod_tiles(outs, 128, 128);
+  if (kind == kAny) tiles = prod_tiles(outs, 128, 128);
   if (tiles >= kMaxBlocks256 / 2) return set_error(DISTDL_ERR_UNSUPPORTED, "linear8: problem too large");
   args.n_out = (int32_t)outs.size();
   args.more_out = nullptr;
@@ -510,10 +539,11 @@ static int launch_prod_as(ProdArgs& args, std::vector<ProdOut>& outs, const std:
     args.more_seg = p->segs.dev;
   }
   if (kind == kLarge) {
-    if constexpr (sizeof(C) == 2) return launch_prod_tile<C, B_TILES, true, 256, 256, 2, 4, 2>(args, tiles, st);
-    else return launch_prod_tile<C, B_TILES, false, 256, 128, 4, 2, 3>(args, tiles, st);
+    if constexpr (sizeof(C) == 2) return launch_prod_tile<C, B_TILES, true, 256, 256, 2, 4, 1, 2>(args, tiles, st);
+    else return launch_prod_tile<C, B_TILES, false, 256, 128, 4, 2, 1, 3>(args, tiles, st);
   }
-  if (kind == kSmall) return launch_prod_tile<C, B_TILES, false, 64, 64, 2, 2, 4>(args, tiles, st);
+  if (kind == kMiddle) return launch_prod_tile<C, B_TILES, false, 128, 128, 2, 2, 2, 4>(args, tiles, st);
+  if (kind == kSmall) return launch_prod_tile<C, B_TILES, false, 64, 64, 2, 2, 2, 6>(args, tiles, st);
   const dim3 grid((unsigned)tiles);
   if (kind == kAny) hipLaunchKernelGGL((prod8_any_kernel<C, B_TILES>), grid, dim3(256), 0, st, args);
   else if (rows <= 16) hipLaunchKernelGGL((prod8_rows_kernel<C, B_TILES, 1, 4>), grid, dim3(512), 0, st, args);
