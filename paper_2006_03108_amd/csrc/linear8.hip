@@ -45,7 +45,8 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
-// Eight codes times their scale, exactly (numbers below 2^-126 aside)
+// Eight codes times their scale, exactly (numbers below 2^-126 aside).  The instruction reads the exponent of `scale` alone.
+__device__ __forceinline__ float scale_exponent(int byte) { return __uint_as_float((uint32_t)byte << 23); }
 __device__ __forceinline__ v8bf codes_to_bf16(uint32_t lo, uint32_t hi, float scale) {
   union {
     v2bf p[4];
@@ -176,14 +177,14 @@ __global__ __launch_bounds__(256) void prod8_any_kernel(ProdArgs args) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const u32x4 c = piece(0, wm + i * 16 + r16, p);
-          const float s = scale_value(sa[i]);
+          const float s = scale_exponent(sa[i]);
           fa[i][0] = codes_to_bf16(c[0], c[1], s);
           fa[i][1] = codes_to_bf16(c[2], c[3], s);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const u32x4 c = piece(1, wn + j * 16 + r16, p);
-          const float s = scale_value(sb[j]);
+          const float s = scale_exponent(sb[j]);
           const v8bf b0 = codes_to_bf16(c[0], c[1], s), b1 = codes_to_bf16(c[2], c[3], s);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -254,13 +255,13 @@ __global__ __launch_bounds__(512) void prod8_rows_kernel(ProdArgs args) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (t0 + 8 * u >= total) break;
-      const float f = scale_value(sb[u]);
+      const float f = scale_exponent(sb[u]);
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         const v8bf b0 = codes_to_bf16(fb[u][p][0], fb[u][p][1], f), b1 = codes_to_bf16(fb[u][p][2], fb[u][p][3], f);
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
-          const float e = scale_value(sa[u][i]);
+          const float e = scale_exponent(sa[u][i]);
           acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b0, codes_to_bf16(fa[u][i][p][0], fa[u][i][p][1], e), acc[i], 0, 0, 0);
           acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b1, codes_to_bf16(fa[u][i][p][2], fa[u][i][p][3], e), acc[i], 0, 0, 0);
         }
@@ -284,14 +285,13 @@ __global__ __launch_bounds__(512) void prod8_rows_kernel(ProdArgs args) {
 // rows of 128 bytes: lane L asks for piece (L & 7) ^ (L >> 3) of row L >> 3, so that row r's piece p lies at p ^ (r & 7) and the lanes
 // that read together find different banks.  Rows and pieces that are not there fail the check of their buffer and arrive as zeros.
 // The scales of the stage's rows come the same way, a byte to a word of LDS.
-// FP8: the codes' own matrix instruction, else bf16 ones on codes that are converted as they leave LDS.  WK = 2: two waves share a
-// part of the tile, each with half of a stage's k, and add up at the end: what a wave does in a stage is a chain
-// (barrier, LDS, conversion, four dependent products), and small tiles have a wave on each SIMD otherwise.
+// FP8: the codes' own matrix instruction, else bf16 ones on codes that are converted as they leave LDS.  WK = 2: a stage is two blocks of
+// 128 k, and half of the waves take one, half the other; they add up at the end.  What a wave does between two barriers is a
+// chain (LDS, conversion, products), of which small tiles would have a short one on each SIMD otherwise.
 template <class C, bool B_TILES, bool FP8, int TM, int TN, int WM, int WN, int WK, int ST>
 __global__ __launch_bounds__(64 * WM * WN * WK) void prod8_tile_kernel(ProdArgs args) {
-  static_assert(!FP8 || WK == 1, "an instruction takes a whole block of k");
   constexpr int NW = WM * WN * WK, MI = TM / WM / 16, NI = TN / WN / 16;
-  constexpr int kData = (TM + TN) * 128, kStage = kData + (TM + TN) * 4;
+  constexpr int kData = (TM + TN) * 128, kBlock = kData + (TM + TN) * 4, kStage = WK * kBlock;
   constexpr int kLoads = (TM + TN) / 8 / NW;                                            // a wave's loads of codes for a stage
   constexpr int kScales = ((TM + TN) / 64 + NW - 1) / NW;                               // and of scales (some twice, where waves are many)
   static_assert((TM + TN) / 8 % NW == 0 && TM % 64 == 0 && TN % 64 == 0, "whole loads");
@@ -306,27 +306,26 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void prod8_tile_kernel(ProdArgs 
   const int wm = wave % WM * (TM / WM), wn = wave / WM % WN * (TN / WN), wk = wave / (WM * WN), r16 = lane & 15, g = lane >> 4;
   const uint32_t lds0 = lds_address(lds);
 
-  // loads: which rows this lane asks for
+  // Loads.  A wave brings groups of eight rows wave, wave + NW, ... of A, then of B, and one or more runs of 64 scales.
+  constexpr int kLoadsA = TM / 8 / NW;
+  static_assert(TM / 8 % NW == 0 && TN / 8 % NW == 0, "the same loads for all waves");
   const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
-  int seg_i = 0;                       // the segment and its block that are loaded next
-  int kb_i = 0, blocks_i = 0, rest_i = 0;
-  lds_u32x4 ra, rb, rsa, rsb;
-  uint32_t voff[kLoads], soff_s[kScales], hop[kScales];
-  auto open = [&]() {                  // the buffers and offsets of segment seg_i
-    const ProdSeg seg = prod_seg(args, out.seg0 + seg_i);
+  int seg_i = -1, left = 0, rest = 0;  // the segment that is loaded; blocks of it that are not yet; k of its last block
+  uint32_t at_k = 0, into = 0;         // first k of the next block; where it goes in LDS
+  lds_u32x4 ra, rb, rs[kScales];
+  uint32_t voff[kLoads], soff[kScales], at_s[kScales], hop[kScales];
+  auto open = [&]() {                  // the buffers and offsets of the next segment
+    const ProdSeg seg = prod_seg(args, out.seg0 + ++seg_i);
     const uint32_t k = (uint32_t)seg.k;
-    blocks_i = (int)((k + 127) / 128);
-    rest_i = (int)(k - (blocks_i - 1) * 128);
-    kb_i = 0;
+    left = (int)((k + 127) / 128);
+    rest = (int)(k - (left - 1) * 128);
+    at_k = 0;
     ra = lds_direct_rsrc(seg.a + (int64_t)m0 * k, (uint32_t)min((int64_t)0x7fffffe0, (int64_t)(out.m - m0) * k));
     rb = lds_direct_rsrc(seg.b + (int64_t)n0 * k, (uint32_t)min((int64_t)0x7fffffe0, (int64_t)(out.n - n0) * k));
-    rsa = lds_direct_rsrc(seg.as, (uint32_t)((int64_t)blocks_i * out.m));
-    rsb = lds_direct_rsrc(seg.bs, (uint32_t)((int64_t)blocks_i * (B_TILES ? (out.n + 127) >> 7 : out.n)));
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int l = wave * kLoads + i, row = l * 8 + (lane >> 3);
-      const bool is_a = l * 8 < TM;
-      const int r = is_a ? row : row - TM;
+      const bool is_a = i < kLoadsA;
+      const int r = ((is_a ? i : i - kLoadsA) * NW + wave) * 8 + (lane >> 3);
       voff[i] = r < (is_a ? out.m - m0 : out.n - n0) ? (uint32_t)r * k + piece : kOob;
     }
 #pragma unroll
@@ -334,52 +333,59 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void prod8_tile_kernel(ProdArgs 
       const int l = (wave * kScales + i) % ((TM + TN) / 64);
       const bool is_a = l * 64 < TM;
       const int r = is_a ? m0 + l * 64 + lane : n0 + l * 64 - TM + lane;
-      if (is_a) soff_s[i] = r < out.m ? r : kOob;
-      else soff_s[i] = r < out.n ? (B_TILES ? (uint32_t)(r >> 7) * blocks_i : r) : kOob;
+      const uint32_t width = is_a ? out.m : B_TILES ? (out.n + 127) >> 7 : out.n;
+      rs[i] = lds_direct_rsrc(is_a ? seg.as : seg.bs, left * width);
+      if (is_a) soff[i] = r < out.m ? r : kOob;
+      else soff[i] = r < out.n ? (B_TILES ? (uint32_t)(r >> 7) * left : r) : kOob;
       hop[i] = is_a ? out.m : B_TILES ? 1 : out.n;
+      at_s[i] = 0;
     }
   };
-  auto load = [&](int buffer) {        // the next block to `buffer`, if there is one
-    if (kb_i == blocks_i) {
-      ++seg_i;
-      open();
-    }
-    const bool last = kb_i == blocks_i - 1;
+  auto load = [&]() {                  // the next block to the next place; zeros behind the last one
+    if (left == 0 && seg_i + 1 < out.segs) open();
+    const bool gone = left <= 0 || (left == 1 && piece >= rest);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int l = wave * kLoads + i;
-      load_to_lds(l * 8 < TM ? ra : rb, lds0 + buffer * kStage + l * 1024, last && piece >= rest_i ? kOob : voff[i], kb_i * 128);
+      const int l = i < kLoadsA ? i * NW + wave : TM / 8 + (i - kLoadsA) * NW + wave;
+      load_to_lds(i < kLoadsA ? ra : rb, lds0 + into + l * 1024, gone ? kOob : voff[i], at_k);
     }
 #pragma unroll
     for (int i = 0; i < kScales; ++i) {
       const int l = (wave * kScales + i) % ((TM + TN) / 64);
-      load_byte_to_lds(l * 64 < TM ? rsa : rsb, lds0 + buffer * kStage + kData + l * 256, soff_s[i], kb_i * hop[i]);
+      load_byte_to_lds(rs[i], lds0 + into + kData + l * 256, left > 0 ? soff[i] : kOob, left > 0 ? at_s[i] : 0);
+      at_s[i] += hop[i];
     }
-    ++kb_i;
+    at_k = left > 1 ? at_k + 128 : 0;
+    --left;
+    into = into == ST * kStage - kBlock ? 0 : into + kBlock;
+  };
+  auto load_stage = [&]() {
+#pragma unroll
+    for (int i = 0; i < WK; ++i) load();
   };
   int total = 0;
   for (int i = 0; i < out.segs; ++i) total += (int)((prod_seg(args, out.seg0 + i).k + 127) / 128);
+  total = (total + WK - 1) / WK;
 
   v4f acc[NI][MI] = {};  // B's rows are the matrix instruction's rows, so that a lane holds four consecutive n of one m
-  open();
 #pragma unroll
   for (int i = 0; i < ST - 1; ++i)
-    if (i < total) load(i);
-  int buffer = 0;
+    if (i < total) load_stage();
+  uint32_t from = 0;
+  const uint32_t at_a = (wm + r16) * 128, at_b = (TM + wn + r16) * 128, at_sa = kData + (wm + r16) * 4, at_sb = kData + (TM + wn + r16) * 4;
+  const uint32_t p0 = (g ^ (r16 & 7)) * 16, p1 = ((g + 4) ^ (r16 & 7)) * 16;
   for (int s = 0; s < total; ++s) {
-    if (total - 1 - s >= ST - 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((ST - 2) * (kLoads + kScales)) : "memory");
+    if (total - 1 - s >= ST - 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((ST - 2) * WK * (kLoads + kScales)) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     lds_barrier();  // this stage is there for all waves, and all have read the one before it
-    if (s + ST - 1 < total) load(buffer == 0 ? ST - 1 : buffer - 1);
-    const char* const at = lds + buffer * kStage;
-    const char* const at_a = at + (wm + r16) * 128;
-    const char* const at_b = at + (TM + wn + r16) * 128;
-    const int p0 = (g ^ (r16 & 7)) * 16, p1 = ((g + 4) ^ (r16 & 7)) * 16;
+    const char* const at = lds + from + wk * kBlock;
+    from = from == (ST - 1) * kStage ? 0 : from + kStage;
+    // The operands' reads first, then the next loads: the scalar work of those runs while LDS answers.
     int sa[MI], sb[NI];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) sa[i] = *(const uint8_t*)(at + kData + (wm + i * 16 + r16) * 4);
+    for (int i = 0; i < MI; ++i) sa[i] = *(const uint8_t*)(at + at_sa + i * 64);
 #pragma unroll
-    for (int j = 0; j < NI; ++j) sb[j] = *(const uint8_t*)(at + kData + (TM + wn + j * 16 + r16) * 4);
+    for (int j = 0; j < NI; ++j) sb[j] = *(const uint8_t*)(at + at_sb + j * 64);
     if constexpr (FP8) {
       auto both = [&](const char* p) {
         const u32x4 lo = *(const u32x4*)(p + p0), hi = *(const u32x4*)(p + p1);
@@ -393,31 +399,37 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void prod8_tile_kernel(ProdArgs 
       };
       v8i fa[MI];
 #pragma unroll
-      for (int i = 0; i < MI; ++i) fa[i] = both(at_a + i * 2048);
+      for (int i = 0; i < MI; ++i) fa[i] = both(at + at_a + i * 2048);
+      v8i fb = both(at + at_b);
+      if (s + ST - 1 < total) load_stage();
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
-        const v8i fb = both(at_b + j * 2048);
+        if (j > 0) fb = both(at + at_b + j * 2048);
 #pragma unroll
         for (int i = 0; i < MI; ++i)
           acc[j][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, fa[i], acc[j][i], 0, 0, 0, sb[j], 0, sa[i]);
       }
     } else {
 #pragma unroll
-      for (int h = 0; h < 2 / WK; ++h) {
-        const int p = WK == 2 ? wk : h;
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t p = h ? p1 : p0;
+        u32x4 ca[MI], cb[NI];
+#pragma unroll
+        for (int i = 0; i < MI; ++i) ca[i] = *(const u32x4*)(at + at_a + i * 2048 + p);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) cb[j] = *(const u32x4*)(at + at_b + j * 2048 + p);
+        if (h == 0 && s + ST - 1 < total) load_stage();
         v8bf fa[MI][2];
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
-          const u32x4 c = *(const u32x4*)(at_a + i * 2048 + (p ? p1 : p0));
-          const float f = scale_value(sa[i]);
-          fa[i][0] = codes_to_bf16(c[0], c[1], f);
-          fa[i][1] = codes_to_bf16(c[2], c[3], f);
+          const float f = scale_exponent(sa[i]);
+          fa[i][0] = codes_to_bf16(ca[i][0], ca[i][1], f);
+          fa[i][1] = codes_to_bf16(ca[i][2], ca[i][3], f);
         }
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-          const u32x4 c = *(const u32x4*)(at_b + j * 2048 + (p ? p1 : p0));
-          const float f = scale_value(sb[j]);
-          const v8bf b0 = codes_to_bf16(c[0], c[1], f), b1 = codes_to_bf16(c[2], c[3], f);
+          const float f = scale_exponent(sb[j]);
+          const v8bf b0 = codes_to_bf16(cb[j][0], cb[j][1], f), b1 = codes_to_bf16(cb[j][2], cb[j][3], f);
 #pragma unroll
           for (int i = 0; i < MI; ++i) {
             acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b0, fa[i][0], acc[j][i], 0, 0, 0);
@@ -426,7 +438,6 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void prod8_tile_kernel(ProdArgs 
         }
       }
     }
-    buffer = buffer == ST - 1 ? 0 : buffer + 1;
   }
   if constexpr (WK == 2) {
     static_assert(TM * TN * 4 <= ST * kStage, "the sums of half the waves fit where the stages were");
@@ -495,7 +506,7 @@ static bool prod_pieces(const std::vector<ProdOut>& outs, const std::vector<Prod
 
 template <class C, bool B_TILES, bool FP8, int TM, int TN, int WM, int WN, int WK, int ST>
 static int launch_prod_tile(const ProdArgs& args, int64_t tiles, hipStream_t st) {
-  constexpr int bytes = ST * ((TM + TN) * 132);
+  constexpr int bytes = ST * WK * (TM + TN) * 132;
   static_assert(bytes <= 160 * 1024, "LDS of a compute unit");
   const int rc = allow_large_lds<prod8_tile_kernel<C, B_TILES, FP8, TM, TN, WM, WN, WK, ST>>();
   if (rc) return rc;
@@ -542,8 +553,8 @@ static int launch_prod_as(ProdArgs& args, std::vector<ProdOut>& outs, const std:
     if constexpr (sizeof(C) == 2) return launch_prod_tile<C, B_TILES, true, 256, 256, 2, 4, 1, 2>(args, tiles, st);
     else return launch_prod_tile<C, B_TILES, false, 256, 128, 4, 2, 1, 3>(args, tiles, st);
   }
-  if (kind == kMiddle) return launch_prod_tile<C, B_TILES, false, 128, 128, 2, 2, 2, 4>(args, tiles, st);
-  if (kind == kSmall) return launch_prod_tile<C, B_TILES, false, 64, 64, 2, 2, 2, 6>(args, tiles, st);
+  if (kind == kMiddle) return launch_prod_tile<C, B_TILES, false, 128, 128, 2, 2, 2, 2>(args, tiles, st);
+  if (kind == kSmall) return launch_prod_tile<C, B_TILES, false, 64, 64, 2, 2, 2, 4>(args, tiles, st);
   const dim3 grid((unsigned)tiles);
   if (kind == kAny) hipLaunchKernelGGL((prod8_any_kernel<C, B_TILES>), grid, dim3(256), 0, st, args);
   else if (rows <= 16) hipLaunchKernelGGL((prod8_rows_kernel<C, B_TILES, 1, 4>), grid, dim3(512), 0, st, args);
