@@ -59,25 +59,36 @@ __device__ __forceinline__ v8bf codes_to_bf16(uint32_t lo, uint32_t hi, float sc
   return u.v;
 }
 
-// A result and a worker's part of a sum, from the table or from the launch's own arguments, into scalar registers.
-typedef const __attribute__((address_space(4))) ProdOut* ProdOutPtr;
-typedef const __attribute__((address_space(4))) ProdSeg* ProdSegPtr;
-__device__ __forceinline__ ProdOut prod_out(const ProdArgs& a, int o) {
-  static_assert(offsetof(ProdArgs, out) == 0, "the kernels' first argument starts with the results");
-  const ProdOutPtr p = (a.more_out ? (ProdOutPtr)(uint64_t)a.more_out : (ProdOutPtr)__builtin_amdgcn_kernarg_segment_ptr()) + o;
-  return ProdOut{p->c, p->m, p->n, p->tile0, p->tiles_m, p->seg0, p->segs};
-}
-__device__ __forceinline__ ProdSeg prod_seg(const ProdArgs& a, int i) {
-  const ProdSegPtr p = (a.more_seg ? (ProdSegPtr)(uint64_t)a.more_seg
-                                   : (ProdSegPtr)((const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(ProdArgs, seg))) + i;
-  return ProdSeg{p->a, p->as, p->b, p->bs, p->k};
-}
-// The result that workgroup `block` belongs to
-__device__ __forceinline__ ProdOut prod_of(const ProdArgs& a, uint32_t block) {
-  int o = 0;
-  while (o + 1 < a.n_out && block >= prod_out(a, o + 1).tile0) ++o;
-  return prod_out(a, o);
-}
+// Results and workers' parts of a sum, from the tables or from the launch's own arguments, read into scalar registers.  The addresses are taken
+// in the kernel itself: the arguments' is not known in a function that the compiler might not inline.
+struct ProdTables {
+  const __attribute__((address_space(4))) ProdOut* outs;
+  const __attribute__((address_space(4))) ProdSeg* segs;
+  int n_out;
+  __device__ __forceinline__ ProdOut out(int i) const {
+    const auto p = outs + i;
+    return ProdOut{p->c, p->m, p->n, p->tile0, p->tiles_m, p->seg0, p->segs};
+  }
+  __device__ __forceinline__ ProdSeg seg(int i) const {
+    const auto p = segs + i;
+    return ProdSeg{p->a, p->as, p->b, p->bs, p->k};
+  }
+  __device__ __forceinline__ ProdOut of(uint32_t block) const {  // the result that workgroup `block` belongs to
+    int o = 0;
+    while (o + 1 < n_out && block >= outs[o + 1].tile0) ++o;
+    return out(o);
+  }
+};
+static_assert(offsetof(ProdArgs, out) == 0, "the kernels' first argument starts with the results");
+#define PROD_TABLES(args)                                                                                                  \
+  ProdTables {                                                                                                             \
+    (args).more_out ? (const __attribute__((address_space(4))) ProdOut*)(uint64_t)(args).more_out                          \
+                    : (const __attribute__((address_space(4))) ProdOut*)__builtin_amdgcn_kernarg_segment_ptr(),            \
+        (args).more_seg ? (const __attribute__((address_space(4))) ProdSeg*)(uint64_t)(args).more_seg                      \
+                        : (const __attribute__((address_space(4))) ProdSeg*)((const __attribute__((address_space(4))) char*) \
+                              __builtin_amdgcn_kernarg_segment_ptr() + offsetof(ProdArgs, seg)),                           \
+        (args).n_out                                                                                                       \
+  }
 
 // 16 codes from k on of a row of `n`, zeros behind its end: one load, of the row's last 16 where it would pass the end, and a shift.
 // WHOLE: they are all there.
@@ -133,18 +144,19 @@ __device__ __forceinline__ void prod_store(uint16_t* c, int m, int n, int cols, 
 template <class C, bool B_TILES>
 __global__ __launch_bounds__(256) void prod8_any_kernel(ProdArgs args) {
   __shared__ u32x4 lds[2][kBlock8][8];
-  const ProdOut out = prod_of(args, blockIdx.x);
+  const ProdTables tables = PROD_TABLES(args);
+  const ProdOut out = tables.of(blockIdx.x);
   const uint32_t tile = blockIdx.x - out.tile0;
   const int m0 = (int)(tile % out.tiles_m) * 128, n0 = (int)(tile / out.tiles_m) * 128;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64, r16 = lane & 15, g = lane >> 4;
   v4f acc[4][4] = {};  // [n][m]: B's rows are the matrix instruction's rows, so that a lane holds four consecutive n of one m
   for (int sg = 0; sg < out.segs; ++sg) {
-    const ProdSeg seg = prod_seg(args, out.seg0 + sg);
+    const ProdSeg seg = tables.seg(out.seg0 + sg);
     const int k = (int)seg.k, blocks = (k + kBlock8 - 1) / kBlock8;
     for (int64_t kb = 0; kb < blocks; ++kb) {
       u32x4 ra[4], rb[4];
-      auto fetch = [&](auto whole) {
+      auto fetch = [&](auto whole) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           // (rows that are not there are the last one once more: what comes of them is not stored)
@@ -170,7 +182,7 @@ __global__ __launch_bounds__(256) void prod8_any_kernel(ProdArgs args) {
         lds[1][r][p ^ (r & 7)] = rb[i];
       }
       __syncthreads();
-      auto piece = [&](int side, int row, int p) { return lds[side][row][(g + 4 * p) ^ (row & 7)]; };
+      auto piece = [&](int side, int row, int p) __attribute__((always_inline)) { return lds[side][row][(g + 4 * p) ^ (row & 7)]; };
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         v8bf fa[4][2];
@@ -210,7 +222,8 @@ __global__ __launch_bounds__(256) void prod8_any_kernel(ProdArgs args) {
 template <class C, bool B_TILES, int MI, int U>
 __global__ __launch_bounds__(512) void prod8_rows_kernel(ProdArgs args) {
   __shared__ v4f meet[8][MI][64];
-  const ProdOut out = prod_of(args, blockIdx.x);
+  const ProdTables tables = PROD_TABLES(args);
+  const ProdOut out = tables.of(blockIdx.x);
   const int n0 = (int)(blockIdx.x - out.tile0) * 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
   // (rows that are not there are others' once more: what comes of them is not stored)
@@ -220,8 +233,8 @@ __global__ __launch_bounds__(512) void prod8_rows_kernel(ProdArgs args) {
   for (int i = 0; i < MI; ++i) m[i] = min(i * 16 + r16, out.m - 1);
   v4f acc[MI] = {};
   int total = 0, sg = 0, base = 0;  // blocks of all segments; the segment at hand and its first block
-  for (int i = 0; i < out.segs; ++i) total += ((int)prod_seg(args, out.seg0 + i).k + 127) / 128;
-  ProdSeg seg = prod_seg(args, out.seg0);
+  for (int i = 0; i < out.segs; ++i) total += ((int)tables.seg(out.seg0 + i).k + 127) / 128;
+  ProdSeg seg = tables.seg(out.seg0);
   int k = (int)seg.k, blocks = (k + 127) / 128;
   for (int t0 = wave; t0 < total; t0 += 8 * U) {
     u32x4 fb[U][2], fa[U][MI][2];
@@ -231,13 +244,13 @@ __global__ __launch_bounds__(512) void prod8_rows_kernel(ProdArgs args) {
       if (t0 + 8 * u >= total) break;
       while (t0 + 8 * u - base >= blocks) {
         base += blocks;
-        seg = prod_seg(args, out.seg0 + ++sg);
+        seg = tables.seg(out.seg0 + ++sg);
         k = (int)seg.k;
         blocks = (k + 127) / 128;
       }
       const int kb = t0 + 8 * u - base;
       const uint8_t* const b = seg.b + (int64_t)n * k;
-      auto fetch = [&](auto whole) {
+      auto fetch = [&](auto whole) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
           const int at = kb * 128 + p * 64 + g * 16;
@@ -285,8 +298,8 @@ __global__ __launch_bounds__(512) void prod8_rows_kernel(ProdArgs args) {
 // rows of 128 bytes: lane L asks for piece (L & 7) ^ (L >> 3) of row L >> 3, so that row r's piece p lies at p ^ (r & 7) and the lanes
 // that read together find different banks.  Rows and pieces that are not there fail the check of their buffer and arrive as zeros.
 // The scales of the stage's rows come the same way, a byte to a word of LDS.
-// FP8: the codes' own matrix instruction, else bf16 ones on codes that are converted as they leave LDS.  WK = 2: a stage is two blocks of
-// 128 k, and half of the waves take one, half the other; they add up at the end.  What a wave does between two barriers is a
+// FP8: the codes' own matrix instruction, else bf16 ones on codes that are converted as they leave LDS.  WK > 1: a stage is WK blocks
+// of 128 k, each for a WK'th of the waves, which add up at the end.  What a wave does between two barriers is a
 // chain (LDS, conversion, products), of which small tiles would have a short one on each SIMD otherwise.
 template <class C, bool B_TILES, bool FP8, int TM, int TN, int WM, int WN, int WK, int ST>
 __global__ __launch_bounds__(64 * WM * WN * WK) void prod8_tile_kernel(ProdArgs args) {
@@ -297,7 +310,8 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void prod8_tile_kernel(ProdArgs 
   static_assert((TM + TN) / 8 % NW == 0 && TM % 64 == 0 && TN % 64 == 0, "whole loads");
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const uint32_t block = xcd_order(blockIdx.x, gridDim.x);
-  const ProdOut out = prod_of(args, block);
+  const ProdTables tables = PROD_TABLES(args);
+  const ProdOut out = tables.of(block);
   const uint32_t tile = block - out.tile0, tiles_n = ((uint32_t)out.n + TN - 1) / TN;
   // eight rows of tiles are walked column by column: what an XCD works on at a time shares its operands in that XCD's L2
   const uint32_t band = tile / (8 * tiles_n), in_band = tile - band * 8 * tiles_n, high = min(8u, out.tiles_m - band * 8);
@@ -314,8 +328,8 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void prod8_tile_kernel(ProdArgs 
   uint32_t at_k = 0, into = 0;         // first k of the next block; where it goes in LDS
   lds_u32x4 ra, rb, rs[kScales];
   uint32_t voff[kLoads], soff[kScales], at_s[kScales], hop[kScales];
-  auto open = [&]() {                  // the buffers and offsets of the next segment
-    const ProdSeg seg = prod_seg(args, out.seg0 + ++seg_i);
+  auto open = [&]() __attribute__((always_inline)) {                  // the buffers and offsets of the next segment
+    const ProdSeg seg = tables.seg(out.seg0 + ++seg_i);
     const uint32_t k = (uint32_t)seg.k;
     left = (int)((k + 127) / 128);
     rest = (int)(k - (left - 1) * 128);
@@ -341,7 +355,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void prod8_tile_kernel(ProdArgs 
       at_s[i] = 0;
     }
   };
-  auto load = [&]() {                  // the next block to the next place; zeros behind the last one
+  auto load = [&]() __attribute__((always_inline)) {                  // the next block to the next place; zeros behind the last one
     if (left == 0 && seg_i + 1 < out.segs) open();
     const bool gone = left <= 0 || (left == 1 && piece >= rest);
 #pragma unroll
@@ -359,12 +373,12 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void prod8_tile_kernel(ProdArgs 
     --left;
     into = into == ST * kStage - kBlock ? 0 : into + kBlock;
   };
-  auto load_stage = [&]() {
+  auto load_stage = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < WK; ++i) load();
   };
   int total = 0;
-  for (int i = 0; i < out.segs; ++i) total += (int)((prod_seg(args, out.seg0 + i).k + 127) / 128);
+  for (int i = 0; i < out.segs; ++i) total += (int)((tables.seg(out.seg0 + i).k + 127) / 128);
   total = (total + WK - 1) / WK;
 
   v4f acc[NI][MI] = {};  // B's rows are the matrix instruction's rows, so that a lane holds four consecutive n of one m
@@ -387,7 +401,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void prod8_tile_kernel(ProdArgs 
 #pragma unroll
     for (int j = 0; j < NI; ++j) sb[j] = *(const uint8_t*)(at + at_sb + j * 64);
     if constexpr (FP8) {
-      auto both = [&](const char* p) {
+      auto both = [&](const char* p) __attribute__((always_inline)) {
         const u32x4 lo = *(const u32x4*)(p + p0), hi = *(const u32x4*)(p + p1);
         v8i f;
 #pragma unroll
@@ -397,14 +411,13 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void prod8_tile_kernel(ProdArgs 
         }
         return f;
       };
+      if (s + ST - 1 < total) load_stage();
       v8i fa[MI];
 #pragma unroll
       for (int i = 0; i < MI; ++i) fa[i] = both(at + at_a + i * 2048);
-      v8i fb = both(at + at_b);
-      if (s + ST - 1 < total) load_stage();
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
-        if (j > 0) fb = both(at + at_b + j * 2048);
+        const v8i fb = both(at + at_b + j * 2048);
 #pragma unroll
         for (int i = 0; i < MI; ++i)
           acc[j][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, fa[i], acc[j][i], 0, 0, 0, sb[j], 0, sa[i]);
@@ -439,22 +452,24 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void prod8_tile_kernel(ProdArgs 
       }
     }
   }
-  if constexpr (WK == 2) {
-    static_assert(TM * TN * 4 <= ST * kStage, "the sums of half the waves fit where the stages were");
-    v4f* const half = (v4f*)lds + (wave % (WM * WN)) * (NI * MI * 64) + lane;
+  if constexpr (WK > 1) {
+    static_assert((WK - 1) * TM * TN * 4 <= ST * kStage, "the other waves' sums fit where the stages were");
+    v4f* const sums = (v4f*)lds + (wave % (WM * WN)) * (NI * MI * 64) + lane;
     lds_barrier();  // (no load is under way: the last stage was waited for)
-    if (wk == 1) {
+    if (wk > 0) {
 #pragma unroll
       for (int j = 0; j < NI; ++j)
 #pragma unroll
-        for (int i = 0; i < MI; ++i) half[(j * MI + i) * 64] = acc[j][i];
+        for (int i = 0; i < MI; ++i) sums[((wk - 1) * WM * WN * NI * MI + j * MI + i) * 64] = acc[j][i];
     }
     lds_barrier();
-    if (wk == 1) return;
+    if (wk > 0) return;
 #pragma unroll
-    for (int j = 0; j < NI; ++j)
+    for (int w = 0; w < WK - 1; ++w)
 #pragma unroll
-      for (int i = 0; i < MI; ++i) acc[j][i] += half[(j * MI + i) * 64];
+      for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int i = 0; i < MI; ++i) acc[j][i] += sums[(w * WM * WN * NI * MI + j * MI + i) * 64];
   }
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
@@ -554,7 +569,7 @@ static int launch_prod_as(ProdArgs& args, std::vector<ProdOut>& outs, const std:
     else return launch_prod_tile<C, B_TILES, false, 256, 128, 4, 2, 1, 3>(args, tiles, st);
   }
   if (kind == kMiddle) return launch_prod_tile<C, B_TILES, false, 128, 128, 2, 2, 2, 2>(args, tiles, st);
-  if (kind == kSmall) return launch_prod_tile<C, B_TILES, false, 64, 64, 2, 2, 2, 4>(args, tiles, st);
+  if (kind == kSmall) return launch_prod_tile<C, B_TILES, false, 64, 64, 1, 2, 4, 2>(args, tiles, st);
   const dim3 grid((unsigned)tiles);
   if (kind == kAny) hipLaunchKernelGGL((prod8_any_kernel<C, B_TILES>), grid, dim3(256), 0, st, args);
   else if (rows <= 16) hipLaunchKernelGGL((prod8_rows_kernel<C, B_TILES, 1, 4>), grid, dim3(512), 0, st, args);

@@ -44,10 +44,12 @@ struct ScanArgs {
 
 // Worker p's arrays, from the table or from the launch's own arguments (of which they are the first).  Read as constants, into scalar
 // registers: a vector load of them would wait for all data under way, and the compiler would take what it gives for different in each lane.
-__device__ __forceinline__ ScanWorker scan_worker(const ScanArgs& s, int p) {
-  static_assert(offsetof(ScanArgs, w) == 0, "the kernels' first argument starts with the workers");
-  typedef const __attribute__((address_space(4))) ScanWorker* Constant;
-  const Constant w = (s.more ? (Constant)(uint64_t)s.more : (Constant)__builtin_amdgcn_kernarg_segment_ptr()) + p;
+// The table's address is taken in the kernel itself: the arguments' is not known in a function that the compiler might not inline.
+static_assert(offsetof(ScanArgs, w) == 0, "the kernels' first argument starts with the workers");
+typedef const __attribute__((address_space(4))) ScanWorker* ScanTable;
+#define SCAN_TABLE(s) ((s).more ? (ScanTable)(uint64_t)(s).more : (ScanTable)__builtin_amdgcn_kernarg_segment_ptr())
+__device__ __forceinline__ ScanWorker scan_worker(ScanTable table, int p) {
+  const ScanTable w = table + p;
   return ScanWorker{w->a, w->x, w->h, w->dh, w->o0, w->o1};
 }
 
@@ -251,6 +253,7 @@ template <class E, int GATE, bool PAIR, bool BACK>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
   constexpr int L = 8;
   __shared__ float lds[kScanWaves][2][kScanCols];
+  const ScanTable table = SCAN_TABLE(s);
   const ScanPlace at = scan_place<PAIR>(s, BACK);
   const int lane = threadIdx.x & 63, wave = BACK ? kScanWaves - 1 - scan_wave() : scan_wave();
   const int hi = min(at.hi, at.len), each = (max(0, hi - at.lo) + kScanWaves - 1) / kScanWaves;
@@ -260,11 +263,11 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
   typedef ScanRaw<E, PAIR> Raw;
   Raw ra[2][L], rx[2][L];  // a run of at most L steps of one worker and the next one, forwards or backwards
   const int steps = to - from;
-  auto load = [&](int done, Raw* a, Raw* x) {
+  auto load = [&](int done, Raw* a, Raw* x) __attribute__((always_inline)) {
     const int t = BACK ? to - 1 - done : from + done;
     const ScanSpan sp = scan_span(s, done < steps ? t : 0);
     const int cnt = done < steps ? min(L, BACK ? t + 1 - max(from, sp.lo) : min(to, sp.hi) - t) : 0;
-    const ScanWorker w = scan_worker(s, sp.p);
+    const ScanWorker w = scan_worker(table, sp.p);
     const int64_t row = ((int64_t)at.b * (sp.hi - sp.lo) + (t - sp.lo) - (BACK ? cnt - 1 : 0)) * s.n_c + at.c;
     const auto pa = scan_rows((const E*)w.a + row), px = scan_rows((const E*)(BACK ? w.dh : w.x) + row);
 #pragma unroll
@@ -282,8 +285,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
     A[v] = 1.f;
     B[v] = 0.f;
   }
-  auto compose = [&](const Raw* ar, const Raw* xr, int cnt) {
-    auto one = [&](int i, bool in) {
+  auto compose = [&](const Raw* ar, const Raw* xr, int cnt) __attribute__((always_inline)) {
+    auto one = [&](int i, bool in) __attribute__((always_inline)) {
       float g[kScanV], x[kScanV];
       ar[i].values(g);
       xr[i].values(x);
@@ -354,12 +357,13 @@ template <class E, int GATE, bool PAIR>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
   constexpr int L = 8;
   __shared__ float lds[2][kScanWaves][2][kScanCols];
+  const ScanTable table = SCAN_TABLE(s);
   const ScanPlace at = scan_place<PAIR>(s, s.segments > 1);
   const int wave = scan_wave();
   const ScanLane off = scan_lane<E, PAIR>(s.n_c - at.c);
   const uint32_t hop = (uint32_t)(s.n_c * sizeof(E));
   ScanRaw<E, PAIR> ra[L], rx[L];
-  auto tile = [&](int t0, bool is) {
+  auto tile = [&](int t0, bool is) __attribute__((always_inline)) {
     ScanTile t;
     const ScanSpan sp = scan_span(s, t0);
     t.p = sp.p;
@@ -369,7 +373,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
     t.cnt = is ? max(0, min(L, t.next - t.from)) : 0;
     t.live = max(0, min(t.cnt, at.len - t.from));
     t.row = ((int64_t)at.b * (sp.hi - sp.lo) + (t.from - sp.lo)) * s.n_c + at.c;
-    const ScanWorker w = scan_worker(s, t.p);
+    const ScanWorker w = scan_worker(table, t.p);
     const auto pa = scan_rows((const E*)w.a + t.row), px = scan_rows((const E*)w.x + t.row);
 #pragma unroll
     for (int i = 0; i < L; ++i) {
@@ -426,7 +430,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
 #pragma unroll
         for (int v = 0; v < kScanV; ++v) u[i][v] = i < now.live ? u[i][v] : 0.f;
     }
-    const auto po = scan_rows((E*)scan_worker(s, now.p).o0 + now.row);
+    const auto po = scan_rows((E*)scan_worker(table, now.p).o0 + now.row);
 #pragma unroll
     for (int i = 0; i < L; ++i) scan_put<E, PAIR>(po, off.where(i < now.cnt), i * hop, u[i]);
     if (!more) break;
@@ -440,12 +444,13 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
   constexpr int L = sizeof(ScanRaw<E, PAIR>) == 4 ? 8 : 4;  // what the registers hold beside the next tile's loads
   constexpr bool X = GATE != DISTDL_GATE_GIVEN;
   __shared__ float lds[2][kScanWaves][2][kScanCols];
+  const ScanTable table = SCAN_TABLE(s);
   const ScanPlace at = scan_place<PAIR>(s, s.segments == 1);
   const int wave = scan_wave(), lane = threadIdx.x & 63;
   const ScanLane off = scan_lane<E, PAIR>(s.n_c - at.c);
   const uint32_t hop = (uint32_t)(s.n_c * sizeof(E));
   ScanRaw<E, PAIR> ra[L], rx[L], rd[L], rh[L], edge;  // edge: the state before a worker's first step, the last one of the worker before
-  auto tile = [&](int t1, bool is) {
+  auto tile = [&](int t1, bool is) __attribute__((always_inline)) {
     ScanTile t;
     const ScanSpan sp = scan_span(s, t1 - 1);
     t.p = sp.p;
@@ -455,7 +460,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
     t.cnt = is ? max(0, min(L, t.from + 1 - t.next)) : 0;
     t.live = t.cnt - max(0, min(t.cnt, t.from + 1 - at.len));  // (steps behind the sequence's end come first)
     t.row = ((int64_t)at.b * (sp.hi - sp.lo) + (t.from - t.cnt + 1 - sp.lo)) * s.n_c + at.c;
-    const ScanWorker w = scan_worker(s, t.p);
+    const ScanWorker w = scan_worker(table, t.p);
     const auto pa = scan_rows((const E*)w.a + t.row), pd = scan_rows((const E*)w.dh + t.row), ph = scan_rows((const E*)w.h + t.row - s.n_c);
     const auto px = scan_rows((const E*)(X ? w.x : w.a) + t.row);
 #pragma unroll
@@ -470,7 +475,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
     }
     const bool first = t.live > 0 && t.from - t.cnt + 1 == t.lo && t.lo > 0;
     const ScanSpan b = scan_span(s, first ? t.lo - 1 : 0);
-    edge.load(scan_rows((const E*)scan_worker(s, b.p).h + ((int64_t)at.b * (b.hi - b.lo) + (b.hi - b.lo - 1)) * s.n_c + at.c), off.where(first), 0);
+    edge.load(scan_rows((const E*)scan_worker(table, b.p).h + ((int64_t)at.b * (b.hi - b.lo) + (b.hi - b.lo - 1)) * s.n_c + at.c), off.where(first), 0);
     return t;
   };
   float start[kScanV];  // the state in front of step 0, in 32 bits
@@ -526,7 +531,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
     const bool more = now.next > at.lo;
     t = tile(more ? now.next : now.next + 1, more);
     scan_meet(lds[turn], A, B, state, back);
-    const ScanWorker w = scan_worker(s, now.p);
+    const ScanWorker w = scan_worker(table, now.p);
     const auto o0 = scan_rows((E*)w.o0 + now.row), o1 = scan_rows((E*)w.o1 + now.row);
 #pragma unroll
     for (int i = 0; i < L; ++i) {
