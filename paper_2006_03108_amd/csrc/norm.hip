@@ -499,7 +499,7 @@ static void launch_norm_fwd(const NormArgs& a, hipStream_t st) {
   norm_shape<false>(a.pieces, [&](auto W, auto R, auto wide) {
     const int rows = norm_threads(W) / (64 * W);
     const int64_t groups = (a.rows + rows - 1) / rows;
-    hipLaunchKernelGGL((norm_fwd_kernel<E, W, R, ROWS16, wide>), dim3((unsigned)std::min<int64_t>(groups, 8192 / W)), dim3(norm_threads(W)), 0, st, a);
+    hipLaunchKernelGGL((norm_fwd_kernel<E, W, R, ROWS16, wide>), dim3((unsigned)std::min<int64_t>(groups, 4096 / W)), dim3(norm_threads(W)), 0, st, a);
   });
 }
 
