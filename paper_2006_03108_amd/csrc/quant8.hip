@@ -5,6 +5,7 @@
 // threads, whose magnitudes meet in LDS.  A thread's 8 x 8 codes are turned in registers and go through LDS, so that both orders
 // are written in runs of a whole block.
 #include <algorithm>
+#include <cstddef>
 
 #include "block8.h"
 #include "common.h"
@@ -25,15 +26,22 @@ struct QuantArgs {
   const QuantArray* more;
   int32_t n;
 };
+// The table's address is taken in the kernel itself, and its records are read as constants, into scalar registers.
+static_assert(offsetof(QuantArgs, a) == 0, "the kernel's first argument starts with the arrays");
+typedef const __attribute__((address_space(4))) QuantArray* QuantTable;
+#define QUANT_TABLE(s) ((s).more ? (QuantTable)(uint64_t)(s).more : (QuantTable)__builtin_amdgcn_kernarg_segment_ptr())
 
 // TILES: one scale for the tile.  Otherwise each order has blocks of its own.
 template <class E, bool TILES>
 __global__ __launch_bounds__(256) void quant8_kernel(QuantArgs args) {
   __shared__ float meet[4][kBlock8];
-  __shared__ alignas(16) uint8_t turned[kBlock8][kBlock8 + 16];
+  // column c's 16-byte piece p lies at p ^ ((c >> 3) & 7): the lanes of a wave write eight columns apart
+  __shared__ alignas(16) uint8_t turned[kBlock8][kBlock8];
+  const QuantTable table = QUANT_TABLE(args);
   int i = 0;
-  while (i + 1 < args.n && blockIdx.x >= (args.more ? args.more[i + 1].tile0 : args.a[i + 1].tile0)) ++i;
-  const QuantArray m = args.more ? args.more[i] : args.a[i];
+  while (i + 1 < args.n && blockIdx.x >= table[i + 1].tile0) ++i;
+  const QuantTable t = table + i;
+  const QuantArray m{t->x, t->q, t->s, t->qt, t->st, t->rows, t->cols, t->tile0, t->tiles_c};
   const uint32_t tile = blockIdx.x - m.tile0;
   const int64_t r0 = (int64_t)(tile / m.tiles_c) * kBlock8, c0 = (int64_t)(tile % m.tiles_c) * kBlock8;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -96,7 +104,7 @@ __global__ __launch_bounds__(256) void quant8_kernel(QuantArgs args) {
     for (int j = 0; j < 8; ++j) {
       const int byte = scale_byte(cmax[j]);
       const float inv = scale_inverse(byte);
-      *(u32x2*)&turned[tx * 8 + j][ty * 8] = u32x2{pack_e4m3(v[0][j] * inv, v[1][j] * inv, v[2][j] * inv, v[3][j] * inv),
+      *(u32x2*)&turned[tx * 8 + j][((ty >> 1) ^ (tx & 7)) * 16 + (ty & 1) * 8] = u32x2{pack_e4m3(v[0][j] * inv, v[1][j] * inv, v[2][j] * inv, v[3][j] * inv),
                                                    pack_e4m3(v[4][j] * inv, v[5][j] * inv, v[6][j] * inv, v[7][j] * inv)};
       if (!TILES && ty == 0 && j < n) m.st[(r0 >> 7) * m.cols + col + j] = (uint8_t)byte;
       if (TILES && threadIdx.x == 0 && j == 0) m.st[(c0 >> 7) * ((m.rows + kBlock8 - 1) >> 7) + (r0 >> 7)] = (uint8_t)byte;
@@ -106,13 +114,14 @@ __global__ __launch_bounds__(256) void quant8_kernel(QuantArgs args) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int c = (threadIdx.x >> 3) + 32 * k, piece = (threadIdx.x & 7) * 16;
+      const uint8_t* const from = &turned[c][piece ^ ((c >> 3) & 7) * 16];
       if (c0 + c >= m.cols) continue;
       const int left = (int)max((int64_t)0, min((int64_t)16, m.rows - r0 - piece));
       uint8_t* to = m.qt + (c0 + c) * m.rows + r0 + piece;
       if (left == 16) {
-        *(u32x4_any*)to = *(const u32x4*)&turned[c][piece];
+        *(u32x4_any*)to = *(const u32x4*)from;
       } else {
-        for (int b = 0; b < left; ++b) to[b] = turned[c][piece + b];
+        for (int b = 0; b < left; ++b) to[b] = from[b];
       }
     }
   }
