@@ -10,6 +10,7 @@
 #include <algorithm>
 #include <cstddef>
 #include <type_traits>
+#include <unordered_map>
 
 #include "block8.h"
 #include "buffer.h"
@@ -139,80 +140,33 @@ __device__ __forceinline__ void prod_store(uint16_t* c, int m, int n, int cols, 
   }
 }
 
-// Any sizes, strides of rows and alignment: 128 x 128 results a workgroup, 64 x 64 a wave, 128 k at a time through LDS.  The 16-byte
-// piece p of row r lies at piece p ^ (r & 7), so that the eight rows that lanes read together lie in different banks.
-template <class C, bool B_TILES>
-__global__ __launch_bounds__(256) void prod8_any_kernel(ProdArgs args) {
-  __shared__ u32x4 lds[2][kBlock8][8];
-  const ProdTables tables = PROD_TABLES(args);
-  const ProdOut out = tables.of(blockIdx.x);
-  const uint32_t tile = blockIdx.x - out.tile0;
-  const int m0 = (int)(tile % out.tiles_m) * 128, n0 = (int)(tile / out.tiles_m) * 128;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64, r16 = lane & 15, g = lane >> 4;
-  v4f acc[4][4] = {};  // [n][m]: B's rows are the matrix instruction's rows, so that a lane holds four consecutive n of one m
-  for (int sg = 0; sg < out.segs; ++sg) {
-    const ProdSeg seg = tables.seg(out.seg0 + sg);
-    const int k = (int)seg.k, blocks = (k + kBlock8 - 1) / kBlock8;
-    for (int64_t kb = 0; kb < blocks; ++kb) {
-      u32x4 ra[4], rb[4];
-      auto fetch = [&](auto whole) __attribute__((always_inline)) {
+// Rows of any length and alignment to rows of whole 16-byte pieces, zeros behind their end: what tiles read where an operand's rows are
+// neither.  One pass over the operands; the products of more than 64 rows that follow take several times as long.
+struct ProdCopy {
+  const uint8_t* from;
+  u32x4* to;
+  uint32_t n, pieces, total, block0;  // codes of a row; pieces of a row, of all rows; first workgroup
+};
+constexpr int kCopyInline = 32;
+struct ProdCopies {
+  ProdCopy c[kCopyInline];
+  const ProdCopy* more;
+  int32_t n;
+};
+__global__ __launch_bounds__(256) void prod8_pieces_kernel(ProdCopies args) {
+  static_assert(offsetof(ProdCopies, c) == 0, "the kernel's first argument starts with the copies");
+  typedef const __attribute__((address_space(4))) ProdCopy* Table;
+  const Table table = args.more ? (Table)(uint64_t)args.more : (Table)__builtin_amdgcn_kernarg_segment_ptr();
+  int i = 0;
+  while (i + 1 < args.n && blockIdx.x >= table[i + 1].block0) ++i;
+  const Table c = table + i;
+  const uint32_t first = (blockIdx.x - c->block0) * 1024 + threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          // (rows that are not there are the last one once more: what comes of them is not stored)
-          const int r = i * 32 + (threadIdx.x >> 3), at = (int)kb * kBlock8 + (threadIdx.x & 7) * 16;
-          ra[i] = load16_codes<decltype(whole)::value>(seg.a + (int64_t)min(m0 + r, out.m - 1) * k, at, k);
-          rb[i] = load16_codes<decltype(whole)::value>(seg.b + (int64_t)min(n0 + r, out.n - 1) * k, at, k);
-        }
-      };
-      if (kb < blocks - 1 || (k & 127) == 0) fetch(std::true_type());
-      else fetch(std::false_type());
-      int sa[4], sb[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t m = min(m0 + wm + i * 16 + r16, out.m - 1), n = min(n0 + wn + i * 16 + r16, out.n - 1);
-        sa[i] = seg.as[kb * out.m + m];
-        sb[i] = B_TILES ? seg.bs[(n >> 7) * blocks + kb] : seg.bs[kb * out.n + n];
-      }
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = i * 32 + (threadIdx.x >> 3), p = threadIdx.x & 7;
-        lds[0][r][p ^ (r & 7)] = ra[i];
-        lds[1][r][p ^ (r & 7)] = rb[i];
-      }
-      __syncthreads();
-      auto piece = [&](int side, int row, int p) __attribute__((always_inline)) { return lds[side][row][(g + 4 * p) ^ (row & 7)]; };
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        v8bf fa[4][2];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const u32x4 c = piece(0, wm + i * 16 + r16, p);
-          const float s = scale_exponent(sa[i]);
-          fa[i][0] = codes_to_bf16(c[0], c[1], s);
-          fa[i][1] = codes_to_bf16(c[2], c[3], s);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const u32x4 c = piece(1, wn + j * 16 + r16, p);
-          const float s = scale_exponent(sb[j]);
-          const v8bf b0 = codes_to_bf16(c[0], c[1], s), b1 = codes_to_bf16(c[2], c[3], s);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b0, fa[i][0], acc[j][i], 0, 0, 0);
-            acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b1, fa[i][1], acc[j][i], 0, 0, 0);
-          }
-        }
-      }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int m = m0 + wm + i * 16 + r16;
-    if (m >= out.m) continue;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) prod_store((C*)out.c, m, n0 + wn + j * 16 + g * 4, out.n, acc[j][i]);
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t at = first + 256 * k;
+    if (at >= c->total) break;
+    const uint32_t row = at / c->pieces, p = at - row * c->pieces;
+    c->to[at] = load16_codes<false>(c->from + (int64_t)row * c->n, (int)p * 16, (int)c->n);
   }
 }
 
@@ -292,8 +246,7 @@ __global__ __launch_bounds__(512) void prod8_rows_kernel(ProdArgs args) {
   }
 }
 
-// ---- rows of whole 16-byte pieces -------------------------------------------
-// TM x TN results a workgroup of WM x WN waves, 128 k a stage, ST stages in LDS.  Stages are filled by loads that go straight to LDS (no
+// Rows of whole 16-byte pieces.  TM x TN results a workgroup of WM x WN waves, 128 k a stage, ST stages in LDS.  Stages are filled by loads that go straight to LDS (no
 // registers, no instructions to store them) while earlier ones are multiplied; a stage costs one barrier.  A wave's load brings eight
 // rows of 128 bytes: lane L asks for piece (L & 7) ^ (L >> 3) of row L >> 3, so that row r's piece p lies at p ^ (r & 7) and the lanes
 // that read together find different banks.  Rows and pieces that are not there fail the check of their buffer and arrive as zeros.
@@ -489,6 +442,8 @@ struct distdl_linear8_plan {
   std::vector<int64_t> fo, fi;  // features of each worker
   distdl::DevArray<distdl::ProdOut> outs;
   distdl::DevArray<distdl::ProdSeg> segs;
+  distdl::DevArray<distdl::ProdCopy> copies;
+  distdl::StreamScratch pieces;
 };
 
 namespace distdl {
@@ -510,13 +465,50 @@ static int64_t prod_tiles(std::vector<ProdOut>& outs, int TM, int TN) {
   return tiles;
 }
 
-// Whether rows are whole 16-byte pieces and all offsets within a tile fit 31 bits.
-static bool prod_pieces(const std::vector<ProdOut>& outs, const std::vector<ProdSeg>& segs) {
-  int64_t most = 0;
-  for (const ProdOut& o : outs) most = std::max<int64_t>(most, std::max(o.m, o.n));
-  for (const ProdSeg& g : segs)
-    if (((uintptr_t)g.a | (uintptr_t)g.b) % 16 || g.k % 16 || g.k > 1 << 22 || most * (g.k / 128 + 1) >= kOob) return false;
-  return true;
+// Makes the rows of all operands whole 16-byte pieces: those that are not are copied to the plan's scratch.
+static int prod_pieces(distdl_linear8_plan* p, const std::vector<ProdOut>& outs, std::vector<ProdSeg>& segs, hipStream_t st) {
+  std::unordered_map<const void*, size_t> seen;  // an operand of several results is copied once: its place in `copies`
+  std::vector<ProdCopy> copies;
+  std::vector<std::pair<const uint8_t**, size_t>> users;
+  int64_t pieces = 0, blocks = 0;
+  for (const ProdOut& o : outs)
+    for (int i = o.seg0; i < o.seg0 + o.segs; ++i) {
+      ProdSeg& g = segs[i];
+      const int64_t wide = (g.k + 15) / 16;
+      const struct {
+        const uint8_t** p;
+        int64_t rows;
+      } sides[2] = {{&g.a, o.m}, {&g.b, o.n}};
+      for (const auto& side : sides) {
+        if (g.k % 16 == 0 && (uintptr_t)*side.p % 16 == 0) continue;
+        const auto it = seen.emplace(*side.p, copies.size());
+        if (it.second) {
+          const int64_t total = side.rows * wide;
+          if (total >= int64_t(1) << 31 || (blocks += (total + 1023) / 1024) >= kMaxBlocks256) return set_error(DISTDL_ERR_UNSUPPORTED, "linear8: problem too large");
+          copies.push_back(ProdCopy{*side.p, (u32x4*)(pieces * 16), (uint32_t)g.k, (uint32_t)wide, (uint32_t)total, (uint32_t)(blocks - (total + 1023) / 1024)});
+          pieces += total;
+        }
+        users.emplace_back(side.p, it.first->second);
+      }
+    }
+  for (ProdSeg& g : segs) g.k = (g.k + 15) / 16 * 16;
+  if (copies.empty()) return DISTDL_OK;
+  float* scratch = nullptr;
+  int rc = p->pieces.get((size_t)pieces * 4, st, &scratch);
+  if (rc) return rc;
+  for (ProdCopy& c : copies) c.to = (u32x4*)((char*)scratch + (uintptr_t)c.to);
+  for (const auto& u : users) *u.first = (const uint8_t*)copies[u.second].to;
+  ProdCopies args;
+  args.n = (int32_t)copies.size();
+  args.more = nullptr;
+  if (copies.size() <= (size_t)kCopyInline) {
+    std::copy(copies.begin(), copies.end(), args.c);
+  } else {
+    if ((rc = p->copies.upload(copies, st))) return rc;
+    args.more = p->copies.dev;
+  }
+  hipLaunchKernelGGL(prod8_pieces_kernel, dim3((unsigned)blocks), dim3(256), 0, st, args);
+  return DISTDL_OK;
 }
 
 template <class C, bool B_TILES, bool FP8, int TM, int TN, int WM, int WN, int WK, int ST>
@@ -530,27 +522,31 @@ static int launch_prod_tile(const ProdArgs& args, int64_t tiles, hipStream_t st)
 }
 
 template <class C, bool B_TILES>
-static int launch_prod_as(ProdArgs& args, std::vector<ProdOut>& outs, const std::vector<ProdSeg>& segs, distdl_linear8_plan* p, hipStream_t st) {
-  enum { kAny, kRows, kSmall, kMiddle, kLarge } kind = kAny;
-  int64_t tiles = 0, rows = 0;
+static int launch_prod_as(ProdArgs& args, std::vector<ProdOut>& outs, std::vector<ProdSeg>& segs, distdl_linear8_plan* p, hipStream_t st) {
+  enum { kRows, kSmall, kMiddle, kLarge } kind;
+  int64_t tiles = 0, rows = 0, longest = 0;
   for (const ProdOut& o : outs) rows = std::max<int64_t>(rows, o.m);
+  for (const ProdSeg& g : segs) longest = std::max<int64_t>(longest, g.k);
   if (rows <= 64) {
     kind = kRows;
-  } else if (prod_pieces(outs, segs)) {
-    // Large tiles need less of their operands from L2, but there have to be enough of them to keep the compute units busy.
+    tiles = prod_tiles(outs, 64, 16);
+  } else {
+    // Offsets within a tile have 31 bits.  Large tiles need less of their operands from L2, but there have to be enough of them to keep the
+    // compute units busy.
+    if (longest > 1 << 24) return set_error(DISTDL_ERR_UNSUPPORTED, "linear8: a sum of %lld products for more than 64 rows", (long long)longest);
+    const int rc = prod_pieces(p, outs, segs, st);
+    if (rc) return rc;
     tiles = prod_tiles(outs, 256, sizeof(C) == 2 ? 256 : 128);
     kind = kLarge;
     if (tiles < 160) {
       tiles = prod_tiles(outs, 128, 128);
       kind = kMiddle;
     }
-    if (tiles < 128) {
+    if (tiles < 128 || longest > 1 << 22) {
       tiles = prod_tiles(outs, 64, 64);
       kind = kSmall;
     }
   }
-  if (kind == kRows) tiles = prod_tiles(outs, 64, 16);
-  if (kind == kAny) tiles = prod_tiles(outs, 128, 128);
   if (tiles >= kMaxBlocks256 / 2) return set_error(DISTDL_ERR_UNSUPPORTED, "linear8: problem too large");
   args.n_out = (int32_t)outs.size();
   args.more_out = nullptr;
@@ -571,14 +567,13 @@ static int launch_prod_as(ProdArgs& args, std::vector<ProdOut>& outs, const std:
   if (kind == kMiddle) return launch_prod_tile<C, B_TILES, false, 128, 128, 2, 2, 2, 2>(args, tiles, st);
   if (kind == kSmall) return launch_prod_tile<C, B_TILES, false, 64, 64, 1, 2, 4, 2>(args, tiles, st);
   const dim3 grid((unsigned)tiles);
-  if (kind == kAny) hipLaunchKernelGGL((prod8_any_kernel<C, B_TILES>), grid, dim3(256), 0, st, args);
-  else if (rows <= 16) hipLaunchKernelGGL((prod8_rows_kernel<C, B_TILES, 1, 4>), grid, dim3(512), 0, st, args);
+  if (rows <= 16) hipLaunchKernelGGL((prod8_rows_kernel<C, B_TILES, 1, 4>), grid, dim3(512), 0, st, args);
   else if (rows <= 32) hipLaunchKernelGGL((prod8_rows_kernel<C, B_TILES, 2, 2>), grid, dim3(512), 0, st, args);
   else hipLaunchKernelGGL((prod8_rows_kernel<C, B_TILES, 4, 2>), grid, dim3(512), 0, st, args);
   return DISTDL_OK;
 }
 
-static int launch_prod(distdl_linear8_plan* p, std::vector<ProdOut>& outs, const std::vector<ProdSeg>& segs, bool f32, bool b_tiles,
+static int launch_prod(distdl_linear8_plan* p, std::vector<ProdOut>& outs, std::vector<ProdSeg>& segs, bool f32, bool b_tiles,
                        const char* name, hipStream_t st) {
   ProdArgs args;
   int rc;
@@ -627,6 +622,8 @@ int distdl_linear8_plan_destroy(distdl_linear8_plan* p) {
   if (!p) return DISTDL_OK;
   p->outs.release();
   p->segs.release();
+  p->copies.release();
+  p->pieces.release();
   delete p;
   return DISTDL_OK;
 }
