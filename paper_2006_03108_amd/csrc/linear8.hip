@@ -5,8 +5,20 @@
 //   weight gradient   dW_ij = dy_i^T x_j               the transposes of both in blocks of rows (along the batch)
 //
 // All three are C[m][n] = sum over segments and k of A[m][k] B[n][k] with k contiguous in both; a worker of the sum is a segment, whose
-// blocks start anew.  Codes times scales are exact in bf16 (one instruction for two), so bf16 matrix instructions
-// add exact products in fp32; measured, sums of 128 to 8192 products of N(0, 1) operands are 1e-8 to 3e-7 of their size off.
+// blocks start anew.  Sums are fp32, from one of two matrix instructions:
+//
+//   v_mfma_scale_f32_16x16x128_f8f6f4 takes codes and scales as they are, at 5 PFLOP/s, but adds eight neighbouring products at a time in a
+//   window: beside a product of 2^8 and 2^8, what lies below 2^3 is cut off (measured, each of the 127 other places; the
+//   groups' sums and the accumulator keep all 24 bits).  A result is off by at most 2^-10 of the sum of the groups' largest products,
+//   1.3e-5 of its size for N(0, 1) operands: 1/300 of a bf16 result's last place.  Bf16 results of large products take it.
+//
+//   v_mfma_f32_16x16x32_bf16 takes codes times scales, which are exact in bf16 (an instruction converts two), at 2.5 PFLOP/s: sums of 128 to 8192
+//   N(0, 1) products are 1e-8 to 3e-7 off.  Fp32 results take it (weight gradients among them), and products whose time
+//   is not that of the matrix instructions.
+//
+// Measured (us): 8 x 4096 x 4096 6.9 (2.4 TB/s of weights; a launch and a trip to memory are most of it), 256 x 4096 x 4096 on 2 x 2 workers 17,
+// 8192 x 4096 x 4096 142 (1.94 PFLOP/s, 73 % of the library's 8192^3), the same in fp32 270 to 290 (0.95 to 1.02 PFLOP/s: conversions, of
+// which a wave makes one for 2.7 products).
 #include <algorithm>
 #include <cstddef>
 #include <type_traits>
@@ -531,21 +543,20 @@ static int launch_prod_as(ProdArgs& args, std::vector<ProdOut>& outs, std::vecto
     kind = kRows;
     tiles = prod_tiles(outs, 64, 16);
   } else {
-    // Offsets within a tile have 31 bits.  Large tiles need less of their operands from L2, but there have to be enough of them to keep the
-    // compute units busy.
+    // Offsets within a tile have 31 bits.
     if (longest > 1 << 24) return set_error(DISTDL_ERR_UNSUPPORTED, "linear8: a sum of %lld products for more than 64 rows", (long long)longest);
     const int rc = prod_pieces(p, outs, segs, st);
     if (rc) return rc;
-    tiles = prod_tiles(outs, 256, sizeof(C) == 2 ? 256 : 128);
+    // What a round of 256 tiles takes for a block of k, in units of 0.05 us: measured at K = 2048 and 4096, 0.59 to 0.67 us for 64 x 64, 1.2 to 1.5
+    // for 128 x 128, 1.9 for 256 x 256 on 8-bit instructions, 2.2 for 256 x 128 on bf16 ones.  (2048 x 4096 x 4096, 128 large
+    // tiles: 61 us for 74 with 512 of 128 x 128; in fp32, 2048^3, 128 large tiles: 35 us for 24 with 256.)
+    const int64_t small = prod_tiles(outs, 64, 64), middle = prod_tiles(outs, 128, 128), large = prod_tiles(outs, 256, sizeof(C) == 2 ? 256 : 128);
+    const auto rounds = [](int64_t n) { return (n + 255) / 256; };
+    const int64_t cost[3] = {rounds(small) * 13, rounds(middle) * 26, rounds(large) * (sizeof(C) == 2 ? 38 : 44)};
     kind = kLarge;
-    if (tiles < 160) {
-      tiles = prod_tiles(outs, 128, 128);
-      kind = kMiddle;
-    }
-    if (tiles < 128 || longest > 1 << 22) {
-      tiles = prod_tiles(outs, 64, 64);
-      kind = kSmall;
-    }
+    if (cost[1] < cost[2]) kind = kMiddle;
+    if (cost[0] < std::min(cost[1], cost[2]) || longest > 1 << 22) kind = kSmall;
+    tiles = kind == kLarge ? large : kind == kMiddle ? prod_tiles(outs, 128, 128) : prod_tiles(outs, 64, 64);
   }
   if (tiles >= kMaxBlocks256 / 2) return set_error(DISTDL_ERR_UNSUPPORTED, "linear8: problem too large");
   args.n_out = (int32_t)outs.size();

@@ -123,6 +123,39 @@ def test_layer(n_b, n_fi, n_fo, P_fo, P_fi, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_tiles(dtype):
+    """Enough work for the largest tiles, with partial ones at both edges and a short last block.  fp32 results as above.  bf16 ones come
+    from the codes' own instruction, which adds eight neighbouring products in a window 2^13 below the largest exponent of the eight and
+    cuts off what lies below it: each product is off by less than 2^-13 of the largest, so a result by 2^-10 of the sum of the largest of
+    each eight, and by 2^-8 of itself for its rounding."""
+    require_gpu()
+    n_b, n_fi, n_fo = 2600, 400, 4040
+    g = torch.Generator(device="cuda").manual_seed(8)
+    rnd = lambda r, c: torch.randn(r, c, generator=g, device="cuda") * torch.exp(torch.randn(r, 1, generator=g, device="cuda"))  # noqa: E731
+    x, w = rnd(n_b, n_fi), rnd(n_fo, n_fi)
+    (xq, xs, xv), (wq, ws, wv) = quantised(x), quantised(w, tiles=True)
+    plan = dd.distdl_linear8_plan_create(n_b, n_fi, n_fo, 1, 1, KINDS[dtype])
+    y = torch.full((n_b, n_fo), 7.0, dtype=KINDS[dtype], device="cuda")
+    dd.distdl_linear8_fwd(plan, [xq], [xs], [wq], [ws], [y])
+    a, b = torch.tensor(xv, device="cuda"), torch.tensor(wv, device="cuda")
+    want = a @ b.t().contiguous()
+    if dtype == "f32":
+        tol = (n_fi / 32 + 4) * 2.0 ** -23 * (a.abs() @ b.abs().t().contiguous())
+    else:
+        tol = 2.0 ** -8 * want.abs()
+        for k in range(0, n_fi, 8):
+            most = torch.zeros_like(want)
+            for i in range(k, k + 8):
+                torch.maximum(most, a[:, i, None].abs() * b[None, :, i].abs(), out=most)
+            tol += 2.0 ** -10 * most
+    off = (y.double() - want).abs() > tol
+    assert not off.any(), f"{int(off.sum())} of {off.numel()} off"
+    again = torch.empty_like(y)
+    dd.distdl_linear8_fwd(plan, [xq], [xs], [wq], [ws], [again])
+    assert torch.equal(y, again)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n_b", [3, 40, 300])
 def test_arrays_that_start_anywhere(n_b, dtype):
     """Codes, scales and results one element into an allocation give the same numbers."""
