@@ -21,7 +21,6 @@
 // which a wave makes one for 2.7 products).
 #include <algorithm>
 #include <cstddef>
-#include <type_traits>
 #include <unordered_map>
 
 #include "block8.h"
@@ -103,18 +102,20 @@ static_assert(offsetof(ProdArgs, out) == 0, "the kernels' first argument starts 
         (args).n_out                                                                                                       \
   }
 
-// 16 codes from k on of a row of `n`, zeros behind its end: one load, of the row's last 16 where it would pass the end, and a shift.
-// WHOLE: they are all there.
-template <bool WHOLE>
-__device__ __forceinline__ u32x4 load16_codes(const uint8_t* row, int k, int n) {
-  if (WHOLE) return *(const u32x4_any*)(row + k);
-  if (n < 16) {  // (a row that holds no 16)
-    u32x4 c = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (k + i < n) c[i >> 2] |= (uint32_t)row[k + i] << (8 * (i & 3));
-    return c;
+// 16 codes from k on of a row of n < 16, zeros behind its end
+__device__ __forceinline__ u32x4 short_row(const uint8_t* row, int k, int n) {
+  uint64_t lo = 0, hi = 0;
+#pragma unroll 1
+  for (int i = k; i < n; ++i) {
+    const uint64_t c = row[i];
+    if (i - k < 8) lo |= c << (8 * (i - k));
+    else hi |= c << (8 * (i - k - 8));
   }
+  return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+// 16 codes from k on of a row of n, zeros behind its end: one load, of the row's last 16 where it would pass the end, and a shift.
+__device__ __forceinline__ u32x4 load16_codes(const uint8_t* row, int k, int n) {
+  if (n < 16) return short_row(row, k, n);
   const int from = min(k, n - 16), skip = min(k - from, 16) * 8;  // bits that are another piece's
   const u32x4 c = *(const u32x4_any*)(row + from);
   uint64_t lo = (uint64_t)c[1] << 32 | c[0], hi = (uint64_t)c[3] << 32 | c[2];
@@ -178,7 +179,7 @@ __global__ __launch_bounds__(256) void prod8_pieces_kernel(ProdCopies args) {
     const uint32_t at = first + 256 * k;
     if (at >= c->total) break;
     const uint32_t row = at / c->pieces, p = at - row * c->pieces;
-    c->to[at] = load16_codes<false>(c->from + (int64_t)row * c->n, (int)p * 16, (int)c->n);
+    c->to[at] = load16_codes(c->from + (int64_t)row * c->n, (int)p * 16, (int)c->n);
   }
 }
 
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(512) void prod8_rows_kernel(ProdArgs args) {
   ProdSeg seg = tables.seg(out.seg0);
   int k = (int)seg.k, blocks = (k + 127) / 128;
   for (int t0 = wave; t0 < total; t0 += 8 * U) {
-    u32x4 fb[U][2], fa[U][MI][2];
+    u32x4 fb[U][2], fa[U][MI][2], mask[U][2];
     int sb[U], sa[U][MI];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -216,17 +217,24 @@ __global__ __launch_bounds__(512) void prod8_rows_kernel(ProdArgs args) {
       }
       const int kb = t0 + 8 * u - base;
       const uint8_t* const b = seg.b + (int64_t)n * k;
-      auto fetch = [&](auto whole) __attribute__((always_inline)) {
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          const int at = kb * 128 + p * 64 + g * 16;
-          fb[u][p] = load16_codes<decltype(whole)::value>(b, at, k);
+      for (int p = 0; p < 2; ++p) {
+        // A piece that passes the row's end is the row's last 16 codes, without those that are another piece's: in which place of
+        // a product a k stands is the same for both operands, and no matter.
+        const int at = kb * 128 + p * 64 + g * 16, from = min(at, k - 16), skip = (at - from) * 8;
 #pragma unroll
-          for (int i = 0; i < MI; ++i) fa[u][i][p] = load16_codes<decltype(whole)::value>(seg.a + (int64_t)m[i] * k, at, k);
+        for (int d = 0; d < 4; ++d) mask[u][p][d] = skip >= 32 * d + 32 ? 0u : 0xFFFFFFFFu << max(0, skip - 32 * d);
+        if (k >= 16) {
+          fb[u][p] = *(const u32x4_any*)(b + from);
+#pragma unroll
+          for (int i = 0; i < MI; ++i) fa[u][i][p] = *(const u32x4_any*)(seg.a + (int64_t)m[i] * k + from);
+        } else {
+          mask[u][p] = u32x4{~0u, ~0u, ~0u, ~0u};
+          fb[u][p] = short_row(b, at, k);
+#pragma unroll
+          for (int i = 0; i < MI; ++i) fa[u][i][p] = short_row(seg.a + (int64_t)m[i] * k, at, k);
         }
-      };
-      if (kb < blocks - 1 || (k & 127) == 0) fetch(std::true_type());
-      else fetch(std::false_type());
+      }
       sb[u] = B_TILES ? seg.bs[(int64_t)(n >> 7) * blocks + kb] : seg.bs[(int64_t)kb * out.n + n];
 #pragma unroll
       for (int i = 0; i < MI; ++i) sa[u][i] = seg.as[(int64_t)kb * out.m + m[i]];
@@ -237,12 +245,14 @@ __global__ __launch_bounds__(512) void prod8_rows_kernel(ProdArgs args) {
       const float f = scale_exponent(sb[u]);
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
-        const v8bf b0 = codes_to_bf16(fb[u][p][0], fb[u][p][1], f), b1 = codes_to_bf16(fb[u][p][2], fb[u][p][3], f);
+        const u32x4 b = fb[u][p] & mask[u][p];
+        const v8bf b0 = codes_to_bf16(b[0], b[1], f), b1 = codes_to_bf16(b[2], b[3], f);
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
           const float e = scale_exponent(sa[u][i]);
-          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b0, codes_to_bf16(fa[u][i][p][0], fa[u][i][p][1], e), acc[i], 0, 0, 0);
-          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b1, codes_to_bf16(fa[u][i][p][2], fa[u][i][p][3], e), acc[i], 0, 0, 0);
+          const u32x4 a = fa[u][i][p] & mask[u][p];
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b0, codes_to_bf16(a[0], a[1], e), acc[i], 0, 0, 0);
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b1, codes_to_bf16(a[2], a[3], e), acc[i], 0, 0, 0);
         }
       }
     }
@@ -580,6 +590,7 @@ static int launch_prod_as(ProdArgs& args, std::vector<ProdOut>& outs, std::vecto
   const dim3 grid((unsigned)tiles);
   if (rows <= 16) hipLaunchKernelGGL((prod8_rows_kernel<C, B_TILES, 1, 4>), grid, dim3(512), 0, st, args);
   else if (rows <= 32) hipLaunchKernelGGL((prod8_rows_kernel<C, B_TILES, 2, 2>), grid, dim3(512), 0, st, args);
+  else if (rows <= 48) hipLaunchKernelGGL((prod8_rows_kernel<C, B_TILES, 3, 2>), grid, dim3(512), 0, st, args);
   else hipLaunchKernelGGL((prod8_rows_kernel<C, B_TILES, 4, 2>), grid, dim3(512), 0, st, args);
   return DISTDL_OK;
 }
