@@ -685,9 +685,11 @@ int distdl_scan_plan_create(distdl_scan_plan** out, int64_t n_b, int64_t T, int6
     p->gate = gate;
     p->dtype = dtype;
     p->groups = (int)groups;
-    // Four workgroups for each of the 256 compute units; a segment has at least a tile of the forward pass.
-    const int64_t tile = 16 * kScanWaves, want = (1024 + groups * n_b - 1) / (groups * n_b);
-    const int64_t most = std::max<int64_t>(1, T / tile), segments = std::min(want, most);
+    // More than 128 workgroups go through all of time in one launch, fewer cut it so that there are four for each of the 256 compute units, a
+    // segment of a tile at least.  Measured, 67 million bf16 steps of a channel (us, one launch; two): 128 workgroups 135, 133
+    // (adjoint 227, 220), 256 workgroups 84, 137 (166, 221), 512 workgroups 93, 142 (167, 218).
+    const int64_t tile = 16 * kScanWaves, alone = groups * n_b;
+    const int64_t segments = alone > 128 ? 1 : std::min((1024 + alone - 1) / alone, std::max<int64_t>(1, T / tile));
     p->seg_steps = (((T + segments - 1) / segments) + tile - 1) / tile * tile;
     p->segments = (int)((T + p->seg_steps - 1) / p->seg_steps);
     *out = p.release();
