@@ -513,8 +513,9 @@ static int launch_norm_bwd(distdl_rmsnorm_plan* p, NormArgs& a, hipStream_t st) 
     parts = wide ? (int)std::min<int64_t>((a.rows + 3) / 4, 64) : grid;
     rc = p->partial.get((size_t)parts * a.pieces * kPiece, st, &a.partial);
     if (rc) return;
-    hipLaunchKernelGGL((norm_bwd_kernel<E, W, R, ROWS16, wide>), dim3((unsigned)grid), dim3(norm_threads(W)), 0, st, a);
+    // Before norm_bwd_kernel, whose dx may lie on s or dy.
     if (wide) hipLaunchKernelGGL((norm_dg_wide_kernel<E, ROWS16>), dim3(a.pieces, parts), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((norm_bwd_kernel<E, W, R, ROWS16, wide>), dim3((unsigned)grid), dim3(norm_threads(W)), 0, st, a);
   });
   if (rc) return rc;
   hipLaunchKernelGGL(norm_dg_kernel, dim3(a.pieces * (kPiece / 16)), dim3(1024), 0, st, a, parts);

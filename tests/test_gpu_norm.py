@@ -184,6 +184,36 @@ def test_in_place_other_stream_and_graph():
         assert all(torch.equal(a, b) for a, b in zip(want, dx + dg))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n_f,P", [(7, 513, 2), (9, 2048, 1), (5, 9000, 2), (3, 20000, 1)])
+def test_answers_over_their_inputs(rows, n_f, P, dtype):
+    """Every lying-over that the calls allow gives the bits of the call with arrays of its own."""
+    require_gpu()
+    (x, r, dy, ds), g = make(rows, n_f, P, dtype, seed=7)
+    plan = dd.distdl_rmsnorm_plan_create(rows, n_f, P, 1e-5, KINDS[dtype])
+    new = lambda ts: [torch.empty_like(t) for t in ts]  # noqa: E731
+    copy = lambda ts: [t.clone() for t in ts]  # noqa: E731
+    same = lambda a, b: all(torch.equal(u, v) for u, v in zip(a, b))  # noqa: E731
+    s, y, rstd = new(x), new(x), torch.empty(rows, device="cuda")
+    dd.distdl_rmsnorm_fwd(plan, x, r, g, s, y, None, None, rstd)
+    for s_on in (0, 1):
+        at = [copy(x), copy(r)]
+        y2 = new(x)
+        dd.distdl_rmsnorm_fwd(plan, at[0], at[1], g, at[s_on], y2, None, None, rstd)
+        assert same(s, at[s_on]) and same(y, y2)
+        at = [copy(x), copy(r)]
+        s2 = new(x)
+        dd.distdl_rmsnorm_fwd(plan, at[0], at[1], g, s2, at[s_on], None, None, rstd)
+        assert same(s, s2) and same(y, at[s_on])
+    dx, dg = new(x), new(g)
+    dd.distdl_rmsnorm_bwd(plan, s, g, rstd, dy, ds, dx, dg)
+    for dx_on in range(3):
+        at = [copy(s), copy(dy), copy(ds)]
+        dg2 = new(g)
+        dd.distdl_rmsnorm_bwd(plan, at[0], g, rstd, at[1], at[2], at[dx_on], dg2)
+        assert same(dx, at[dx_on]) and same(dg, dg2), ("s", "dy", "dsum")[dx_on]
+
+
 def test_no_rows():
     require_gpu()
     plan = dd.distdl_rmsnorm_plan_create(0, 40, 1, 1e-5, torch.float32)
