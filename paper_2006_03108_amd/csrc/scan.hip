@@ -7,8 +7,7 @@
 // Each channel is a chain of its own; along time the steps are affine maps, which compose: (A, B) after (A', B') is
 // (A A', A B' + B).  So a workgroup of eight waves takes a tile of steps, L to a wave, and 64 V channels: each wave composes its steps,
 // the eight maps meet in LDS, and each wave then runs its steps from the state in front of it, all from registers.  Where
-// sequences and channels are too few for that to fill the card, time is cut into segments as well: a first launch composes each
-// segment's map, the second starts every segment from the maps before it (time is read twice there, once from HBM).
+// sequences and channels fill the card, a workgroup goes through all of time; where they are few, every tile is a workgroup's (below).
 // The workers' boundaries are those of arrays only: a state passes them as it passes tiles.
 #include <algorithm>
 #include <cstddef>
@@ -35,11 +34,14 @@ struct ScanArgs {
   const ScanWorker* more;
   int64_t n_c;
   int32_t T, part, extra;  // worker p has part + (p < extra) steps
-  int32_t P, n_b, groups, segments, seg_steps;
+  int32_t P, n_b, groups;
   const int32_t* lengths;
   const float *h0, *end;  // end: dhT of the adjoint
   float *hT;              // forward: hT; adjoint: dh0
-  float* maps;            // [n_b][segments][2][n_c]
+  // the kernels of few chains:
+  uint64_t* words;               // tickets taken; then what the tiles publish
+  uint32_t tasks, tiles;         // of all chains; of one
+  uint32_t tiles_wide, tiles_rest;  // of a worker with part + 1 steps, with part
 };
 
 // Worker p's arrays, from the table or from the launch's own arguments (of which they are the first).  Read as constants, into scalar
@@ -162,30 +164,37 @@ __device__ __forceinline__ void scan_gate(float g, float& a, float& rest) {
   }
 }
 
+// One more gate of a run of them.  The product of given gates is held finite: it meets states of zero, which stay zero.
+template <int GATE>
+__device__ __forceinline__ float scan_more(float A, float a) {
+  return GATE == DISTDL_GATE_GIVEN ? __builtin_amdgcn_fmed3f(A * a, -3.40282347e38f, 3.40282347e38f) : A * a;
+}
+
 // (the compiler does not know that it is the same in all lanes, and would make every branch on it one of lanes)
 __device__ __forceinline__ int scan_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 struct ScanPlace {
-  int group, seg, b, c, n;  // c: first channel of the group; n: channels of this lane
-  int len, lo, hi;          // steps of the sequence; of the segment
+  int group, b, c;  // c: first channel of the group
+  int n, len;       // channels of this lane; steps of the sequence
 };
 template <bool PAIR>
-__device__ __forceinline__ ScanPlace scan_place(const ScanArgs& s, bool reversed) {
+__device__ __forceinline__ ScanPlace scan_place(const ScanArgs& s, uint32_t chain) {
   ScanPlace r;
-  uint32_t at = xcd_order(blockIdx.x, gridDim.x);
-  if (reversed) at = gridDim.x - 1 - at;
-  r.group = at % s.groups;
-  at /= s.groups;
-  r.b = at % s.n_b;
-  r.seg = at / s.n_b;
+  r.group = chain % s.groups;
+  r.b = chain / s.groups;
   r.c = r.group * kScanCols;
   const int64_t left = s.n_c - r.c;
   const int lane = threadIdx.x & 63;
   r.n = (scan_channel<PAIR>(lane, 0) < left) + (scan_channel<PAIR>(lane, 1) < left);
-  r.len = s.lengths ? max(0, min(s.T, (int)__builtin_amdgcn_readfirstlane(s.lengths[r.b]))) : s.T;
-  r.lo = r.seg * s.seg_steps;
-  r.hi = s.T - r.lo < s.seg_steps ? s.T : r.lo + s.seg_steps;
+  r.len = s.lengths ? max(0, min(s.T, ((const __attribute__((address_space(4))) int32_t*)(uint64_t)s.lengths)[r.b])) : s.T;
   return r;
+}
+
+// h0, or dhT of the adjoint
+template <bool PAIR>
+__device__ __forceinline__ void scan_start(const ScanArgs& s, const ScanPlace& at, const float* from, float* state) {
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v) state[v] = from && v < at.n ? from[at.b * s.n_c + at.c + scan_channel<PAIR>(threadIdx.x & 63, v)] : 0.f;
 }
 
 // The maps of all waves, each behind the one before it: `mine` is the state in front of this wave's steps, `state` that behind the tile.
@@ -207,137 +216,10 @@ __device__ __forceinline__ void scan_meet(float (*lds)[2][kScanCols], const floa
   }
 }
 
-// The state in front of a segment: that of the sequence through the maps of the segments before (behind) it.  A wave composes an eighth of
-// them, eight loads at a time, and the eighths meet like the waves' steps.
-template <bool BACK, bool PAIR>
-__device__ __forceinline__ void scan_start(const ScanArgs& s, const ScanPlace& at, float (*lds)[2][kScanCols], float* state) {
-  const float* from = BACK ? s.end : s.h0;
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int v = 0; v < kScanV; ++v) state[v] = from && v < at.n ? from[at.b * s.n_c + at.c + scan_channel<PAIR>(lane, v)] : 0.f;
-  const int n = BACK ? s.segments - 1 - at.seg : at.seg;
-  if (n == 0) return;
-  const int each = (n + kScanWaves - 1) / kScanWaves, i0 = min(n, scan_wave() * each), i1 = min(n, i0 + each);
-  const int64_t hop = (BACK ? -2 : 2) * s.n_c;
-  const float* m = s.maps + ((int64_t)at.b * s.segments + (BACK ? s.segments - 1 - i0 : i0)) * 2 * s.n_c + at.c;
-  float A[kScanV], B[kScanV], mine[kScanV];
-#pragma unroll
-  for (int v = 0; v < kScanV; ++v) {
-    A[v] = 1.f;
-    B[v] = 0.f;
-  }
-  for (int i = i0; i < i1; i += 8) {
-    float f[8][kScanV], u[8][kScanV];
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-#pragma unroll
-      for (int v = 0; v < kScanV; ++v) {
-        const bool is = i + k < i1 && v < at.n;
-        f[k][v] = is ? m[k * hop + scan_channel<PAIR>(lane, v)] : 1.f;
-        u[k][v] = is ? m[k * hop + s.n_c + scan_channel<PAIR>(lane, v)] : 0.f;
-      }
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-#pragma unroll
-      for (int v = 0; v < kScanV; ++v) {
-        A[v] *= f[k][v];
-        B[v] = fmaf(f[k][v], B[v], u[k][v]);
-      }
-    m += 8 * hop;
-  }
-  scan_meet(lds, A, B, state, mine);
-}
-
-// A segment's map: a wave composes an eighth of the steps, the eighths meet at the end.
-template <class E, int GATE, bool PAIR, bool BACK>
-__global__ __launch_bounds__(64 * kScanWaves) void scan_map_kernel(ScanArgs s) {
-  constexpr int L = 8;
-  __shared__ float lds[kScanWaves][2][kScanCols];
-  const ScanTable table = SCAN_TABLE(s);
-  const ScanPlace at = scan_place<PAIR>(s, BACK);
-  const int lane = threadIdx.x & 63, wave = BACK ? kScanWaves - 1 - scan_wave() : scan_wave();
-  const int hi = min(at.hi, at.len), each = (max(0, hi - at.lo) + kScanWaves - 1) / kScanWaves;
-  const int from = min(hi, at.lo + wave * each), to = min(hi, from + each);
-  const ScanLane off = scan_lane<E, PAIR>(s.n_c - at.c);
-  const uint32_t hop = (uint32_t)(s.n_c * sizeof(E));
-  typedef ScanRaw<E, PAIR> Raw;
-  Raw ra[2][L], rx[2][L];  // a run of at most L steps of one worker and the next one, forwards or backwards
-  const int steps = to - from;
-  auto load = [&](int done, Raw* a, Raw* x) __attribute__((always_inline)) {
-    const int t = BACK ? to - 1 - done : from + done;
-    const ScanSpan sp = scan_span(s, done < steps ? t : 0);
-    const int cnt = done < steps ? min(L, BACK ? t + 1 - max(from, sp.lo) : min(to, sp.hi) - t) : 0;
-    const ScanWorker w = scan_worker(table, sp.p);
-    const int64_t row = ((int64_t)at.b * (sp.hi - sp.lo) + (t - sp.lo) - (BACK ? cnt - 1 : 0)) * s.n_c + at.c;
-    const auto pa = scan_rows((const E*)w.a + row), px = scan_rows((const E*)(BACK ? w.dh : w.x) + row);
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-      const ScanLane o = off.where(i < cnt);
-      const uint32_t step = i < cnt ? (BACK ? cnt - 1 - i : i) * hop : 0;
-      a[i].load(pa, o, step);
-      x[i].load(px, o, step);
-    }
-    return cnt;
-  };
-  float A[kScanV], B[kScanV];
-#pragma unroll
-  for (int v = 0; v < kScanV; ++v) {
-    A[v] = 1.f;
-    B[v] = 0.f;
-  }
-  auto compose = [&](const Raw* ar, const Raw* xr, int cnt) __attribute__((always_inline)) {
-    auto one = [&](int i, bool in) __attribute__((always_inline)) {
-      float g[kScanV], x[kScanV];
-      ar[i].values(g);
-      xr[i].values(x);
-#pragma unroll
-      for (int v = 0; v < kScanV; ++v) {
-        float a, rest;
-        scan_gate<GATE>(g[v], a, rest);
-        a = in ? a : 1.f;  // (and x is 0)
-        A[v] *= a;
-        B[v] = BACK ? a * (B[v] + x[v]) : fmaf(a, B[v], rest * x[v]);
-      }
-    };
-    if (cnt == L) {
-#pragma unroll
-      for (int i = 0; i < L; ++i) one(i, true);
-    } else {
-#pragma unroll
-      for (int i = 0; i < L; ++i) one(i, i < cnt);
-    }
-  };
-  int done = 0, c0 = load(0, ra[0], rx[0]);
-  while (c0 > 0) {
-    done += c0;
-    const int c1 = load(done, ra[1], rx[1]);
-    compose(ra[0], rx[0], c0);
-    done += c1;
-    c0 = load(done, ra[0], rx[0]);
-    compose(ra[1], rx[1], c1);
-  }
-  float state[kScanV] = {}, mine[kScanV], all[kScanV];
-  scan_meet(lds, A, B, state, mine);  // B of the whole: the map of zero
-#pragma unroll
-  for (int v = 0; v < kScanV; ++v) {
-    all[v] = 1.f;
-    for (int w = 0; w < kScanWaves; ++w) all[v] *= lds[w][0][v * 64 + lane];
-  }
-  if (scan_wave() == 0) {
-    float* m = s.maps + ((int64_t)at.b * s.segments + at.seg) * 2 * s.n_c + at.c;
-#pragma unroll
-    for (int v = 0; v < kScanV; ++v)
-      if (v < at.n) {
-        m[scan_channel<PAIR>(lane, v)] = all[v];
-        m[s.n_c + scan_channel<PAIR>(lane, v)] = state[v];
-      }
-  }
-}
-
 // hT, or dh0 of the adjoint
 template <bool PAIR>
 __device__ __forceinline__ void scan_finish(const ScanArgs& s, const ScanPlace& at, const float* state) {
-  if (!s.hT || scan_wave() != 0) return;
+  if (!s.hT) return;
   float* to = s.hT + at.b * s.n_c + at.c;
 #pragma unroll
   for (int v = 0; v < kScanV; ++v)
@@ -358,7 +240,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
   constexpr int L = 8;
   __shared__ float lds[2][kScanWaves][2][kScanCols];
   const ScanTable table = SCAN_TABLE(s);
-  const ScanPlace at = scan_place<PAIR>(s, s.segments > 1);
+  const ScanPlace at = scan_place<PAIR>(s, xcd_order(blockIdx.x, gridDim.x));
   const int wave = scan_wave();
   const ScanLane off = scan_lane<E, PAIR>(s.n_c - at.c);
   const uint32_t hop = (uint32_t)(s.n_c * sizeof(E));
@@ -368,7 +250,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
     const ScanSpan sp = scan_span(s, t0);
     t.p = sp.p;
     t.lo = sp.lo;
-    t.next = min(min(at.hi, sp.hi), t0 + kScanWaves * L);
+    t.next = min(sp.hi, t0 + kScanWaves * L);
     t.from = t0 + wave * L;
     t.cnt = is ? max(0, min(L, t.next - t.from)) : 0;
     t.live = max(0, min(t.cnt, at.len - t.from));
@@ -383,9 +265,9 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
     }
     return t;
   };
-  ScanTile t = tile(at.lo, true);
+  ScanTile t = tile(0, true);
   float state[kScanV];
-  scan_start<false, PAIR>(s, at, lds[1], state);
+  scan_start<PAIR>(s, at, s.h0, state);
   for (int turn = 0;; turn ^= 1) {
     float a[L][kScanV], u[L][kScanV], A[kScanV], B[kScanV], h[kScanV];
 #pragma unroll
@@ -408,16 +290,16 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
     }
 #pragma unroll
     for (int v = 0; v < kScanV; ++v) {
-      A[v] = a[0][v];
+      A[v] = scan_more<GATE>(1.f, a[0][v]);
       B[v] = u[0][v];
 #pragma unroll
       for (int i = 1; i < L; ++i) {
-        A[v] *= a[i][v];
+        A[v] = scan_more<GATE>(A[v], a[i][v]);
         B[v] = fmaf(a[i][v], B[v], u[i][v]);
       }
     }
     const ScanTile now = t;
-    const bool more = now.next < at.hi;
+    const bool more = now.next < s.T;
     t = tile(more ? now.next : now.next - 1, more);
     scan_meet(lds[turn], A, B, state, h);
 #pragma unroll
@@ -435,7 +317,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
     for (int i = 0; i < L; ++i) scan_put<E, PAIR>(po, off.where(i < now.cnt), i * hop, u[i]);
     if (!more) break;
   }
-  if (at.hi == s.T) scan_finish<PAIR>(s, at, state);
+  if (wave == 0) scan_finish<PAIR>(s, at, state);
 }
 
 // Backwards in time: wave 0 has a tile's last steps, and step i of a wave is the i-th from its end.
@@ -445,8 +327,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
   constexpr bool X = GATE != DISTDL_GATE_GIVEN;
   __shared__ float lds[2][kScanWaves][2][kScanCols];
   const ScanTable table = SCAN_TABLE(s);
-  const ScanPlace at = scan_place<PAIR>(s, s.segments == 1);
-  const int wave = scan_wave(), lane = threadIdx.x & 63;
+  const ScanPlace at = scan_place<PAIR>(s, xcd_order(blockIdx.x, gridDim.x));
+  const int wave = scan_wave();
   const ScanLane off = scan_lane<E, PAIR>(s.n_c - at.c);
   const uint32_t hop = (uint32_t)(s.n_c * sizeof(E));
   ScanRaw<E, PAIR> ra[L], rx[L], rd[L], rh[L], edge;  // edge: the state before a worker's first step, the last one of the worker before
@@ -455,7 +337,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
     const ScanSpan sp = scan_span(s, t1 - 1);
     t.p = sp.p;
     t.lo = sp.lo;
-    t.next = max(max(at.lo, sp.lo), t1 - kScanWaves * L);
+    t.next = max(sp.lo, t1 - kScanWaves * L);
     t.from = t1 - 1 - wave * L;  // step i: from - i
     t.cnt = is ? max(0, min(L, t.from + 1 - t.next)) : 0;
     t.live = t.cnt - max(0, min(t.cnt, t.from + 1 - at.len));  // (steps behind the sequence's end come first)
@@ -479,11 +361,10 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
     return t;
   };
   float start[kScanV];  // the state in front of step 0, in 32 bits
-#pragma unroll
-  for (int v = 0; v < kScanV; ++v) start[v] = s.h0 && v < at.n ? s.h0[at.b * s.n_c + at.c + scan_channel<PAIR>(lane, v)] : 0.f;
-  ScanTile t = tile(at.hi, true);
+  scan_start<PAIR>(s, at, s.h0, start);
+  ScanTile t = tile(s.T, true);
   float state[kScanV];
-  scan_start<true, PAIR>(s, at, lds[1], state);
+  scan_start<PAIR>(s, at, s.end, state);
   for (int turn = 0;; turn ^= 1) {
     // dx = d rest, da = d slope
     float a[L][kScanV], d[L][kScanV], rest[L][kScanV], slope[L][kScanV], A[kScanV], B[kScanV], back[kScanV];
@@ -519,16 +400,16 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
     }
 #pragma unroll
     for (int v = 0; v < kScanV; ++v) {
-      A[v] = a[0][v];
+      A[v] = scan_more<GATE>(1.f, a[0][v]);
       B[v] = a[0][v] * d[0][v];
 #pragma unroll
       for (int i = 1; i < L; ++i) {
-        A[v] *= a[i][v];
+        A[v] = scan_more<GATE>(A[v], a[i][v]);
         B[v] = a[i][v] * (B[v] + d[i][v]);
       }
     }
     const ScanTile now = t;
-    const bool more = now.next > at.lo;
+    const bool more = now.next > 0;
     t = tile(more ? now.next : now.next + 1, more);
     scan_meet(lds[turn], A, B, state, back);
     const ScanWorker w = scan_worker(table, now.p);
@@ -550,7 +431,339 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
     }
     if (!more) break;
   }
-  if (at.lo == 0) scan_finish<PAIR>(s, at, state);
+  if (wave == 0) scan_finish<PAIR>(s, at, state);
+}
+
+// Few chains: time is split, and each tile of it is one workgroup's, which reads it once.  A workgroup keeps the tile in registers, composes its
+// map and publishes that; the state in front of the tile is that in front of its run of kScanSuper tiles through the maps of the tiles before it
+// in the run; the run's last tile publishes the state behind it.  So sums have one order whatever the order of the workgroups.
+//
+// What is published are words of a number and the pass's tag, written and read as one: a word with the tag is there, and nothing else
+// has to be ordered.  Which tile a workgroup takes is decided by the ticket that it draws when it starts, tiles in the order of
+// time: who waits, waits for tickets drawn before its own, so the lowest ticket not yet done never waits and every wait ends, however
+// few workgroups the card holds at a time.  Tickets go on from pass to pass: their quotient by the pass's tiles is the tag.
+//
+// Measured (us): 65536 x 1024 bf16 on four workers 100 (4.0 TB/s), adjoint of 7 x 2049 x 1001 fp32 71 (4.8 TB/s); with time read twice, once for the
+// maps, 145 and 88; without the waits 94 and 74, and the rest is what a workgroup takes from its start to its stores, two at a time on a
+// compute unit.  Gates made twice instead of held (tiles twice as long): 100 and 85.  Workgroups that go from tile to tile and have the next
+// one's loads under way, whose loads the waits then stand behind: 133 and 83.  Four waves: 107 and 83, sixteen: 215 and 122.
+constexpr int kScanSuper = 2 * kScanWaves;
+constexpr int kScanFew = 128;    // chains at most
+constexpr int kScanShort = 128;  // steps that one workgroup goes through as fast
+
+// Steps of a wave, forwards and backwards: what 64 registers hold of them (16 for two workgroups on a compute unit, 24 for one: the same time).
+constexpr int kFewSteps = 16, kFewBack = 8;
+
+__global__ __launch_bounds__(256) void scan_clear_kernel(uint64_t* words, size_t n) {
+  for (size_t i = blockIdx.x * (size_t)256 + threadIdx.x; i < n; i += gridDim.x * (size_t)256) words[i] = 0;
+}
+
+__device__ __forceinline__ void scan_publish(uint64_t* to, const float* v, uint32_t tag) {
+#pragma unroll
+  for (int i = 0; i < kScanV; ++i)
+    __hip_atomic_store(to + i * 64 + (threadIdx.x & 63), (uint64_t)tag << 32 | __float_as_uint(v[i]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Waits for the words of N places (a place that is null is not waited for).  A later tag also ends the wait.
+template <int N>
+__device__ __forceinline__ void scan_await(const uint64_t* const (&from)[N], float (&v)[N][kScanV], uint32_t tag) {
+  const uint64_t* lead = nullptr;  // the last of them alone first: whoever waits should not fill the memory's queues
+#pragma unroll
+  for (int k = 0; k < N; ++k) lead = from[k] ? from[k] : lead;
+  if (lead)
+    while (!__all((int32_t)((uint32_t)(__hip_atomic_load(lead + 64 + (threadIdx.x & 63), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >> 32) - tag) >= 0))
+      __builtin_amdgcn_s_sleep(2);
+  for (;;) {
+    uint64_t w[N][kScanV];
+    bool there = true;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int i = 0; i < kScanV; ++i)
+        w[k][i] = from[k] ? __hip_atomic_load(from[k] + i * 64 + (threadIdx.x & 63), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : (uint64_t)tag << 32;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int i = 0; i < kScanV; ++i) {
+        there &= (int32_t)((uint32_t)(w[k][i] >> 32) - tag) >= 0;
+        v[k][i] = __uint_as_float((uint32_t)w[k][i]);
+      }
+    if (__all(there)) return;
+    __builtin_amdgcn_s_sleep(1);
+  }
+}
+
+struct ScanTask {
+  uint32_t tag, chain, k;  // k: tile of the chain in the order of the pass
+};
+__device__ __forceinline__ ScanTask scan_task(const ScanArgs& s, uint32_t (&lds)[2]) {
+  if (threadIdx.x == 0) {
+    const uint64_t ticket = __hip_atomic_fetch_add(s.words, (uint64_t)1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const uint64_t pass = ticket / s.tasks;
+    lds[0] = (uint32_t)pass + 1;
+    lds[1] = (uint32_t)(ticket - pass * s.tasks);
+  }
+  __syncthreads();
+  const uint32_t chains = (uint32_t)s.groups * s.n_b, at = __builtin_amdgcn_readfirstlane(lds[1]);
+  ScanTask t;
+  t.tag = __builtin_amdgcn_readfirstlane(lds[0]);
+  t.k = at / chains;
+  t.chain = at - t.k * chains;
+  return t;
+}
+
+// Where tile `tile` lies: its worker, the worker's steps, the tile's first one and the one behind it.
+struct ScanSlice {
+  int p, lo, hi, from, to;
+};
+__device__ __forceinline__ ScanSlice scan_slice(const ScanArgs& s, uint32_t tile, int steps) {
+  const uint32_t wide = s.extra * s.tiles_wide;
+  ScanSlice r;
+  if (tile < wide) {
+    r.p = tile / s.tiles_wide;
+    tile -= r.p * s.tiles_wide;
+    r.lo = r.p * (s.part + 1);
+    r.hi = r.lo + s.part + 1;
+  } else {
+    const uint32_t q = (tile - wide) / s.tiles_rest;
+    tile -= wide + q * s.tiles_rest;
+    r.p = s.extra + q;
+    r.lo = s.extra * (s.part + 1) + q * s.part;
+    r.hi = r.lo + s.part;
+  }
+  r.from = r.lo + tile * steps;
+  r.to = min(r.hi, r.from + steps);
+  return r;
+}
+
+// From the map of each wave's steps: publishes the tile's, gives the state in front of this wave's steps and, in the last wave, that behind the tile.
+template <int GATE, bool PAIR>
+__device__ __forceinline__ void scan_join(const ScanArgs& s, const ScanPlace& at, const ScanTask& task, const float* from, float (*own)[2][kScanCols],
+                                          float (*run)[2][kScanCols], float* front, const float* A, const float* B, float* mine, float* end) {
+  const int lane = threadIdx.x & 63, wave = scan_wave();
+  const uint32_t super = task.k / kScanSuper, j = task.k % kScanSuper;
+  const bool closes = j == kScanSuper - 1, last = task.k == s.tiles - 1;
+  uint64_t* const maps = s.words + 16 + ((size_t)task.chain * s.tiles + super * kScanSuper) * 2 * kScanCols;  // those of the run
+  uint64_t* const states = s.words + 16 + (size_t)s.groups * s.n_b * s.tiles * 2 * kScanCols +
+                           ((size_t)task.chain * ((s.tiles + kScanSuper - 1) / kScanSuper) + super) * kScanCols;  // the one behind the run
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v) {
+    own[wave][0][v * 64 + lane] = A[v];
+    own[wave][1][v * 64 + lane] = B[v];
+  }
+  __syncthreads();
+  if (wave == kScanWaves - 1 && !closes && !last) {
+    float all[kScanV], sum[kScanV];
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) {
+      all[v] = 1.f;
+      sum[v] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kScanWaves; ++w) {
+        all[v] = scan_more<GATE>(all[v], own[w][0][v * 64 + lane]);
+        sum[v] = fmaf(own[w][0][v * 64 + lane], sum[v], own[w][1][v * 64 + lane]);
+      }
+    }
+    scan_publish(maps + j * 2 * kScanCols, all, task.tag);
+    scan_publish(maps + (j * 2 + 1) * kScanCols, sum, task.tag);
+  }
+  const uint32_t i = 2 * wave;  // the maps of two tiles of the run
+  const uint64_t* const m = maps + i * 2 * kScanCols;
+  const uint64_t* const words[4] = {i < j ? m : nullptr, i < j ? m + kScanCols : nullptr, i + 1 < j ? m + 2 * kScanCols : nullptr,
+                                    i + 1 < j ? m + 3 * kScanCols : nullptr};
+  float got[4][kScanV];
+  scan_await(words, got, task.tag);
+  if (wave == 0) {
+    float start[1][kScanV];
+    const uint64_t* const before[1] = {states - kScanCols};
+    if (super > 0) scan_await(before, start, task.tag);
+    else scan_start<PAIR>(s, at, from, start[0]);
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) front[v * 64 + lane] = start[0][v];
+  }
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v) {
+    const float a0 = i < j ? got[0][v] : 1.f, a1 = i + 1 < j ? got[2][v] : 1.f;  // (the others are zeros)
+    run[wave][0][v * 64 + lane] = scan_more<GATE>(a0, a1);
+    run[wave][1][v * 64 + lane] = fmaf(a1, got[1][v], got[3][v]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v) {
+    float state = front[v * 64 + lane];
+#pragma unroll
+    for (int w = 0; w < kScanWaves; ++w) state = fmaf(run[w][0][v * 64 + lane], state, run[w][1][v * 64 + lane]);
+#pragma unroll
+    for (int w = 0; w < kScanWaves; ++w) {
+      if (w == wave) mine[v] = state;
+      state = fmaf(own[w][0][v * 64 + lane], state, own[w][1][v * 64 + lane]);
+    }
+    end[v] = state;
+  }
+  if (wave == kScanWaves - 1) {
+    if (last) scan_finish<PAIR>(s, at, end);
+    else if (closes) scan_publish(states, end, task.tag);
+  }
+}
+
+template <class E, int GATE, bool PAIR>
+__global__ __launch_bounds__(64 * kScanWaves, 4) void scan_few_fwd_kernel(ScanArgs s) {
+  constexpr int L = kFewSteps;
+  __shared__ float own[kScanWaves][2][kScanCols], run[kScanWaves][2][kScanCols], front[kScanCols];
+  __shared__ uint32_t drawn[2];
+  const ScanTable table = SCAN_TABLE(s);
+  const ScanTask task = scan_task(s, drawn);
+  const ScanPlace at = scan_place<PAIR>(s, task.chain);
+  const int wave = scan_wave();
+  const ScanLane off = scan_lane<E, PAIR>(s.n_c - at.c);
+  const uint32_t hop = (uint32_t)(s.n_c * sizeof(E));
+  const ScanSlice t = scan_slice(s, task.k, kScanWaves * L);
+  const int first = t.from + wave * L, cnt = max(0, min(L, t.to - first)), live = max(0, min(cnt, at.len - first));
+  const int64_t row = ((int64_t)at.b * (t.hi - t.lo) + (first - t.lo)) * s.n_c + at.c;
+  const ScanWorker w = scan_worker(table, t.p);
+  const auto pa = scan_rows((const E*)w.a + row), px = scan_rows((const E*)w.x + row), po = scan_rows((E*)w.o0 + row);
+  ScanRaw<E, PAIR> ra[L], rx[L];
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    const ScanLane o = off.where(i < live);
+    ra[i].load(pa, o, i * hop);
+    rx[i].load(px, o, i * hop);
+  }
+  float a[L][kScanV], u[L][kScanV], A[kScanV], B[kScanV], h[kScanV], end[kScanV];
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    float g[kScanV], x[kScanV];
+    ra[i].values(g);
+    rx[i].values(x);
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) {
+      float rest;
+      scan_gate<GATE>(g[v], a[i][v], rest);
+      u[i][v] = rest * x[v];  // (0 where there is no step)
+    }
+  }
+  if (live < L) {
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int v = 0; v < kScanV; ++v) a[i][v] = i < live ? a[i][v] : 1.f;
+  }
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v) {
+    A[v] = 1.f;
+    B[v] = 0.f;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      A[v] = scan_more<GATE>(A[v], a[i][v]);
+      B[v] = fmaf(a[i][v], B[v], u[i][v]);
+    }
+  }
+  scan_join<GATE, PAIR>(s, at, task, s.h0, own, run, front, A, B, h, end);
+#pragma unroll
+  for (int i = 0; i < L; ++i)
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) u[i][v] = h[v] = fmaf(a[i][v], h[v], u[i][v]);
+  if (live < L) {
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int v = 0; v < kScanV; ++v) u[i][v] = i < live ? u[i][v] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < L; ++i) scan_put<E, PAIR>(po, off.where(i < cnt), i * hop, u[i]);
+}
+
+// Backwards in time: tile 0 and wave 0 have the last steps, and step i of a wave is the i-th from its end.
+template <class E, int GATE, bool PAIR>
+__global__ __launch_bounds__(64 * kScanWaves, 4) void scan_few_bwd_kernel(ScanArgs s) {
+  constexpr int L = kFewBack;
+  constexpr bool X = GATE != DISTDL_GATE_GIVEN;
+  __shared__ float own[kScanWaves][2][kScanCols], run[kScanWaves][2][kScanCols], front[kScanCols];
+  __shared__ uint32_t drawn[2];
+  const ScanTable table = SCAN_TABLE(s);
+  const ScanTask task = scan_task(s, drawn);
+  const ScanPlace at = scan_place<PAIR>(s, task.chain);
+  const int wave = scan_wave();
+  const ScanLane off = scan_lane<E, PAIR>(s.n_c - at.c);
+  const uint32_t hop = (uint32_t)(s.n_c * sizeof(E));
+  const ScanSlice t = scan_slice(s, s.tiles - 1 - task.k, kScanWaves * L);
+  const int from = t.to - 1 - wave * L, cnt = max(0, min(L, from + 1 - t.from));  // step i: from - i
+  const int dead = max(0, min(cnt, from + 1 - at.len));                           // steps behind the sequence's end; they come first
+  const int64_t row = ((int64_t)at.b * (t.hi - t.lo) + (from - cnt + 1 - t.lo)) * s.n_c + at.c;
+  const ScanWorker w = scan_worker(table, t.p);
+  const auto pa = scan_rows((const E*)w.a + row), pd = scan_rows((const E*)w.dh + row), ph = scan_rows((const E*)w.h + row - s.n_c);
+  const auto px = scan_rows((const E*)(X ? w.x : w.a) + row), o0 = scan_rows((E*)w.o0 + row), o1 = scan_rows((E*)w.o1 + row);
+  ScanRaw<E, PAIR> ra[L], rx[L], rd[L], rh[L], edge;  // edge: the state before a worker's first step, the last one of the worker before
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    const bool in = i >= dead && i < cnt;
+    const ScanLane o = off.where(in);
+    const uint32_t step = in ? (cnt - 1 - i) * hop : 0;
+    ra[i].load(pa, o, step);
+    rd[i].load(pd, o, step);
+    if (X) rx[i].load(px, o, step);
+    rh[i].load(ph, off.where(in && from - i > t.lo), step);
+  }
+  const bool edged = cnt > dead && from - cnt + 1 == t.lo && t.lo > 0;
+  const ScanSpan b = scan_span(s, edged ? t.lo - 1 : 0);
+  edge.load(scan_rows((const E*)scan_worker(table, b.p).h + ((int64_t)at.b * (b.hi - b.lo) + (b.hi - b.lo - 1)) * s.n_c + at.c), off.where(edged), 0);
+  float last[kScanV];  // the state in front of a worker's first step, of the first worker in 32 bits
+  if (t.lo == 0) scan_start<PAIR>(s, at, s.h0, last);
+  // dx = d rest, da = d slope
+  float a[L][kScanV], d[L][kScanV], rest[L][kScanV], slope[L][kScanV], A[kScanV], B[kScanV], back[kScanV], end[kScanV];
+  if (t.lo > 0) edge.values(last);
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    float g[kScanV], x[kScanV] = {}, before[kScanV];
+    ra[i].values(g);
+    rd[i].values(d[i]);
+    if (X) rx[i].values(x);
+    rh[i].values(before);
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) {
+      if (from - i == t.lo) before[v] = last[v];
+      scan_gate<GATE>(g[v], a[i][v], rest[i][v]);
+      slope[i][v] = X ? (before[v] - x[v]) * (a[i][v] * rest[i][v]) : before[v];
+    }
+  }
+  if (dead > 0 || cnt < L) {
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const bool in = i >= dead && i < cnt;
+#pragma unroll
+      for (int v = 0; v < kScanV; ++v) {
+        a[i][v] = in ? a[i][v] : 1.f;  // (d is 0 there)
+        rest[i][v] = in ? rest[i][v] : 0.f;
+        slope[i][v] = in ? slope[i][v] : 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v) {
+    A[v] = 1.f;
+    B[v] = 0.f;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      A[v] = scan_more<GATE>(A[v], a[i][v]);
+      B[v] = a[i][v] * (B[v] + d[i][v]);
+    }
+  }
+  scan_join<GATE, PAIR>(s, at, task, s.end, own, run, front, A, B, back, end);
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    float da[kScanV], dx[kScanV];
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) {
+      const float all = d[i][v] + back[v];
+      back[v] = a[i][v] * all;
+      da[v] = all * slope[i][v];
+      dx[v] = all * rest[i][v];
+    }
+    const ScanLane o = off.where(i < cnt);
+    const uint32_t step = i < cnt ? (cnt - 1 - i) * hop : 0;
+    scan_put<E, PAIR>(o0, o, step, da);
+    scan_put<E, PAIR>(o1, o, step, dx);
+  }
 }
 
 // One token of each row: its state lies at row slots[row] of the pool.  A row without a slot of the pool is idle.
@@ -591,10 +804,10 @@ struct distdl_scan_plan {
   int64_t n_b = 0, T = 0, n_c = 0;
   int P = 1, gate = 0;
   distdl_dtype dtype = DISTDL_F32;
-  int groups = 1, segments = 1;
-  int64_t seg_steps = 0;
+  int groups = 1;
+  bool few = false;  // chains, so that time has to be split
   distdl::DevArray<distdl::ScanWorker> table;
-  distdl::StreamScratch maps;
+  distdl::StreamScratch words[2][2];  // by direction and kind of tiles, which have numbers of their own
 };
 
 namespace distdl {
@@ -614,8 +827,6 @@ static int scan_args(distdl_scan_plan* p, const std::vector<ScanWorker>& w, hipS
   s->P = p->P;
   s->n_b = (int32_t)p->n_b;
   s->groups = p->groups;
-  s->segments = p->segments;
-  s->seg_steps = (int32_t)p->seg_steps;
   int rc = DISTDL_OK;
   if (p->P <= kScanInline) {
     std::copy(w.begin(), w.end(), s->w);
@@ -623,20 +834,49 @@ static int scan_args(distdl_scan_plan* p, const std::vector<ScanWorker>& w, hipS
     if ((rc = p->table.upload(w, st))) return rc;
     s->more = p->table.dev;
   }
-  s->maps = nullptr;
-  if (p->segments > 1) rc = p->maps.get((size_t)p->n_b * p->segments * 2 * p->n_c, st, &s->maps);
   return rc;
 }
 
-template <class E, int GATE, bool PAIR>
-static void launch_scan(const ScanArgs& s, bool back, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)s.groups * s.n_b * s.segments)), block(64 * kScanWaves);
-  if (s.segments > 1) {
-    if (back) hipLaunchKernelGGL((scan_map_kernel<E, GATE, PAIR, true>), grid, block, 0, st, s);
-    else hipLaunchKernelGGL((scan_map_kernel<E, GATE, PAIR, false>), grid, block, 0, st, s);
+// What the tiles of `steps` steps publish.  The memory starts as zeros, the tag of no pass; a recorded pass cannot see to that.
+static int scan_words(StreamScratch& scratch, int steps, hipStream_t st, ScanArgs* s) {
+  s->tiles_wide = (s->part + 1 + steps - 1) / steps;
+  s->tiles_rest = (s->part + steps - 1) / steps;
+  s->tiles = s->extra * s->tiles_wide + (s->P - s->extra) * s->tiles_rest;
+  const int64_t chains = (int64_t)s->groups * s->n_b, supers = (s->tiles + kScanSuper - 1) / kScanSuper;
+  s->tasks = (uint32_t)(chains * s->tiles);
+  const size_t words = 16 + (size_t)chains * (2 * (int64_t)s->tiles + supers) * kScanCols;
+  bool is_new = true;
+  for (const StreamScratch::Block& b : scratch.blocks) is_new = is_new && b.stream != st;
+  if (is_new) {
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    DISTDL_HIP_TRY(hipStreamIsCapturing(st, &capture));
+    if (capture != hipStreamCaptureStatusNone)
+      return set_error(DISTDL_ERR_INVALID_ARG, "scan: the plan's first call on this stream, which is being captured");
   }
-  if (back) hipLaunchKernelGGL((scan_bwd_kernel<E, GATE, PAIR>), grid, block, 0, st, s);
-  else hipLaunchKernelGGL((scan_fwd_kernel<E, GATE, PAIR>), grid, block, 0, st, s);
+  float* at = nullptr;
+  const int rc = scratch.get(2 * words, st, &at);
+  if (rc) return rc;
+  s->words = (uint64_t*)at;
+  if (is_new)
+    hipLaunchKernelGGL(scan_clear_kernel, dim3((unsigned)std::min<size_t>((words + 255) / 256, 4096)), dim3(256), 0, st, s->words, words);
+  DISTDL_HIP_TRY(hipGetLastError());
+  return DISTDL_OK;
+}
+
+template <class E, int GATE, bool PAIR>
+static int launch_scan(distdl_scan_plan* p, ScanArgs& s, bool back, hipStream_t st) {
+  const dim3 block(64 * kScanWaves);
+  if (p->few) {
+    const int rc = scan_words(p->words[back][PAIR], kScanWaves * (back ? kFewBack : kFewSteps), st, &s);
+    if (rc) return rc;
+    if (back) hipLaunchKernelGGL((scan_few_bwd_kernel<E, GATE, PAIR>), dim3(s.tasks), dim3(64 * kScanWaves), 0, st, s);
+    else hipLaunchKernelGGL((scan_few_fwd_kernel<E, GATE, PAIR>), dim3(s.tasks), dim3(64 * kScanWaves), 0, st, s);
+  } else {
+    const dim3 grid((unsigned)((int64_t)s.groups * s.n_b));
+    if (back) hipLaunchKernelGGL((scan_bwd_kernel<E, GATE, PAIR>), grid, block, 0, st, s);
+    else hipLaunchKernelGGL((scan_fwd_kernel<E, GATE, PAIR>), grid, block, 0, st, s);
+  }
+  return DISTDL_OK;
 }
 
 // Whether every row of every array starts at a multiple of two elements.
@@ -685,13 +925,9 @@ int distdl_scan_plan_create(distdl_scan_plan** out, int64_t n_b, int64_t T, int6
     p->gate = gate;
     p->dtype = dtype;
     p->groups = (int)groups;
-    // More than 128 workgroups go through all of time in one launch, fewer cut it so that there are four for each of the 256 compute units, a
-    // segment of a tile at least.  Measured, 67 million bf16 steps of a channel (us, one launch; two): 128 workgroups 135, 133
-    // (adjoint 227, 220), 256 workgroups 84, 137 (166, 221), 512 workgroups 93, 142 (167, 218).
-    const int64_t tile = 16 * kScanWaves, alone = groups * n_b;
-    const int64_t segments = alone > 128 ? 1 : std::min((1024 + alone - 1) / alone, std::max<int64_t>(1, T / tile));
-    p->seg_steps = (((T + segments - 1) / segments) + tile - 1) / tile * tile;
-    p->segments = (int)((T + p->seg_steps - 1) / p->seg_steps);
+    // Measured (us, one workgroup through all of time; one for a tile): 67 million bf16 steps in 128 chains 123, 104 (adjoint 223, 187), in
+    // 256 chains 84, 95 (167, 174); 32 chains of 128 steps 6.5, 6.8 (9.7, 7.8), of 256 9.9, 7.7 (15.6, 8.9), of 1024 30, 11 (49, 18).
+    p->few = groups * n_b <= kScanFew && T > kScanShort && T / P >= 64 && groups * n_b * (T / 64 + P) < int64_t(1) << 30;
     *out = p.release();
     return DISTDL_OK;
   });
@@ -700,7 +936,8 @@ int distdl_scan_plan_create(distdl_scan_plan** out, int64_t n_b, int64_t T, int6
 int distdl_scan_plan_destroy(distdl_scan_plan* p) {
   if (!p) return DISTDL_OK;
   p->table.release();
-  p->maps.release();
+  for (auto& of : p->words)
+    for (auto& w : of) w.release();
   delete p;
   return DISTDL_OK;
 }
@@ -729,10 +966,11 @@ int distdl_scan_fwd(distdl_scan_plan* p, const void* const a_dev[], const void* 
     {
       ProfScope prof("scan_fwd", st_);
       scan_kind(p->dtype, p->gate, [&](auto e, auto gate) {
-        if (scan_pairs(p, w)) launch_scan<decltype(e), decltype(gate)::value, true>(s, false, st_);
-        else launch_scan<decltype(e), decltype(gate)::value, false>(s, false, st_);
+        rc = scan_pairs(p, w) ? launch_scan<decltype(e), decltype(gate)::value, true>(p, s, false, st_)
+                              : launch_scan<decltype(e), decltype(gate)::value, false>(p, s, false, st_);
       });
     }
+    if (rc) return rc;
     DISTDL_HIP_TRY(hipGetLastError());
     return DISTDL_OK;
   });
@@ -766,10 +1004,11 @@ int distdl_scan_bwd(distdl_scan_plan* p, const void* const a_dev[], const void* 
     {
       ProfScope prof("scan_bwd", st_);
       scan_kind(p->dtype, p->gate, [&](auto e, auto gate) {
-        if (scan_pairs(p, w)) launch_scan<decltype(e), decltype(gate)::value, true>(s, true, st_);
-        else launch_scan<decltype(e), decltype(gate)::value, false>(s, true, st_);
+        rc = scan_pairs(p, w) ? launch_scan<decltype(e), decltype(gate)::value, true>(p, s, true, st_)
+                              : launch_scan<decltype(e), decltype(gate)::value, false>(p, s, true, st_);
       });
     }
+    if (rc) return rc;
     DISTDL_HIP_TRY(hipGetLastError());
     return DISTDL_OK;
   });

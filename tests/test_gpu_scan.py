@@ -106,6 +106,77 @@ def test_many_channels_in_one_segment():
     check(3, 140, 70000, 1, "bf16", True, ragged=True, seed=5)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,T,C,P", [(1, 20011, 130, 2), (2, 9001, 35, 3), (128, 600, 2, 1), (129, 600, 2, 1), (1, 12345, 1, 7), (1, 2300, 40, 20)])
+def test_long(n, T, C, P, dtype):
+    require_gpu()
+    check(n, T, C, P, dtype, True, ragged=n > 1, seed=11)
+
+
+@pytest.mark.parametrize("n,T", [(2, 40), (2, 9000), (140, 700)])
+def test_a_state_of_zero_stays_zero(n, T):
+    """Given gates whose product is beyond the type's range leave zeros alone; the state that enters later is carried as by single steps."""
+    require_gpu()
+    C = 6
+    a, x = torch.full((n, T, C), 1e3, device="cuda"), torch.zeros(n, T, C, device="cuda")
+    a[:, T - 3:] = 0.5
+    x[:, T - 3] = 8.0
+    plan = dd.distdl_scan_plan_create(n, T, C, 1, "given", torch.float32)
+    h, hT = [torch.full_like(x, 3.0)], torch.empty(n, C, device="cuda")
+    dd.distdl_scan_fwd(plan, [a], [x], None, None, h, hT)
+    assert not h[0][:, :T - 3].any()
+    assert h[0][:, T - 3:].equal(torch.tensor([8.0, 4.0, 2.0], device="cuda")[None, :, None].expand(n, 3, C)) and (hT == 2).all()
+    a[:, T - 3:] = 1e3
+    da, dx, dh0 = [torch.empty_like(x)], [torch.empty_like(x)], torch.empty(n, C, device="cuda")
+    dh = torch.zeros_like(x)
+    dh[:, 0] = 2.0
+    dd.distdl_scan_bwd(plan, [a], None, h, None, None, [dh], None, da, dx, dh0)
+    assert not dx[0][:, 1:].any() and (dx[0][:, 0] == 2).all() and (dh0 == 2000).all() and not da[0].any()
+
+
+@pytest.mark.parametrize("T", [900, 9000])
+def test_passes_one_after_the_other(T):
+    """Calls of both directions, eager, on two streams and replayed, leave each other's results alone."""
+    require_gpu()
+    n, C = 2, 150
+    ds = [make(n, T, C, 2, "bf16", True, False, seed=s) for s in (1, 2)]
+    plan = dd.distdl_scan_plan_create(n, T, C, 2, "sigmoid", torch.bfloat16)
+    new = lambda: [torch.zeros_like(t) for t in ds[0]["x"]]  # noqa: E731
+
+    def run(d, out):
+        dd.distdl_scan_fwd(plan, d["a"], d["x"], d["h0"], None, out[0], None)
+        dd.distdl_scan_bwd(plan, d["a"], d["x"], out[0], d["h0"], None, d["dh"], d["dhT"], out[1], out[2], None)
+
+    want = [[new() for _ in range(3)] for _ in ds]
+    for d, w in zip(ds, want):
+        run(d, w)
+    torch.cuda.synchronize()
+    same = lambda a, b: all(torch.equal(u, v) for s, t in zip(a, b) for u, v in zip(s, t))  # noqa: E731
+    streams, outs = [torch.cuda.Stream() for _ in ds], [[new() for _ in range(3)] for _ in ds]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for d, s, o in zip(ds, streams, outs):
+            with torch.cuda.stream(s):
+                run(d, o)
+    torch.cuda.synchronize()
+    assert all(same(w, o) for w, o in zip(want, outs))
+    graph, out = torch.cuda.CUDAGraph(), [new() for _ in range(3)]
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=streams[0]):
+        run(ds[0], out)
+    for _ in range(3):
+        for t in out:
+            for u in t:
+                u.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(want[0], out)
+        with torch.cuda.stream(streams[0]):
+            run(ds[1], outs[1])
+        torch.cuda.synchronize()
+        assert same(want[1], outs[1])
+
+
 def test_defaults_and_lengths_outside():
     """No h0, lengths, dhT: zeros and whole sequences; lengths below zero and beyond T are cut."""
     require_gpu()
