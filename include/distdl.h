@@ -409,7 +409,7 @@ int distdl_dot_static(const void* const a_dev[], const void* const b_dev[], cons
  * travel with the launch, so a call with arrays that a plan has not seen
  * neither copies a table nor fails while its stream is being captured (the
  * update of many arrays does both, as the other layers do); scratch is still
- * allocated by a plan's first call on a stream.
+ * allocated by a plan's first call on a stream, which cannot be a recorded one.
  *
  * 8-BIT NUMBERS.  A code is e4m3 (no infinities, largest 448); a block of 128
  * consecutive numbers of a row shares a scale 2^(byte - 127), one byte
@@ -440,7 +440,8 @@ int distdl_quant8(const void* const x_dev[], const int64_t rows[], const int64_t
  *        [fi_j][fo_i] (the transpose) in tiles
  * bwd_w: dW_ij [fo_i][fi_j] = dy_i^T x_j, from dyt_i [fo_i][n_b] and xt_j
  *        [fi_j][n_b] in blocks of rows (that is, along the batch)
- * Each is what distdl_quant8 writes.  Outputs must not overlap inputs. */
+ * Each is what distdl_quant8 writes.  Outputs must not overlap inputs.
+ * UNSUPPORTED: results of more than 64 rows with sums of more than 2^24. */
 typedef struct distdl_linear8_plan distdl_linear8_plan;
 int distdl_linear8_plan_create(distdl_linear8_plan** out, int64_t n_b, int64_t n_fi, int64_t n_fo, int P_fo,
                                int P_fi, distdl_dtype dtype);
@@ -492,7 +493,10 @@ int distdl_rmsnorm_bwd(distdl_rmsnorm_plan* plan, const void* const s_dev[], con
  * step: one token for each row: state_dev[slots[row]] is read and
  *   overwritten, h is the new state in the tensor's type.  slots NULL: row i has
  *   state i.  A row whose slot is not in 0 .. n_slots - 1 is idle: its h is 0
- *   and no state changes.  Slots of one call must differ. */
+ *   and no state changes.  Slots of one call must differ.
+ * Steps are composed: the product of given gates is held within the range of
+ * 32 bits, so a state of zero stays zero under any finite gates.
+ * UNSUPPORTED: T from 2^30 or n_c from 2^25 on. */
 typedef enum { DISTDL_GATE_GIVEN = 0, DISTDL_GATE_SIGMOID = 1 } distdl_gate;
 typedef struct distdl_scan_plan distdl_scan_plan;
 int distdl_scan_plan_create(distdl_scan_plan** out, int64_t n_b, int64_t T, int64_t n_c, int P, distdl_gate gate,

@@ -493,8 +493,8 @@ def _one(what, t, kinds, numel):
 
 
 def _many(what, ts, kinds, numels):
-    """Their addresses as the library reads them; None stays NULL.  (Small passes are bound by the host: a hundred arrays take 10 us
-    here, and half as long again with a call for each and an array of ctypes.)"""
+    """Their addresses as the library reads them; None stays NULL.  (Small passes are bound by the host: four lists of
+    ten arrays take 21 us here, and 27 with a call for each array and an array of ctypes.)"""
     if ts is None:
         return None
     if len(ts) != len(numels):

@@ -6,7 +6,7 @@
 // One pass: every number is read and written once, 16 bytes an element with 8-bit moments and a 32-bit gradient, 28 with 32-bit ones, so
 // memory bounds it.  A workgroup takes consecutive elements of one array, from a table made with the plan; a thread takes
 // eight at a time, so that 16 lanes (one DPP row) hold a block of 128 and its scales need no LDS.  Measured: 168 million weights, bf16
-// gradients, 8-bit moments and bf16 copies 518 us (5.2 TB/s); 67 million with fp32 moments and copies 348 us (5.4 TB/s).  A thread
+// gradients, 8-bit moments and bf16 copies 509 to 565 us (4.8 to 5.3 TB/s); 67 million with fp32 moments and copies 348 us (5.4 TB/s).  A thread
 // has eight elements of fp32 moments (twice as many: 361 us) and sixteen of 8-bit ones (half as many: 550 us, twice: 603).
 //
 // 8-bit moments: m and r = sqrt(v) as e4m3 codes (r, since v has twice the range), rounded up or down at random with the

@@ -16,8 +16,8 @@
 //   N(0, 1) products are 1e-8 to 3e-7 off.  Fp32 results take it (weight gradients among them), and products whose time
 //   is not that of the matrix instructions.
 //
-// Measured (us): 8 x 4096 x 4096 6.9 (2.4 TB/s of weights; a launch and a trip to memory are most of it), 256 x 4096 x 4096 on 2 x 2 workers 17,
-// 8192 x 4096 x 4096 142 (1.94 PFLOP/s, 73 % of the library's 8192^3), the same in fp32 270 to 290 (0.95 to 1.02 PFLOP/s: conversions, of
+// Measured (us): 8 x 4096 x 4096 7 (2.4 TB/s of weights; a launch and a trip to memory are most of it), 256 x 4096 x 4096 on 2 x 2 workers 17 to 18,
+// 8192 x 4096 x 4096 142 to 154 (1.8 to 1.9 PFLOP/s, 73 % of the library's 8192^3), the same in fp32 265 to 290 (0.95 to 1.02 PFLOP/s: conversions, of
 // which a wave makes one for 2.7 products).
 #include <algorithm>
 #include <cstddef>

@@ -7,9 +7,13 @@
 // and write every element once and are bound by memory, so a row is held in registers between its sum and its use, and a workgroup that
 // goes from row to row has the next row's loads under way meanwhile.  A wave takes pieces of 512 features of one worker, each through a
 // buffer that ends with the worker's row, so that features that are not there need no test.  A row belongs to 1, 4, 8 or 16 waves, by
-// what keeps at most two pieces in a wave; wider rows (over 16384 features) are read twice, the second time from the caches.
+// what keeps at most two pieces in a wave (adjoint: one); rows wider than that, over 16384 features (adjoint: 8192), are read twice, the second
+// time from the caches, and dg is made by a launch of its own in front.
 // ROWS16: every row starts at a multiple of 16 bytes, a lane's eight features are neighbours (two accesses of fp32, one of bf16).  Otherwise
 // they are 64 apart, each access at its natural alignment: wide accesses that straddle cost more than narrow ones.
+//
+// Measured: forward 8192 x 4096 bf16 on two workers, residual in, sum and 8-bit codes out, 50 us (4.8 TB/s); adjoint 5003 x 2000 fp32 on three workers
+// 34 us (4.7 TB/s) and 5 for the sum of dg's parts; forward 4 x 4096 3.7 us, a launch and a trip to memory.
 #include <algorithm>
 #include <cstddef>
 

@@ -74,8 +74,8 @@ __device__ __forceinline__ ScanSpan scan_span(const ScanArgs& s, int t) {
 }
 
 // The two channels of a lane in one step: neighbours in one access of twice the size (PAIR), where every row starts at a multiple of that, and
-// otherwise 64 apart in two, each at its natural alignment.  Measured, 7 x 2049 steps of fp32, adjoint: 1024 channels in pairs 92 us;
-// 1001 and 1002 channels in pairs that straddle 203 and 163 us.
+// otherwise 64 apart in two, each at its natural alignment.  Measured (us, pairs; one by one): bf16 65536 x 1024
+// 102, 154, adjoint of 8 x 4096 x 2048 180, 194, of 16 x 2048 x 2048 168, 197; fp32 16 x 2048 x 2048 160, 159, its adjoint 277, 286.
 template <bool PAIR>
 __device__ __forceinline__ int scan_channel(int lane, int v) { return PAIR ? lane * 2 + v : lane + 64 * v; }
 
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
 // time: who waits, waits for tickets drawn before its own, so the lowest ticket not yet done never waits and every wait ends, however
 // few workgroups the card holds at a time.  Tickets go on from pass to pass: their quotient by the pass's tiles is the tag.
 //
-// Measured (us): 65536 x 1024 bf16 on four workers 100 (4.0 TB/s), adjoint of 7 x 2049 x 1001 fp32 71 (4.8 TB/s); with time read twice, once for the
+// Measured (us): 65536 x 1024 bf16 on four workers 100 to 105 (3.9 to 4.0 TB/s), adjoint of 7 x 2049 x 1001 fp32 71 to 75 (4.6 to 4.9 TB/s); with time read twice, once for the
 // maps, 145 and 88; without the waits 94 and 74, and the rest is what a workgroup takes from its start to its stores, two at a time on a
 // compute unit.  Gates made twice instead of held (tiles twice as long): 100 and 85.  Workgroups that go from tile to tile and have the next
 // one's loads under way, whose loads the waits then stand behind: 133 and 83.  Four waves: 107 and 83, sixteen: 215 and 122.
