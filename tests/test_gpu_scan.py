@@ -177,6 +177,34 @@ def test_passes_one_after_the_other(T):
         assert same(want[1], outs[1])
 
 
+def test_first_call_cannot_be_recorded():
+    """What few chains publish needs memory that starts as zeros: refused while the stream is captured, and fine afterwards."""
+    require_gpu()
+    d = make(2, 700, 20, 1, "f32", True, False)
+    plan = dd.distdl_scan_plan_create(2, 700, 20, 1, "sigmoid", torch.float32)
+    h, want = [torch.zeros_like(d["x"][0])], [torch.zeros_like(d["x"][0])]
+    stream, graph, mark = torch.cuda.Stream(), torch.cuda.CUDAGraph(), torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()
+    call = lambda to: dd.distdl_scan_fwd(plan, d["a"], d["x"], d["h0"], None, to, None)  # noqa: E731
+    with torch.cuda.graph(graph, stream=stream):
+        mark.add_(1)
+        with pytest.raises(dd.DistdlError, match="captured"):
+            call(h)
+    torch.cuda.synchronize()
+    assert not h[0].any()
+    with torch.cuda.stream(stream):
+        call(want)
+    torch.cuda.synchronize()
+    again = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(again, stream=stream):
+        call(h)
+    for _ in range(2):
+        h[0].zero_()
+        again.replay()
+        torch.cuda.synchronize()
+        assert want[0].any() and torch.equal(h[0], want[0])
+
+
 def test_defaults_and_lengths_outside():
     """No h0, lengths, dhT: zeros and whole sequences; lengths below zero and beyond T are cut."""
     require_gpu()
