@@ -6,7 +6,7 @@
 // are written in runs of a whole block.
 //
 // Measured: 8192 x 4096 bf16 to codes in both orders 31 us (4.4 TB/s).  A thread with half the elements, 512 to a
-// workgroup: 48 us.
+// workgroup: 48 us.  Neighbouring tiles on one XCD: 36 us for 33.  Codes of one order alone: 25 to 28.
 #include <algorithm>
 #include <cstddef>
 

@@ -926,8 +926,9 @@ int distdl_scan_plan_create(distdl_scan_plan** out, int64_t n_b, int64_t T, int6
     p->dtype = dtype;
     p->groups = (int)groups;
     // Measured (us, one workgroup through all of time; one for a tile): 67 million bf16 steps in 128 chains 123, 104 (adjoint 223, 187), in
-    // 256 chains 84, 95 (167, 174); 32 chains of 128 steps 6.5, 6.8 (9.7, 7.8), of 256 9.9, 7.7 (15.6, 8.9), of 1024 30, 11 (49, 18).
-    p->few = groups * n_b <= kScanFew && T > kScanShort && T / P >= 64 && groups * n_b * (T / 64 + P) < int64_t(1) << 30;
+    // 256 chains 84, 95 (167, 174); 32 chains of 128 steps 6.5, 6.8 (9.7, 7.8), of 256 9.9, 7.7 (15.6, 8.9), of 1024 30, 11 (49, 18); 8 chains of
+    // 4096 steps on 128 workers 232, 28 (410, 29).  A worker has eight steps at least, so that what tiles publish (2 KiB each) is no more than an array.
+    p->few = groups * n_b <= kScanFew && T > kScanShort && T / P >= 8 && groups * n_b * (T / 64 + P) < int64_t(1) << 30;
     *out = p.release();
     return DISTDL_OK;
   });

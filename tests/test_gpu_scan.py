@@ -107,7 +107,7 @@ def test_many_channels_in_one_segment():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("n,T,C,P", [(1, 20011, 130, 2), (2, 9001, 35, 3), (128, 600, 2, 1), (129, 600, 2, 1), (1, 12345, 1, 7), (1, 2300, 40, 20)])
+@pytest.mark.parametrize("n,T,C,P", [(1, 20011, 130, 2), (2, 9001, 35, 3), (128, 600, 2, 1), (129, 600, 2, 1), (1, 12345, 1, 7), (1, 2300, 40, 20), (2, 700, 40, 64), (1, 257, 9, 32)])
 def test_long(n, T, C, P, dtype):
     require_gpu()
     check(n, T, C, P, dtype, True, ragged=n > 1, seed=11)
