@@ -290,10 +290,10 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
     }
 #pragma unroll
     for (int v = 0; v < kScanV; ++v) {
-      A[v] = scan_more<GATE>(1.f, a[0][v]);
-      B[v] = u[0][v];
+      A[v] = 1.f;
+      B[v] = 0.f;  // (times the first gate as well, so that one that is not a number stays in the map)
 #pragma unroll
-      for (int i = 1; i < L; ++i) {
+      for (int i = 0; i < L; ++i) {
         A[v] = scan_more<GATE>(A[v], a[i][v]);
         B[v] = fmaf(a[i][v], B[v], u[i][v]);
       }

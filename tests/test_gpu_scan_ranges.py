@@ -1,0 +1,62 @@
+"""The recurrence at the ends of its range: what is not a number inside a sequence, and behind its end.
+
+Steps are composed in runs of eight or more, tiles of 64 or 128 are joined within a workgroup or across them, so positions at the start, in the
+middle and at the end of each are taken.  Nothing here has a tolerance: what a number must not reach stays as it was, to the bit."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2006_03108_amd as dd
+from gpu_util import require_gpu
+
+pytestmark = pytest.mark.gpu
+# one workgroup through all of time (few steps; many chains), and one for each tile
+SIZES = [(2, 100, 9, 1), (140, 300, 2, 2), (2, 700, 9, 1), (1, 2300, 130, 3)]
+
+
+def rnd(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")
+
+
+def cut(x, P):
+    sizes = [x.shape[1] // P + (r < x.shape[1] % P) for r in range(P)]
+    return [t.contiguous() for t in x.split(sizes, 1)]
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("gate", ["given", "sigmoid"])
+@pytest.mark.parametrize("n,T,C,P", SIZES)
+def test_a_gate_that_is_not_a_number(n, T, C, P, gate, kind):
+    """A NaN gate makes its channel NaN from its step on, forwards and backwards, also where the state in front of it is zero; nothing else changes."""
+    require_gpu()
+    plan = dd.distdl_scan_plan_create(n, T, C, P, gate, kind)
+    a, x, dh = torch.sigmoid(rnd(1, n, T, C)).to(kind), rnd(2, n, T, C).to(kind), rnd(3, n, T, C).to(kind)
+    x[:, :T // 2] = 0  # (no h0 either: the states up to there are zero)
+
+    def run(gates, h=None):
+        out = [[torch.empty_like(t) for t in cut(x, P)] for _ in range(3)]
+        hT, dh0 = torch.empty(n, C, device="cuda"), torch.empty(n, C, device="cuda")
+        dd.distdl_scan_fwd(plan, cut(gates, P), cut(x, P), None, None, out[0], hT)
+        dd.distdl_scan_bwd(plan, cut(gates, P), cut(x, P), out[0] if h is None else cut(h, P), None, None, cut(dh, P), None, out[1], out[2], dh0)
+        return [torch.cat(t, 1) for t in out] + [hT, dh0]
+
+    h, da, dx, hT, dh0 = run(a)
+    for at in (0, 1, 8, 64, 77, T // 2 + 3, T - 1):
+        b, c = n - 1, at % C
+        gates = a.clone()
+        gates[b, at, c] = float("nan")
+        h2, da2, dx2, hT2, dh02 = run(gates, h)
+        here = torch.zeros(n, T, C, dtype=torch.bool, device="cuda")
+        here[b, at:, c] = True
+        assert torch.equal(torch.isnan(h2), here) and torch.equal(h2[~here], h[~here]), at
+        end = torch.zeros(n, C, dtype=torch.bool, device="cuda")
+        end[b, c] = True
+        assert torch.equal(torch.isnan(hT2), end) and torch.equal(hT2[~end], hT[~end]), at
+        # d of the step itself does not know its gate, and with given gates neither does da
+        here = torch.zeros(n, T, C, dtype=torch.bool, device="cuda")
+        here[b, :at, c] = True
+        own = here.clone()
+        own[b, at, c] = gate == "sigmoid"
+        for got, want, bad in ((da2, da, own), (dx2, dx, own)):
+            assert torch.equal(torch.isnan(got), bad) and torch.equal(got[~bad], want[~bad]), at
+        assert torch.equal(torch.isnan(dh02), end) and torch.equal(dh02[~end], dh0[~end]), at
