@@ -421,8 +421,9 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
       for (int v = 0; v < kScanV; ++v) {
         const float all = d[i][v] + back[v];
         back[v] = a[i][v] * all;
-        da[v] = all * slope[i][v];
-        dx[v] = all * rest[i][v];
+        const float live = i < now.cnt - now.live ? 0.f : all;  // (what passes through the steps behind a sequence's end may be infinite)
+        da[v] = live * slope[i][v];
+        dx[v] = live * rest[i][v];
       }
       const ScanLane o = off.where(i < now.cnt);
       const uint32_t step = i < now.cnt ? (now.cnt - 1 - i) * hop : 0;
@@ -756,8 +757,9 @@ __global__ __launch_bounds__(64 * kScanWaves, 4) void scan_few_bwd_kernel(ScanAr
     for (int v = 0; v < kScanV; ++v) {
       const float all = d[i][v] + back[v];
       back[v] = a[i][v] * all;
-      da[v] = all * slope[i][v];
-      dx[v] = all * rest[i][v];
+      const float live = i < dead ? 0.f : all;  // (what passes through the steps behind a sequence's end may be infinite)
+      da[v] = live * slope[i][v];
+      dx[v] = live * rest[i][v];
     }
     const ScanLane o = off.where(i < cnt);
     const uint32_t step = i < cnt ? (cnt - 1 - i) * hop : 0;

@@ -60,3 +60,33 @@ def test_a_gate_that_is_not_a_number(n, T, C, P, gate, kind):
         for got, want, bad in ((da2, da, own), (dx2, dx, own)):
             assert torch.equal(torch.isnan(got), bad) and torch.equal(got[~bad], want[~bad]), at
         assert torch.equal(torch.isnan(dh02), end) and torch.equal(dh02[~end], dh0[~end]), at
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("gate", ["given", "sigmoid"])
+@pytest.mark.parametrize("n,T,C,P", SIZES)
+def test_steps_behind_the_end_get_zeros(n, T, C, P, gate, kind):
+    """Whatever the gradient of the last state is, and whatever lies behind the end, the gradients there are zeros; dhT passes to the sequence itself."""
+    require_gpu()
+    plan = dd.distdl_scan_plan_create(n, T, C, P, gate, kind)
+    a, x, dh = torch.sigmoid(rnd(1, n, T, C)).to(kind), rnd(2, n, T, C).to(kind), rnd(3, n, T, C).to(kind)
+    h0, dhT = rnd(4, n, C), rnd(5, n, C)
+    for end in (0, 1, T // 3, 64, T - 1):
+        lengths = torch.full((n,), end, dtype=torch.int32, device="cuda")
+        behind = torch.arange(T, device="cuda")[None, :, None].expand(n, T, C) >= end
+        bad = dhT.clone()
+        bad[:, 0], bad[:, 1] = float("inf"), float("nan")
+        out = [[torch.full_like(t, 7.0) for t in cut(x, P)] for _ in range(5)]
+        dh0 = [torch.empty(n, C, device="cuda") for _ in range(2)]
+        poisoned = [cut(t.masked_fill(behind, float("nan")), P) for t in (a, x, dh)]
+        dd.distdl_scan_fwd(plan, poisoned[0], poisoned[1], h0, lengths, out[0], None)
+        dd.distdl_scan_bwd(plan, poisoned[0], poisoned[1], out[0], h0, lengths, poisoned[2], dhT, out[1], out[2], dh0[0])
+        dd.distdl_scan_bwd(plan, poisoned[0], poisoned[1], out[0], h0, lengths, poisoned[2], bad, out[3], out[4], dh0[1])
+        for t in out:
+            assert not torch.cat(t, 1)[behind].any(), end
+        for want, got in zip(out[1:3], out[3:5]):
+            want, got = torch.cat(want, 1), torch.cat(got, 1)
+            assert torch.equal(got[:, :, 2:], want[:, :, 2:]) and torch.isnan(got[:, :end, 1]).all(), end
+            assert not torch.isfinite(got[:, end - 1:end, 0]).any(), end
+        if end == 0:
+            assert torch.equal(dh0[0], dhT) and torch.equal(dh0[1][:, 0], bad[:, 0]) and torch.isnan(dh0[1][:, 1]).all()
