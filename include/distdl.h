@@ -494,8 +494,10 @@ int distdl_rmsnorm_bwd(distdl_rmsnorm_plan* plan, const void* const s_dev[], con
  *   overwritten, h is the new state in the tensor's type.  slots NULL: row i has
  *   state i.  A row whose slot is not in 0 .. n_slots - 1 is idle: its h is 0
  *   and no state changes.  Slots of one call must differ.
- * Steps are composed: the product of given gates is held within the range of
- * 32 bits, so a state of zero stays zero under any finite gates.
+ * Steps are composed in runs.  Products of given gates have the range of 64
+ * bits (up to 2^1000 in a run), so what single steps keep in the range of 32
+ * bits, the sum of their terms' magnitudes included, comes out as by single
+ * steps, and a state of zero stays zero under any finite gates.
  * UNSUPPORTED: T from 2^30 or n_c from 2^25 on. */
 typedef enum { DISTDL_GATE_GIVEN = 0, DISTDL_GATE_SIGMOID = 1 } distdl_gate;
 typedef struct distdl_scan_plan distdl_scan_plan;

@@ -164,11 +164,42 @@ __device__ __forceinline__ void scan_gate(float g, float& a, float& rest) {
   }
 }
 
-// One more gate of a run of them.  The product of given gates is held finite: it meets states of zero, which stay zero.
+// The factor of a map.  Sigmoid gates are at most one, and a product of them that is lost to zero would have lost any state.  Given gates may grow and
+// shrink in turn: their product is a number of 64 bits, of at most 2^1000, and so is a state on its way through maps.  What single steps keep in the
+// range of 32 bits is in range there, and a state of zero, which meets no infinity, stays zero.  Measured (us; products held in the range of 32 bits before):
+// 65536 x 1024 bf16 107 (102), its adjoint 186 (173), 32768 x 1024 fp32 93 (93), its adjoint 144 (140); with many chains no difference.
 template <int GATE>
-__device__ __forceinline__ float scan_more(float A, float a) {
-  return GATE == DISTDL_GATE_GIVEN ? __builtin_amdgcn_fmed3f(A * a, -3.40282347e38f, 3.40282347e38f) : A * a;
-}
+struct ScanProduct {
+  typedef float Factor;
+  float m = 1.f;
+  __device__ __forceinline__ void more(float a) { m *= a; }
+  __device__ __forceinline__ Factor factor() const { return m; }
+};
+template <>
+struct ScanProduct<DISTDL_GATE_GIVEN> {
+  typedef double Factor;
+  float m = 1.f;  // product of mantissas of 1/2 to 1: of a wave's steps it is no less than 2^-16
+  int e = 0;
+  __device__ __forceinline__ void more(float a) {
+    m *= __builtin_amdgcn_frexp_mantf(a);
+    e += __builtin_amdgcn_frexp_expf(a);
+  }
+  __device__ __forceinline__ Factor factor() const { return __builtin_amdgcn_ldexp((double)m, min(e, 1000)); }
+};
+template <int GATE>
+using ScanFactor = typename ScanProduct<GATE>::Factor;
+
+__device__ __forceinline__ float scan_apply(float A, float state, float B) { return fmaf(A, state, B); }
+__device__ __forceinline__ double scan_apply(double A, double state, float B) { return fma(A, state, (double)B); }
+__device__ __forceinline__ float scan_then(float first, float then) { return first * then; }
+__device__ __forceinline__ double scan_then(double first, double then) { return fmax(fmin(first * then, 0x1p1000), -0x1p1000); }
+
+// The maps of a workgroup's waves
+template <int GATE>
+struct ScanMaps {
+  ScanFactor<GATE> A[kScanWaves][kScanCols];
+  float B[kScanWaves][kScanCols];
+};
 
 // (the compiler does not know that it is the same in all lanes, and would make every branch on it one of lanes)
 __device__ __forceinline__ int scan_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
@@ -198,21 +229,30 @@ __device__ __forceinline__ void scan_start(const ScanArgs& s, const ScanPlace& a
 }
 
 // The maps of all waves, each behind the one before it: `mine` is the state in front of this wave's steps, `state` that behind the tile.
-__device__ __forceinline__ void scan_meet(float (*lds)[2][kScanCols], const float* A, const float* B, float* state, float* mine) {
+template <int GATE>
+__device__ __forceinline__ void scan_meet(ScanMaps<GATE>& lds, const ScanFactor<GATE>* A, const float* B, float* state, float* mine) {
   const int wave = scan_wave(), lane = threadIdx.x & 63;
 #pragma unroll
   for (int v = 0; v < kScanV; ++v) {
-    lds[wave][0][v * 64 + lane] = A[v];
-    lds[wave][1][v * 64 + lane] = B[v];
+    lds.A[wave][v * 64 + lane] = A[v];
+    lds.B[wave][v * 64 + lane] = B[v];
   }
   __syncthreads();
+  ScanFactor<GATE> at[kScanV], here[kScanV];
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v) at[v] = state[v];
 #pragma unroll
   for (int w = 0; w < kScanWaves; ++w) {
 #pragma unroll
     for (int v = 0; v < kScanV; ++v) {
-      if (w == wave) mine[v] = state[v];
-      state[v] = fmaf(lds[w][0][v * 64 + lane], state[v], lds[w][1][v * 64 + lane]);
+      if (w == wave) here[v] = at[v];
+      at[v] = scan_apply(lds.A[w][v * 64 + lane], at[v], lds.B[w][v * 64 + lane]);
     }
+  }
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v) {
+    mine[v] = here[v];
+    state[v] = at[v];
   }
 }
 
@@ -238,7 +278,7 @@ struct ScanTile {
 template <class E, int GATE, bool PAIR>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
   constexpr int L = 8;
-  __shared__ float lds[2][kScanWaves][2][kScanCols];
+  __shared__ ScanMaps<GATE> lds[2];
   const ScanTable table = SCAN_TABLE(s);
   const ScanPlace at = scan_place<PAIR>(s, xcd_order(blockIdx.x, gridDim.x));
   const int wave = scan_wave();
@@ -269,7 +309,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
   float state[kScanV];
   scan_start<PAIR>(s, at, s.h0, state);
   for (int turn = 0;; turn ^= 1) {
-    float a[L][kScanV], u[L][kScanV], A[kScanV], B[kScanV], h[kScanV];
+    float a[L][kScanV], u[L][kScanV], B[kScanV], h[kScanV];
+    ScanFactor<GATE> A[kScanV];
 #pragma unroll
     for (int i = 0; i < L; ++i) {
       float g[kScanV], x[kScanV];
@@ -290,18 +331,19 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_fwd_kernel(ScanArgs s) {
     }
 #pragma unroll
     for (int v = 0; v < kScanV; ++v) {
-      A[v] = 1.f;
+      ScanProduct<GATE> all;
       B[v] = 0.f;  // (times the first gate as well, so that one that is not a number stays in the map)
 #pragma unroll
       for (int i = 0; i < L; ++i) {
-        A[v] = scan_more<GATE>(A[v], a[i][v]);
+        all.more(a[i][v]);
         B[v] = fmaf(a[i][v], B[v], u[i][v]);
       }
+      A[v] = all.factor();
     }
     const ScanTile now = t;
     const bool more = now.next < s.T;
     t = tile(more ? now.next : now.next - 1, more);
-    scan_meet(lds[turn], A, B, state, h);
+    scan_meet<GATE>(lds[turn], A, B, state, h);
 #pragma unroll
     for (int i = 0; i < L; ++i)
 #pragma unroll
@@ -325,7 +367,7 @@ template <class E, int GATE, bool PAIR>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
   constexpr int L = sizeof(ScanRaw<E, PAIR>) == 4 ? 8 : 4;  // what the registers hold beside the next tile's loads
   constexpr bool X = GATE != DISTDL_GATE_GIVEN;
-  __shared__ float lds[2][kScanWaves][2][kScanCols];
+  __shared__ ScanMaps<GATE> lds[2];
   const ScanTable table = SCAN_TABLE(s);
   const ScanPlace at = scan_place<PAIR>(s, xcd_order(blockIdx.x, gridDim.x));
   const int wave = scan_wave();
@@ -367,8 +409,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
   scan_start<PAIR>(s, at, s.end, state);
   for (int turn = 0;; turn ^= 1) {
     // dx = d rest, da = d slope
-    float a[L][kScanV], d[L][kScanV], rest[L][kScanV], slope[L][kScanV], A[kScanV], B[kScanV], back[kScanV];
-    float last[kScanV];
+    float a[L][kScanV], d[L][kScanV], rest[L][kScanV], slope[L][kScanV], B[kScanV], back[kScanV], last[kScanV];
+    ScanFactor<GATE> A[kScanV];
     edge.values(last);
 #pragma unroll
     for (int v = 0; v < kScanV; ++v) last[v] = t.lo == 0 ? start[v] : last[v];
@@ -400,18 +442,20 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
     }
 #pragma unroll
     for (int v = 0; v < kScanV; ++v) {
-      A[v] = scan_more<GATE>(1.f, a[0][v]);
+      ScanProduct<GATE> all;
+      all.more(a[0][v]);
       B[v] = a[0][v] * d[0][v];
 #pragma unroll
       for (int i = 1; i < L; ++i) {
-        A[v] = scan_more<GATE>(A[v], a[i][v]);
+        all.more(a[i][v]);
         B[v] = a[i][v] * (B[v] + d[i][v]);
       }
+      A[v] = all.factor();
     }
     const ScanTile now = t;
     const bool more = now.next > 0;
     t = tile(more ? now.next : now.next + 1, more);
-    scan_meet(lds[turn], A, B, state, back);
+    scan_meet<GATE>(lds[turn], A, B, state, back);
     const ScanWorker w = scan_worker(table, now.p);
     const auto o0 = scan_rows((E*)w.o0 + now.row), o1 = scan_rows((E*)w.o1 + now.row);
 #pragma unroll
@@ -459,36 +503,46 @@ __global__ __launch_bounds__(256) void scan_clear_kernel(uint64_t* words, size_t
   for (size_t i = blockIdx.x * (size_t)256 + threadIdx.x; i < n; i += gridDim.x * (size_t)256) words[i] = 0;
 }
 
-__device__ __forceinline__ void scan_publish(uint64_t* to, const float* v, uint32_t tag) {
+// A word: a number of 32 bits and the tag; or the upper 35 bits of one of 64, rounded (the range, and the 24 significant bits of the others), and 29 of the tag.
+constexpr uint64_t kScanTag29 = (uint64_t(1) << 29) - 1;
+__device__ __forceinline__ uint64_t scan_word(float v, uint32_t tag) { return (uint64_t)tag << 32 | __float_as_uint(v); }
+__device__ __forceinline__ uint64_t scan_word(double v, uint32_t tag) {
+  return (((uint64_t)__double_as_longlong(v) + (kScanTag29 + 1) / 2) & ~kScanTag29) | (tag & kScanTag29);
+}
+__device__ __forceinline__ bool scan_there(float, uint64_t word, uint32_t tag) { return (int32_t)((uint32_t)(word >> 32) - tag) >= 0; }
+__device__ __forceinline__ bool scan_there(double, uint64_t word, uint32_t tag) { return (int32_t)(((uint32_t)word - tag) << 3) >= 0; }
+__device__ __forceinline__ void scan_number(uint64_t word, float& v) { v = __uint_as_float((uint32_t)word); }
+__device__ __forceinline__ void scan_number(uint64_t word, double& v) { v = __longlong_as_double((long long)(word & ~kScanTag29)); }
+
+template <class F>
+__device__ __forceinline__ void scan_publish(uint64_t* to, const F* v, uint32_t tag) {
 #pragma unroll
   for (int i = 0; i < kScanV; ++i)
-    __hip_atomic_store(to + i * 64 + (threadIdx.x & 63), (uint64_t)tag << 32 | __float_as_uint(v[i]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(to + i * 64 + (threadIdx.x & 63), scan_word(v[i], tag), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// Waits for the words of N places (a place that is null is not waited for).  A later tag also ends the wait.
-template <int N>
-__device__ __forceinline__ void scan_await(const uint64_t* const (&from)[N], float (&v)[N][kScanV], uint32_t tag) {
+// Waits for the words of N places (a place that is null is not waited for): states, or factors (F) and sums of maps in turn.  A later tag also
+// ends the wait.
+template <class F, int N>
+__device__ __forceinline__ void scan_await(const uint64_t* const (&from)[N], uint64_t (&w)[N][kScanV], uint32_t tag) {
   const uint64_t* lead = nullptr;  // the last of them alone first: whoever waits should not fill the memory's queues
 #pragma unroll
   for (int k = 0; k < N; ++k) lead = from[k] ? from[k] : lead;
   if (lead)
-    while (!__all((int32_t)((uint32_t)(__hip_atomic_load(lead + 64 + (threadIdx.x & 63), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >> 32) - tag) >= 0))
+    while (!__all(scan_there(0.f, __hip_atomic_load(lead + 64 + (threadIdx.x & 63), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), tag)))
       __builtin_amdgcn_s_sleep(2);
   for (;;) {
-    uint64_t w[N][kScanV];
     bool there = true;
 #pragma unroll
     for (int k = 0; k < N; ++k)
 #pragma unroll
       for (int i = 0; i < kScanV; ++i)
-        w[k][i] = from[k] ? __hip_atomic_load(from[k] + i * 64 + (threadIdx.x & 63), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : (uint64_t)tag << 32;
+        w[k][i] = from[k] ? __hip_atomic_load(from[k] + i * 64 + (threadIdx.x & 63), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)
+                          : N > 1 && k % 2 == 0 ? scan_word(F(0), tag) : scan_word(0.f, tag);
 #pragma unroll
     for (int k = 0; k < N; ++k)
 #pragma unroll
-      for (int i = 0; i < kScanV; ++i) {
-        there &= (int32_t)((uint32_t)(w[k][i] >> 32) - tag) >= 0;
-        v[k][i] = __uint_as_float((uint32_t)w[k][i]);
-      }
+      for (int i = 0; i < kScanV; ++i) there &= N > 1 && k % 2 == 0 ? scan_there(F(0), w[k][i], tag) : scan_there(0.f, w[k][i], tag);
     if (__all(there)) return;
     __builtin_amdgcn_s_sleep(1);
   }
@@ -539,8 +593,9 @@ __device__ __forceinline__ ScanSlice scan_slice(const ScanArgs& s, uint32_t tile
 
 // From the map of each wave's steps: publishes the tile's, gives the state in front of this wave's steps and, in the last wave, that behind the tile.
 template <int GATE, bool PAIR>
-__device__ __forceinline__ void scan_join(const ScanArgs& s, const ScanPlace& at, const ScanTask& task, const float* from, float (*own)[2][kScanCols],
-                                          float (*run)[2][kScanCols], float* front, const float* A, const float* B, float* mine, float* end) {
+__device__ __forceinline__ void scan_join(const ScanArgs& s, const ScanPlace& at, const ScanTask& task, const float* from, ScanMaps<GATE>& own,
+                                          ScanMaps<GATE>& run, float* front, const ScanFactor<GATE>* A, const float* B, float* mine, float* end) {
+  typedef ScanFactor<GATE> F;
   const int lane = threadIdx.x & 63, wave = scan_wave();
   const uint32_t super = task.k / kScanSuper, j = task.k % kScanSuper;
   const bool closes = j == kScanSuper - 1, last = task.k == s.tiles - 1;
@@ -549,58 +604,78 @@ __device__ __forceinline__ void scan_join(const ScanArgs& s, const ScanPlace& at
                            ((size_t)task.chain * ((s.tiles + kScanSuper - 1) / kScanSuper) + super) * kScanCols;  // the one behind the run
 #pragma unroll
   for (int v = 0; v < kScanV; ++v) {
-    own[wave][0][v * 64 + lane] = A[v];
-    own[wave][1][v * 64 + lane] = B[v];
+    own.A[wave][v * 64 + lane] = A[v];
+    own.B[wave][v * 64 + lane] = B[v];
   }
   __syncthreads();
   if (wave == kScanWaves - 1 && !closes && !last) {
-    float all[kScanV], sum[kScanV];
+    F all[kScanV], sum[kScanV];
 #pragma unroll
     for (int v = 0; v < kScanV; ++v) {
-      all[v] = 1.f;
-      sum[v] = 0.f;
+      all[v] = 1;
+      sum[v] = 0;
 #pragma unroll
       for (int w = 0; w < kScanWaves; ++w) {
-        all[v] = scan_more<GATE>(all[v], own[w][0][v * 64 + lane]);
-        sum[v] = fmaf(own[w][0][v * 64 + lane], sum[v], own[w][1][v * 64 + lane]);
+        all[v] = scan_then(all[v], own.A[w][v * 64 + lane]);
+        sum[v] = scan_apply(own.A[w][v * 64 + lane], sum[v], own.B[w][v * 64 + lane]);
       }
     }
+    float last_sum[kScanV];
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) last_sum[v] = sum[v];
     scan_publish(maps + j * 2 * kScanCols, all, task.tag);
-    scan_publish(maps + (j * 2 + 1) * kScanCols, sum, task.tag);
+    scan_publish(maps + (j * 2 + 1) * kScanCols, last_sum, task.tag);
   }
   const uint32_t i = 2 * wave;  // the maps of two tiles of the run
   const uint64_t* const m = maps + i * 2 * kScanCols;
   const uint64_t* const words[4] = {i < j ? m : nullptr, i < j ? m + kScanCols : nullptr, i + 1 < j ? m + 2 * kScanCols : nullptr,
                                     i + 1 < j ? m + 3 * kScanCols : nullptr};
-  float got[4][kScanV];
-  scan_await(words, got, task.tag);
+  uint64_t got[4][kScanV];
+  scan_await<F>(words, got, task.tag);
   if (wave == 0) {
-    float start[1][kScanV];
+    float start[kScanV];
     const uint64_t* const before[1] = {states - kScanCols};
-    if (super > 0) scan_await(before, start, task.tag);
-    else scan_start<PAIR>(s, at, from, start[0]);
+    uint64_t word[1][kScanV];
+    if (super > 0) {
+      scan_await<float>(before, word, task.tag);
 #pragma unroll
-    for (int v = 0; v < kScanV; ++v) front[v * 64 + lane] = start[0][v];
+      for (int v = 0; v < kScanV; ++v) scan_number(word[0][v], start[v]);
+    } else {
+      scan_start<PAIR>(s, at, from, start);
+    }
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) front[v * 64 + lane] = start[v];
   }
 #pragma unroll
   for (int v = 0; v < kScanV; ++v) {
-    const float a0 = i < j ? got[0][v] : 1.f, a1 = i + 1 < j ? got[2][v] : 1.f;  // (the others are zeros)
-    run[wave][0][v * 64 + lane] = scan_more<GATE>(a0, a1);
-    run[wave][1][v * 64 + lane] = fmaf(a1, got[1][v], got[3][v]);
+    F a0, a1;
+    float b0, b1;
+    scan_number(got[0][v], a0);
+    scan_number(got[1][v], b0);
+    scan_number(got[2][v], a1);
+    scan_number(got[3][v], b1);
+    a0 = i < j ? a0 : F(1);  // (the others are zeros)
+    a1 = i + 1 < j ? a1 : F(1);
+    run.A[wave][v * 64 + lane] = scan_then(a0, a1);
+    run.B[wave][v * 64 + lane] = (float)scan_apply(a1, F(b0), b1);
   }
   __syncthreads();
+  F state[kScanV];
 #pragma unroll
-  for (int v = 0; v < kScanV; ++v) {
-    float state = front[v * 64 + lane];
+  for (int v = 0; v < kScanV; ++v) state[v] = front[v * 64 + lane];
 #pragma unroll
-    for (int w = 0; w < kScanWaves; ++w) state = fmaf(run[w][0][v * 64 + lane], state, run[w][1][v * 64 + lane]);
+  for (int w = 0; w < kScanWaves; ++w)
 #pragma unroll
-    for (int w = 0; w < kScanWaves; ++w) {
-      if (w == wave) mine[v] = state;
-      state = fmaf(own[w][0][v * 64 + lane], state, own[w][1][v * 64 + lane]);
+    for (int v = 0; v < kScanV; ++v) state[v] = scan_apply(run.A[w][v * 64 + lane], state[v], run.B[w][v * 64 + lane]);
+#pragma unroll
+  for (int w = 0; w < kScanWaves; ++w)
+#pragma unroll
+    for (int v = 0; v < kScanV; ++v) {
+      if (w == wave) mine[v] = state[v];
+      state[v] = scan_apply(own.A[w][v * 64 + lane], state[v], own.B[w][v * 64 + lane]);
     }
-    end[v] = state;
-  }
+#pragma unroll
+  for (int v = 0; v < kScanV; ++v) end[v] = state[v];
   if (wave == kScanWaves - 1) {
     if (last) scan_finish<PAIR>(s, at, end);
     else if (closes) scan_publish(states, end, task.tag);
@@ -610,7 +685,8 @@ __device__ __forceinline__ void scan_join(const ScanArgs& s, const ScanPlace& at
 template <class E, int GATE, bool PAIR>
 __global__ __launch_bounds__(64 * kScanWaves, 4) void scan_few_fwd_kernel(ScanArgs s) {
   constexpr int L = kFewSteps;
-  __shared__ float own[kScanWaves][2][kScanCols], run[kScanWaves][2][kScanCols], front[kScanCols];
+  __shared__ ScanMaps<GATE> own, run;
+  __shared__ float front[kScanCols];
   __shared__ uint32_t drawn[2];
   const ScanTable table = SCAN_TABLE(s);
   const ScanTask task = scan_task(s, drawn);
@@ -630,7 +706,8 @@ __global__ __launch_bounds__(64 * kScanWaves, 4) void scan_few_fwd_kernel(ScanAr
     ra[i].load(pa, o, i * hop);
     rx[i].load(px, o, i * hop);
   }
-  float a[L][kScanV], u[L][kScanV], A[kScanV], B[kScanV], h[kScanV], end[kScanV];
+  float a[L][kScanV], u[L][kScanV], B[kScanV], h[kScanV], end[kScanV];
+  ScanFactor<GATE> A[kScanV];
 #pragma unroll
   for (int i = 0; i < L; ++i) {
     float g[kScanV], x[kScanV];
@@ -651,13 +728,14 @@ __global__ __launch_bounds__(64 * kScanWaves, 4) void scan_few_fwd_kernel(ScanAr
   }
 #pragma unroll
   for (int v = 0; v < kScanV; ++v) {
-    A[v] = 1.f;
+    ScanProduct<GATE> all;
     B[v] = 0.f;
 #pragma unroll
     for (int i = 0; i < L; ++i) {
-      A[v] = scan_more<GATE>(A[v], a[i][v]);
+      all.more(a[i][v]);
       B[v] = fmaf(a[i][v], B[v], u[i][v]);
     }
+    A[v] = all.factor();
   }
   scan_join<GATE, PAIR>(s, at, task, s.h0, own, run, front, A, B, h, end);
 #pragma unroll
@@ -679,7 +757,8 @@ template <class E, int GATE, bool PAIR>
 __global__ __launch_bounds__(64 * kScanWaves, 4) void scan_few_bwd_kernel(ScanArgs s) {
   constexpr int L = kFewBack;
   constexpr bool X = GATE != DISTDL_GATE_GIVEN;
-  __shared__ float own[kScanWaves][2][kScanCols], run[kScanWaves][2][kScanCols], front[kScanCols];
+  __shared__ ScanMaps<GATE> own, run;
+  __shared__ float front[kScanCols];
   __shared__ uint32_t drawn[2];
   const ScanTable table = SCAN_TABLE(s);
   const ScanTask task = scan_task(s, drawn);
@@ -711,7 +790,8 @@ __global__ __launch_bounds__(64 * kScanWaves, 4) void scan_few_bwd_kernel(ScanAr
   float last[kScanV];  // the state in front of a worker's first step, of the first worker in 32 bits
   if (t.lo == 0) scan_start<PAIR>(s, at, s.h0, last);
   // dx = d rest, da = d slope
-  float a[L][kScanV], d[L][kScanV], rest[L][kScanV], slope[L][kScanV], A[kScanV], B[kScanV], back[kScanV], end[kScanV];
+  float a[L][kScanV], d[L][kScanV], rest[L][kScanV], slope[L][kScanV], B[kScanV], back[kScanV], end[kScanV];
+  ScanFactor<GATE> A[kScanV];
   if (t.lo > 0) edge.values(last);
 #pragma unroll
   for (int i = 0; i < L; ++i) {
@@ -741,13 +821,14 @@ __global__ __launch_bounds__(64 * kScanWaves, 4) void scan_few_bwd_kernel(ScanAr
   }
 #pragma unroll
   for (int v = 0; v < kScanV; ++v) {
-    A[v] = 1.f;
+    ScanProduct<GATE> all;
     B[v] = 0.f;
 #pragma unroll
     for (int i = 0; i < L; ++i) {
-      A[v] = scan_more<GATE>(A[v], a[i][v]);
+      all.more(a[i][v]);
       B[v] = a[i][v] * (B[v] + d[i][v]);
     }
+    A[v] = all.factor();
   }
   scan_join<GATE, PAIR>(s, at, task, s.end, own, run, front, A, B, back, end);
 #pragma unroll

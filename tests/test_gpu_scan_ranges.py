@@ -90,3 +90,70 @@ def test_steps_behind_the_end_get_zeros(n, T, C, P, gate, kind):
             assert not torch.isfinite(got[:, end - 1:end, 0]).any(), end
         if end == 0:
             assert torch.equal(dh0[0], dhT) and torch.equal(dh0[1][:, 0], bad[:, 0]) and torch.isnan(dh0[1][:, 1]).all()
+
+
+def sequential(a, x, state, back=False):
+    """Single steps, rounded to 32 bits each; numpy's products of powers of two are exact within the type's range."""
+    out = np.empty_like(x)
+    with np.errstate(over="ignore", under="ignore"):
+        for t in range(a.shape[1])[::-1 if back else 1]:
+            if back:
+                state = np.float32(x[:, t] + state)
+                out[:, t] = state
+                state = a[:, t] * state
+            else:
+                state = out[:, t] = a[:, t] * state + x[:, t]
+    return out, state
+
+
+@pytest.mark.parametrize("order", ["up first", "down first"])
+@pytest.mark.parametrize("steps", [1, 5, 40, 70, 260])
+@pytest.mark.parametrize("n,T,C,P", [(2, 128, 9, 1), (140, 1100, 2, 2), (2, 1100, 9, 1), (1, 2600, 130, 3)])
+def test_products_of_gates_beyond_the_range_of_states(n, T, C, P, steps, order):
+    """Given gates that multiply up to 2^220 and down again, in so many steps each, carry a small state (down first: a large one) as single steps do,
+    to the bit: everything is a power of two.  The same for the adjoint's chain."""
+    require_gpu()
+    if 2 * steps > T:
+        pytest.skip("more steps than there are")
+    rise = 220 // steps if steps <= 5 else -(-220 // steps)
+    rise = min(rise, 120)
+    total, sign = min(220, rise * steps), 1 if order == "up first" else -1
+    period = np.zeros(2 * steps + 7)
+    period[:steps] = [min(rise, max(0, total - rise * i)) for i in range(steps)]
+    period[steps + 3:2 * steps + 3] = -period[:steps]
+    power = sign * np.tile(period, T // len(period) + 1)[:T]
+    gates = np.broadcast_to(2.0 ** power[None, :, None], (n, T, C)).astype(np.float32).copy()
+    gates[:, :, 1] *= -1
+    start = np.float32(2.0 ** (-sign * 110))
+    h0 = np.full((n, C), start, np.float32)
+    h0[:, 1] = 0
+    zero = np.zeros((n, T, C), np.float32)
+    on = lambda v: torch.tensor(v, device="cuda")  # noqa: E731
+    plan = dd.distdl_scan_plan_create(n, T, C, P, "given", torch.float32)
+    h, hT = [torch.empty_like(t) for t in cut(on(zero), P)], torch.empty(n, C, device="cuda")
+    dd.distdl_scan_fwd(plan, cut(on(gates), P), cut(on(zero), P), on(h0), None, h, hT)
+    want, last = sequential(gates, zero, h0)
+    assert np.isfinite(want).all() and want[:, :, 0].all()
+    assert np.array_equal(torch.cat(h, 1).cpu().numpy(), want) and np.array_equal(hT.cpu().numpy(), last)
+    backwards = gates[:, ::-1].copy()
+    da, dx, dh0 = [torch.empty_like(t) for t in h], [torch.empty_like(t) for t in h], torch.empty(n, C, device="cuda")
+    dd.distdl_scan_bwd(plan, cut(on(backwards), P), None, cut(on(zero), P), None, None, cut(on(zero), P), on(h0), da, dx, dh0)
+    want, last = sequential(backwards, zero, h0, back=True)
+    assert np.isfinite(want).all() and want[:, :, 0].all()
+    assert np.array_equal(torch.cat(dx, 1).cpu().numpy(), want) and np.array_equal(dh0.cpu().numpy(), last)
+
+
+@pytest.mark.parametrize("n,T,C,P", SIZES)
+def test_states_that_leave_the_range_are_infinite(n, T, C, P):
+    """A state that single steps take out of range is infinite from there on, and not a number that a bound has cut."""
+    require_gpu()
+    at = 70 if T > 100 else 20
+    gates, x = torch.ones(n, T, C, device="cuda"), torch.zeros(n, T, C, device="cuda")
+    gates[:, at:at + 3] = 2.0 ** 60
+    gates[:, at + 5:at + 7] = 2.0 ** -100
+    h0 = torch.full((n, C), 2.0 ** -20, device="cuda")
+    plan = dd.distdl_scan_plan_create(n, T, C, P, "given", torch.float32)
+    h, hT = [torch.empty_like(t) for t in cut(x, P)], torch.empty(n, C, device="cuda")
+    dd.distdl_scan_fwd(plan, cut(gates, P), cut(x, P), h0, None, h, hT)
+    h = torch.cat(h, 1)
+    assert torch.isfinite(h[:, :at + 2]).all() and torch.isinf(h[:, at + 2:at + 5]).all()
