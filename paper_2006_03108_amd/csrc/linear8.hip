@@ -21,7 +21,8 @@
 // which a wave makes one for 2.7 products).
 #include <algorithm>
 #include <cstddef>
-#include <unordered_map>
+#include <map>
+#include <tuple>
 
 #include "block8.h"
 #include "buffer.h"
@@ -489,7 +490,9 @@ static int64_t prod_tiles(std::vector<ProdOut>& outs, int TM, int TN) {
 
 // Makes the rows of all operands whole 16-byte pieces: those that are not are copied to the plan's scratch.
 static int prod_pieces(distdl_linear8_plan* p, const std::vector<ProdOut>& outs, std::vector<ProdSeg>& segs, hipStream_t st) {
-  std::unordered_map<const void*, size_t> seen;  // an operand of several results is copied once: its place in `copies`
+  // An operand of several results is copied once: its place in `copies`.  Operands may start at one address and differ in rows or their length
+  // (a matrix and its first rows), so these belong to what is remembered.
+  std::map<std::tuple<const void*, int64_t, int64_t>, size_t> seen;
   std::vector<ProdCopy> copies;
   std::vector<std::pair<const uint8_t**, size_t>> users;
   int64_t pieces = 0, blocks = 0;
@@ -503,7 +506,7 @@ static int prod_pieces(distdl_linear8_plan* p, const std::vector<ProdOut>& outs,
       } sides[2] = {{&g.a, o.m}, {&g.b, o.n}};
       for (const auto& side : sides) {
         if (g.k % 16 == 0 && (uintptr_t)*side.p % 16 == 0) continue;
-        const auto it = seen.emplace(*side.p, copies.size());
+        const auto it = seen.emplace(std::make_tuple((const void*)*side.p, side.rows, g.k), copies.size());
         if (it.second) {
           const int64_t total = side.rows * wide;
           if (total >= int64_t(1) << 31 || (blocks += (total + 1023) / 1024) >= kMaxBlocks256) return set_error(DISTDL_ERR_UNSUPPORTED, "linear8: problem too large");
