@@ -425,6 +425,8 @@ int distdl_dot_static(const void* const a_dev[], const void* const b_dev[], cons
  *   s of its rows, and codes qt [cols][rows] and scales st of the rows of its
  *   transpose; either pair may be NULL.  tiles != 0: one scale for each tile
  *   of 128 x 128, the same in both orders.  Outputs must not overlap inputs.
+ *   It keeps nothing: threads may call it at once, and its first call can be
+ *   recorded.  More than 48 arrays take a launch for each 48.
  * ---------------------------------------------------------------------- */
 int distdl_quant8(const void* const x_dev[], const int64_t rows[], const int64_t cols[], int n_arrays, int tiles,
                   void* const q_dev[], void* const s_dev[], void* const qt_dev[], void* const st_dev[],

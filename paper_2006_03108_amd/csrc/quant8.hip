@@ -23,24 +23,25 @@ struct QuantArray {
   uint32_t tile0, tiles_c;   // first workgroup; tiles side by side
 };
 
-constexpr int kQuantInline = 16;
+// The arrays travel with the launch; more of them take several launches.  A table on the device would have to belong to someone: this call has
+// no plan, and may be made by several threads, recorded, and made again with other arrays, without end.  Up to 16 arrays take 1 KiB of arguments,
+// more of them launches with 3 KiB (us, 1 array 8.5 and 8.7; 40 arrays 57 and 52.5, as with a table).
+template <int N>
 struct QuantArgs {
-  QuantArray a[kQuantInline];
-  const QuantArray* more;
+  QuantArray a[N];
   int32_t n;
 };
-// The table's address is taken in the kernel itself, and its records are read as constants, into scalar registers.
-static_assert(offsetof(QuantArgs, a) == 0, "the kernel's first argument starts with the arrays");
+// The arguments' address is taken in the kernel itself, and the records are read as constants, into scalar registers.
+static_assert(offsetof(QuantArgs<16>, a) == 0, "the kernel's first argument starts with the arrays");
 typedef const __attribute__((address_space(4))) QuantArray* QuantTable;
-#define QUANT_TABLE(s) ((s).more ? (QuantTable)(uint64_t)(s).more : (QuantTable)__builtin_amdgcn_kernarg_segment_ptr())
 
 // TILES: one scale for the tile.  Otherwise each order has blocks of its own.
-template <class E, bool TILES>
-__global__ __launch_bounds__(256) void quant8_kernel(QuantArgs args) {
+template <class E, bool TILES, int N>
+__global__ __launch_bounds__(256) void quant8_kernel(QuantArgs<N> args) {
   __shared__ float meet[4][kBlock8];
   // column c's 16-byte piece p lies at p ^ ((c >> 3) & 7): the lanes of a wave write eight columns apart
   __shared__ alignas(16) uint8_t turned[kBlock8][kBlock8];
-  const QuantTable table = QUANT_TABLE(args);
+  const QuantTable table = (QuantTable)__builtin_amdgcn_kernarg_segment_ptr();
   int i = 0;
   while (i + 1 < args.n && blockIdx.x >= table[i + 1].tile0) ++i;
   const QuantTable t = table + i;
@@ -130,11 +131,28 @@ __global__ __launch_bounds__(256) void quant8_kernel(QuantArgs args) {
   }
 }
 
-static SlotCache* quant_tables() {  // of calls with many arrays, one cache a device
-  static SlotCache tables[64];
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess) return nullptr;
-  return &tables[dev & 63];
+template <int N>
+static int launch_quant(const std::vector<QuantArray>& a, int64_t all_tiles, bool tiles, distdl_dtype dtype, hipStream_t st) {
+  for (size_t first = 0; first < a.size(); first += N) {
+    QuantArgs<N> args;
+    args.n = (int32_t)std::min(a.size() - first, (size_t)N);
+    const uint32_t tile0 = a[first].tile0;
+    const int64_t end = first + args.n < a.size() ? a[first + args.n].tile0 : all_tiles;
+    for (int i = 0; i < args.n; ++i) {
+      args.a[i] = a[first + i];
+      args.a[i].tile0 -= tile0;
+    }
+    const dim3 grid((unsigned)(end - tile0)), block(256);
+    if (dtype == DISTDL_F32) {
+      if (tiles) hipLaunchKernelGGL((quant8_kernel<float, true, N>), grid, block, 0, st, args);
+      else hipLaunchKernelGGL((quant8_kernel<float, false, N>), grid, block, 0, st, args);
+    } else {
+      if (tiles) hipLaunchKernelGGL((quant8_kernel<uint16_t, true, N>), grid, block, 0, st, args);
+      else hipLaunchKernelGGL((quant8_kernel<uint16_t, false, N>), grid, block, 0, st, args);
+    }
+    DISTDL_HIP_TRY(hipGetLastError());
+  }
+  return DISTDL_OK;
 }
 
 }  // namespace distdl
@@ -168,30 +186,7 @@ extern "C" int distdl_quant8(const void* const x_dev[], const int64_t rows[], co
     }
     if (a.empty()) return DISTDL_OK;
     hipStream_t st_ = (hipStream_t)stream;
-    QuantArgs args;
-    args.more = nullptr;
-    args.n = (int32_t)a.size();
-    if (a.size() <= (size_t)kQuantInline) {
-      std::copy(a.begin(), a.end(), args.a);
-    } else {
-      SlotCache* const tables = quant_tables();
-      if (!tables) return set_error(DISTDL_ERR_HIP, "quant8: no device");
-      const int rc = tables->upload(a.data(), a.size() * sizeof(QuantArray), st_);
-      if (rc) return rc;
-      args.more = (const QuantArray*)tables->dev();
-    }
-    {
-      ProfScope prof("quant8", st_);
-      const dim3 grid((unsigned)at), block(256);
-      if (dtype == DISTDL_F32) {
-        if (tiles) hipLaunchKernelGGL((quant8_kernel<float, true>), grid, block, 0, st_, args);
-        else hipLaunchKernelGGL((quant8_kernel<float, false>), grid, block, 0, st_, args);
-      } else {
-        if (tiles) hipLaunchKernelGGL((quant8_kernel<uint16_t, true>), grid, block, 0, st_, args);
-        else hipLaunchKernelGGL((quant8_kernel<uint16_t, false>), grid, block, 0, st_, args);
-      }
-    }
-    DISTDL_HIP_TRY(hipGetLastError());
-    return DISTDL_OK;
+    ProfScope prof("quant8", st_);
+    return a.size() <= 16 ? launch_quant<16>(a, at, tiles != 0, dtype, st_) : launch_quant<48>(a, at, tiles != 0, dtype, st_);
   });
 }
