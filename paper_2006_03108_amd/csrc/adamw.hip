@@ -4,7 +4,7 @@
 //   p  = p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
 // One pass: every number is read and written once, 16 bytes an element with 8-bit moments and a 32-bit gradient, 28 with 32-bit ones, so
-// memory bounds it.  A workgroup takes consecutive elements of one array, from a table made with the plan; a thread takes
+// memory bounds it.  A workgroup takes consecutive elements of one array, from a table that a stream's first call makes; a thread takes
 // eight at a time, so that 16 lanes (one DPP row) hold a block of 128 and its scales need no LDS.  Measured: 168 million weights, bf16
 // gradients, 8-bit moments and bf16 copies 509 to 565 us (4.8 to 5.3 TB/s); 67 million with fp32 moments and copies 348 us (5.4 TB/s).  A thread
 // has eight elements of fp32 moments (twice as many: 361 us) and sixteen of 8-bit ones (half as many: 550 us, twice: 603).
@@ -39,7 +39,7 @@ struct AdamArray {  // what a launch needs of one array
   uint16_t* copy;
   int64_t count;
   uint32_t place;  // of its first element in the hash: the arrays lie one behind the other, each at a multiple of 128
-  uint32_t pad_;
+  uint32_t chunk0;  // its first workgroup
 };
 
 struct AdamArgs {
@@ -51,6 +51,20 @@ struct AdamArgs {
   const int64_t* step;
   const float* gscale;
 };
+
+// What each workgroup takes: the last array whose first workgroup is not behind it (those of no elements come before the array that is at their place).
+__global__ __launch_bounds__(256) void adamw_chunks_kernel(AdamChunk* __restrict__ chunks, uint32_t n_chunks, const AdamArray* __restrict__ arrays,
+                                                           uint32_t n_arrays) {
+  const uint32_t c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= n_chunks) return;
+  uint32_t lo = 0, hi = n_arrays;  // arrays[lo].chunk0 <= c < arrays[hi].chunk0
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) / 2;
+    if (arrays[mid].chunk0 <= c) lo = mid;
+    else hi = mid;
+  }
+  chunks[c] = AdamChunk{lo, c - arrays[lo].chunk0};
+}
 
 // (the multipliers are 2^32 over the golden ratio and the fractions of sqrt(2) and sqrt(3))
 __device__ __forceinline__ uint32_t adam_noise(uint32_t place, uint32_t key) {
@@ -186,11 +200,10 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamChunk* __restrict_
 
 struct distdl_adamw_plan {
   std::vector<int64_t> count;
-  std::vector<uint32_t> place;
+  std::vector<uint32_t> place, chunk0;
   bool g16 = false, s8 = false;
   int64_t n_chunks = 0;
-  distdl::AdamChunk* d_chunks = nullptr;
-  std::vector<distdl::AdamChunk> chunks;
+  distdl::StreamScratch chunks;
   distdl::DevArray<distdl::AdamArray> arrays;
 };
 
@@ -217,13 +230,13 @@ int distdl_adamw_plan_create(distdl_adamw_plan** out, const int64_t count[], int
     p->g16 = g_dtype == DISTDL_BF16;
     p->s8 = states8 != 0;
     p->n_chunks = chunks;
-    p->chunks.reserve((size_t)chunks);
-    int64_t place = 0;
+    int64_t place = 0, at = 0;
     for (int i = 0; i < n_arrays; ++i) {
       p->count.push_back(count[i]);
       p->place.push_back((uint32_t)place);
       place += (count[i] + kBlock8 - 1) / kBlock8 * kBlock8;
-      for (int64_t c = 0; c * size < count[i]; ++c) p->chunks.push_back(AdamChunk{(uint32_t)i, (uint32_t)c});
+      p->chunk0.push_back((uint32_t)at);
+      at += (count[i] + size - 1) / size;
     }
     *out = p.release();
     return DISTDL_OK;
@@ -232,7 +245,7 @@ int distdl_adamw_plan_create(distdl_adamw_plan** out, const int64_t count[], int
 
 int distdl_adamw_plan_destroy(distdl_adamw_plan* p) {
   if (!p) return DISTDL_OK;
-  if (p->d_chunks) (void)hipFree(p->d_chunks);
+  p->chunks.release();
   p->arrays.release();
   delete p;
   return DISTDL_OK;
@@ -256,7 +269,7 @@ int distdl_adamw_step(distdl_adamw_plan* p, void* const p_dev[], const void* con
     for (size_t i = 0; i < n; ++i) {
       AdamArray& a = arrays[i];
       a = AdamArray{(float*)p_dev[i], g_dev[i], m_dev[i], v_dev[i], p->s8 ? (uint8_t*)ms_dev[i] : nullptr,
-                    p->s8 ? (uint8_t*)vs_dev[i] : nullptr, copy_dev ? (uint16_t*)copy_dev[i] : nullptr, p->count[i], p->place[i], 0};
+                    p->s8 ? (uint8_t*)vs_dev[i] : nullptr, copy_dev ? (uint16_t*)copy_dev[i] : nullptr, p->count[i], p->place[i], p->chunk0[i]};
       if (p->count[i] == 0) continue;
       if (!a.p || !a.g || !a.m || !a.v || (p->s8 && (!a.ms || !a.vs)))
         return set_error(DISTDL_ERR_NULL, "adamw_step: array %zu is null", i);
@@ -266,23 +279,24 @@ int distdl_adamw_step(distdl_adamw_plan* p, void* const p_dev[], const void* con
     }
     if (p->n_chunks == 0) return DISTDL_OK;
     hipStream_t st_ = (hipStream_t)stream;
-    if (!p->d_chunks) {  // with the plan's first call, on its stream's device; not while a capture would record the copy
+    bool is_new = true;  // to this stream, whose first call makes the table of workgroups
+    for (const StreamScratch::Block& b : p->chunks.blocks) is_new = is_new && b.stream != st_;
+    if (is_new) {
       hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
       DISTDL_HIP_TRY(hipStreamIsCapturing(st_, &cap));
       if (cap != hipStreamCaptureStatusNone)
-        return set_error(DISTDL_ERR_INVALID_ARG, "adamw_step: a plan's first call cannot be captured");
-      AdamChunk* dev = nullptr;
-      DISTDL_HIP_TRY(hipMalloc((void**)&dev, p->chunks.size() * sizeof(AdamChunk)));
-      hipError_t e = hipMemcpy(dev, p->chunks.data(), p->chunks.size() * sizeof(AdamChunk), hipMemcpyHostToDevice);
-      if (e != hipSuccess) {
-        (void)hipFree(dev);
-        return set_error(DISTDL_ERR_HIP, "hipMemcpy failed: %s", hipGetErrorString(e));
-      }
-      p->d_chunks = dev;
-      std::vector<AdamChunk>().swap(p->chunks);
+        return set_error(DISTDL_ERR_INVALID_ARG, "adamw_step: the plan's first call on this stream, which is being captured");
     }
     int rc = p->arrays.upload(arrays, st_);
     if (rc) return rc;
+    float* table = nullptr;
+    static_assert(sizeof(AdamChunk) == 2 * sizeof(float), "two words a workgroup");
+    if ((rc = p->chunks.get(2 * (size_t)p->n_chunks, st_, &table))) return rc;
+    AdamChunk* const chunks = (AdamChunk*)table;
+    if (is_new) {
+      hipLaunchKernelGGL(adamw_chunks_kernel, dim3((unsigned)((p->n_chunks + 255) / 256)), dim3(256), 0, st_, chunks, (uint32_t)p->n_chunks, p->arrays.dev, (uint32_t)n);
+      DISTDL_HIP_TRY(hipGetLastError());
+    }
     const double t = h->step_dev ? 1.0 : (double)h->step;
     AdamArgs s;
     s.beta1 = (float)h->beta1;
@@ -304,11 +318,11 @@ int distdl_adamw_step(distdl_adamw_plan* p, void* const p_dev[], const void* con
       ProfScope prof("adamw", st_);
       const dim3 grid((unsigned)p->n_chunks);
       if (p->s8) {
-        if (p->g16) hipLaunchKernelGGL((adamw_kernel<true, true>), grid, dim3(256), 0, st_, p->d_chunks, p->arrays.dev, s);
-        else hipLaunchKernelGGL((adamw_kernel<false, true>), grid, dim3(256), 0, st_, p->d_chunks, p->arrays.dev, s);
+        if (p->g16) hipLaunchKernelGGL((adamw_kernel<true, true>), grid, dim3(256), 0, st_, chunks, p->arrays.dev, s);
+        else hipLaunchKernelGGL((adamw_kernel<false, true>), grid, dim3(256), 0, st_, chunks, p->arrays.dev, s);
       } else {
-        if (p->g16) hipLaunchKernelGGL((adamw_kernel<true, false>), grid, dim3(256), 0, st_, p->d_chunks, p->arrays.dev, s);
-        else hipLaunchKernelGGL((adamw_kernel<false, false>), grid, dim3(256), 0, st_, p->d_chunks, p->arrays.dev, s);
+        if (p->g16) hipLaunchKernelGGL((adamw_kernel<true, false>), grid, dim3(256), 0, st_, chunks, p->arrays.dev, s);
+        else hipLaunchKernelGGL((adamw_kernel<false, false>), grid, dim3(256), 0, st_, chunks, p->arrays.dev, s);
       }
     }
     DISTDL_HIP_TRY(hipGetLastError());
