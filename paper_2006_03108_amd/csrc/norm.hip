@@ -265,7 +265,7 @@ __global__ __launch_bounds__(norm_threads(W)) void norm_fwd_kernel(NormArgs a) {
         const NormWorker& p = at[k].w;
         if (p.s) norm_put<E, ROWS16>(norm_row<E>(p.s, row, p.n), at[k].col, lane, v[k]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[k][i] *= rstd * g[k][i];
+        for (int i = 0; i < 8; ++i) v[k][i] = v[k][i] * rstd * g[k][i];  // (n = s rstd first, as the adjoint has it)
         if (p.y) norm_put<E, ROWS16>(norm_row<E>(p.y, row, p.n), at[k].col, lane, v[k]);
         if (p.q) norm_put_codes<ROWS16>(at[k], row, a.rows, lane, v[k]);
       }
