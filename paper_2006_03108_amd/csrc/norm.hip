@@ -15,6 +15,7 @@
 // Measured: forward 8192 x 4096 bf16 on two workers, residual in, sum and 8-bit codes out, 50 us (4.8 TB/s); adjoint 5003 x 2000 fp32 on three workers
 // 34 us (4.7 TB/s) and 5 for the sum of dg's parts; forward 4 x 4096 3.7 us, a launch and a trip to memory.
 #include <algorithm>
+#include <cfloat>
 #include <cstddef>
 
 #include "block8.h"
@@ -481,7 +482,7 @@ static int norm_args(distdl_rmsnorm_plan* p, const std::vector<NormWorker>& w, h
   a->pieces = p->pieces;
   a->rows = p->rows;
   a->inv_n = (float)(1.0 / (double)p->n_f);
-  a->eps = (float)p->eps;
+  a->eps = p->eps > 0 ? std::max((float)p->eps, FLT_MIN) : 0.f;  // (rows of zeros stay zeros under any eps that is not zero)
   a->partial = nullptr;
   if (p->P <= kNormInline) {
     std::copy(w.begin(), w.end(), a->w);

@@ -27,3 +27,25 @@ def test_answers_from_the_row_factors(rows, n_f, P, dtype):
         assert torch.equal(y[j], want.to(KINDS[dtype]))
         codes, scales = blocks.quantise(want.double().cpu().numpy(), 1, 128)
         assert np.array_equal(qs[j].cpu().numpy().T, scales) and np.array_equal(q[j].cpu().numpy(), codes)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("eps", [1e-30, 1e-42, 1e-60])
+def test_rows_of_zeros_under_a_tiny_eps(eps, dtype):
+    """Rows of zeros (masked ones) answer zeros, and their gradients are finite, for an eps that 32 bits do not hold either."""
+    require_gpu()
+    rows, n_f, P = 6, 700, 2
+    (x, dy, _, _), g = make(rows, n_f, P, dtype, seed=7)
+    for t in x:
+        t[::2] = 0
+    for t in dy:
+        t[::2] = 0
+    plan = dd.distdl_rmsnorm_plan_create(rows, n_f, P, eps, KINDS[dtype])
+    y, rstd = [torch.empty_like(t) for t in x], torch.empty(rows, device="cuda")
+    dd.distdl_rmsnorm_fwd(plan, x, None, g, None, y, None, None, rstd)
+    assert torch.isfinite(rstd).all()
+    dx, dg = [torch.empty_like(t) for t in x], [torch.empty_like(t) for t in g]
+    dd.distdl_rmsnorm_bwd(plan, x, g, rstd, dy, None, dx, dg)
+    for t in y + dx:
+        assert not t[::2].any() and torch.isfinite(t).all() and t[1::2].any()
+    assert all(torch.isfinite(t).all() for t in dg)
