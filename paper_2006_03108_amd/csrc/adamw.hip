@@ -15,6 +15,8 @@
 // random bits are a hash of the seed, the step and the element's place, so a call repeats to the bit.
 //
 // Products and sums are not contracted into fused ones: the update is the same, to the bit, as that of the formula's operations one by one.
+#include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "block8.h"
@@ -306,7 +308,7 @@ int distdl_adamw_step(distdl_adamw_plan* p, void* const p_dev[], const void* con
     s.decay = (float)(1 - h->lr * h->weight_decay);
     s.rate = (float)(h->lr / (1 - std::pow(h->beta1, t)));
     s.grow = (float)(1 / std::sqrt(1 - std::pow(h->beta2, t)));
-    s.eps = (float)h->eps;
+    s.eps = std::max((float)h->eps, FLT_MIN);  // (never the zero that a smaller one would be in 32 bits: weights without gradients would divide by it)
     s.key = h->seed * 0x6A09E667u + (uint32_t)h->step * 0xBB67AE85u;
     s.lr = h->lr;
     s.b1 = h->beta1;

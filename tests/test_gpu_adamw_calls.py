@@ -70,3 +70,18 @@ def test_first_call_cannot_be_recorded():
             dd.distdl_adamw_step(plan, d["p"], d["g"], d["m"], d["v"], step=1, **HYPER)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(before, d["p"]))
+
+
+@pytest.mark.parametrize("states8", [False, True])
+@pytest.mark.parametrize("eps", [1e-30, 1e-42, 1e-60])
+def test_weights_without_gradients_under_a_tiny_eps(eps, states8):
+    """They only decay, for an eps that 32 bits do not hold either."""
+    require_gpu()
+    n = 1000
+    d = make([n], False)
+    d["g"][0][:500], p = 0, d["p"][0].clone()
+    moments = start8([n]) if states8 else dict(m=[torch.zeros(n, device="cuda")], v=[torch.zeros(n, device="cuda")])
+    plan = dd.distdl_adamw_plan_create([n], torch.float32, states8=states8)
+    dd.distdl_adamw_step(plan, d["p"], d["g"], **moments, step=1, **dict(HYPER, eps=eps))
+    decay = torch.tensor(1 - HYPER["lr"] * HYPER["weight_decay"], dtype=torch.float64).float().cuda()
+    assert torch.equal(d["p"][0][:500], p[:500] * decay) and torch.isfinite(d["p"][0]).all()
