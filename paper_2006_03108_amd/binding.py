@@ -485,7 +485,9 @@ def _split(n, parts):
 
 
 def _one(what, t, kinds, numel):
-    """The address of a dense device tensor of `numel` elements of one of `kinds`."""
+    """The address of a dense device tensor of `numel` elements of one of `kinds`; None is NULL, which the library takes or refuses."""
+    if t is None:
+        return None
     if t.dtype not in kinds or t.numel() != numel or not t.is_contiguous() or not t.is_cuda:
         raise DistdlError(ERR_INVALID_ARG, f"{what}: a {'' if t.is_contiguous() else 'strided '}{t.dtype} tensor of shape {tuple(t.shape)} "
                                            f"on {t.device}, where {numel} dense elements of {' or '.join(map(str, kinds))} on a GPU are wanted")
@@ -493,15 +495,19 @@ def _one(what, t, kinds, numel):
 
 
 def _many(what, ts, kinds, numels):
-    """Their addresses as the library reads them; None stays NULL.  (Small passes are bound by the host: four lists of
+    """Their addresses as the library reads them; None, of all or of one, stays NULL.  (Small passes are bound by the host: four lists of
     ten arrays take 21 us here, and 27 with a call for each array and an array of ctypes.)"""
     if ts is None:
         return None
     if len(ts) != len(numels):
         raise DistdlError(ERR_INVALID_ARG, f"{what}: {len(ts)} tensors, {len(numels)} are wanted")
-    return struct.pack("%dQ" % len(ts), *[
-        t.data_ptr() if t.dtype in kinds and t.numel() == n and t.is_contiguous() and t.is_cuda else _one(what, t, kinds, n)
-        for t, n in zip(ts, numels)])
+    form = "%dQ" % len(ts)
+    try:
+        return struct.pack(form, *[
+            t.data_ptr() if t.dtype in kinds and t.numel() == n and t.is_contiguous() and t.is_cuda else _one(what, t, kinds, n)
+            for t, n in zip(ts, numels)])
+    except AttributeError:  # (a None)
+        return struct.pack(form, *[_one(what, t, kinds, n) or 0 for t, n in zip(ts, numels)])
 
 
 def _maybe(what, t, kinds, numel):

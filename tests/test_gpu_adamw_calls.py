@@ -85,3 +85,19 @@ def test_weights_without_gradients_under_a_tiny_eps(eps, states8):
     dd.distdl_adamw_step(plan, d["p"], d["g"], **moments, step=1, **dict(HYPER, eps=eps))
     decay = torch.tensor(1 - HYPER["lr"] * HYPER["weight_decay"], dtype=torch.float64).float().cuda()
     assert torch.equal(d["p"][0][:500], p[:500] * decay) and torch.isfinite(d["p"][0]).all()
+
+
+def test_copies_of_some_arrays():
+    """None among the bf16 copies: that array gets none."""
+    require_gpu()
+    counts = [300, 5000, 7]
+    runs = []
+    for some in (False, True):
+        d = make(counts, False)
+        copies = [torch.full((n,), 7.0, dtype=torch.bfloat16, device="cuda") for n in counts]
+        plan = dd.distdl_adamw_plan_create(counts, torch.float32)
+        dd.distdl_adamw_step(plan, d["p"], d["g"], d["m"], d["v"], p16=[copies[0], None, copies[2]] if some else copies, step=1, **HYPER)
+        runs.append((d["p"], copies))
+    (p, full), (p2, partial) = runs
+    assert all(torch.equal(a, b) for a, b in zip(p, p2))
+    assert torch.equal(full[0], partial[0]) and torch.equal(full[2], partial[2]) and (partial[1] == 7).all() and torch.equal(full[1], p[1].bfloat16())
