@@ -58,7 +58,8 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
-// Eight codes times their scale, exactly (numbers below 2^-126 aside).  The instruction reads the exponent of `scale` alone.
+// Eight codes times their scale, exactly: bf16's numbers go down to 2^-133, and what lies below in an operand is all that is rounded.  The instruction
+// reads the exponent of `scale` alone.
 __device__ __forceinline__ float scale_exponent(int byte) { return __uint_as_float((uint32_t)byte << 23); }
 __device__ __forceinline__ v8bf codes_to_bf16(uint32_t lo, uint32_t hi, float scale) {
   union {

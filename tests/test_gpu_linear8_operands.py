@@ -98,3 +98,19 @@ def test_every_tile_with_hard_operands(m, n, dtype, moved):
         dw = torch.full((m, n), 7.0, device="cuda")
         dd.distdl_linear8_bwd_w(plan, [shift(aq[0])], [aq[1]], [shift(bq[0])], [bq[1]], [dw])
         held(dw, [(aq[2], bq[2])], "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n", [(4, 64), (40, 64), (300, 520), (1000, 2040), (4096, 4090)])
+def test_operands_below_the_normal_numbers(m, n, dtype):
+    """Numbers down to 2^-133 count in full where the other operand brings their products back into range."""
+    require_gpu()
+    x, w = torch.zeros(m, 128, device="cuda"), torch.zeros(n, 128, device="cuda")
+    size = (torch.arange(m, device="cuda") % 15 + 1).double()
+    x[:, 0] = (size * 2.0 ** -133).float()
+    w[:, 0] = 2.0 ** 100
+    xq, wq = quantised(x), quantised(w, tiles=True)
+    plan = dd.distdl_linear8_plan_create(m, 128, n, 1, 1, KINDS[dtype])
+    y = torch.empty(m, n, dtype=KINDS[dtype], device="cuda")
+    dd.distdl_linear8_fwd(plan, [xq[0]], [xq[1]], [wq[0]], [wq[1]], [y])
+    assert torch.equal(y.double(), (size * 2.0 ** -33)[:, None].expand(m, n))
