@@ -5,20 +5,23 @@
 //   weight gradient   dW_ij = dy_i^T x_j               the transposes of both in blocks of rows (along the batch)
 //
 // All three are C[m][n] = sum over segments and k of A[m][k] B[n][k] with k contiguous in both; a worker of the sum is a segment, whose
-// blocks start anew.  Sums are fp32, from one of two matrix instructions:
+// blocks start anew.  Accumulators are fp32, fed by one of two matrix instructions:
 //
 //   v_mfma_scale_f32_16x16x128_f8f6f4 takes codes and scales as they are, at 5 PFLOP/s, but adds eight neighbouring products at a time in a
 //   window: beside a product of 2^8 and 2^8, what lies below 2^3 is cut off (measured, each of the 127 other places; the
 //   groups' sums and the accumulator keep all 24 bits).  A result is off by at most 2^-10 of the sum of the groups' largest products,
-//   1.3e-5 of its size for N(0, 1) operands: 1/300 of a bf16 result's last place.  Bf16 results of large products take it.
+//   1.3e-5 of its size for N(0, 1) operands: 1/300 of a bf16 result's last place.  That is fewer bits than an fp32 sum has, and a choice:
+//   each operand's rounding to codes puts a product off by up to 2^-4 of itself already.  Bf16 results whose cheapest tiles are the largest take it: 1.2 % of
+//   those of 4096^3 differ from the rounded fp32 sum's (3.2 % where the numbers of a row differ by factors of exp(2 N(0, 1))), by one place, and both are equally far
+//   (1.66e-3 of their size) from the unrounded sum.  A plan for fp32 results never takes it.
 //
 //   v_mfma_f32_16x16x32_bf16 takes codes times scales, which are exact in bf16 (an instruction converts two), at 2.5 PFLOP/s: sums of 128 to 8192
 //   N(0, 1) products are 1e-8 to 3e-7 off.  Fp32 results take it (weight gradients among them), and products whose time
 //   is not that of the matrix instructions.
 //
-// Measured (us): 8 x 4096 x 4096 7 (2.4 TB/s of weights; a launch and a trip to memory are most of it), 256 x 4096 x 4096 on 2 x 2 workers 17 to 18,
-// 8192 x 4096 x 4096 142 to 154 (1.8 to 1.9 PFLOP/s, 73 % of the library's 8192^3), the same in fp32 265 to 290 (0.95 to 1.02 PFLOP/s: conversions, of
-// which a wave makes one for 2.7 products).
+// Measured (us a launch by the profiler, which counts its start and end, 2.5 for a launch of one workgroup): 8 x 4096 x 4096 7.2 (2.3 TB/s of weights; a launch
+// and a trip to memory are most of it), 256 x 4096 x 4096 on 2 x 2 workers 18 (a pass among others 15), 8192 x 4096 x 4096 142 to 154 (1.8 to 1.9 PFLOP/s, 73 % of
+// the library's 8192^3), the same in fp32 265 to 290 (0.95 to 1.02 PFLOP/s: conversions, of which a wave makes one for 2.7 products).
 #include <algorithm>
 #include <cstddef>
 #include <map>

@@ -12,7 +12,8 @@
 // ROWS16: every row starts at a multiple of 16 bytes, a lane's eight features are neighbours (two accesses of fp32, one of bf16).  Otherwise
 // they are 64 apart, each access at its natural alignment: wide accesses that straddle cost more than narrow ones.
 //
-// Measured: forward 8192 x 4096 bf16 on two workers, residual in, sum and 8-bit codes out, 50 us (4.8 TB/s); adjoint 5003 x 2000 fp32 on three workers
+// Measured: forward 8192 x 4096 bf16 on two workers, residual in, sum and 8-bit codes out, 50 us (4.8 TB/s), on one with a bf16 answer in their place 51 (5.2 TB/s), its
+// adjoint 52 (5.2 TB/s) and 5 for the sum of dg's parts; adjoint 5003 x 2000 fp32 on three workers, of whose pieces of 512 places half are empty,
 // 34 us (4.7 TB/s) and 5 for the sum of dg's parts; forward 4 x 4096 3.7 us, a launch and a trip to memory.
 #include <algorithm>
 #include <cfloat>

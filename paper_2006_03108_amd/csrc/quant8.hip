@@ -5,8 +5,10 @@
 // threads, whose magnitudes meet in LDS.  A thread's 8 x 8 codes are turned in registers and go through LDS, so that both orders
 // are written in runs of a whole block.
 //
-// Measured: 8192 x 4096 bf16 to codes in both orders 31 us (4.4 TB/s).  A thread with half the elements, 512 to a
-// workgroup: 48 us.  Neighbouring tiles on one XCD: 36 us for 33.  Codes of one order alone: 25 to 28.
+// Measured: 8192 x 4096 bf16 to codes in both orders 31 us (4.3 TB/s), to the transposed ones alone 33 (3.0 TB/s), of an array that other work has put out of the
+// caches; the same array again and again 27, 21 (rows alone 21).  4096 x 4096 fp32 in tiles, both orders, again and again 17.  145 registers for blocks of rows leave three
+// waves to a SIMD, and a call for one order holds both orders' maxima.  A thread with half the elements, 512 to a
+// workgroup: 48 us.  Neighbouring tiles on one XCD: 36 us for 33.
 #include <algorithm>
 #include <cstddef>
 

@@ -488,12 +488,15 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_bwd_kernel(ScanArgs s) {
 // time: who waits, waits for tickets drawn before its own, so the lowest ticket not yet done never waits and every wait ends, however
 // few workgroups the card holds at a time.  Tickets go on from pass to pass: their quotient by the pass's tiles is the tag.
 //
-// Measured (us): 65536 x 1024 bf16 on four workers 100 to 105 (3.9 to 4.0 TB/s), adjoint of 7 x 2049 x 1001 fp32 71 to 75 (4.6 to 4.9 TB/s); with time read twice, once for the
-// maps, 145 and 88; without the waits 94 and 74, and the rest is what a workgroup takes from its start to its stores, two at a time on a
-// compute unit.  Gates made twice instead of held (tiles twice as long): 100 and 85.  Workgroups that go from tile to tile and have the next
+// Measured (us): 65536 x 1024 bf16 on four workers 98 to 102 (4.0 to 4.1 TB/s), adjoint of 7 x 2049 x 1001 fp32 66 to 71 (4.6 to 4.9 TB/s where nothing is cut); with time
+// read twice, once for the maps, 145 and 88.  What a tile takes from its workgroup's start to its stores, two at a time on a compute unit, bounds it.
+// Gates made twice instead of held (tiles twice as long): 100 and 85.  Workgroups that go from tile to tile and have the next
 // one's loads under way, whose loads the waits then stand behind: 133 and 83.  Four waves: 107 and 83, sixteen: 215 and 122.
 constexpr int kScanSuper = 2 * kScanWaves;
-constexpr int kScanFew = 128;    // chains at most
+// Chains at most.  Between 128 and 256 the better kernel depends on the steps as well (us, sigmoid gates, one workgroup through all of time; one for a tile): 136
+// chains of 512 bf16 steps 18, 20 (adjoint 29, 30), of 2048 56, 47 (121, 99), of 8192 235, 177 (458, 356); 160 chains 18, 21 (30, 33), 57, 54 (127, 136),
+// 243, 206 (483, 412); 192 chains 18, 23 (32, 37), 65, 67 (139, 133), 265, 242 (514, 505).  128 is where the second is the better or equal one for all.
+constexpr int kScanFew = 128;
 constexpr int kScanShort = 128;  // steps that one workgroup goes through as fast
 
 // Steps of a wave, forwards and backwards: what 64 registers hold of them (16 for two workgroups on a compute unit, 24 for one: the same time).
