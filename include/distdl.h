@@ -553,6 +553,56 @@ int distdl_adamw_step(distdl_adamw_plan* plan, void* const p_dev[], const void* 
                       const distdl_adamw_args* args, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Operators of rows of logits whose vocabulary P workers share: x_j [rows][v_j]
+ * dense, the vocabulary split by the balanced split, which is how the outputs
+ * of an affine layer lie.  z = x / temperature (from 1e-6 to 1e6), p the
+ * softmax of a row over all workers' entries (the all-reduces of the workers'
+ * maxima and sums).  Pointers travel with the launch up to 16 workers; scratch
+ * is allocated by a plan's first call of a kind on a stream, which cannot be a
+ * recorded one.  Calls and recorded graphs of one plan and stream share it:
+ * they run one after another.  rows may be 0.
+ *   An entry of -inf has no share: p = 0, and it adds 0 to the entropy and to
+ * gradients.  A row of nothing else has lse -inf, log probabilities -inf,
+ * entropy 0 and gradients 0.  A row with +inf or a NaN answers NaN.  Masks of
+ * the type's lowest value are numbers: a row of them alone is an even one (but
+ * logprob_bwd, whose lse cannot hold how many they are, gives gradients 0 to
+ * rows with an lse below -1e30).
+ *
+ * logprob_fwd: lse = log sum exp z;  logp = z[target] - lse, and 0 where the
+ *   target is not in 0 .. n_v - 1 (targets are int32 [rows]);  entropy =
+ *   - sum p log p;  the n_top (0 to 64, at most n_v) largest entries of each
+ *   row in order, of equal ones the first: their places top_ids (int32) and
+ *   log probabilities top_logp, [rows][n_top].  A NaN is no alternative; where
+ *   too few are left the place is -1.  Any output may be NULL, not all.
+ * logprob_bwd: dx = (dlogp (1[target] - p) - dentropy p (log p + entropy)) /
+ *   temperature, from the lse and entropy that fwd wrote.  dlogp (with the
+ *   targets) or dentropy (with the entropy) may be NULL; rows without a target
+ *   have no part in dlogp.  A row whose gradients are 0 gets zeros without
+ *   being read.  dx may lie on x.
+ * distill_fwd_bwd: a teacher's n_top (1 to 1024) logits or log probabilities
+ *   for each row, fp32 [rows][n_top], at the places ids (int32); a place that
+ *   is not in 0 .. n_v - 1 is not used, one that comes twice counts twice.
+ *   t = softmax of teacher / temperature over the used ones;
+ *   loss = sum t (log t - log p), unweighted;
+ *   dx = weight / temperature (p - t), the gradient of weight * loss
+ *   (weight_dev [rows] NULL: 1).  Rows with no used place, or only ones of
+ *   -inf, have loss 0 and gradient 0, rows of weight 0 gradient 0.  One
+ *   place with any finite logit gives the cross entropy.  loss or dx may be
+ *   NULL; dx may lie on x. */
+typedef struct distdl_logits_plan distdl_logits_plan;
+int distdl_logits_plan_create(distdl_logits_plan** out, int64_t rows, int64_t n_v, int P, distdl_dtype dtype);
+int distdl_logits_plan_destroy(distdl_logits_plan* plan);
+int distdl_logprob_fwd(distdl_logits_plan* plan, const void* const x_dev[], const int32_t* targets_dev, float* logp_dev,
+                       float* lse_dev, float* entropy_dev, int32_t* top_ids_dev, float* top_logp_dev, int n_top,
+                       double temperature, void* stream);
+int distdl_logprob_bwd(distdl_logits_plan* plan, const void* const x_dev[], const int32_t* targets_dev,
+                       const float* lse_dev, const float* entropy_dev, const float* dlogp_dev,
+                       const float* dentropy_dev, void* const dx_dev[], double temperature, void* stream);
+int distdl_distill_fwd_bwd(distdl_logits_plan* plan, const void* const x_dev[], const int32_t* ids_dev,
+                           const float* teacher_dev, int n_top, const float* weight_dev, float* loss_dev,
+                           void* const dx_dev[], double temperature, void* stream);
+
+/* ------------------------------------------------------------------------
  * Measurement support.  plan_stats: cell counts behind the algorithmic-bytes
  * figures of the halo kernels, summed over all workers and per sample and
  * channel: out[0] halo cells (in-domain, non-owned), out[1] zero-padding

@@ -18,6 +18,8 @@ Modules
                 algorithms; the point-wise / loss glue of the Sec. 5 network.
   blocks        beyond the paper: the operators of gated recurrent blocks
                 (norm, 8-bit numbers, recurrence, AdamW), whole tensors.
+  tokens        beyond the paper: the gated delta rule, and operators of rows of
+                logits (log probabilities, distillation), whole tensors.
 
 Parity pins: every function here is checked in tests/ (run with -m "not gpu")
 against values the paper prints (App. B.1 examples, App. C table), against

@@ -99,6 +99,11 @@ _SIGS = {
     "distdl_adamw_plan_create": [C.POINTER(_vp), _p64, _i, _i, _i],
     "distdl_adamw_plan_destroy": [_vp],
     "distdl_adamw_step": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp],
+    "distdl_logits_plan_create": [C.POINTER(_vp), _i64, _i64, _i, _i],
+    "distdl_logits_plan_destroy": [_vp],
+    "distdl_logprob_fwd": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, C.c_double, _vp],
+    "distdl_logprob_bwd": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_double, _vp],
+    "distdl_distill_fwd_bwd": [_vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, C.c_double, _vp],
     "distdl_dot": [_pp, _pp, _p64, _i, _i, _vp, _vp],
     "distdl_dot_static": [_pp, _pp, _p64, _i, _i, _vp, _vp],
     "distdl_relu_fwd": [_pp, _pp, _p64, _i, _vp],
@@ -533,7 +538,7 @@ class _Handle:
             pass
 
 
-_F32 = (torch.float32,)
+_F32, _I32 = (torch.float32,), (torch.int32,)
 
 
 def distdl_quant8(x, q, s, qt, st, tiles=False):
@@ -678,6 +683,48 @@ def distdl_adamw_step(plan, p, g, m, v, ms=None, vs=None, p16=None, *, lr, beta1
                                  _many("v", v, plan.state_kind, n), _many("ms", ms, _SCALES, plan.blocks) if scales else None,
                                  _many("vs", vs, _SCALES, plan.blocks) if scales else None, _many("p16", p16, (torch.bfloat16,), n),
                                  C.byref(args), _stream()))
+
+
+# ---- logits ----------------------------------------------------------------
+
+def distdl_logits_plan_create(rows, n_v, P, dtype=torch.bfloat16):
+    h = C.c_void_p()
+    _check(lib.distdl_logits_plan_create(C.byref(h), rows, n_v, P, _dtype_code(dtype)))
+    kind = _F32 if _dtype_code(dtype) == DISTDL_F32 else (torch.bfloat16,)
+    return _Handle(h, lib.distdl_logits_plan_destroy, kind=kind, rows=rows, n=[rows * v for v in _split(n_v, P)])
+
+
+def _row_lists(what, rows, *ts):
+    """Columns of the [rows, k] tensors that are given; 0 if none is."""
+    sizes = {tuple(t.shape) for t in ts if t is not None}
+    if len(sizes) > 1 or any(len(s) != 2 or s[0] != rows for s in sizes):
+        raise DistdlError(ERR_INVALID_ARG, f"{what}: tensors of shapes {sorted(sizes)}, where [{rows}, k] is wanted of all")
+    return sizes.pop()[1] if sizes else 0
+
+
+def distdl_logprob_fwd(plan, x, targets, logp, lse, entropy, top_ids=None, top_logp=None, temperature=1.0):
+    """targets: int32 [rows].  Any of the outputs logp, lse, entropy (fp32 [rows]), top_ids (int32 [rows, k]), top_logp (fp32 [rows, k])
+    may be None."""
+    r, k = plan.rows, _row_lists("logprob_fwd", plan.rows, top_ids, top_logp)
+    _check(lib.distdl_logprob_fwd(plan.handle, _many("x", x, plan.kind, plan.n), _maybe("targets", targets, _I32, r), _maybe("logp", logp, _F32, r),
+                                  _maybe("lse", lse, _F32, r), _maybe("entropy", entropy, _F32, r), _maybe("top_ids", top_ids, _I32, r * k),
+                                  _maybe("top_logp", top_logp, _F32, r * k), k, temperature, _stream()))
+
+
+def distdl_logprob_bwd(plan, x, targets, lse, entropy, dlogp, dentropy, dx, temperature=1.0):
+    """dlogp, or entropy and dentropy, may be None."""
+    r = plan.rows
+    _check(lib.distdl_logprob_bwd(plan.handle, _many("x", x, plan.kind, plan.n), _maybe("targets", targets, _I32, r), _maybe("lse", lse, _F32, r),
+                                  _maybe("entropy", entropy, _F32, r), _maybe("dlogp", dlogp, _F32, r), _maybe("dentropy", dentropy, _F32, r),
+                                  _many("dx", dx, plan.kind, plan.n), temperature, _stream()))
+
+
+def distdl_distill_fwd_bwd(plan, x, ids, teacher, weight, loss, dx, temperature=1.0):
+    """ids: int32 [rows, k], teacher: fp32 [rows, k].  weight, and loss (fp32 [rows]) or dx, may be None."""
+    r, k = plan.rows, _row_lists("distill_fwd_bwd", plan.rows, ids, teacher)
+    _check(lib.distdl_distill_fwd_bwd(plan.handle, _many("x", x, plan.kind, plan.n), _maybe("ids", ids, _I32, r * k),
+                                      _maybe("teacher", teacher, _F32, r * k), k, _maybe("weight", weight, _F32, r), _maybe("loss", loss, _F32, r),
+                                      _many("dx", dx, plan.kind, plan.n), temperature, _stream()))
 
 
 def _numels(ts):

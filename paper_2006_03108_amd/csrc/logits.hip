@@ -1,0 +1,863 @@
+// Log probabilities, entropy and top alternatives of rows of logits whose vocabulary P workers share, their adjoint, and the
+// divergence from a teacher's top logits with its gradient.
+//
+//   z = x / temperature,  lse = log sum exp z,  log p_i = z_i - lse,  H = lse - sum p_i z_i
+//   adjoint of (log p_t, H)   dx_i = (dlogp (1[i = t] - p_i) - dH p_i (log p_i + H)) / temperature
+//   divergence                sum_k pi_k (log pi_k - log p_{id_k}),  pi = softmax of the teacher's logits / temperature
+//                             dx_i = weight / temperature (p_i - sum_{k: id_k = i} pi_k)
+//
+// The sums over the vocabulary are the all-reduce of the workers' sums: a workgroup reads a row's parts one behind the other, once,
+// with a running maximum.  Everything is in units of log 2: d_i = x_i c - mc, c = log2(e) / temperature, mc = c max x as it was
+// rounded, so that exp2(d_i) and what is made of mc belong together whatever mc lost, and the partial sums of lanes, waves and parts meet by
+// factors exp2(mc - mc').  Then lse = ln 2 (mc + log2 s) and H = ln 2 (log2 s - w / s), s = sum exp2(d), w = sum exp2(d) d: both
+// terms of H are positive.
+#include <algorithm>
+#include <cfloat>
+#include <climits>
+#include <cstddef>
+
+#include "block8.h"
+#include "common.h"
+#include "profile.h"
+
+namespace distdl {
+
+constexpr int kLogitsInline = 16;   // workers whose pointers travel with the launch; more are in a table
+constexpr int kLogitsThreads = 256;
+constexpr int kLogitsWaves = kLogitsThreads / 64;
+constexpr int kTopMost = 64;        // alternatives: one to a lane
+constexpr int kStoredMost = 1024;   // a teacher's logits for one row
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct LogitsWorker {
+  const void* x;
+  void* dx;
+};
+
+struct LogitsArgs {
+  LogitsWorker w[kLogitsInline];
+  const LogitsWorker* more;
+  int64_t rows;
+  int32_t n_v, P, part, extra;     // worker j has part + (j < extra) entries
+  int32_t vec_wide, vec_rest;      // vectors of eight entries of a worker with part + 1, with part
+  int32_t splits, per;             // of a row's vectors, and how many each has
+  float c, inv_t;
+  int32_t n_top;
+  const int32_t* targets;
+  float *logp, *lse, *entropy;
+  int32_t* ids;
+  float* top;
+  const float *dlogp, *dentropy;   // adjoint; lse and entropy are inputs there
+  const int32_t* stored_ids;       // the teacher's
+  const float *stored, *weight;
+  float* loss;
+  float4* parts;                   // (max, mc, s, w) of each split
+  uint64_t* part_top;              // kTopMost keys of each split
+  float* stored_x;                 // the student's logits at the teacher's places
+};
+
+static_assert(offsetof(LogitsArgs, w) == 0, "the kernels' first argument starts with the workers");
+typedef const __attribute__((address_space(4))) LogitsWorker* LogitsTable;
+// (read as constants, into scalar registers; the address of the arguments is taken in the kernel itself)
+#define LOGITS_TABLE(s) ((s).more ? (LogitsTable)(uint64_t)(s).more : (LogitsTable)__builtin_amdgcn_kernarg_segment_ptr())
+
+struct LogitsPart {  // worker j's share of the vocabulary
+  int32_t n, first, vec0, vecs;
+};
+__device__ __forceinline__ LogitsPart logits_part(const LogitsArgs& s, int j) {
+  const bool wide = j < s.extra;
+  LogitsPart p;
+  p.n = s.part + wide;
+  p.first = j * s.part + min(j, s.extra);
+  p.vecs = wide ? s.vec_wide : s.vec_rest;
+  p.vec0 = wide ? j * s.vec_wide : s.extra * s.vec_wide + (j - s.extra) * s.vec_rest;
+  return p;
+}
+// the worker of entry `id`
+__device__ __forceinline__ int logits_worker_of(const LogitsArgs& s, int id) {
+  const int64_t wide = (int64_t)s.extra * (s.part + 1);
+  return id < wide ? id / (s.part + 1) : s.extra + (int)((id - wide) / s.part);
+}
+template <class E>
+__device__ __forceinline__ float logits_at(const LogitsArgs& s, LogitsTable table, int64_t row, int id) {
+  const int j = logits_worker_of(s, id);
+  const LogitsPart p = logits_part(s, j);
+  return ld((const E*)table[j].x, (size_t)(row * p.n + (id - p.first)));
+}
+
+// Eight neighbouring entries of a row.  A part's last vector starts so that it ends with the part, and of its entries those from `from`
+// on are its own: every load is whole and inside the row.  (Parts of fewer than eight entries are read one by one.)
+template <class E>
+struct LogitsVector {
+  Eight<E> raw;
+  int at, from;
+  __device__ __forceinline__ void load(const E* row, int n, int v, int end) {
+    at = max(0, min(8 * v, n - 8));
+    from = v < end ? 8 * v - at : 8;
+    if (n >= 8) raw.load(row + at, 8);
+    else raw.load(row, n);
+  }
+  // values; -inf in the places that are not its own, if `edge` (uniform) says that there may be such
+  __device__ __forceinline__ void values(float* f, int n, bool edge) const {
+    raw.values(f);
+    if (edge) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = i >= from && i < n ? f[i] : -INFINITY;
+    }
+  }
+};
+template <class E>
+constexpr int logits_batch() { return sizeof(E) == 2 ? 4 : 2; }  // vectors of a lane under way: 64 bytes
+
+// f(worker, part, first vector of the lane's batch, end) for the batches of the split's vectors
+template <int B, int THREADS, class F>
+__device__ __forceinline__ void logits_each(const LogitsArgs& s, int split, F f) {
+  const int lo = split * s.per, hi = min(lo + s.per, s.extra * s.vec_wide + (s.P - s.extra) * s.vec_rest);
+  for (int j = 0; j < s.P; ++j) {
+    const LogitsPart p = logits_part(s, j);
+    const int from = max(0, lo - p.vec0), to = min(p.vecs, hi - p.vec0);
+    for (int base = from; base < to; base += THREADS * B) f(j, p, base, to);
+  }
+}
+
+// ---- sums -----------------------------------------------------------------
+// Where the maximum is so far from 0 that m c may be no number (masks of the type's lowest value that leave nothing else), d is (x - m) c,
+// which costs an operation more and is 0 or out of exp2's range.
+constexpr float kFar = 1e30f;
+
+struct LogitsSums {
+  float m = -INFINITY, mc = 0.f, s = 0.f, w = 0.f;
+  __device__ __forceinline__ bool far() const { return fabsf(m) >= kFar && m != -INFINITY; }
+  // d of an entry
+  __device__ __forceinline__ float of(float x, float c) const { return far() ? (x - m) * c : fmaf(x, c, -mc); }
+  __device__ __forceinline__ bool none() const { return m == -INFINITY && s == 0.f; }  // every entry is -inf
+  // the reference moves up to the maximum m1
+  __device__ __forceinline__ void raise(float m1, float c) {
+    const float mc1 = m1 == -INFINITY ? 0.f : m1 * c;
+    // (where there is nothing to move, nowhere)
+    const float shift = m == -INFINITY ? 0.f : fmaxf(fabsf(m) >= kFar || fabsf(m1) >= kFar ? (m - m1) * c : mc - mc1, -kFar);
+    const float f = __builtin_amdgcn_exp2f(shift);
+    w = f * fmaf(s, shift, w);
+    s *= f;
+    m = m1;
+    mc = mc1;
+  }
+  __device__ __forceinline__ void join(LogitsSums o, float c) {
+    const float m1 = fmaxf(m, o.m);
+    raise(m1, c);
+    o.raise(m1, c);
+    s += o.s;
+    w += o.w;
+  }
+  __device__ __forceinline__ void join_lanes(float c) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      LogitsSums other;
+      other.m = __shfl_xor(m, o, 64);
+      other.mc = __shfl_xor(mc, o, 64);
+      other.s = __shfl_xor(s, o, 64);
+      other.w = __shfl_xor(w, o, 64);
+      join(other, c);
+    }
+  }
+  // The sums of all waves, for all threads.  `shared`: a place for each wave.
+  template <int WAVES>
+  __device__ __forceinline__ void join_waves(float4* shared, float c) {
+    join_lanes(c);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = make_float4(m, mc, s, w);
+    __syncthreads();
+    LogitsSums all;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) {
+      const float4 v = shared[i];
+      LogitsSums one;
+      one.m = v.x, one.mc = v.y, one.s = v.z, one.w = v.w;
+      all.join(one, c);
+    }
+    *this = all;
+  }
+};
+
+// A batch of a lane's values.  The entropy's w counts what exp2 makes 0 as 0, -inf too.
+template <int N, bool ENTROPY>
+__device__ __forceinline__ void logits_add(LogitsSums& a, const float (&f)[N], float most, float c) {
+  a.raise(fmaxf(a.m, most), c);
+  if (__builtin_expect(__any(a.far()), 0)) {
+#pragma unroll 1
+    for (int i = 0; i < N; ++i) {
+      float x = f[0];
+#pragma unroll
+      for (int k = 1; k < N; ++k) x = i == k ? f[k] : x;
+      const float d = a.of(x, c), e = __builtin_amdgcn_exp2f(d);
+      a.s += e;
+      if (ENTROPY) a.w = fmaf(e, fmaxf(d, -200.f), a.w);
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float d = fmaf(f[i], c, -a.mc), e = __builtin_amdgcn_exp2f(d);
+    a.s += e;
+    if (ENTROPY) a.w = fmaf(e, fmaxf(d, -200.f), a.w);
+  }
+}
+__device__ __forceinline__ float max8(const float* f) {
+  return fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
+}
+
+// ---- top alternatives -----------------------------------------------------
+// An entry's key: its value as an integer in the same order, above the complement of its place, so that larger keys come first.  0 is no entry.
+__device__ __forceinline__ int32_t order_of(float v) {
+  const int32_t b = (int32_t)__float_as_uint(v + 0.f);  // (-0 is 0)
+  return v != v ? INT_MIN : b ^ ((b >> 31) & 0x7fffffff);  // (a NaN is no alternative)
+}
+__device__ __forceinline__ uint64_t key_of(int32_t order, int id) { return (uint64_t)((uint32_t)order ^ 0x80000000u) << 32 | (uint32_t)~id; }
+__device__ __forceinline__ float value_of(uint64_t key) {
+  const int32_t o = (int32_t)((uint32_t)(key >> 32) ^ 0x80000000u);
+  return __uint_as_float((uint32_t)(o ^ ((o >> 31) & 0x7fffffff)));
+}
+
+template <class T>
+__device__ __forceinline__ T other_lane(T v, int o) {
+  if constexpr (sizeof(T) == 8) {
+    const uint32_t lo = __shfl_xor((int)(uint32_t)v, o, 64), hi = __shfl_xor((int)(uint32_t)(v >> 32), o, 64);
+    return (T)((uint64_t)hi << 32 | lo);
+  } else {
+    return __shfl_xor(v, o, 64);
+  }
+}
+template <class T>
+__device__ __forceinline__ T turned_lanes(T v) { return other_lane(v, 63); }
+// the last rounds of a bitonic sort: a bitonic sequence of `n` lanes becomes a descending one where `down`, else ascending
+template <int N, class T>
+__device__ __forceinline__ T bitonic(T v, bool down) {
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) {
+    const T u = other_lane(v, o);
+    const bool large = ((threadIdx.x & o) == 0) == down;
+    v = large == (u > v) ? u : v;
+  }
+  return v;
+}
+template <class T>
+__device__ __forceinline__ T sorted_lanes(T v) {  // descending
+  v = bitonic<2>(v, (threadIdx.x & 2) == 0);
+  v = bitonic<4>(v, (threadIdx.x & 4) == 0);
+  v = bitonic<8>(v, (threadIdx.x & 8) == 0);
+  v = bitonic<16>(v, (threadIdx.x & 16) == 0);
+  v = bitonic<32>(v, (threadIdx.x & 32) == 0);
+  return bitonic<64>(v, true);
+}
+// the 64 largest keys of two descending lists
+__device__ __forceinline__ uint64_t merged_lanes(uint64_t a, uint64_t b) {
+  b = turned_lanes(b);
+  return bitonic<64>(a > b ? a : b, true);
+}
+
+// A wave's 64 best entries, descending over the lanes, and a buffer of those that wait.  Entries at or below `floor`, the n-th best so far, can
+// not be among the n: a wave meets entries in the order of their places, so of equal values the first stay.
+struct TopList {
+  uint64_t best = 0;
+  int32_t floor = INT_MIN;
+  int waiting = 0;
+  static constexpr int kRoom = 64 + 512;
+  __device__ __forceinline__ void set_floor(int n_top) {
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(best >> 32), n_top - 1);
+    floor = max(floor, (int32_t)(hi ^ 0x80000000u));
+  }
+  // From the largest of each lane's first entries: the n-th of them is no better than the n-th of all.
+  __device__ __forceinline__ void start(float most, int n_top) {
+    const int32_t nth = __builtin_amdgcn_readlane(sorted_lanes(order_of(most)), n_top - 1);
+    floor = max(nth, INT_MIN + 1) - 1;
+  }
+  __device__ __forceinline__ void flush(uint64_t* buffer, int n_top) {
+    const int lane = threadIdx.x & 63;
+    while (waiting > 0) {
+      const int n = min(waiting, 64), from = waiting - n;
+      best = merged_lanes(best, sorted_lanes(lane < n ? buffer[from + lane] : 0));
+      waiting = from;
+    }
+    __builtin_amdgcn_wave_barrier();
+    set_floor(n_top);
+  }
+  // a vector of each lane
+  __device__ __forceinline__ void take(uint64_t* buffer, const float* f, int id, int from, int upto, int n_top) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int32_t o = order_of(f[i]);
+      const bool in = o > floor && i >= from && i < upto;
+      const uint64_t all = __ballot(in);
+      if (in) buffer[waiting + __popcll(all & ((uint64_t(1) << lane) - 1))] = key_of(o, id + i);
+      waiting += __popcll(all);
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (waiting >= 64) flush(buffer, n_top);
+  }
+};
+
+// What a row's sums and alternatives come to.  Every wave has the sums; wave 0 has the list.
+template <class E>
+__device__ __forceinline__ void logits_finish(const LogitsArgs& s, LogitsTable table, int64_t row, const LogitsSums& a, uint64_t best) {
+  const float total = __builtin_amdgcn_logf(a.s);  // log2
+  const bool none = a.none();
+  if (threadIdx.x == 0) {
+    if (s.lse) s.lse[row] = none ? -INFINITY : a.far() ? fmaf(a.m, s.inv_t, kLn2 * total) : kLn2 * (a.mc + total);
+    if (s.entropy) s.entropy[row] = none ? 0.f : kLn2 * (total - a.w / a.s);
+    if (s.logp) {
+      const int t = s.targets[row];
+      float v = 0.f;
+      if (t >= 0 && t < s.n_v) v = none ? -INFINITY : kLn2 * (a.of(logits_at<E>(s, table, row, t), s.c) - total);
+      s.logp[row] = v;
+    }
+  }
+  if (s.n_top > 0 && threadIdx.x < s.n_top) {
+    const int64_t o = row * s.n_top + threadIdx.x;
+    if (s.ids) s.ids[o] = best ? (int32_t)~(uint32_t)best : -1;
+    if (s.top) s.top[o] = none || !best ? -INFINITY : kLn2 * (a.of(value_of(best), s.c) - total);
+  }
+}
+
+// A row, or one of its splits, to a workgroup.
+template <class E, bool ENTROPY, bool TOP>
+__global__ __launch_bounds__(kLogitsThreads) void logits_fwd_kernel(LogitsArgs s) {
+  constexpr int B = logits_batch<E>();
+  __shared__ float4 sums[kLogitsWaves];
+  __shared__ uint64_t buffers[TOP ? kLogitsWaves * TopList::kRoom : 1];
+  const LogitsTable table = LOGITS_TABLE(s);
+  const int64_t row = blockIdx.x / (uint32_t)s.splits;
+  const int split = blockIdx.x % (uint32_t)s.splits, tid = threadIdx.x, wave = tid >> 6;
+  uint64_t* const buffer = buffers + (TOP ? wave * TopList::kRoom : 0);
+  LogitsSums a;
+  TopList list;
+  bool first = true;
+  logits_each<B, kLogitsThreads>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
+    const E* const x = (const E*)table[j].x + row * p.n;
+    LogitsVector<E> v[B];
+    float f[B * 8], most[B], all = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < B; ++b) v[b].load(x, p.n, base + b * kLogitsThreads + tid, to);
+    const bool edge = base + B * kLogitsThreads >= to;  // (a last vector, or none)
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      v[b].values(f + 8 * b, p.n, edge);
+      most[b] = max8(f + 8 * b);
+      all = fmaxf(all, most[b]);
+    }
+    logits_add<B * 8, ENTROPY>(a, f, all, s.c);
+    if constexpr (TOP) {
+      if (first) list.start(all, s.n_top);
+      first = false;
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+        if (__any(order_of(most[b]) > list.floor)) list.take(buffer, f + 8 * b, p.first + v[b].at, v[b].from, p.n, s.n_top);
+    }
+  });
+  if constexpr (TOP) {
+    list.flush(buffer, s.n_top);
+    buffer[tid & 63] = list.best;
+  }
+  a.join_waves<kLogitsWaves>(sums, s.c);
+  if constexpr (TOP) {
+    if (wave == 0)
+      for (int i = 1; i < kLogitsWaves; ++i) list.best = merged_lanes(list.best, buffers[i * TopList::kRoom + tid]);
+  }
+  if (s.splits == 1) {
+    logits_finish<E>(s, table, row, a, list.best);
+    return;
+  }
+  if (tid == 0) s.parts[blockIdx.x] = make_float4(a.m, a.mc, a.s, a.w);
+  if (TOP && tid < s.n_top) s.part_top[(int64_t)blockIdx.x * s.n_top + tid] = list.best;
+}
+
+// The splits of a row meet, in a fixed order.
+__device__ __forceinline__ LogitsSums logits_joined(const LogitsArgs& s, int64_t row, float4* shared) {
+  LogitsSums a;
+  for (int i = threadIdx.x; i < s.splits; i += kLogitsThreads) {
+    const float4 v = s.parts[row * s.splits + i];
+    LogitsSums one;
+    one.m = v.x, one.mc = v.y, one.s = v.z, one.w = v.w;
+    a.join(one, s.c);
+  }
+  a.join_waves<kLogitsWaves>(shared, s.c);
+  return a;
+}
+
+template <class E>
+__global__ __launch_bounds__(kLogitsThreads) void logits_join_kernel(LogitsArgs s) {
+  __shared__ float4 sums[kLogitsWaves];
+  __shared__ uint64_t lists[kLogitsWaves * 64];
+  const LogitsTable table = LOGITS_TABLE(s);
+  const int64_t row = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint64_t best = 0;
+  if (s.n_top > 0) {
+    for (int i = wave; i < s.splits; i += kLogitsWaves) {
+      const uint64_t more = lane < s.n_top ? s.part_top[(row * s.splits + i) * s.n_top + lane] : 0;
+      best = merged_lanes(best, more);
+    }
+    lists[tid] = best;
+  }
+  const LogitsSums a = logits_joined(s, row, sums);
+  if (s.n_top > 0 && wave == 0)
+    for (int i = 1; i < kLogitsWaves; ++i) best = merged_lanes(best, lists[i * 64 + lane]);
+  logits_finish<E>(s, table, row, a, best);
+}
+
+// ---- adjoint --------------------------------------------------------------
+template <class E>
+__device__ __forceinline__ void logits_store(E* row, const float* f, int at, int from, int n, bool edge) {
+  if (edge && (from > 0 || n < 8)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i >= from && i < n) st(row, (size_t)(at + i), f[i]);
+  } else {
+    store8(row + at, f, 8);
+  }
+}
+
+template <class E, bool ENTROPY>
+__global__ __launch_bounds__(kLogitsThreads) void logits_bwd_kernel(LogitsArgs s) {
+  constexpr int B = logits_batch<E>();
+  const LogitsTable table = LOGITS_TABLE(s);
+  const int64_t row = blockIdx.x / (uint32_t)s.splits;
+  const int split = blockIdx.x % (uint32_t)s.splits, tid = threadIdx.x;
+  const int target = s.targets ? s.targets[row] : -1;
+  const bool live = target >= 0 && target < s.n_v;
+  const float lse = s.lse[row], weight = live ? s.dlogp[row] : 0.f, back = ENTROPY ? s.dentropy[row] : 0.f;
+  // dx = p (one + two log2 p) / temperature, and the target's dlogp
+  const float one = (-weight - (ENTROPY ? back * s.entropy[row] : 0.f)) * s.inv_t, two = -back * kLn2 * s.inv_t;
+  const bool nothing = (weight == 0.f && back == 0.f) || lse < -kFar;  // such rows are not read
+  const bool far = lse >= kFar;
+  const float lc = lse * (1.f / kLn2), at_target = weight * s.inv_t;
+  logits_each<B, kLogitsThreads>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
+    const E* const x = (const E*)table[j].x + row * p.n;
+    E* const dx = (E*)table[j].dx + row * p.n;
+    LogitsVector<E> v[B];
+    const bool edge = base + B * kLogitsThreads >= to;  // (a last vector, or none)
+    if (!nothing) {
+#pragma unroll
+      for (int b = 0; b < B; ++b) v[b].load(x, p.n, base + b * kLogitsThreads + tid, to);
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      float f[8] = {};
+      const int i0 = base + b * kLogitsThreads + tid;
+      const int at = max(0, min(8 * i0, p.n - 8)), from = i0 < to ? 8 * i0 - at : 8;
+      if (!nothing) {
+        v[b].values(f, p.n, edge);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float d = far ? fmaf(f[i], s.inv_t, -lse) * (1.f / kLn2) : fmaf(f[i], s.c, -lc), e = __builtin_amdgcn_exp2f(d);
+          f[i] = ENTROPY ? e * fmaf(two, fmaxf(d, -200.f), one) : e * one;
+          if (live && p.first + at + i == target) f[i] += at_target;
+        }
+      }
+      logits_store(dx, f, at, from, p.n, edge);
+    }
+  });
+}
+
+// ---- divergence from a teacher's top logits -------------------------------
+struct Stored {
+  int32_t id[kStoredMost];
+  float p[kStoredMost];  // the teacher's probabilities
+  float x[kStoredMost];  // the student's logits
+  float red[kLogitsWaves];
+};
+__device__ __forceinline__ float group_max(float v, float* red) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = red[0];
+#pragma unroll
+  for (int i = 1; i < kLogitsWaves; ++i) v = fmaxf(v, red[i]);
+  return v;
+}
+__device__ __forceinline__ float group_sum(float v, float* red) {
+  v = wave_sum(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = red[0];
+#pragma unroll
+  for (int i = 1; i < kLogitsWaves; ++i) v += red[i];
+  return v;
+}
+// The teacher's probabilities of a row: false if it has stored nothing.  total: log2 of their sum relative to `most`.
+__device__ __forceinline__ bool stored_load(const LogitsArgs& s, int64_t row, Stored& t, float& mc, float& total) {
+  float most = -INFINITY;
+  bool odd = false;
+  for (int k = threadIdx.x; k < s.n_top; k += kLogitsThreads) {
+    const int id = s.stored_ids[row * s.n_top + k];
+    const bool in = id >= 0 && id < s.n_v;
+    const float v = in ? s.stored[row * s.n_top + k] : -INFINITY;
+    t.id[k] = in ? id : -1;
+    t.p[k] = v;
+    most = fmaxf(most, v);
+    odd = odd || v != v;
+  }
+  most = group_max(odd ? INFINITY : most, t.red);  // (a NaN ends as NaN: inf - inf)
+  if (most == -INFINITY) return false;
+  mc = most * s.c;
+  float sum = 0.f;
+  for (int k = threadIdx.x; k < s.n_top; k += kLogitsThreads) sum += __builtin_amdgcn_exp2f(fmaf(t.p[k], s.c, -mc));
+  sum = group_sum(sum, t.red);
+  total = __builtin_amdgcn_logf(sum);
+  return true;
+}
+// The row's loss, and the teacher's logits in t.p become probabilities.  a, stotal: the student's.
+__device__ __forceinline__ float stored_loss(const LogitsArgs& s, Stored& t, float mc, float total, const LogitsSums& a, float stotal) {
+  float loss = 0.f;
+  const float inv = __builtin_amdgcn_exp2f(-total);
+  for (int k = threadIdx.x; k < s.n_top; k += kLogitsThreads) {
+    const float d = fmaf(t.p[k], s.c, -mc), p = __builtin_amdgcn_exp2f(d) * inv;
+    if (!(p == 0.f)) loss = fmaf(p, (d - total) - (a.of(t.x[k], s.c) - stotal), loss);
+    t.p[k] = p;
+  }
+  return kLn2 * group_sum(loss, t.red);
+}
+
+// FIRST: the sums of a split and the student's logits at the teacher's places in it.  Else the loss and the gradient, of rows that
+// are one workgroup's (splits == 1, which reads the row for its sums too) or of a split.
+template <class E, bool FIRST>
+__global__ __launch_bounds__(kLogitsThreads) void distill_kernel(LogitsArgs s) {
+  constexpr int B = logits_batch<E>();
+  __shared__ float4 sums[kLogitsWaves];
+  __shared__ Stored t;
+  const LogitsTable table = LOGITS_TABLE(s);
+  const int64_t row = blockIdx.x / (uint32_t)s.splits;
+  const int split = blockIdx.x % (uint32_t)s.splits, tid = threadIdx.x;
+  float weight = s.weight ? s.weight[row] : 1.f, mc = 0.f, total = 0.f;
+  LogitsSums a;
+  bool any = false;
+  if (FIRST) {
+    const int lo = split * s.per, hi = lo + s.per;
+    for (int k = tid; k < s.n_top; k += kLogitsThreads) {
+      const int id = s.stored_ids[row * s.n_top + k];
+      if (id < 0 || id >= s.n_v) continue;
+      const LogitsPart p = logits_part(s, logits_worker_of(s, id));
+      const int v = p.vec0 + (id - p.first) / 8;
+      if (v >= lo && v < hi) s.stored_x[row * s.n_top + k] = logits_at<E>(s, table, row, id);
+    }
+  } else {
+    any = stored_load(s, row, t, mc, total);
+    if (!any) weight = 0.f;
+    if (any)
+      for (int k = tid; k < s.n_top; k += kLogitsThreads)
+        t.x[k] = t.id[k] < 0 ? 0.f : s.splits > 1 ? s.stored_x[row * s.n_top + k] : logits_at<E>(s, table, row, t.id[k]);
+  }
+  const bool sum_here = FIRST || s.splits == 1;
+  if (sum_here && (FIRST || any)) {
+    logits_each<B, kLogitsThreads>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
+      const E* const x = (const E*)table[j].x + row * p.n;
+      LogitsVector<E> v[B];
+      float f[B * 8], all = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < B; ++b) v[b].load(x, p.n, base + b * kLogitsThreads + tid, to);
+      const bool edge = base + B * kLogitsThreads >= to;  // (a last vector, or none)
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
+        v[b].values(f + 8 * b, p.n, edge);
+        all = fmaxf(all, max8(f + 8 * b));
+      }
+      logits_add<B * 8, false>(a, f, all, s.c);
+    });
+    a.join_waves<kLogitsWaves>(sums, s.c);
+  }
+  if (FIRST) {
+    if (tid == 0) s.parts[blockIdx.x] = make_float4(a.m, a.mc, a.s, 0.f);
+    return;
+  }
+  if (any && !sum_here) a = logits_joined(s, row, sums);
+  const float stotal = __builtin_amdgcn_logf(a.s);
+  if (any && a.none()) {  // no entry that the student could answer with: an infinite loss, and nothing to follow
+    if (tid == 0 && split == 0 && s.loss) s.loss[row] = INFINITY;
+    weight = 0.f;
+  } else if (any) {
+    const float loss = stored_loss(s, t, mc, total, a, stotal);
+    if (tid == 0 && split == 0 && s.loss) s.loss[row] = loss;
+  } else if (tid == 0 && split == 0 && s.loss) {
+    s.loss[row] = 0.f;
+  }
+  if (!table[0].dx) return;
+  const float scale = weight * s.inv_t, off = a.mc + stotal;
+  const bool far = a.far();
+  const bool nothing = weight == 0.f;  // such rows are not read
+  __syncthreads();
+  logits_each<B, kLogitsThreads>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
+    const E* const x = (const E*)table[j].x + row * p.n;
+    E* const dx = (E*)table[j].dx + row * p.n;
+    LogitsVector<E> v[B];
+    const bool edge = base + B * kLogitsThreads >= to;  // (a last vector, or none)
+    if (!nothing) {
+#pragma unroll
+      for (int b = 0; b < B; ++b) v[b].load(x, p.n, base + b * kLogitsThreads + tid, to);
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      float f[8] = {};
+      const int i0 = base + b * kLogitsThreads + tid;
+      const int at = max(0, min(8 * i0, p.n - 8)), from = i0 < to ? 8 * i0 - at : 8;
+      if (!nothing) {
+        v[b].values(f, p.n, edge);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = scale * __builtin_amdgcn_exp2f(far ? a.of(f[i], s.c) - stotal : fmaf(f[i], s.c, -off));
+      }
+      logits_store(dx, f, at, from, p.n, edge);
+    }
+  });
+  if (nothing) return;
+  __syncthreads();  // the teacher's places are written once more, behind the stores above
+  const int lo = split * s.per, hi = lo + s.per;
+  for (int k = tid; k < s.n_top; k += kLogitsThreads) {
+    const int id = t.id[k];
+    if (id < 0) continue;
+    const int j = logits_worker_of(s, id);
+    const LogitsPart p = logits_part(s, j);
+    const int v = p.vec0 + (id - p.first) / 8;
+    if (v < lo || v >= hi) continue;
+    bool is_first = true;
+    float sum = 0.f;
+    for (int i = 0; i < s.n_top; ++i) {  // (a place that is stored twice has the sum, and its first one writes it)
+      const bool same = t.id[i] == id;
+      sum += same ? t.p[i] : 0.f;
+      if (same && i < k) is_first = false;
+    }
+    if (is_first) st((E*)table[j].dx, (size_t)(row * p.n + (id - p.first)), scale * (__builtin_amdgcn_exp2f(a.of(t.x[k], s.c) - stotal) - sum));
+  }
+}
+
+}  // namespace distdl
+
+struct distdl_logits_plan {
+  int64_t rows = 0;
+  int32_t n_v = 0;
+  int P = 1;
+  distdl_dtype dtype = DISTDL_F32;
+  distdl::DevArray<distdl::LogitsWorker> table;
+  distdl::StreamScratch scratch;
+};
+
+namespace distdl {
+
+// Workgroups of a row.  A row is one workgroup's where rows fill the card; else it is cut, down to two batches of a workgroup.
+static int logits_splits(int64_t rows, int vecs, int batch) {
+  const int64_t wanted = (1024 + rows - 1) / rows, most = std::max(1, vecs / (2 * batch * kLogitsThreads));
+  return rows >= 512 ? 1 : (int)std::min(wanted, most);
+}
+
+static int logits_args(distdl_logits_plan* p, const void* const x_dev[], void* const dx_dev[], double temperature, hipStream_t st, LogitsArgs* s) {
+  if (!(temperature >= 1e-6 && temperature <= 1e6)) return set_error(DISTDL_ERR_INVALID_ARG, "logits: temperature %g", temperature);
+  const size_t size = dtype_size(p->dtype);
+  std::vector<LogitsWorker> w((size_t)p->P);
+  for (int j = 0; j < p->P; ++j) {
+    if (!x_dev[j] || (dx_dev && !dx_dev[j])) return set_error(DISTDL_ERR_NULL, "logits: %s[%d] is null", x_dev[j] ? "dx" : "x", j);
+    if ((uintptr_t)x_dev[j] % size || (dx_dev && (uintptr_t)dx_dev[j] % size))
+      return set_error(DISTDL_ERR_INVALID_ARG, "logits: an array of worker %d is not aligned to its elements", j);
+    w[j] = LogitsWorker{x_dev[j], dx_dev ? dx_dev[j] : nullptr};
+  }
+  *s = LogitsArgs{};
+  if (p->P <= kLogitsInline) {
+    std::copy(w.begin(), w.end(), s->w);
+  } else {
+    const int rc = p->table.upload(w, st);
+    if (rc) return rc;
+    s->more = p->table.dev;
+  }
+  s->rows = p->rows;
+  s->n_v = p->n_v;
+  s->P = p->P;
+  s->part = p->n_v / p->P;
+  s->extra = p->n_v % p->P;
+  s->vec_rest = (s->part + 7) / 8;
+  s->vec_wide = (s->part + 8) / 8;
+  s->c = (float)(1.4426950408889634 / temperature);
+  s->inv_t = (float)(1.0 / temperature);
+  const int vecs = s->extra * s->vec_wide + (s->P - s->extra) * s->vec_rest;
+  s->splits = logits_splits(p->rows, vecs, size == 2 ? logits_batch<uint16_t>() : logits_batch<float>());
+  s->per = (vecs + s->splits - 1) / s->splits;
+  return DISTDL_OK;
+}
+
+// floats of scratch on this stream; a plan's first call there cannot be a recorded one
+static int logits_scratch(distdl_logits_plan* p, size_t floats, hipStream_t st, float** out) {
+  bool is_new = true;
+  for (const StreamScratch::Block& b : p->scratch.blocks) is_new = is_new && (b.stream != st || b.floats < floats);
+  if (is_new) {
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    DISTDL_HIP_TRY(hipStreamIsCapturing(st, &capture));
+    if (capture != hipStreamCaptureStatusNone)
+      return set_error(DISTDL_ERR_INVALID_ARG, "logits: the plan's first such call on this stream, which is being captured");
+  }
+  return p->scratch.get(floats, st, out);
+}
+
+static int logits_aligned(const char* call, std::initializer_list<const void*> all) {
+  for (const void* v : all)
+    if ((uintptr_t)v % 4) return set_error(DISTDL_ERR_INVALID_ARG, "%s: an array of the rows is not aligned to its elements", call);
+  return DISTDL_OK;
+}
+
+template <class E, bool ENTROPY>
+static void launch_logits_fwd(const LogitsArgs& s, hipStream_t st) {
+  const dim3 grid((unsigned)(s.rows * s.splits)), block(kLogitsThreads);
+  if (s.n_top > 0) hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, true>), grid, block, 0, st, s);
+  else hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, false>), grid, block, 0, st, s);
+  if (s.splits > 1) hipLaunchKernelGGL((logits_join_kernel<E>), dim3((unsigned)s.rows), block, 0, st, s);
+}
+
+template <class E>
+static void launch_distill(const LogitsArgs& s, hipStream_t st) {
+  const dim3 grid((unsigned)(s.rows * s.splits)), block(kLogitsThreads);
+  if (s.splits > 1) hipLaunchKernelGGL((distill_kernel<E, true>), grid, block, 0, st, s);
+  hipLaunchKernelGGL((distill_kernel<E, false>), grid, block, 0, st, s);
+}
+
+}  // namespace distdl
+
+using namespace distdl;
+
+extern "C" {
+
+int distdl_logits_plan_create(distdl_logits_plan** out, int64_t rows, int64_t n_v, int P, distdl_dtype dtype) {
+  if (!out) return set_error(DISTDL_ERR_NULL, "logits_plan_create: null argument");
+  *out = nullptr;
+  if (rows < 0 || n_v < 1 || P < 1) return set_error(DISTDL_ERR_INVALID_ARG, "logits_plan_create: %lld rows of %lld entries on %d workers",
+                                                     (long long)rows, (long long)n_v, P);
+  if (dtype != DISTDL_F32 && dtype != DISTDL_BF16) return set_error(DISTDL_ERR_UNSUPPORTED, "unknown dtype");
+  if (n_v < P) return set_error(DISTDL_ERR_EMPTY_PARTITION, "logits: %lld entries over %d workers", (long long)n_v, P);
+  if (n_v > 1 << 28 || rows >= kMaxBlocks256 || P > 1 << 12) return set_error(DISTDL_ERR_UNSUPPORTED, "logits: problem too large");
+  return guarded([&]() -> int {
+    std::unique_ptr<distdl_logits_plan> p(new distdl_logits_plan());
+    p->rows = rows;
+    p->n_v = (int32_t)n_v;
+    p->P = P;
+    p->dtype = dtype;
+    *out = p.release();
+    return DISTDL_OK;
+  });
+}
+
+int distdl_logits_plan_destroy(distdl_logits_plan* p) {
+  if (!p) return DISTDL_OK;
+  p->table.release();
+  p->scratch.release();
+  delete p;
+  return DISTDL_OK;
+}
+
+int distdl_logprob_fwd(distdl_logits_plan* p, const void* const x_dev[], const int32_t* targets_dev, float* logp_dev, float* lse_dev,
+                       float* entropy_dev, int32_t* top_ids_dev, float* top_logp_dev, int n_top, double temperature, void* stream) {
+  if (!p || !x_dev) return set_error(DISTDL_ERR_NULL, "logprob_fwd: null argument");
+  if (n_top < 0 || n_top > p->n_v) return set_error(DISTDL_ERR_INVALID_ARG, "logprob_fwd: %d alternatives of %d entries", n_top, p->n_v);
+  if (n_top > kTopMost) return set_error(DISTDL_ERR_UNSUPPORTED, "logprob_fwd: more than %d alternatives", kTopMost);
+  if (p->rows == 0) return DISTDL_OK;
+  if (logp_dev && !targets_dev) return set_error(DISTDL_ERR_NULL, "logprob_fwd: log probabilities without targets");
+  if (n_top > 0 && !top_ids_dev && !top_logp_dev) return set_error(DISTDL_ERR_NULL, "logprob_fwd: alternatives without a place for them");
+  if (n_top == 0 && (top_ids_dev || top_logp_dev)) return set_error(DISTDL_ERR_INVALID_ARG, "logprob_fwd: a place for no alternatives");
+  if (!logp_dev && !lse_dev && !entropy_dev && n_top == 0) return set_error(DISTDL_ERR_NULL, "logprob_fwd: no output");
+  return guarded([&]() -> int {
+    hipStream_t st_ = (hipStream_t)stream;
+    LogitsArgs s;
+    int rc;
+    if ((rc = logits_aligned("logprob_fwd", {targets_dev, logp_dev, lse_dev, entropy_dev, top_ids_dev, top_logp_dev}))) return rc;
+    if ((rc = logits_args(p, x_dev, nullptr, temperature, st_, &s))) return rc;
+    s.targets = targets_dev;
+    s.logp = logp_dev;
+    s.lse = lse_dev;
+    s.entropy = entropy_dev;
+    s.n_top = n_top;
+    s.ids = top_ids_dev;
+    s.top = top_logp_dev;
+    if (s.splits > 1) {
+      const size_t blocks = (size_t)p->rows * s.splits;
+      float* at = nullptr;
+      if ((rc = logits_scratch(p, blocks * (4 + 2 * (size_t)n_top), st_, &at))) return rc;
+      s.parts = (float4*)at;
+      s.part_top = (uint64_t*)(at + blocks * 4);
+    }
+    {
+      ProfScope prof("logprob_fwd", st_);
+      if (p->dtype == DISTDL_F32) entropy_dev ? launch_logits_fwd<float, true>(s, st_) : launch_logits_fwd<float, false>(s, st_);
+      else entropy_dev ? launch_logits_fwd<uint16_t, true>(s, st_) : launch_logits_fwd<uint16_t, false>(s, st_);
+    }
+    DISTDL_HIP_TRY(hipGetLastError());
+    return DISTDL_OK;
+  });
+}
+
+int distdl_logprob_bwd(distdl_logits_plan* p, const void* const x_dev[], const int32_t* targets_dev, const float* lse_dev,
+                       const float* entropy_dev, const float* dlogp_dev, const float* dentropy_dev, void* const dx_dev[], double temperature,
+                       void* stream) {
+  if (!p || !x_dev || !dx_dev) return set_error(DISTDL_ERR_NULL, "logprob_bwd: null argument");
+  if (p->rows == 0) return DISTDL_OK;
+  if (!lse_dev || (!dlogp_dev && !dentropy_dev)) return set_error(DISTDL_ERR_NULL, "logprob_bwd: no lse, or no gradient");
+  if (dlogp_dev && !targets_dev) return set_error(DISTDL_ERR_NULL, "logprob_bwd: gradients of log probabilities without targets");
+  if (dentropy_dev && !entropy_dev) return set_error(DISTDL_ERR_NULL, "logprob_bwd: the entropy's gradient without the entropy");
+  return guarded([&]() -> int {
+    hipStream_t st_ = (hipStream_t)stream;
+    LogitsArgs s;
+    int rc;
+    if ((rc = logits_aligned("logprob_bwd", {targets_dev, lse_dev, entropy_dev, dlogp_dev, dentropy_dev}))) return rc;
+    if ((rc = logits_args(p, x_dev, dx_dev, temperature, st_, &s))) return rc;
+    s.targets = dlogp_dev ? targets_dev : nullptr;
+    s.lse = const_cast<float*>(lse_dev);
+    s.entropy = const_cast<float*>(entropy_dev);
+    s.dlogp = dlogp_dev;
+    s.dentropy = dentropy_dev;
+    {
+      ProfScope prof("logprob_bwd", st_);
+      const dim3 grid((unsigned)(s.rows * s.splits)), block(kLogitsThreads);
+      if (p->dtype == DISTDL_F32) {
+        if (dentropy_dev) hipLaunchKernelGGL((logits_bwd_kernel<float, true>), grid, block, 0, st_, s);
+        else hipLaunchKernelGGL((logits_bwd_kernel<float, false>), grid, block, 0, st_, s);
+      } else {
+        if (dentropy_dev) hipLaunchKernelGGL((logits_bwd_kernel<uint16_t, true>), grid, block, 0, st_, s);
+        else hipLaunchKernelGGL((logits_bwd_kernel<uint16_t, false>), grid, block, 0, st_, s);
+      }
+    }
+    DISTDL_HIP_TRY(hipGetLastError());
+    return DISTDL_OK;
+  });
+}
+
+int distdl_distill_fwd_bwd(distdl_logits_plan* p, const void* const x_dev[], const int32_t* ids_dev, const float* teacher_dev, int n_top,
+                           const float* weight_dev, float* loss_dev, void* const dx_dev[], double temperature, void* stream) {
+  if (!p || !x_dev) return set_error(DISTDL_ERR_NULL, "distill: null argument");
+  if (n_top < 1) return set_error(DISTDL_ERR_INVALID_ARG, "distill: %d teacher logits a row", n_top);
+  if (n_top > kStoredMost) return set_error(DISTDL_ERR_UNSUPPORTED, "distill: more than %d teacher logits a row", kStoredMost);
+  if (p->rows == 0) return DISTDL_OK;
+  if (!ids_dev || !teacher_dev || (!loss_dev && !dx_dev)) return set_error(DISTDL_ERR_NULL, "distill: no teacher, or no output");
+  return guarded([&]() -> int {
+    hipStream_t st_ = (hipStream_t)stream;
+    LogitsArgs s;
+    int rc;
+    if ((rc = logits_aligned("distill", {ids_dev, teacher_dev, weight_dev, loss_dev}))) return rc;
+    if ((rc = logits_args(p, x_dev, dx_dev, temperature, st_, &s))) return rc;
+    s.stored_ids = ids_dev;
+    s.stored = teacher_dev;
+    s.n_top = n_top;
+    s.weight = weight_dev;
+    s.loss = loss_dev;
+    if (s.splits > 1) {
+      const size_t blocks = (size_t)p->rows * s.splits;
+      float* at = nullptr;
+      if ((rc = logits_scratch(p, blocks * 4 + (size_t)p->rows * n_top, st_, &at))) return rc;
+      s.parts = (float4*)at;
+      s.stored_x = at + blocks * 4;
+    }
+    {
+      ProfScope prof("distill", st_);
+      if (p->dtype == DISTDL_F32) launch_distill<float>(s, st_);
+      else launch_distill<uint16_t>(s, st_);
+    }
+    DISTDL_HIP_TRY(hipGetLastError());
+    return DISTDL_OK;
+  });
+}
+
+}  // extern "C"
