@@ -522,6 +522,52 @@ int distdl_scan_step(const void* a_dev, const void* x_dev, float* state_dev, int
                      const int32_t* slots_dev, void* h_dev, int64_t rows, int64_t n_c, distdl_gate gate,
                      distdl_dtype dtype, void* stream);
 
+/* Gated delta rule over T steps that P workers share: a recurrence whose state
+ * S is a matrix [d_k][d_v] (fp32) for each of n_h heads.
+ *   u_t = beta_t (v_t - a_t S_{t-1}^T k_t),  a_t = exp(g_t)
+ *   S_t = a_t S_{t-1} + k_t u_t^T,  o_t = scale S_t^T q_t
+ * A worker's q and k are [n_b][T_p][n_hk][d_k], v and o [n_b][T_p][n_h][d_v] of
+ * the plan's dtype, g (the logarithm of the factor; NULL: 0) and beta
+ * [n_b][T_p][n_h] fp32; states are [n_b][n_h][d_k][d_v].  n_hk divides n_h:
+ * heads h n_h / n_hk and those behind it share key and query head h.
+ * fwd: o of all steps and, if not NULL, the last states hT.  h0 NULL: zeros.
+ *   lengths [n_b] (int32, NULL: all T; values are cut to 0 .. T): steps from a
+ *   sequence's length on are not read, their o is 0, and hT is the state at
+ *   its end.
+ * bwd: from the inputs of fwd, d_o and dhT (NULL: zeros): dq and dk (summed
+ *   over the heads that share them), dv, dbeta and, if not NULL, dg and dh0.
+ *   Steps from a sequence's length on get zeros.  The states are made again.
+ * step: one token for each row, q and k [rows][n_hk][d_k], v and o
+ *   [rows][n_h][d_v], g and beta [rows][n_h]: the states of
+ *   state_dev[slots[row]], [n_slots][n_h][d_k][d_v], are read and overwritten.
+ *   slots NULL: row i has state i.  A row whose slot is not in
+ *   0 .. n_slots - 1 is idle: its o is 0 and no state changes.  Slots of one
+ *   call must differ.
+ * Outputs must not overlap inputs.  A factor below exp(-200) is 0.  The
+ * numbers between (states, what a step adds) have 24 bits in every product;
+ * of what bf16 tensors alone depend on, 16.
+ * fwd and bwd keep what chunks of steps need in the plan's scratch, bwd two
+ * states for each 64 steps (32 with fp32 tensors): calls and recorded graphs
+ * of one plan and stream share it, they run one after another.
+ * UNSUPPORTED: d_k from 129 on, n_h d_v from 2^22 on. */
+typedef struct distdl_delta_plan distdl_delta_plan;
+int distdl_delta_plan_create(distdl_delta_plan** out, int64_t n_b, int64_t T, int64_t n_h, int64_t n_hk, int64_t d_k,
+                             int64_t d_v, int P, double scale, distdl_dtype dtype);
+int distdl_delta_plan_destroy(distdl_delta_plan* plan);
+int distdl_delta_fwd(distdl_delta_plan* plan, const void* const q_dev[], const void* const k_dev[],
+                     const void* const v_dev[], const float* const g_dev[], const float* const beta_dev[],
+                     const float* h0_dev, const int32_t* lengths_dev, void* const o_dev[], float* hT_dev,
+                     void* stream);
+int distdl_delta_bwd(distdl_delta_plan* plan, const void* const q_dev[], const void* const k_dev[],
+                     const void* const v_dev[], const float* const g_dev[], const float* const beta_dev[],
+                     const float* h0_dev, const int32_t* lengths_dev, const void* const do_dev[],
+                     const float* dhT_dev, void* const dq_dev[], void* const dk_dev[], void* const dv_dev[],
+                     float* const dg_dev[], float* const dbeta_dev[], float* dh0_dev, void* stream);
+int distdl_delta_step(const void* q_dev, const void* k_dev, const void* v_dev, const float* g_dev,
+                      const float* beta_dev, float* state_dev, int64_t n_slots, const int32_t* slots_dev,
+                      void* o_dev, int64_t rows, int64_t n_h, int64_t n_hk, int64_t d_k, int64_t d_v, double scale,
+                      distdl_dtype dtype, void* stream);
+
 /* AdamW over many arrays at once: count[i] weights p (fp32) each, gradients g
  * of g_dtype, first and second moments, in one launch.
  *   g' = g * *gscale_dev (NULL: 1);  m = beta1 m + (1 - beta1) g';

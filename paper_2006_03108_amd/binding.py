@@ -99,6 +99,11 @@ _SIGS = {
     "distdl_adamw_plan_create": [C.POINTER(_vp), _p64, _i, _i, _i],
     "distdl_adamw_plan_destroy": [_vp],
     "distdl_adamw_step": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp],
+    "distdl_delta_plan_create": [C.POINTER(_vp), _i64, _i64, _i64, _i64, _i64, _i64, _i, C.c_double, _i],
+    "distdl_delta_plan_destroy": [_vp],
+    "distdl_delta_fwd": [_vp] * 11,
+    "distdl_delta_bwd": [_vp] * 17,
+    "distdl_delta_step": [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _i64, C.c_double, _i, _vp],
     "distdl_logits_plan_create": [C.POINTER(_vp), _i64, _i64, _i, _i],
     "distdl_logits_plan_destroy": [_vp],
     "distdl_logprob_fwd": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, C.c_double, _vp],
@@ -683,6 +688,50 @@ def distdl_adamw_step(plan, p, g, m, v, ms=None, vs=None, p16=None, *, lr, beta1
                                  _many("v", v, plan.state_kind, n), _many("ms", ms, _SCALES, plan.blocks) if scales else None,
                                  _many("vs", vs, _SCALES, plan.blocks) if scales else None, _many("p16", p16, (torch.bfloat16,), n),
                                  C.byref(args), _stream()))
+
+
+# ---- gated delta rule -------------------------------------------------------
+
+def distdl_delta_plan_create(n_b, T, n_h, n_hk, d_k, d_v, P, scale, dtype=torch.bfloat16):
+    """n_h heads of values and states, n_hk heads of queries and keys; scale: of the outputs."""
+    h = C.c_void_p()
+    _check(lib.distdl_delta_plan_create(C.byref(h), n_b, T, n_h, n_hk, d_k, d_v, P, scale, _dtype_code(dtype)))
+    kind, rows = _F32 if _dtype_code(dtype) == DISTDL_F32 else (torch.bfloat16,), [n_b * t for t in _split(T, P)]
+    return _Handle(h, lib.distdl_delta_plan_destroy, kind=kind, nk=[n * n_hk * d_k for n in rows], nv=[n * n_h * d_v for n in rows],
+                   ng=[n * n_h for n in rows], state=n_b * n_h * d_k * d_v, n_b=n_b)
+
+
+def _delta_inputs(plan, q, k, v, g, beta, h0, lengths):
+    return (plan.handle, _many("q", q, plan.kind, plan.nk), _many("k", k, plan.kind, plan.nk), _many("v", v, plan.kind, plan.nv),
+            _many("g", g, _F32, plan.ng), _many("beta", beta, _F32, plan.ng), _maybe("h0", h0, _F32, plan.state),
+            _maybe("lengths", lengths, _I32, plan.n_b))
+
+
+def distdl_delta_fwd(plan, q, k, v, g, beta, h0, lengths, o, hT):
+    """g (no decay), h0, lengths and hT may be None."""
+    _check(lib.distdl_delta_fwd(*_delta_inputs(plan, q, k, v, g, beta, h0, lengths), _many("o", o, plan.kind, plan.nv),
+                                _maybe("hT", hT, _F32, plan.state), _stream()))
+
+
+def distdl_delta_bwd(plan, q, k, v, g, beta, h0, lengths, do, dhT, dq, dk, dv, dg, dbeta, dh0):
+    """g, h0, lengths, dhT, dg and dh0 may be None."""
+    _check(lib.distdl_delta_bwd(*_delta_inputs(plan, q, k, v, g, beta, h0, lengths), _many("do", do, plan.kind, plan.nv),
+                                _maybe("dhT", dhT, _F32, plan.state), _many("dq", dq, plan.kind, plan.nk), _many("dk", dk, plan.kind, plan.nk),
+                                _many("dv", dv, plan.kind, plan.nv), _many("dg", dg, _F32, plan.ng), _many("dbeta", dbeta, _F32, plan.ng),
+                                _maybe("dh0", dh0, _F32, plan.state), _stream()))
+
+
+def distdl_delta_step(q, k, v, g, beta, state, slots, o, scale):
+    """q, k: [rows, n_hk, d_k], v, o: [rows, n_h, d_v]; g (or None), beta: fp32 [rows, n_h]; state: fp32 [n_slots, n_h, d_k, d_v]; slots: int32
+    [rows], or None for state i of row i."""
+    if q.dim() != 3 or v.dim() != 3 or state.dim() != 4 or q.shape[0] != v.shape[0] or state.shape[1:] != (v.shape[1], q.shape[2], v.shape[2]):
+        raise DistdlError(ERR_INVALID_ARG, f"delta_step: queries of shape {tuple(q.shape)}, values of shape {tuple(v.shape)}, "
+                                           f"states of shape {tuple(state.shape)}")
+    (rows, n_hk, d_k), (_, n_h, d_v), kind = q.shape, v.shape, (q.dtype,)
+    _check(lib.distdl_delta_step(_one("q", q, kind, q.numel()), _one("k", k, kind, q.numel()), _one("v", v, kind, v.numel()),
+                                 _maybe("g", g, _F32, rows * n_h), _one("beta", beta, _F32, rows * n_h), _one("state", state, _F32, state.numel()),
+                                 state.shape[0], _maybe("slots", slots, _I32, rows), _one("o", o, kind, v.numel()), rows, n_h, n_hk, d_k, d_v, scale,
+                                 _dtype_code(q.dtype), _stream()))
 
 
 # ---- logits ----------------------------------------------------------------

@@ -1,0 +1,1279 @@
+// The gated delta rule over time that P workers share, its adjoint, and the step of single tokens.
+//
+//   u_t = beta_t (v_t - a_t S_{t-1}^T k_t),  S_t = a_t S_{t-1} + k_t u_t^T,  o_t = scale S_t^T q_t,  a_t = exp(g_t)
+//
+// A state S [d_k][d_v] is changed by each step in a direction of its own, so steps do not compose as those of an elementwise
+// recurrence do.  But what the C steps of a chunk do to each other is triangular.  With G_i the sum of g over the chunk's steps up to i and
+// D_ij = exp(G_i - G_j), S the state in front of the chunk:
+//   A = strictly lower (beta_i D_ij k_i k_j),  T = (1 + A)^-1,  P = lower (scale D_ij q_i k_j)
+//   X = V - exp(G) (K S),  U = T (beta X),  O = scale exp(G) (Q S) + P U,  S' = exp(G_C) S + K^T (exp(G_C - G) U)
+// A, T and P need no state: one launch makes them for all chunks (delta_prepare_kernel).  What is left goes through time, and its columns
+// (of d_v) are independent: a wave has 16 or 32 columns of a head's state in its registers and goes through all chunks, from product to
+// product without LDS or barriers (delta.h).  Differences of G are exact: sums in 64 bits, kept as a multiple of 1/64 and the rest.
+#include <algorithm>
+#include <cmath>
+
+#include "delta.h"
+#include "profile.h"
+
+namespace distdl {
+
+template <class E>
+constexpr int delta_chunk_steps() { return sizeof(E) == 2 ? 64 : 32; }  // (three pieces of every operand would not fit in LDS)
+
+// A factor of exp(-200) is 0 in 32 bits, and so is what it stands between.
+__device__ __forceinline__ float bounded(float g) { return g < -200.f ? -200.f : g; }
+
+// ---- a chunk's own matrices -----------------------------------------------
+template <class E, int C, int DK>
+struct DeltaPrepareShared {
+  static constexpr int kRow = DK + 8, kLine = C + 4;
+  union {
+    uint16_t rows[2][delta_pieces<E>()][C][kRow];  // K, Q
+    float inner[2][C][kLine];                      // K K^T, Q K^T
+  };
+  float a[C][kLine], t[C][kLine];
+  float whole[C], rest[C], beta[C];  // G = whole + rest
+};
+
+// (1 + a)^-1 of a strictly lower matrix in `a`, into `t`, zeros above the diagonal.  Blocks of 16 on the diagonal by substitution, a
+// column to a lane; block (i, j) is -T_ii sum_k A_ik T_kj, by distance from the diagonal, in fp32 products.
+template <int C, int LINE>
+__device__ __forceinline__ void delta_inverse(const float (*a)[LINE], float (*t)[LINE]) {
+  constexpr int N = C / 16;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+  if (wave < N) {
+    const int at = wave * 16;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float v = i == col ? 1.f : 0.f;
+#pragma unroll
+      for (int j = 0; j < i; ++j) v = fmaf(-a[at + i][at + j], x[j], v);
+      x[i] = v;
+    }
+    if (g == 0) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) t[at + i][at + col] = x[i];
+    }
+  }
+  for (int d = 1; d < N; ++d) {
+    __syncthreads();
+    const int i = wave + d, j = wave;
+    if (i < N) {
+      f32x4 sum = {};
+      for (int k = j; k < i; ++k) {
+        const f32x4 left = *(const f32x4*)&a[i * 16 + col][k * 16 + 4 * g];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(left[r], t[k * 16 + 4 * g + r][j * 16 + col], sum, 0, 0, 0);
+      }
+      f32x4 out = {};
+      const f32x4 left = *(const f32x4*)&t[i * 16 + col][i * 16 + 4 * g];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) out = __builtin_amdgcn_mfma_f32_16x16x4f32(left[r], -sum[r], out, 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        t[i * 16 + 4 * g + r][j * 16 + col] = out[r];
+        t[j * 16 + 4 * g + r][i * 16 + col] = 0.f;
+      }
+    }
+  }
+  __syncthreads();
+}
+
+// The places along a fragment's sum that a lane has: element e of step ks.
+__device__ __forceinline__ int delta_place(int ks, int e) { return 32 * ks + (e >> 2) * 16 + 4 * ((threadIdx.x & 63) >> 4) + (e & 3); }
+
+template <class E, int C, int DK, bool BACK>
+__global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs s) {
+  typedef DeltaSizes<C, DK> Z;
+  typedef DeltaPrepareShared<E, C, DK> Shared;
+  constexpr int NI = delta_pieces<E>();
+  extern __shared__ char delta_lds[];
+  Shared& m = *(Shared*)delta_lds;
+  const DeltaTable table = DELTA_TABLE(s);
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, row = lane & 15, g = lane >> 4;
+  const int hk = blockIdx.x % (uint32_t)s.n_hk, at_chunk = blockIdx.x / (uint32_t)s.n_hk;
+  const int c = at_chunk % s.chunks, b = at_chunk / s.chunks;
+  const DeltaChunk at = delta_chunk<C>(s, b, c);
+  if (at.live == 0) return;  // nobody reads what would be here
+  const int64_t step0 = (int64_t)b * at.steps + at.first;  // of the worker's arrays
+  const DeltaTable w = table + at.p;
+
+  // rows of K and Q, zeros behind the end of the sequence and of the row
+  for (int i = tid; i < 2 * C * (DK / 8); i += 256) {
+    const int what = i / (C * (DK / 8)), t = i / (DK / 8) % C, col = i % (DK / 8) * 8;
+    const E* const from = (const E*)(what ? w->q : w->k) + ((step0 + t) * s.n_hk + hk) * s.d_k + col;
+    Eight<E> raw;
+    raw.load(from, t < at.live ? min(8, s.d_k - col) : 0);
+    if constexpr (NI == 1) {
+      *(u32x4*)&m.rows[what][0][t][col] = raw.a;
+    } else {
+      float v[8];
+      raw.values(v);
+      const Pieces<3> p = split8(v);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) *(u32x4*)&m.rows[what][k][t][col] = p.p[k];
+    }
+  }
+  __syncthreads();
+
+  // their fragments
+  const int64_t key = ((int64_t)b * s.chunks + c) * s.n_hk + hk, key_at = key * Z::kKeyPiece * NI;
+  for (int f = wave; f < 2 * Z::kTiles * Z::kKeySteps; f += 4) {
+    const int what = f / (Z::kTiles * Z::kKeySteps), i = f % (Z::kTiles * Z::kKeySteps), mt = i / Z::kKeySteps, ks = i % Z::kKeySteps;
+    Pieces<NI> v;
+#pragma unroll
+    for (int k = 0; k < NI; ++k) {
+      const uint16_t* const r = &m.rows[what][k][mt * 16 + row][32 * ks + 4 * g];
+      const u32x2 lo = *(const u32x2*)r, hi = *(const u32x2*)(r + 16);
+      v.p[k] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+    }
+    store_fragment((what ? s.qf : s.kf) + key_at + (int64_t)i * NI * kFragment, v);
+  }
+  for (int f = wave; f < (BACK ? 2 : 1) * Z::kKeyTiles * Z::kSteps; f += 4) {
+    const int what = f / (Z::kKeyTiles * Z::kSteps), i = f % (Z::kKeyTiles * Z::kSteps), mt = i / Z::kSteps, ts = i % Z::kSteps;
+    Pieces<NI> v;
+#pragma unroll
+    for (int k = 0; k < NI; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; e += 2)
+        v.p[k][e / 2] = m.rows[what][k][delta_place(ts, e)][mt * 16 + row] | (uint32_t)m.rows[what][k][delta_place(ts, e + 1)][mt * 16 + row] << 16;
+    store_fragment((what ? s.qtf : s.ktf) + key_at + (int64_t)i * NI * kFragment, v);
+  }
+
+  // K K^T and Q K^T, tiles on and below the diagonal
+  constexpr int kLower = Z::kTiles * (Z::kTiles + 1) / 2, kJobs = (2 * kLower + 3) / 4;
+  f32x4 acc[kJobs];
+#pragma unroll
+  for (int i = 0; i < kJobs; ++i) {
+    const int job = wave + 4 * i;
+    acc[i] = f32x4{};
+    if (job < 2 * kLower) {
+      const int what = job / kLower, tile = job % kLower, mt = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, nt = tile - mt * (mt + 1) / 2;
+      for (int ks = 0; ks < Z::kKeySteps; ++ks) {
+        Pieces<NI> left, right;
+#pragma unroll
+        for (int k = 0; k < NI; ++k) {
+          left.p[k] = *(const u32x4*)&m.rows[what][k][mt * 16 + row][32 * ks + 8 * g];
+          right.p[k] = *(const u32x4*)&m.rows[0][k][nt * 16 + row][32 * ks + 8 * g];
+        }
+        acc[i] = multiply(left, right, acc[i]);
+      }
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kJobs; ++i) {
+    const int job = wave + 4 * i;
+    if (job < 2 * kLower) {
+      const int what = job / kLower, tile = job % kLower, mt = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, nt = tile - mt * (mt + 1) / 2;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) m.inner[what][mt * 16 + 4 * g + r][nt * 16 + row] = acc[i][r];
+    }
+  }
+
+  for (int e = 0; e < s.each; ++e) {
+    const int h = hk * s.each + e;
+    const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h;
+    __syncthreads();
+    if (wave == 0) {  // the sums of g
+      const bool live = lane < at.live;
+      const int64_t o = (step0 + lane) * s.n_h + h;
+      double sum = live && w->g ? (double)bounded(w->g[o]) : 0.0;
+#pragma unroll
+      for (int d = 1; d < C; d *= 2) {
+        const double before = __shfl_up(sum, d, 64);
+        if (lane >= d) sum += before;
+      }
+      const double last = __shfl(sum, C - 1, 64);
+      if (lane < C) {
+        const float whole = (float)(rint(sum * 64.0) * (1.0 / 64.0)), beta = live ? w->beta[o] : 0.f;
+        m.whole[lane] = whole;
+        m.rest[lane] = (float)(sum - (double)whole);
+        m.beta[lane] = beta;
+        float* const out = s.steps + head * kStepNumbers * C + lane;
+        out[kSince * C] = expf((float)sum);
+        out[kUntil * C] = expf((float)(last - sum));
+        out[kBeta * C] = beta;
+        out[kWhole * C] = whole;
+        out[kRest * C] = m.rest[lane];
+      }
+    }
+    __syncthreads();
+    auto decay = [&](int i, int j) { return expf((m.whole[i] - m.whole[j]) + (m.rest[i] - m.rest[j])); };
+    for (int i = tid; i < C * C; i += 256) {
+      const int r = i / C, k = i % C;
+      if (k < r) m.a[r][k] = m.beta[r] * decay(r, k) * m.inner[0][r][k];
+      else m.a[r][k] = 0.f;
+    }
+    __syncthreads();
+    delta_inverse<C>(m.a, m.t);
+    // fragments that are not all zeros
+    for (int f = wave; f < Z::kTiles * Z::kSteps; f += 4) {
+      const int mt = f / Z::kSteps, ts = f % Z::kSteps, i = mt * 16 + row;
+      const int64_t o = head * Z::kStepPiece * kInner + (int64_t)f * kInner * kFragment;
+      float v[8];
+      if (ts * 2 <= mt) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] = m.t[i][delta_place(ts, x)];
+        store_fragment(s.tf + o, split8(v));
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const int j = delta_place(ts, x);
+          v[x] = j <= i ? s.scale * decay(i, j) * m.inner[1][i][j] : 0.f;
+        }
+        store_fragment(s.pf + o, split8(v));
+      }
+      if (BACK && mt / 2 <= ts) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] = m.t[delta_place(ts, x)][i];
+        store_fragment(s.ttf + o, split8(v));
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const int j = delta_place(ts, x);
+          v[x] = i <= j ? s.scale * decay(j, i) * m.inner[1][j][i] : 0.f;
+        }
+        store_fragment(s.ptf + o, split8(v));
+      }
+    }
+  }
+}
+
+// ---- through time ---------------------------------------------------------
+// A wave's tile of a worker's rows: step 16 mt + 4 g + r of the chunk, column `col` of the head; nothing outside the live steps and the columns.
+template <class E>
+struct DeltaColumns {
+  __amdgpu_buffer_rsrc_t rows;
+  uint32_t hop;
+  __device__ __forceinline__ DeltaColumns(const void* base, int64_t first, const DeltaArgs& s, int h)
+      : rows(rsrc_of((const E*)base + (first * s.n_h + h) * s.d_v, kOob)), hop((uint32_t)(s.n_h * s.d_v) * (uint32_t)sizeof(E)) {}
+  __device__ __forceinline__ uint32_t offset(int step, int col, bool in) const { return in ? (uint32_t)step * hop + (uint32_t)col * (uint32_t)sizeof(E) : kOob; }
+  __device__ __forceinline__ uint32_t raw(int step, int col, bool in) const {
+    if constexpr (sizeof(E) == 4) return __builtin_amdgcn_raw_buffer_load_b32(rows, offset(step, col, in), 0, 0);
+    else return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rows, offset(step, col, in), 0, 0);
+  }
+  static __device__ __forceinline__ float value(uint32_t raw) { return __uint_as_float(sizeof(E) == 4 ? raw : raw << 16); }
+  __device__ __forceinline__ float load(int step, int col, bool in) const { return value(raw(step, col, in)); }
+  __device__ __forceinline__ void store(int step, int col, bool in, float v) const {
+    if constexpr (sizeof(E) == 4) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), rows, offset(step, col, in), 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16(to_bf16(v), rows, offset(step, col, in), 0, 0);
+  }
+};
+
+struct DeltaChain {  // a wave's sequence, head and first column
+  int b, h, col;
+};
+template <int NT>
+__device__ __forceinline__ DeltaChain delta_chain(const DeltaArgs& s) {
+  const uint32_t i = xcd_order(blockIdx.x, gridDim.x);  // a head's slices share an L2
+  const uint32_t chain = i / (uint32_t)s.slices, slice = i % (uint32_t)s.slices;
+  return DeltaChain{(int)(chain / (uint32_t)s.n_h), (int)(chain % (uint32_t)s.n_h), (int)slice * 16 * NT};
+}
+
+// Pieces of a product whose results the tensors' type rounds to bf16: what lies below 16 bits does not show there.
+template <class E>
+constexpr int delta_rounded() { return sizeof(E) == 2 ? 2 : 3; }
+
+template <class E, int C, int DK, int NT, bool STORE>
+__global__ __launch_bounds__(64, 1) void delta_fwd_kernel(DeltaArgs s) {
+  typedef DeltaSizes<C, DK> Z;
+  constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>();
+  const DeltaTable table = DELTA_TABLE(s);
+  const int lane = threadIdx.x, g = lane >> 4;
+  const DeltaChain chain = delta_chain<NT>(s);
+  const int b = chain.b, h = chain.h, hk = h / s.each, col = chain.col + (lane & 15);
+  f32x4 state[Z::kKeyTiles][NT];
+  const int64_t state_at = ((int64_t)b * s.n_h + h) * s.d_k * s.d_v;
+#pragma unroll
+  for (int i = 0; i < Z::kKeyTiles; ++i)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int k = 16 * i + 4 * g + r, v = col + 16 * n;
+        state[i][n][r] = s.h0 && k < s.d_k && v < s.d_v ? s.h0[state_at + (int64_t)k * s.d_v + v] : 0.f;
+      }
+
+  for (int c = 0; c < s.chunks; ++c) {
+    const DeltaChunk at = delta_chunk<C>(s, b, c);
+    const int64_t step0 = (int64_t)b * at.steps + at.first;
+    const DeltaColumns<E> out(STORE ? nullptr : table[at.p].o, step0, s, h);
+    if (at.live == 0) {
+      if (!STORE) {
+#pragma unroll
+        for (int mt = 0; mt < Z::kTiles; ++mt)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int t = 16 * mt + 4 * g + r;
+              out.store(t, col + 16 * n, t < at.n && col + 16 * n < s.d_v, 0.f);
+            }
+      }
+      continue;
+    }
+    const int64_t key_at = (((int64_t)b * s.chunks + c) * s.n_hk + hk) * Z::kKeyPiece * NI;
+    const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h, step_at = head * Z::kStepPiece * kInner;
+    const uint16_t *const kf = s.kf + key_at, *const qf = s.qf + key_at, *const ktf = s.ktf + key_at, *const tf = s.tf + step_at, *const pf = s.pf + step_at;
+    const float* const steps = s.steps + head * kStepNumbers * C;
+    const DeltaColumns<E> values(table[at.p].v, step0, s, h);
+    uint32_t raw[Z::kTiles][NT][4];
+#pragma unroll
+    for (int mt = 0; mt < Z::kTiles; ++mt)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int t = 16 * mt + 4 * g + r;
+          raw[mt][n][r] = values.raw(t, col + 16 * n, t < at.live && col + 16 * n < s.d_v);
+        }
+    if (STORE) {
+      float* const to = s.states + head * DK * s.dvp;
+#pragma unroll
+      for (int i = 0; i < Z::kKeyTiles; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (col + 16 * n < s.dvp) to[(int64_t)(16 * i + 4 * g + r) * s.dvp + col + 16 * n] = state[i][n][r];
+    }
+    // K S and Q S
+    f32x4 ks[Z::kTiles][NT] = {}, qs[Z::kTiles][NT] = {};
+#pragma unroll
+    for (int k = 0; k < Z::kKeySteps; ++k) {
+      Pieces<3> right[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) right[n] = split_tiles(state[2 * k][n], state[2 * k + 1][n]);
+#pragma unroll
+      for (int mt = 0; mt < Z::kTiles; ++mt) {
+        const Pieces<NI> left = load_fragment<NI>(kf + (mt * Z::kKeySteps + k) * NI * kFragment);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) ks[mt][n] = multiply(left, right[n], ks[mt][n]);
+      }
+      if (!STORE) {
+#pragma unroll
+        for (int mt = 0; mt < Z::kTiles; ++mt) {
+          const Pieces<NI> left = load_fragment<NI>(qf + (mt * Z::kKeySteps + k) * NI * kFragment);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) qs[mt][n] = multiply(left, first_pieces<NO>(right[n]), qs[mt][n]);
+        }
+      }
+    }
+    // X, and beta X
+    f32x4 u[Z::kTiles][NT];
+#pragma unroll
+    for (int mt = 0; mt < Z::kTiles; ++mt) {
+      const f32x4 since = *(const f32x4*)(steps + 16 * mt + 4 * g), beta = *(const f32x4*)(steps + kBeta * C + 16 * mt + 4 * g);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float x = fmaf(-since[r], ks[mt][n][r], DeltaColumns<E>::value(raw[mt][n][r]));
+          ks[mt][n][r] = beta[r] * x;
+          if (STORE && col + 16 * n < s.dvp) s.x[(head * C + 16 * mt + 4 * g + r) * s.dvp + col + 16 * n] = x;
+        }
+    }
+    // U = T (beta X)
+#pragma unroll
+    for (int k = 0; k < Z::kSteps; ++k) {
+      Pieces<3> right[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) right[n] = split_tiles(ks[2 * k][n], ks[2 * k + 1][n]);
+#pragma unroll
+      for (int mt = 2 * k; mt < Z::kTiles; ++mt) {
+        const Pieces<kInner> left = load_fragment<kInner>(tf + (mt * Z::kSteps + k) * kInner * kFragment);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) u[mt][n] = multiply(left, right[n], k == 0 ? f32x4{} : u[mt][n]);
+      }
+    }
+    // O
+    if (!STORE) {
+#pragma unroll
+      for (int mt = 0; mt < Z::kTiles; ++mt) {
+        const f32x4 since = *(const f32x4*)(steps + 16 * mt + 4 * g);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) qs[mt][n] *= since * s.scale;
+      }
+#pragma unroll
+      for (int k = 0; k < Z::kSteps; ++k) {
+        Pieces<NO> right[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) right[n] = first_pieces<NO>(split_tiles(u[2 * k][n], u[2 * k + 1][n]));
+#pragma unroll
+        for (int mt = 2 * k; mt < Z::kTiles; ++mt) {
+          const Pieces<NO> left = load_fragment<NO>(pf + (mt * Z::kSteps + k) * kInner * kFragment);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) qs[mt][n] = multiply(left, right[n], qs[mt][n]);
+        }
+      }
+#pragma unroll
+      for (int mt = 0; mt < Z::kTiles; ++mt)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int t = 16 * mt + 4 * g + r;
+            out.store(t, col + 16 * n, t < at.n && col + 16 * n < s.d_v, t < at.live ? qs[mt][n][r] : 0.f);
+          }
+    } else {
+#pragma unroll
+      for (int mt = 0; mt < Z::kTiles; ++mt)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (col + 16 * n < s.dvp) s.u[(head * C + 16 * mt + 4 * g + r) * s.dvp + col + 16 * n] = u[mt][n][r];
+    }
+    // S'
+    const float decay = steps[C - 1];
+#pragma unroll
+    for (int mt = 0; mt < Z::kTiles; ++mt) {
+      const f32x4 until = *(const f32x4*)(steps + kUntil * C + 16 * mt + 4 * g);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) u[mt][n] *= until;
+    }
+#pragma unroll
+    for (int i = 0; i < Z::kKeyTiles; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) state[i][n] *= decay;
+#pragma unroll
+    for (int k = 0; k < Z::kSteps; ++k) {
+      Pieces<3> right[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) right[n] = split_tiles(u[2 * k][n], u[2 * k + 1][n]);
+#pragma unroll
+      for (int i = 0; i < Z::kKeyTiles; ++i) {
+        const Pieces<NI> left = load_fragment<NI>(ktf + (i * Z::kSteps + k) * NI * kFragment);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) state[i][n] = multiply(left, right[n], state[i][n]);
+      }
+    }
+  }
+  if (s.hT) {
+#pragma unroll
+    for (int i = 0; i < Z::kKeyTiles; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int k = 16 * i + 4 * g + r, v = col + 16 * n;
+          if (k < s.d_k && v < s.d_v) s.hT[state_at + (int64_t)k * s.d_v + v] = state[i][n][r];
+        }
+  }
+}
+
+// The gradient of the state, backwards through the chunks:
+//   dU = P^T dO + exp(G_C - G) (K dS'),  dR = T^T dU,  dS = exp(G_C) dS' + Q^T (scale exp(G) dO) - K^T (exp(G) beta dR)
+// with R = beta X.  dS' and dR are kept for the kernel behind it.
+template <class E, int C, int DK, int NT>
+__global__ __launch_bounds__(64, 1) void delta_bwd_kernel(DeltaArgs s) {
+  typedef DeltaSizes<C, DK> Z;
+  constexpr int NI = delta_pieces<E>();
+  const DeltaTable table = DELTA_TABLE(s);
+  const int lane = threadIdx.x, g = lane >> 4;
+  const DeltaChain chain = delta_chain<NT>(s);
+  const int b = chain.b, h = chain.h, hk = h / s.each, col = chain.col + (lane & 15);
+  f32x4 state[Z::kKeyTiles][NT];  // dS
+  const int64_t state_at = ((int64_t)b * s.n_h + h) * s.d_k * s.d_v;
+#pragma unroll
+  for (int i = 0; i < Z::kKeyTiles; ++i)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int k = 16 * i + 4 * g + r, v = col + 16 * n;
+        state[i][n][r] = s.dhT && k < s.d_k && v < s.d_v ? s.dhT[state_at + (int64_t)k * s.d_v + v] : 0.f;
+      }
+
+  for (int c = s.chunks - 1; c >= 0; --c) {
+    const DeltaChunk at = delta_chunk<C>(s, b, c);
+    if (at.live == 0) continue;
+    const int64_t step0 = (int64_t)b * at.steps + at.first;
+    const int64_t key_at = (((int64_t)b * s.chunks + c) * s.n_hk + hk) * Z::kKeyPiece * NI;
+    const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h, step_at = head * Z::kStepPiece * kInner;
+    const uint16_t *const kf = s.kf + key_at, *const ktf = s.ktf + key_at, *const qtf = s.qtf + key_at, *const ttf = s.ttf + step_at, *const ptf = s.ptf + step_at;
+    const float* const steps = s.steps + head * kStepNumbers * C;
+    const DeltaColumns<E> grads(table[at.p].d_o, step0, s, h);
+    f32x4 d_o[Z::kTiles][NT];
+#pragma unroll
+    for (int mt = 0; mt < Z::kTiles; ++mt)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int t = 16 * mt + 4 * g + r;
+          d_o[mt][n][r] = grads.load(t, col + 16 * n, t < at.live && col + 16 * n < s.d_v);
+        }
+    {
+      float* const to = s.dstates + head * DK * s.dvp;
+#pragma unroll
+      for (int i = 0; i < Z::kKeyTiles; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (col + 16 * n < s.dvp) to[(int64_t)(16 * i + 4 * g + r) * s.dvp + col + 16 * n] = state[i][n][r];
+    }
+    f32x4 du[Z::kTiles][NT] = {}, dr[Z::kTiles][NT];
+#pragma unroll
+    for (int k = 0; k < Z::kKeySteps; ++k) {
+      Pieces<3> right[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) right[n] = split_tiles(state[2 * k][n], state[2 * k + 1][n]);
+#pragma unroll
+      for (int mt = 0; mt < Z::kTiles; ++mt) {
+        const Pieces<NI> left = load_fragment<NI>(kf + (mt * Z::kKeySteps + k) * NI * kFragment);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) du[mt][n] = multiply(left, right[n], du[mt][n]);
+      }
+    }
+#pragma unroll
+    for (int mt = 0; mt < Z::kTiles; ++mt) {
+      const f32x4 until = *(const f32x4*)(steps + kUntil * C + 16 * mt + 4 * g);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) du[mt][n] *= until;
+    }
+#pragma unroll
+    for (int k = 0; k < Z::kSteps; ++k) {
+      Pieces<NI> right[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) right[n] = first_pieces<NI>(split_tiles(d_o[2 * k][n], d_o[2 * k + 1][n]));  // (bf16 numbers are their upper halves)
+#pragma unroll
+      for (int mt = 0; mt < Z::kTiles && mt < 2 * k + 2; ++mt) {
+        const Pieces<kInner> left = load_fragment<kInner>(ptf + (mt * Z::kSteps + k) * kInner * kFragment);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) du[mt][n] = multiply(left, right[n], du[mt][n]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < Z::kSteps; ++k) {
+      Pieces<3> right[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) right[n] = split_tiles(du[2 * k][n], du[2 * k + 1][n]);
+#pragma unroll
+      for (int mt = 0; mt < Z::kTiles && mt < 2 * k + 2; ++mt) {
+        const Pieces<kInner> left = load_fragment<kInner>(ttf + (mt * Z::kSteps + k) * kInner * kFragment);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) dr[mt][n] = multiply(left, right[n], mt >= 2 * k ? f32x4{} : dr[mt][n]);
+      }
+    }
+    const float decay = steps[C - 1];
+#pragma unroll
+    for (int i = 0; i < Z::kKeyTiles; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) state[i][n] *= decay;
+#pragma unroll
+    for (int mt = 0; mt < Z::kTiles; ++mt) {
+      const f32x4 since = *(const f32x4*)(steps + 16 * mt + 4 * g), beta = *(const f32x4*)(steps + kBeta * C + 16 * mt + 4 * g);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (col + 16 * n < s.dvp) s.dr[(head * C + 16 * mt + 4 * g + r) * s.dvp + col + 16 * n] = dr[mt][n][r];
+        d_o[mt][n] *= since * s.scale;
+        dr[mt][n] *= -(since * beta);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < Z::kSteps; ++k) {
+      Pieces<3> one[NT], two[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        one[n] = split_tiles(d_o[2 * k][n], d_o[2 * k + 1][n]);
+        two[n] = split_tiles(dr[2 * k][n], dr[2 * k + 1][n]);
+      }
+#pragma unroll
+      for (int i = 0; i < Z::kKeyTiles; ++i) {
+        const Pieces<NI> q = load_fragment<NI>(qtf + (i * Z::kSteps + k) * NI * kFragment), kk = load_fragment<NI>(ktf + (i * Z::kSteps + k) * NI * kFragment);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) state[i][n] = multiply(kk, two[n], multiply(q, one[n], state[i][n]));
+      }
+    }
+  }
+  if (s.dh0) {
+#pragma unroll
+    for (int i = 0; i < Z::kKeyTiles; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int k = 16 * i + 4 * g + r, v = col + 16 * n;
+          if (k < s.d_k && v < s.d_v) s.dh0[state_at + (int64_t)k * s.d_v + v] = state[i][n][r];
+        }
+  }
+}
+
+// ---- a chunk's gradients --------------------------------------------------
+// With the states and their gradients known, chunks are independent.  A workgroup has a chunk of a key's head, whose heads it adds up in order:
+//   dA = -strictly lower (dR U^T),  dP = lower (dO U^T),  M = dA beta D,  N = scale D dP,  M and N of k_i k_j and q_i k_j
+//   dq = N K + scale exp(G) (dO S^T)
+//   dk = N^T Q + (M + M^T) K - exp(G) beta (dR S^T) + Y,  Y = exp(G_C - G) (U dS'^T)
+//   dv = beta dR,  dbeta_i = dR_i X_i + sum_j dA_ij D_ij k_i k_j
+//   dG_i = sums of (M k k + N q k) over row i less those over column i, and the rows' products of q, k with what they were multiplied by; what
+//   exp(G_C) multiplies goes to the last step;  dg_t = sum of dG from t on
+template <class E, int C, int DK>
+struct DeltaGradShared {
+  static constexpr int kRow = 72, kLine = C + 4, kTiles = C / 16, kKeyTiles = DK / 16;  // 64 columns at a time
+  union {
+    struct {
+      uint16_t dr[3][C][kRow], u[3][C][kRow], d_o[delta_pieces<E>()][C][kRow];
+    };
+    float inner[2][C][kLine];  // M + M^T, N
+  };
+  float row_sum[2][kTiles][C], col_sum[2][kTiles][C], beta_sum[kTiles][C];
+  float dots[kKeyTiles][C], ends[kKeyTiles][C], xs[C], both[kKeyTiles];
+};
+
+__device__ __forceinline__ float sum16(float v) {  // over a row of 16 lanes
+  v += row_rotated<8>(v);
+  v += row_rotated<4>(v);
+  v += row_rotated<2>(v);
+  return v + row_rotated<1>(v);
+}
+
+template <class E, int C, int DK>
+__global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
+  typedef DeltaSizes<C, DK> Z;
+  typedef DeltaGradShared<E, C, DK> Shared;
+  constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>();
+  constexpr int kMine = Z::kTiles * Z::kKeyTiles / 8;  // tiles of a wave: one column of keys, some rows of steps
+  constexpr int kLower = Z::kTiles * (Z::kTiles + 1) / 2, kJobs = (2 * kLower + 7) / 8;
+  extern __shared__ char delta_lds[];
+  Shared& m = *(Shared*)delta_lds;
+  const DeltaTable table = DELTA_TABLE(s);
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, row = lane & 15, g = lane >> 4;
+  const int kt = wave % Z::kKeyTiles, mt0 = wave / Z::kKeyTiles * kMine, key = kt * 16 + row;
+  const int hk = blockIdx.x % (uint32_t)s.n_hk, at_chunk = blockIdx.x / (uint32_t)s.n_hk;
+  const int c = at_chunk % s.chunks, b = at_chunk / s.chunks;
+  const DeltaChunk at = delta_chunk<C>(s, b, c);
+  const DeltaTable w = table + at.p;
+  const int64_t step0 = (int64_t)b * at.steps + at.first;
+  E* const dq = (E*)w->dq, * const dk = (E*)w->dk, * const dv = (E*)w->dv;
+  if (at.live == 0) {
+    for (int i = tid; i < at.n * s.d_k; i += 512) {
+      const int64_t o = ((step0 + i / s.d_k) * s.n_hk + hk) * s.d_k + i % s.d_k;
+      st(dq, (size_t)o, 0.f);
+      st(dk, (size_t)o, 0.f);
+    }
+    for (int i = tid; i < at.n * s.each * s.d_v; i += 512) {
+      const int t = i / (s.each * s.d_v), j = i % (s.each * s.d_v);
+      st(dv, (size_t)(((step0 + t) * s.n_h + hk * s.each) * s.d_v + j), 0.f);
+    }
+    for (int i = tid; i < at.n * s.each; i += 512) {
+      const int64_t o = (step0 + i / s.each) * s.n_h + hk * s.each + i % s.each;
+      if (w->dg) w->dg[o] = 0.f;
+      w->dbeta[o] = 0.f;
+    }
+    return;
+  }
+  const int64_t key_at = (((int64_t)b * s.chunks + c) * s.n_hk + hk) * Z::kKeyPiece * NI;
+  const uint16_t *const kf = s.kf + key_at, *const qf = s.qf + key_at, *const ktf = s.ktf + key_at, *const qtf = s.qtf + key_at;
+  f32x4 sum_q[kMine] = {}, sum_k[kMine] = {};
+
+  for (int e = 0; e < s.each; ++e) {
+    const int h = hk * s.each + e;
+    const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h;
+    const float* const steps = s.steps + head * kStepNumbers * C;
+    f32x4 os[kMine] = {}, rs[kMine] = {}, us[kMine] = {}, acc[kJobs] = {};
+    float xdot = 0.f, both = 0.f;
+    for (int v0 = 0; v0 < s.d_v; v0 += 64) {
+      __syncthreads();
+      if (tid < C * 8) {
+        const int t = tid >> 3, col = (tid & 7) * 8, v = v0 + col;
+        float r8[8] = {}, u8[8] = {}, x8[8] = {};
+        if (v < s.dvp) {
+          const int64_t o = (head * C + t) * s.dvp + v;
+          Eight<float> raw;
+          raw.load(s.dr + o, 8);
+          raw.values(r8);
+          raw.load(s.u + o, 8);
+          raw.values(u8);
+          raw.load(s.x + o, 8);
+          raw.values(x8);
+        }
+        Eight<E> grads;
+        const int64_t o = ((step0 + t) * s.n_h + h) * s.d_v + v;
+        grads.load((const E*)w->d_o + o, t < at.live ? max(0, min(8, s.d_v - v)) : 0);
+        const float beta = steps[kBeta * C + t];
+        float out[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          xdot = fmaf(r8[i], x8[i], xdot);
+          out[i] = t < at.live ? beta * r8[i] : 0.f;
+        }
+        if (t < at.n && v < s.d_v) store8(dv + o, out, min(8, s.d_v - v));
+        const Pieces<3> rp = split8(r8), up = split8(u8);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          *(u32x4*)&m.dr[k][t][col] = rp.p[k];
+          *(u32x4*)&m.u[k][t][col] = up.p[k];
+        }
+        if constexpr (NI == 1) {
+          *(u32x4*)&m.d_o[0][t][col] = grads.a;
+        } else {
+          float o8[8];
+          grads.values(o8);
+          const Pieces<3> op = split8(o8);
+#pragma unroll
+          for (int k = 0; k < 3; ++k) *(u32x4*)&m.d_o[k][t][col] = op.p[k];
+        }
+      }
+      __syncthreads();
+      for (int ks = 0; ks < 2 && v0 + 32 * ks < s.dvp; ++ks) {
+        const int at8 = 32 * ks + 8 * g, v = v0 + at8;
+        float s8[8] = {}, d8[8] = {};
+        if (v < s.dvp) {
+          const int64_t o = (head * DK + key) * s.dvp + v;
+          Eight<float> raw;
+          raw.load(s.states + o, 8);
+          raw.values(s8);
+          raw.load(s.dstates + o, 8);
+          raw.values(d8);
+        }
+        if (mt0 == 0) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) both = fmaf(s8[i], d8[i], both);
+        }
+        const Pieces<3> sp = split8(s8), dp = split8(d8);
+        auto rows3 = [&](const uint16_t (*from)[C][Shared::kRow], int mt) {
+          Pieces<3> o;
+#pragma unroll
+          for (int k = 0; k < 3; ++k) o.p[k] = *(const u32x4*)&from[k][mt * 16 + row][at8];
+          return o;
+        };
+        auto grads = [&](int mt) {
+          Pieces<NI> o;
+#pragma unroll
+          for (int k = 0; k < NI; ++k) o.p[k] = *(const u32x4*)&m.d_o[k][mt * 16 + row][at8];
+          return o;
+        };
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+          os[i] = multiply(grads(mt0 + i), sp, os[i]);
+          rs[i] = multiply(rows3(m.dr, mt0 + i), sp, rs[i]);
+          us[i] = multiply(rows3(m.u, mt0 + i), dp, us[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kJobs; ++i) {
+          const int job = wave + 8 * i;
+          if (job < 2 * kLower) {
+            const int what = job / kLower, tile = job % kLower, mt = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, nt = tile - mt * (mt + 1) / 2;
+            const Pieces<3> right = rows3(m.u, nt);
+            if (what) acc[i] = multiply(grads(mt), right, acc[i]);
+            else acc[i] = multiply(rows3(m.dr, mt), right, acc[i]);
+          }
+        }
+      }
+    }
+    __syncthreads();
+    // M and N
+#pragma unroll
+    for (int x = 0; x < kJobs; ++x) {
+      const int job = wave + 8 * x;
+      if (job >= 2 * kLower) continue;
+      const int what = job / kLower, tile = job % kLower, mt = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, nt = tile - mt * (mt + 1) / 2;
+      f32x4 dots = {};
+      for (int ks = 0; ks < Z::kKeySteps; ++ks)
+        dots = multiply(load_fragment<NI>((what ? qf : kf) + (mt * Z::kKeySteps + ks) * NI * kFragment),
+                        load_fragment<NI>(kf + (nt * Z::kKeySteps + ks) * NI * kFragment), dots);
+      const int j = nt * 16 + row;
+      const float whole = steps[kWhole * C + j], rest = steps[kRest * C + j];
+      float down = 0.f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = mt * 16 + 4 * g + r;
+        const bool below = i > j, in = what ? i >= j : below;
+        const float decay = in ? expf((steps[kWhole * C + i] - whole) + (steps[kRest * C + i] - rest)) : 0.f;
+        const float d = in ? decay * (what ? s.scale * acc[x][r] : -acc[x][r]) : 0.f, beta = what ? 1.f : steps[kBeta * C + i];
+        const float mine = d * beta, part = below ? mine * dots[r] : 0.f;
+        down += part;
+        const float across = sum16(part), for_beta = sum16(below ? d * dots[r] : 0.f);
+        if (row == 0) {
+          m.row_sum[what][nt][i] = across;
+          if (!what) m.beta_sum[nt][i] = for_beta;
+        }
+        if (what) {
+          m.inner[1][i][j] = mine;
+          if (mt != nt) m.inner[1][nt * 16 + 4 * g + r][mt * 16 + row] = 0.f;
+        } else if (below || mt != nt) {
+          m.inner[0][i][j] = mine;
+          m.inner[0][j][i] = mine;
+        } else if (i == j) {
+          m.inner[0][i][j] = 0.f;
+        }
+      }
+      down += __shfl_xor(down, 16, 64);
+      down += __shfl_xor(down, 32, 64);
+      if (g == 0) m.col_sum[what][mt][j] = down;
+    }
+    // what the states' products come to
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int t = (mt0 + i) * 16 + 4 * g + r;
+        const bool in = t < at.live && key < s.d_k;
+        const int64_t o = ((step0 + t) * s.n_hk + hk) * s.d_k + key;
+        const float qv = in ? ld((const E*)w->q, (size_t)o) : 0.f, kv = in ? ld((const E*)w->k, (size_t)o) : 0.f;
+        const float since = steps[kSince * C + t], one = s.scale * since * os[i][r], two = since * steps[kBeta * C + t] * rs[i][r],
+                    three = steps[kUntil * C + t] * us[i][r];
+        const float all = sum16(fmaf(qv, one, -kv * (two + three))), end = sum16(kv * three);
+        if (row == 0) {
+          m.dots[kt][t] = all;
+          m.ends[kt][t] = end;
+        }
+        sum_q[i][r] += one;
+        sum_k[i][r] += three - two;
+      }
+    }
+    both = wave_sum(both);
+    if (lane == 0 && mt0 == 0) m.both[kt] = both;
+    xdot += __shfl_xor(xdot, 1, 64);
+    xdot += __shfl_xor(xdot, 2, 64);
+    xdot += __shfl_xor(xdot, 4, 64);
+    if ((tid & 7) == 0 && tid < C * 8) m.xs[tid >> 3] = xdot;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < Z::kSteps; ++k) {
+      const Pieces<NI> kk = load_fragment<NI>(ktf + (kt * Z::kSteps + k) * NI * kFragment), qq = load_fragment<NI>(qtf + (kt * Z::kSteps + k) * NI * kFragment);
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        const int mt = mt0 + i, t = mt * 16 + row;
+        auto across = [&](const float (*from)[Shared::kLine]) {
+          return first_pieces<NO>(split_tiles(*(const f32x4*)&from[t][32 * k + 4 * g], *(const f32x4*)&from[t][32 * k + 16 + 4 * g]));
+        };
+        sum_k[i] = multiply(across(m.inner[0]), kk, sum_k[i]);
+        if (2 * k <= mt) sum_q[i] = multiply(across(m.inner[1]), kk, sum_q[i]);
+        if (mt / 2 <= k) {
+          float v[8];
+#pragma unroll
+          for (int x = 0; x < 8; ++x) v[x] = m.inner[1][delta_place(k, x)][t];
+          sum_k[i] = multiply(first_pieces<NO>(split8(v)), qq, sum_k[i]);
+        }
+      }
+    }
+    if (wave == 0 && (w->dg || w->dbeta)) {
+      const bool in = lane < C;
+      float d = 0.f, end = 0.f, for_beta = in ? m.xs[lane] : 0.f;
+      if (in) {
+        const int tile = lane >> 4;
+        for (int what = 0; what < 2; ++what) {
+          for (int i = 0; i <= tile; ++i) d += m.row_sum[what][i][lane];
+          for (int i = tile; i < Z::kTiles; ++i) d -= m.col_sum[what][i][lane];
+        }
+        for (int i = 0; i <= tile; ++i) for_beta += m.beta_sum[i][lane];
+        for (int i = 0; i < Z::kKeyTiles; ++i) {
+          d += m.dots[i][lane];
+          end += m.ends[i][lane];
+        }
+      }
+      end = wave_sum(end);
+      float all = 0.f;
+      for (int i = 0; i < Z::kKeyTiles; ++i) all += m.both[i];
+      if (lane == C - 1) d += end + steps[C - 1] * all;
+#pragma unroll
+      for (int o = 1; o < C; o *= 2) {
+        const float later = __shfl_down(d, o, 64);
+        if (lane + o < C) d += later;
+      }
+      if (lane < at.n) {
+        const int64_t o = (step0 + lane) * s.n_h + h;
+        if (w->dg) w->dg[o] = lane < at.live ? d : 0.f;
+        w->dbeta[o] = lane < at.live ? for_beta : 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kMine; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int t = (mt0 + i) * 16 + 4 * g + r;
+      if (t < at.n && key < s.d_k) {
+        const int64_t o = ((step0 + t) * s.n_hk + hk) * s.d_k + key;
+        st(dq, (size_t)o, t < at.live ? sum_q[i][r] : 0.f);
+        st(dk, (size_t)o, t < at.live ? sum_k[i][r] : 0.f);
+      }
+    }
+}
+
+// ---- single tokens --------------------------------------------------------
+// One step of each row: a workgroup has Q V columns of a head's state in its registers, thread (i, j) columns V j and rows i, i + 256 / Q, ...  Read
+// once: o = scale (a S^T q + (q k) u) needs no second pass over the new state.  Bound by reading and writing the states.
+template <class E, int V, int Q>
+__global__ __launch_bounds__(256) void delta_step_kernel(const E* __restrict__ q, const E* __restrict__ k, const E* __restrict__ v,
+                                                         const float* __restrict__ g, const float* __restrict__ beta, float* __restrict__ state,
+                                                         const int32_t* __restrict__ slots, E* __restrict__ o, int64_t n_slots, int n_h, int each,
+                                                         int d_k, int d_v, int groups, float scale) {
+  constexpr int kGroups = 256 / Q, R = 128 / kGroups;
+  __shared__ float keys[128], queries[128];
+  __shared__ float sums[4][Q][2 * V + 1];
+  const int tid = threadIdx.x, j = tid % Q, i = tid / Q;
+  const uint32_t group = blockIdx.x % (uint32_t)groups, at = blockIdx.x / (uint32_t)groups;
+  const int64_t row = at / (uint32_t)n_h;
+  const int h = at % (uint32_t)n_h, col = ((int)group * Q + j) * V;
+  const int64_t slot = slots ? slots[row] : row;
+  const bool in = col < d_v;
+  E* const out = o + ((int64_t)row * n_h + h) * d_v + col;
+  if (slot < 0 || slot >= n_slots) {
+    if (i == 0 && in) {
+#pragma unroll
+      for (int x = 0; x < V; ++x) st(out, (size_t)x, 0.f);
+    }
+    return;
+  }
+  const int64_t key = ((int64_t)row * (n_h / each) + h / each) * d_k, head = (int64_t)row * n_h + h;
+  float* const mine = state + ((slot * n_h + h) * d_k + i) * (int64_t)d_v + col;
+  float part[R][V];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const bool is = in && i + r * kGroups < d_k;
+    float* const from = mine + (int64_t)r * kGroups * d_v;
+    if constexpr (V == 4) {
+      const f32x4 x = is ? *(const f32x4*)from : f32x4{};
+#pragma unroll
+      for (int y = 0; y < 4; ++y) part[r][y] = x[y];
+    } else {
+      part[r][0] = is ? *from : 0.f;
+    }
+  }
+  if (tid < 128) {
+    keys[tid] = tid < d_k ? ld(k, (size_t)(key + tid)) : 0.f;
+    queries[tid] = tid < d_k ? ld(q, (size_t)(key + tid)) : 0.f;
+  }
+  const float a = g ? expf(g[head]) : 1.f, b = beta[head];
+  float value[V];
+#pragma unroll
+  for (int x = 0; x < V; ++x) value[x] = in ? ld(v, (size_t)(head * d_v + col + x)) : 0.f;
+  __syncthreads();
+  float sum[2 * V + 1] = {}, kr[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const float kk = keys[i + r * kGroups], qq = queries[i + r * kGroups];
+    kr[r] = kk;
+#pragma unroll
+    for (int x = 0; x < V; ++x) {
+      sum[x] = fmaf(part[r][x], kk, sum[x]);
+      sum[V + x] = fmaf(part[r][x], qq, sum[V + x]);
+    }
+    sum[2 * V] = fmaf(kk, qq, sum[2 * V]);
+  }
+  // over the rows: the lanes of a wave that have these columns, then the waves
+#pragma unroll
+  for (int x = 0; x < 2 * V + 1; ++x)
+#pragma unroll
+    for (int d = Q; d < 64; d *= 2) sum[x] += __shfl_xor(sum[x], d, 64);
+  if ((tid & 63) < Q) {
+#pragma unroll
+    for (int x = 0; x < 2 * V + 1; ++x) sums[tid >> 6][j][x] = sum[x];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < 2 * V + 1; ++x) sum[x] = (sums[0][j][x] + sums[1][j][x]) + (sums[2][j][x] + sums[3][j][x]);
+  float u[V];
+#pragma unroll
+  for (int x = 0; x < V; ++x) u[x] = b * fmaf(-a, sum[x], value[x]);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (!in || i + r * kGroups >= d_k) continue;
+    float* const to = mine + (int64_t)r * kGroups * d_v;
+    if constexpr (V == 4) {
+      f32x4 x;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) x[y] = fmaf(kr[r], u[y], a * part[r][y]);
+      *(f32x4*)to = x;
+    } else {
+      *to = fmaf(kr[r], u[0], a * part[r][0]);
+    }
+  }
+  if (i == 0 && in) {
+#pragma unroll
+    for (int x = 0; x < V; ++x) st(out, (size_t)x, scale * fmaf(sum[2 * V], u[x], a * sum[V + x]));
+  }
+}
+
+}  // namespace distdl
+
+struct distdl_delta_plan {
+  int32_t n_b = 0, T = 0, n_h = 0, n_hk = 0, d_k = 0, d_v = 0, P = 1;
+  float scale = 1;
+  distdl_dtype dtype = DISTDL_F32;
+  distdl::DevArray<distdl::DeltaWorker> table;
+  distdl::StreamScratch scratch;
+};
+
+namespace distdl {
+
+constexpr int kDeltaKeys = 128;  // d_k: the state's rows are registers
+
+static int delta_check(const void* v, size_t size, const char* what, int j) {
+  if (!v) return set_error(DISTDL_ERR_NULL, "delta: %s[%d] is null", what, j);
+  if ((uintptr_t)v % size) return set_error(DISTDL_ERR_INVALID_ARG, "delta: %s[%d] is not aligned to its elements", what, j);
+  return DISTDL_OK;
+}
+
+static int delta_args(distdl_delta_plan* p, const std::vector<DeltaWorker>& w, hipStream_t st, DeltaArgs* s) {
+  *s = DeltaArgs{};
+  if (p->P <= kDeltaInline) {
+    std::copy(w.begin(), w.end(), s->w);
+  } else {
+    const int rc = p->table.upload(w, st);
+    if (rc) return rc;
+    s->more = p->table.dev;
+  }
+  const int C = p->dtype == DISTDL_F32 ? delta_chunk_steps<float>() : delta_chunk_steps<uint16_t>();
+  s->P = p->P;
+  s->T = p->T;
+  s->part = p->T / p->P;
+  s->extra = p->T % p->P;
+  s->chunks_wide = (s->part + C) / C;
+  s->chunks_rest = (s->part + C - 1) / C;
+  s->chunks = s->extra * s->chunks_wide + (s->P - s->extra) * s->chunks_rest;
+  s->n_b = p->n_b;
+  s->n_h = p->n_h;
+  s->n_hk = p->n_hk;
+  s->each = p->n_h / p->n_hk;
+  s->d_k = p->d_k;
+  s->d_v = p->d_v;
+  s->dvp = (p->d_v + 15) / 16 * 16;
+  s->scale = p->scale;
+  return DISTDL_OK;
+}
+
+// The scratch of a call, one array behind the other at multiples of 256 bytes.
+template <class E, int C, int DK>
+static int delta_scratch(distdl_delta_plan* p, bool back, hipStream_t st, DeltaArgs* s) {
+  typedef DeltaSizes<C, DK> Z;
+  const size_t keys = (size_t)s->n_b * s->chunks * s->n_hk, heads = (size_t)s->n_b * s->chunks * s->n_h;
+  const size_t key = keys * Z::kKeyPiece * delta_pieces<E>() * 2, step = heads * Z::kStepPiece * kInner * 2, state = heads * DK * s->dvp * 4,
+               rows = heads * C * s->dvp * 4;
+  struct Part {
+    void** at;
+    size_t bytes;
+  } parts[] = {{(void**)&s->kf, key}, {(void**)&s->ktf, key}, {(void**)&s->qf, key}, {(void**)&s->qtf, back ? key : 0},
+               {(void**)&s->tf, step}, {(void**)&s->pf, step}, {(void**)&s->ttf, back ? step : 0}, {(void**)&s->ptf, back ? step : 0},
+               {(void**)&s->steps, heads * kStepNumbers * C * 4}, {(void**)&s->states, back ? state : 0}, {(void**)&s->dstates, back ? state : 0},
+               {(void**)&s->u, back ? rows : 0}, {(void**)&s->x, back ? rows : 0}, {(void**)&s->dr, back ? rows : 0}};
+  size_t all = 0;
+  for (const Part& v : parts) all += (v.bytes + 255) / 256 * 256;
+  bool is_new = true;
+  for (const StreamScratch::Block& v : p->scratch.blocks) is_new = is_new && (v.stream != st || v.floats < all / 4);
+  if (is_new) {
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    DISTDL_HIP_TRY(hipStreamIsCapturing(st, &capture));
+    if (capture != hipStreamCaptureStatusNone)
+      return set_error(DISTDL_ERR_INVALID_ARG, "delta: the plan's first such call on this stream, which is being captured");
+  }
+  float* base = nullptr;
+  const int rc = p->scratch.get(all / 4, st, &base);
+  if (rc) return rc;
+  char* at = (char*)base;
+  for (const Part& v : parts) {
+    *v.at = v.bytes ? at : nullptr;
+    at += (v.bytes + 255) / 256 * 256;
+  }
+  return DISTDL_OK;
+}
+
+template <class E, int C, int DK, bool BACK>
+static int launch_delta(distdl_delta_plan* p, DeltaArgs& s, hipStream_t st) {
+  int rc = delta_scratch<E, C, DK>(p, BACK, st, &s);
+  if (rc) return rc;
+  constexpr auto prepare = delta_prepare_kernel<E, C, DK, BACK>;
+  if ((rc = allow_large_lds<prepare>())) return rc;
+  const dim3 chunks((unsigned)((int64_t)s.n_b * s.chunks * s.n_hk));
+  hipLaunchKernelGGL(prepare, chunks, dim3(256), sizeof(DeltaPrepareShared<E, C, DK>), st, s);
+  // A wave takes 32 columns where that many waves fill the card: it reads the chunks' matrices half as often.
+  const int64_t chains = (int64_t)s.n_b * s.n_h;
+  const bool two = s.d_v > 16 && chains * ((s.d_v + 31) / 32) >= 1024;
+  s.slices = two ? (s.d_v + 31) / 32 : (s.d_v + 15) / 16;
+  const dim3 waves((unsigned)(chains * s.slices));
+  if (two) hipLaunchKernelGGL((delta_fwd_kernel<E, C, DK, 2, BACK>), waves, dim3(64), 0, st, s);
+  else hipLaunchKernelGGL((delta_fwd_kernel<E, C, DK, 1, BACK>), waves, dim3(64), 0, st, s);
+  if constexpr (BACK) {
+    if (two) hipLaunchKernelGGL((delta_bwd_kernel<E, C, DK, 2>), waves, dim3(64), 0, st, s);
+    else hipLaunchKernelGGL((delta_bwd_kernel<E, C, DK, 1>), waves, dim3(64), 0, st, s);
+    constexpr auto grad = delta_grad_kernel<E, C, DK>;
+    if ((rc = allow_large_lds<grad>())) return rc;
+    hipLaunchKernelGGL(grad, chunks, dim3(512), sizeof(DeltaGradShared<E, C, DK>), st, s);
+  }
+  return DISTDL_OK;
+}
+
+template <bool BACK>
+static int launch_delta(distdl_delta_plan* p, DeltaArgs& s, hipStream_t st) {
+  const bool wide = p->d_k > 64;
+  if (p->dtype == DISTDL_F32)
+    return wide ? launch_delta<float, delta_chunk_steps<float>(), 128, BACK>(p, s, st) : launch_delta<float, delta_chunk_steps<float>(), 64, BACK>(p, s, st);
+  return wide ? launch_delta<uint16_t, delta_chunk_steps<uint16_t>(), 128, BACK>(p, s, st)
+              : launch_delta<uint16_t, delta_chunk_steps<uint16_t>(), 64, BACK>(p, s, st);
+}
+
+template <class E, int V, int Q>
+static void launch_delta_step(const void* q, const void* k, const void* v, const float* g, const float* beta, float* state, const int32_t* slots,
+                              void* o, int64_t n_slots, int64_t rows, int n_h, int each, int d_k, int d_v, float scale, hipStream_t st) {
+  const int groups = (d_v + V * Q - 1) / (V * Q);
+  hipLaunchKernelGGL((delta_step_kernel<E, V, Q>), dim3((unsigned)(rows * n_h * groups)), dim3(256), 0, st, (const E*)q, (const E*)k, (const E*)v, g,
+                     beta, state, slots, (E*)o, n_slots, n_h, each, d_k, d_v, groups, scale);
+}
+
+template <class E>
+static void delta_step_kind(const void* q, const void* k, const void* v, const float* g, const float* beta, float* state, const int32_t* slots, void* o,
+                            int64_t n_slots, int64_t rows, int n_h, int each, int d_k, int d_v, float scale, hipStream_t st) {
+  if (d_v % 4 || (uintptr_t)state % 16)
+    launch_delta_step<E, 1, 32>(q, k, v, g, beta, state, slots, o, n_slots, rows, n_h, each, d_k, d_v, scale, st);
+  else if (d_v <= 32 || rows * n_h < 512)
+    launch_delta_step<E, 4, 8>(q, k, v, g, beta, state, slots, o, n_slots, rows, n_h, each, d_k, d_v, scale, st);
+  else
+    launch_delta_step<E, 4, 32>(q, k, v, g, beta, state, slots, o, n_slots, rows, n_h, each, d_k, d_v, scale, st);
+}
+
+// What every call asks of the sizes.
+static int delta_sizes(const char* call, int64_t n_h, int64_t n_hk, int64_t d_k, int64_t d_v, double scale, distdl_dtype dtype) {
+  if (n_h < 1 || n_hk < 1 || d_k < 1 || d_v < 1) return set_error(DISTDL_ERR_INVALID_ARG, "%s: sizes must be >= 1", call);
+  if (n_h % n_hk) return set_error(DISTDL_ERR_INVALID_ARG, "%s: %lld heads on %lld heads of keys", call, (long long)n_h, (long long)n_hk);
+  if (!std::isfinite(scale)) return set_error(DISTDL_ERR_INVALID_ARG, "%s: scale %g", call, scale);
+  if (dtype != DISTDL_F32 && dtype != DISTDL_BF16) return set_error(DISTDL_ERR_UNSUPPORTED, "unknown dtype");
+  if (d_k > kDeltaKeys) return set_error(DISTDL_ERR_UNSUPPORTED, "%s: d_k of more than %d", call, kDeltaKeys);
+  if (n_h > 1 << 20 || d_v > 1 << 20 || n_h * d_v > 1 << 22) return set_error(DISTDL_ERR_UNSUPPORTED, "%s: problem too large", call);
+  return DISTDL_OK;
+}
+
+}  // namespace distdl
+
+using namespace distdl;
+
+extern "C" {
+
+int distdl_delta_plan_create(distdl_delta_plan** out, int64_t n_b, int64_t T, int64_t n_h, int64_t n_hk, int64_t d_k, int64_t d_v, int P, double scale,
+                             distdl_dtype dtype) {
+  if (!out) return set_error(DISTDL_ERR_NULL, "delta_plan_create: null argument");
+  *out = nullptr;
+  if (n_b < 1 || T < 1 || P < 1) return set_error(DISTDL_ERR_INVALID_ARG, "delta_plan_create: sizes must be >= 1");
+  const int rc = delta_sizes("delta_plan_create", n_h, n_hk, d_k, d_v, scale, dtype);
+  if (rc) return rc;
+  if (T < P) return set_error(DISTDL_ERR_EMPTY_PARTITION, "delta: %lld steps over %d workers", (long long)T, P);
+  if (T >= int64_t(1) << 30 || n_b >= 1 << 20 || n_b * (T / 32 + P) >= kMaxBlocks256 / n_hk / 2 || n_b * n_h * ((d_v + 15) / 16) >= kMaxBlocks256)
+    return set_error(DISTDL_ERR_UNSUPPORTED, "delta: problem too large");
+  return guarded([&]() -> int {
+    std::unique_ptr<distdl_delta_plan> p(new distdl_delta_plan());
+    p->n_b = (int32_t)n_b;
+    p->T = (int32_t)T;
+    p->n_h = (int32_t)n_h;
+    p->n_hk = (int32_t)n_hk;
+    p->d_k = (int32_t)d_k;
+    p->d_v = (int32_t)d_v;
+    p->P = P;
+    p->scale = (float)scale;
+    p->dtype = dtype;
+    *out = p.release();
+    return DISTDL_OK;
+  });
+}
+
+int distdl_delta_plan_destroy(distdl_delta_plan* p) {
+  if (!p) return DISTDL_OK;
+  p->table.release();
+  p->scratch.release();
+  delete p;
+  return DISTDL_OK;
+}
+
+int distdl_delta_fwd(distdl_delta_plan* p, const void* const q_dev[], const void* const k_dev[], const void* const v_dev[], const float* const g_dev[],
+                     const float* const beta_dev[], const float* h0_dev, const int32_t* lengths_dev, void* const o_dev[], float* hT_dev, void* stream) {
+  if (!p || !q_dev || !k_dev || !v_dev || !beta_dev || !o_dev) return set_error(DISTDL_ERR_NULL, "delta_fwd: null argument");
+  if ((uintptr_t)h0_dev % 4 || (uintptr_t)lengths_dev % 4 || (uintptr_t)hT_dev % 4)
+    return set_error(DISTDL_ERR_INVALID_ARG, "delta_fwd: h0, lengths or hT is not aligned to its elements");
+  return guarded([&]() -> int {
+    const size_t size = dtype_size(p->dtype);
+    std::vector<DeltaWorker> w((size_t)p->P);
+    int rc;
+    for (int j = 0; j < p->P; ++j) {
+      if ((rc = delta_check(q_dev[j], size, "q", j)) || (rc = delta_check(k_dev[j], size, "k", j)) || (rc = delta_check(v_dev[j], size, "v", j)) ||
+          (g_dev && (rc = delta_check(g_dev[j], 4, "g", j))) || (rc = delta_check(beta_dev[j], 4, "beta", j)) ||
+          (rc = delta_check(o_dev[j], size, "o", j)))
+        return rc;
+      w[j] = DeltaWorker{q_dev[j], k_dev[j], v_dev[j], g_dev ? g_dev[j] : nullptr, beta_dev[j], o_dev[j]};
+    }
+    hipStream_t st_ = (hipStream_t)stream;
+    DeltaArgs s;
+    if ((rc = delta_args(p, w, st_, &s))) return rc;
+    s.h0 = h0_dev;
+    s.lengths = lengths_dev;
+    s.hT = hT_dev;
+    {
+      ProfScope prof("delta_fwd", st_);
+      rc = launch_delta<false>(p, s, st_);
+    }
+    if (rc) return rc;
+    DISTDL_HIP_TRY(hipGetLastError());
+    return DISTDL_OK;
+  });
+}
+
+int distdl_delta_bwd(distdl_delta_plan* p, const void* const q_dev[], const void* const k_dev[], const void* const v_dev[], const float* const g_dev[],
+                     const float* const beta_dev[], const float* h0_dev, const int32_t* lengths_dev, const void* const do_dev[], const float* dhT_dev,
+                     void* const dq_dev[], void* const dk_dev[], void* const dv_dev[], float* const dg_dev[], float* const dbeta_dev[], float* dh0_dev,
+                     void* stream) {
+  if (!p || !q_dev || !k_dev || !v_dev || !beta_dev || !do_dev || !dq_dev || !dk_dev || !dv_dev || !dbeta_dev)
+    return set_error(DISTDL_ERR_NULL, "delta_bwd: null argument");
+  if (dg_dev && !g_dev) return set_error(DISTDL_ERR_NULL, "delta_bwd: gradients of g without g");
+  if ((uintptr_t)h0_dev % 4 || (uintptr_t)lengths_dev % 4 || (uintptr_t)dhT_dev % 4 || (uintptr_t)dh0_dev % 4)
+    return set_error(DISTDL_ERR_INVALID_ARG, "delta_bwd: h0, lengths, dhT or dh0 is not aligned to its elements");
+  return guarded([&]() -> int {
+    const size_t size = dtype_size(p->dtype);
+    std::vector<DeltaWorker> w((size_t)p->P);
+    int rc;
+    for (int j = 0; j < p->P; ++j) {
+      if ((rc = delta_check(q_dev[j], size, "q", j)) || (rc = delta_check(k_dev[j], size, "k", j)) || (rc = delta_check(v_dev[j], size, "v", j)) ||
+          (g_dev && (rc = delta_check(g_dev[j], 4, "g", j))) || (rc = delta_check(beta_dev[j], 4, "beta", j)) ||
+          (rc = delta_check(do_dev[j], size, "do", j)) || (rc = delta_check(dq_dev[j], size, "dq", j)) || (rc = delta_check(dk_dev[j], size, "dk", j)) ||
+          (rc = delta_check(dv_dev[j], size, "dv", j)) || (dg_dev && (rc = delta_check(dg_dev[j], 4, "dg", j))) ||
+          (rc = delta_check(dbeta_dev[j], 4, "dbeta", j)))
+        return rc;
+      w[j] = DeltaWorker{q_dev[j],  k_dev[j],  v_dev[j],  g_dev ? g_dev[j] : nullptr,   beta_dev[j],  nullptr,
+                         do_dev[j], dq_dev[j], dk_dev[j], dv_dev[j], dg_dev ? dg_dev[j] : nullptr, dbeta_dev[j]};
+    }
+    hipStream_t st_ = (hipStream_t)stream;
+    DeltaArgs s;
+    if ((rc = delta_args(p, w, st_, &s))) return rc;
+    s.h0 = h0_dev;
+    s.lengths = lengths_dev;
+    s.dhT = dhT_dev;
+    s.dh0 = dh0_dev;
+    {
+      ProfScope prof("delta_bwd", st_);
+      rc = launch_delta<true>(p, s, st_);
+    }
+    if (rc) return rc;
+    DISTDL_HIP_TRY(hipGetLastError());
+    return DISTDL_OK;
+  });
+}
+
+int distdl_delta_step(const void* q_dev, const void* k_dev, const void* v_dev, const float* g_dev, const float* beta_dev, float* state_dev,
+                      int64_t n_slots, const int32_t* slots_dev, void* o_dev, int64_t rows, int64_t n_h, int64_t n_hk, int64_t d_k, int64_t d_v,
+                      double scale, distdl_dtype dtype, void* stream) {
+  if (rows < 0 || n_slots < 0) return set_error(DISTDL_ERR_INVALID_ARG, "delta_step: %lld rows, %lld slots", (long long)rows, (long long)n_slots);
+  const int rc = delta_sizes("delta_step", n_h, n_hk, d_k, d_v, scale, dtype);
+  if (rc) return rc;
+  if (rows == 0) return DISTDL_OK;
+  if (!q_dev || !k_dev || !v_dev || !beta_dev || !o_dev || (!state_dev && n_slots > 0)) return set_error(DISTDL_ERR_NULL, "delta_step: null argument");
+  if (!slots_dev && n_slots < rows) return set_error(DISTDL_ERR_INVALID_ARG, "delta_step: %lld states for %lld rows", (long long)n_slots, (long long)rows);
+  if (rows >= kMaxBlocks256 / (n_h * ((d_v + 31) / 32))) return set_error(DISTDL_ERR_UNSUPPORTED, "delta_step: problem too large");
+  const size_t size = dtype_size(dtype);
+  if ((uintptr_t)q_dev % size || (uintptr_t)k_dev % size || (uintptr_t)v_dev % size || (uintptr_t)o_dev % size || (uintptr_t)g_dev % 4 ||
+      (uintptr_t)beta_dev % 4 || (uintptr_t)state_dev % 4 || (uintptr_t)slots_dev % 4)
+    return set_error(DISTDL_ERR_INVALID_ARG, "delta_step: an array is not aligned to its elements");
+  hipStream_t st_ = (hipStream_t)stream;
+  {
+    ProfScope prof("delta_step", st_);
+    auto* launch = dtype == DISTDL_F32 ? delta_step_kind<float> : delta_step_kind<uint16_t>;
+    launch(q_dev, k_dev, v_dev, g_dev, beta_dev, state_dev, slots_dev, o_dev, n_slots, rows, (int)n_h, (int)(n_h / n_hk), (int)d_k, (int)d_v,
+           (float)scale, st_);
+  }
+  DISTDL_HIP_TRY(hipGetLastError());
+  return DISTDL_OK;
+}
+
+}  // extern "C"
