@@ -3,7 +3,7 @@
 // A matrix operand of v_mfma_f32_16x16x32_bf16 is, for each lane, eight numbers of a row (or column) lane % 16: a fragment of 16 x 32
 // numbers, 1 KiB.  The sums' order is free, so the 32 numbers that a fragment is summed over are taken as lane group g = lane / 16
 // gets them from two 16 x 16 tiles of results: 4 g + 0 .. 3 of the first, 4 g + 0 .. 3 of the second.  So one product's results are the next one's
-// right operand as they lie in the registers, and the chain of a chunk's products needs no LDS.
+// right operand as they lie in the lanes.
 //
 // Numbers that are not bf16 already are sums of three bf16 parts, which hold all 24 bits (hi, and what is left, twice); products keep
 // the parts whose sum of ranks is below three: six products of two such operands, three of one with a bf16 operand.
@@ -20,6 +20,7 @@
 
 namespace distdl {
 
+constexpr int kChunk = 64;        // steps
 constexpr int kDeltaInline = 16;  // workers whose pointers travel with the launch; more are in a table
 
 struct DeltaWorker {
@@ -61,25 +62,33 @@ typedef const __attribute__((address_space(4))) DeltaWorker* DeltaTable;
 struct DeltaChunk {
   int32_t p, first, n, steps, live;
 };
-template <int C>
 __device__ __forceinline__ DeltaChunk delta_chunk(const DeltaArgs& s, int b, int c) {
   DeltaChunk r;
   const int wide = s.extra * s.chunks_wide;
   if (c < wide) {
     r.p = c / s.chunks_wide;
-    r.first = (c - r.p * s.chunks_wide) * C;
+    r.first = (c - r.p * s.chunks_wide) * kChunk;
     r.steps = s.part + 1;
   } else {
     const int i = (c - wide) / s.chunks_rest;
     r.p = s.extra + i;
-    r.first = (c - wide - i * s.chunks_rest) * C;
+    r.first = (c - wide - i * s.chunks_rest) * kChunk;
     r.steps = s.part;
   }
-  r.n = min(C, r.steps - r.first);
+  r.n = min(kChunk, r.steps - r.first);
   const int64_t at = (int64_t)r.p * s.part + min(r.p, s.extra) + r.first;  // of the whole
   const int64_t len = s.lengths ? s.lengths[b] : s.T;
   r.live = (int)max((int64_t)0, min((int64_t)r.n, len - at));
   return r;
+}
+
+// How many chunks have steps inside sequence b; they come first.
+__device__ __forceinline__ int delta_live_chunks(const DeltaArgs& s, int b) {
+  const int len = s.lengths ? max(0, min(s.lengths[b], s.T)) : s.T;
+  if (len == 0) return 0;
+  const int last = len - 1, wide = s.extra * (s.part + 1);
+  if (last < wide) return last / (s.part + 1) * s.chunks_wide + last % (s.part + 1) / kChunk + 1;
+  return s.extra * s.chunks_wide + (last - wide) / s.part * s.chunks_rest + (last - wide) % s.part / kChunk + 1;
 }
 
 // ---- operand pieces -------------------------------------------------------

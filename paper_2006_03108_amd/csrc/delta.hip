@@ -8,18 +8,16 @@
 //   A = strictly lower (beta_i D_ij k_i k_j),  T = (1 + A)^-1,  P = lower (scale D_ij q_i k_j)
 //   X = V - exp(G) (K S),  U = T (beta X),  O = scale exp(G) (Q S) + P U,  S' = exp(G_C) S + K^T (exp(G_C - G) U)
 // A, T and P need no state: one launch makes them for all chunks (delta_prepare_kernel).  What is left goes through time, and its columns
-// (of d_v) are independent: a wave has 16 or 32 columns of a head's state in its registers and goes through all chunks, from product to
-// product without LDS or barriers (delta.h).  Differences of G are exact: sums in 64 bits, kept as a multiple of 1/64 and the rest.
+// (of d_v) are independent: a workgroup has 16 or 32 columns of a head's state in its registers and goes through all chunks, from product
+// to product.  Differences of G are exact: sums in 64 bits, kept as a multiple of 1/64 and the rest.
 #include <algorithm>
 #include <cmath>
 
 #include "delta.h"
+#include "lds_direct.h"
 #include "profile.h"
 
 namespace distdl {
-
-template <class E>
-constexpr int delta_chunk_steps() { return sizeof(E) == 2 ? 64 : 32; }  // (three pieces of every operand would not fit in LDS)
 
 // A factor of exp(-200) is 0 in 32 bits, and so is what it stands between.
 __device__ __forceinline__ float bounded(float g) { return g < -200.f ? -200.f : g; }
@@ -95,7 +93,7 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs s) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, row = lane & 15, g = lane >> 4;
   const int hk = blockIdx.x % (uint32_t)s.n_hk, at_chunk = blockIdx.x / (uint32_t)s.n_hk;
   const int c = at_chunk % s.chunks, b = at_chunk / s.chunks;
-  const DeltaChunk at = delta_chunk<C>(s, b, c);
+  const DeltaChunk at = delta_chunk(s, b, c);
   if (at.live == 0) return;  // nobody reads what would be here
   const int64_t step0 = (int64_t)b * at.steps + at.first;  // of the worker's arrays
   const DeltaTable w = table + at.p;
@@ -261,7 +259,7 @@ struct DeltaColumns {
   }
 };
 
-struct DeltaChain {  // a wave's sequence, head and first column
+struct DeltaChain {  // a workgroup's sequence, head and first column
   int b, h, col;
 };
 template <int NT>
@@ -275,330 +273,398 @@ __device__ __forceinline__ DeltaChain delta_chain(const DeltaArgs& s) {
 template <class E>
 constexpr int delta_rounded() { return sizeof(E) == 2 ? 2 : 3; }
 
-template <class E, int C, int DK, int NT, bool STORE>
-__global__ __launch_bounds__(64, 1) void delta_fwd_kernel(DeltaArgs s) {
-  typedef DeltaSizes<C, DK> Z;
-  constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>();
+// An operand that the four waves of a workgroup make together and all read: [steps of the sum][column tiles][pieces][lanes].
+template <int STEPS, int NT, int N>
+struct DeltaShared {
+  u32x4 v[STEPS][NT][N][64];
+  __device__ __forceinline__ Pieces<N> read(int k, int n) const {
+    Pieces<N> o;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o.p[i] = v[k][n][i][threadIdx.x & 63];
+    return o;
+  }
+  // tile `tile` of 16 rows: half of a step
+  __device__ __forceinline__ void write(int tile, int n, f32x4 x) {
+    const Pieces<3> p = split_tiles(x, f32x4{});
+#pragma unroll
+    for (int i = 0; i < N; ++i) ((u32x2*)&v[tile >> 1][n][i][threadIdx.x & 63])[tile & 1] = u32x2{p.p[i][0], p.p[i][1]};
+  }
+  // tiles 2 k and 2 k + 1
+  __device__ __forceinline__ void write(int k, int n, f32x4 x, f32x4 y) {
+    const Pieces<3> p = split_tiles(x, y);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[k][n][i][threadIdx.x & 63] = p.p[i];
+  }
+};
+template <int COUNT, int N>
+struct DeltaFragments {
+  Pieces<N> v[COUNT];
+  // fragments `from`, `from` + 1, ..., of STRIDE pieces each
+  template <int STRIDE>
+  __device__ __forceinline__ void load(const uint16_t* at, int from) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) v[i] = load_fragment<N>(at + (int64_t)(from + i) * STRIDE * kFragment);
+  }
+};
+
+// A workgroup of four waves takes 16 NT columns of a head's state through all chunks.  Wave w has the tile of steps 16 w .. 16 w + 15 of every product
+// over keys or steps, and a quarter of the state's rows, so the chunk's matrices are read by one wave each, straight into the registers that the
+// last chunk's have left: every load has most of a chunk's time.  What the waves make for each other, in pieces, goes through LDS: the state, beta X and
+// U, a barrier for each, which waits for LDS alone (lds_barrier).
+template <class E, int DK, int NT, bool STORE>
+__global__ __launch_bounds__(256, 1) void delta_fwd_kernel(DeltaArgs s) {
+  typedef DeltaSizes<kChunk, DK> Z;
+  constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>(), KT = DK / 64, KS = Z::kKeySteps;
+  __shared__ DeltaShared<KS, NT, 3> for_keys;
+  __shared__ DeltaShared<2, NT, 3> for_inner, for_state;
+  __shared__ DeltaShared<2, NT, STORE ? 1 : NO> for_out;
   const DeltaTable table = DELTA_TABLE(s);
-  const int lane = threadIdx.x, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4;
   const DeltaChain chain = delta_chain<NT>(s);
   const int b = chain.b, h = chain.h, hk = h / s.each, col = chain.col + (lane & 15);
-  f32x4 state[Z::kKeyTiles][NT];
+  f32x4 state[KT][NT];
   const int64_t state_at = ((int64_t)b * s.n_h + h) * s.d_k * s.d_v;
 #pragma unroll
-  for (int i = 0; i < Z::kKeyTiles; ++i)
+  for (int i = 0; i < KT; ++i)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int k = 16 * i + 4 * g + r, v = col + 16 * n;
+        const int k = 16 * (wave * KT + i) + 4 * g + r, v = col + 16 * n;
         state[i][n][r] = s.h0 && k < s.d_k && v < s.d_v ? s.h0[state_at + (int64_t)k * s.d_v + v] : 0.f;
       }
+  const int chunks = delta_live_chunks(s, b);
+  const int64_t chunk0 = (int64_t)b * s.chunks;
 
-  for (int c = 0; c < s.chunks; ++c) {
-    const DeltaChunk at = delta_chunk<C>(s, b, c);
-    const int64_t step0 = (int64_t)b * at.steps + at.first;
-    const DeltaColumns<E> out(STORE ? nullptr : table[at.p].o, step0, s, h);
-    if (at.live == 0) {
-      if (!STORE) {
+  DeltaFragments<KS, NI> kf, qf;
+  DeltaFragments<2, kInner> tf;
+  DeltaFragments<2, NO> pf;
+  DeltaFragments<2 * KT, NI> ktf;
+  f32x4 since, until, beta, next_since, next_until, next_beta;
+  float decay, next_decay;
+  uint32_t raw[NT][4];
+  auto load_keys = [&](int c) {
+    const int64_t at = ((chunk0 + c) * s.n_hk + hk) * Z::kKeyPiece * NI;
+    kf.template load<NI>(s.kf + at, wave * KS);
+    if (!STORE) qf.template load<NI>(s.qf + at, wave * KS);
+  };
+  auto load_inner = [&](int c) { tf.template load<kInner>(s.tf + ((chunk0 + c) * s.n_h + h) * Z::kStepPiece * kInner, wave * 2); };
+  auto load_last = [&](int c) {
+    if (!STORE) pf.template load<kInner>(s.pf + ((chunk0 + c) * s.n_h + h) * Z::kStepPiece * kInner, wave * 2);
+    ktf.template load<NI>(s.ktf + ((chunk0 + c) * s.n_hk + hk) * Z::kKeyPiece * NI, wave * KT * 2);
+  };
+  auto load_steps = [&](int c) {
+    const float* const at = s.steps + ((chunk0 + c) * s.n_h + h) * kStepNumbers * kChunk + 16 * wave + 4 * g;
+    next_since = *(const f32x4*)(at + kSince * kChunk);
+    next_until = *(const f32x4*)(at + kUntil * kChunk);
+    next_beta = *(const f32x4*)(at + kBeta * kChunk);
+    next_decay = s.steps[((chunk0 + c) * s.n_h + h) * kStepNumbers * kChunk + kChunk - 1];
+  };
+  auto load_values = [&](const DeltaChunk& at) {
+    const DeltaColumns<E> values(table[at.p].v, (int64_t)b * at.steps + at.first, s, h);
 #pragma unroll
-        for (int mt = 0; mt < Z::kTiles; ++mt)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int t = 16 * mt + 4 * g + r;
-              out.store(t, col + 16 * n, t < at.n && col + 16 * n < s.d_v, 0.f);
-            }
+      for (int r = 0; r < 4; ++r) {
+        const int t = 16 * wave + 4 * g + r;
+        raw[n][r] = values.raw(t, col + 16 * n, t < at.live && col + 16 * n < s.d_v);
       }
-      continue;
+  };
+  auto write_state = [&](int c) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if constexpr (KT == 2) for_keys.write(wave, n, state[0][n], state[1][n]);
+      else for_keys.write(wave, n, state[0][n]);
     }
-    const int64_t key_at = (((int64_t)b * s.chunks + c) * s.n_hk + hk) * Z::kKeyPiece * NI;
-    const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h, step_at = head * Z::kStepPiece * kInner;
-    const uint16_t *const kf = s.kf + key_at, *const qf = s.qf + key_at, *const ktf = s.ktf + key_at, *const tf = s.tf + step_at, *const pf = s.pf + step_at;
-    const float* const steps = s.steps + head * kStepNumbers * C;
-    const DeltaColumns<E> values(table[at.p].v, step0, s, h);
-    uint32_t raw[Z::kTiles][NT][4];
+    if (STORE && c < chunks) {
+      float* const to = s.states + ((chunk0 + c) * s.n_h + h) * DK * s.dvp;
 #pragma unroll
-    for (int mt = 0; mt < Z::kTiles; ++mt)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int t = 16 * mt + 4 * g + r;
-          raw[mt][n][r] = values.raw(t, col + 16 * n, t < at.live && col + 16 * n < s.d_v);
-        }
-    if (STORE) {
-      float* const to = s.states + head * DK * s.dvp;
-#pragma unroll
-      for (int i = 0; i < Z::kKeyTiles; ++i)
+      for (int i = 0; i < KT; ++i)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (col + 16 * n < s.dvp) to[(int64_t)(16 * i + 4 * g + r) * s.dvp + col + 16 * n] = state[i][n][r];
+            if (col + 16 * n < s.dvp) to[(int64_t)(16 * (wave * KT + i) + 4 * g + r) * s.dvp + col + 16 * n] = state[i][n][r];
     }
-    // K S and Q S
-    f32x4 ks[Z::kTiles][NT] = {}, qs[Z::kTiles][NT] = {};
+  };
+  if (chunks > 0) {
+    load_values(delta_chunk(s, b, 0));
+    load_steps(0);
+    load_keys(0);
+    load_inner(0);
+    load_last(0);
+    write_state(0);
+  }
+  lds_barrier();
+  for (int c = 0; c < chunks; ++c) {
+    const DeltaChunk at = delta_chunk(s, b, c);
+    const int next = min(c + 1, chunks - 1);
+    const int64_t head = (chunk0 + c) * s.n_h + h;
+    since = next_since, until = next_until, beta = next_beta, decay = next_decay;
+    // X = V - exp(G) (K S)
+    f32x4 x[NT] = {}, out[NT] = {};
 #pragma unroll
-    for (int k = 0; k < Z::kKeySteps; ++k) {
-      Pieces<3> right[NT];
+    for (int k = 0; k < KS; ++k)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) right[n] = split_tiles(state[2 * k][n], state[2 * k + 1][n]);
+      for (int n = 0; n < NT; ++n) x[n] = multiply(kf.v[k], for_keys.read(k, n), x[n]);
 #pragma unroll
-      for (int mt = 0; mt < Z::kTiles; ++mt) {
-        const Pieces<NI> left = load_fragment<NI>(kf + (mt * Z::kKeySteps + k) * NI * kFragment);
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) ks[mt][n] = multiply(left, right[n], ks[mt][n]);
-      }
-      if (!STORE) {
+      for (int r = 0; r < 4; ++r) x[n][r] = fmaf(-since[r], x[n][r], DeltaColumns<E>::value(raw[n][r]));
+      for_inner.write(wave, n, x[n] * beta);
+      if (STORE && col + 16 * n < s.dvp) {
 #pragma unroll
-        for (int mt = 0; mt < Z::kTiles; ++mt) {
-          const Pieces<NI> left = load_fragment<NI>(qf + (mt * Z::kKeySteps + k) * NI * kFragment);
-#pragma unroll
-          for (int n = 0; n < NT; ++n) qs[mt][n] = multiply(left, first_pieces<NO>(right[n]), qs[mt][n]);
-        }
-      }
-    }
-    // X, and beta X
-    f32x4 u[Z::kTiles][NT];
-#pragma unroll
-    for (int mt = 0; mt < Z::kTiles; ++mt) {
-      const f32x4 since = *(const f32x4*)(steps + 16 * mt + 4 * g), beta = *(const f32x4*)(steps + kBeta * C + 16 * mt + 4 * g);
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float x = fmaf(-since[r], ks[mt][n][r], DeltaColumns<E>::value(raw[mt][n][r]));
-          ks[mt][n][r] = beta[r] * x;
-          if (STORE && col + 16 * n < s.dvp) s.x[(head * C + 16 * mt + 4 * g + r) * s.dvp + col + 16 * n] = x;
-        }
-    }
-    // U = T (beta X)
-#pragma unroll
-    for (int k = 0; k < Z::kSteps; ++k) {
-      Pieces<3> right[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) right[n] = split_tiles(ks[2 * k][n], ks[2 * k + 1][n]);
-#pragma unroll
-      for (int mt = 2 * k; mt < Z::kTiles; ++mt) {
-        const Pieces<kInner> left = load_fragment<kInner>(tf + (mt * Z::kSteps + k) * kInner * kFragment);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) u[mt][n] = multiply(left, right[n], k == 0 ? f32x4{} : u[mt][n]);
+        for (int r = 0; r < 4; ++r) s.x[(head * kChunk + 16 * wave + 4 * g + r) * s.dvp + col + 16 * n] = x[n][r];
       }
     }
-    // O
+    lds_barrier();
+    // U = T (beta X); Q S meanwhile
+    f32x4 u[NT] = {};
+#pragma unroll
+    for (int n = 0; n < NT; ++n) u[n] = multiply(tf.v[0], for_inner.read(0, n), u[n]);
+    if (wave >= 2) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) u[n] = multiply(tf.v[1], for_inner.read(1, n), u[n]);
+    }
     if (!STORE) {
 #pragma unroll
-      for (int mt = 0; mt < Z::kTiles; ++mt) {
-        const f32x4 since = *(const f32x4*)(steps + 16 * mt + 4 * g);
+      for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) qs[mt][n] *= since * s.scale;
-      }
-#pragma unroll
-      for (int k = 0; k < Z::kSteps; ++k) {
-        Pieces<NO> right[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) right[n] = first_pieces<NO>(split_tiles(u[2 * k][n], u[2 * k + 1][n]));
-#pragma unroll
-        for (int mt = 2 * k; mt < Z::kTiles; ++mt) {
-          const Pieces<NO> left = load_fragment<NO>(pf + (mt * Z::kSteps + k) * kInner * kFragment);
-#pragma unroll
-          for (int n = 0; n < NT; ++n) qs[mt][n] = multiply(left, right[n], qs[mt][n]);
-        }
-      }
-#pragma unroll
-      for (int mt = 0; mt < Z::kTiles; ++mt)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int t = 16 * mt + 4 * g + r;
-            out.store(t, col + 16 * n, t < at.n && col + 16 * n < s.d_v, t < at.live ? qs[mt][n][r] : 0.f);
-          }
-    } else {
-#pragma unroll
-      for (int mt = 0; mt < Z::kTiles; ++mt)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (col + 16 * n < s.dvp) s.u[(head * C + 16 * mt + 4 * g + r) * s.dvp + col + 16 * n] = u[mt][n][r];
-    }
-    // S'
-    const float decay = steps[C - 1];
-#pragma unroll
-    for (int mt = 0; mt < Z::kTiles; ++mt) {
-      const f32x4 until = *(const f32x4*)(steps + kUntil * C + 16 * mt + 4 * g);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) u[mt][n] *= until;
+        for (int n = 0; n < NT; ++n) out[n] = multiply(qf.v[k], first_pieces<NO>(for_keys.read(k, n)), out[n]);
     }
 #pragma unroll
-    for (int i = 0; i < Z::kKeyTiles; ++i)
+    for (int n = 0; n < NT; ++n) {
+      if (!STORE) for_out.write(wave, n, u[n]);
+      for_state.write(wave, n, u[n] * until);
+      if (STORE && col + 16 * n < s.dvp) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s.u[(head * kChunk + 16 * wave + 4 * g + r) * s.dvp + col + 16 * n] = u[n][r];
+      }
+    }
+    load_keys(next);
+    load_inner(next);
+    load_steps(next);
+    load_values(delta_chunk(s, b, next));
+    lds_barrier();
+    // S' = exp(G_C) S + K^T (exp(G_C - G) U)
+#pragma unroll
+    for (int i = 0; i < KT; ++i)
 #pragma unroll
       for (int n = 0; n < NT; ++n) state[i][n] *= decay;
 #pragma unroll
-    for (int k = 0; k < Z::kSteps; ++k) {
-      Pieces<3> right[NT];
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) right[n] = split_tiles(u[2 * k][n], u[2 * k + 1][n]);
+      for (int n = 0; n < NT; ++n) {
+        const Pieces<3> right = for_state.read(k, n);
 #pragma unroll
-      for (int i = 0; i < Z::kKeyTiles; ++i) {
-        const Pieces<NI> left = load_fragment<NI>(ktf + (i * Z::kSteps + k) * NI * kFragment);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) state[i][n] = multiply(left, right[n], state[i][n]);
+        for (int i = 0; i < KT; ++i) state[i][n] = multiply(ktf.v[i * 2 + k], right, state[i][n]);
       }
+    write_state(c + 1);
+    // O = scale exp(G) (Q S) + P U
+    if constexpr (!STORE) {
+      const DeltaColumns<E> to(table[at.p].o, (int64_t)b * at.steps + at.first, s, h);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        out[n] = multiply(pf.v[0], for_out.read(0, n), out[n] * (since * s.scale));
+        if (wave >= 2) out[n] = multiply(pf.v[1], for_out.read(1, n), out[n]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int t = 16 * wave + 4 * g + r;
+          to.store(t, col + 16 * n, t < at.n && col + 16 * n < s.d_v, t < at.live ? out[n][r] : 0.f);
+        }
+      }
+    }
+    load_last(next);
+    lds_barrier();
+  }
+  if (!STORE) {
+    for (int c = chunks; c < s.chunks; ++c) {
+      const DeltaChunk at = delta_chunk(s, b, c);
+      const DeltaColumns<E> to(table[at.p].o, (int64_t)b * at.steps + at.first, s, h);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int t = 16 * wave + 4 * g + r;
+          to.store(t, col + 16 * n, t < at.n && col + 16 * n < s.d_v, 0.f);
+        }
     }
   }
   if (s.hT) {
 #pragma unroll
-    for (int i = 0; i < Z::kKeyTiles; ++i)
+    for (int i = 0; i < KT; ++i)
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int k = 16 * i + 4 * g + r, v = col + 16 * n;
+          const int k = 16 * (wave * KT + i) + 4 * g + r, v = col + 16 * n;
           if (k < s.d_k && v < s.d_v) s.hT[state_at + (int64_t)k * s.d_v + v] = state[i][n][r];
         }
   }
 }
 
-// The gradient of the state, backwards through the chunks:
+// The gradient of the state, backwards through the chunks, in the same way:
 //   dU = P^T dO + exp(G_C - G) (K dS'),  dR = T^T dU,  dS = exp(G_C) dS' + Q^T (scale exp(G) dO) - K^T (exp(G) beta dR)
 // with R = beta X.  dS' and dR are kept for the kernel behind it.
-template <class E, int C, int DK, int NT>
-__global__ __launch_bounds__(64, 1) void delta_bwd_kernel(DeltaArgs s) {
-  typedef DeltaSizes<C, DK> Z;
-  constexpr int NI = delta_pieces<E>();
+template <class E, int DK, int NT>
+__global__ __launch_bounds__(256, 1) void delta_bwd_kernel(DeltaArgs s) {
+  typedef DeltaSizes<kChunk, DK> Z;
+  constexpr int NI = delta_pieces<E>(), KT = DK / 64, KS = Z::kKeySteps;
+  __shared__ DeltaShared<KS, NT, 3> for_keys;
+  __shared__ DeltaShared<2, NT, NI> for_out[2];      // dO, by turns
+  __shared__ DeltaShared<2, NT, 3> for_queries[2];   // scale exp(G) dO, by turns
+  __shared__ DeltaShared<2, NT, 3> for_inner, for_state;
   const DeltaTable table = DELTA_TABLE(s);
-  const int lane = threadIdx.x, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4;
   const DeltaChain chain = delta_chain<NT>(s);
   const int b = chain.b, h = chain.h, hk = h / s.each, col = chain.col + (lane & 15);
-  f32x4 state[Z::kKeyTiles][NT];  // dS
+  f32x4 state[KT][NT];  // dS
   const int64_t state_at = ((int64_t)b * s.n_h + h) * s.d_k * s.d_v;
 #pragma unroll
-  for (int i = 0; i < Z::kKeyTiles; ++i)
+  for (int i = 0; i < KT; ++i)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int k = 16 * i + 4 * g + r, v = col + 16 * n;
+        const int k = 16 * (wave * KT + i) + 4 * g + r, v = col + 16 * n;
         state[i][n][r] = s.dhT && k < s.d_k && v < s.d_v ? s.dhT[state_at + (int64_t)k * s.d_v + v] : 0.f;
       }
+  const int chunks = delta_live_chunks(s, b);
+  const int64_t chunk0 = (int64_t)b * s.chunks;
 
-  for (int c = s.chunks - 1; c >= 0; --c) {
-    const DeltaChunk at = delta_chunk<C>(s, b, c);
-    if (at.live == 0) continue;
-    const int64_t step0 = (int64_t)b * at.steps + at.first;
-    const int64_t key_at = (((int64_t)b * s.chunks + c) * s.n_hk + hk) * Z::kKeyPiece * NI;
-    const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h, step_at = head * Z::kStepPiece * kInner;
-    const uint16_t *const kf = s.kf + key_at, *const ktf = s.ktf + key_at, *const qtf = s.qtf + key_at, *const ttf = s.ttf + step_at, *const ptf = s.ptf + step_at;
-    const float* const steps = s.steps + head * kStepNumbers * C;
-    const DeltaColumns<E> grads(table[at.p].d_o, step0, s, h);
-    f32x4 d_o[Z::kTiles][NT];
+  DeltaFragments<KS, NI> kf;
+  DeltaFragments<2, kInner> ttf, ptf;
+  DeltaFragments<2 * KT, NI> ktf, qtf;
+  f32x4 since, until, beta, next_since, next_until, next_beta;
+  float decay, next_decay;
+  uint32_t raw[NT][4];
+  auto load_first = [&](int c) {
+    kf.template load<NI>(s.kf + ((chunk0 + c) * s.n_hk + hk) * Z::kKeyPiece * NI, wave * KS);
+    ptf.template load<kInner>(s.ptf + ((chunk0 + c) * s.n_h + h) * Z::kStepPiece * kInner, wave * 2);
+  };
+  auto load_inner = [&](int c) { ttf.template load<kInner>(s.ttf + ((chunk0 + c) * s.n_h + h) * Z::kStepPiece * kInner, wave * 2); };
+  auto load_last = [&](int c) {
+    const int64_t at = ((chunk0 + c) * s.n_hk + hk) * Z::kKeyPiece * NI;
+    ktf.template load<NI>(s.ktf + at, wave * KT * 2);
+    qtf.template load<NI>(s.qtf + at, wave * KT * 2);
+  };
+  auto load_steps = [&](int c) {
+    const float* const at = s.steps + ((chunk0 + c) * s.n_h + h) * kStepNumbers * kChunk + 16 * wave + 4 * g;
+    next_since = *(const f32x4*)(at + kSince * kChunk);
+    next_until = *(const f32x4*)(at + kUntil * kChunk);
+    next_beta = *(const f32x4*)(at + kBeta * kChunk);
+    next_decay = s.steps[((chunk0 + c) * s.n_h + h) * kStepNumbers * kChunk + kChunk - 1];
+  };
+  auto load_grads = [&](const DeltaChunk& at) {
+    const DeltaColumns<E> grads(table[at.p].d_o, (int64_t)b * at.steps + at.first, s, h);
 #pragma unroll
-    for (int mt = 0; mt < Z::kTiles; ++mt)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int r = 0; r < 4; ++r) {
+        const int t = 16 * wave + 4 * g + r;
+        raw[n][r] = grads.raw(t, col + 16 * n, t < at.live && col + 16 * n < s.d_v);
+      }
+  };
+  auto write_grads = [&](int turn) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int t = 16 * mt + 4 * g + r;
-          d_o[mt][n][r] = grads.load(t, col + 16 * n, t < at.live && col + 16 * n < s.d_v);
-        }
-    {
-      float* const to = s.dstates + head * DK * s.dvp;
+    for (int n = 0; n < NT; ++n) {
+      f32x4 v;
 #pragma unroll
-      for (int i = 0; i < Z::kKeyTiles; ++i)
+      for (int r = 0; r < 4; ++r) v[r] = DeltaColumns<E>::value(raw[n][r]);
+      for_out[turn].write(wave, n, v);  // (bf16 numbers are their upper halves)
+      for_queries[turn].write(wave, n, v * (next_since * s.scale));
+    }
+  };
+  auto write_state = [&](int c) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if constexpr (KT == 2) for_keys.write(wave, n, state[0][n], state[1][n]);
+      else for_keys.write(wave, n, state[0][n]);
+    }
+    if (c >= 0) {
+      float* const to = s.dstates + ((chunk0 + c) * s.n_h + h) * DK * s.dvp;
+#pragma unroll
+      for (int i = 0; i < KT; ++i)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (col + 16 * n < s.dvp) to[(int64_t)(16 * i + 4 * g + r) * s.dvp + col + 16 * n] = state[i][n][r];
+            if (col + 16 * n < s.dvp) to[(int64_t)(16 * (wave * KT + i) + 4 * g + r) * s.dvp + col + 16 * n] = state[i][n][r];
     }
-    f32x4 du[Z::kTiles][NT] = {}, dr[Z::kTiles][NT];
+  };
+  if (chunks > 0) {
+    const int c = chunks - 1;
+    load_grads(delta_chunk(s, b, c));
+    load_steps(c);
+    load_first(c);
+    load_inner(c);
+    load_last(c);
+    write_grads(c & 1);
+    write_state(c);
+  }
+  lds_barrier();
+  for (int c = chunks - 1; c >= 0; --c) {
+    const int next = max(c - 1, 0);
+    const int64_t head = (chunk0 + c) * s.n_h + h;
+    since = next_since, until = next_until, beta = next_beta, decay = next_decay;
+    load_grads(delta_chunk(s, b, next));
+    load_steps(next);
+    f32x4 u[NT] = {};
 #pragma unroll
-    for (int k = 0; k < Z::kKeySteps; ++k) {
-      Pieces<3> right[NT];
+    for (int k = 0; k < KS; ++k)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) right[n] = split_tiles(state[2 * k][n], state[2 * k + 1][n]);
+      for (int n = 0; n < NT; ++n) u[n] = multiply(kf.v[k], for_keys.read(k, n), u[n]);
 #pragma unroll
-      for (int mt = 0; mt < Z::kTiles; ++mt) {
-        const Pieces<NI> left = load_fragment<NI>(kf + (mt * Z::kKeySteps + k) * NI * kFragment);
+    for (int n = 0; n < NT; ++n) {
+      u[n] *= until;
+      u[n] = multiply(ptf.v[1], for_out[c & 1].read(1, n), u[n]);
+      if (wave < 2) u[n] = multiply(ptf.v[0], for_out[c & 1].read(0, n), u[n]);
+      for_inner.write(wave, n, u[n]);
+    }
+    load_first(next);
+    lds_barrier();
+    f32x4 r_[NT] = {};
 #pragma unroll
-        for (int n = 0; n < NT; ++n) du[mt][n] = multiply(left, right[n], du[mt][n]);
+    for (int n = 0; n < NT; ++n) {
+      r_[n] = multiply(ttf.v[1], for_inner.read(1, n), r_[n]);
+      if (wave < 2) r_[n] = multiply(ttf.v[0], for_inner.read(0, n), r_[n]);
+      for_state.write(wave, n, r_[n] * -(since * beta));
+      if (col + 16 * n < s.dvp) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s.dr[(head * kChunk + 16 * wave + 4 * g + r) * s.dvp + col + 16 * n] = r_[n][r];
       }
     }
 #pragma unroll
-    for (int mt = 0; mt < Z::kTiles; ++mt) {
-      const f32x4 until = *(const f32x4*)(steps + kUntil * C + 16 * mt + 4 * g);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) du[mt][n] *= until;
-    }
-#pragma unroll
-    for (int k = 0; k < Z::kSteps; ++k) {
-      Pieces<NI> right[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) right[n] = first_pieces<NI>(split_tiles(d_o[2 * k][n], d_o[2 * k + 1][n]));  // (bf16 numbers are their upper halves)
-#pragma unroll
-      for (int mt = 0; mt < Z::kTiles && mt < 2 * k + 2; ++mt) {
-        const Pieces<kInner> left = load_fragment<kInner>(ptf + (mt * Z::kSteps + k) * kInner * kFragment);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) du[mt][n] = multiply(left, right[n], du[mt][n]);
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < Z::kSteps; ++k) {
-      Pieces<3> right[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) right[n] = split_tiles(du[2 * k][n], du[2 * k + 1][n]);
-#pragma unroll
-      for (int mt = 0; mt < Z::kTiles && mt < 2 * k + 2; ++mt) {
-        const Pieces<kInner> left = load_fragment<kInner>(ttf + (mt * Z::kSteps + k) * kInner * kFragment);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) dr[mt][n] = multiply(left, right[n], mt >= 2 * k ? f32x4{} : dr[mt][n]);
-      }
-    }
-    const float decay = steps[C - 1];
-#pragma unroll
-    for (int i = 0; i < Z::kKeyTiles; ++i)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) state[i][n] *= decay;
-#pragma unroll
-    for (int mt = 0; mt < Z::kTiles; ++mt) {
-      const f32x4 since = *(const f32x4*)(steps + 16 * mt + 4 * g), beta = *(const f32x4*)(steps + kBeta * C + 16 * mt + 4 * g);
+    for (int i = 0; i < KT; ++i)
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
+        state[i][n] *= decay;
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (col + 16 * n < s.dvp) s.dr[(head * C + 16 * mt + 4 * g + r) * s.dvp + col + 16 * n] = dr[mt][n][r];
-        d_o[mt][n] *= since * s.scale;
-        dr[mt][n] *= -(since * beta);
+        for (int k = 0; k < 2; ++k) state[i][n] = multiply(qtf.v[i * 2 + k], for_queries[c & 1].read(k, n), state[i][n]);
       }
-    }
+    load_inner(next);
+    lds_barrier();
 #pragma unroll
-    for (int k = 0; k < Z::kSteps; ++k) {
-      Pieces<3> one[NT], two[NT];
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        one[n] = split_tiles(d_o[2 * k][n], d_o[2 * k + 1][n]);
-        two[n] = split_tiles(dr[2 * k][n], dr[2 * k + 1][n]);
-      }
+        const Pieces<3> right = for_state.read(k, n);
 #pragma unroll
-      for (int i = 0; i < Z::kKeyTiles; ++i) {
-        const Pieces<NI> q = load_fragment<NI>(qtf + (i * Z::kSteps + k) * NI * kFragment), kk = load_fragment<NI>(ktf + (i * Z::kSteps + k) * NI * kFragment);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) state[i][n] = multiply(kk, two[n], multiply(q, one[n], state[i][n]));
+        for (int i = 0; i < KT; ++i) state[i][n] = multiply(ktf.v[i * 2 + k], right, state[i][n]);
       }
-    }
+    write_state(c - 1);
+    write_grads((c & 1) ^ 1);
+    load_last(next);
+    lds_barrier();
   }
   if (s.dh0) {
 #pragma unroll
-    for (int i = 0; i < Z::kKeyTiles; ++i)
+    for (int i = 0; i < KT; ++i)
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int k = 16 * i + 4 * g + r, v = col + 16 * n;
+          const int k = 16 * (wave * KT + i) + 4 * g + r, v = col + 16 * n;
           if (k < s.d_k && v < s.d_v) s.dh0[state_at + (int64_t)k * s.d_v + v] = state[i][n][r];
         }
   }
@@ -646,7 +712,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
   const int kt = wave % Z::kKeyTiles, mt0 = wave / Z::kKeyTiles * kMine, key = kt * 16 + row;
   const int hk = blockIdx.x % (uint32_t)s.n_hk, at_chunk = blockIdx.x / (uint32_t)s.n_hk;
   const int c = at_chunk % s.chunks, b = at_chunk / s.chunks;
-  const DeltaChunk at = delta_chunk<C>(s, b, c);
+  const DeltaChunk at = delta_chunk(s, b, c);
   const DeltaTable w = table + at.p;
   const int64_t step0 = (int64_t)b * at.steps + at.first;
   E* const dq = (E*)w->dq, * const dk = (E*)w->dk, * const dv = (E*)w->dv;
@@ -1021,7 +1087,7 @@ static int delta_args(distdl_delta_plan* p, const std::vector<DeltaWorker>& w, h
     if (rc) return rc;
     s->more = p->table.dev;
   }
-  const int C = p->dtype == DISTDL_F32 ? delta_chunk_steps<float>() : delta_chunk_steps<uint16_t>();
+  constexpr int C = kChunk;
   s->P = p->P;
   s->T = p->T;
   s->part = p->T / p->P;
@@ -1041,8 +1107,9 @@ static int delta_args(distdl_delta_plan* p, const std::vector<DeltaWorker>& w, h
 }
 
 // The scratch of a call, one array behind the other at multiples of 256 bytes.
-template <class E, int C, int DK>
+template <class E, int DK>
 static int delta_scratch(distdl_delta_plan* p, bool back, hipStream_t st, DeltaArgs* s) {
+  constexpr int C = kChunk;
   typedef DeltaSizes<C, DK> Z;
   const size_t keys = (size_t)s->n_b * s->chunks * s->n_hk, heads = (size_t)s->n_b * s->chunks * s->n_h;
   const size_t key = keys * Z::kKeyPiece * delta_pieces<E>() * 2, step = heads * Z::kStepPiece * kInner * 2, state = heads * DK * s->dvp * 4,
@@ -1075,24 +1142,25 @@ static int delta_scratch(distdl_delta_plan* p, bool back, hipStream_t st, DeltaA
   return DISTDL_OK;
 }
 
-template <class E, int C, int DK, bool BACK>
+template <class E, int DK, bool BACK>
 static int launch_delta(distdl_delta_plan* p, DeltaArgs& s, hipStream_t st) {
-  int rc = delta_scratch<E, C, DK>(p, BACK, st, &s);
+  constexpr int C = kChunk;
+  int rc = delta_scratch<E, DK>(p, BACK, st, &s);
   if (rc) return rc;
   constexpr auto prepare = delta_prepare_kernel<E, C, DK, BACK>;
   if ((rc = allow_large_lds<prepare>())) return rc;
   const dim3 chunks((unsigned)((int64_t)s.n_b * s.chunks * s.n_hk));
   hipLaunchKernelGGL(prepare, chunks, dim3(256), sizeof(DeltaPrepareShared<E, C, DK>), st, s);
-  // A wave takes 32 columns where that many waves fill the card: it reads the chunks' matrices half as often.
+  // A workgroup takes 32 columns where there are more than enough for two on each compute unit: it reads the chunks' matrices half as often.
   const int64_t chains = (int64_t)s.n_b * s.n_h;
-  const bool two = s.d_v > 16 && chains * ((s.d_v + 31) / 32) >= 1024;
+  const bool two = s.d_v > 16 && chains * ((s.d_v + 15) / 16) > 512;
   s.slices = two ? (s.d_v + 31) / 32 : (s.d_v + 15) / 16;
-  const dim3 waves((unsigned)(chains * s.slices));
-  if (two) hipLaunchKernelGGL((delta_fwd_kernel<E, C, DK, 2, BACK>), waves, dim3(64), 0, st, s);
-  else hipLaunchKernelGGL((delta_fwd_kernel<E, C, DK, 1, BACK>), waves, dim3(64), 0, st, s);
+  const dim3 groups((unsigned)(chains * s.slices));
+  if (two) hipLaunchKernelGGL((delta_fwd_kernel<E, DK, 2, BACK>), groups, dim3(256), 0, st, s);
+  else hipLaunchKernelGGL((delta_fwd_kernel<E, DK, 1, BACK>), groups, dim3(256), 0, st, s);
   if constexpr (BACK) {
-    if (two) hipLaunchKernelGGL((delta_bwd_kernel<E, C, DK, 2>), waves, dim3(64), 0, st, s);
-    else hipLaunchKernelGGL((delta_bwd_kernel<E, C, DK, 1>), waves, dim3(64), 0, st, s);
+    if (two) hipLaunchKernelGGL((delta_bwd_kernel<E, DK, 2>), groups, dim3(256), 0, st, s);
+    else hipLaunchKernelGGL((delta_bwd_kernel<E, DK, 1>), groups, dim3(256), 0, st, s);
     constexpr auto grad = delta_grad_kernel<E, C, DK>;
     if ((rc = allow_large_lds<grad>())) return rc;
     hipLaunchKernelGGL(grad, chunks, dim3(512), sizeof(DeltaGradShared<E, C, DK>), st, s);
@@ -1103,10 +1171,8 @@ static int launch_delta(distdl_delta_plan* p, DeltaArgs& s, hipStream_t st) {
 template <bool BACK>
 static int launch_delta(distdl_delta_plan* p, DeltaArgs& s, hipStream_t st) {
   const bool wide = p->d_k > 64;
-  if (p->dtype == DISTDL_F32)
-    return wide ? launch_delta<float, delta_chunk_steps<float>(), 128, BACK>(p, s, st) : launch_delta<float, delta_chunk_steps<float>(), 64, BACK>(p, s, st);
-  return wide ? launch_delta<uint16_t, delta_chunk_steps<uint16_t>(), 128, BACK>(p, s, st)
-              : launch_delta<uint16_t, delta_chunk_steps<uint16_t>(), 64, BACK>(p, s, st);
+  if (p->dtype == DISTDL_F32) return wide ? launch_delta<float, 128, BACK>(p, s, st) : launch_delta<float, 64, BACK>(p, s, st);
+  return wide ? launch_delta<uint16_t, 128, BACK>(p, s, st) : launch_delta<uint16_t, 64, BACK>(p, s, st);
 }
 
 template <class E, int V, int Q>
@@ -1153,7 +1219,7 @@ int distdl_delta_plan_create(distdl_delta_plan** out, int64_t n_b, int64_t T, in
   const int rc = delta_sizes("delta_plan_create", n_h, n_hk, d_k, d_v, scale, dtype);
   if (rc) return rc;
   if (T < P) return set_error(DISTDL_ERR_EMPTY_PARTITION, "delta: %lld steps over %d workers", (long long)T, P);
-  if (T >= int64_t(1) << 30 || n_b >= 1 << 20 || n_b * (T / 32 + P) >= kMaxBlocks256 / n_hk / 2 || n_b * n_h * ((d_v + 15) / 16) >= kMaxBlocks256)
+  if (T >= int64_t(1) << 30 || n_b >= 1 << 20 || n_b * (T / kChunk + P) >= kMaxBlocks256 / n_hk / 2 || n_b * n_h * ((d_v + 15) / 16) >= kMaxBlocks256)
     return set_error(DISTDL_ERR_UNSUPPORTED, "delta: problem too large");
   return guarded([&]() -> int {
     std::unique_ptr<distdl_delta_plan> p(new distdl_delta_plan());
