@@ -82,14 +82,54 @@ __device__ __forceinline__ DeltaChunk delta_chunk(const DeltaArgs& s, int b, int
   return r;
 }
 
-// How many chunks have steps inside sequence b; they come first.
-__device__ __forceinline__ int delta_live_chunks(const DeltaArgs& s, int b) {
-  const int len = s.lengths ? max(0, min(s.lengths[b], s.T)) : s.T;
+__device__ __forceinline__ int delta_length(const DeltaArgs& s, int b) {
+  return __builtin_amdgcn_readfirstlane(s.lengths ? max(0, min(s.lengths[b], s.T)) : s.T);
+}
+// How many chunks have some of a sequence's steps; they come first.
+__device__ __forceinline__ int delta_live_chunks(const DeltaArgs& s, int len) {
   if (len == 0) return 0;
   const int last = len - 1, wide = s.extra * (s.part + 1);
   if (last < wide) return last / (s.part + 1) * s.chunks_wide + last % (s.part + 1) / kChunk + 1;
   return s.extra * s.chunks_wide + (last - wide) / s.part * s.chunks_rest + (last - wide) % s.part / kChunk + 1;
 }
+
+// A walk along the chunks that reads nothing but a worker's pointers, where it comes to another worker: two of its arrays.
+struct DeltaWalk {
+  int32_t p, first, steps, before;  // before: the worker's first step
+  const char *one, *two;
+  template <class F>
+  __device__ __forceinline__ void enter(const DeltaArgs& s, int worker, F pointers) {
+    p = worker;
+    steps = s.part + (p < s.extra);
+    before = p * s.part + min(p, s.extra);
+    pointers(p, one, two);
+  }
+  template <class F>
+  __device__ __forceinline__ void start(const DeltaArgs& s, int c, F pointers) {
+    const int wide = s.extra * s.chunks_wide;
+    const int worker = c < wide ? c / s.chunks_wide : s.extra + (c - wide) / s.chunks_rest;
+    enter(s, worker, pointers);
+    first = (c < wide ? c % s.chunks_wide : (c - wide) % s.chunks_rest) * kChunk;
+  }
+  template <class F>
+  __device__ __forceinline__ void ahead(const DeltaArgs& s, F pointers) {
+    first += kChunk;
+    if (first >= steps) {
+      enter(s, p + 1, pointers);
+      first = 0;
+    }
+  }
+  template <class F>
+  __device__ __forceinline__ void back(const DeltaArgs& s, F pointers) {
+    first -= kChunk;
+    if (first < 0) {
+      enter(s, p - 1, pointers);
+      first = (steps - 1) / kChunk * kChunk;
+    }
+  }
+  __device__ __forceinline__ int count() const { return min(kChunk, steps - first); }
+  __device__ __forceinline__ int live(int len) const { return max(0, min(count(), len - before - first)); }
+};
 
 // ---- operand pieces -------------------------------------------------------
 typedef __bf16 delta_bf16x8 __attribute__((ext_vector_type(8)));

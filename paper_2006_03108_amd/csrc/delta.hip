@@ -283,6 +283,26 @@ struct DeltaShared {
     for (int i = 0; i < N; ++i) o.p[i] = v[k][n][i][threadIdx.x & 63];
     return o;
   }
+  // c[n] += left b for the `count` steps from `first` on: all of b is read before the first product, which the compiler would otherwise make wait
+  // for one read after the other
+  template <int COUNT, int NA>
+  __device__ __forceinline__ void multiply_into(const Pieces<NA>* left, int first, f32x4 (&c)[NT]) const {
+    Pieces<N> right[COUNT][NT];
+#pragma unroll
+    for (int k = 0; k < COUNT; ++k)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) right[k][n] = read(first + k, n);
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 odd[NT] = {};
+#pragma unroll
+    for (int k = 0; k < COUNT; ++k)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) (k & 1 ? odd : c)[n] = multiply(left[k], right[k][n], (k & 1 ? odd : c)[n]);
+    if (COUNT > 1) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) c[n] += odd[n];
+    }
+  }
   // tile `tile` of 16 rows: half of a step
   __device__ __forceinline__ void write(int tile, int n, f32x4 x) {
     const Pieces<3> p = split_tiles(x, f32x4{});
@@ -307,12 +327,33 @@ struct DeltaFragments {
   }
 };
 
+// Whether two workgroups share a compute unit: 256 registers each are enough.
+template <class E, int DK, int NT, bool BACK>
+constexpr int delta_two_groups() { return (sizeof(E) == 2 ? DK == 64 || NT == 1 || !BACK : DK == 64 && NT == 1) ? 2 : 1; }
+
+// A wave's rows of the state += left b
+template <int KT, int NT, int NA>
+__device__ __forceinline__ void delta_state(const DeltaShared<2, NT, 3>& b, const Pieces<NA>* left, f32x4 (&state)[KT][NT]) {
+  Pieces<3> right[2][NT];
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) right[k][n] = b.read(k, n);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < KT; ++i) state[i][n] = multiply(left[i * 2 + k], right[k][n], state[i][n]);
+}
+
 // A workgroup of four waves takes 16 NT columns of a head's state through all chunks.  Wave w has the tile of steps 16 w .. 16 w + 15 of every product
 // over keys or steps, and a quarter of the state's rows, so the chunk's matrices are read by one wave each, straight into the registers that the
 // last chunk's have left: every load has most of a chunk's time.  What the waves make for each other, in pieces, goes through LDS: the state, beta X and
 // U, a barrier for each, which waits for LDS alone (lds_barrier).
 template <class E, int DK, int NT, bool STORE>
-__global__ __launch_bounds__(256, 1) void delta_fwd_kernel(DeltaArgs s) {
+__global__ __launch_bounds__(256, (delta_two_groups<E, DK, NT, false>())) void delta_fwd_kernel(DeltaArgs s) {
   typedef DeltaSizes<kChunk, DK> Z;
   constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>(), KT = DK / 64, KS = Z::kKeySteps;
   __shared__ DeltaShared<KS, NT, 3> for_keys;
@@ -333,7 +374,7 @@ __global__ __launch_bounds__(256, 1) void delta_fwd_kernel(DeltaArgs s) {
         const int k = 16 * (wave * KT + i) + 4 * g + r, v = col + 16 * n;
         state[i][n][r] = s.h0 && k < s.d_k && v < s.d_v ? s.h0[state_at + (int64_t)k * s.d_v + v] : 0.f;
       }
-  const int chunks = delta_live_chunks(s, b);
+  const int len = delta_length(s, b), chunks = delta_live_chunks(s, len);
   const int64_t chunk0 = (int64_t)b * s.chunks;
 
   DeltaFragments<KS, NI> kf, qf;
@@ -360,14 +401,17 @@ __global__ __launch_bounds__(256, 1) void delta_fwd_kernel(DeltaArgs s) {
     next_beta = *(const f32x4*)(at + kBeta * kChunk);
     next_decay = s.steps[((chunk0 + c) * s.n_h + h) * kStepNumbers * kChunk + kChunk - 1];
   };
-  auto load_values = [&](const DeltaChunk& at) {
-    const DeltaColumns<E> values(table[at.p].v, (int64_t)b * at.steps + at.first, s, h);
+  auto pointers = [&](int p, const char*& one, const char*& two) { one = (const char*)table[p].v, two = (const char*)table[p].o; };
+  DeltaWalk walk;
+  auto load_values = [&]() {
+    const DeltaColumns<E> values(walk.one, (int64_t)b * walk.steps + walk.first, s, h);
+    const int live = walk.live(len);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int t = 16 * wave + 4 * g + r;
-        raw[n][r] = values.raw(t, col + 16 * n, t < at.live && col + 16 * n < s.d_v);
+        raw[n][r] = values.raw(t, col + 16 * n, t < live && col + 16 * n < s.d_v);
       }
   };
   auto write_state = [&](int c) {
@@ -388,25 +432,24 @@ __global__ __launch_bounds__(256, 1) void delta_fwd_kernel(DeltaArgs s) {
     }
   };
   if (chunks > 0) {
-    load_values(delta_chunk(s, b, 0));
+    walk.start(s, 0, pointers);
+    load_values();
     load_steps(0);
     load_keys(0);
     load_inner(0);
     load_last(0);
     write_state(0);
   }
+  __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);  // (so that the loop's waits count its own loads alone)
   lds_barrier();
   for (int c = 0; c < chunks; ++c) {
-    const DeltaChunk at = delta_chunk(s, b, c);
-    const int next = min(c + 1, chunks - 1);
+    const int next = min(c + 1, chunks - 1), count = walk.count(), live = walk.live(len);
+    const DeltaColumns<E> to(walk.two, (int64_t)b * walk.steps + walk.first, s, h);
     const int64_t head = (chunk0 + c) * s.n_h + h;
     since = next_since, until = next_until, beta = next_beta, decay = next_decay;
     // X = V - exp(G) (K S)
     f32x4 x[NT] = {}, out[NT] = {};
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) x[n] = multiply(kf.v[k], for_keys.read(k, n), x[n]);
+    for_keys.template multiply_into<KS>(kf.v, 0, x);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -420,18 +463,8 @@ __global__ __launch_bounds__(256, 1) void delta_fwd_kernel(DeltaArgs s) {
     lds_barrier();
     // U = T (beta X); Q S meanwhile
     f32x4 u[NT] = {};
-#pragma unroll
-    for (int n = 0; n < NT; ++n) u[n] = multiply(tf.v[0], for_inner.read(0, n), u[n]);
-    if (wave >= 2) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n) u[n] = multiply(tf.v[1], for_inner.read(1, n), u[n]);
-    }
-    if (!STORE) {
-#pragma unroll
-      for (int k = 0; k < KS; ++k)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) out[n] = multiply(qf.v[k], first_pieces<NO>(for_keys.read(k, n)), out[n]);
-    }
+    if (wave >= 2) for_inner.template multiply_into<2>(tf.v, 0, u);
+    else for_inner.template multiply_into<1>(tf.v, 0, u);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       if (!STORE) for_out.write(wave, n, u[n]);
@@ -441,36 +474,40 @@ __global__ __launch_bounds__(256, 1) void delta_fwd_kernel(DeltaArgs s) {
         for (int r = 0; r < 4; ++r) s.u[(head * kChunk + 16 * wave + 4 * g + r) * s.dvp + col + 16 * n] = u[n][r];
       }
     }
+    if constexpr (!STORE) {
+      f32x4 odd[NT] = {};
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) (k & 1 ? odd : out)[n] = multiply(qf.v[k], first_pieces<NO>(for_keys.read(k, n)), (k & 1 ? odd : out)[n]);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) out[n] += odd[n];
+    }
     load_keys(next);
     load_inner(next);
     load_steps(next);
-    load_values(delta_chunk(s, b, next));
+    if (next > c) walk.ahead(s, pointers);
+    load_values();
     lds_barrier();
     // S' = exp(G_C) S + K^T (exp(G_C - G) U)
 #pragma unroll
     for (int i = 0; i < KT; ++i)
 #pragma unroll
       for (int n = 0; n < NT; ++n) state[i][n] *= decay;
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const Pieces<3> right = for_state.read(k, n);
-#pragma unroll
-        for (int i = 0; i < KT; ++i) state[i][n] = multiply(ktf.v[i * 2 + k], right, state[i][n]);
-      }
+    delta_state<KT, NT>(for_state, ktf.v, state);
     write_state(c + 1);
     // O = scale exp(G) (Q S) + P U
     if constexpr (!STORE) {
-      const DeltaColumns<E> to(table[at.p].o, (int64_t)b * at.steps + at.first, s, h);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) out[n] *= since * s.scale;
+      if (wave >= 2) for_out.template multiply_into<2>(pf.v, 0, out);
+      else for_out.template multiply_into<1>(pf.v, 0, out);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        out[n] = multiply(pf.v[0], for_out.read(0, n), out[n] * (since * s.scale));
-        if (wave >= 2) out[n] = multiply(pf.v[1], for_out.read(1, n), out[n]);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int t = 16 * wave + 4 * g + r;
-          to.store(t, col + 16 * n, t < at.n && col + 16 * n < s.d_v, t < at.live ? out[n][r] : 0.f);
+          to.store(t, col + 16 * n, t < count && col + 16 * n < s.d_v, t < live ? out[n][r] : 0.f);
         }
       }
     }
@@ -507,7 +544,7 @@ __global__ __launch_bounds__(256, 1) void delta_fwd_kernel(DeltaArgs s) {
 //   dU = P^T dO + exp(G_C - G) (K dS'),  dR = T^T dU,  dS = exp(G_C) dS' + Q^T (scale exp(G) dO) - K^T (exp(G) beta dR)
 // with R = beta X.  dS' and dR are kept for the kernel behind it.
 template <class E, int DK, int NT>
-__global__ __launch_bounds__(256, 1) void delta_bwd_kernel(DeltaArgs s) {
+__global__ __launch_bounds__(256, (delta_two_groups<E, DK, NT, true>())) void delta_bwd_kernel(DeltaArgs s) {
   typedef DeltaSizes<kChunk, DK> Z;
   constexpr int NI = delta_pieces<E>(), KT = DK / 64, KS = Z::kKeySteps;
   __shared__ DeltaShared<KS, NT, 3> for_keys;
@@ -529,7 +566,7 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_kernel(DeltaArgs s) {
         const int k = 16 * (wave * KT + i) + 4 * g + r, v = col + 16 * n;
         state[i][n][r] = s.dhT && k < s.d_k && v < s.d_v ? s.dhT[state_at + (int64_t)k * s.d_v + v] : 0.f;
       }
-  const int chunks = delta_live_chunks(s, b);
+  const int len = delta_length(s, b), chunks = delta_live_chunks(s, len);
   const int64_t chunk0 = (int64_t)b * s.chunks;
 
   DeltaFragments<KS, NI> kf;
@@ -555,14 +592,17 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_kernel(DeltaArgs s) {
     next_beta = *(const f32x4*)(at + kBeta * kChunk);
     next_decay = s.steps[((chunk0 + c) * s.n_h + h) * kStepNumbers * kChunk + kChunk - 1];
   };
-  auto load_grads = [&](const DeltaChunk& at) {
-    const DeltaColumns<E> grads(table[at.p].d_o, (int64_t)b * at.steps + at.first, s, h);
+  auto pointers = [&](int p, const char*& one, const char*& two) { one = two = (const char*)table[p].d_o; };
+  DeltaWalk walk;
+  auto load_grads = [&]() {
+    const DeltaColumns<E> grads(walk.one, (int64_t)b * walk.steps + walk.first, s, h);
+    const int live = walk.live(len);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int t = 16 * wave + 4 * g + r;
-        raw[n][r] = grads.raw(t, col + 16 * n, t < at.live && col + 16 * n < s.d_v);
+        raw[n][r] = grads.raw(t, col + 16 * n, t < live && col + 16 * n < s.d_v);
       }
   };
   auto write_grads = [&](int turn) {
@@ -594,7 +634,8 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_kernel(DeltaArgs s) {
   };
   if (chunks > 0) {
     const int c = chunks - 1;
-    load_grads(delta_chunk(s, b, c));
+    walk.start(s, c, pointers);
+    load_grads();
     load_steps(c);
     load_first(c);
     load_inner(c);
@@ -602,32 +643,30 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_kernel(DeltaArgs s) {
     write_grads(c & 1);
     write_state(c);
   }
+  __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);  // (so that the loop's waits count its own loads alone)
   lds_barrier();
   for (int c = chunks - 1; c >= 0; --c) {
     const int next = max(c - 1, 0);
     const int64_t head = (chunk0 + c) * s.n_h + h;
     since = next_since, until = next_until, beta = next_beta, decay = next_decay;
-    load_grads(delta_chunk(s, b, next));
+    if (next < c) walk.back(s, pointers);
+    load_grads();
     load_steps(next);
     f32x4 u[NT] = {};
+    for_keys.template multiply_into<KS>(kf.v, 0, u);
 #pragma unroll
-    for (int k = 0; k < KS; ++k)
+    for (int n = 0; n < NT; ++n) u[n] *= until;
+    if (wave < 2) for_out[c & 1].template multiply_into<2>(ptf.v, 0, u);
+    else for_out[c & 1].template multiply_into<1>(ptf.v + 1, 1, u);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) u[n] = multiply(kf.v[k], for_keys.read(k, n), u[n]);
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      u[n] *= until;
-      u[n] = multiply(ptf.v[1], for_out[c & 1].read(1, n), u[n]);
-      if (wave < 2) u[n] = multiply(ptf.v[0], for_out[c & 1].read(0, n), u[n]);
-      for_inner.write(wave, n, u[n]);
-    }
+    for (int n = 0; n < NT; ++n) for_inner.write(wave, n, u[n]);
     load_first(next);
     lds_barrier();
     f32x4 r_[NT] = {};
+    if (wave < 2) for_inner.template multiply_into<2>(ttf.v, 0, r_);
+    else for_inner.template multiply_into<1>(ttf.v + 1, 1, r_);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      r_[n] = multiply(ttf.v[1], for_inner.read(1, n), r_[n]);
-      if (wave < 2) r_[n] = multiply(ttf.v[0], for_inner.read(0, n), r_[n]);
       for_state.write(wave, n, r_[n] * -(since * beta));
       if (col + 16 * n < s.dvp) {
 #pragma unroll
@@ -637,21 +676,11 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_kernel(DeltaArgs s) {
 #pragma unroll
     for (int i = 0; i < KT; ++i)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        state[i][n] *= decay;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) state[i][n] = multiply(qtf.v[i * 2 + k], for_queries[c & 1].read(k, n), state[i][n]);
-      }
+      for (int n = 0; n < NT; ++n) state[i][n] *= decay;
+    delta_state<KT, NT>(for_queries[c & 1], qtf.v, state);
     load_inner(next);
     lds_barrier();
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const Pieces<3> right = for_state.read(k, n);
-#pragma unroll
-        for (int i = 0; i < KT; ++i) state[i][n] = multiply(ktf.v[i * 2 + k], right, state[i][n]);
-      }
+    delta_state<KT, NT>(for_state, ktf.v, state);
     write_state(c - 1);
     write_grads((c & 1) ^ 1);
     load_last(next);
