@@ -93,37 +93,36 @@ __device__ __forceinline__ int delta_live_chunks(const DeltaArgs& s, int len) {
   return s.extra * s.chunks_wide + (last - wide) / s.part * s.chunks_rest + (last - wide) % s.part / kChunk + 1;
 }
 
-// A walk along the chunks that reads nothing but a worker's pointers, where it comes to another worker: two of its arrays.
+// A walk along the chunks that reads nothing but a worker's pointer, where it comes to another worker: one of its arrays.
 struct DeltaWalk {
   int32_t p, first, steps, before;  // before: the worker's first step
-  const char *one, *two;
+  const char* array;
   template <class F>
-  __device__ __forceinline__ void enter(const DeltaArgs& s, int worker, F pointers) {
+  __device__ __forceinline__ void enter(const DeltaArgs& s, int worker, F pointer) {
     p = worker;
     steps = s.part + (p < s.extra);
     before = p * s.part + min(p, s.extra);
-    pointers(p, one, two);
+    array = (const char*)pointer(p);
   }
   template <class F>
-  __device__ __forceinline__ void start(const DeltaArgs& s, int c, F pointers) {
+  __device__ __forceinline__ void start(const DeltaArgs& s, int c, F pointer) {
     const int wide = s.extra * s.chunks_wide;
-    const int worker = c < wide ? c / s.chunks_wide : s.extra + (c - wide) / s.chunks_rest;
-    enter(s, worker, pointers);
+    enter(s, c < wide ? c / s.chunks_wide : s.extra + (c - wide) / s.chunks_rest, pointer);
     first = (c < wide ? c % s.chunks_wide : (c - wide) % s.chunks_rest) * kChunk;
   }
   template <class F>
-  __device__ __forceinline__ void ahead(const DeltaArgs& s, F pointers) {
+  __device__ __forceinline__ void ahead(const DeltaArgs& s, F pointer) {
     first += kChunk;
     if (first >= steps) {
-      enter(s, p + 1, pointers);
+      enter(s, p + 1, pointer);
       first = 0;
     }
   }
   template <class F>
-  __device__ __forceinline__ void back(const DeltaArgs& s, F pointers) {
+  __device__ __forceinline__ void back(const DeltaArgs& s, F pointer) {
     first -= kChunk;
     if (first < 0) {
-      enter(s, p - 1, pointers);
+      enter(s, p - 1, pointer);
       first = (steps - 1) / kChunk * kChunk;
     }
   }

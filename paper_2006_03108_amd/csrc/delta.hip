@@ -239,23 +239,45 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs s) {
 }
 
 // ---- through time ---------------------------------------------------------
-// A wave's tile of a worker's rows: step 16 mt + 4 g + r of the chunk, column `col` of the head; nothing outside the live steps and the columns.
-template <class E>
+// A head's columns of a chunk's rows.  A wave has the steps 16 w + 4 g + r and the columns lane % 16 + 16 n: offsets that no chunk changes, and
+// columns that do not exist fail the check of any buffer.  Steps from `n` on fail that of this chunk's.
+template <class E, int NT>
 struct DeltaColumns {
-  __amdgpu_buffer_rsrc_t rows;
-  uint32_t hop;
-  __device__ __forceinline__ DeltaColumns(const void* base, int64_t first, const DeltaArgs& s, int h)
-      : rows(rsrc_of((const E*)base + (first * s.n_h + h) * s.d_v, kOob)), hop((uint32_t)(s.n_h * s.d_v) * (uint32_t)sizeof(E)) {}
-  __device__ __forceinline__ uint32_t offset(int step, int col, bool in) const { return in ? (uint32_t)step * hop + (uint32_t)col * (uint32_t)sizeof(E) : kOob; }
-  __device__ __forceinline__ uint32_t raw(int step, int col, bool in) const {
-    if constexpr (sizeof(E) == 4) return __builtin_amdgcn_raw_buffer_load_b32(rows, offset(step, col, in), 0, 0);
-    else return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rows, offset(step, col, in), 0, 0);
+  typedef std::conditional_t<sizeof(E) == 4, uint32_t, uint16_t> Raw;  // (as loaded: a conversion would wait for it)
+  uint32_t off[NT][4];
+  uint32_t hop, row;
+  __device__ __forceinline__ DeltaColumns(const DeltaArgs& s, int tile, int col) : hop((uint32_t)(s.n_h * s.d_v) * (uint32_t)sizeof(E)), row((uint32_t)s.d_v * (uint32_t)sizeof(E)) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        off[n][r] = col + 16 * n < s.d_v ? (uint32_t)(16 * tile + 4 * ((threadIdx.x & 63) >> 4) + r) * hop + (uint32_t)(col + 16 * n) * (uint32_t)sizeof(E) : kOob;
   }
-  static __device__ __forceinline__ float value(uint32_t raw) { return __uint_as_float(sizeof(E) == 4 ? raw : raw << 16); }
-  __device__ __forceinline__ float load(int step, int col, bool in) const { return value(raw(step, col, in)); }
-  __device__ __forceinline__ void store(int step, int col, bool in, float v) const {
-    if constexpr (sizeof(E) == 4) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), rows, offset(step, col, in), 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b16(to_bf16(v), rows, offset(step, col, in), 0, 0);
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows(const DeltaArgs& s, const DeltaWalk& at, int b, int h, int n) const {
+    n = __builtin_amdgcn_readfirstlane(n);  // (uniform; what the compiler takes for a lane's own it would load in a loop over lanes)
+    return rsrc_of((const E*)at.array + (((int64_t)b * at.steps + at.first) * s.n_h + h) * s.d_v, n > 0 ? (uint32_t)(n - 1) * hop + row : 0u);
+  }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, Raw (&raw)[NT][4]) const {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if constexpr (sizeof(E) == 4) raw[n][r] = __builtin_amdgcn_raw_buffer_load_b32(from, off[n][r], 0, 0);
+        else raw[n][r] = __builtin_amdgcn_raw_buffer_load_b16(from, off[n][r], 0, 0);
+      }
+  }
+  static __device__ __forceinline__ f32x4 values(const Raw (&raw)[4]) {
+    f32x4 v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = __uint_as_float(sizeof(E) == 4 ? raw[r] : (uint32_t)raw[r] << 16);
+    return v;
+  }
+  __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t to, int n, f32x4 v) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if constexpr (sizeof(E) == 4) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[r]), to, off[n][r], 0, 0);
+      else __builtin_amdgcn_raw_buffer_store_b16(to_bf16(v[r]), to, off[n][r], 0, 0);
+    }
   }
 };
 
@@ -316,20 +338,84 @@ struct DeltaShared {
     for (int i = 0; i < N; ++i) v[k][n][i][threadIdx.x & 63] = p.p[i];
   }
 };
-template <int COUNT, int N>
+// Every STRIDE-th piece from piece `from` on begins a fragment.  `at`: the first one's place, `hop`: from chunk to chunk.
+template <int COUNT, int N, int STRIDE>
 struct DeltaFragments {
   Pieces<N> v[COUNT];
-  // fragments `from`, `from` + 1, ..., of STRIDE pieces each
-  template <int STRIDE>
-  __device__ __forceinline__ void load(const uint16_t* at, int from) {
+  const char* at;
+  int64_t hop;
+  __device__ __forceinline__ void start(const uint16_t* base, int64_t chunk0, int heads, int head, int64_t numbers, int c, int from) {
+    hop = (int64_t)heads * numbers * 2;
+    at = (const char*)base + ((chunk0 + c) * heads + head) * numbers * 2 + (int64_t)from * kFragment * 2;
+  }
+  __device__ __forceinline__ void load() {
+    const __amdgpu_buffer_rsrc_t from = rsrc_of(at, kOob);
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) v[i] = load_fragment<N>(at + (int64_t)(from + i) * STRIDE * kFragment);
+    for (int i = 0; i < COUNT; ++i)
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const int o = (i * STRIDE + k) * kFragment * 2;
+        v[i].p[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, (threadIdx.x & 63) * 16 + (o & 4095), o & ~4095, 0));
+      }
   }
 };
+// exp(G), exp(G_C - G), beta of a wave's steps, and exp(G_C)
+struct DeltaSteps {
+  f32x4 since, until, beta;
+  float decay;
+  const float* at;
+  int64_t hop;
+  __device__ __forceinline__ void start(const DeltaArgs& s, int64_t chunk0, int h, int c) {
+    hop = (int64_t)s.n_h * kStepNumbers * kChunk;
+    at = s.steps + ((chunk0 + c) * s.n_h + h) * kStepNumbers * kChunk;
+  }
+  __device__ __forceinline__ void load(int tile) {
+    const __amdgpu_buffer_rsrc_t from = rsrc_of(at, kStepNumbers * kChunk * 4);
+    const uint32_t o = (uint32_t)(16 * tile + 4 * ((threadIdx.x & 63) >> 4)) * 4;
+    since = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, o, kSince * kChunk * 4, 0));
+    until = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, o, kUntil * kChunk * 4, 0));
+    beta = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, o, kBeta * kChunk * 4, 0));
+    decay = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, 0, (kChunk - 1) * 4, 0));
+  }
+};
+// Tiles of results in fp32, as they lie in the lanes.
+template <int TILES, int NT>
+struct DeltaTiles {
+  f32x4 v[TILES][NT][64];
+};
 
-// Whether two workgroups share a compute unit: 256 registers each are enough.
-template <class E, int DK, int NT, bool BACK>
-constexpr int delta_two_groups() { return (sizeof(E) == 2 ? DK == 64 || NT == 1 || !BACK : DK == 64 && NT == 1) ? 2 : 1; }
+// A wave's rows of the state as the operand of a step over keys.  With DK = 64 they are half a step, the other half is zeros.
+template <int KT, int NT>
+__device__ __forceinline__ void delta_own(const f32x4 (&state)[KT][NT], int wave, Pieces<3> (&own)[NT]) {
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    if constexpr (KT == 2) own[n] = split_tiles(state[0][n], state[1][n]);
+    else own[n] = wave & 1 ? split_tiles(f32x4{}, state[0][n]) : split_tiles(state[0][n], f32x4{});
+  }
+}
+// K times a wave's rows of the state: its part of every tile of steps
+template <int NT, int NA>
+__device__ __forceinline__ void delta_partial(const Pieces<NA>* left, const Pieces<3> (&own)[NT], int wave, DeltaTiles<16, NT>& to) {
+  f32x4 part[4][NT];
+#pragma unroll
+  for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) part[mt][n] = multiply(left[mt], own[n], f32x4{});
+#pragma unroll
+  for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) to.v[mt * 4 + wave][n][threadIdx.x & 63] = part[mt][n];
+}
+template <int NT>
+__device__ __forceinline__ void delta_joined(const DeltaTiles<16, NT>& from, int tile, f32x4 (&x)[NT]) {
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    f32x4 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = from.v[tile * 4 + i][n][threadIdx.x & 63];
+    x[n] = (v[0] + v[1]) + (v[2] + v[3]);
+  }
+}
 
 // A wave's rows of the state += left b
 template <int KT, int NT, int NA>
@@ -348,21 +434,80 @@ __device__ __forceinline__ void delta_state(const DeltaShared<2, NT, 3>& b, cons
       for (int i = 0; i < KT; ++i) state[i][n] = multiply(left[i * 2 + k], right[k][n], state[i][n]);
 }
 
-// A workgroup of four waves takes 16 NT columns of a head's state through all chunks.  Wave w has the tile of steps 16 w .. 16 w + 15 of every product
-// over keys or steps, and a quarter of the state's rows, so the chunk's matrices are read by one wave each, straight into the registers that the
-// last chunk's have left: every load has most of a chunk's time.  What the waves make for each other, in pieces, goes through LDS: the state, beta X and
-// U, a barrier for each, which waits for LDS alone (lds_barrier).
+// A workgroup takes 16 NT columns of a head's state through all chunks.  Of its first four waves, wave w has a quarter of the state's rows and the tile of steps
+// 16 w .. 16 w + 15 of X and U, so the chunk's matrices are read by one wave each, straight into the registers that the last chunk's have left:
+// every load has most of a chunk's time.  K S is the sum of what the waves' rows give.  These parts, beta X and U go through LDS, a barrier for each, which
+// waits for LDS alone (lds_barrier).  Four more waves make the outputs, which nothing waits for.
 template <class E, int DK, int NT, bool STORE>
-__global__ __launch_bounds__(256, (delta_two_groups<E, DK, NT, false>())) void delta_fwd_kernel(DeltaArgs s) {
+__global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaArgs s) {
   typedef DeltaSizes<kChunk, DK> Z;
+  typedef DeltaColumns<E, NT> Columns;
   constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>(), KT = DK / 64, KS = Z::kKeySteps;
-  __shared__ DeltaShared<KS, NT, 3> for_keys;
+  __shared__ DeltaTiles<16, NT> of_keys;  // K S: tile of steps, wave
+  __shared__ DeltaShared<STORE ? 1 : KS, NT, NO> for_queries;
   __shared__ DeltaShared<2, NT, 3> for_inner, for_state;
   __shared__ DeltaShared<2, NT, STORE ? 1 : NO> for_out;
   const DeltaTable table = DELTA_TABLE(s);
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, tile = wave & 3;
   const DeltaChain chain = delta_chain<NT>(s);
   const int b = chain.b, h = chain.h, hk = h / s.each, col = chain.col + (lane & 15);
+  const int len = delta_length(s, b), chunks = delta_live_chunks(s, len);
+  const int64_t chunk0 = (int64_t)b * s.chunks;
+  const Columns columns(s, tile, col);
+  DeltaWalk walk;
+
+  if (!STORE && wave >= 4) {  // O = scale exp(G) (Q S) + P U
+    auto outputs = [&](int p) { return table[p].o; };
+    DeltaFragments<KS, NI, NI> qf;
+    DeltaFragments<2, NO, kInner> pf;
+    DeltaSteps steps;
+    qf.start(s.qf, chunk0, s.n_hk, hk, Z::kKeyPiece * NI, 0, tile * KS * NI);
+    pf.start(s.pf, chunk0, s.n_h, h, Z::kStepPiece * kInner, 0, tile * 2 * kInner);
+    steps.start(s, chunk0, h, 0);
+    walk.start(s, 0, outputs);
+    if (chunks > 0) {
+      qf.load();
+      pf.load();
+      steps.load(tile);
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);  // (so that the loop's waits count its own loads alone)
+    for (int c = 0; c < chunks; ++c) {
+      const bool more = c + 1 < chunks;
+      lds_barrier();
+      f32x4 out[NT] = {};
+      for_queries.template multiply_into<KS>(qf.v, 0, out);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) out[n] *= steps.since * s.scale;
+      if (more) qf.at += qf.hop, steps.at += steps.hop;
+      qf.load();
+      steps.load(tile);
+      lds_barrier();
+      lds_barrier();
+      if (wave >= 6) for_out.template multiply_into<2>(pf.v, 0, out);
+      else for_out.template multiply_into<1>(pf.v, 0, out);
+      if (more) pf.at += pf.hop;
+      pf.load();
+      const int count = walk.count(), live = walk.live(len);
+      const __amdgpu_buffer_rsrc_t to = columns.rows(s, walk, b, h, count);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        if (live < count) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) out[n][r] = 16 * tile + 4 * g + r < live ? out[n][r] : 0.f;
+        }
+        columns.store(to, n, out[n]);
+      }
+      if (c + 1 < s.chunks) walk.ahead(s, outputs);
+    }
+    for (int c = chunks; c < s.chunks; ++c) {
+      const __amdgpu_buffer_rsrc_t to = columns.rows(s, walk, b, h, walk.count());
+#pragma unroll
+      for (int n = 0; n < NT; ++n) columns.store(to, n, f32x4{});
+      if (c + 1 < s.chunks) walk.ahead(s, outputs);
+    }
+    return;
+  }
+
   f32x4 state[KT][NT];
   const int64_t state_at = ((int64_t)b * s.n_h + h) * s.d_k * s.d_v;
 #pragma unroll
@@ -374,54 +519,50 @@ __global__ __launch_bounds__(256, (delta_two_groups<E, DK, NT, false>())) void d
         const int k = 16 * (wave * KT + i) + 4 * g + r, v = col + 16 * n;
         state[i][n][r] = s.h0 && k < s.d_k && v < s.d_v ? s.h0[state_at + (int64_t)k * s.d_v + v] : 0.f;
       }
-  const int len = delta_length(s, b), chunks = delta_live_chunks(s, len);
-  const int64_t chunk0 = (int64_t)b * s.chunks;
-
-  DeltaFragments<KS, NI> kf, qf;
-  DeltaFragments<2, kInner> tf;
-  DeltaFragments<2, NO> pf;
-  DeltaFragments<2 * KT, NI> ktf;
-  f32x4 since, until, beta, next_since, next_until, next_beta;
-  float decay, next_decay;
-  uint32_t raw[NT][4];
-  auto load_keys = [&](int c) {
-    const int64_t at = ((chunk0 + c) * s.n_hk + hk) * Z::kKeyPiece * NI;
-    kf.template load<NI>(s.kf + at, wave * KS);
-    if (!STORE) qf.template load<NI>(s.qf + at, wave * KS);
-  };
-  auto load_inner = [&](int c) { tf.template load<kInner>(s.tf + ((chunk0 + c) * s.n_h + h) * Z::kStepPiece * kInner, wave * 2); };
-  auto load_last = [&](int c) {
-    if (!STORE) pf.template load<kInner>(s.pf + ((chunk0 + c) * s.n_h + h) * Z::kStepPiece * kInner, wave * 2);
-    ktf.template load<NI>(s.ktf + ((chunk0 + c) * s.n_hk + hk) * Z::kKeyPiece * NI, wave * KT * 2);
-  };
-  auto load_steps = [&](int c) {
-    const float* const at = s.steps + ((chunk0 + c) * s.n_h + h) * kStepNumbers * kChunk + 16 * wave + 4 * g;
-    next_since = *(const f32x4*)(at + kSince * kChunk);
-    next_until = *(const f32x4*)(at + kUntil * kChunk);
-    next_beta = *(const f32x4*)(at + kBeta * kChunk);
-    next_decay = s.steps[((chunk0 + c) * s.n_h + h) * kStepNumbers * kChunk + kChunk - 1];
-  };
-  auto pointers = [&](int p, const char*& one, const char*& two) { one = (const char*)table[p].v, two = (const char*)table[p].o; };
-  DeltaWalk walk;
-  auto load_values = [&]() {
-    const DeltaColumns<E> values(walk.one, (int64_t)b * walk.steps + walk.first, s, h);
-    const int live = walk.live(len);
+  auto values = [&](int p) { return table[p].v; };
+  DeltaFragments<4, NI, KS * NI> kf;  // of all tiles of steps, for the wave's step over keys
+  DeltaFragments<2, kInner, kInner> tf;
+  DeltaFragments<2 * KT, NI, NI> ktf;
+  DeltaSteps steps;
+  kf.start(s.kf, chunk0, s.n_hk, hk, Z::kKeyPiece * NI, 0, wave * KT / 2 * NI);
+  ktf.start(s.ktf, chunk0, s.n_hk, hk, Z::kKeyPiece * NI, 0, tile * KT * 2 * NI);
+  tf.start(s.tf, chunk0, s.n_h, h, Z::kStepPiece * kInner, 0, tile * 2 * kInner);
+  steps.start(s, chunk0, h, 0);
+  walk.start(s, 0, values);
+  typename Columns::Raw raw[NT][4];
+  if (chunks > 0) {
+    columns.load(columns.rows(s, walk, b, h, walk.live(len)), raw);
+    kf.load();
+    tf.load();
+    ktf.load();
+    steps.load(tile);
+  }
+  __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
+  for (int c = 0; c < chunks; ++c) {
+    const bool more = c + 1 < chunks;
+    const int64_t head = (chunk0 + c) * s.n_h + h;
+    // K S
+    Pieces<3> own[NT];
+    delta_own<KT, NT>(state, wave, own);
+    delta_partial<NT>(kf.v, own, wave, of_keys);
+    if constexpr (!STORE) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = 16 * wave + 4 * g + r;
-        raw[n][r] = values.raw(t, col + 16 * n, t < live && col + 16 * n < s.d_v);
-      }
-  };
-  auto write_state = [&](int c) {
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      if constexpr (KT == 2) for_keys.write(wave, n, state[0][n], state[1][n]);
-      else for_keys.write(wave, n, state[0][n]);
+        for (int k = 0; k < NO; ++k) {
+          if constexpr (KT == 2) {
+            for_queries.v[wave][n][k][lane] = own[n].p[k];
+          } else {
+            const u32x4 v = own[n].p[k];
+            ((u32x2*)&for_queries.v[wave >> 1][n][k][lane])[wave & 1] = wave & 1 ? u32x2{v[2], v[3]} : u32x2{v[0], v[1]};
+          }
+        }
     }
-    if (STORE && c < chunks) {
-      float* const to = s.states + ((chunk0 + c) * s.n_h + h) * DK * s.dvp;
+    if (more) kf.at += kf.hop;
+    kf.load();
+    lds_barrier();
+    if constexpr (STORE) {
+      float* const to = s.states + head * DK * s.dvp;
 #pragma unroll
       for (int i = 0; i < KT; ++i)
 #pragma unroll
@@ -430,102 +571,49 @@ __global__ __launch_bounds__(256, (delta_two_groups<E, DK, NT, false>())) void d
           for (int r = 0; r < 4; ++r)
             if (col + 16 * n < s.dvp) to[(int64_t)(16 * (wave * KT + i) + 4 * g + r) * s.dvp + col + 16 * n] = state[i][n][r];
     }
-  };
-  if (chunks > 0) {
-    walk.start(s, 0, pointers);
-    load_values();
-    load_steps(0);
-    load_keys(0);
-    load_inner(0);
-    load_last(0);
-    write_state(0);
-  }
-  __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);  // (so that the loop's waits count its own loads alone)
-  lds_barrier();
-  for (int c = 0; c < chunks; ++c) {
-    const int next = min(c + 1, chunks - 1), count = walk.count(), live = walk.live(len);
-    const DeltaColumns<E> to(walk.two, (int64_t)b * walk.steps + walk.first, s, h);
-    const int64_t head = (chunk0 + c) * s.n_h + h;
-    since = next_since, until = next_until, beta = next_beta, decay = next_decay;
     // X = V - exp(G) (K S)
-    f32x4 x[NT] = {}, out[NT] = {};
-    for_keys.template multiply_into<KS>(kf.v, 0, x);
+    f32x4 x[NT];
+    delta_joined<NT>(of_keys, tile, x);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) x[n][r] = fmaf(-since[r], x[n][r], DeltaColumns<E>::value(raw[n][r]));
-      for_inner.write(wave, n, x[n] * beta);
+      x[n] = Columns::values(raw[n]) - steps.since * x[n];
+      for_inner.write(wave, n, x[n] * steps.beta);
       if (STORE && col + 16 * n < s.dvp) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) s.x[(head * kChunk + 16 * wave + 4 * g + r) * s.dvp + col + 16 * n] = x[n][r];
       }
     }
+    if (more) walk.ahead(s, values);
+    columns.load(columns.rows(s, walk, b, h, walk.live(len)), raw);
     lds_barrier();
-    // U = T (beta X); Q S meanwhile
+    // U = T (beta X)
     f32x4 u[NT] = {};
     if (wave >= 2) for_inner.template multiply_into<2>(tf.v, 0, u);
     else for_inner.template multiply_into<1>(tf.v, 0, u);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
+      for_state.write(wave, n, u[n] * steps.until);
       if (!STORE) for_out.write(wave, n, u[n]);
-      for_state.write(wave, n, u[n] * until);
       if (STORE && col + 16 * n < s.dvp) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) s.u[(head * kChunk + 16 * wave + 4 * g + r) * s.dvp + col + 16 * n] = u[n][r];
       }
     }
-    if constexpr (!STORE) {
-      f32x4 odd[NT] = {};
-#pragma unroll
-      for (int k = 0; k < KS; ++k)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) (k & 1 ? odd : out)[n] = multiply(qf.v[k], first_pieces<NO>(for_keys.read(k, n)), (k & 1 ? odd : out)[n]);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) out[n] += odd[n];
-    }
-    load_keys(next);
-    load_inner(next);
-    load_steps(next);
-    if (next > c) walk.ahead(s, pointers);
-    load_values();
-    lds_barrier();
-    // S' = exp(G_C) S + K^T (exp(G_C - G) U)
 #pragma unroll
     for (int i = 0; i < KT; ++i)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) state[i][n] *= decay;
-    delta_state<KT, NT>(for_state, ktf.v, state);
-    write_state(c + 1);
-    // O = scale exp(G) (Q S) + P U
-    if constexpr (!STORE) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n) out[n] *= since * s.scale;
-      if (wave >= 2) for_out.template multiply_into<2>(pf.v, 0, out);
-      else for_out.template multiply_into<1>(pf.v, 0, out);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int t = 16 * wave + 4 * g + r;
-          to.store(t, col + 16 * n, t < count && col + 16 * n < s.d_v, t < live ? out[n][r] : 0.f);
-        }
-      }
+      for (int n = 0; n < NT; ++n) state[i][n] *= steps.decay;
+    if (more) {
+      tf.at += tf.hop;
+      steps.at += steps.hop;
     }
-    load_last(next);
+    tf.load();
+    steps.load(tile);
     lds_barrier();
-  }
-  if (!STORE) {
-    for (int c = chunks; c < s.chunks; ++c) {
-      const DeltaChunk at = delta_chunk(s, b, c);
-      const DeltaColumns<E> to(table[at.p].o, (int64_t)b * at.steps + at.first, s, h);
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int t = 16 * wave + 4 * g + r;
-          to.store(t, col + 16 * n, t < at.n && col + 16 * n < s.d_v, 0.f);
-        }
-    }
+    // S' = exp(G_C) S + K^T (exp(G_C - G) U)
+    delta_state<KT, NT>(for_state, ktf.v, state);
+    if (more) ktf.at += ktf.hop;
+    ktf.load();
   }
   if (s.hT) {
 #pragma unroll
@@ -542,19 +630,81 @@ __global__ __launch_bounds__(256, (delta_two_groups<E, DK, NT, false>())) void d
 
 // The gradient of the state, backwards through the chunks, in the same way:
 //   dU = P^T dO + exp(G_C - G) (K dS'),  dR = T^T dU,  dS = exp(G_C) dS' + Q^T (scale exp(G) dO) - K^T (exp(G) beta dR)
-// with R = beta X.  dS' and dR are kept for the kernel behind it.
+// with R = beta X.  dS' and dR are kept for the kernel behind it.  The second four waves make the two products of dO, a chunk ahead.
 template <class E, int DK, int NT>
-__global__ __launch_bounds__(256, (delta_two_groups<E, DK, NT, true>())) void delta_bwd_kernel(DeltaArgs s) {
+__global__ __launch_bounds__(512, 2) void delta_bwd_kernel(DeltaArgs s) {
   typedef DeltaSizes<kChunk, DK> Z;
+  typedef DeltaColumns<E, NT> Columns;
   constexpr int NI = delta_pieces<E>(), KT = DK / 64, KS = Z::kKeySteps;
-  __shared__ DeltaShared<KS, NT, 3> for_keys;
-  __shared__ DeltaShared<2, NT, NI> for_out[2];      // dO, by turns
-  __shared__ DeltaShared<2, NT, 3> for_queries[2];   // scale exp(G) dO, by turns
+  __shared__ DeltaTiles<16, NT> of_keys;         // K dS': tile of steps, wave
   __shared__ DeltaShared<2, NT, 3> for_inner, for_state;
+  __shared__ DeltaShared<2, NT, NI> grads;     // dO
+  __shared__ DeltaShared<2, NT, 3> for_queries;  // scale exp(G) dO
+  __shared__ DeltaTiles<4, NT> of_inner[2];       // P^T dO, by turns
+  __shared__ DeltaTiles<4 * KT, NT> of_queries[2];  // Q^T (scale exp(G) dO)
   const DeltaTable table = DELTA_TABLE(s);
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, tile = wave & 3;
   const DeltaChain chain = delta_chain<NT>(s);
   const int b = chain.b, h = chain.h, hk = h / s.each, col = chain.col + (lane & 15);
+  const int len = delta_length(s, b), chunks = delta_live_chunks(s, len);
+  const int64_t chunk0 = (int64_t)b * s.chunks;
+
+  if (wave >= 4) {
+    if (chunks == 0) return;
+    const Columns columns(s, tile, col);
+    auto arrays = [&](int p) { return table[p].d_o; };
+    DeltaWalk walk;
+    DeltaFragments<2, kInner, kInner> ptf;
+    DeltaFragments<2 * KT, NI, NI> qtf;
+    DeltaSteps steps;
+    int c = chunks - 1;  // the chunk that is made
+    ptf.start(s.ptf, chunk0, s.n_h, h, Z::kStepPiece * kInner, c, tile * 2 * kInner);
+    qtf.start(s.qtf, chunk0, s.n_hk, hk, Z::kKeyPiece * NI, c, tile * KT * 2 * NI);
+    steps.start(s, chunk0, h, c);
+    walk.start(s, c, arrays);
+    typename Columns::Raw raw[NT][4];
+    columns.load(columns.rows(s, walk, b, h, walk.live(len)), raw);
+    ptf.load();
+    qtf.load();
+    steps.load(tile);
+    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);  // (so that the loop's waits count its own loads alone)
+    // Three barriers a chunk, one chunk before the other waves.
+    for (int i = chunks; i >= 0; --i) {
+      const bool more = c > 0;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const f32x4 v = Columns::values(raw[n]);
+        grads.write(tile, n, v);  // (bf16 numbers are their upper halves)
+        for_queries.write(tile, n, v * (steps.since * s.scale));
+      }
+      if (more) {
+        walk.back(s, arrays);
+        steps.at -= steps.hop;
+      }
+      columns.load(columns.rows(s, walk, b, h, walk.live(len)), raw);
+      steps.load(tile);
+      lds_barrier();
+      f32x4 u[NT] = {}, sum[KT][NT] = {};
+      if (wave < 6) grads.template multiply_into<2>(ptf.v, 0, u);
+      else grads.template multiply_into<1>(ptf.v + 1, 1, u);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) of_inner[c & 1].v[tile][n][lane] = u[n];
+      if (more) ptf.at -= ptf.hop;
+      ptf.load();
+      delta_state<KT, NT>(for_queries, qtf.v, sum);
+#pragma unroll
+      for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) of_queries[c & 1].v[tile * KT + k][n][lane] = sum[k][n];
+      if (more) qtf.at -= qtf.hop;
+      qtf.load();
+      lds_barrier();
+      lds_barrier();
+      c -= more;
+    }
+    return;
+  }
+
   f32x4 state[KT][NT];  // dS
   const int64_t state_at = ((int64_t)b * s.n_h + h) * s.d_k * s.d_v;
 #pragma unroll
@@ -566,63 +716,36 @@ __global__ __launch_bounds__(256, (delta_two_groups<E, DK, NT, true>())) void de
         const int k = 16 * (wave * KT + i) + 4 * g + r, v = col + 16 * n;
         state[i][n][r] = s.dhT && k < s.d_k && v < s.d_v ? s.dhT[state_at + (int64_t)k * s.d_v + v] : 0.f;
       }
-  const int len = delta_length(s, b), chunks = delta_live_chunks(s, len);
-  const int64_t chunk0 = (int64_t)b * s.chunks;
-
-  DeltaFragments<KS, NI> kf;
-  DeltaFragments<2, kInner> ttf, ptf;
-  DeltaFragments<2 * KT, NI> ktf, qtf;
-  f32x4 since, until, beta, next_since, next_until, next_beta;
-  float decay, next_decay;
-  uint32_t raw[NT][4];
-  auto load_first = [&](int c) {
-    kf.template load<NI>(s.kf + ((chunk0 + c) * s.n_hk + hk) * Z::kKeyPiece * NI, wave * KS);
-    ptf.template load<kInner>(s.ptf + ((chunk0 + c) * s.n_h + h) * Z::kStepPiece * kInner, wave * 2);
-  };
-  auto load_inner = [&](int c) { ttf.template load<kInner>(s.ttf + ((chunk0 + c) * s.n_h + h) * Z::kStepPiece * kInner, wave * 2); };
-  auto load_last = [&](int c) {
-    const int64_t at = ((chunk0 + c) * s.n_hk + hk) * Z::kKeyPiece * NI;
-    ktf.template load<NI>(s.ktf + at, wave * KT * 2);
-    qtf.template load<NI>(s.qtf + at, wave * KT * 2);
-  };
-  auto load_steps = [&](int c) {
-    const float* const at = s.steps + ((chunk0 + c) * s.n_h + h) * kStepNumbers * kChunk + 16 * wave + 4 * g;
-    next_since = *(const f32x4*)(at + kSince * kChunk);
-    next_until = *(const f32x4*)(at + kUntil * kChunk);
-    next_beta = *(const f32x4*)(at + kBeta * kChunk);
-    next_decay = s.steps[((chunk0 + c) * s.n_h + h) * kStepNumbers * kChunk + kChunk - 1];
-  };
-  auto pointers = [&](int p, const char*& one, const char*& two) { one = two = (const char*)table[p].d_o; };
-  DeltaWalk walk;
-  auto load_grads = [&]() {
-    const DeltaColumns<E> grads(walk.one, (int64_t)b * walk.steps + walk.first, s, h);
-    const int live = walk.live(len);
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = 16 * wave + 4 * g + r;
-        raw[n][r] = grads.raw(t, col + 16 * n, t < live && col + 16 * n < s.d_v);
-      }
-  };
-  auto write_grads = [&](int turn) {
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      f32x4 v;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = DeltaColumns<E>::value(raw[n][r]);
-      for_out[turn].write(wave, n, v);  // (bf16 numbers are their upper halves)
-      for_queries[turn].write(wave, n, v * (next_since * s.scale));
-    }
-  };
-  auto write_state = [&](int c) {
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      if constexpr (KT == 2) for_keys.write(wave, n, state[0][n], state[1][n]);
-      else for_keys.write(wave, n, state[0][n]);
-    }
-    if (c >= 0) {
-      float* const to = s.dstates + ((chunk0 + c) * s.n_h + h) * DK * s.dvp;
+  DeltaFragments<4, NI, KS * NI> kf;
+  DeltaFragments<2, kInner, kInner> ttf;
+  DeltaFragments<2 * KT, NI, NI> ktf;
+  DeltaSteps steps;
+  const int last = max(chunks - 1, 0);
+  kf.start(s.kf, chunk0, s.n_hk, hk, Z::kKeyPiece * NI, last, wave * KT / 2 * NI);
+  ktf.start(s.ktf, chunk0, s.n_hk, hk, Z::kKeyPiece * NI, last, tile * KT * 2 * NI);
+  ttf.start(s.ttf, chunk0, s.n_h, h, Z::kStepPiece * kInner, last, tile * 2 * kInner);
+  steps.start(s, chunk0, h, last);
+  if (chunks > 0) {
+    kf.load();
+    ttf.load();
+    ktf.load();
+    steps.load(tile);
+    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
+    lds_barrier();
+    lds_barrier();
+    lds_barrier();
+  }
+  for (int c = chunks - 1; c >= 0; --c) {
+    const bool more = c > 0;
+    const int64_t head = (chunk0 + c) * s.n_h + h;
+    Pieces<3> own[NT];
+    delta_own<KT, NT>(state, wave, own);
+    delta_partial<NT>(kf.v, own, wave, of_keys);
+    if (more) kf.at -= kf.hop;
+    kf.load();
+    lds_barrier();
+    {
+      float* const to = s.dstates + head * DK * s.dvp;
 #pragma unroll
       for (int i = 0; i < KT; ++i)
 #pragma unroll
@@ -631,43 +754,17 @@ __global__ __launch_bounds__(256, (delta_two_groups<E, DK, NT, true>())) void de
           for (int r = 0; r < 4; ++r)
             if (col + 16 * n < s.dvp) to[(int64_t)(16 * (wave * KT + i) + 4 * g + r) * s.dvp + col + 16 * n] = state[i][n][r];
     }
-  };
-  if (chunks > 0) {
-    const int c = chunks - 1;
-    walk.start(s, c, pointers);
-    load_grads();
-    load_steps(c);
-    load_first(c);
-    load_inner(c);
-    load_last(c);
-    write_grads(c & 1);
-    write_state(c);
-  }
-  __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);  // (so that the loop's waits count its own loads alone)
-  lds_barrier();
-  for (int c = chunks - 1; c >= 0; --c) {
-    const int next = max(c - 1, 0);
-    const int64_t head = (chunk0 + c) * s.n_h + h;
-    since = next_since, until = next_until, beta = next_beta, decay = next_decay;
-    if (next < c) walk.back(s, pointers);
-    load_grads();
-    load_steps(next);
-    f32x4 u[NT] = {};
-    for_keys.template multiply_into<KS>(kf.v, 0, u);
+    f32x4 u[NT];
+    delta_joined<NT>(of_keys, tile, u);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) u[n] *= until;
-    if (wave < 2) for_out[c & 1].template multiply_into<2>(ptf.v, 0, u);
-    else for_out[c & 1].template multiply_into<1>(ptf.v + 1, 1, u);
-#pragma unroll
-    for (int n = 0; n < NT; ++n) for_inner.write(wave, n, u[n]);
-    load_first(next);
+    for (int n = 0; n < NT; ++n) for_inner.write(wave, n, of_inner[c & 1].v[wave][n][lane] + u[n] * steps.until);
     lds_barrier();
     f32x4 r_[NT] = {};
     if (wave < 2) for_inner.template multiply_into<2>(ttf.v, 0, r_);
     else for_inner.template multiply_into<1>(ttf.v + 1, 1, r_);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      for_state.write(wave, n, r_[n] * -(since * beta));
+      for_state.write(wave, n, r_[n] * -(steps.since * steps.beta));
       if (col + 16 * n < s.dvp) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) s.dr[(head * kChunk + 16 * wave + 4 * g + r) * s.dvp + col + 16 * n] = r_[n][r];
@@ -676,15 +773,17 @@ __global__ __launch_bounds__(256, (delta_two_groups<E, DK, NT, true>())) void de
 #pragma unroll
     for (int i = 0; i < KT; ++i)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) state[i][n] *= decay;
-    delta_state<KT, NT>(for_queries[c & 1], qtf.v, state);
-    load_inner(next);
+      for (int n = 0; n < NT; ++n) state[i][n] = of_queries[c & 1].v[wave * KT + i][n][lane] + state[i][n] * steps.decay;
+    if (more) {
+      ttf.at -= ttf.hop;
+      steps.at -= steps.hop;
+    }
+    ttf.load();
+    steps.load(tile);
     lds_barrier();
     delta_state<KT, NT>(for_state, ktf.v, state);
-    write_state(c - 1);
-    write_grads((c & 1) ^ 1);
-    load_last(next);
-    lds_barrier();
+    if (more) ktf.at -= ktf.hop;
+    ktf.load();
   }
   if (s.dh0) {
 #pragma unroll
@@ -1180,16 +1279,16 @@ static int launch_delta(distdl_delta_plan* p, DeltaArgs& s, hipStream_t st) {
   if ((rc = allow_large_lds<prepare>())) return rc;
   const dim3 chunks((unsigned)((int64_t)s.n_b * s.chunks * s.n_hk));
   hipLaunchKernelGGL(prepare, chunks, dim3(256), sizeof(DeltaPrepareShared<E, C, DK>), st, s);
-  // A workgroup takes 32 columns where there are more than enough for two on each compute unit: it reads the chunks' matrices half as often.
+  // A workgroup, of which a compute unit holds one, takes 32 columns where those of 16 would be more than a round.
   const int64_t chains = (int64_t)s.n_b * s.n_h;
-  const bool two = s.d_v > 16 && chains * ((s.d_v + 15) / 16) > 512;
+  const bool two = s.d_v > 16 && chains * ((s.d_v + 15) / 16) > 256;
   s.slices = two ? (s.d_v + 31) / 32 : (s.d_v + 15) / 16;
   const dim3 groups((unsigned)(chains * s.slices));
-  if (two) hipLaunchKernelGGL((delta_fwd_kernel<E, DK, 2, BACK>), groups, dim3(256), 0, st, s);
-  else hipLaunchKernelGGL((delta_fwd_kernel<E, DK, 1, BACK>), groups, dim3(256), 0, st, s);
+  if (two) hipLaunchKernelGGL((delta_fwd_kernel<E, DK, 2, BACK>), groups, dim3(BACK ? 256 : 512), 0, st, s);
+  else hipLaunchKernelGGL((delta_fwd_kernel<E, DK, 1, BACK>), groups, dim3(BACK ? 256 : 512), 0, st, s);
   if constexpr (BACK) {
-    if (two) hipLaunchKernelGGL((delta_bwd_kernel<E, DK, 2>), groups, dim3(256), 0, st, s);
-    else hipLaunchKernelGGL((delta_bwd_kernel<E, DK, 1>), groups, dim3(256), 0, st, s);
+    if (two) hipLaunchKernelGGL((delta_bwd_kernel<E, DK, 2>), groups, dim3(512), 0, st, s);
+    else hipLaunchKernelGGL((delta_bwd_kernel<E, DK, 1>), groups, dim3(512), 0, st, s);
     constexpr auto grad = delta_grad_kernel<E, C, DK>;
     if ((rc = allow_large_lds<grad>())) return rc;
     hipLaunchKernelGGL(grad, chunks, dim3(512), sizeof(DeltaGradShared<E, C, DK>), st, s);
