@@ -28,10 +28,12 @@ struct DeltaPrepareShared {
   static constexpr int kRow = DK + 8, kLine = C + 4;
   union {
     uint16_t rows[2][delta_pieces<E>()][C][kRow];  // K, Q
-    float inner[2][C][kLine];                      // K K^T, Q K^T
+    struct {
+      float a[C][kLine], t[C][kLine], p[C][kLine];
+    };
   };
-  float a[C][kLine], t[C][kLine];
-  float whole[C], rest[C], beta[C];  // G = whole + rest
+  static constexpr int kHeads = 2;  // (with four, two workgroups share a compute unit instead of three)
+  float whole[kHeads][C], rest[kHeads][C], beta[kHeads][C];  // G = whole + rest
 };
 
 // (1 + a)^-1 of a strictly lower matrix in `a`, into `t`, zeros above the diagonal.  Blocks of 16 on the diagonal by substitution, a
@@ -42,14 +44,18 @@ __device__ __forceinline__ void delta_inverse(const float (*a)[LINE], float (*t)
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
   if (wave < N) {
     const int at = wave * 16;
+    f32x4 left[16][4];  // the block's rows, the same for all lanes
+#pragma unroll
+    for (int i = 1; i < 16; ++i)
+#pragma unroll
+      for (int j = 0; j < i; j += 4) left[i][j / 4] = *(const f32x4*)&a[at + i][at + j];
     float x[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float v = i == col ? 1.f : 0.f;
+    for (int i = 0; i < 16; ++i) x[i] = i == col ? 1.f : 0.f;
 #pragma unroll
-      for (int j = 0; j < i; ++j) v = fmaf(-a[at + i][at + j], x[j], v);
-      x[i] = v;
-    }
+    for (int j = 0; j < 15; ++j)
+#pragma unroll
+      for (int i = j + 1; i < 16; ++i) x[i] = fmaf(-left[i][j / 4][j % 4], x[j], x[i]);
     if (g == 0) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) t[at + i][at + col] = x[i];
@@ -82,8 +88,18 @@ __device__ __forceinline__ void delta_inverse(const float (*a)[LINE], float (*t)
 // The places along a fragment's sum that a lane has: element e of step ks.
 __device__ __forceinline__ int delta_place(int ks, int e) { return 32 * ks + (e >> 2) * 16 + 4 * ((threadIdx.x & 63) >> 4) + (e & 3); }
 
+// Tiles on and below the diagonal, by rows.
+struct DeltaLower {
+  int mt, nt;
+};
+__device__ __forceinline__ DeltaLower delta_lower(int tile) {
+  const int mt = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0;
+  return DeltaLower{mt, tile - mt * (mt + 1) / 2};
+}
+
+// A workgroup has a chunk of a key's head and its heads, whose matrices have K K^T and Q K^T in common: these stay in registers.
 template <class E, int C, int DK, bool BACK>
-__global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs s) {
+__global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
   typedef DeltaSizes<C, DK> Z;
   typedef DeltaPrepareShared<E, C, DK> Shared;
   constexpr int NI = delta_pieces<E>();
@@ -98,17 +114,50 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs s) {
   const int64_t step0 = (int64_t)b * at.steps + at.first;  // of the worker's arrays
   const DeltaTable w = table + at.p;
 
+  // The sums of g for a head, by a wave.
+  auto sum_up = [&](int e) {
+    if (wave >= Shared::kHeads || e + wave >= s.each) return;
+    const int h = hk * s.each + e + wave;
+    const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h;
+    const bool live = lane < at.live;
+    const int64_t o = (step0 + lane) * s.n_h + h;
+    const float beta = live ? w->beta[o] : 0.f;
+    double sum = live && w->g ? (double)bounded(w->g[o]) : 0.0;
+#pragma unroll
+    for (int d = 1; d < C; d *= 2) {
+      const double before = __shfl_up(sum, d, 64);
+      if (lane >= d) sum += before;
+    }
+    const double last = __shfl(sum, C - 1, 64);
+    const float whole = (float)(rint(sum * 64.0) * (1.0 / 64.0)), rest = (float)(sum - (double)whole);
+    m.whole[wave][lane] = whole;
+    m.rest[wave][lane] = rest;
+    m.beta[wave][lane] = beta;
+    float* const out = s.steps + head * kStepNumbers * C + lane;
+    out[kSince * C] = expf((float)sum);
+    out[kUntil * C] = expf((float)(last - sum));
+    out[kBeta * C] = beta;
+    out[kWhole * C] = whole;
+    out[kRest * C] = rest;
+  };
+
   // rows of K and Q, zeros behind the end of the sequence and of the row
-  for (int i = tid; i < 2 * C * (DK / 8); i += 256) {
-    const int what = i / (C * (DK / 8)), t = i / (DK / 8) % C, col = i % (DK / 8) * 8;
-    const E* const from = (const E*)(what ? w->q : w->k) + ((step0 + t) * s.n_hk + hk) * s.d_k + col;
-    Eight<E> raw;
-    raw.load(from, t < at.live ? min(8, s.d_k - col) : 0);
+  constexpr int kPieces = 2 * C * (DK / 8) / 256;
+  Eight<E> raw[kPieces];
+#pragma unroll
+  for (int x = 0; x < kPieces; ++x) {
+    const int i = tid + 256 * x, what = i / (C * (DK / 8)), t = i / (DK / 8) % C, col = i % (DK / 8) * 8;
+    raw[x].load((const E*)(what ? w->q : w->k) + ((step0 + t) * s.n_hk + hk) * s.d_k + col, t < at.live ? min(8, s.d_k - col) : 0);
+  }
+  sum_up(0);
+#pragma unroll
+  for (int x = 0; x < kPieces; ++x) {
+    const int i = tid + 256 * x, what = i / (C * (DK / 8)), t = i / (DK / 8) % C, col = i % (DK / 8) * 8;
     if constexpr (NI == 1) {
-      *(u32x4*)&m.rows[what][0][t][col] = raw.a;
+      *(u32x4*)&m.rows[what][0][t][col] = raw[x].a;
     } else {
       float v[8];
-      raw.values(v);
+      raw[x].values(v);
       const Pieces<3> p = split8(v);
 #pragma unroll
       for (int k = 0; k < 3; ++k) *(u32x4*)&m.rows[what][k][t][col] = p.p[k];
@@ -140,70 +189,49 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs s) {
     store_fragment((what ? s.qtf : s.ktf) + key_at + (int64_t)i * NI * kFragment, v);
   }
 
-  // K K^T and Q K^T, tiles on and below the diagonal
-  constexpr int kLower = Z::kTiles * (Z::kTiles + 1) / 2, kJobs = (2 * kLower + 3) / 4;
-  f32x4 acc[kJobs];
+  // K K^T and Q K^T, tiles on and below the diagonal: a wave has the same tiles of both
+  constexpr int kLower = Z::kTiles * (Z::kTiles + 1) / 2, kJobs = (kLower + 3) / 4;
+  f32x4 kk[kJobs] = {}, qk[kJobs] = {};
 #pragma unroll
   for (int i = 0; i < kJobs; ++i) {
-    const int job = wave + 4 * i;
-    acc[i] = f32x4{};
-    if (job < 2 * kLower) {
-      const int what = job / kLower, tile = job % kLower, mt = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, nt = tile - mt * (mt + 1) / 2;
-      for (int ks = 0; ks < Z::kKeySteps; ++ks) {
-        Pieces<NI> left, right;
+    if (wave + 4 * i >= kLower) continue;
+    const DeltaLower at_tile = delta_lower(wave + 4 * i);
+    for (int ks = 0; ks < Z::kKeySteps; ++ks) {
+      Pieces<NI> one, two, right;
 #pragma unroll
-        for (int k = 0; k < NI; ++k) {
-          left.p[k] = *(const u32x4*)&m.rows[what][k][mt * 16 + row][32 * ks + 8 * g];
-          right.p[k] = *(const u32x4*)&m.rows[0][k][nt * 16 + row][32 * ks + 8 * g];
-        }
-        acc[i] = multiply(left, right, acc[i]);
+      for (int k = 0; k < NI; ++k) {
+        one.p[k] = *(const u32x4*)&m.rows[0][k][at_tile.mt * 16 + row][32 * ks + 8 * g];
+        two.p[k] = *(const u32x4*)&m.rows[1][k][at_tile.mt * 16 + row][32 * ks + 8 * g];
+        right.p[k] = *(const u32x4*)&m.rows[0][k][at_tile.nt * 16 + row][32 * ks + 8 * g];
       }
-    }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kJobs; ++i) {
-    const int job = wave + 4 * i;
-    if (job < 2 * kLower) {
-      const int what = job / kLower, tile = job % kLower, mt = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, nt = tile - mt * (mt + 1) / 2;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) m.inner[what][mt * 16 + 4 * g + r][nt * 16 + row] = acc[i][r];
+      kk[i] = multiply(one, right, kk[i]);
+      qk[i] = multiply(two, right, qk[i]);
     }
   }
 
   for (int e = 0; e < s.each; ++e) {
-    const int h = hk * s.each + e;
+    const int h = hk * s.each + e, slot = e % Shared::kHeads;
     const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h;
     __syncthreads();
-    if (wave == 0) {  // the sums of g
-      const bool live = lane < at.live;
-      const int64_t o = (step0 + lane) * s.n_h + h;
-      double sum = live && w->g ? (double)bounded(w->g[o]) : 0.0;
-#pragma unroll
-      for (int d = 1; d < C; d *= 2) {
-        const double before = __shfl_up(sum, d, 64);
-        if (lane >= d) sum += before;
-      }
-      const double last = __shfl(sum, C - 1, 64);
-      if (lane < C) {
-        const float whole = (float)(rint(sum * 64.0) * (1.0 / 64.0)), beta = live ? w->beta[o] : 0.f;
-        m.whole[lane] = whole;
-        m.rest[lane] = (float)(sum - (double)whole);
-        m.beta[lane] = beta;
-        float* const out = s.steps + head * kStepNumbers * C + lane;
-        out[kSince * C] = expf((float)sum);
-        out[kUntil * C] = expf((float)(last - sum));
-        out[kBeta * C] = beta;
-        out[kWhole * C] = whole;
-        out[kRest * C] = m.rest[lane];
-      }
+    if (e > 0 && slot == 0) {
+      sum_up(e);
+      __syncthreads();
     }
-    __syncthreads();
-    auto decay = [&](int i, int j) { return expf((m.whole[i] - m.whole[j]) + (m.rest[i] - m.rest[j])); };
-    for (int i = tid; i < C * C; i += 256) {
-      const int r = i / C, k = i % C;
-      if (k < r) m.a[r][k] = m.beta[r] * decay(r, k) * m.inner[0][r][k];
-      else m.a[r][k] = 0.f;
+    // A and P, zeros above the diagonal
+#pragma unroll
+    for (int x = 0; x < kJobs; ++x) {
+      if (wave + 4 * x >= kLower) continue;
+      const DeltaLower at_tile = delta_lower(wave + 4 * x);
+      const int j = at_tile.nt * 16 + row;
+      const float whole = m.whole[slot][j], rest = m.rest[slot][j];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = at_tile.mt * 16 + 4 * g + r;
+        const float decay = i >= j ? expf((m.whole[slot][i] - whole) + (m.rest[slot][i] - rest)) : 0.f;
+        m.a[i][j] = i > j ? m.beta[slot][i] * decay * kk[x][r] : 0.f;
+        m.p[i][j] = i >= j ? s.scale * decay * qk[x][r] : 0.f;
+        if (at_tile.mt != at_tile.nt) m.p[at_tile.nt * 16 + 4 * g + r][at_tile.mt * 16 + row] = 0.f;
+      }
     }
     __syncthreads();
     delta_inverse<C>(m.a, m.t);
@@ -211,28 +239,22 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(DeltaArgs s) {
     for (int f = wave; f < Z::kTiles * Z::kSteps; f += 4) {
       const int mt = f / Z::kSteps, ts = f % Z::kSteps, i = mt * 16 + row;
       const int64_t o = head * Z::kStepPiece * kInner + (int64_t)f * kInner * kFragment;
-      float v[8];
       if (ts * 2 <= mt) {
-#pragma unroll
-        for (int x = 0; x < 8; ++x) v[x] = m.t[i][delta_place(ts, x)];
-        store_fragment(s.tf + o, split8(v));
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          const int j = delta_place(ts, x);
-          v[x] = j <= i ? s.scale * decay(i, j) * m.inner[1][i][j] : 0.f;
-        }
-        store_fragment(s.pf + o, split8(v));
+        auto across = [&](const float (*from)[Shared::kLine]) {
+          return split_tiles(*(const f32x4*)&from[i][32 * ts + 4 * g], *(const f32x4*)&from[i][32 * ts + 16 + 4 * g]);
+        };
+        store_fragment(s.tf + o, across(m.t));
+        store_fragment(s.pf + o, across(m.p));
       }
       if (BACK && mt / 2 <= ts) {
+        auto down = [&](const float (*from)[Shared::kLine]) {
+          float v[8];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) v[x] = m.t[delta_place(ts, x)][i];
-        store_fragment(s.ttf + o, split8(v));
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          const int j = delta_place(ts, x);
-          v[x] = i <= j ? s.scale * decay(j, i) * m.inner[1][j][i] : 0.f;
-        }
-        store_fragment(s.ptf + o, split8(v));
+          for (int x = 0; x < 8; ++x) v[x] = from[delta_place(ts, x)][i];
+          return split8(v);
+        };
+        store_fragment(s.ttf + o, down(m.t));
+        store_fragment(s.ptf + o, down(m.p));
       }
     }
   }
@@ -817,6 +839,7 @@ struct DeltaGradShared {
   };
   float row_sum[2][kTiles][C], col_sum[2][kTiles][C], beta_sum[kTiles][C];
   float dots[kKeyTiles][C], ends[kKeyTiles][C], xs[C], both[kKeyTiles];
+  float steps[kStepNumbers][C];
 };
 
 __device__ __forceinline__ float sum16(float v) {  // over a row of 16 lanes
@@ -825,19 +848,27 @@ __device__ __forceinline__ float sum16(float v) {  // over a row of 16 lanes
   v += row_rotated<2>(v);
   return v + row_rotated<1>(v);
 }
+// four numbers in pieces
+__device__ __forceinline__ void split_four(const f32x4& v, u32x2 (&o)[3]) {
+  const Pieces<3> p = split_tiles(v, f32x4{});
+#pragma unroll
+  for (int k = 0; k < 3; ++k) o[k] = u32x2{p.p[k][0], p.p[k][1]};
+}
 
+// Bound by the time of its loads: sixteen waves to a workgroup, of which a compute unit holds one, hide them better than eight with twice the registers
+// (4 x 2048 steps x 16 heads, bf16: see the table of figures).
 template <class E, int C, int DK>
-__global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
+__global__ __launch_bounds__(1024, 4) void delta_grad_kernel(DeltaArgs s) {
   typedef DeltaSizes<C, DK> Z;
   typedef DeltaGradShared<E, C, DK> Shared;
-  constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>();
-  constexpr int kMine = Z::kTiles * Z::kKeyTiles / 8;  // tiles of a wave: one column of keys, some rows of steps
-  constexpr int kLower = Z::kTiles * (Z::kTiles + 1) / 2, kJobs = (2 * kLower + 7) / 8;
+  constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>(), W = 16;
+  constexpr int kMine = Z::kTiles * Z::kKeyTiles / W;  // tiles of a wave: one column of keys, some rows of steps
+  constexpr int kLower = Z::kTiles * (Z::kTiles + 1) / 2, kJobs = (2 * kLower + W - 1) / W;
   extern __shared__ char delta_lds[];
   Shared& m = *(Shared*)delta_lds;
   const DeltaTable table = DELTA_TABLE(s);
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, row = lane & 15, g = lane >> 4;
-  const int kt = wave % Z::kKeyTiles, mt0 = wave / Z::kKeyTiles * kMine, key = kt * 16 + row;
+  int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kt = wave % Z::kKeyTiles, mt0 = wave / Z::kKeyTiles * kMine;
   const int hk = blockIdx.x % (uint32_t)s.n_hk, at_chunk = blockIdx.x / (uint32_t)s.n_hk;
   const int c = at_chunk % s.chunks, b = at_chunk / s.chunks;
   const DeltaChunk at = delta_chunk(s, b, c);
@@ -845,16 +876,15 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
   const int64_t step0 = (int64_t)b * at.steps + at.first;
   E* const dq = (E*)w->dq, * const dk = (E*)w->dk, * const dv = (E*)w->dv;
   if (at.live == 0) {
-    for (int i = tid; i < at.n * s.d_k; i += 512) {
+    for (int i = tid; i < at.n * s.d_k; i += 64 * W) {
       const int64_t o = ((step0 + i / s.d_k) * s.n_hk + hk) * s.d_k + i % s.d_k;
       st(dq, (size_t)o, 0.f);
       st(dk, (size_t)o, 0.f);
     }
-    for (int i = tid; i < at.n * s.each * s.d_v; i += 512) {
-      const int t = i / (s.each * s.d_v), j = i % (s.each * s.d_v);
-      st(dv, (size_t)(((step0 + t) * s.n_h + hk * s.each) * s.d_v + j), 0.f);
-    }
-    for (int i = tid; i < at.n * s.each; i += 512) {
+    const int columns = s.each * s.d_v;
+    for (int64_t i = tid; i < (int64_t)at.n * columns; i += 64 * W)
+      st(dv, (size_t)(((step0 + i / columns) * s.n_h + hk * s.each) * s.d_v + i % columns), 0.f);
+    for (int i = tid; i < at.n * s.each; i += 64 * W) {
       const int64_t o = (step0 + i / s.each) * s.n_h + hk * s.each + i % s.each;
       if (w->dg) w->dg[o] = 0.f;
       w->dbeta[o] = 0.f;
@@ -864,72 +894,79 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
   const int64_t key_at = (((int64_t)b * s.chunks + c) * s.n_hk + hk) * Z::kKeyPiece * NI;
   const uint16_t *const kf = s.kf + key_at, *const qf = s.qf + key_at, *const ktf = s.ktf + key_at, *const qtf = s.qtf + key_at;
   f32x4 sum_q[kMine] = {}, sum_k[kMine] = {};
+  // rows of the keys' arrays: a lane's key in step 16 mt0 + 4 g of the chunk, and steps behind it; what does not exist fails the checks
+  const uint32_t hop = (uint32_t)(s.n_hk * s.d_k) * (uint32_t)sizeof(E), key0 = (uint32_t)(kt * 16 + (tid & 15));
+  const uint32_t key_off = key0 < (uint32_t)s.d_k ? (uint32_t)(mt0 * 16 + 4 * ((tid & 63) >> 4)) * hop + key0 * (uint32_t)sizeof(E) : kOob;
+  auto key_rows = [&](const void* array, int n) {
+    n = __builtin_amdgcn_readfirstlane(n);
+    return rsrc_of((const E*)array + (step0 * s.n_hk + hk) * s.d_k, (uint32_t)(n - 1) * hop + (uint32_t)s.d_k * (uint32_t)sizeof(E));
+  };
+  auto key_value = [&](__amdgpu_buffer_rsrc_t from, int i, int r) {
+    const uint32_t step = (uint32_t)(i * 16 + r) * hop;
+    if constexpr (sizeof(E) == 4) return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, key_off, step, 0));
+    else return __uint_as_float((uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, key_off, step, 0) << 16);
+  };
 
   for (int e = 0; e < s.each; ++e) {
+    // (What is made of the thread's number is made again for each head: kept, it would not fit the registers.)
+    asm volatile("" : "+v"(tid));
+    const int lane = tid & 63, row = lane & 15, g = lane >> 4, key = kt * 16 + row;
     const int h = hk * s.each + e;
     const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h;
-    const float* const steps = s.steps + head * kStepNumbers * C;
+    __syncthreads();
+    if (tid < kStepNumbers * C) m.steps[tid / C][tid % C] = s.steps[head * kStepNumbers * C + tid];
+    __syncthreads();
     f32x4 os[kMine] = {}, rs[kMine] = {}, us[kMine] = {}, acc[kJobs] = {};
     float xdot = 0.f, both = 0.f;
+    // a thread's four columns of dR, U, X and dO
+    const int t4 = tid >> 4, col4 = (tid & 15) * 4;
+    const float beta4 = m.steps[kBeta][t4];
     for (int v0 = 0; v0 < s.d_v; v0 += 64) {
-      __syncthreads();
-      if (tid < C * 8) {
-        const int t = tid >> 3, col = (tid & 7) * 8, v = v0 + col;
-        float r8[8] = {}, u8[8] = {}, x8[8] = {};
-        if (v < s.dvp) {
-          const int64_t o = (head * C + t) * s.dvp + v;
-          Eight<float> raw;
-          raw.load(s.dr + o, 8);
-          raw.values(r8);
-          raw.load(s.u + o, 8);
-          raw.values(u8);
-          raw.load(s.x + o, 8);
-          raw.values(x8);
-        }
-        Eight<E> grads;
-        const int64_t o = ((step0 + t) * s.n_h + h) * s.d_v + v;
-        grads.load((const E*)w->d_o + o, t < at.live ? max(0, min(8, s.d_v - v)) : 0);
-        const float beta = steps[kBeta * C + t];
-        float out[8];
+      const int v = v0 + col4;
+      f32x4 r4 = {}, u4 = {}, x4 = {};
+      float o4[4] = {};
+      if (v < s.dvp) {
+        const int64_t o = (head * C + t4) * s.dvp + v;
+        r4 = *(const f32x4*)(s.dr + o);
+        u4 = *(const f32x4*)(s.u + o);
+        x4 = *(const f32x4*)(s.x + o);
+      }
+      const int64_t o = ((step0 + t4) * s.n_h + h) * s.d_v + v;
+      if (t4 < at.live) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          xdot = fmaf(r8[i], x8[i], xdot);
-          out[i] = t < at.live ? beta * r8[i] : 0.f;
-        }
-        if (t < at.n && v < s.d_v) store8(dv + o, out, min(8, s.d_v - v));
-        const Pieces<3> rp = split8(r8), up = split8(u8);
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {
-          *(u32x4*)&m.dr[k][t][col] = rp.p[k];
-          *(u32x4*)&m.u[k][t][col] = up.p[k];
-        }
-        if constexpr (NI == 1) {
-          *(u32x4*)&m.d_o[0][t][col] = grads.a;
-        } else {
-          float o8[8];
-          grads.values(o8);
-          const Pieces<3> op = split8(o8);
-#pragma unroll
-          for (int k = 0; k < 3; ++k) *(u32x4*)&m.d_o[k][t][col] = op.p[k];
-        }
+        for (int i = 0; i < 4; ++i)
+          if (v + i < s.d_v) o4[i] = ld((const E*)w->d_o, (size_t)(o + i));
       }
       __syncthreads();
-      for (int ks = 0; ks < 2 && v0 + 32 * ks < s.dvp; ++ks) {
-        const int at8 = 32 * ks + 8 * g, v = v0 + at8;
-        float s8[8] = {}, d8[8] = {};
-        if (v < s.dvp) {
-          const int64_t o = (head * DK + key) * s.dvp + v;
-          Eight<float> raw;
-          raw.load(s.states + o, 8);
-          raw.values(s8);
-          raw.load(s.dstates + o, 8);
-          raw.values(d8);
-        }
-        if (mt0 == 0) {
+      u32x2 p[3];
+      split_four(r4, p);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) both = fmaf(s8[i], d8[i], both);
+      for (int k = 0; k < 3; ++k) *(u32x2*)&m.dr[k][t4][col4] = p[k];
+      split_four(u4, p);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) *(u32x2*)&m.u[k][t4][col4] = p[k];
+      split_four(f32x4{o4[0], o4[1], o4[2], o4[3]}, p);  // (bf16 numbers are their upper halves)
+#pragma unroll
+      for (int k = 0; k < NI; ++k) *(u32x2*)&m.d_o[k][t4][col4] = p[k];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        xdot = fmaf(r4[i], x4[i], xdot);
+        if (t4 < at.n && v + i < s.d_v) st(dv, (size_t)(o + i), t4 < at.live ? beta4 * r4[i] : 0.f);
+      }
+#pragma unroll 1
+      for (int ks = 0; ks < 2; ++ks) {
+        if (v0 + 32 * ks >= s.dvp) break;
+        const int at8 = 32 * ks + 8 * g;
+        f32x4 s8[2] = {}, d8[2] = {};
+        if (v0 + at8 < s.dvp) {
+          const int64_t o = (head * DK + key) * s.dvp + v0 + at8;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            s8[i] = *(const f32x4*)(s.states + o + 4 * i);
+            d8[i] = *(const f32x4*)(s.dstates + o + 4 * i);
+          }
         }
-        const Pieces<3> sp = split8(s8), dp = split8(d8);
         auto rows3 = [&](const uint16_t (*from)[C][Shared::kRow], int mt) {
           Pieces<3> o;
 #pragma unroll
@@ -943,46 +980,62 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
           return o;
         };
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-          os[i] = multiply(grads(mt0 + i), sp, os[i]);
-          rs[i] = multiply(rows3(m.dr, mt0 + i), sp, rs[i]);
-          us[i] = multiply(rows3(m.u, mt0 + i), dp, us[i]);
-        }
-#pragma unroll
         for (int i = 0; i < kJobs; ++i) {
-          const int job = wave + 8 * i;
+          const int job = wave + W * i;
           if (job < 2 * kLower) {
-            const int what = job / kLower, tile = job % kLower, mt = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, nt = tile - mt * (mt + 1) / 2;
-            const Pieces<3> right = rows3(m.u, nt);
-            if (what) acc[i] = multiply(grads(mt), right, acc[i]);
-            else acc[i] = multiply(rows3(m.dr, mt), right, acc[i]);
+            const DeltaLower at_tile = delta_lower(job % kLower);
+            const Pieces<3> right = rows3(m.u, at_tile.nt);
+            if (job / kLower) acc[i] = multiply(grads(at_tile.mt), right, acc[i]);
+            else acc[i] = multiply(rows3(m.dr, at_tile.mt), right, acc[i]);
           }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if (mt0 == 0) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) both = fmaf(s8[i / 4][i % 4], d8[i / 4][i % 4], both);
+        }
+        {
+          const Pieces<3> sp = split_tiles(s8[0], s8[1]);
+#pragma unroll
+          for (int i = 0; i < kMine; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            os[i] = multiply(grads(mt0 + i), sp, os[i]);
+            rs[i] = multiply(rows3(m.dr, mt0 + i), sp, rs[i]);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const Pieces<3> dp = split_tiles(d8[0], d8[1]);
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) us[i] = multiply(rows3(m.u, mt0 + i), dp, us[i]);
       }
     }
     __syncthreads();
+    asm volatile("" : "+v"(tid));
     // M and N
 #pragma unroll
     for (int x = 0; x < kJobs; ++x) {
-      const int job = wave + 8 * x;
+      const int job = wave + W * x;
       if (job >= 2 * kLower) continue;
-      const int what = job / kLower, tile = job % kLower, mt = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, nt = tile - mt * (mt + 1) / 2;
-      f32x4 dots = {};
+      const int what = job / kLower;
+      const DeltaLower at_tile = delta_lower(job % kLower);
+      const int mt = at_tile.mt, nt = at_tile.nt, j = nt * 16 + row;
+      __builtin_amdgcn_sched_barrier(0);  // (one tile after the other: interleaved they do not fit the registers)
+      f32x4 inner = {};  // K K^T or Q K^T
+#pragma unroll
       for (int ks = 0; ks < Z::kKeySteps; ++ks)
-        dots = multiply(load_fragment<NI>((what ? qf : kf) + (mt * Z::kKeySteps + ks) * NI * kFragment),
-                        load_fragment<NI>(kf + (nt * Z::kKeySteps + ks) * NI * kFragment), dots);
-      const int j = nt * 16 + row;
-      const float whole = steps[kWhole * C + j], rest = steps[kRest * C + j];
+        inner = multiply(load_fragment<NI>((what ? qf : kf) + (mt * Z::kKeySteps + ks) * NI * kFragment),
+                         load_fragment<NI>(kf + (nt * Z::kKeySteps + ks) * NI * kFragment), inner);
+      const float whole = m.steps[kWhole][j], rest = m.steps[kRest][j];
       float down = 0.f;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int i = mt * 16 + 4 * g + r;
         const bool below = i > j, in = what ? i >= j : below;
-        const float decay = in ? expf((steps[kWhole * C + i] - whole) + (steps[kRest * C + i] - rest)) : 0.f;
-        const float d = in ? decay * (what ? s.scale * acc[x][r] : -acc[x][r]) : 0.f, beta = what ? 1.f : steps[kBeta * C + i];
-        const float mine = d * beta, part = below ? mine * dots[r] : 0.f;
+        const float decay = in ? expf((m.steps[kWhole][i] - whole) + (m.steps[kRest][i] - rest)) : 0.f;
+        const float d = in ? decay * (what ? s.scale * acc[x][r] : -acc[x][r]) : 0.f, beta = what ? 1.f : m.steps[kBeta][i];
+        const float mine = d * beta, part = below ? mine * inner[r] : 0.f;
         down += part;
-        const float across = sum16(part), for_beta = sum16(below ? d * dots[r] : 0.f);
+        const float across = sum16(part), for_beta = sum16(below ? d * inner[r] : 0.f);
         if (row == 0) {
           m.row_sum[what][nt][i] = across;
           if (!what) m.beta_sum[nt][i] = for_beta;
@@ -990,7 +1043,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
         if (what) {
           m.inner[1][i][j] = mine;
           if (mt != nt) m.inner[1][nt * 16 + 4 * g + r][mt * 16 + row] = 0.f;
-        } else if (below || mt != nt) {
+        } else if (below) {
           m.inner[0][i][j] = mine;
           m.inner[0][j][i] = mine;
         } else if (i == j) {
@@ -1004,14 +1057,13 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
     // what the states' products come to
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int t = (mt0 + i) * 16 + 4 * g + r;
-        const bool in = t < at.live && key < s.d_k;
-        const int64_t o = ((step0 + t) * s.n_hk + hk) * s.d_k + key;
-        const float qv = in ? ld((const E*)w->q, (size_t)o) : 0.f, kv = in ? ld((const E*)w->k, (size_t)o) : 0.f;
-        const float since = steps[kSince * C + t], one = s.scale * since * os[i][r], two = since * steps[kBeta * C + t] * rs[i][r],
-                    three = steps[kUntil * C + t] * us[i][r];
+        const float qv = key_value(key_rows(w->q, at.live), i, r), kv = key_value(key_rows(w->k, at.live), i, r);
+        const float since = m.steps[kSince][t], one = s.scale * since * os[i][r], two = since * m.steps[kBeta][t] * rs[i][r],
+                    three = m.steps[kUntil][t] * us[i][r];
         const float all = sum16(fmaf(qv, one, -kv * (two + three))), end = sum16(kv * three);
         if (row == 0) {
           m.dots[kt][t] = all;
@@ -1023,10 +1075,8 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
     }
     both = wave_sum(both);
     if (lane == 0 && mt0 == 0) m.both[kt] = both;
-    xdot += __shfl_xor(xdot, 1, 64);
-    xdot += __shfl_xor(xdot, 2, 64);
-    xdot += __shfl_xor(xdot, 4, 64);
-    if ((tid & 7) == 0 && tid < C * 8) m.xs[tid >> 3] = xdot;
+    xdot = sum16(xdot);
+    if ((tid & 15) == 0) m.xs[t4] = xdot;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < Z::kSteps; ++k) {
@@ -1034,6 +1084,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
         const int mt = mt0 + i, t = mt * 16 + row;
+        __builtin_amdgcn_sched_barrier(0);
         auto across = [&](const float (*from)[Shared::kLine]) {
           return first_pieces<NO>(split_tiles(*(const f32x4*)&from[t][32 * k + 4 * g], *(const f32x4*)&from[t][32 * k + 16 + 4 * g]));
         };
@@ -1047,25 +1098,21 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
         }
       }
     }
-    if (wave == 0 && (w->dg || w->dbeta)) {
-      const bool in = lane < C;
-      float d = 0.f, end = 0.f, for_beta = in ? m.xs[lane] : 0.f;
-      if (in) {
-        const int tile = lane >> 4;
-        for (int what = 0; what < 2; ++what) {
-          for (int i = 0; i <= tile; ++i) d += m.row_sum[what][i][lane];
-          for (int i = tile; i < Z::kTiles; ++i) d -= m.col_sum[what][i][lane];
-        }
-        for (int i = 0; i <= tile; ++i) for_beta += m.beta_sum[i][lane];
-        for (int i = 0; i < Z::kKeyTiles; ++i) {
-          d += m.dots[i][lane];
-          end += m.ends[i][lane];
-        }
+    if (wave == 0) {
+      const int tile = lane >> 4;
+      float d = 0.f, end = 0.f, for_beta = m.xs[lane], all = 0.f;
+      for (int what = 0; what < 2; ++what) {
+        for (int i = 0; i <= tile; ++i) d += m.row_sum[what][i][lane];
+        for (int i = tile; i < Z::kTiles; ++i) d -= m.col_sum[what][i][lane];
+      }
+      for (int i = 0; i <= tile; ++i) for_beta += m.beta_sum[i][lane];
+      for (int i = 0; i < Z::kKeyTiles; ++i) {
+        d += m.dots[i][lane];
+        end += m.ends[i][lane];
+        all += m.both[i];
       }
       end = wave_sum(end);
-      float all = 0.f;
-      for (int i = 0; i < Z::kKeyTiles; ++i) all += m.both[i];
-      if (lane == C - 1) d += end + steps[C - 1] * all;
+      if (lane == C - 1) d += end + m.steps[kSince][C - 1] * all;
 #pragma unroll
       for (int o = 1; o < C; o *= 2) {
         const float later = __shfl_down(d, o, 64);
@@ -1078,15 +1125,20 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
       }
     }
   }
+  const __amdgpu_buffer_rsrc_t to_q = key_rows(dq, at.n), to_k = key_rows(dk, at.n);
 #pragma unroll
   for (int i = 0; i < kMine; ++i)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int t = (mt0 + i) * 16 + 4 * g + r;
-      if (t < at.n && key < s.d_k) {
-        const int64_t o = ((step0 + t) * s.n_hk + hk) * s.d_k + key;
-        st(dq, (size_t)o, t < at.live ? sum_q[i][r] : 0.f);
-        st(dk, (size_t)o, t < at.live ? sum_k[i][r] : 0.f);
+      const bool in = (mt0 + i) * 16 + 4 * ((tid & 63) >> 4) + r < at.live;
+      const uint32_t step = (uint32_t)(i * 16 + r) * hop;
+      const float q = in ? sum_q[i][r] : 0.f, k = in ? sum_k[i][r] : 0.f;
+      if constexpr (sizeof(E) == 4) {
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(q), to_q, key_off, step, 0);
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(k), to_k, key_off, step, 0);
+      } else {
+        __builtin_amdgcn_raw_buffer_store_b16(to_bf16(q), to_q, key_off, step, 0);
+        __builtin_amdgcn_raw_buffer_store_b16(to_bf16(k), to_k, key_off, step, 0);
       }
     }
 }
@@ -1291,7 +1343,7 @@ static int launch_delta(distdl_delta_plan* p, DeltaArgs& s, hipStream_t st) {
     else hipLaunchKernelGGL((delta_bwd_kernel<E, DK, 1>), groups, dim3(512), 0, st, s);
     constexpr auto grad = delta_grad_kernel<E, C, DK>;
     if ((rc = allow_large_lds<grad>())) return rc;
-    hipLaunchKernelGGL(grad, chunks, dim3(512), sizeof(DeltaGradShared<E, C, DK>), st, s);
+    hipLaunchKernelGGL(grad, chunks, dim3(1024), sizeof(DeltaGradShared<E, C, DK>), st, s);
   }
   return DISTDL_OK;
 }
