@@ -15,8 +15,10 @@
 #include <cfloat>
 #include <climits>
 #include <cstddef>
+#include <type_traits>
 
 #include "block8.h"
+#include "buffer.h"
 #include "common.h"
 #include "profile.h"
 
@@ -86,30 +88,64 @@ __device__ __forceinline__ float logits_at(const LogitsArgs& s, LogitsTable tabl
 }
 
 // Eight neighbouring entries of a row.  A part's last vector starts so that it ends with the part, and of its entries those from `from`
-// on are its own: every load is whole and inside the row.  (Parts of fewer than eight entries are read one by one.)
-template <class E>
+// on are its own: every load is whole and inside the row.  TINY: parts of fewer than eight entries, read one by one.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t logits_row(const void* x, int64_t row, int n, size_t size) {
+  return rsrc_of((const char*)x + row * n * size, (uint32_t)n * (uint32_t)size);
+}
+template <class E, bool TINY>
 struct LogitsVector {
-  Eight<E> raw;
-  int at, from;
-  __device__ __forceinline__ void load(const E* row, int n, int v, int end) {
-    at = max(0, min(8 * v, n - 8));
-    from = v < end ? 8 * v - at : 8;
-    if (n >= 8) raw.load(row + at, 8);
-    else raw.load(row, n);
+  u32x4 raw[sizeof(E) / 2];
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t row, int n, int v) {
+    if constexpr (TINY) {
+      uint32_t e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {  // (what lies behind the row fails the check and is 0)
+        if constexpr (sizeof(E) == 4) e[i] = __builtin_amdgcn_raw_buffer_load_b32(row, i * 4, 0, 0);
+        else e[i] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(row, i * 2, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(E) == 4) raw[0][i] = e[i], raw[1][i] = e[i + 4];
+        else raw[0][i] = e[2 * i] | e[2 * i + 1] << 16;
+      }
+    } else {
+      const uint32_t o = (uint32_t)min(8 * v, n - 8) * (uint32_t)sizeof(E);
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(E) / 2; ++i) raw[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(row, o, i * 16, 0));
+    }
   }
-  // values; -inf in the places that are not its own, if `edge` (uniform) says that there may be such
-  __device__ __forceinline__ void values(float* f, int n, bool edge) const {
-    raw.values(f);
+  // Values; -inf in the places that are not its own.  edge: there may be vectors behind `end`; ragged: the part's last one may begin before its place
+  // (both uniform).
+  __device__ __forceinline__ void values(float* f, int n, int v, int end, bool edge, bool ragged) {
     if (edge) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(E) / 2; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) raw[i][k] = v < end ? raw[i][k] : sizeof(E) == 4 ? 0xff800000u : 0xff80ff80u;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(E) == 4) {
+        f[i] = __uint_as_float(raw[0][i]);
+        f[i + 4] = __uint_as_float(raw[1][i]);
+      } else {
+        f[2 * i] = bf16_lo(raw[0][i]);
+        f[2 * i + 1] = bf16_hi(raw[0][i]);
+      }
+    }
+    if (ragged) {
+      const int from = v < end ? first_of(n, v) : 8;
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[i] = i >= from && i < n ? f[i] : -INFINITY;
     }
   }
+  static __device__ __forceinline__ int place(int n, int v) { return max(0, min(8 * v, n - 8)); }
+  static __device__ __forceinline__ int first_of(int n, int v) { return 8 * v - place(n, v); }
 };
 template <class E>
 constexpr int logits_batch() { return sizeof(E) == 2 ? 4 : 2; }  // vectors of a lane under way: 64 bytes
 
-// f(worker, part, first vector of the lane's batch, end) for the batches of the split's vectors
+// f(worker, part, first vector of the workgroup's batch, end) for the batches of the split's vectors
 template <int B, int THREADS, class F>
 __device__ __forceinline__ void logits_each(const LogitsArgs& s, int split, F f) {
   const int lo = split * s.per, hi = min(lo + s.per, s.extra * s.vec_wide + (s.P - s.extra) * s.vec_rest);
@@ -150,15 +186,12 @@ struct LogitsSums {
     w += o.w;
   }
   __device__ __forceinline__ void join_lanes(float c) {
+    float most = m;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      LogitsSums other;
-      other.m = __shfl_xor(m, o, 64);
-      other.mc = __shfl_xor(mc, o, 64);
-      other.s = __shfl_xor(s, o, 64);
-      other.w = __shfl_xor(w, o, 64);
-      join(other, c);
-    }
+    for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+    raise(most, c);
+    s = wave_sum(s);
+    w = wave_sum(w);
   }
   // The sums of all waves, for all threads.  `shared`: a place for each wave.
   template <int WAVES>
@@ -184,12 +217,9 @@ template <int N, bool ENTROPY>
 __device__ __forceinline__ void logits_add(LogitsSums& a, const float (&f)[N], float most, float c) {
   a.raise(fmaxf(a.m, most), c);
   if (__builtin_expect(__any(a.far()), 0)) {
-#pragma unroll 1
-    for (int i = 0; i < N; ++i) {
-      float x = f[0];
 #pragma unroll
-      for (int k = 1; k < N; ++k) x = i == k ? f[k] : x;
-      const float d = a.of(x, c), e = __builtin_amdgcn_exp2f(d);
+    for (int i = 0; i < N; ++i) {
+      const float d = a.of(f[i], c), e = __builtin_amdgcn_exp2f(d);
       a.s += e;
       if (ENTROPY) a.w = fmaf(e, fmaxf(d, -200.f), a.w);
     }
@@ -320,7 +350,7 @@ __device__ __forceinline__ void logits_finish(const LogitsArgs& s, LogitsTable t
 }
 
 // A row, or one of its splits, to a workgroup.
-template <class E, bool ENTROPY, bool TOP>
+template <class E, bool ENTROPY, bool TOP, bool TINY>
 __global__ __launch_bounds__(kLogitsThreads) void logits_fwd_kernel(LogitsArgs s) {
   constexpr int B = logits_batch<E>();
   __shared__ float4 sums[kLogitsWaves];
@@ -333,15 +363,16 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_fwd_kernel(LogitsArgs s
   TopList list;
   bool first = true;
   logits_each<B, kLogitsThreads>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
-    const E* const x = (const E*)table[j].x + row * p.n;
-    LogitsVector<E> v[B];
+    const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
+    typedef LogitsVector<E, TINY> Vector;
+    Vector v[B];
     float f[B * 8], most[B], all = -INFINITY;
+    const int v0 = base + tid, end = base + B * kLogitsThreads;
 #pragma unroll
-    for (int b = 0; b < B; ++b) v[b].load(x, p.n, base + b * kLogitsThreads + tid, to);
-    const bool edge = base + B * kLogitsThreads >= to;  // (a last vector, or none)
+    for (int b = 0; b < B; ++b) v[b].load(x, p.n, v0 + b * kLogitsThreads);
 #pragma unroll
     for (int b = 0; b < B; ++b) {
-      v[b].values(f + 8 * b, p.n, edge);
+      v[b].values(f + 8 * b, p.n, v0 + b * kLogitsThreads, to, end > to, p.n % 8 != 0 && end >= p.vecs);
       most[b] = max8(f + 8 * b);
       all = fmaxf(all, most[b]);
     }
@@ -351,7 +382,10 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_fwd_kernel(LogitsArgs s
       first = false;
 #pragma unroll
       for (int b = 0; b < B; ++b)
-        if (__any(order_of(most[b]) > list.floor)) list.take(buffer, f + 8 * b, p.first + v[b].at, v[b].from, p.n, s.n_top);
+        if (__any(order_of(most[b]) > list.floor)) {
+          const int i = v0 + b * kLogitsThreads;
+          list.take(buffer, f + 8 * b, p.first + Vector::place(p.n, i), i < to ? Vector::first_of(p.n, i) : 8, p.n, s.n_top);
+        }
     }
   });
   if constexpr (TOP) {
@@ -417,7 +451,7 @@ __device__ __forceinline__ void logits_store(E* row, const float* f, int at, int
   }
 }
 
-template <class E, bool ENTROPY>
+template <class E, bool ENTROPY, bool TINY>
 __global__ __launch_bounds__(kLogitsThreads) void logits_bwd_kernel(LogitsArgs s) {
   constexpr int B = logits_batch<E>();
   const LogitsTable table = LOGITS_TABLE(s);
@@ -432,21 +466,22 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_bwd_kernel(LogitsArgs s
   const bool far = lse >= kFar;
   const float lc = lse * (1.f / kLn2), at_target = weight * s.inv_t;
   logits_each<B, kLogitsThreads>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
-    const E* const x = (const E*)table[j].x + row * p.n;
+    const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
     E* const dx = (E*)table[j].dx + row * p.n;
-    LogitsVector<E> v[B];
+    typedef LogitsVector<E, TINY> Vector;
+    Vector v[B];
     const bool edge = base + B * kLogitsThreads >= to;  // (a last vector, or none)
     if (!nothing) {
 #pragma unroll
-      for (int b = 0; b < B; ++b) v[b].load(x, p.n, base + b * kLogitsThreads + tid, to);
+      for (int b = 0; b < B; ++b) v[b].load(x, p.n, base + b * kLogitsThreads + tid);
     }
 #pragma unroll
     for (int b = 0; b < B; ++b) {
       float f[8] = {};
       const int i0 = base + b * kLogitsThreads + tid;
-      const int at = max(0, min(8 * i0, p.n - 8)), from = i0 < to ? 8 * i0 - at : 8;
+      const int at = Vector::place(p.n, i0), from = i0 < to ? Vector::first_of(p.n, i0) : 8;
       if (!nothing) {
-        v[b].values(f, p.n, edge);
+        v[b].values(f, p.n, i0, to, false, false);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float d = far ? fmaf(f[i], s.inv_t, -lse) * (1.f / kLn2) : fmaf(f[i], s.c, -lc), e = __builtin_amdgcn_exp2f(d);
@@ -523,7 +558,7 @@ __device__ __forceinline__ float stored_loss(const LogitsArgs& s, Stored& t, flo
 
 // FIRST: the sums of a split and the student's logits at the teacher's places in it.  Else the loss and the gradient, of rows that
 // are one workgroup's (splits == 1, which reads the row for its sums too) or of a split.
-template <class E, bool FIRST>
+template <class E, bool FIRST, bool TINY>
 __global__ __launch_bounds__(kLogitsThreads) void distill_kernel(LogitsArgs s) {
   constexpr int B = logits_batch<E>();
   __shared__ float4 sums[kLogitsWaves];
@@ -553,15 +588,15 @@ __global__ __launch_bounds__(kLogitsThreads) void distill_kernel(LogitsArgs s) {
   const bool sum_here = FIRST || s.splits == 1;
   if (sum_here && (FIRST || any)) {
     logits_each<B, kLogitsThreads>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
-      const E* const x = (const E*)table[j].x + row * p.n;
-      LogitsVector<E> v[B];
+      const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
+      LogitsVector<E, TINY> v[B];
       float f[B * 8], all = -INFINITY;
+      const int v0 = base + tid, end = base + B * kLogitsThreads;
 #pragma unroll
-      for (int b = 0; b < B; ++b) v[b].load(x, p.n, base + b * kLogitsThreads + tid, to);
-      const bool edge = base + B * kLogitsThreads >= to;  // (a last vector, or none)
+      for (int b = 0; b < B; ++b) v[b].load(x, p.n, v0 + b * kLogitsThreads);
 #pragma unroll
       for (int b = 0; b < B; ++b) {
-        v[b].values(f + 8 * b, p.n, edge);
+        v[b].values(f + 8 * b, p.n, v0 + b * kLogitsThreads, to, end > to, p.n % 8 != 0 && end >= p.vecs);
         all = fmaxf(all, max8(f + 8 * b));
       }
       logits_add<B * 8, false>(a, f, all, s.c);
@@ -589,21 +624,22 @@ __global__ __launch_bounds__(kLogitsThreads) void distill_kernel(LogitsArgs s) {
   const bool nothing = weight == 0.f;  // such rows are not read
   __syncthreads();
   logits_each<B, kLogitsThreads>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
-    const E* const x = (const E*)table[j].x + row * p.n;
+    const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
     E* const dx = (E*)table[j].dx + row * p.n;
-    LogitsVector<E> v[B];
+    typedef LogitsVector<E, TINY> Vector;
+    Vector v[B];
     const bool edge = base + B * kLogitsThreads >= to;  // (a last vector, or none)
     if (!nothing) {
 #pragma unroll
-      for (int b = 0; b < B; ++b) v[b].load(x, p.n, base + b * kLogitsThreads + tid, to);
+      for (int b = 0; b < B; ++b) v[b].load(x, p.n, base + b * kLogitsThreads + tid);
     }
 #pragma unroll
     for (int b = 0; b < B; ++b) {
       float f[8] = {};
       const int i0 = base + b * kLogitsThreads + tid;
-      const int at = max(0, min(8 * i0, p.n - 8)), from = i0 < to ? 8 * i0 - at : 8;
+      const int at = Vector::place(p.n, i0), from = i0 < to ? Vector::first_of(p.n, i0) : 8;
       if (!nothing) {
-        v[b].values(f, p.n, edge);
+        v[b].values(f, p.n, i0, to, false, false);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] = scale * __builtin_amdgcn_exp2f(far ? a.of(f[i], s.c) - stotal : fmaf(f[i], s.c, -off));
       }
@@ -702,19 +738,32 @@ static int logits_aligned(const char* call, std::initializer_list<const void*> a
   return DISTDL_OK;
 }
 
-template <class E, bool ENTROPY>
+template <class E, bool ENTROPY, bool TINY>
 static void launch_logits_fwd(const LogitsArgs& s, hipStream_t st) {
   const dim3 grid((unsigned)(s.rows * s.splits)), block(kLogitsThreads);
-  if (s.n_top > 0) hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, true>), grid, block, 0, st, s);
-  else hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, false>), grid, block, 0, st, s);
+  if (s.n_top > 0) hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, true, TINY>), grid, block, 0, st, s);
+  else hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, false, TINY>), grid, block, 0, st, s);
   if (s.splits > 1) hipLaunchKernelGGL((logits_join_kernel<E>), dim3((unsigned)s.rows), block, 0, st, s);
 }
 
-template <class E>
+template <class E, bool ENTROPY, bool TINY>
+static void launch_logits_bwd(const LogitsArgs& s, hipStream_t st) {
+  hipLaunchKernelGGL((logits_bwd_kernel<E, ENTROPY, TINY>), dim3((unsigned)(s.rows * s.splits)), dim3(kLogitsThreads), 0, st, s);
+}
+
+template <class E, bool TINY>
 static void launch_distill(const LogitsArgs& s, hipStream_t st) {
   const dim3 grid((unsigned)(s.rows * s.splits)), block(kLogitsThreads);
-  if (s.splits > 1) hipLaunchKernelGGL((distill_kernel<E, true>), grid, block, 0, st, s);
-  hipLaunchKernelGGL((distill_kernel<E, false>), grid, block, 0, st, s);
+  if (s.splits > 1) hipLaunchKernelGGL((distill_kernel<E, true, TINY>), grid, block, 0, st, s);
+  hipLaunchKernelGGL((distill_kernel<E, false, TINY>), grid, block, 0, st, s);
+}
+
+// f(element, whether there is an option, whether a worker has fewer than eight entries)
+template <class F>
+static void logits_kind(distdl_dtype dtype, bool option, bool tiny, F f) {
+  auto by_tiny = [&](auto e, auto o) { tiny ? f(e, o, std::true_type()) : f(e, o, std::false_type()); };
+  auto by_option = [&](auto e) { option ? by_tiny(e, std::true_type()) : by_tiny(e, std::false_type()); };
+  dtype == DISTDL_F32 ? by_option(float()) : by_option(uint16_t());
 }
 
 }  // namespace distdl
@@ -782,8 +831,8 @@ int distdl_logprob_fwd(distdl_logits_plan* p, const void* const x_dev[], const i
     }
     {
       ProfScope prof("logprob_fwd", st_);
-      if (p->dtype == DISTDL_F32) entropy_dev ? launch_logits_fwd<float, true>(s, st_) : launch_logits_fwd<float, false>(s, st_);
-      else entropy_dev ? launch_logits_fwd<uint16_t, true>(s, st_) : launch_logits_fwd<uint16_t, false>(s, st_);
+      logits_kind(p->dtype, entropy_dev != nullptr, s.part < 8,
+                  [&](auto e, auto entropy, auto tiny) { launch_logits_fwd<decltype(e), decltype(entropy)::value, decltype(tiny)::value>(s, st_); });
     }
     DISTDL_HIP_TRY(hipGetLastError());
     return DISTDL_OK;
@@ -811,14 +860,8 @@ int distdl_logprob_bwd(distdl_logits_plan* p, const void* const x_dev[], const i
     s.dentropy = dentropy_dev;
     {
       ProfScope prof("logprob_bwd", st_);
-      const dim3 grid((unsigned)(s.rows * s.splits)), block(kLogitsThreads);
-      if (p->dtype == DISTDL_F32) {
-        if (dentropy_dev) hipLaunchKernelGGL((logits_bwd_kernel<float, true>), grid, block, 0, st_, s);
-        else hipLaunchKernelGGL((logits_bwd_kernel<float, false>), grid, block, 0, st_, s);
-      } else {
-        if (dentropy_dev) hipLaunchKernelGGL((logits_bwd_kernel<uint16_t, true>), grid, block, 0, st_, s);
-        else hipLaunchKernelGGL((logits_bwd_kernel<uint16_t, false>), grid, block, 0, st_, s);
-      }
+      logits_kind(p->dtype, dentropy_dev != nullptr, s.part < 8,
+                  [&](auto e, auto entropy, auto tiny) { launch_logits_bwd<decltype(e), decltype(entropy)::value, decltype(tiny)::value>(s, st_); });
     }
     DISTDL_HIP_TRY(hipGetLastError());
     return DISTDL_OK;
@@ -852,8 +895,7 @@ int distdl_distill_fwd_bwd(distdl_logits_plan* p, const void* const x_dev[], con
     }
     {
       ProfScope prof("distill", st_);
-      if (p->dtype == DISTDL_F32) launch_distill<float>(s, st_);
-      else launch_distill<uint16_t>(s, st_);
+      logits_kind(p->dtype, false, s.part < 8, [&](auto e, auto, auto tiny) { launch_distill<decltype(e), decltype(tiny)::value>(s, st_); });
     }
     DISTDL_HIP_TRY(hipGetLastError());
     return DISTDL_OK;
