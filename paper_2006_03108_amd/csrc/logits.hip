@@ -215,7 +215,7 @@ struct LogitsSums {
 // A batch of a lane's values.  The entropy's w counts what exp2 makes 0 as 0, -inf too.
 template <int N, bool ENTROPY>
 __device__ __forceinline__ void logits_add(LogitsSums& a, const float (&f)[N], float most, float c) {
-  a.raise(fmaxf(a.m, most), c);
+  if (__any(most > a.m)) a.raise(fmaxf(a.m, most), c);
   if (__builtin_expect(__any(a.far()), 0)) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -232,9 +232,13 @@ __device__ __forceinline__ void logits_add(LogitsSums& a, const float (&f)[N], f
     if (ENTROPY) a.w = fmaf(e, fmaxf(d, -200.f), a.w);
   }
 }
-__device__ __forceinline__ float max8(const float* f) {
-  return fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
+// (fmaxf of loaded numbers costs an instruction more for each, which makes signalling NaNs quiet)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
 }
+__device__ __forceinline__ float max8(const float* f) { return max3(max3(max3(f[0], f[1], f[2]), f[3], f[4]), max3(f[5], f[6], f[7]), f[7]); }
 
 // ---- top alternatives -----------------------------------------------------
 // An entry's key: its value as an integer in the same order, above the complement of its place, so that larger keys come first.  0 is no entry.
@@ -285,21 +289,24 @@ __device__ __forceinline__ uint64_t merged_lanes(uint64_t a, uint64_t b) {
   return bitonic<64>(a > b ? a : b, true);
 }
 
-// A wave's 64 best entries, descending over the lanes, and a buffer of those that wait.  Entries at or below `floor`, the n-th best so far, can
-// not be among the n: a wave meets entries in the order of their places, so of equal values the first stay.
+// A wave's 64 best entries, descending over the lanes, and a buffer of those that wait.  Values at or below `floor`, the n-th best so far, can
+// not be among the n: a wave meets entries in the order of their places, so of equal values the first stay.  (A NaN, at first, lets all pass.)
 struct TopList {
   uint64_t best = 0;
-  int32_t floor = INT_MIN;
+  float floor = NAN;
   int waiting = 0;
   static constexpr int kRoom = 64 + 512;
+  __device__ __forceinline__ bool passes(float v) const { return !(v <= floor); }
   __device__ __forceinline__ void set_floor(int n_top) {
     const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(best >> 32), n_top - 1);
-    floor = max(floor, (int32_t)(hi ^ 0x80000000u));
+    const float nth = value_of((uint64_t)hi << 32);
+    if (hi != 0 && !(nth <= floor)) floor = nth;
   }
-  // From the largest of each lane's first entries: the n-th of them is no better than the n-th of all.
+  // From the largest of each lane's first entries: the n-th of them is no better than the n-th of all, and may be it.
   __device__ __forceinline__ void start(float most, int n_top) {
     const int32_t nth = __builtin_amdgcn_readlane(sorted_lanes(order_of(most)), n_top - 1);
-    floor = max(nth, INT_MIN + 1) - 1;
+    const int32_t below = nth == 0 ? order_of(-FLT_MIN) : nth - 1;  // (-0, which comes next, is no less than 0)
+    if (nth > order_of(-INFINITY)) floor = __uint_as_float((uint32_t)(below ^ ((below >> 31) & 0x7fffffff)));
   }
   __device__ __forceinline__ void flush(uint64_t* buffer, int n_top) {
     const int lane = threadIdx.x & 63;
@@ -311,25 +318,41 @@ struct TopList {
     __builtin_amdgcn_wave_barrier();
     set_floor(n_top);
   }
-  // a vector of each lane
-  __device__ __forceinline__ void take(uint64_t* buffer, const float* f, int id, int from, int upto, int n_top) {
-    const int lane = threadIdx.x & 63;
+  __device__ __forceinline__ void push(uint64_t* buffer, bool in, float v, int id) {
+    const uint64_t all = __ballot(in);
+    if (in) buffer[waiting + __popcll(all & ((uint64_t(1) << (threadIdx.x & 63)) - 1))] = key_of(order_of(v), id);
+    waiting += __popcll(all);
+  }
+  // A vector of each lane, some lane's largest value `most` of which passes; mostly it is one value of one lane.
+  __device__ __forceinline__ void take(uint64_t* buffer, const float* f, float most, int id, int from, int upto, int n_top) {
+    int count = 0, first = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int32_t o = order_of(f[i]);
-      const bool in = o > floor && i >= from && i < upto;
-      const uint64_t all = __ballot(in);
-      if (in) buffer[waiting + __popcll(all & ((uint64_t(1) << lane) - 1))] = key_of(o, id + i);
-      waiting += __popcll(all);
+    for (int i = 7; i >= 0; --i) {
+      const bool in = passes(f[i]) && f[i] == f[i] && i >= from && i < upto;
+      count += in;
+      first = in ? i : first;
+    }
+    if (!__any(count > 1)) {
+      push(buffer, count > 0, most, id + first);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) push(buffer, passes(f[i]) && f[i] == f[i] && i >= from && i < upto, f[i], id + i);
     }
     __builtin_amdgcn_wave_barrier();
     if (waiting >= 64) flush(buffer, n_top);
   }
 };
 
-// What a row's sums and alternatives come to.  Every wave has the sums; wave 0 has the list.
+// The target's logit, for the first thread: it is asked for before the row is read.
 template <class E>
-__device__ __forceinline__ void logits_finish(const LogitsArgs& s, LogitsTable table, int64_t row, const LogitsSums& a, uint64_t best) {
+__device__ __forceinline__ float logits_target(const LogitsArgs& s, LogitsTable table, int64_t row) {
+  if (threadIdx.x != 0 || !s.logp) return 0.f;
+  const int t = s.targets[row];
+  return t >= 0 && t < s.n_v ? logits_at<E>(s, table, row, t) : 0.f;
+}
+
+// What a row's sums and alternatives come to.  Every wave has the sums; wave 0 has the list.
+__device__ __forceinline__ void logits_finish(const LogitsArgs& s, int64_t row, const LogitsSums& a, uint64_t best, float x_target) {
   const float total = __builtin_amdgcn_logf(a.s);  // log2
   const bool none = a.none();
   if (threadIdx.x == 0) {
@@ -338,7 +361,7 @@ __device__ __forceinline__ void logits_finish(const LogitsArgs& s, LogitsTable t
     if (s.logp) {
       const int t = s.targets[row];
       float v = 0.f;
-      if (t >= 0 && t < s.n_v) v = none ? -INFINITY : kLn2 * (a.of(logits_at<E>(s, table, row, t), s.c) - total);
+      if (t >= 0 && t < s.n_v) v = none ? -INFINITY : kLn2 * (a.of(x_target, s.c) - total);
       s.logp[row] = v;
     }
   }
@@ -351,14 +374,15 @@ __device__ __forceinline__ void logits_finish(const LogitsArgs& s, LogitsTable t
 
 // A row, or one of its splits, to a workgroup.
 template <class E, bool ENTROPY, bool TOP, bool TINY>
-__global__ __launch_bounds__(kLogitsThreads) void logits_fwd_kernel(LogitsArgs s) {
-  constexpr int B = logits_batch<E>();
+__global__ __launch_bounds__(kLogitsThreads, 8) void logits_fwd_kernel(LogitsArgs s) {
+  constexpr int B = logits_batch<E>(), H = TOP ? B / 2 : B;  // vectors at a time: beside a list there are fewer registers
   __shared__ float4 sums[kLogitsWaves];
   __shared__ uint64_t buffers[TOP ? kLogitsWaves * TopList::kRoom : 1];
   const LogitsTable table = LOGITS_TABLE(s);
   const int64_t row = blockIdx.x / (uint32_t)s.splits;
   const int split = blockIdx.x % (uint32_t)s.splits, tid = threadIdx.x, wave = tid >> 6;
   uint64_t* const buffer = buffers + (TOP ? wave * TopList::kRoom : 0);
+  const float x_target = s.splits == 1 ? logits_target<E>(s, table, row) : 0.f;
   LogitsSums a;
   TopList list;
   bool first = true;
@@ -366,26 +390,29 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_fwd_kernel(LogitsArgs s
     const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
     typedef LogitsVector<E, TINY> Vector;
     Vector v[B];
-    float f[B * 8], most[B], all = -INFINITY;
     const int v0 = base + tid, end = base + B * kLogitsThreads;
 #pragma unroll
     for (int b = 0; b < B; ++b) v[b].load(x, p.n, v0 + b * kLogitsThreads);
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-      v[b].values(f + 8 * b, p.n, v0 + b * kLogitsThreads, to, end > to, p.n % 8 != 0 && end >= p.vecs);
-      most[b] = max8(f + 8 * b);
-      all = fmaxf(all, most[b]);
-    }
-    logits_add<B * 8, ENTROPY>(a, f, all, s.c);
-    if constexpr (TOP) {
-      if (first) list.start(all, s.n_top);
-      first = false;
+    for (int half = 0; half < B / H; ++half) {
+      float f[H * 8], most[H], all = -INFINITY;
 #pragma unroll
-      for (int b = 0; b < B; ++b)
-        if (__any(order_of(most[b]) > list.floor)) {
-          const int i = v0 + b * kLogitsThreads;
-          list.take(buffer, f + 8 * b, p.first + Vector::place(p.n, i), i < to ? Vector::first_of(p.n, i) : 8, p.n, s.n_top);
-        }
+      for (int b = 0; b < H; ++b) {
+        v[half * H + b].values(f + 8 * b, p.n, v0 + (half * H + b) * kLogitsThreads, to, end > to, p.n % 8 != 0 && end >= p.vecs);
+        most[b] = max8(f + 8 * b);
+        all = fmaxf(all, most[b]);
+      }
+      logits_add<H * 8, ENTROPY>(a, f, all, s.c);
+      if constexpr (TOP) {
+        if (first) list.start(all, s.n_top);
+        first = false;
+#pragma unroll
+        for (int b = 0; b < H; ++b)
+          if (__any(list.passes(most[b]))) {
+            const int i = v0 + (half * H + b) * kLogitsThreads;
+            list.take(buffer, f + 8 * b, most[b], p.first + Vector::place(p.n, i), i < to ? Vector::first_of(p.n, i) : 8, p.n, s.n_top);
+          }
+      }
     }
   });
   if constexpr (TOP) {
@@ -398,7 +425,7 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_fwd_kernel(LogitsArgs s
       for (int i = 1; i < kLogitsWaves; ++i) list.best = merged_lanes(list.best, buffers[i * TopList::kRoom + tid]);
   }
   if (s.splits == 1) {
-    logits_finish<E>(s, table, row, a, list.best);
+    logits_finish(s, row, a, list.best, x_target);
     return;
   }
   if (tid == 0) s.parts[blockIdx.x] = make_float4(a.m, a.mc, a.s, a.w);
@@ -406,15 +433,16 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_fwd_kernel(LogitsArgs s
 }
 
 // The splits of a row meet, in a fixed order.
+template <int THREADS>
 __device__ __forceinline__ LogitsSums logits_joined(const LogitsArgs& s, int64_t row, float4* shared) {
   LogitsSums a;
-  for (int i = threadIdx.x; i < s.splits; i += kLogitsThreads) {
+  for (int i = threadIdx.x; i < s.splits; i += THREADS) {
     const float4 v = s.parts[row * s.splits + i];
     LogitsSums one;
     one.m = v.x, one.mc = v.y, one.s = v.z, one.w = v.w;
     a.join(one, s.c);
   }
-  a.join_waves<kLogitsWaves>(shared, s.c);
+  a.join_waves<THREADS / 64>(shared, s.c);
   return a;
 }
 
@@ -425,6 +453,8 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_join_kernel(LogitsArgs 
   const LogitsTable table = LOGITS_TABLE(s);
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const float x_target = logits_target<E>(s, table, row);
+  const LogitsSums a = logits_joined<kLogitsThreads>(s, row, sums);
   uint64_t best = 0;
   if (s.n_top > 0) {
     for (int i = wave; i < s.splits; i += kLogitsWaves) {
@@ -432,11 +462,11 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_join_kernel(LogitsArgs 
       best = merged_lanes(best, more);
     }
     lists[tid] = best;
+    __syncthreads();
+    if (wave == 0)
+      for (int i = 1; i < kLogitsWaves; ++i) best = merged_lanes(best, lists[i * 64 + lane]);
   }
-  const LogitsSums a = logits_joined(s, row, sums);
-  if (s.n_top > 0 && wave == 0)
-    for (int i = 1; i < kLogitsWaves; ++i) best = merged_lanes(best, lists[i * 64 + lane]);
-  logits_finish<E>(s, table, row, a, best);
+  logits_finish(s, row, a, best, x_target);
 }
 
 // ---- adjoint --------------------------------------------------------------
@@ -499,8 +529,9 @@ struct Stored {
   int32_t id[kStoredMost];
   float p[kStoredMost];  // the teacher's probabilities
   float x[kStoredMost];  // the student's logits
-  float red[kLogitsWaves];
+  float red[16];
 };
+template <int WAVES>
 __device__ __forceinline__ float group_max(float v, float* red) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
@@ -509,9 +540,10 @@ __device__ __forceinline__ float group_max(float v, float* red) {
   __syncthreads();
   v = red[0];
 #pragma unroll
-  for (int i = 1; i < kLogitsWaves; ++i) v = fmaxf(v, red[i]);
+  for (int i = 1; i < WAVES; ++i) v = fmaxf(v, red[i]);
   return v;
 }
+template <int WAVES>
 __device__ __forceinline__ float group_sum(float v, float* red) {
   v = wave_sum(v);
   __syncthreads();
@@ -519,14 +551,15 @@ __device__ __forceinline__ float group_sum(float v, float* red) {
   __syncthreads();
   v = red[0];
 #pragma unroll
-  for (int i = 1; i < kLogitsWaves; ++i) v += red[i];
+  for (int i = 1; i < WAVES; ++i) v += red[i];
   return v;
 }
 // The teacher's probabilities of a row: false if it has stored nothing.  total: log2 of their sum relative to `most`.
+template <int THREADS>
 __device__ __forceinline__ bool stored_load(const LogitsArgs& s, int64_t row, Stored& t, float& mc, float& total) {
   float most = -INFINITY;
   bool odd = false;
-  for (int k = threadIdx.x; k < s.n_top; k += kLogitsThreads) {
+  for (int k = threadIdx.x; k < s.n_top; k += THREADS) {
     const int id = s.stored_ids[row * s.n_top + k];
     const bool in = id >= 0 && id < s.n_v;
     const float v = in ? s.stored[row * s.n_top + k] : -INFINITY;
@@ -535,121 +568,33 @@ __device__ __forceinline__ bool stored_load(const LogitsArgs& s, int64_t row, St
     most = fmaxf(most, v);
     odd = odd || v != v;
   }
-  most = group_max(odd ? INFINITY : most, t.red);  // (a NaN ends as NaN: inf - inf)
+  most = group_max<THREADS / 64>(odd ? INFINITY : most, t.red);  // (a NaN ends as NaN: inf - inf)
   if (most == -INFINITY) return false;
   mc = most * s.c;
   float sum = 0.f;
-  for (int k = threadIdx.x; k < s.n_top; k += kLogitsThreads) sum += __builtin_amdgcn_exp2f(fmaf(t.p[k], s.c, -mc));
-  sum = group_sum(sum, t.red);
+  for (int k = threadIdx.x; k < s.n_top; k += THREADS) sum += __builtin_amdgcn_exp2f(fmaf(t.p[k], s.c, -mc));
+  sum = group_sum<THREADS / 64>(sum, t.red);
   total = __builtin_amdgcn_logf(sum);
   return true;
 }
 // The row's loss, and the teacher's logits in t.p become probabilities.  a, stotal: the student's.
+template <int THREADS>
 __device__ __forceinline__ float stored_loss(const LogitsArgs& s, Stored& t, float mc, float total, const LogitsSums& a, float stotal) {
   float loss = 0.f;
   const float inv = __builtin_amdgcn_exp2f(-total);
-  for (int k = threadIdx.x; k < s.n_top; k += kLogitsThreads) {
+  for (int k = threadIdx.x; k < s.n_top; k += THREADS) {
     const float d = fmaf(t.p[k], s.c, -mc), p = __builtin_amdgcn_exp2f(d) * inv;
     if (!(p == 0.f)) loss = fmaf(p, (d - total) - (a.of(t.x[k], s.c) - stotal), loss);
     t.p[k] = p;
   }
-  return kLn2 * group_sum(loss, t.red);
+  return kLn2 * group_sum<THREADS / 64>(loss, t.red);
 }
 
-// FIRST: the sums of a split and the student's logits at the teacher's places in it.  Else the loss and the gradient, of rows that
-// are one workgroup's (splits == 1, which reads the row for its sums too) or of a split.
-template <class E, bool FIRST, bool TINY>
-__global__ __launch_bounds__(kLogitsThreads) void distill_kernel(LogitsArgs s) {
-  constexpr int B = logits_batch<E>();
-  __shared__ float4 sums[kLogitsWaves];
-  __shared__ Stored t;
-  const LogitsTable table = LOGITS_TABLE(s);
-  const int64_t row = blockIdx.x / (uint32_t)s.splits;
-  const int split = blockIdx.x % (uint32_t)s.splits, tid = threadIdx.x;
-  float weight = s.weight ? s.weight[row] : 1.f, mc = 0.f, total = 0.f;
-  LogitsSums a;
-  bool any = false;
-  if (FIRST) {
-    const int lo = split * s.per, hi = lo + s.per;
-    for (int k = tid; k < s.n_top; k += kLogitsThreads) {
-      const int id = s.stored_ids[row * s.n_top + k];
-      if (id < 0 || id >= s.n_v) continue;
-      const LogitsPart p = logits_part(s, logits_worker_of(s, id));
-      const int v = p.vec0 + (id - p.first) / 8;
-      if (v >= lo && v < hi) s.stored_x[row * s.n_top + k] = logits_at<E>(s, table, row, id);
-    }
-  } else {
-    any = stored_load(s, row, t, mc, total);
-    if (!any) weight = 0.f;
-    if (any)
-      for (int k = tid; k < s.n_top; k += kLogitsThreads)
-        t.x[k] = t.id[k] < 0 ? 0.f : s.splits > 1 ? s.stored_x[row * s.n_top + k] : logits_at<E>(s, table, row, t.id[k]);
-  }
-  const bool sum_here = FIRST || s.splits == 1;
-  if (sum_here && (FIRST || any)) {
-    logits_each<B, kLogitsThreads>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
-      const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
-      LogitsVector<E, TINY> v[B];
-      float f[B * 8], all = -INFINITY;
-      const int v0 = base + tid, end = base + B * kLogitsThreads;
-#pragma unroll
-      for (int b = 0; b < B; ++b) v[b].load(x, p.n, v0 + b * kLogitsThreads);
-#pragma unroll
-      for (int b = 0; b < B; ++b) {
-        v[b].values(f + 8 * b, p.n, v0 + b * kLogitsThreads, to, end > to, p.n % 8 != 0 && end >= p.vecs);
-        all = fmaxf(all, max8(f + 8 * b));
-      }
-      logits_add<B * 8, false>(a, f, all, s.c);
-    });
-    a.join_waves<kLogitsWaves>(sums, s.c);
-  }
-  if (FIRST) {
-    if (tid == 0) s.parts[blockIdx.x] = make_float4(a.m, a.mc, a.s, 0.f);
-    return;
-  }
-  if (any && !sum_here) a = logits_joined(s, row, sums);
-  const float stotal = __builtin_amdgcn_logf(a.s);
-  if (any && a.none()) {  // no entry that the student could answer with: an infinite loss, and nothing to follow
-    if (tid == 0 && split == 0 && s.loss) s.loss[row] = INFINITY;
-    weight = 0.f;
-  } else if (any) {
-    const float loss = stored_loss(s, t, mc, total, a, stotal);
-    if (tid == 0 && split == 0 && s.loss) s.loss[row] = loss;
-  } else if (tid == 0 && split == 0 && s.loss) {
-    s.loss[row] = 0.f;
-  }
-  if (!table[0].dx) return;
-  const float scale = weight * s.inv_t, off = a.mc + stotal;
-  const bool far = a.far();
-  const bool nothing = weight == 0.f;  // such rows are not read
-  __syncthreads();
-  logits_each<B, kLogitsThreads>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
-    const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
-    E* const dx = (E*)table[j].dx + row * p.n;
-    typedef LogitsVector<E, TINY> Vector;
-    Vector v[B];
-    const bool edge = base + B * kLogitsThreads >= to;  // (a last vector, or none)
-    if (!nothing) {
-#pragma unroll
-      for (int b = 0; b < B; ++b) v[b].load(x, p.n, base + b * kLogitsThreads + tid);
-    }
-#pragma unroll
-    for (int b = 0; b < B; ++b) {
-      float f[8] = {};
-      const int i0 = base + b * kLogitsThreads + tid;
-      const int at = Vector::place(p.n, i0), from = i0 < to ? Vector::first_of(p.n, i0) : 8;
-      if (!nothing) {
-        v[b].values(f, p.n, i0, to, false, false);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = scale * __builtin_amdgcn_exp2f(far ? a.of(f[i], s.c) - stotal : fmaf(f[i], s.c, -off));
-      }
-      logits_store(dx, f, at, from, p.n, edge);
-    }
-  });
-  if (nothing) return;
-  __syncthreads();  // the teacher's places are written once more, behind the stores above
-  const int lo = split * s.per, hi = lo + s.per;
-  for (int k = tid; k < s.n_top; k += kLogitsThreads) {
+// The teacher's places among a split's vectors lo .. hi - 1 are written once more.  off: log2 of the sum, and its reference.
+template <class E, int THREADS>
+__device__ __forceinline__ void stored_places(const LogitsArgs& s, LogitsTable table, int64_t row, const Stored& t, const LogitsSums& a, float stotal, float scale,
+                                              int lo, int hi) {
+  for (int k = threadIdx.x; k < s.n_top; k += THREADS) {
     const int id = t.id[k];
     if (id < 0) continue;
     const int j = logits_worker_of(s, id);
@@ -667,6 +612,178 @@ __global__ __launch_bounds__(kLogitsThreads) void distill_kernel(LogitsArgs s) {
   }
 }
 
+// FIRST: the sums of a split and the student's logits at the teacher's places in it.  Else the loss and the gradient, of rows that
+// are one workgroup's (splits == 1, which reads the row for its sums too) or of a split.
+template <class E, bool FIRST, bool TINY, int THREADS>
+__global__ __launch_bounds__(THREADS) void distill_kernel(LogitsArgs s) {
+  constexpr int B = logits_batch<E>();
+  __shared__ float4 sums[THREADS / 64];
+  __shared__ Stored t;
+  const LogitsTable table = LOGITS_TABLE(s);
+  const int64_t row = blockIdx.x / (uint32_t)s.splits;
+  const int split = blockIdx.x % (uint32_t)s.splits, tid = threadIdx.x;
+  float weight = s.weight ? s.weight[row] : 1.f, mc = 0.f, total = 0.f;
+  LogitsSums a;
+  bool any = false;
+  if (FIRST) {
+    const int lo = split * s.per, hi = lo + s.per;
+    for (int k = tid; k < s.n_top; k += THREADS) {
+      const int id = s.stored_ids[row * s.n_top + k];
+      if (id < 0 || id >= s.n_v) continue;
+      const LogitsPart p = logits_part(s, logits_worker_of(s, id));
+      const int v = p.vec0 + (id - p.first) / 8;
+      if (v >= lo && v < hi) s.stored_x[row * s.n_top + k] = logits_at<E>(s, table, row, id);
+    }
+  } else {
+    any = stored_load<THREADS>(s, row, t, mc, total);
+    if (!any) weight = 0.f;
+    if (any)
+      for (int k = tid; k < s.n_top; k += THREADS)
+        t.x[k] = t.id[k] < 0 ? 0.f : s.splits > 1 ? s.stored_x[row * s.n_top + k] : logits_at<E>(s, table, row, t.id[k]);
+  }
+  const bool sum_here = FIRST || s.splits == 1;
+  if (sum_here && (FIRST || any)) {
+    logits_each<B, THREADS>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
+      const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
+      LogitsVector<E, TINY> v[B];
+      float f[B * 8], all = -INFINITY;
+      const int v0 = base + tid, end = base + B * THREADS;
+#pragma unroll
+      for (int b = 0; b < B; ++b) v[b].load(x, p.n, v0 + b * THREADS);
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
+        v[b].values(f + 8 * b, p.n, v0 + b * THREADS, to, end > to, p.n % 8 != 0 && end >= p.vecs);
+        all = fmaxf(all, max8(f + 8 * b));
+      }
+      logits_add<B * 8, false>(a, f, all, s.c);
+    });
+    a.join_waves<THREADS / 64>(sums, s.c);
+  }
+  if (FIRST) {
+    if (tid == 0) s.parts[blockIdx.x] = make_float4(a.m, a.mc, a.s, 0.f);
+    return;
+  }
+  if (any && !sum_here) a = logits_joined<THREADS>(s, row, sums);
+  const float stotal = __builtin_amdgcn_logf(a.s);
+  if (any && a.none()) {  // no entry that the student could answer with: an infinite loss, and nothing to follow
+    if (tid == 0 && split == 0 && s.loss) s.loss[row] = INFINITY;
+    weight = 0.f;
+  } else if (any) {
+    const float loss = stored_loss<THREADS>(s, t, mc, total, a, stotal);
+    if (tid == 0 && split == 0 && s.loss) s.loss[row] = loss;
+  } else if (tid == 0 && split == 0 && s.loss) {
+    s.loss[row] = 0.f;
+  }
+  if (!table[0].dx) return;
+  const float scale = weight * s.inv_t, off = a.mc + stotal;
+  const bool far = a.far();
+  const bool nothing = weight == 0.f;  // such rows are not read
+  __syncthreads();
+  logits_each<B, THREADS>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
+    const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
+    E* const dx = (E*)table[j].dx + row * p.n;
+    typedef LogitsVector<E, TINY> Vector;
+    Vector v[B];
+    const bool edge = base + B * THREADS >= to;  // (a last vector, or none)
+    if (!nothing) {
+#pragma unroll
+      for (int b = 0; b < B; ++b) v[b].load(x, p.n, base + b * THREADS + tid);
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      float f[8] = {};
+      const int i0 = base + b * THREADS + tid;
+      const int at = Vector::place(p.n, i0), from = i0 < to ? Vector::first_of(p.n, i0) : 8;
+      if (!nothing) {
+        v[b].values(f, p.n, i0, to, false, false);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = scale * __builtin_amdgcn_exp2f(far ? a.of(f[i], s.c) - stotal : fmaf(f[i], s.c, -off));
+      }
+      logits_store(dx, f, at, from, p.n, edge);
+    }
+  });
+  if (nothing) return;
+  __syncthreads();  // (behind the stores above)
+  stored_places<E, THREADS>(s, table, row, t, a, stotal, scale, split * s.per, split * s.per + s.per);
+}
+
+// Rows that fit a workgroup's registers (up to 65536 entries of bf16, 32768 of fp32) are read once.  Slot by slot: a slot has a vector for each thread, of one
+// worker.  Longer ones would leave a compute unit one workgroup, which reads, computes and writes in turn: 4096 x 131072, bf16, 648 us that way, 640 us read
+// twice.
+template <class E>
+constexpr int distill_slots() { return sizeof(E) == 2 ? 16 : 8; }
+template <class E, int THREADS>
+__global__ __launch_bounds__(THREADS) void distill_kept_kernel(LogitsArgs s) {
+  constexpr int S = distill_slots<E>();
+  typedef LogitsVector<E, false> Vector;
+  __shared__ float4 sums[THREADS / 64];
+  __shared__ Stored t;
+  const LogitsTable table = LOGITS_TABLE(s);
+  const int64_t row = blockIdx.x;
+  const int tid = threadIdx.x;
+  // f(slot, worker, part, first vector)
+  auto slots = [&](auto f) {
+    int j = 0, base = 0;
+    LogitsPart p = logits_part(s, 0);
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      if (j < s.P) {
+        f(i, j, p, base);
+        base += THREADS;
+        if (base >= p.vecs) {
+          ++j;
+          base = 0;
+          p = logits_part(s, min(j, s.P - 1));
+        }
+      }
+    }
+  };
+  Vector v[S];
+  slots([&](int i, int j, const LogitsPart& p, int base) { v[i].load(logits_row(table[j].x, row, p.n, sizeof(E)), p.n, base + tid); });
+  float weight = s.weight ? s.weight[row] : 1.f, mc = 0.f, total = 0.f;
+  const bool any = stored_load<THREADS>(s, row, t, mc, total);
+  if (any) {
+    for (int k = tid; k < s.n_top; k += THREADS) t.x[k] = t.id[k] < 0 ? 0.f : logits_at<E>(s, table, row, t.id[k]);
+  } else {
+    weight = 0.f;
+  }
+  LogitsSums a;
+  if (any) {
+    slots([&](int i, int j, const LogitsPart& p, int base) {
+      float f[8];
+      v[i].values(f, p.n, base + tid, p.vecs, base + THREADS > p.vecs, p.n % 8 != 0 && base + THREADS >= p.vecs);
+      logits_add<8, false>(a, f, max8(f), s.c);
+    });
+    a.template join_waves<THREADS / 64>(sums, s.c);
+  }
+  const float stotal = __builtin_amdgcn_logf(a.s);
+  float loss = 0.f;
+  if (any && a.none()) {  // no entry that the student could answer with: an infinite loss, and nothing to follow
+    loss = INFINITY;
+    weight = 0.f;
+  } else if (any) {
+    loss = stored_loss<THREADS>(s, t, mc, total, a, stotal);
+  }
+  if (tid == 0 && s.loss) s.loss[row] = loss;
+  const float scale = weight * s.inv_t, off = a.mc + stotal;
+  const bool nothing = weight == 0.f, far = a.far();
+  __syncthreads();  // (places of the row are read above, of dx on x)
+  slots([&](int i, int j, const LogitsPart& p, int base) {
+    E* const dx = (E*)table[j].dx + row * p.n;
+    float f[8] = {};
+    if (!nothing) {
+      v[i].values(f, p.n, base + tid, p.vecs, false, false);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) f[k] = scale * __builtin_amdgcn_exp2f(far ? a.of(f[k], s.c) - stotal : fmaf(f[k], s.c, -off));
+    }
+    const int at = Vector::place(p.n, base + tid), from = base + tid < p.vecs ? Vector::first_of(p.n, base + tid) : 8;
+    logits_store(dx, f, at, from, p.n, base + THREADS >= p.vecs);
+  });
+  if (nothing) return;
+  __syncthreads();  // (behind the stores above)
+  stored_places<E, THREADS>(s, table, row, t, a, stotal, scale, 0, INT_MAX);
+}
+
 }  // namespace distdl
 
 struct distdl_logits_plan {
@@ -680,9 +797,9 @@ struct distdl_logits_plan {
 
 namespace distdl {
 
-// Workgroups of a row.  A row is one workgroup's where rows fill the card; else it is cut, down to two batches of a workgroup.
+// Workgroups of a row.  A row is one workgroup's where rows fill the card; else it is cut, down to half a batch of a workgroup.
 static int logits_splits(int64_t rows, int vecs, int batch) {
-  const int64_t wanted = (1024 + rows - 1) / rows, most = std::max(1, vecs / (2 * batch * kLogitsThreads));
+  const int64_t wanted = (1024 + rows - 1) / rows, most = std::max(1, vecs / (batch * kLogitsThreads / 2));
   return rows >= 512 ? 1 : (int)std::min(wanted, most);
 }
 
@@ -751,11 +868,35 @@ static void launch_logits_bwd(const LogitsArgs& s, hipStream_t st) {
   hipLaunchKernelGGL((logits_bwd_kernel<E, ENTROPY, TINY>), dim3((unsigned)(s.rows * s.splits)), dim3(kLogitsThreads), 0, st, s);
 }
 
+// Threads of a workgroup that keeps a row in its registers; 0: none does.
+static int distill_threads(const LogitsArgs& s, int slots) {
+  if (s.part < 8) return 0;
+  for (int threads : {256, 512}) {
+    const int64_t wide = (s.vec_wide + threads - 1) / threads, rest = (s.vec_rest + threads - 1) / threads;
+    if (s.extra * wide + (s.P - s.extra) * rest <= slots) return threads;
+  }
+  return 0;
+}
+
 template <class E, bool TINY>
-static void launch_distill(const LogitsArgs& s, hipStream_t st) {
+static void launch_distill(const LogitsArgs& s, bool gradient, hipStream_t st) {
   const dim3 grid((unsigned)(s.rows * s.splits)), block(kLogitsThreads);
-  if (s.splits > 1) hipLaunchKernelGGL((distill_kernel<E, true, TINY>), grid, block, 0, st, s);
-  hipLaunchKernelGGL((distill_kernel<E, false, TINY>), grid, block, 0, st, s);
+  const int kept = s.splits == 1 && gradient ? distill_threads(s, distill_slots<E>()) : 0;
+  if (kept == 256) hipLaunchKernelGGL((distill_kept_kernel<E, 256>), grid, dim3(256), 0, st, s);
+  else if (kept == 512) hipLaunchKernelGGL((distill_kept_kernel<E, 512>), grid, dim3(512), 0, st, s);
+  if (kept) return;
+  // A row that is read twice should still be in the last cache (256 MB) then: so many threads that the rows under way are half of that.
+  const size_t bytes = (size_t)s.n_v * sizeof(E);
+  if (s.splits > 1) {
+    hipLaunchKernelGGL((distill_kernel<E, true, TINY, kLogitsThreads>), grid, block, 0, st, s);
+    hipLaunchKernelGGL((distill_kernel<E, false, TINY, kLogitsThreads>), grid, block, 0, st, s);
+  } else if (bytes <= 64 << 10 || TINY) {
+    hipLaunchKernelGGL((distill_kernel<E, false, TINY, kLogitsThreads>), grid, block, 0, st, s);
+  } else if (bytes <= 128 << 10) {
+    hipLaunchKernelGGL((distill_kernel<E, false, false, 512>), grid, dim3(512), 0, st, s);
+  } else {
+    hipLaunchKernelGGL((distill_kernel<E, false, false, 1024>), grid, dim3(1024), 0, st, s);
+  }
 }
 
 // f(element, whether there is an option, whether a worker has fewer than eight entries)
@@ -895,7 +1036,7 @@ int distdl_distill_fwd_bwd(distdl_logits_plan* p, const void* const x_dev[], con
     }
     {
       ProfScope prof("distill", st_);
-      logits_kind(p->dtype, false, s.part < 8, [&](auto e, auto, auto tiny) { launch_distill<decltype(e), decltype(tiny)::value>(s, st_); });
+      logits_kind(p->dtype, false, s.part < 8, [&](auto e, auto, auto tiny) { launch_distill<decltype(e), decltype(tiny)::value>(s, dx_dev != nullptr, st_); });
     }
     DISTDL_HIP_TRY(hipGetLastError());
     return DISTDL_OK;
