@@ -118,6 +118,7 @@ struct LogitsVector {
   // (both uniform).
   __device__ __forceinline__ void values(float* f, int n, int v, int end, bool edge, bool ragged) {
     if (edge) {
+      asm volatile("");  // (a branch: as selections they would cost every vector an instruction for each entry)
 #pragma unroll
       for (int i = 0; i < (int)sizeof(E) / 2; ++i)
 #pragma unroll
@@ -134,6 +135,7 @@ struct LogitsVector {
       }
     }
     if (ragged) {
+      asm volatile("");
       const int from = v < end ? first_of(n, v) : 8;
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[i] = i >= from && i < n ? f[i] : -INFINITY;
@@ -289,6 +291,20 @@ __device__ __forceinline__ uint64_t merged_lanes(uint64_t a, uint64_t b) {
   return bitonic<64>(a > b ? a : b, true);
 }
 
+// `best` and `waiting` keys of a buffer in LDS.  (Out of line: it is rarely called, and the registers are the streaming loop's.)
+typedef __attribute__((address_space(3))) uint64_t* TopBuffer;
+__device__ __attribute__((noinline)) uint64_t top_flushed(uint64_t best, TopBuffer buffer, int waiting) {
+  const int lane = threadIdx.x & 63;
+  while (waiting > 0) {
+    const int n = min(waiting, 64), from = waiting - n;
+    best = merged_lanes(best, sorted_lanes(lane < n ? (uint64_t)buffer[from + lane] : (uint64_t)0));
+    waiting = from;
+  }
+  __builtin_amdgcn_wave_barrier();
+  return best;
+}
+__device__ __attribute__((noinline)) int32_t top_nth(int32_t order, int n) { return __builtin_amdgcn_readlane(sorted_lanes(order), n - 1); }
+
 // A wave's 64 best entries, descending over the lanes, and a buffer of those that wait.  Values at or below `floor`, the n-th best so far, can
 // not be among the n: a wave meets entries in the order of their places, so of equal values the first stay.  (A NaN, at first, lets all pass.)
 struct TopList {
@@ -304,18 +320,13 @@ struct TopList {
   }
   // From the largest of each lane's first entries: the n-th of them is no better than the n-th of all, and may be it.
   __device__ __forceinline__ void start(float most, int n_top) {
-    const int32_t nth = __builtin_amdgcn_readlane(sorted_lanes(order_of(most)), n_top - 1);
+    const int32_t nth = top_nth(order_of(most), n_top);
     const int32_t below = nth == 0 ? order_of(-FLT_MIN) : nth - 1;  // (-0, which comes next, is no less than 0)
     if (nth > order_of(-INFINITY)) floor = __uint_as_float((uint32_t)(below ^ ((below >> 31) & 0x7fffffff)));
   }
   __device__ __forceinline__ void flush(uint64_t* buffer, int n_top) {
-    const int lane = threadIdx.x & 63;
-    while (waiting > 0) {
-      const int n = min(waiting, 64), from = waiting - n;
-      best = merged_lanes(best, sorted_lanes(lane < n ? buffer[from + lane] : 0));
-      waiting = from;
-    }
-    __builtin_amdgcn_wave_barrier();
+    best = top_flushed(best, (TopBuffer)buffer, waiting);
+    waiting = 0;
     set_floor(n_top);
   }
   __device__ __forceinline__ void push(uint64_t* buffer, bool in, float v, int id) {
@@ -375,7 +386,7 @@ __device__ __forceinline__ void logits_finish(const LogitsArgs& s, int64_t row, 
 // A row, or one of its splits, to a workgroup.
 template <class E, bool ENTROPY, bool TOP, bool TINY>
 __global__ __launch_bounds__(kLogitsThreads, 8) void logits_fwd_kernel(LogitsArgs s) {
-  constexpr int B = logits_batch<E>(), H = TOP ? B / 2 : B;  // vectors at a time: beside a list there are fewer registers
+  constexpr int B = logits_batch<E>() / (TOP ? 2 : 1);
   __shared__ float4 sums[kLogitsWaves];
   __shared__ uint64_t buffers[TOP ? kLogitsWaves * TopList::kRoom : 1];
   const LogitsTable table = LOGITS_TABLE(s);
@@ -386,35 +397,73 @@ __global__ __launch_bounds__(kLogitsThreads, 8) void logits_fwd_kernel(LogitsArg
   LogitsSums a;
   TopList list;
   bool first = true;
-  logits_each<B, kLogitsThreads>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
-    const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
-    typedef LogitsVector<E, TINY> Vector;
-    Vector v[B];
-    const int v0 = base + tid, end = base + B * kLogitsThreads;
+  typedef LogitsVector<E, TINY> Vector;
+  if constexpr (TOP) {
+    // The next vectors are under way while these are looked through; one place in the code for both, and for what is rarely done.
+    const int lo = split * s.per, hi = min(lo + s.per, s.extra * s.vec_wide + (s.P - s.extra) * s.vec_rest);
+    for (int j = 0; j < s.P; ++j) {
+      const LogitsPart p = logits_part(s, j);
+      const int from = max(0, lo - p.vec0), to = min(p.vecs, hi - p.vec0);
+      if (from >= to) continue;
+      const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
+      Vector next[B];
 #pragma unroll
-    for (int b = 0; b < B; ++b) v[b].load(x, p.n, v0 + b * kLogitsThreads);
+      for (int b = 0; b < B; ++b) next[b].load(x, p.n, from + tid + b * kLogitsThreads);
+      for (int base = from; base < to; base += B * kLogitsThreads) {
+        const int v0 = base + tid, end = base + B * kLogitsThreads;
+        Vector v[B];
 #pragma unroll
-    for (int half = 0; half < B / H; ++half) {
-      float f[H * 8], most[H], all = -INFINITY;
+        for (int b = 0; b < B; ++b) {
+          v[b] = next[b];
+          next[b].load(x, p.n, v0 + (b + B) * kLogitsThreads);
+        }
+        float f[B * 8], most[B], all = -INFINITY;
 #pragma unroll
-      for (int b = 0; b < H; ++b) {
-        v[half * H + b].values(f + 8 * b, p.n, v0 + (half * H + b) * kLogitsThreads, to, end > to, p.n % 8 != 0 && end >= p.vecs);
-        most[b] = max8(f + 8 * b);
-        all = fmaxf(all, most[b]);
-      }
-      logits_add<H * 8, ENTROPY>(a, f, all, s.c);
-      if constexpr (TOP) {
+        for (int b = 0; b < B; ++b) {
+          v[b].values(f + 8 * b, p.n, v0 + b * kLogitsThreads, to, end > to, p.n % 8 != 0 && end >= p.vecs);
+          most[b] = max8(f + 8 * b);
+          all = fmaxf(all, most[b]);
+        }
+        logits_add<B * 8, ENTROPY>(a, f, all, s.c);
         if (first) list.start(all, s.n_top);
         first = false;
+        bool any = false;
 #pragma unroll
-        for (int b = 0; b < H; ++b)
-          if (__any(list.passes(most[b]))) {
-            const int i = v0 + (half * H + b) * kLogitsThreads;
-            list.take(buffer, f + 8 * b, most[b], p.first + Vector::place(p.n, i), i < to ? Vector::first_of(p.n, i) : 8, p.n, s.n_top);
+        for (int b = 0; b < B; ++b) any = any || list.passes(most[b]);
+        if (__any(any)) {
+#pragma unroll 1
+          for (int b = 0; b < B; ++b) {
+            float g[8], of = most[0];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[i] = f[i];
+#pragma unroll
+            for (int c = 1; c < B; ++c) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) g[i] = b == c ? f[8 * c + i] : g[i];
+              of = b == c ? most[c] : of;
+            }
+            const int i = v0 + b * kLogitsThreads;
+            list.take(buffer, g, of, p.first + Vector::place(p.n, i), i < to ? Vector::first_of(p.n, i) : 8, p.n, s.n_top);
           }
+        }
       }
     }
-  });
+  } else {
+    logits_each<B, kLogitsThreads>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
+      const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
+      Vector v[B];
+      float f[B * 8], all = -INFINITY;
+      const int v0 = base + tid, end = base + B * kLogitsThreads;
+#pragma unroll
+      for (int b = 0; b < B; ++b) v[b].load(x, p.n, v0 + b * kLogitsThreads);
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
+        v[b].values(f + 8 * b, p.n, v0 + b * kLogitsThreads, to, end > to, p.n % 8 != 0 && end >= p.vecs);
+        all = fmaxf(all, max8(f + 8 * b));
+      }
+      logits_add<B * 8, ENTROPY>(a, f, all, s.c);
+    });
+  }
   if constexpr (TOP) {
     list.flush(buffer, s.n_top);
     buffer[tid & 63] = list.best;
