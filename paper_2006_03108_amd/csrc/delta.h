@@ -50,7 +50,7 @@ struct DeltaArgs {
   uint16_t *tf, *pf, *ttf, *ptf;      // fragments of T and P, and of their transposes
   float* steps;                       // of each step: kStepNumbers of them, [C] each
   float *states, *dstates;            // [DK][dvp] at a chunk's start; the gradient at its end
-  float *u, *x, *dr;                  // [C][dvp]
+  float *u, *dr;                      // [C][dvp]
 };
 
 static_assert(offsetof(DeltaArgs, w) == 0, "the kernels' first argument starts with the workers");
@@ -209,7 +209,7 @@ struct DeltaSizes {
   static constexpr int64_t kKeyPiece = (int64_t)C * DK, kStepPiece = (int64_t)C * C;
 };
 constexpr int kInner = 3;  // pieces of T and P
-// exp(G), exp(G_C - G), beta, and the two parts of G
+// exp(G), exp(G_C - G), beta, and the two parts of G / log 2
 constexpr int kSince = 0, kUntil = 1, kBeta = 2, kWhole = 3, kRest = 4, kStepNumbers = 5;
 
 }  // namespace distdl

@@ -9,7 +9,7 @@
 //   X = V - exp(G) (K S),  U = T (beta X),  O = scale exp(G) (Q S) + P U,  S' = exp(G_C) S + K^T (exp(G_C - G) U)
 // A, T and P need no state: one launch makes them for all chunks (delta_prepare_kernel).  What is left goes through time, and its columns
 // (of d_v) are independent: a workgroup has 16 or 32 columns of a head's state in its registers and goes through all chunks, from product
-// to product.  Differences of G are exact: sums in 64 bits, kept as a multiple of 1/64 and the rest.
+// to product.  Differences of G are exact: sums in 64 bits and in units of log 2, kept as a multiple of 1/64 and the rest.
 #include <algorithm>
 #include <cmath>
 
@@ -22,7 +22,11 @@ namespace distdl {
 // A factor of exp(-200) is 0 in 32 bits, and so is what it stands between.
 __device__ __forceinline__ float bounded(float g) { return g < -200.f ? -200.f : g; }
 
+// beta's gradient is dR U / beta, what beta multiplies being U / beta.  So a beta of 0 counts as 2^-100: what it adds to a state does not show.
+__device__ __forceinline__ float nonzero(float beta) { return fabsf(beta) < 0x1p-100f ? 0x1p-100f : beta; }
+
 // ---- a chunk's own matrices -----------------------------------------------
+// (The waves of these kernels meet over LDS alone, so their barriers leave global loads and stores under way: lds_barrier.)
 template <class E, int C, int DK>
 struct DeltaPrepareShared {
   static constexpr int kRow = DK + 8, kLine = C + 4;
@@ -62,7 +66,7 @@ __device__ __forceinline__ void delta_inverse(const float (*a)[LINE], float (*t)
     }
   }
   for (int d = 1; d < N; ++d) {
-    __syncthreads();
+    lds_barrier();
     const int i = wave + d, j = wave;
     if (i < N) {
       f32x4 sum = {};
@@ -82,7 +86,7 @@ __device__ __forceinline__ void delta_inverse(const float (*a)[LINE], float (*t)
       }
     }
   }
-  __syncthreads();
+  lds_barrier();
 }
 
 // The places along a fragment's sum that a lane has: element e of step ks.
@@ -121,8 +125,8 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
     const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h;
     const bool live = lane < at.live;
     const int64_t o = (step0 + lane) * s.n_h + h;
-    const float beta = live ? w->beta[o] : 0.f;
-    double sum = live && w->g ? (double)bounded(w->g[o]) : 0.0;
+    const float beta = live ? nonzero(w->beta[o]) : 0.f;
+    double sum = live && w->g ? (double)bounded(w->g[o]) * 1.4426950408889634 : 0.0;
 #pragma unroll
     for (int d = 1; d < C; d *= 2) {
       const double before = __shfl_up(sum, d, 64);
@@ -134,8 +138,8 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
     m.rest[wave][lane] = rest;
     m.beta[wave][lane] = beta;
     float* const out = s.steps + head * kStepNumbers * C + lane;
-    out[kSince * C] = expf((float)sum);
-    out[kUntil * C] = expf((float)(last - sum));
+    out[kSince * C] = __builtin_amdgcn_exp2f((float)sum);
+    out[kUntil * C] = __builtin_amdgcn_exp2f((float)(last - sum));
     out[kBeta * C] = beta;
     out[kWhole * C] = whole;
     out[kRest * C] = rest;
@@ -163,7 +167,7 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
       for (int k = 0; k < 3; ++k) *(u32x4*)&m.rows[what][k][t][col] = p.p[k];
     }
   }
-  __syncthreads();
+  lds_barrier();
 
   // their fragments
   const int64_t key = ((int64_t)b * s.chunks + c) * s.n_hk + hk, key_at = key * Z::kKeyPiece * NI;
@@ -212,10 +216,10 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
   for (int e = 0; e < s.each; ++e) {
     const int h = hk * s.each + e, slot = e % Shared::kHeads;
     const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h;
-    __syncthreads();
+    lds_barrier();
     if (e > 0 && slot == 0) {
       sum_up(e);
-      __syncthreads();
+      lds_barrier();
     }
     // A and P, zeros above the diagonal
 #pragma unroll
@@ -227,13 +231,13 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int i = at_tile.mt * 16 + 4 * g + r;
-        const float decay = i >= j ? expf((m.whole[slot][i] - whole) + (m.rest[slot][i] - rest)) : 0.f;
+        const float decay = i >= j ? __builtin_amdgcn_exp2f((m.whole[slot][i] - whole) + (m.rest[slot][i] - rest)) : 0.f;
         m.a[i][j] = i > j ? m.beta[slot][i] * decay * kk[x][r] : 0.f;
         m.p[i][j] = i >= j ? s.scale * decay * qk[x][r] : 0.f;
         if (at_tile.mt != at_tile.nt) m.p[at_tile.nt * 16 + 4 * g + r][at_tile.mt * 16 + row] = 0.f;
       }
     }
-    __syncthreads();
+    lds_barrier();
     delta_inverse<C>(m.a, m.t);
     // fragments that are not all zeros
     for (int f = wave; f < Z::kTiles * Z::kSteps; f += 4) {
@@ -600,10 +604,6 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
     for (int n = 0; n < NT; ++n) {
       x[n] = Columns::values(raw[n]) - steps.since * x[n];
       for_inner.write(wave, n, x[n] * steps.beta);
-      if (STORE && col + 16 * n < s.dvp) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s.x[(head * kChunk + 16 * wave + 4 * g + r) * s.dvp + col + 16 * n] = x[n][r];
-      }
     }
     if (more) walk.ahead(s, values);
     columns.load(columns.rows(s, walk, b, h, walk.live(len)), raw);
@@ -825,21 +825,22 @@ __global__ __launch_bounds__(512, 2) void delta_bwd_kernel(DeltaArgs s) {
 //   dA = -strictly lower (dR U^T),  dP = lower (dO U^T),  M = dA beta D,  N = scale D dP,  M and N of k_i k_j and q_i k_j
 //   dq = N K + scale exp(G) (dO S^T)
 //   dk = N^T Q + (M + M^T) K - exp(G) beta (dR S^T) + Y,  Y = exp(G_C - G) (U dS'^T)
-//   dv = beta dR,  dbeta_i = dR_i X_i + sum_j dA_ij D_ij k_i k_j
+//   dv = beta dR,  dbeta_i = dR_i U_i / beta_i  (u = beta r, and dbeta = du r, of the step itself)
 //   dG_i = sums of (M k k + N q k) over row i less those over column i, and the rows' products of q, k with what they were multiplied by; what
 //   exp(G_C) multiplies goes to the last step;  dg_t = sum of dG from t on
 template <class E, int C, int DK>
 struct DeltaGradShared {
-  static constexpr int kRow = 72, kLine = C + 4, kTiles = C / 16, kKeyTiles = DK / 16;  // 64 columns at a time
+  static constexpr int kRow = 72, kTiles = C / 16, kKeyTiles = DK / 16;  // 64 columns at a time
   union {
     struct {
       uint16_t dr[3][C][kRow], u[3][C][kRow], d_o[delta_pieces<E>()][C][kRow];
     };
-    float inner[2][C][kLine];  // M + M^T, N
+    uint16_t inner[3][delta_rounded<E>()][C][kRow];  // M + M^T, N, N^T
   };
-  float row_sum[2][kTiles][C], col_sum[2][kTiles][C], beta_sum[kTiles][C];
-  float dots[kKeyTiles][C], ends[kKeyTiles][C], xs[C], both[kKeyTiles];
+  float row_sum[2][kTiles][C], col_sum[2][kTiles][C];
+  float dots[kKeyTiles][C], ends[kKeyTiles][C], us[C], both[kKeyTiles];
   float steps[kStepNumbers][C];
+  E keys[2][C][DK + 8];  // Q, K
 };
 
 __device__ __forceinline__ float sum16(float v) {  // over a row of 16 lanes
@@ -848,20 +849,14 @@ __device__ __forceinline__ float sum16(float v) {  // over a row of 16 lanes
   v += row_rotated<2>(v);
   return v + row_rotated<1>(v);
 }
-// four numbers in pieces
-__device__ __forceinline__ void split_four(const f32x4& v, u32x2 (&o)[3]) {
-  const Pieces<3> p = split_tiles(v, f32x4{});
-#pragma unroll
-  for (int k = 0; k < 3; ++k) o[k] = u32x2{p.p[k][0], p.p[k][1]};
-}
 
-// Bound by the time of its loads: sixteen waves to a workgroup, of which a compute unit holds one, hide them better than eight with twice the registers
-// (4 x 2048 steps x 16 heads, bf16: see the table of figures).
+// Bound by the time and the bytes of its loads (a compute unit holds one workgroup): a thread's part of the next 64 columns, of this head or of the next
+// one, is loaded into the registers that this one's have left.
 template <class E, int C, int DK>
-__global__ __launch_bounds__(1024, 4) void delta_grad_kernel(DeltaArgs s) {
+__global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
   typedef DeltaSizes<C, DK> Z;
   typedef DeltaGradShared<E, C, DK> Shared;
-  constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>(), W = 16;
+  constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>(), W = 8;
   constexpr int kMine = Z::kTiles * Z::kKeyTiles / W;  // tiles of a wave: one column of keys, some rows of steps
   constexpr int kLower = Z::kTiles * (Z::kTiles + 1) / 2, kJobs = (2 * kLower + W - 1) / W;
   extern __shared__ char delta_lds[];
@@ -893,125 +888,186 @@ __global__ __launch_bounds__(1024, 4) void delta_grad_kernel(DeltaArgs s) {
   }
   const int64_t key_at = (((int64_t)b * s.chunks + c) * s.n_hk + hk) * Z::kKeyPiece * NI;
   const uint16_t *const kf = s.kf + key_at, *const qf = s.qf + key_at, *const ktf = s.ktf + key_at, *const qtf = s.qtf + key_at;
-  f32x4 sum_q[kMine] = {}, sum_k[kMine] = {};
-  // rows of the keys' arrays: a lane's key in step 16 mt0 + 4 g of the chunk, and steps behind it; what does not exist fails the checks
+  const int64_t head0 = ((int64_t)b * s.chunks + c) * s.n_h + hk * s.each;
+  // rows of the keys' gradients: a lane's key in step 16 mt0 + 4 g of the chunk, and steps behind it; what does not exist fails the checks
   const uint32_t hop = (uint32_t)(s.n_hk * s.d_k) * (uint32_t)sizeof(E), key0 = (uint32_t)(kt * 16 + (tid & 15));
   const uint32_t key_off = key0 < (uint32_t)s.d_k ? (uint32_t)(mt0 * 16 + 4 * ((tid & 63) >> 4)) * hop + key0 * (uint32_t)sizeof(E) : kOob;
-  auto key_rows = [&](const void* array, int n) {
+  auto key_rows = [&](void* array, int n) {
     n = __builtin_amdgcn_readfirstlane(n);
     return rsrc_of((const E*)array + (step0 * s.n_hk + hk) * s.d_k, (uint32_t)(n - 1) * hop + (uint32_t)s.d_k * (uint32_t)sizeof(E));
   };
-  auto key_value = [&](__amdgpu_buffer_rsrc_t from, int i, int r) {
-    const uint32_t step = (uint32_t)(i * 16 + r) * hop;
-    if constexpr (sizeof(E) == 4) return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, key_off, step, 0));
-    else return __uint_as_float((uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, key_off, step, 0) << 16);
+  // A thread's eight columns of dR, U and dO in a step, and a lane's of the state and its gradient in a key's row.  Offsets inside a head's
+  // arrays; columns that do not exist, and steps behind the end, fail the checks.
+  const uint32_t stage_off = (uint32_t)((tid >> 3) * s.dvp + (tid & 7) * 8) * 4, state_off = (uint32_t)((kt * 16 + (tid & 15)) * s.dvp + 8 * ((tid & 63) >> 4)) * 4;
+  u32x4 r8[2], u8[2], s8[2][2], d8[2][2];
+  u32x4 o8[sizeof(E) / 2];
+  const bool whole_eights = s.d_v % 8 == 0;
+  auto load_stage = [&](int e, int v0) {
+    const int64_t rows = (head0 + e) * C * s.dvp;
+    const int v = v0 + (tid & 7) * 8;
+    const uint32_t o = v < s.dvp ? stage_off : kOob;
+    const __amdgpu_buffer_rsrc_t from_r = rsrc_of(s.dr + rows + v0, kOob), from_u = rsrc_of(s.u + rows + v0, kOob);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      r8[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_r, o, 16 * i, 0));
+      u8[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_u, o, 16 * i, 0));
+    }
+    const int t = tid >> 3;
+    const E* const from = (const E*)w->d_o + (step0 * s.n_h + hk * s.each + e) * s.d_v;
+    if (whole_eights) {
+      const __amdgpu_buffer_rsrc_t from_o = rsrc_of(from + v0, kOob);
+      const uint32_t o = t < at.live && v < s.d_v ? (uint32_t)(t * s.n_h * s.d_v + (tid & 7) * 8) * (uint32_t)sizeof(E) : kOob;
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(E) / 2; ++i) o8[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_o, o, 16 * i, 0));
+    } else {
+      Eight<E> raw;
+      raw.load(from + (int64_t)t * s.n_h * s.d_v + v, t < at.live ? max(0, min(8, s.d_v - v)) : 0);
+      o8[0] = raw.a;
+      if constexpr (sizeof(E) == 4) o8[1] = raw.b;
+    }
   };
+  auto load_states = [&](int e, int v0, int ks) {
+    const int64_t rows = (head0 + e) * DK * s.dvp + v0 + 32 * ks;
+    const uint32_t o = v0 + 32 * ks + 8 * ((tid & 63) >> 4) < s.dvp ? state_off : kOob;
+    const __amdgpu_buffer_rsrc_t from_s = rsrc_of(s.states + rows, kOob), from_d = rsrc_of(s.dstates + rows, kOob);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      s8[ks][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_s, o, 16 * i, 0));
+      d8[ks][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_d, o, 16 * i, 0));
+    }
+  };
+  auto numbers = [](const u32x4 (&raw)[2], float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(raw[i / 4][i % 4]);
+  };
+  load_stage(0, 0);
+  load_states(0, 0, 0);
+  load_states(0, 0, 1);
+  // K K^T and Q K^T, of all heads, and the rows of Q and K
+  f32x4 inner[kJobs];
+#pragma unroll
+  for (int x = 0; x < kJobs; ++x) {
+    const int job = min(wave + W * x, 2 * kLower - 1);
+    const DeltaLower at_tile = delta_lower(job % kLower);
+    const uint16_t* const left = job / kLower ? qf : kf;
+    Pieces<NI> one[Z::kKeySteps], two[Z::kKeySteps];
+#pragma unroll
+    for (int ks = 0; ks < Z::kKeySteps; ++ks) {
+      one[ks] = load_fragment<NI>(left + (at_tile.mt * Z::kKeySteps + ks) * NI * kFragment);
+      two[ks] = load_fragment<NI>(kf + (at_tile.nt * Z::kKeySteps + ks) * NI * kFragment);
+    }
+    inner[x] = f32x4{};
+#pragma unroll
+    for (int ks = 0; ks < Z::kKeySteps; ++ks) inner[x] = multiply(one[ks], two[ks], inner[x]);
+  }
+  for (int x = tid; x < 2 * C * (DK / 8); x += 64 * W) {
+    const int what = x / (C * (DK / 8)), t = x / (DK / 8) % C, col = x % (DK / 8) * 8;
+    Eight<E> raw;
+    raw.load((const E*)(what ? w->k : w->q) + ((step0 + t) * s.n_hk + hk) * s.d_k + col, t < at.live ? min(8, s.d_k - col) : 0);
+    *(u32x4*)&m.keys[what][t][col] = raw.a;
+    if constexpr (sizeof(E) == 4) *(u32x4*)&m.keys[what][t][col + 4] = raw.b;
+  }
+  f32x4 sum_q[kMine] = {}, sum_k[kMine] = {};
 
   for (int e = 0; e < s.each; ++e) {
     // (What is made of the thread's number is made again for each head: kept, it would not fit the registers.)
     asm volatile("" : "+v"(tid));
     const int lane = tid & 63, row = lane & 15, g = lane >> 4, key = kt * 16 + row;
     const int h = hk * s.each + e;
-    const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h;
-    __syncthreads();
-    if (tid < kStepNumbers * C) m.steps[tid / C][tid % C] = s.steps[head * kStepNumbers * C + tid];
-    __syncthreads();
+    lds_barrier();
+    if (tid < kStepNumbers * C) m.steps[tid / C][tid % C] = s.steps[(head0 + e) * kStepNumbers * C + tid];
+    lds_barrier();
     f32x4 os[kMine] = {}, rs[kMine] = {}, us[kMine] = {}, acc[kJobs] = {};
-    float xdot = 0.f, both = 0.f;
-    // a thread's four columns of dR, U, X and dO
-    const int t4 = tid >> 4, col4 = (tid & 15) * 4;
-    const float beta4 = m.steps[kBeta][t4];
+    float udot = 0.f, both = 0.f;
+    const int t8 = tid >> 3, col8 = (tid & 7) * 8;
     for (int v0 = 0; v0 < s.d_v; v0 += 64) {
-      const int v = v0 + col4;
-      f32x4 r4 = {}, u4 = {}, x4 = {};
-      float o4[4] = {};
-      if (v < s.dvp) {
-        const int64_t o = (head * C + t4) * s.dvp + v;
-        r4 = *(const f32x4*)(s.dr + o);
-        u4 = *(const f32x4*)(s.u + o);
-        x4 = *(const f32x4*)(s.x + o);
+      const bool same = v0 + 64 < s.d_v, more = same || e + 1 < s.each;  // (the last loads are made again, and not used)
+      const int next_e = same || !more ? e : e + 1, next_v = same ? v0 + 64 : more ? 0 : v0;
+      lds_barrier();
+      {
+        float r[8], u[8], out[8];
+        numbers(r8, r);
+        numbers(u8, u);
+        const Pieces<3> rp = split8(r), up = split8(u);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          *(u32x4*)&m.dr[k][t8][col8] = rp.p[k];
+          *(u32x4*)&m.u[k][t8][col8] = up.p[k];
+        }
+        if constexpr (NI == 1) {
+          *(u32x4*)&m.d_o[0][t8][col8] = o8[0];
+        } else {
+          float o[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[i] = __uint_as_float(o8[i / 4 * (sizeof(E) / 4)][i % 4]);
+          const Pieces<3> op = split8(o);
+#pragma unroll
+          for (int k = 0; k < 3; ++k) *(u32x4*)&m.d_o[k][t8][col8] = op.p[k];
+        }
+        const float beta = m.steps[kBeta][t8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          udot = fmaf(r[i], u[i], udot);
+          out[i] = t8 < at.live ? beta * r[i] : 0.f;
+        }
+        const int v = v0 + col8;
+        if (t8 < at.n && v < s.d_v) store8(dv + ((step0 + t8) * s.n_h + h) * s.d_v + v, out, min(8, s.d_v - v));
       }
-      const int64_t o = ((step0 + t4) * s.n_h + h) * s.d_v + v;
-      if (t4 < at.live) {
+      load_stage(next_e, next_v);
+      lds_barrier();
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (v + i < s.d_v) o4[i] = ld((const E*)w->d_o, (size_t)(o + i));
-      }
-      __syncthreads();
-      u32x2 p[3];
-      split_four(r4, p);
-#pragma unroll
-      for (int k = 0; k < 3; ++k) *(u32x2*)&m.dr[k][t4][col4] = p[k];
-      split_four(u4, p);
-#pragma unroll
-      for (int k = 0; k < 3; ++k) *(u32x2*)&m.u[k][t4][col4] = p[k];
-      split_four(f32x4{o4[0], o4[1], o4[2], o4[3]}, p);  // (bf16 numbers are their upper halves)
-#pragma unroll
-      for (int k = 0; k < NI; ++k) *(u32x2*)&m.d_o[k][t4][col4] = p[k];
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        xdot = fmaf(r4[i], x4[i], xdot);
-        if (t4 < at.n && v + i < s.d_v) st(dv, (size_t)(o + i), t4 < at.live ? beta4 * r4[i] : 0.f);
-      }
-#pragma unroll 1
       for (int ks = 0; ks < 2; ++ks) {
-        if (v0 + 32 * ks >= s.dvp) break;
-        const int at8 = 32 * ks + 8 * g;
-        f32x4 s8[2] = {}, d8[2] = {};
-        if (v0 + at8 < s.dvp) {
-          const int64_t o = (head * DK + key) * s.dvp + v0 + at8;
+        if (v0 + 32 * ks < s.dvp) {
+          const int at8 = 32 * ks + 8 * g;
+          float sv[8], dv_[8];
+          numbers(s8[ks], sv);
+          numbers(d8[ks], dv_);
+          if (mt0 == 0) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            s8[i] = *(const f32x4*)(s.states + o + 4 * i);
-            d8[i] = *(const f32x4*)(s.dstates + o + 4 * i);
+            for (int i = 0; i < 8; ++i) both = fmaf(sv[i], dv_[i], both);
           }
-        }
-        auto rows3 = [&](const uint16_t (*from)[C][Shared::kRow], int mt) {
-          Pieces<3> o;
+          const Pieces<3> sp = split8(sv), dp = split8(dv_);
+          auto rows3 = [&](const uint16_t (*from)[C][Shared::kRow], int mt) {
+            Pieces<3> o;
 #pragma unroll
-          for (int k = 0; k < 3; ++k) o.p[k] = *(const u32x4*)&from[k][mt * 16 + row][at8];
-          return o;
-        };
-        auto grads = [&](int mt) {
-          Pieces<NI> o;
+            for (int k = 0; k < 3; ++k) o.p[k] = *(const u32x4*)&from[k][mt * 16 + row][at8];
+            return o;
+          };
+          auto grads = [&](int mt) {
+            Pieces<NI> o;
 #pragma unroll
-          for (int k = 0; k < NI; ++k) o.p[k] = *(const u32x4*)&m.d_o[k][mt * 16 + row][at8];
-          return o;
-        };
-#pragma unroll
-        for (int i = 0; i < kJobs; ++i) {
-          const int job = wave + W * i;
-          if (job < 2 * kLower) {
-            const DeltaLower at_tile = delta_lower(job % kLower);
-            const Pieces<3> right = rows3(m.u, at_tile.nt);
-            if (job / kLower) acc[i] = multiply(grads(at_tile.mt), right, acc[i]);
-            else acc[i] = multiply(rows3(m.dr, at_tile.mt), right, acc[i]);
-          }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if (mt0 == 0) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) both = fmaf(s8[i / 4][i % 4], d8[i / 4][i % 4], both);
-        }
-        {
-          const Pieces<3> sp = split_tiles(s8[0], s8[1]);
+            for (int k = 0; k < NI; ++k) o.p[k] = *(const u32x4*)&m.d_o[k][mt * 16 + row][at8];
+            return o;
+          };
 #pragma unroll
           for (int i = 0; i < kMine; ++i) {
-            __builtin_amdgcn_sched_barrier(0);
             os[i] = multiply(grads(mt0 + i), sp, os[i]);
             rs[i] = multiply(rows3(m.dr, mt0 + i), sp, rs[i]);
+            us[i] = multiply(rows3(m.u, mt0 + i), dp, us[i]);
+          }
+#pragma unroll
+          for (int i = 0; i < kJobs; ++i) {
+            const int job = wave + W * i;
+            if (job < 2 * kLower) {
+              const DeltaLower at_tile = delta_lower(job % kLower);
+              const Pieces<3> right = rows3(m.u, at_tile.nt);
+              if (job / kLower) acc[i] = multiply(grads(at_tile.mt), right, acc[i]);
+              else acc[i] = multiply(rows3(m.dr, at_tile.mt), right, acc[i]);
+            }
           }
         }
-        __builtin_amdgcn_sched_barrier(0);
-        const Pieces<3> dp = split_tiles(d8[0], d8[1]);
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) us[i] = multiply(rows3(m.u, mt0 + i), dp, us[i]);
+        load_states(next_e, next_v, ks);
       }
     }
-    __syncthreads();
+    lds_barrier();
     asm volatile("" : "+v"(tid));
-    // M and N
+    Pieces<NI> kk[Z::kSteps], qq[Z::kSteps];
+#pragma unroll
+    for (int k = 0; k < Z::kSteps; ++k) {
+      kk[k] = load_fragment<NI>(ktf + (kt * Z::kSteps + k) * NI * kFragment);
+      qq[k] = load_fragment<NI>(qtf + (kt * Z::kSteps + k) * NI * kFragment);
+    }
+    // M and N, in pieces
 #pragma unroll
     for (int x = 0; x < kJobs; ++x) {
       const int job = wave + W * x;
@@ -1019,35 +1075,45 @@ __global__ __launch_bounds__(1024, 4) void delta_grad_kernel(DeltaArgs s) {
       const int what = job / kLower;
       const DeltaLower at_tile = delta_lower(job % kLower);
       const int mt = at_tile.mt, nt = at_tile.nt, j = nt * 16 + row;
-      __builtin_amdgcn_sched_barrier(0);  // (one tile after the other: interleaved they do not fit the registers)
-      f32x4 inner = {};  // K K^T or Q K^T
-#pragma unroll
-      for (int ks = 0; ks < Z::kKeySteps; ++ks)
-        inner = multiply(load_fragment<NI>((what ? qf : kf) + (mt * Z::kKeySteps + ks) * NI * kFragment),
-                         load_fragment<NI>(kf + (nt * Z::kKeySteps + ks) * NI * kFragment), inner);
+      f32x4 mine;
+      const int i0 = mt * 16 + 4 * g;
+      const f32x4 whole_i = *(const f32x4*)&m.steps[kWhole][i0], rest_i = *(const f32x4*)&m.steps[kRest][i0], beta_i = *(const f32x4*)&m.steps[kBeta][i0];
       const float whole = m.steps[kWhole][j], rest = m.steps[kRest][j];
       float down = 0.f;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int i = mt * 16 + 4 * g + r;
+        const int i = i0 + r;
         const bool below = i > j, in = what ? i >= j : below;
-        const float decay = in ? expf((m.steps[kWhole][i] - whole) + (m.steps[kRest][i] - rest)) : 0.f;
-        const float d = in ? decay * (what ? s.scale * acc[x][r] : -acc[x][r]) : 0.f, beta = what ? 1.f : m.steps[kBeta][i];
-        const float mine = d * beta, part = below ? mine * inner[r] : 0.f;
+        const float decay = in ? __builtin_amdgcn_exp2f((whole_i[r] - whole) + (rest_i[r] - rest)) : 0.f;
+        mine[r] = in ? decay * (what ? s.scale * acc[x][r] : -acc[x][r] * beta_i[r]) : 0.f;
+        const float part = below ? mine[r] * inner[x][r] : 0.f;
         down += part;
-        const float across = sum16(part), for_beta = sum16(below ? d * inner[r] : 0.f);
-        if (row == 0) {
-          m.row_sum[what][nt][i] = across;
-          if (!what) m.beta_sum[nt][i] = for_beta;
-        }
+        const float across = sum16(part);
+        if (row == 0) m.row_sum[what][nt][i] = across;
+      }
+      const Pieces<3> p = split_tiles(mine, f32x4{});
+#pragma unroll
+      for (int k = 0; k < NO; ++k) {
+        const u32x2 v = {p.p[k][0], p.p[k][1]};
         if (what) {
-          m.inner[1][i][j] = mine;
-          if (mt != nt) m.inner[1][nt * 16 + 4 * g + r][mt * 16 + row] = 0.f;
-        } else if (below) {
-          m.inner[0][i][j] = mine;
-          m.inner[0][j][i] = mine;
-        } else if (i == j) {
-          m.inner[0][i][j] = 0.f;
+          *(u32x2*)&m.inner[2][k][j][i0] = v;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) m.inner[1][k][i0 + r][j] = (uint16_t)(v[r / 2] >> (16 * (r & 1)));
+          if (mt != nt) {  // above the diagonal
+            *(u32x2*)&m.inner[1][k][j][i0] = u32x2{0, 0};
+            *(u32x2*)&m.inner[2][k][mt * 16 + row][nt * 16 + 4 * g] = u32x2{0, 0};
+          }
+        } else if (mt != nt) {
+          *(u32x2*)&m.inner[0][k][j][i0] = v;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) m.inner[0][k][i0 + r][j] = (uint16_t)(v[r / 2] >> (16 * (r & 1)));
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const uint16_t one = (uint16_t)(v[r / 2] >> (16 * (r & 1)));
+            if (i0 + r >= j) m.inner[0][k][i0 + r][j] = one;
+            if (i0 + r > j) m.inner[0][k][j][i0 + r] = one;
+          }
         }
       }
       down += __shfl_xor(down, 16, 64);
@@ -1055,57 +1121,60 @@ __global__ __launch_bounds__(1024, 4) void delta_grad_kernel(DeltaArgs s) {
       if (g == 0) m.col_sum[what][mt][j] = down;
     }
     // what the states' products come to
+    {
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < kMine; ++i) {
+        const int t0 = (mt0 + i) * 16 + 4 * g;
+        const f32x4 since = *(const f32x4*)&m.steps[kSince][t0], until = *(const f32x4*)&m.steps[kUntil][t0], beta = *(const f32x4*)&m.steps[kBeta][t0];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = (mt0 + i) * 16 + 4 * g + r;
-        const float qv = key_value(key_rows(w->q, at.live), i, r), kv = key_value(key_rows(w->k, at.live), i, r);
-        const float since = m.steps[kSince][t], one = s.scale * since * os[i][r], two = since * m.steps[kBeta][t] * rs[i][r],
-                    three = m.steps[kUntil][t] * us[i][r];
-        const float all = sum16(fmaf(qv, one, -kv * (two + three))), end = sum16(kv * three);
-        if (row == 0) {
-          m.dots[kt][t] = all;
-          m.ends[kt][t] = end;
+        for (int r = 0; r < 4; ++r) {
+          const int t = t0 + r;
+          const float qv = ld(m.keys[0][t], (size_t)key), kv = ld(m.keys[1][t], (size_t)key);
+          const float one = s.scale * since[r] * os[i][r], two = since[r] * beta[r] * rs[i][r], three = until[r] * us[i][r];
+          const float all = sum16(fmaf(qv, one, -kv * (two + three))), end = sum16(kv * three);
+          if (row == 0) {
+            m.dots[kt][t] = all;
+            m.ends[kt][t] = end;
+          }
+          sum_q[i][r] += one;
+          sum_k[i][r] += three - two;
         }
-        sum_q[i][r] += one;
-        sum_k[i][r] += three - two;
       }
     }
     both = wave_sum(both);
     if (lane == 0 && mt0 == 0) m.both[kt] = both;
-    xdot = sum16(xdot);
-    if ((tid & 15) == 0) m.xs[t4] = xdot;
-    __syncthreads();
+    udot += __shfl_xor(udot, 1, 64);
+    udot += __shfl_xor(udot, 2, 64);
+    udot += __shfl_xor(udot, 4, 64);
+    if ((tid & 7) == 0) m.us[tid >> 3] = udot;
+    lds_barrier();
 #pragma unroll
     for (int k = 0; k < Z::kSteps; ++k) {
-      const Pieces<NI> kk = load_fragment<NI>(ktf + (kt * Z::kSteps + k) * NI * kFragment), qq = load_fragment<NI>(qtf + (kt * Z::kSteps + k) * NI * kFragment);
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
-        const int mt = mt0 + i, t = mt * 16 + row;
-        __builtin_amdgcn_sched_barrier(0);
-        auto across = [&](const float (*from)[Shared::kLine]) {
-          return first_pieces<NO>(split_tiles(*(const f32x4*)&from[t][32 * k + 4 * g], *(const f32x4*)&from[t][32 * k + 16 + 4 * g]));
-        };
-        sum_k[i] = multiply(across(m.inner[0]), kk, sum_k[i]);
-        if (2 * k <= mt) sum_q[i] = multiply(across(m.inner[1]), kk, sum_q[i]);
-        if (mt / 2 <= k) {
-          float v[8];
+        const int mt = mt0 + i;
+        auto across = [&](int what) {
+          Pieces<NO> o;
 #pragma unroll
-          for (int x = 0; x < 8; ++x) v[x] = m.inner[1][delta_place(k, x)][t];
-          sum_k[i] = multiply(first_pieces<NO>(split8(v)), qq, sum_k[i]);
-        }
+          for (int x = 0; x < NO; ++x) {
+            const uint16_t* const from = &m.inner[what][x][mt * 16 + row][32 * k + 4 * g];
+            const u32x2 lo = *(const u32x2*)from, hi = *(const u32x2*)(from + 16);
+            o.p[x] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+          }
+          return o;
+        };
+        sum_k[i] = multiply(across(0), kk[k], sum_k[i]);
+        if (2 * k <= mt) sum_q[i] = multiply(across(1), kk[k], sum_q[i]);
+        if (mt / 2 <= k) sum_k[i] = multiply(across(2), qq[k], sum_k[i]);
       }
     }
     if (wave == 0) {
       const int tile = lane >> 4;
-      float d = 0.f, end = 0.f, for_beta = m.xs[lane], all = 0.f;
+      float d = 0.f, end = 0.f, for_beta = lane < at.live ? m.us[lane] / m.steps[kBeta][lane] : 0.f, all = 0.f;
       for (int what = 0; what < 2; ++what) {
         for (int i = 0; i <= tile; ++i) d += m.row_sum[what][i][lane];
         for (int i = tile; i < Z::kTiles; ++i) d -= m.col_sum[what][i][lane];
       }
-      for (int i = 0; i <= tile; ++i) for_beta += m.beta_sum[i][lane];
       for (int i = 0; i < Z::kKeyTiles; ++i) {
         d += m.dots[i][lane];
         end += m.ends[i][lane];
@@ -1121,7 +1190,7 @@ __global__ __launch_bounds__(1024, 4) void delta_grad_kernel(DeltaArgs s) {
       if (lane < at.n) {
         const int64_t o = (step0 + lane) * s.n_h + h;
         if (w->dg) w->dg[o] = lane < at.live ? d : 0.f;
-        w->dbeta[o] = lane < at.live ? for_beta : 0.f;
+        w->dbeta[o] = for_beta;
       }
     }
   }
@@ -1300,7 +1369,7 @@ static int delta_scratch(distdl_delta_plan* p, bool back, hipStream_t st, DeltaA
   } parts[] = {{(void**)&s->kf, key}, {(void**)&s->ktf, key}, {(void**)&s->qf, key}, {(void**)&s->qtf, back ? key : 0},
                {(void**)&s->tf, step}, {(void**)&s->pf, step}, {(void**)&s->ttf, back ? step : 0}, {(void**)&s->ptf, back ? step : 0},
                {(void**)&s->steps, heads * kStepNumbers * C * 4}, {(void**)&s->states, back ? state : 0}, {(void**)&s->dstates, back ? state : 0},
-               {(void**)&s->u, back ? rows : 0}, {(void**)&s->x, back ? rows : 0}, {(void**)&s->dr, back ? rows : 0}};
+               {(void**)&s->u, back ? rows : 0}, {(void**)&s->dr, back ? rows : 0}};
   size_t all = 0;
   for (const Part& v : parts) all += (v.bytes + 255) / 256 * 256;
   bool is_new = true;
@@ -1343,7 +1412,7 @@ static int launch_delta(distdl_delta_plan* p, DeltaArgs& s, hipStream_t st) {
     else hipLaunchKernelGGL((delta_bwd_kernel<E, DK, 1>), groups, dim3(512), 0, st, s);
     constexpr auto grad = delta_grad_kernel<E, C, DK>;
     if ((rc = allow_large_lds<grad>())) return rc;
-    hipLaunchKernelGGL(grad, chunks, dim3(1024), sizeof(DeltaGradShared<E, C, DK>), st, s);
+    hipLaunchKernelGGL(grad, chunks, dim3(512), sizeof(DeltaGradShared<E, C, DK>), st, s);
   }
   return DISTDL_OK;
 }
