@@ -1450,7 +1450,8 @@ static int delta_sizes(const char* call, int64_t n_h, int64_t n_hk, int64_t d_k,
   if (!std::isfinite(scale)) return set_error(DISTDL_ERR_INVALID_ARG, "%s: scale %g", call, scale);
   if (dtype != DISTDL_F32 && dtype != DISTDL_BF16) return set_error(DISTDL_ERR_UNSUPPORTED, "unknown dtype");
   if (d_k > kDeltaKeys) return set_error(DISTDL_ERR_UNSUPPORTED, "%s: d_k of more than %d", call, kDeltaKeys);
-  if (n_h > 1 << 20 || d_v > 1 << 20 || n_h * d_v > 1 << 22) return set_error(DISTDL_ERR_UNSUPPORTED, "%s: problem too large", call);
+  // (a chunk of an array of keys or values stays below 2^31 bytes: the kernels' offsets inside it have 32 bits)
+  if (n_h > 1 << 20 || d_v > 1 << 20 || n_h * d_v > 1 << 22 || n_hk * d_k > 1 << 22) return set_error(DISTDL_ERR_UNSUPPORTED, "%s: problem too large", call);
   return DISTDL_OK;
 }
 
