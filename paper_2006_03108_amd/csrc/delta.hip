@@ -840,8 +840,16 @@ struct DeltaGradShared {
   float row_sum[2][kTiles][C], col_sum[2][kTiles][C];
   float dots[kKeyTiles][C], ends[kKeyTiles][C], us[C], both[kKeyTiles];
   float steps[kStepNumbers][C];
-  E keys[2][C][DK + 8];  // Q, K
 };
+
+// Element e of a lane's eight: a sum of pieces is exact from the smallest on.
+template <int N>
+__device__ __forceinline__ float from_fragment(const Pieces<N>& p, int e) {
+  float v = 0.f;
+#pragma unroll
+  for (int k = N - 1; k >= 0; --k) v += e & 1 ? bf16_hi(p.p[k][e / 2]) : bf16_lo(p.p[k][e / 2]);
+  return v;
+}
 
 __device__ __forceinline__ float sum16(float v) {  // over a row of 16 lanes
   v += row_rotated<8>(v);
@@ -854,6 +862,7 @@ __device__ __forceinline__ float sum16(float v) {  // over a row of 16 lanes
 // one, is loaded into the registers that this one's have left.
 template <class E, int C, int DK>
 __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
+  static_assert(C == 64, "two steps of a sum over steps");
   typedef DeltaSizes<C, DK> Z;
   typedef DeltaGradShared<E, C, DK> Shared;
   constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>(), W = 8;
@@ -943,7 +952,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
   load_stage(0, 0);
   load_states(0, 0, 0);
   load_states(0, 0, 1);
-  // K K^T and Q K^T, of all heads, and the rows of Q and K
+  // K K^T and Q K^T, of all heads
   f32x4 inner[kJobs];
 #pragma unroll
   for (int x = 0; x < kJobs; ++x) {
@@ -959,13 +968,6 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
     inner[x] = f32x4{};
 #pragma unroll
     for (int ks = 0; ks < Z::kKeySteps; ++ks) inner[x] = multiply(one[ks], two[ks], inner[x]);
-  }
-  for (int x = tid; x < 2 * C * (DK / 8); x += 64 * W) {
-    const int what = x / (C * (DK / 8)), t = x / (DK / 8) % C, col = x % (DK / 8) * 8;
-    Eight<E> raw;
-    raw.load((const E*)(what ? w->k : w->q) + ((step0 + t) * s.n_hk + hk) * s.d_k + col, t < at.live ? min(8, s.d_k - col) : 0);
-    *(u32x4*)&m.keys[what][t][col] = raw.a;
-    if constexpr (sizeof(E) == 4) *(u32x4*)&m.keys[what][t][col + 4] = raw.b;
   }
   f32x4 sum_q[kMine] = {}, sum_k[kMine] = {};
 
@@ -1120,7 +1122,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
       down += __shfl_xor(down, 32, 64);
       if (g == 0) m.col_sum[what][mt][j] = down;
     }
-    // what the states' products come to
+    // what the states' products come to (a lane's numbers of the fragments of Q^T and K^T are its numbers of a tile of results)
     {
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
@@ -1129,7 +1131,8 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int t = t0 + r;
-          const float qv = ld(m.keys[0][t], (size_t)key), kv = ld(m.keys[1][t], (size_t)key);
+          const int at8 = i % 2 * 4 + r;  // (a wave's first tile is an even one)
+          const float qv = from_fragment(mt0 + i < 2 ? qq[0] : qq[1], at8), kv = from_fragment(mt0 + i < 2 ? kk[0] : kk[1], at8);
           const float one = s.scale * since[r] * os[i][r], two = since[r] * beta[r] * rs[i][r], three = until[r] * us[i][r];
           const float all = sum16(fmaf(qv, one, -kv * (two + three))), end = sum16(kv * three);
           if (row == 0) {
