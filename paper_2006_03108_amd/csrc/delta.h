@@ -48,6 +48,7 @@ struct DeltaArgs {
   uint16_t *kf, *ktf, *qf, *qtf;      // fragments of K, K^T, Q, Q^T
   // ... and for each sequence, chunk and head
   uint16_t *tf, *pf, *ttf, *ptf;      // fragments of T and P, and of their transposes
+  float* tiles;                       // A and P, tiles on and below the diagonal as they lie in the lanes
   float* steps;                       // of each step: kStepNumbers of them, [C] each
   float *states, *dstates;            // [DK][dvp] at a chunk's start; the gradient at its end
   float *u, *dr;                      // [C][dvp]
@@ -203,7 +204,7 @@ __device__ __forceinline__ void store_fragment(uint16_t* at, const Pieces<N>& v)
 
 template <int C, int DK>
 struct DeltaSizes {
-  static constexpr int kTiles = C / 16, kSteps = C / 32;       // of a chunk's steps as rows, and as what is summed over
+  static constexpr int kTiles = C / 16, kLower = kTiles * (kTiles + 1) / 2, kSteps = C / 32;       // of a chunk's steps as rows, and as what is summed over
   static constexpr int kKeyTiles = DK / 16, kKeySteps = DK / 32;
   // numbers of one piece of all fragments
   static constexpr int64_t kKeyPiece = (int64_t)C * DK, kStepPiece = (int64_t)C * C;

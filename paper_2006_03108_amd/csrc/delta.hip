@@ -194,7 +194,7 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
   }
 
   // K K^T and Q K^T, tiles on and below the diagonal: a wave has the same tiles of both
-  constexpr int kLower = Z::kTiles * (Z::kTiles + 1) / 2, kJobs = (kLower + 3) / 4;
+  constexpr int kLower = Z::kLower, kJobs = (kLower + 3) / 4;
   f32x4 kk[kJobs] = {}, qk[kJobs] = {};
 #pragma unroll
   for (int i = 0; i < kJobs; ++i) {
@@ -228,13 +228,21 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
       const DeltaLower at_tile = delta_lower(wave + 4 * x);
       const int j = at_tile.nt * 16 + row;
       const float whole = m.whole[slot][j], rest = m.rest[slot][j];
+      f32x4 a, p;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int i = at_tile.mt * 16 + 4 * g + r;
         const float decay = i >= j ? __builtin_amdgcn_exp2f((m.whole[slot][i] - whole) + (m.rest[slot][i] - rest)) : 0.f;
-        m.a[i][j] = i > j ? m.beta[slot][i] * decay * kk[x][r] : 0.f;
-        m.p[i][j] = i >= j ? s.scale * decay * qk[x][r] : 0.f;
+        a[r] = i > j ? m.beta[slot][i] * decay * kk[x][r] : 0.f;
+        p[r] = i >= j ? s.scale * decay * qk[x][r] : 0.f;
+        m.a[i][j] = a[r];
+        m.p[i][j] = p[r];
         if (at_tile.mt != at_tile.nt) m.p[at_tile.nt * 16 + 4 * g + r][at_tile.mt * 16 + row] = 0.f;
+      }
+      if constexpr (BACK) {
+        f32x4* const to = (f32x4*)s.tiles + (head * 2 * kLower + wave + 4 * x) * 64 + lane;
+        to[0] = a;
+        to[kLower * 64] = p;
       }
     }
     lds_barrier();
@@ -837,9 +845,10 @@ struct DeltaGradShared {
     };
     uint16_t inner[3][delta_rounded<E>()][C][kRow];  // M + M^T, N, N^T
   };
-  float row_sum[2][kTiles][C], col_sum[2][kTiles][C];
+  float row_sum[2][kTiles][C], col_sum[2][2][C];
   float dots[kKeyTiles][C], ends[kKeyTiles][C], us[C], both[kKeyTiles];
   float steps[kStepNumbers][C];
+  f32x4 kept[2 * kTiles * kKeyTiles / 8][512];  // a thread's sums over the heads in front
 };
 
 // Element e of a lane's eight: a sum of pieces is exact from the smallest on.
@@ -867,17 +876,103 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
   typedef DeltaGradShared<E, C, DK> Shared;
   constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>(), W = 8;
   constexpr int kMine = Z::kTiles * Z::kKeyTiles / W;  // tiles of a wave: one column of keys, some rows of steps
-  constexpr int kLower = Z::kTiles * (Z::kTiles + 1) / 2, kJobs = (2 * kLower + W - 1) / W;
+  constexpr bool kBoth = kMine == 2;  // with 64 keys a wave has tiles of M and of N, with 128 of one of them
   extern __shared__ char delta_lds[];
   Shared& m = *(Shared*)delta_lds;
   const DeltaTable table = DELTA_TABLE(s);
   int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kt = wave % Z::kKeyTiles, mt0 = wave / Z::kKeyTiles * kMine;
-  const int hk = blockIdx.x % (uint32_t)s.n_hk, at_chunk = blockIdx.x / (uint32_t)s.n_hk;
-  const int c = at_chunk % s.chunks, b = at_chunk / s.chunks;
-  const DeltaChunk at = delta_chunk(s, b, c);
+  // Of M and N a wave has the tiles (mt, nt) of its rows mt, which it reads anyway, and one column nt <= mt (the two waves of a SIMD have about as many).
+  const int wave_what = wave >> 2, nt = kBoth || wave_what == 0 ? wave & 3 : 3 - (wave & 3);
+  struct Item {  // a chunk of a key's head
+    DeltaChunk at;
+    int hk;
+    int64_t step0, key0, head0;
+    const E* d_o;
+  };
+  auto item_of = [&](int i) {
+    Item x;
+    x.hk = i % (uint32_t)s.n_hk;
+    const int at_chunk = i / (uint32_t)s.n_hk, c = at_chunk % s.chunks, b = at_chunk / s.chunks;
+    x.at = delta_chunk(s, b, c);
+    x.at.live = __builtin_amdgcn_readfirstlane(x.at.live);
+    x.step0 = (int64_t)b * x.at.steps + x.at.first;
+    x.key0 = ((int64_t)b * s.chunks + c) * s.n_hk + x.hk;
+    x.head0 = x.key0 * s.each;
+    x.d_o = (const E*)table[x.at.p].d_o + (x.step0 * s.n_h + x.hk * s.each) * s.d_v;
+    return x;
+  };
+  // A thread's eight columns of dR, U and dO in a step, and a lane's of the state and its gradient in a key's row.  Offsets inside a head's
+  // arrays; columns that do not exist, and steps behind the end, fail the checks.
+  const uint32_t stage_off = (uint32_t)((tid >> 3) * s.dvp + (tid & 7) * 8) * 4, state_off = (uint32_t)((kt * 16 + (tid & 15)) * s.dvp + 8 * ((tid & 63) >> 4)) * 4;
+  u32x4 r8[2], u8[2], s8[2][2], d8[2][2];
+  u32x4 o8[sizeof(E) / 2];
+  const bool whole_eights = s.d_v % 8 == 0;
+  auto load_stage = [&](const Item& x, int e, int v0, uint32_t size) {
+    const int64_t rows = (x.head0 + e) * C * s.dvp;
+    const int v = v0 + (tid & 7) * 8;
+    const uint32_t o = v < s.dvp ? stage_off : kOob;
+    const __amdgpu_buffer_rsrc_t from_r = rsrc_of(s.dr + rows + v0, size), from_u = rsrc_of(s.u + rows + v0, size);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      r8[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_r, o, 16 * i, 0));
+      u8[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_u, o, 16 * i, 0));
+    }
+    const int t = tid >> 3;
+    const E* const from = x.d_o + e * s.d_v;
+    if (whole_eights) {
+      const __amdgpu_buffer_rsrc_t from_o = rsrc_of(from + v0, size);
+      const uint32_t o = t < x.at.live && v < s.d_v ? (uint32_t)(t * s.n_h * s.d_v + (tid & 7) * 8) * (uint32_t)sizeof(E) : kOob;
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(E) / 2; ++i) o8[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_o, o, 16 * i, 0));
+    } else {
+      Eight<E> raw;
+      raw.load(from + (int64_t)t * s.n_h * s.d_v + v, t < x.at.live && size ? max(0, min(8, s.d_v - v)) : 0);
+      o8[0] = raw.a;
+      if constexpr (sizeof(E) == 4) o8[1] = raw.b;
+    }
+  };
+  auto load_states = [&](const Item& x, int e, int v0, int ks, uint32_t size) {
+    const int64_t rows = (x.head0 + e) * DK * s.dvp + v0 + 32 * ks;
+    const uint32_t o = v0 + 32 * ks + 8 * ((tid & 63) >> 4) < s.dvp ? state_off : kOob;
+    const __amdgpu_buffer_rsrc_t from_s = rsrc_of(s.states + rows, size), from_d = rsrc_of(s.dstates + rows, size);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      s8[ks][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_s, o, 16 * i, 0));
+      d8[ks][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_d, o, 16 * i, 0));
+    }
+  };
+  auto numbers = [](const u32x4 (&raw)[2], float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(raw[i / 4][i % 4]);
+  };
+  auto load_pieces = [&](const uint16_t* fragments, int at_byte) {
+    const __amdgpu_buffer_rsrc_t from = rsrc_of(fragments, kOob);
+    Pieces<NI> o;
+#pragma unroll
+    for (int k = 0; k < NI; ++k) o.p[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, (tid & 63) * 16, at_byte + k * kFragment * 2, 0));
+    return o;
+  };
+  float step;
+  auto load_first = [&](const Item& x, int e, bool there) {
+    const uint32_t size = there && x.at.live > 0 ? kOob : 0;
+    const __amdgpu_buffer_rsrc_t from = rsrc_of(s.steps + (x.head0 + e) * kStepNumbers * C, size ? kStepNumbers * C * 4 : 0);
+    step = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, tid * 4, 0, 0));
+    load_stage(x, e, 0, size);
+    load_states(x, e, 0, 0, size);
+    load_states(x, e, 0, 1, size);
+  };
+
+  const int items = s.n_b * s.chunks * s.n_hk;
+  Item it = item_of(blockIdx.x);
+  load_first(it, 0, true);
+  for (int i = blockIdx.x; i < items; i += gridDim.x) {
+  const bool another = i + (int)gridDim.x < items;
+  const Item next = item_of(another ? i + (int)gridDim.x : i);
+  const DeltaChunk at = it.at;
+  const int hk = it.hk;
+  const int64_t step0 = it.step0, head0 = it.head0;
   const DeltaTable w = table + at.p;
-  const int64_t step0 = (int64_t)b * at.steps + at.first;
   E* const dq = (E*)w->dq, * const dk = (E*)w->dk, * const dv = (E*)w->dv;
   if (at.live == 0) {
     for (int i = tid; i < at.n * s.d_k; i += 64 * W) {
@@ -893,98 +988,24 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
       if (w->dg) w->dg[o] = 0.f;
       w->dbeta[o] = 0.f;
     }
-    return;
+    load_first(next, 0, another);
+    it = next;
+    continue;
   }
-  const int64_t key_at = (((int64_t)b * s.chunks + c) * s.n_hk + hk) * Z::kKeyPiece * NI;
-  const uint16_t *const kf = s.kf + key_at, *const qf = s.qf + key_at, *const ktf = s.ktf + key_at, *const qtf = s.qtf + key_at;
-  const int64_t head0 = ((int64_t)b * s.chunks + c) * s.n_h + hk * s.each;
-  // rows of the keys' gradients: a lane's key in step 16 mt0 + 4 g of the chunk, and steps behind it; what does not exist fails the checks
-  const uint32_t hop = (uint32_t)(s.n_hk * s.d_k) * (uint32_t)sizeof(E), key0 = (uint32_t)(kt * 16 + (tid & 15));
-  const uint32_t key_off = key0 < (uint32_t)s.d_k ? (uint32_t)(mt0 * 16 + 4 * ((tid & 63) >> 4)) * hop + key0 * (uint32_t)sizeof(E) : kOob;
-  auto key_rows = [&](void* array, int n) {
-    n = __builtin_amdgcn_readfirstlane(n);
-    return rsrc_of((const E*)array + (step0 * s.n_hk + hk) * s.d_k, (uint32_t)(n - 1) * hop + (uint32_t)s.d_k * (uint32_t)sizeof(E));
-  };
-  // A thread's eight columns of dR, U and dO in a step, and a lane's of the state and its gradient in a key's row.  Offsets inside a head's
-  // arrays; columns that do not exist, and steps behind the end, fail the checks.
-  const uint32_t stage_off = (uint32_t)((tid >> 3) * s.dvp + (tid & 7) * 8) * 4, state_off = (uint32_t)((kt * 16 + (tid & 15)) * s.dvp + 8 * ((tid & 63) >> 4)) * 4;
-  u32x4 r8[2], u8[2], s8[2][2], d8[2][2];
-  u32x4 o8[sizeof(E) / 2];
-  const bool whole_eights = s.d_v % 8 == 0;
-  auto load_stage = [&](int e, int v0) {
-    const int64_t rows = (head0 + e) * C * s.dvp;
-    const int v = v0 + (tid & 7) * 8;
-    const uint32_t o = v < s.dvp ? stage_off : kOob;
-    const __amdgpu_buffer_rsrc_t from_r = rsrc_of(s.dr + rows + v0, kOob), from_u = rsrc_of(s.u + rows + v0, kOob);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      r8[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_r, o, 16 * i, 0));
-      u8[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_u, o, 16 * i, 0));
-    }
-    const int t = tid >> 3;
-    const E* const from = (const E*)w->d_o + (step0 * s.n_h + hk * s.each + e) * s.d_v;
-    if (whole_eights) {
-      const __amdgpu_buffer_rsrc_t from_o = rsrc_of(from + v0, kOob);
-      const uint32_t o = t < at.live && v < s.d_v ? (uint32_t)(t * s.n_h * s.d_v + (tid & 7) * 8) * (uint32_t)sizeof(E) : kOob;
-#pragma unroll
-      for (int i = 0; i < (int)sizeof(E) / 2; ++i) o8[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_o, o, 16 * i, 0));
-    } else {
-      Eight<E> raw;
-      raw.load(from + (int64_t)t * s.n_h * s.d_v + v, t < at.live ? max(0, min(8, s.d_v - v)) : 0);
-      o8[0] = raw.a;
-      if constexpr (sizeof(E) == 4) o8[1] = raw.b;
-    }
-  };
-  auto load_states = [&](int e, int v0, int ks) {
-    const int64_t rows = (head0 + e) * DK * s.dvp + v0 + 32 * ks;
-    const uint32_t o = v0 + 32 * ks + 8 * ((tid & 63) >> 4) < s.dvp ? state_off : kOob;
-    const __amdgpu_buffer_rsrc_t from_s = rsrc_of(s.states + rows, kOob), from_d = rsrc_of(s.dstates + rows, kOob);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      s8[ks][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_s, o, 16 * i, 0));
-      d8[ks][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_d, o, 16 * i, 0));
-    }
-  };
-  auto numbers = [](const u32x4 (&raw)[2], float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(raw[i / 4][i % 4]);
-  };
-  load_stage(0, 0);
-  load_states(0, 0, 0);
-  load_states(0, 0, 1);
-  // K K^T and Q K^T, of all heads
-  f32x4 inner[kJobs];
-#pragma unroll
-  for (int x = 0; x < kJobs; ++x) {
-    const int job = min(wave + W * x, 2 * kLower - 1);
-    const DeltaLower at_tile = delta_lower(job % kLower);
-    const uint16_t* const left = job / kLower ? qf : kf;
-    Pieces<NI> one[Z::kKeySteps], two[Z::kKeySteps];
-#pragma unroll
-    for (int ks = 0; ks < Z::kKeySteps; ++ks) {
-      one[ks] = load_fragment<NI>(left + (at_tile.mt * Z::kKeySteps + ks) * NI * kFragment);
-      two[ks] = load_fragment<NI>(kf + (at_tile.nt * Z::kKeySteps + ks) * NI * kFragment);
-    }
-    inner[x] = f32x4{};
-#pragma unroll
-    for (int ks = 0; ks < Z::kKeySteps; ++ks) inner[x] = multiply(one[ks], two[ks], inner[x]);
-  }
-  f32x4 sum_q[kMine] = {}, sum_k[kMine] = {};
-
+  const int64_t key_at = it.key0 * Z::kKeyPiece * NI;
+  const uint16_t *const ktf = s.ktf + key_at, *const qtf = s.qtf + key_at;
   for (int e = 0; e < s.each; ++e) {
     // (What is made of the thread's number is made again for each head: kept, it would not fit the registers.)
     asm volatile("" : "+v"(tid));
     const int lane = tid & 63, row = lane & 15, g = lane >> 4, key = kt * 16 + row;
     const int h = hk * s.each + e;
     lds_barrier();
-    if (tid < kStepNumbers * C) m.steps[tid / C][tid % C] = s.steps[(head0 + e) * kStepNumbers * C + tid];
-    lds_barrier();
-    f32x4 os[kMine] = {}, rs[kMine] = {}, us[kMine] = {}, acc[kJobs] = {};
+    if (tid < kStepNumbers * C) m.steps[tid / C][tid % C] = step;
+    f32x4 os[kMine] = {}, rs[kMine] = {}, us[kMine] = {}, acc[4] = {};
     float udot = 0.f, both = 0.f;
     const int t8 = tid >> 3, col8 = (tid & 7) * 8;
     for (int v0 = 0; v0 < s.d_v; v0 += 64) {
-      const bool same = v0 + 64 < s.d_v, more = same || e + 1 < s.each;  // (the last loads are made again, and not used)
-      const int next_e = same || !more ? e : e + 1, next_v = same ? v0 + 64 : more ? 0 : v0;
+      const uint32_t more = v0 + 64 < s.d_v ? kOob : 0;  // (the loads behind the last ones are of nothing)
       lds_barrier();
       {
         float r[8], u[8], out[8];
@@ -1015,7 +1036,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
         const int v = v0 + col8;
         if (t8 < at.n && v < s.d_v) store8(dv + ((step0 + t8) * s.n_h + h) * s.d_v + v, out, min(8, s.d_v - v));
       }
-      load_stage(next_e, next_v);
+      load_stage(it, e, v0 + 64, more);
       lds_barrier();
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
@@ -1035,30 +1056,29 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
             for (int k = 0; k < 3; ++k) o.p[k] = *(const u32x4*)&from[k][mt * 16 + row][at8];
             return o;
           };
-          auto grads = [&](int mt) {
-            Pieces<NI> o;
+          const Pieces<3> right = rows3(m.u, nt);
+          auto products = [&](auto what) {
 #pragma unroll
-            for (int k = 0; k < NI; ++k) o.p[k] = *(const u32x4*)&m.d_o[k][mt * 16 + row][at8];
-            return o;
-          };
+            for (int i = 0; i < kMine; ++i) {
+              Pieces<NI> o;
 #pragma unroll
-          for (int i = 0; i < kMine; ++i) {
-            os[i] = multiply(grads(mt0 + i), sp, os[i]);
-            rs[i] = multiply(rows3(m.dr, mt0 + i), sp, rs[i]);
-            us[i] = multiply(rows3(m.u, mt0 + i), dp, us[i]);
-          }
-#pragma unroll
-          for (int i = 0; i < kJobs; ++i) {
-            const int job = wave + W * i;
-            if (job < 2 * kLower) {
-              const DeltaLower at_tile = delta_lower(job % kLower);
-              const Pieces<3> right = rows3(m.u, at_tile.nt);
-              if (job / kLower) acc[i] = multiply(grads(at_tile.mt), right, acc[i]);
-              else acc[i] = multiply(rows3(m.dr, at_tile.mt), right, acc[i]);
+              for (int k = 0; k < NI; ++k) o.p[k] = *(const u32x4*)&m.d_o[k][(mt0 + i) * 16 + row][at8];
+              const Pieces<3> r = rows3(m.dr, mt0 + i), u = rows3(m.u, mt0 + i);
+              os[i] = multiply(o, sp, os[i]);
+              rs[i] = multiply(r, sp, rs[i]);
+              us[i] = multiply(u, dp, us[i]);
+              if (mt0 + i >= nt) {
+                if constexpr (what != 1) acc[i] = multiply(r, right, acc[i]);
+                if constexpr (what == 1) acc[i] = multiply(o, right, acc[i]);
+                if constexpr (what == 2) acc[2 + i % 2] = multiply(o, right, acc[2 + i % 2]);
+              }
             }
-          }
+          };
+          if constexpr (kBoth) products(std::integral_constant<int, 2>());
+          else if (wave_what) products(std::integral_constant<int, 1>());
+          else products(std::integral_constant<int, 0>());
         }
-        load_states(next_e, next_v, ks);
+        load_states(it, e, v0 + 64, ks, more);
       }
     }
     lds_barrier();
@@ -1066,33 +1086,46 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
     Pieces<NI> kk[Z::kSteps], qq[Z::kSteps];
 #pragma unroll
     for (int k = 0; k < Z::kSteps; ++k) {
-      kk[k] = load_fragment<NI>(ktf + (kt * Z::kSteps + k) * NI * kFragment);
-      qq[k] = load_fragment<NI>(qtf + (kt * Z::kSteps + k) * NI * kFragment);
+      kk[k] = load_pieces(ktf, (kt * Z::kSteps + k) * NI * kFragment * 2);
+      qq[k] = load_pieces(qtf, (kt * Z::kSteps + k) * NI * kFragment * 2);
     }
-    // M and N, in pieces
+    const __amdgpu_buffer_rsrc_t tiles = rsrc_of(s.tiles + (head0 + e) * Z::kLower * 2 * 256, kOob);
+    f32x4 made[4];
 #pragma unroll
-    for (int x = 0; x < kJobs; ++x) {
-      const int job = wave + W * x;
-      if (job >= 2 * kLower) continue;
-      const int what = job / kLower;
-      const DeltaLower at_tile = delta_lower(job % kLower);
-      const int mt = at_tile.mt, nt = at_tile.nt, j = nt * 16 + row;
-      f32x4 mine;
+    for (int x = 0; x < 4; ++x) {
+      const int mt = max(mt0 + x % kMine, nt);
+      made[x] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(tiles, lane * 16, ((kBoth ? x / 2 : wave_what) * Z::kLower + mt * (mt + 1) / 2 + nt) * 1024, 0));
+    }
+    const bool last = e + 1 == s.each;
+    load_first(last ? next : it, last ? 0 : e + 1, !last || another);
+    // M and N, in pieces; what A and P were made of is in them still: M k k = -dA A, and N q k = dP P
+    const int j = nt * 16 + row;
+    const float whole = m.steps[kWhole][j], rest = m.steps[kRest][j];
+    float down[2] = {};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int what = kBoth ? x / 2 : wave_what, mt = mt0 + x % kMine;
+      if (mt < nt) continue;
+      f32x4 mine, across;
       const int i0 = mt * 16 + 4 * g;
       const f32x4 whole_i = *(const f32x4*)&m.steps[kWhole][i0], rest_i = *(const f32x4*)&m.steps[kRest][i0], beta_i = *(const f32x4*)&m.steps[kBeta][i0];
-      const float whole = m.steps[kWhole][j], rest = m.steps[kRest][j];
-      float down = 0.f;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int i = i0 + r;
         const bool below = i > j, in = what ? i >= j : below;
-        const float decay = in ? __builtin_amdgcn_exp2f((whole_i[r] - whole) + (rest_i[r] - rest)) : 0.f;
-        mine[r] = in ? decay * (what ? s.scale * acc[x][r] : -acc[x][r] * beta_i[r]) : 0.f;
-        const float part = below ? mine[r] * inner[x][r] : 0.f;
-        down += part;
-        const float across = sum16(part);
-        if (row == 0) m.row_sum[what][nt][i] = across;
+        float decay = __builtin_amdgcn_exp2f(in ? (whole_i[r] - whole) + (rest_i[r] - rest) : 0.f);
+        asm volatile("" : "+v"(decay));  // (no branch around it)
+        float all = decay * acc[x][r] * (what ? s.scale : -beta_i[r]);
+        asm volatile("" : "+v"(all));
+        mine[r] = in ? all : 0.f;
+        float part = what ? acc[x][r] * made[x][r] : -acc[x][r] * made[x][r];
+        asm volatile("" : "+v"(part));
+        part = below ? part : 0.f;
+        down[kBoth ? x / 2 : 0] += part;
+        across[r] = sum16(part);
       }
+      const float mine_of = row < 2 ? row ? across[1] : across[0] : row == 2 ? across[2] : across[3];
+      if (row < 4) m.row_sum[what][nt][i0 + row] = mine_of;
       const Pieces<3> p = split_tiles(mine, f32x4{});
 #pragma unroll
       for (int k = 0; k < NO; ++k) {
@@ -1101,7 +1134,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
           *(u32x2*)&m.inner[2][k][j][i0] = v;
 #pragma unroll
           for (int r = 0; r < 4; ++r) m.inner[1][k][i0 + r][j] = (uint16_t)(v[r / 2] >> (16 * (r & 1)));
-          if (mt != nt) {  // above the diagonal
+          if ((mt ^ nt) == 1) {  // above the diagonal, in a step of the sum that is not all zeros
             *(u32x2*)&m.inner[1][k][j][i0] = u32x2{0, 0};
             *(u32x2*)&m.inner[2][k][mt * 16 + row][nt * 16 + 4 * g] = u32x2{0, 0};
           }
@@ -1118,29 +1151,36 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
           }
         }
       }
-      down += __shfl_xor(down, 16, 64);
-      down += __shfl_xor(down, 32, 64);
-      if (g == 0) m.col_sum[what][mt][j] = down;
+    }
+#pragma unroll
+    for (int x = 0; x < (kBoth ? 2 : 1); ++x) {
+      down[x] += __shfl_xor(down[x], 16, 64);
+      down[x] += __shfl_xor(down[x], 32, 64);
+      if (g == 0) m.col_sum[kBoth ? x : wave_what][mt0 / 2][j] = down[x];
     }
     // what the states' products come to (a lane's numbers of the fragments of Q^T and K^T are its numbers of a tile of results)
+    f32x4 sum_q[kMine], sum_k[kMine];
     {
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
         const int t0 = (mt0 + i) * 16 + 4 * g;
+        f32x4 all, end;
         const f32x4 since = *(const f32x4*)&m.steps[kSince][t0], until = *(const f32x4*)&m.steps[kUntil][t0], beta = *(const f32x4*)&m.steps[kBeta][t0];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int t = t0 + r;
           const int at8 = i % 2 * 4 + r;  // (a wave's first tile is an even one)
           const float qv = from_fragment(mt0 + i < 2 ? qq[0] : qq[1], at8), kv = from_fragment(mt0 + i < 2 ? kk[0] : kk[1], at8);
           const float one = s.scale * since[r] * os[i][r], two = since[r] * beta[r] * rs[i][r], three = until[r] * us[i][r];
-          const float all = sum16(fmaf(qv, one, -kv * (two + three))), end = sum16(kv * three);
-          if (row == 0) {
-            m.dots[kt][t] = all;
-            m.ends[kt][t] = end;
-          }
-          sum_q[i][r] += one;
-          sum_k[i][r] += three - two;
+          all[r] = sum16(fmaf(qv, one, -kv * (two + three)));
+          end[r] = sum16(kv * three);
+          sum_q[i][r] = one;
+          sum_k[i][r] = three - two;
+        }
+        const float one_all = row < 2 ? row ? all[1] : all[0] : row == 2 ? all[2] : all[3];
+        const float one_end = row < 2 ? row ? end[1] : end[0] : row == 2 ? end[2] : end[3];
+        if (row < 4) {
+          m.dots[kt][t0 + row] = one_all;
+          m.ends[kt][t0 + row] = one_end;
         }
       }
     }
@@ -1174,10 +1214,17 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
     if (wave == 0) {
       const int tile = lane >> 4;
       float d = 0.f, end = 0.f, for_beta = lane < at.live ? m.us[lane] / m.steps[kBeta][lane] : 0.f, all = 0.f;
+#pragma unroll
       for (int what = 0; what < 2; ++what) {
-        for (int i = 0; i <= tile; ++i) d += m.row_sum[what][i][lane];
-        for (int i = tile; i < Z::kTiles; ++i) d -= m.col_sum[what][i][lane];
+#pragma unroll
+        for (int i = 0; i < Z::kTiles; ++i) {
+          const float v = m.row_sum[what][i][lane];  // (what no wave wrote is not used)
+          d += i <= tile ? v : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < Z::kTiles / kMine; ++i) d -= m.col_sum[what][i][lane];
       }
+#pragma unroll
       for (int i = 0; i < Z::kKeyTiles; ++i) {
         d += m.dots[i][lane];
         end += m.ends[i][lane];
@@ -1196,23 +1243,47 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
         w->dbeta[o] = for_beta;
       }
     }
-  }
-  const __amdgpu_buffer_rsrc_t to_q = key_rows(dq, at.n), to_k = key_rows(dk, at.n);
+    if (e > 0) {
 #pragma unroll
-  for (int i = 0; i < kMine; ++i)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const bool in = (mt0 + i) * 16 + 4 * ((tid & 63) >> 4) + r < at.live;
-      const uint32_t step = (uint32_t)(i * 16 + r) * hop;
-      const float q = in ? sum_q[i][r] : 0.f, k = in ? sum_k[i][r] : 0.f;
-      if constexpr (sizeof(E) == 4) {
-        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(q), to_q, key_off, step, 0);
-        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(k), to_k, key_off, step, 0);
-      } else {
-        __builtin_amdgcn_raw_buffer_store_b16(to_bf16(q), to_q, key_off, step, 0);
-        __builtin_amdgcn_raw_buffer_store_b16(to_bf16(k), to_k, key_off, step, 0);
+      for (int i = 0; i < kMine; ++i) {
+        sum_q[i] += m.kept[i][tid];
+        sum_k[i] += m.kept[kMine + i][tid];
       }
     }
+    if (e + 1 < s.each) {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        m.kept[i][tid] = sum_q[i];
+        m.kept[kMine + i][tid] = sum_k[i];
+      }
+      continue;
+    }
+    // rows of the keys' gradients: a lane's key in step 16 mt0 + 4 g of the chunk, and steps behind it; what does not exist fails the checks
+    const uint32_t hop = (uint32_t)(s.n_hk * s.d_k) * (uint32_t)sizeof(E);
+    const uint32_t key_off = key < s.d_k ? (uint32_t)(mt0 * 16 + 4 * g) * hop + (uint32_t)key * (uint32_t)sizeof(E) : kOob;
+    auto key_rows = [&](void* array, int n) {
+      n = __builtin_amdgcn_readfirstlane(n);
+      return rsrc_of((const E*)array + (step0 * s.n_hk + hk) * s.d_k, (uint32_t)(n - 1) * hop + (uint32_t)s.d_k * (uint32_t)sizeof(E));
+    };
+    const __amdgpu_buffer_rsrc_t to_q = key_rows(dq, at.n), to_k = key_rows(dk, at.n);
+#pragma unroll
+    for (int i = 0; i < kMine; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const bool in = (mt0 + i) * 16 + 4 * g + r < at.live;
+        const uint32_t step_off = (uint32_t)(i * 16 + r) * hop;
+        const float q = in ? sum_q[i][r] : 0.f, k = in ? sum_k[i][r] : 0.f;
+        if constexpr (sizeof(E) == 4) {
+          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(q), to_q, key_off, step_off, 0);
+          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(k), to_k, key_off, step_off, 0);
+        } else {
+          __builtin_amdgcn_raw_buffer_store_b16(to_bf16(q), to_q, key_off, step_off, 0);
+          __builtin_amdgcn_raw_buffer_store_b16(to_bf16(k), to_k, key_off, step_off, 0);
+        }
+      }
+  }
+  it = next;
+  }
 }
 
 // ---- single tokens --------------------------------------------------------
@@ -1371,7 +1442,7 @@ static int delta_scratch(distdl_delta_plan* p, bool back, hipStream_t st, DeltaA
     size_t bytes;
   } parts[] = {{(void**)&s->kf, key}, {(void**)&s->ktf, key}, {(void**)&s->qf, key}, {(void**)&s->qtf, back ? key : 0},
                {(void**)&s->tf, step}, {(void**)&s->pf, step}, {(void**)&s->ttf, back ? step : 0}, {(void**)&s->ptf, back ? step : 0},
-               {(void**)&s->steps, heads * kStepNumbers * C * 4}, {(void**)&s->states, back ? state : 0}, {(void**)&s->dstates, back ? state : 0},
+               {(void**)&s->tiles, back ? heads * 2 * Z::kLower * 1024 : 0}, {(void**)&s->steps, heads * kStepNumbers * C * 4}, {(void**)&s->states, back ? state : 0}, {(void**)&s->dstates, back ? state : 0},
                {(void**)&s->u, back ? rows : 0}, {(void**)&s->dr, back ? rows : 0}};
   size_t all = 0;
   for (const Part& v : parts) all += (v.bytes + 255) / 256 * 256;
@@ -1415,7 +1486,7 @@ static int launch_delta(distdl_delta_plan* p, DeltaArgs& s, hipStream_t st) {
     else hipLaunchKernelGGL((delta_bwd_kernel<E, DK, 1>), groups, dim3(512), 0, st, s);
     constexpr auto grad = delta_grad_kernel<E, C, DK>;
     if ((rc = allow_large_lds<grad>())) return rc;
-    hipLaunchKernelGGL(grad, chunks, dim3(512), sizeof(DeltaGradShared<E, C, DK>), st, s);
+    hipLaunchKernelGGL(grad, dim3(std::min(chunks.x, 256u)), dim3(512), sizeof(DeltaGradShared<E, C, DK>), st, s);
   }
   return DISTDL_OK;
 }
