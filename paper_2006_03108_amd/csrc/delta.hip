@@ -881,7 +881,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
   Shared& m = *(Shared*)delta_lds;
   const DeltaTable table = DELTA_TABLE(s);
   int tid = threadIdx.x;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kt = wave % Z::kKeyTiles, mt0 = wave / Z::kKeyTiles * kMine;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kt = kBoth ? wave & 3 : wave, mt0 = wave / Z::kKeyTiles * kMine;
   // Of M and N a wave has the tiles (mt, nt) of its rows mt, which it reads anyway, and one column nt <= mt (the two waves of a SIMD have about as many).
   const int wave_what = wave >> 2, nt = kBoth || wave_what == 0 ? wave & 3 : 3 - (wave & 3);
   struct Item {  // a chunk of a key's head
@@ -905,7 +905,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
   // A thread's eight columns of dR, U and dO in a step, and a lane's of the state and its gradient in a key's row.  Offsets inside a head's
   // arrays; columns that do not exist, and steps behind the end, fail the checks.
   const uint32_t stage_off = (uint32_t)((tid >> 3) * s.dvp + (tid & 7) * 8) * 4, state_off = (uint32_t)((kt * 16 + (tid & 15)) * s.dvp + 8 * ((tid & 63) >> 4)) * 4;
-  u32x4 r8[2], u8[2], s8[2][2], d8[2][2];
+  u32x4 r8[2], u8[2], s8[2], d8[2];
   u32x4 o8[sizeof(E) / 2];
   const bool whole_eights = s.d_v % 8 == 0;
   auto load_stage = [&](const Item& x, int e, int v0, uint32_t size) {
@@ -932,15 +932,15 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
       if constexpr (sizeof(E) == 4) o8[1] = raw.b;
     }
   };
-  auto load_states = [&](const Item& x, int e, int v0, int ks, uint32_t size) {
-    const int64_t rows = (x.head0 + e) * DK * s.dvp + v0 + 32 * ks;
-    const uint32_t o = v0 + 32 * ks + 8 * ((tid & 63) >> 4) < s.dvp ? state_off : kOob;
-    const __amdgpu_buffer_rsrc_t from_s = rsrc_of(s.states + rows, size), from_d = rsrc_of(s.dstates + rows, size);
+  auto load_eight = [&](const float* states, const Item& x, int e, int v0, uint32_t size, u32x4 (&to)[2]) {
+    const __amdgpu_buffer_rsrc_t from = rsrc_of(states + (x.head0 + e) * DK * s.dvp + v0, size);
+    const uint32_t o = v0 + 8 * ((tid & 63) >> 4) < s.dvp ? state_off : kOob;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      s8[ks][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_s, o, 16 * i, 0));
-      d8[ks][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from_d, o, 16 * i, 0));
-    }
+    for (int i = 0; i < 2; ++i) to[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, o, 16 * i, 0));
+  };
+  auto load_states = [&](const Item& x, int e, uint32_t size) {
+    load_eight(s.states, x, e, 0, size, s8);
+    load_eight(s.dstates, x, e, 0, size, d8);
   };
   auto numbers = [](const u32x4 (&raw)[2], float (&v)[8]) {
 #pragma unroll
@@ -959,13 +959,15 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
     const __amdgpu_buffer_rsrc_t from = rsrc_of(s.steps + (x.head0 + e) * kStepNumbers * C, size ? kStepNumbers * C * 4 : 0);
     step = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, tid * 4, 0, 0));
     load_stage(x, e, 0, size);
-    load_states(x, e, 0, 0, size);
-    load_states(x, e, 0, 1, size);
+    return size;
   };
 
   const int items = s.n_b * s.chunks * s.n_hk;
   Item it = item_of(blockIdx.x);
-  load_first(it, 0, true);
+  {
+    const uint32_t size = load_first(it, 0, true);
+    load_states(it, 0, size);
+  }
   for (int i = blockIdx.x; i < items; i += gridDim.x) {
   const bool another = i + (int)gridDim.x < items;
   const Item next = item_of(another ? i + (int)gridDim.x : i);
@@ -988,7 +990,8 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
       if (w->dg) w->dg[o] = 0.f;
       w->dbeta[o] = 0.f;
     }
-    load_first(next, 0, another);
+    const uint32_t size = load_first(next, 0, another);
+    load_states(next, 0, size);
     it = next;
     continue;
   }
@@ -1003,6 +1006,13 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
     if (tid < kStepNumbers * C) m.steps[tid / C][tid % C] = step;
     f32x4 os[kMine] = {}, rs[kMine] = {}, us[kMine] = {}, acc[4] = {};
     float udot = 0.f, both = 0.f;
+    const __amdgpu_buffer_rsrc_t tiles = rsrc_of(s.tiles + (head0 + e) * Z::kLower * 2 * 256, kOob);
+    f32x4 made[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int mt = max(mt0 + x % kMine, nt);
+      made[x] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(tiles, lane * 16, ((kBoth ? x / 2 : wave_what) * Z::kLower + mt * (mt + 1) / 2 + nt) * 1024, 0));
+    }
     const int t8 = tid >> 3, col8 = (tid & 7) * 8;
     for (int v0 = 0; v0 < s.d_v; v0 += 64) {
       const uint32_t more = v0 + 64 < s.d_v ? kOob : 0;  // (the loads behind the last ones are of nothing)
@@ -1043,30 +1053,31 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
         if (v0 + 32 * ks < s.dvp) {
           const int at8 = 32 * ks + 8 * g;
           float sv[8], dv_[8];
-          numbers(s8[ks], sv);
-          numbers(d8[ks], dv_);
+          numbers(s8, sv);
+          numbers(d8, dv_);
           if (mt0 == 0) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) both = fmaf(sv[i], dv_[i], both);
           }
-          const Pieces<3> sp = split8(sv), dp = split8(dv_);
+          const int next_v = v0 + 32 * ks + 32;
+          const uint32_t more_v = next_v < s.dvp ? kOob : 0;
           auto rows3 = [&](const uint16_t (*from)[C][Shared::kRow], int mt) {
             Pieces<3> o;
 #pragma unroll
             for (int k = 0; k < 3; ++k) o.p[k] = *(const u32x4*)&from[k][mt * 16 + row][at8];
             return o;
           };
-          const Pieces<3> right = rows3(m.u, nt);
           auto products = [&](auto what) {
+            const Pieces<3> right = rows3(m.u, nt), sp = split8(sv);
+            load_eight(s.states, it, e, next_v, more_v, s8);
 #pragma unroll
             for (int i = 0; i < kMine; ++i) {
               Pieces<NI> o;
 #pragma unroll
               for (int k = 0; k < NI; ++k) o.p[k] = *(const u32x4*)&m.d_o[k][(mt0 + i) * 16 + row][at8];
-              const Pieces<3> r = rows3(m.dr, mt0 + i), u = rows3(m.u, mt0 + i);
+              const Pieces<3> r = rows3(m.dr, mt0 + i);
               os[i] = multiply(o, sp, os[i]);
               rs[i] = multiply(r, sp, rs[i]);
-              us[i] = multiply(u, dp, us[i]);
               if (mt0 + i >= nt) {
                 if constexpr (what != 1) acc[i] = multiply(r, right, acc[i]);
                 if constexpr (what == 1) acc[i] = multiply(o, right, acc[i]);
@@ -1077,8 +1088,12 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
           if constexpr (kBoth) products(std::integral_constant<int, 2>());
           else if (wave_what) products(std::integral_constant<int, 1>());
           else products(std::integral_constant<int, 0>());
+          numbers(d8, dv_);
+          const Pieces<3> dp = split8(dv_);
+          load_eight(s.dstates, it, e, next_v, more_v, d8);
+#pragma unroll
+          for (int i = 0; i < kMine; ++i) us[i] = multiply(rows3(m.u, mt0 + i), dp, us[i]);
         }
-        load_states(it, e, v0 + 64, ks, more);
       }
     }
     lds_barrier();
@@ -1089,56 +1104,40 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
       kk[k] = load_pieces(ktf, (kt * Z::kSteps + k) * NI * kFragment * 2);
       qq[k] = load_pieces(qtf, (kt * Z::kSteps + k) * NI * kFragment * 2);
     }
-    const __amdgpu_buffer_rsrc_t tiles = rsrc_of(s.tiles + (head0 + e) * Z::kLower * 2 * 256, kOob);
-    f32x4 made[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int mt = max(mt0 + x % kMine, nt);
-      made[x] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(tiles, lane * 16, ((kBoth ? x / 2 : wave_what) * Z::kLower + mt * (mt + 1) / 2 + nt) * 1024, 0));
-    }
-    const bool last = e + 1 == s.each;
-    load_first(last ? next : it, last ? 0 : e + 1, !last || another);
     // M and N, in pieces; what A and P were made of is in them still: M k k = -dA A, and N q k = dP P
     const int j = nt * 16 + row;
     const float whole = m.steps[kWhole][j], rest = m.steps[kRest][j];
     float down[2] = {};
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int what = kBoth ? x / 2 : wave_what, mt = mt0 + x % kMine;
-      if (mt < nt) continue;
+    auto tile_of = [&](auto what, auto diagonal, int x, int mt) {
       f32x4 mine, across;
       const int i0 = mt * 16 + 4 * g;
       const f32x4 whole_i = *(const f32x4*)&m.steps[kWhole][i0], rest_i = *(const f32x4*)&m.steps[kRest][i0], beta_i = *(const f32x4*)&m.steps[kBeta][i0];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int i = i0 + r;
-        const bool below = i > j, in = what ? i >= j : below;
+        const bool below = !diagonal || 4 * g + r > row, in = below || (what && 4 * g + r == row);
         float decay = __builtin_amdgcn_exp2f(in ? (whole_i[r] - whole) + (rest_i[r] - rest) : 0.f);
-        asm volatile("" : "+v"(decay));  // (no branch around it)
-        float all = decay * acc[x][r] * (what ? s.scale : -beta_i[r]);
-        asm volatile("" : "+v"(all));
+        if constexpr (diagonal) asm volatile("" : "+v"(decay));  // (no branch around it)
+        const float all = decay * acc[x][r] * (what ? s.scale : -beta_i[r]), part = what ? acc[x][r] * made[x][r] : -acc[x][r] * made[x][r];
         mine[r] = in ? all : 0.f;
-        float part = what ? acc[x][r] * made[x][r] : -acc[x][r] * made[x][r];
-        asm volatile("" : "+v"(part));
-        part = below ? part : 0.f;
-        down[kBoth ? x / 2 : 0] += part;
-        across[r] = sum16(part);
+        const float mine_part = below ? part : 0.f;
+        down[kBoth ? x / 2 : 0] += mine_part;
+        across[r] = sum16(mine_part);
       }
-      const float mine_of = row < 2 ? row ? across[1] : across[0] : row == 2 ? across[2] : across[3];
-      if (row < 4) m.row_sum[what][nt][i0 + row] = mine_of;
+      const float across_of = row < 2 ? row ? across[1] : across[0] : row == 2 ? across[2] : across[3];
+      if (row < 4) m.row_sum[what][nt][i0 + row] = across_of;
       const Pieces<3> p = split_tiles(mine, f32x4{});
 #pragma unroll
       for (int k = 0; k < NO; ++k) {
         const u32x2 v = {p.p[k][0], p.p[k][1]};
-        if (what) {
+        if constexpr (what) {
           *(u32x2*)&m.inner[2][k][j][i0] = v;
 #pragma unroll
           for (int r = 0; r < 4; ++r) m.inner[1][k][i0 + r][j] = (uint16_t)(v[r / 2] >> (16 * (r & 1)));
-          if ((mt ^ nt) == 1) {  // above the diagonal, in a step of the sum that is not all zeros
+          if (!diagonal && (mt ^ nt) == 1) {  // above the diagonal, in a step of the sum that is not all zeros
             *(u32x2*)&m.inner[1][k][j][i0] = u32x2{0, 0};
             *(u32x2*)&m.inner[2][k][mt * 16 + row][nt * 16 + 4 * g] = u32x2{0, 0};
           }
-        } else if (mt != nt) {
+        } else if constexpr (!diagonal) {
           *(u32x2*)&m.inner[0][k][j][i0] = v;
 #pragma unroll
           for (int r = 0; r < 4; ++r) m.inner[0][k][i0 + r][j] = (uint16_t)(v[r / 2] >> (16 * (r & 1)));
@@ -1146,12 +1145,34 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const uint16_t one = (uint16_t)(v[r / 2] >> (16 * (r & 1)));
-            if (i0 + r >= j) m.inner[0][k][i0 + r][j] = one;
-            if (i0 + r > j) m.inner[0][k][j][i0 + r] = one;
+            if (4 * g + r >= row) m.inner[0][k][i0 + r][j] = one;
+            if (4 * g + r > row) m.inner[0][k][j][i0 + r] = one;
           }
         }
       }
+    };
+    auto tiles_of = [&](auto what, int first, int count) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int mt = mt0 + x % kMine;
+        if (x < first || x >= first + count || mt < nt) continue;
+        if (mt == nt) tile_of(what, std::true_type(), x, mt);
+        else tile_of(what, std::false_type(), x, mt);
+      }
+    };
+    if (kBoth) {
+      tiles_of(std::integral_constant<int, 0>(), 0, 2);
+      tiles_of(std::integral_constant<int, 1>(), 2, 2);
+    } else if (wave_what) {
+      tiles_of(std::integral_constant<int, 1>(), 0, 4);
+    } else {
+      tiles_of(std::integral_constant<int, 0>(), 0, 4);
     }
+    // the next columns: of the next head, or of another chunk
+    const bool last = e + 1 == s.each;
+    const Item& then = last ? next : it;
+    const int then_e = last ? 0 : e + 1;
+    const uint32_t then_size = load_first(then, then_e, !last || another);
 #pragma unroll
     for (int x = 0; x < (kBoth ? 2 : 1); ++x) {
       down[x] += __shfl_xor(down[x], 16, 64);
@@ -1191,6 +1212,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
     udot += __shfl_xor(udot, 4, 64);
     if ((tid & 7) == 0) m.us[tid >> 3] = udot;
     lds_barrier();
+    load_states(then, then_e, then_size);
 #pragma unroll
     for (int k = 0; k < Z::kSteps; ++k) {
 #pragma unroll
