@@ -843,13 +843,15 @@ struct DeltaGradShared {
     struct {
       uint16_t dr[3][C][kRow], u[3][C][kRow], d_o[delta_pieces<E>()][C][kRow];
     };
-    uint16_t inner[3][delta_rounded<E>()][C][kRow];  // M + M^T, N, N^T
+    uint16_t inner[3][delta_rounded<E>()][C][kRow];  // M + M^T, N, N^T; in a row, a lane's eight numbers of a step of the sum one behind the other
   };
   float row_sum[2][kTiles][C], col_sum[2][2][C];
   float dots[kKeyTiles][C], ends[kKeyTiles][C], us[C], both[kKeyTiles];
   float steps[kStepNumbers][C];
   f32x4 kept[2 * kTiles * kKeyTiles / 8][512];  // a thread's sums over the heads in front
 };
+
+__device__ __forceinline__ int place_of(int col) { return (col & 0x23) | (col >> 2 & 3) << 3 | (col >> 4 & 1) << 2; }
 
 // Element e of a lane's eight: a sum of pieces is exact from the smallest on.
 template <int N>
@@ -1130,23 +1132,23 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
       for (int k = 0; k < NO; ++k) {
         const u32x2 v = {p.p[k][0], p.p[k][1]};
         if constexpr (what) {
-          *(u32x2*)&m.inner[2][k][j][i0] = v;
+          *(u32x2*)&m.inner[2][k][j][place_of(i0)] = v;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) m.inner[1][k][i0 + r][j] = (uint16_t)(v[r / 2] >> (16 * (r & 1)));
+          for (int r = 0; r < 4; ++r) m.inner[1][k][i0 + r][place_of(j)] = (uint16_t)(v[r / 2] >> (16 * (r & 1)));
           if (!diagonal && (mt ^ nt) == 1) {  // above the diagonal, in a step of the sum that is not all zeros
-            *(u32x2*)&m.inner[1][k][j][i0] = u32x2{0, 0};
-            *(u32x2*)&m.inner[2][k][mt * 16 + row][nt * 16 + 4 * g] = u32x2{0, 0};
+            *(u32x2*)&m.inner[1][k][j][place_of(i0)] = u32x2{0, 0};
+            *(u32x2*)&m.inner[2][k][mt * 16 + row][place_of(nt * 16 + 4 * g)] = u32x2{0, 0};
           }
         } else if constexpr (!diagonal) {
-          *(u32x2*)&m.inner[0][k][j][i0] = v;
+          *(u32x2*)&m.inner[0][k][j][place_of(i0)] = v;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) m.inner[0][k][i0 + r][j] = (uint16_t)(v[r / 2] >> (16 * (r & 1)));
+          for (int r = 0; r < 4; ++r) m.inner[0][k][i0 + r][place_of(j)] = (uint16_t)(v[r / 2] >> (16 * (r & 1)));
         } else {
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const uint16_t one = (uint16_t)(v[r / 2] >> (16 * (r & 1)));
-            if (4 * g + r >= row) m.inner[0][k][i0 + r][j] = one;
-            if (4 * g + r > row) m.inner[0][k][j][i0 + r] = one;
+            if (4 * g + r >= row) m.inner[0][k][i0 + r][place_of(j)] = one;
+            if (4 * g + r > row) m.inner[0][k][j][place_of(i0) + r] = one;
           }
         }
       }
@@ -1222,9 +1224,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
           Pieces<NO> o;
 #pragma unroll
           for (int x = 0; x < NO; ++x) {
-            const uint16_t* const from = &m.inner[what][x][mt * 16 + row][32 * k + 4 * g];
-            const u32x2 lo = *(const u32x2*)from, hi = *(const u32x2*)(from + 16);
-            o.p[x] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+            o.p[x] = *(const u32x4*)&m.inner[what][x][mt * 16 + row][32 * k + 8 * g];
           }
           return o;
         };
