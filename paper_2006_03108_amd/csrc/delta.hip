@@ -25,6 +25,10 @@ __device__ __forceinline__ float bounded(float g) { return g < -200.f ? -200.f :
 // beta's gradient is dR U / beta, what beta multiplies being U / beta.  So a beta of 0 counts as 2^-100: what it adds to a state does not show.
 __device__ __forceinline__ float nonzero(float beta) { return fabsf(beta) < 0x1p-100f ? 0x1p-100f : beta; }
 
+// Pieces of a product whose results the tensors' type rounds to bf16: what lies below 16 bits does not show there.
+template <class E>
+constexpr int delta_rounded() { return sizeof(E) == 2 ? 2 : 3; }
+
 // ---- a chunk's own matrices -----------------------------------------------
 // (The waves of these kernels meet over LDS alone, so their barriers leave global loads and stores under way: lds_barrier.)
 template <class E, int C, int DK>
@@ -106,7 +110,7 @@ template <class E, int C, int DK, bool BACK>
 __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
   typedef DeltaSizes<C, DK> Z;
   typedef DeltaPrepareShared<E, C, DK> Shared;
-  constexpr int NI = delta_pieces<E>();
+  constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>();
   extern __shared__ char delta_lds[];
   Shared& m = *(Shared*)delta_lds;
   const DeltaTable table = DELTA_TABLE(s);
@@ -171,7 +175,7 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
 
   // their fragments
   const int64_t key = ((int64_t)b * s.chunks + c) * s.n_hk + hk, key_at = key * Z::kKeyPiece * NI;
-  for (int f = wave; f < 2 * Z::kTiles * Z::kKeySteps; f += 4) {
+  for (int f = wave; f < (BACK ? 1 : 2) * Z::kTiles * Z::kKeySteps; f += 4) {  // (the adjoint needs no Q and no P as they are)
     const int what = f / (Z::kTiles * Z::kKeySteps), i = f % (Z::kTiles * Z::kKeySteps), mt = i / Z::kKeySteps, ks = i % Z::kKeySteps;
     Pieces<NI> v;
 #pragma unroll
@@ -256,7 +260,7 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
           return split_tiles(*(const f32x4*)&from[i][32 * ts + 4 * g], *(const f32x4*)&from[i][32 * ts + 16 + 4 * g]);
         };
         store_fragment(s.tf + o, across(m.t));
-        store_fragment(s.pf + o, across(m.p));
+        if constexpr (!BACK) store_fragment(s.pf + head * Z::kStepPiece * NO + (int64_t)f * NO * kFragment, first_pieces<NO>(across(m.p)));
       }
       if (BACK && mt / 2 <= ts) {
         auto down = [&](const float (*from)[Shared::kLine]) {
@@ -325,10 +329,6 @@ __device__ __forceinline__ DeltaChain delta_chain(const DeltaArgs& s) {
   return DeltaChain{(int)(chain / (uint32_t)s.n_h), (int)(chain % (uint32_t)s.n_h), (int)slice * 16 * NT};
 }
 
-// Pieces of a product whose results the tensors' type rounds to bf16: what lies below 16 bits does not show there.
-template <class E>
-constexpr int delta_rounded() { return sizeof(E) == 2 ? 2 : 3; }
-
 // An operand that the four waves of a workgroup make together and all read: [steps of the sum][column tiles][pieces][lanes].
 template <int STEPS, int NT, int N>
 struct DeltaShared {
@@ -382,15 +382,17 @@ struct DeltaFragments {
     hop = (int64_t)heads * numbers * 2;
     at = (const char*)base + ((chunk0 + c) * heads + head) * numbers * 2 + (int64_t)from * kFragment * 2;
   }
-  __device__ __forceinline__ void load() {
-    const __amdgpu_buffer_rsrc_t from = rsrc_of(at, kOob);
+  // fragments first .. last - 1; the others' loads are of nothing
+  __device__ __forceinline__ void load(int first = 0, int last = COUNT) {
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i)
+    for (int i = 0; i < COUNT; ++i) {
+      const __amdgpu_buffer_rsrc_t from = rsrc_of(at, i >= first && i < last ? kOob : 0);
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         const int o = (i * STRIDE + k) * kFragment * 2;
         v[i].p[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, (threadIdx.x & 63) * 16 + (o & 4095), o & ~4095, 0));
       }
+    }
   }
 };
 // exp(G), exp(G_C - G), beta of a wave's steps, and exp(G_C)
@@ -493,15 +495,16 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
   if (!STORE && wave >= 4) {  // O = scale exp(G) (Q S) + P U
     auto outputs = [&](int p) { return table[p].o; };
     DeltaFragments<KS, NI, NI> qf;
-    DeltaFragments<2, NO, kInner> pf;
+    DeltaFragments<2, NO, NO> pf;
+    const int steps_in = tile < 2 ? 1 : 2;  // of the sums over steps, those that are not all zeros
     DeltaSteps steps;
     qf.start(s.qf, chunk0, s.n_hk, hk, Z::kKeyPiece * NI, 0, tile * KS * NI);
-    pf.start(s.pf, chunk0, s.n_h, h, Z::kStepPiece * kInner, 0, tile * 2 * kInner);
+    pf.start(s.pf, chunk0, s.n_h, h, Z::kStepPiece * NO, 0, tile * 2 * NO);
     steps.start(s, chunk0, h, 0);
     walk.start(s, 0, outputs);
     if (chunks > 0) {
       qf.load();
-      pf.load();
+      pf.load(0, steps_in);
       steps.load(tile);
     }
     __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);  // (so that the loop's waits count its own loads alone)
@@ -520,7 +523,7 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
       if (wave >= 6) for_out.template multiply_into<2>(pf.v, 0, out);
       else for_out.template multiply_into<1>(pf.v, 0, out);
       if (more) pf.at += pf.hop;
-      pf.load();
+      pf.load(0, steps_in);
       const int count = walk.count(), live = walk.live(len);
       const __amdgpu_buffer_rsrc_t to = columns.rows(s, walk, b, h, count);
 #pragma unroll
@@ -556,6 +559,7 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
   auto values = [&](int p) { return table[p].v; };
   DeltaFragments<4, NI, KS * NI> kf;  // of all tiles of steps, for the wave's step over keys
   DeltaFragments<2, kInner, kInner> tf;
+  const int steps_in = wave < 2 ? 1 : 2;
   DeltaFragments<2 * KT, NI, NI> ktf;
   DeltaSteps steps;
   kf.start(s.kf, chunk0, s.n_hk, hk, Z::kKeyPiece * NI, 0, wave * KT / 2 * NI);
@@ -567,7 +571,7 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
   if (chunks > 0) {
     columns.load(columns.rows(s, walk, b, h, walk.live(len)), raw);
     kf.load();
-    tf.load();
+    tf.load(0, steps_in);
     ktf.load();
     steps.load(tile);
   }
@@ -637,7 +641,7 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
       tf.at += tf.hop;
       steps.at += steps.hop;
     }
-    tf.load();
+    tf.load(0, steps_in);
     steps.load(tile);
     lds_barrier();
     // S' = exp(G_C) S + K^T (exp(G_C - G) U)
@@ -694,7 +698,7 @@ __global__ __launch_bounds__(512, 2) void delta_bwd_kernel(DeltaArgs s) {
     walk.start(s, c, arrays);
     typename Columns::Raw raw[NT][4];
     columns.load(columns.rows(s, walk, b, h, walk.live(len)), raw);
-    ptf.load();
+    ptf.load(tile / 2);
     qtf.load();
     steps.load(tile);
     __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);  // (so that the loop's waits count its own loads alone)
@@ -720,7 +724,7 @@ __global__ __launch_bounds__(512, 2) void delta_bwd_kernel(DeltaArgs s) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) of_inner[c & 1].v[tile][n][lane] = u[n];
       if (more) ptf.at -= ptf.hop;
-      ptf.load();
+      ptf.load(tile / 2);
       delta_state<KT, NT>(for_queries, qtf.v, sum);
 #pragma unroll
       for (int k = 0; k < KT; ++k)
@@ -757,7 +761,7 @@ __global__ __launch_bounds__(512, 2) void delta_bwd_kernel(DeltaArgs s) {
   steps.start(s, chunk0, h, last);
   if (chunks > 0) {
     kf.load();
-    ttf.load();
+    ttf.load(wave / 2);
     ktf.load();
     steps.load(tile);
     __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
@@ -808,7 +812,7 @@ __global__ __launch_bounds__(512, 2) void delta_bwd_kernel(DeltaArgs s) {
       ttf.at -= ttf.hop;
       steps.at -= steps.hop;
     }
-    ttf.load();
+    ttf.load(wave / 2);
     steps.load(tile);
     lds_barrier();
     delta_state<KT, NT>(for_state, ktf.v, state);
@@ -1462,8 +1466,8 @@ static int delta_scratch(distdl_delta_plan* p, bool back, hipStream_t st, DeltaA
   struct Part {
     void** at;
     size_t bytes;
-  } parts[] = {{(void**)&s->kf, key}, {(void**)&s->ktf, key}, {(void**)&s->qf, key}, {(void**)&s->qtf, back ? key : 0},
-               {(void**)&s->tf, step}, {(void**)&s->pf, step}, {(void**)&s->ttf, back ? step : 0}, {(void**)&s->ptf, back ? step : 0},
+  } parts[] = {{(void**)&s->kf, key}, {(void**)&s->ktf, key}, {(void**)&s->qf, back ? 0 : key}, {(void**)&s->qtf, back ? key : 0},
+               {(void**)&s->tf, step}, {(void**)&s->pf, back ? 0 : step / kInner * delta_rounded<E>()}, {(void**)&s->ttf, back ? step : 0}, {(void**)&s->ptf, back ? step : 0},
                {(void**)&s->tiles, back ? heads * 2 * Z::kLower * 1024 : 0}, {(void**)&s->steps, heads * kStepNumbers * C * 4}, {(void**)&s->states, back ? state : 0}, {(void**)&s->dstates, back ? state : 0},
                {(void**)&s->u, back ? rows : 0}, {(void**)&s->dr, back ? rows : 0}};
   size_t all = 0;
