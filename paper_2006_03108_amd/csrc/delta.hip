@@ -29,6 +29,10 @@ __device__ __forceinline__ float nonzero(float beta) { return fabsf(beta) < 0x1p
 template <class E>
 constexpr int delta_rounded() { return sizeof(E) == 2 ? 2 : 3; }
 
+// Whether K^T is made of K where it is used.
+template <class E>
+constexpr bool delta_turned() { return sizeof(E) == 2; }
+
 // ---- a chunk's own matrices -----------------------------------------------
 // (The waves of these kernels meet over LDS alone, so their barriers leave global loads and stores under way: lds_barrier.)
 template <class E, int C, int DK>
@@ -186,7 +190,7 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
     }
     store_fragment((what ? s.qf : s.kf) + key_at + (int64_t)i * NI * kFragment, v);
   }
-  for (int f = wave; f < (BACK ? 2 : 1) * Z::kKeyTiles * Z::kSteps; f += 4) {
+  for (int f = wave; f < (BACK ? 2 : delta_turned<E>() ? 0 : 1) * Z::kKeyTiles * Z::kSteps; f += 4) {
     const int what = f / (Z::kKeyTiles * Z::kSteps), i = f % (Z::kKeyTiles * Z::kSteps), mt = i / Z::kSteps, ts = i % Z::kSteps;
     Pieces<NI> v;
 #pragma unroll
@@ -329,6 +333,9 @@ __device__ __forceinline__ DeltaChain delta_chain(const DeltaArgs& s) {
   return DeltaChain{(int)(chain / (uint32_t)s.n_h), (int)(chain % (uint32_t)s.n_h), (int)slice * 16 * NT};
 }
 
+struct Nothing {
+  __device__ __forceinline__ void operator()() const {}
+};
 // An operand that the four waves of a workgroup make together and all read: [steps of the sum][column tiles][pieces][lanes].
 template <int STEPS, int NT, int N>
 struct DeltaShared {
@@ -341,13 +348,15 @@ struct DeltaShared {
   }
   // c[n] += left b for the `count` steps from `first` on: all of b is read before the first product, which the compiler would otherwise make wait
   // for one read after the other
-  template <int COUNT, int NA>
-  __device__ __forceinline__ void multiply_into(const Pieces<NA>* left, int first, f32x4 (&c)[NT]) const {
+  template <int COUNT, int NA, class F = Nothing>
+  __device__ __forceinline__ void multiply_into(const Pieces<NA>* left, int first, f32x4 (&c)[NT], F while_reading = F()) const {
     Pieces<N> right[COUNT][NT];
 #pragma unroll
     for (int k = 0; k < COUNT; ++k)
 #pragma unroll
       for (int n = 0; n < NT; ++n) right[k][n] = read(first + k, n);
+    __builtin_amdgcn_sched_barrier(0);
+    while_reading();
     __builtin_amdgcn_sched_barrier(0);
     f32x4 odd[NT] = {};
 #pragma unroll
@@ -414,6 +423,34 @@ struct DeltaSteps {
     decay = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, 0, (kChunk - 1) * 4, 0));
   }
 };
+// K^T of a wave's keys from K of the same: a product of tiles of steps with a matrix of zeros and ones has K's numbers where a lane of the left operand K^T
+// wants them.  With bf16 keys that is 8 products and 16 other instructions in the time of the partial sums' reads, and 16 of 62 KiB less to load for a
+// chunk (222 us instead of 238 for 8192 steps of 32 heads); with the three pieces of fp32 keys it is three times that, and fragments are loaded.
+template <int KT>
+struct DeltaTurn {
+  u32x4 ones[KT];  // (16 keys of the 32) of a fragment
+  __device__ __forceinline__ DeltaTurn(int wave) {
+    const int at = (int)(threadIdx.x & 15) - 4 * (int)((threadIdx.x & 63) >> 4);  // a lane's element that is 1, of four
+    const uint32_t lo = at == 0 ? 0x3f80u : at == 1 ? 0x3f800000u : 0u, hi = at == 2 ? 0x3f80u : at == 3 ? 0x3f800000u : 0u;
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      const bool second = KT == 2 ? i == 1 : (wave & 1) != 0;
+      ones[i] = second ? u32x4{0u, 0u, lo, hi} : u32x4{lo, hi, 0u, 0u};
+    }
+  }
+  __device__ __forceinline__ void operator()(const Pieces<1> (&k)[4], Pieces<1> (&turned)[2 * KT]) const {
+#pragma unroll
+    for (int i = 0; i < KT; ++i)
+#pragma unroll
+      for (int mt = 0; mt < 4; ++mt) {
+        const f32x4 v = multiply(k[mt], Pieces<1>{ones[i]}, f32x4{});
+        turned[i * 2 + mt / 2].p[0][mt % 2 * 2] = to_bf16(v[0], v[1]);  // (exact)
+        turned[i * 2 + mt / 2].p[0][mt % 2 * 2 + 1] = to_bf16(v[2], v[3]);
+      }
+  }
+  template <int N, int M>
+  __device__ __forceinline__ void operator()(const Pieces<N>&, Pieces<M>&) const {}
+};
 // Tiles of results in fp32, as they lie in the lanes.
 template <int TILES, int NT>
 struct DeltaTiles {
@@ -430,37 +467,45 @@ __device__ __forceinline__ void delta_own(const f32x4 (&state)[KT][NT], int wave
   }
 }
 // K times a wave's rows of the state: its part of every tile of steps
-template <int NT, int NA>
-__device__ __forceinline__ void delta_partial(const Pieces<NA>* left, const Pieces<3> (&own)[NT], int wave, DeltaTiles<16, NT>& to) {
+template <int NT, int NA, class F>
+__device__ __forceinline__ void delta_partial(const Pieces<NA>* left, const Pieces<3> (&own)[NT], int wave, DeltaTiles<16, NT>& to, F meanwhile) {
   f32x4 part[4][NT];
 #pragma unroll
   for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
     for (int n = 0; n < NT; ++n) part[mt][n] = multiply(left[mt], own[n], f32x4{});
+  __builtin_amdgcn_sched_barrier(0);
+  meanwhile();
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
     for (int n = 0; n < NT; ++n) to.v[mt * 4 + wave][n][threadIdx.x & 63] = part[mt][n];
 }
-template <int NT>
-__device__ __forceinline__ void delta_joined(const DeltaTiles<16, NT>& from, int tile, f32x4 (&x)[NT]) {
+template <int NT, class F>
+__device__ __forceinline__ void delta_joined(const DeltaTiles<16, NT>& from, int tile, f32x4 (&x)[NT], F while_reading) {
+  f32x4 v[NT][4];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    f32x4 v[4];
+  for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = from.v[tile * 4 + i][n][threadIdx.x & 63];
-    x[n] = (v[0] + v[1]) + (v[2] + v[3]);
-  }
+    for (int i = 0; i < 4; ++i) v[n][i] = from.v[tile * 4 + i][n][threadIdx.x & 63];
+  __builtin_amdgcn_sched_barrier(0);
+  while_reading();
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int n = 0; n < NT; ++n) x[n] = (v[n][0] + v[n][1]) + (v[n][2] + v[n][3]);
 }
 
 // A wave's rows of the state += left b
-template <int KT, int NT, int NA>
-__device__ __forceinline__ void delta_state(const DeltaShared<2, NT, 3>& b, const Pieces<NA>* left, f32x4 (&state)[KT][NT]) {
+template <int KT, int NT, int NA, class F = Nothing>
+__device__ __forceinline__ void delta_state(const DeltaShared<2, NT, 3>& b, const Pieces<NA>* left, f32x4 (&state)[KT][NT], F while_reading = F()) {
   Pieces<3> right[2][NT];
 #pragma unroll
   for (int k = 0; k < 2; ++k)
 #pragma unroll
     for (int n = 0; n < NT; ++n) right[k][n] = b.read(k, n);
+  __builtin_amdgcn_sched_barrier(0);
+  while_reading();
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int k = 0; k < 2; ++k)
@@ -561,9 +606,11 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
   DeltaFragments<2, kInner, kInner> tf;
   const int steps_in = wave < 2 ? 1 : 2;
   DeltaFragments<2 * KT, NI, NI> ktf;
+  constexpr bool kTurned = delta_turned<E>();
+  const DeltaTurn<KT> turn(wave);
   DeltaSteps steps;
   kf.start(s.kf, chunk0, s.n_hk, hk, Z::kKeyPiece * NI, 0, wave * KT / 2 * NI);
-  ktf.start(s.ktf, chunk0, s.n_hk, hk, Z::kKeyPiece * NI, 0, tile * KT * 2 * NI);
+  if constexpr (!kTurned) ktf.start(s.ktf, chunk0, s.n_hk, hk, Z::kKeyPiece * NI, 0, tile * KT * 2 * NI);
   tf.start(s.tf, chunk0, s.n_h, h, Z::kStepPiece * kInner, 0, tile * 2 * kInner);
   steps.start(s, chunk0, h, 0);
   walk.start(s, 0, values);
@@ -572,7 +619,7 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
     columns.load(columns.rows(s, walk, b, h, walk.live(len)), raw);
     kf.load();
     tf.load(0, steps_in);
-    ktf.load();
+    if constexpr (!kTurned) ktf.load();
     steps.load(tile);
   }
   __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
@@ -582,7 +629,9 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
     // K S
     Pieces<3> own[NT];
     delta_own<KT, NT>(state, wave, own);
-    delta_partial<NT>(kf.v, own, wave, of_keys);
+    delta_partial<NT>(kf.v, own, wave, of_keys, [&] {
+      if constexpr (!kTurned) ktf.load();
+    });
     if constexpr (!STORE) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -597,7 +646,6 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
         }
     }
     if (more) kf.at += kf.hop;
-    kf.load();
     lds_barrier();
     if constexpr (STORE) {
       float* const to = s.states + head * DK * s.dvp;
@@ -611,7 +659,10 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
     }
     // X = V - exp(G) (K S)
     f32x4 x[NT];
-    delta_joined<NT>(of_keys, tile, x);
+    delta_joined<NT>(of_keys, tile, x, [&] {
+      if constexpr (kTurned) turn(kf.v, ktf.v);
+      kf.load();
+    });
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       x[n] = Columns::values(raw[n]) - steps.since * x[n];
@@ -641,13 +692,13 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
       tf.at += tf.hop;
       steps.at += steps.hop;
     }
-    tf.load(0, steps_in);
-    steps.load(tile);
     lds_barrier();
     // S' = exp(G_C) S + K^T (exp(G_C - G) U)
-    delta_state<KT, NT>(for_state, ktf.v, state);
-    if (more) ktf.at += ktf.hop;
-    ktf.load();
+    delta_state<KT, NT>(for_state, ktf.v, state, [&] {
+      tf.load(0, steps_in);
+      steps.load(tile);
+    });
+    if (!kTurned && more) ktf.at += ktf.hop;
   }
   if (s.hT) {
 #pragma unroll
@@ -774,9 +825,8 @@ __global__ __launch_bounds__(512, 2) void delta_bwd_kernel(DeltaArgs s) {
     const int64_t head = (chunk0 + c) * s.n_h + h;
     Pieces<3> own[NT];
     delta_own<KT, NT>(state, wave, own);
-    delta_partial<NT>(kf.v, own, wave, of_keys);
+    delta_partial<NT>(kf.v, own, wave, of_keys, [&] { ktf.load(); });
     if (more) kf.at -= kf.hop;
-    kf.load();
     lds_barrier();
     {
       float* const to = s.dstates + head * DK * s.dvp;
@@ -789,7 +839,7 @@ __global__ __launch_bounds__(512, 2) void delta_bwd_kernel(DeltaArgs s) {
             if (col + 16 * n < s.dvp) to[(int64_t)(16 * (wave * KT + i) + 4 * g + r) * s.dvp + col + 16 * n] = state[i][n][r];
     }
     f32x4 u[NT];
-    delta_joined<NT>(of_keys, tile, u);
+    delta_joined<NT>(of_keys, tile, u, [&] { kf.load(); });
 #pragma unroll
     for (int n = 0; n < NT; ++n) for_inner.write(wave, n, of_inner[c & 1].v[wave][n][lane] + u[n] * steps.until);
     lds_barrier();
@@ -812,12 +862,12 @@ __global__ __launch_bounds__(512, 2) void delta_bwd_kernel(DeltaArgs s) {
       ttf.at -= ttf.hop;
       steps.at -= steps.hop;
     }
-    ttf.load(wave / 2);
-    steps.load(tile);
     lds_barrier();
-    delta_state<KT, NT>(for_state, ktf.v, state);
+    delta_state<KT, NT>(for_state, ktf.v, state, [&] {
+      ttf.load(wave / 2);
+      steps.load(tile);
+    });
     if (more) ktf.at -= ktf.hop;
-    ktf.load();
   }
   if (s.dh0) {
 #pragma unroll
@@ -1466,7 +1516,7 @@ static int delta_scratch(distdl_delta_plan* p, bool back, hipStream_t st, DeltaA
   struct Part {
     void** at;
     size_t bytes;
-  } parts[] = {{(void**)&s->kf, key}, {(void**)&s->ktf, key}, {(void**)&s->qf, back ? 0 : key}, {(void**)&s->qtf, back ? key : 0},
+  } parts[] = {{(void**)&s->kf, key}, {(void**)&s->ktf, back || !delta_turned<E>() ? key : 0}, {(void**)&s->qf, back ? 0 : key}, {(void**)&s->qtf, back ? key : 0},
                {(void**)&s->tf, step}, {(void**)&s->pf, back ? 0 : step / kInner * delta_rounded<E>()}, {(void**)&s->ttf, back ? step : 0}, {(void**)&s->ptf, back ? step : 0},
                {(void**)&s->tiles, back ? heads * 2 * Z::kLower * 1024 : 0}, {(void**)&s->steps, heads * kStepNumbers * C * 4}, {(void**)&s->states, back ? state : 0}, {(void**)&s->dstates, back ? state : 0},
                {(void**)&s->u, back ? rows : 0}, {(void**)&s->dr, back ? rows : 0}};
