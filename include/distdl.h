@@ -547,7 +547,7 @@ int distdl_scan_step(const void* a_dev, const void* x_dev, float* state_dev, int
  * numbers between (states, what a step adds) have 24 bits in every product;
  * of what bf16 tensors alone depend on, 16.
  * fwd and bwd keep what chunks of steps need in the plan's scratch, bwd two
- * states for each 64 steps (32 with fp32 tensors): calls and recorded graphs
+ * states for each 64 steps: calls and recorded graphs
  * of one plan and stream share it, they run one after another.
  * UNSUPPORTED: d_k from 129 on, n_h d_v from 2^22 on. */
 typedef struct distdl_delta_plan distdl_delta_plan;

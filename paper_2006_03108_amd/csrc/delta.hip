@@ -1619,7 +1619,7 @@ int distdl_delta_plan_create(distdl_delta_plan** out, int64_t n_b, int64_t T, in
   const int rc = delta_sizes("delta_plan_create", n_h, n_hk, d_k, d_v, scale, dtype);
   if (rc) return rc;
   if (T < P) return set_error(DISTDL_ERR_EMPTY_PARTITION, "delta: %lld steps over %d workers", (long long)T, P);
-  if (T >= int64_t(1) << 30 || n_b >= 1 << 20 || n_b * (T / kChunk + P) >= kMaxBlocks256 / n_hk / 2 || n_b * n_h * ((d_v + 15) / 16) >= kMaxBlocks256)
+  if (T >= int64_t(1) << 30 || n_b >= 1 << 20 || n_b * (T / kChunk + P) >= kMaxBlocks256 / n_hk / 2 || n_b * n_h * ((d_v + 15) / 16) >= kMaxBlocks256 / 2)
     return set_error(DISTDL_ERR_UNSUPPORTED, "delta: problem too large");
   return guarded([&]() -> int {
     std::unique_ptr<distdl_delta_plan> p(new distdl_delta_plan());

@@ -38,6 +38,7 @@ def test_plans():
     assert code(dd.distdl_delta_plan_create, 1, 1 << 31, 2, 1, 8, 8, 1, 1.0) == UNSUPPORTED
     assert code(dd.distdl_delta_plan_create, 1, 4, 1 << 12, 1, 8, 1 << 12, 1, 1.0) == UNSUPPORTED
     assert code(dd.distdl_delta_plan_create, 1, 4, 1 << 16, 1 << 16, 128, 1, 1, 1.0) == UNSUPPORTED
+    assert code(dd.distdl_delta_plan_create, 1 << 19, 1, 16, 1, 1, 16, 1, 1.0) == UNSUPPORTED  # 2^32 threads of a launch
     assert code(dd.distdl_delta_plan_create, 1, 4, 2, 1, 8, 8, 1, 1.0, torch.float16) == UNSUPPORTED
     assert code(dd.distdl_logits_plan_create, -1, 8, 1) == INVALID
     assert code(dd.distdl_logits_plan_create, 4, 0, 1) == INVALID
