@@ -158,6 +158,46 @@ __device__ __forceinline__ void logits_each(const LogitsArgs& s, int split, F f)
   }
 }
 
+// ---- lanes ----------------------------------------------------------------
+// The number of lane l ^ O (a power of two, or 63).  IN_REGISTERS: moved within the vector registers, which takes a tenth of the time of a way through LDS, but the
+// vector units': for rows that are cut, whose few waves wait for chains of moves (8 rows of 65536 with 20 alternatives: 17.8 -> 16.6 us).  Where waves are
+// many, they have enough to do besides (64 alternatives of 2048 rows of 131072: 223 us in registers, 211 through LDS).
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false);
+}
+template <int O>
+__device__ __forceinline__ uint32_t moved_lane(uint32_t v) {
+  if constexpr (O == 63) {
+    return moved_lane<32>(moved_lane<16>(moved<0x140>(v)));  // (rows of 16 lanes mirrored)
+  } else if constexpr (O == 32) {
+    const auto w = __builtin_amdgcn_permlane32_swap(v, v, false, false);  // the lower half's twice, the upper half's twice
+    return threadIdx.x & 32 ? w[0] : w[1];
+  } else if constexpr (O == 16) {
+    const auto w = __builtin_amdgcn_permlane16_swap(v, v, false, false);  // the even rows' twice, the odd rows' twice
+    return threadIdx.x & 16 ? w[0] : w[1];
+  } else {
+    static_assert(O == 8 || O == 4 || O == 2 || O == 1, "lanes of a row");
+    if constexpr (O == 8) return moved<0x128>(v);                    // rotated by 8
+    else if constexpr (O == 4) return moved<0x1b>(moved<0x141>(v));  // eights mirrored, then fours
+    else return moved<O == 2 ? 0x4e : 0xb1>(v);                      // within fours
+  }
+}
+template <int O, bool IN_REGISTERS>
+__device__ __forceinline__ uint32_t other_lane_bits(uint32_t v) {
+  if constexpr (IN_REGISTERS) return moved_lane<O>(v);
+  else return (uint32_t)__shfl_xor((int)v, O, 64);
+}
+template <int O, bool IN_REGISTERS, class T>
+__device__ __forceinline__ T other_lane(T v) {
+  if constexpr (sizeof(T) == 8) {
+    const uint32_t lo = other_lane_bits<O, IN_REGISTERS>((uint32_t)v), hi = other_lane_bits<O, IN_REGISTERS>((uint32_t)(v >> 32));
+    return (T)((uint64_t)hi << 32 | lo);
+  } else {
+    return __builtin_bit_cast(T, other_lane_bits<O, IN_REGISTERS>(__builtin_bit_cast(uint32_t, v)));
+  }
+}
+
 // ---- sums -----------------------------------------------------------------
 // Where the maximum is so far from 0 that m c may be no number (masks of the type's lowest value that leave nothing else), d is (x - m) c,
 // which costs an operation more and is 0 or out of exp2's range.
@@ -254,64 +294,59 @@ __device__ __forceinline__ float value_of(uint64_t key) {
   return __uint_as_float((uint32_t)(o ^ ((o >> 31) & 0x7fffffff)));
 }
 
-template <class T>
-__device__ __forceinline__ T other_lane(T v, int o) {
-  if constexpr (sizeof(T) == 8) {
-    const uint32_t lo = __shfl_xor((int)(uint32_t)v, o, 64), hi = __shfl_xor((int)(uint32_t)(v >> 32), o, 64);
-    return (T)((uint64_t)hi << 32 | lo);
-  } else {
-    return __shfl_xor(v, o, 64);
-  }
-}
-template <class T>
-__device__ __forceinline__ T turned_lanes(T v) { return other_lane(v, 63); }
 // the last rounds of a bitonic sort: a bitonic sequence of `n` lanes becomes a descending one where `down`, else ascending
-template <int N, class T>
+template <int N, bool IN_REGISTERS, class T>
 __device__ __forceinline__ T bitonic(T v, bool down) {
-#pragma unroll
-  for (int o = N / 2; o > 0; o >>= 1) {
-    const T u = other_lane(v, o);
-    const bool large = ((threadIdx.x & o) == 0) == down;
-    v = large == (u > v) ? u : v;
+  if constexpr (N > 1) {
+    constexpr int O = N / 2;
+    const T u = other_lane<O, IN_REGISTERS>(v);
+    const bool large = ((threadIdx.x & O) == 0) == down;
+    return bitonic<O, IN_REGISTERS>(large == (u > v) ? u : v, down);
+  } else {
+    return v;
   }
-  return v;
 }
-template <class T>
+template <bool IN_REGISTERS, class T>
 __device__ __forceinline__ T sorted_lanes(T v) {  // descending
-  v = bitonic<2>(v, (threadIdx.x & 2) == 0);
-  v = bitonic<4>(v, (threadIdx.x & 4) == 0);
-  v = bitonic<8>(v, (threadIdx.x & 8) == 0);
-  v = bitonic<16>(v, (threadIdx.x & 16) == 0);
-  v = bitonic<32>(v, (threadIdx.x & 32) == 0);
-  return bitonic<64>(v, true);
+  v = bitonic<2, IN_REGISTERS>(v, (threadIdx.x & 2) == 0);
+  v = bitonic<4, IN_REGISTERS>(v, (threadIdx.x & 4) == 0);
+  v = bitonic<8, IN_REGISTERS>(v, (threadIdx.x & 8) == 0);
+  v = bitonic<16, IN_REGISTERS>(v, (threadIdx.x & 16) == 0);
+  v = bitonic<32, IN_REGISTERS>(v, (threadIdx.x & 32) == 0);
+  return bitonic<64, IN_REGISTERS>(v, true);
 }
 // the 64 largest keys of two descending lists
+template <bool IN_REGISTERS>
 __device__ __forceinline__ uint64_t merged_lanes(uint64_t a, uint64_t b) {
-  b = turned_lanes(b);
-  return bitonic<64>(a > b ? a : b, true);
+  b = other_lane<63, IN_REGISTERS>(b);
+  return bitonic<64, IN_REGISTERS>(a > b ? a : b, true);
 }
 
 // `best` and `waiting` keys of a buffer in LDS.  (Out of line: it is rarely called, and the registers are the streaming loop's.)
 typedef __attribute__((address_space(3))) uint64_t* TopBuffer;
+template <bool FEW>
 __device__ __attribute__((noinline)) uint64_t top_flushed(uint64_t best, TopBuffer buffer, int waiting) {
   const int lane = threadIdx.x & 63;
   while (waiting > 0) {
     const int n = min(waiting, 64), from = waiting - n;
-    best = merged_lanes(best, sorted_lanes(lane < n ? (uint64_t)buffer[from + lane] : (uint64_t)0));
+    best = merged_lanes<FEW>(best, sorted_lanes<FEW>(lane < n ? (uint64_t)buffer[from + lane] : (uint64_t)0));
     waiting = from;
   }
   __builtin_amdgcn_wave_barrier();
   return best;
 }
-__device__ __attribute__((noinline)) int32_t top_nth(int32_t order, int n) { return __builtin_amdgcn_readlane(sorted_lanes(order), n - 1); }
+template <bool FEW>
+__device__ __attribute__((noinline)) int32_t top_nth(int32_t order, int n) { return __builtin_amdgcn_readlane(sorted_lanes<FEW>(order), n - 1); }
+
+constexpr int kTopRoom = 64 + 512;  // keys that wait: a vector of each lane beside less than 64
 
 // A wave's 64 best entries, descending over the lanes, and a buffer of those that wait.  Values at or below `floor`, the n-th best so far, can
-// not be among the n: a wave meets entries in the order of their places, so of equal values the first stay.  (A NaN, at first, lets all pass.)
+// not be among the n: a wave meets entries in the order of their places, so of equal values the first stay.  (A NaN, at first, lets all pass.)  FEW: rows are cut.
+template <bool FEW>
 struct TopList {
   uint64_t best = 0;
   float floor = NAN;
   int waiting = 0;
-  static constexpr int kRoom = 64 + 512;
   __device__ __forceinline__ bool passes(float v) const { return !(v <= floor); }
   __device__ __forceinline__ void set_floor(int n_top) {
     const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(best >> 32), n_top - 1);
@@ -320,12 +355,12 @@ struct TopList {
   }
   // From the largest of each lane's first entries: the n-th of them is no better than the n-th of all, and may be it.
   __device__ __forceinline__ void start(float most, int n_top) {
-    const int32_t nth = top_nth(order_of(most), n_top);
+    const int32_t nth = top_nth<FEW>(order_of(most), n_top);
     const int32_t below = nth == 0 ? order_of(-FLT_MIN) : nth - 1;  // (-0, which comes next, is no less than 0)
     if (nth > order_of(-INFINITY)) floor = __uint_as_float((uint32_t)(below ^ ((below >> 31) & 0x7fffffff)));
   }
   __device__ __forceinline__ void flush(uint64_t* buffer, int n_top) {
-    best = top_flushed(best, (TopBuffer)buffer, waiting);
+    best = top_flushed<FEW>(best, (TopBuffer)buffer, waiting);
     waiting = 0;
     set_floor(n_top);
   }
@@ -384,18 +419,18 @@ __device__ __forceinline__ void logits_finish(const LogitsArgs& s, int64_t row, 
 }
 
 // A row, or one of its splits, to a workgroup.
-template <class E, bool ENTROPY, bool TOP, bool TINY>
+template <class E, bool ENTROPY, bool TOP, bool FEW, bool TINY>
 __global__ __launch_bounds__(kLogitsThreads, 8) void logits_fwd_kernel(LogitsArgs s) {
   constexpr int B = logits_batch<E>() / (TOP ? 2 : 1);
   __shared__ float4 sums[kLogitsWaves];
-  __shared__ uint64_t buffers[TOP ? kLogitsWaves * TopList::kRoom : 1];
+  __shared__ uint64_t buffers[TOP ? kLogitsWaves * kTopRoom : 1];
   const LogitsTable table = LOGITS_TABLE(s);
   const int64_t row = blockIdx.x / (uint32_t)s.splits;
   const int split = blockIdx.x % (uint32_t)s.splits, tid = threadIdx.x, wave = tid >> 6;
-  uint64_t* const buffer = buffers + (TOP ? wave * TopList::kRoom : 0);
+  uint64_t* const buffer = buffers + (TOP ? wave * kTopRoom : 0);
   const float x_target = s.splits == 1 ? logits_target<E>(s, table, row) : 0.f;
   LogitsSums a;
-  TopList list;
+  TopList<FEW> list;
   bool first = true;
   typedef LogitsVector<E, TINY> Vector;
   if constexpr (TOP) {
@@ -471,7 +506,7 @@ __global__ __launch_bounds__(kLogitsThreads, 8) void logits_fwd_kernel(LogitsArg
   a.join_waves<kLogitsWaves>(sums, s.c);
   if constexpr (TOP) {
     if (wave == 0)
-      for (int i = 1; i < kLogitsWaves; ++i) list.best = merged_lanes(list.best, buffers[i * TopList::kRoom + tid]);
+      for (int i = 1; i < kLogitsWaves; ++i) list.best = merged_lanes<FEW>(list.best, buffers[i * kTopRoom + tid]);
   }
   if (s.splits == 1) {
     logits_finish(s, row, a, list.best, x_target);
@@ -502,18 +537,31 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_join_kernel(LogitsArgs 
   const LogitsTable table = LOGITS_TABLE(s);
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // The lists of four splits at a time, the first ones asked for before the sums are joined.
+  constexpr int N = 4;
+  uint64_t more[N];
+  auto load = [&](int first) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int split = first + i * kLogitsWaves;
+      more[i] = split < s.splits && lane < s.n_top ? s.part_top[(row * s.splits + split) * s.n_top + lane] : 0;
+    }
+  };
   const float x_target = logits_target<E>(s, table, row);
+  load(wave);
   const LogitsSums a = logits_joined<kLogitsThreads>(s, row, sums);
   uint64_t best = 0;
   if (s.n_top > 0) {
-    for (int i = wave; i < s.splits; i += kLogitsWaves) {
-      const uint64_t more = lane < s.n_top ? s.part_top[(row * s.splits + i) * s.n_top + lane] : 0;
-      best = merged_lanes(best, more);
+    for (int first = wave; first < s.splits; first += N * kLogitsWaves) {
+      if (first != wave) load(first);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (first + i * kLogitsWaves < s.splits) best = merged_lanes<true>(best, more[i]);
     }
     lists[tid] = best;
     __syncthreads();
     if (wave == 0)
-      for (int i = 1; i < kLogitsWaves; ++i) best = merged_lanes(best, lists[i * 64 + lane]);
+      for (int i = 1; i < kLogitsWaves; ++i) best = merged_lanes<true>(best, lists[i * 64 + lane]);
   }
   logits_finish(s, row, a, best, x_target);
 }
@@ -907,8 +955,9 @@ static int logits_aligned(const char* call, std::initializer_list<const void*> a
 template <class E, bool ENTROPY, bool TINY>
 static void launch_logits_fwd(const LogitsArgs& s, hipStream_t st) {
   const dim3 grid((unsigned)(s.rows * s.splits)), block(kLogitsThreads);
-  if (s.n_top > 0) hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, true, TINY>), grid, block, 0, st, s);
-  else hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, false, TINY>), grid, block, 0, st, s);
+  if (s.n_top > 0 && s.splits > 1) hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, true, true, TINY>), grid, block, 0, st, s);
+  else if (s.n_top > 0) hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, true, false, TINY>), grid, block, 0, st, s);
+  else hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, false, false, TINY>), grid, block, 0, st, s);
   if (s.splits > 1) hipLaunchKernelGGL((logits_join_kernel<E>), dim3((unsigned)s.rows), block, 0, st, s);
 }
 
