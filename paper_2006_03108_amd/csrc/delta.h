@@ -52,6 +52,7 @@ struct DeltaArgs {
   float* steps;                       // of each step: kStepNumbers of them, [C] each
   float *states, *dstates;            // [DK][dvp] at a chunk's start; the gradient at its end
   float *u, *dr;                      // [C][dvp]
+  float* keys;                        // parts of dq and dk, where a chunk's heads are workgroups of their own
 };
 
 static_assert(offsetof(DeltaArgs, w) == 0, "the kernels' first argument starts with the workers");

@@ -109,7 +109,7 @@ __device__ __forceinline__ DeltaLower delta_lower(int tile) {
   return DeltaLower{mt, tile - mt * (mt + 1) / 2};
 }
 
-// A workgroup has a chunk of a key's head and its heads, whose matrices have K K^T and Q K^T in common: these stay in registers.
+// A workgroup has a chunk of a key's head and its heads (or a share of them), whose matrices have K K^T and Q K^T in common: these stay in registers.
 template <class E, int C, int DK, bool BACK>
 __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
   typedef DeltaSizes<C, DK> Z;
@@ -120,7 +120,8 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
   const DeltaTable table = DELTA_TABLE(s);
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, row = lane & 15, g = lane >> 4;
   const int hk = blockIdx.x % (uint32_t)s.n_hk, at_chunk = blockIdx.x / (uint32_t)s.n_hk;
-  const int c = at_chunk % s.chunks, b = at_chunk / s.chunks;
+  const int c = at_chunk % s.chunks, b = at_chunk / s.chunks, share = blockIdx.y, shares = gridDim.y;
+  const int e_first = share * s.each / shares, e_end = (share + 1) * s.each / shares;
   const DeltaChunk at = delta_chunk(s, b, c);
   if (at.live == 0) return;  // nobody reads what would be here
   const int64_t step0 = (int64_t)b * at.steps + at.first;  // of the worker's arrays
@@ -128,7 +129,7 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
 
   // The sums of g for a head, by a wave.
   auto sum_up = [&](int e) {
-    if (wave >= Shared::kHeads || e + wave >= s.each) return;
+    if (wave >= Shared::kHeads || e + wave >= e_end) return;
     const int h = hk * s.each + e + wave;
     const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h;
     const bool live = lane < at.live;
@@ -161,7 +162,7 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
     const int i = tid + 256 * x, what = i / (C * (DK / 8)), t = i / (DK / 8) % C, col = i % (DK / 8) * 8;
     raw[x].load((const E*)(what ? w->q : w->k) + ((step0 + t) * s.n_hk + hk) * s.d_k + col, t < at.live ? min(8, s.d_k - col) : 0);
   }
-  sum_up(0);
+  sum_up(e_first);
 #pragma unroll
   for (int x = 0; x < kPieces; ++x) {
     const int i = tid + 256 * x, what = i / (C * (DK / 8)), t = i / (DK / 8) % C, col = i % (DK / 8) * 8;
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
 
   // their fragments
   const int64_t key = ((int64_t)b * s.chunks + c) * s.n_hk + hk, key_at = key * Z::kKeyPiece * NI;
-  for (int f = wave; f < (BACK ? 1 : 2) * Z::kTiles * Z::kKeySteps; f += 4) {  // (the adjoint needs no Q and no P as they are)
+  for (int f = wave + 4 * share; f < (BACK ? 1 : 2) * Z::kTiles * Z::kKeySteps; f += 4 * shares) {  // (the adjoint needs no Q and no P as they are)
     const int what = f / (Z::kTiles * Z::kKeySteps), i = f % (Z::kTiles * Z::kKeySteps), mt = i / Z::kKeySteps, ks = i % Z::kKeySteps;
     Pieces<NI> v;
 #pragma unroll
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
     }
     store_fragment((what ? s.qf : s.kf) + key_at + (int64_t)i * NI * kFragment, v);
   }
-  for (int f = wave; f < (BACK ? 2 : delta_turned<E>() ? 0 : 1) * Z::kKeyTiles * Z::kSteps; f += 4) {
+  for (int f = wave + 4 * share; f < (BACK ? 2 : delta_turned<E>() ? 0 : 1) * Z::kKeyTiles * Z::kSteps; f += 4 * shares) {
     const int what = f / (Z::kKeyTiles * Z::kSteps), i = f % (Z::kKeyTiles * Z::kSteps), mt = i / Z::kSteps, ts = i % Z::kSteps;
     Pieces<NI> v;
 #pragma unroll
@@ -221,11 +222,11 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
     }
   }
 
-  for (int e = 0; e < s.each; ++e) {
-    const int h = hk * s.each + e, slot = e % Shared::kHeads;
+  for (int e = e_first; e < e_end; ++e) {
+    const int h = hk * s.each + e, slot = (e - e_first) % Shared::kHeads;
     const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h;
     lds_barrier();
-    if (e > 0 && slot == 0) {
+    if (e > e_first && slot == 0) {
       sum_up(e);
       lds_barrier();
     }
@@ -923,9 +924,40 @@ __device__ __forceinline__ float sum16(float v) {  // over a row of 16 lanes
   return v + row_rotated<1>(v);
 }
 
+// Rows of the keys' gradients: a lane's key in step 16 mt0 + 4 g of the chunk, and steps behind it; what does not exist fails the checks.  `first`: the chunk's
+// first number in the arrays.
+template <class E, int N>
+__device__ __forceinline__ void delta_store_keys(const DeltaArgs& s, int64_t first, E* dq, E* dk, const DeltaChunk& at, int mt0, int key, const f32x4 (&sum_q)[N],
+                                                 const f32x4 (&sum_k)[N]) {
+  const int g = (threadIdx.x & 63) >> 4;
+  const uint32_t hop = (uint32_t)(s.n_hk * s.d_k) * (uint32_t)sizeof(E);
+  const uint32_t key_off = key < s.d_k ? (uint32_t)(mt0 * 16 + 4 * g) * hop + (uint32_t)key * (uint32_t)sizeof(E) : kOob;
+  auto key_rows = [&](E* array, int n) {
+    n = __builtin_amdgcn_readfirstlane(n);
+    return rsrc_of(array + first, (uint32_t)(n - 1) * hop + (uint32_t)s.d_k * (uint32_t)sizeof(E));
+  };
+  const __amdgpu_buffer_rsrc_t to_q = key_rows(dq, at.n), to_k = key_rows(dk, at.n);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const bool in = (mt0 + i) * 16 + 4 * g + r < at.live;
+      const uint32_t step_off = (uint32_t)(i * 16 + r) * hop;
+      const float q = in ? sum_q[i][r] : 0.f, k = in ? sum_k[i][r] : 0.f;
+      if constexpr (sizeof(E) == 4) {
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(q), to_q, key_off, step_off, 0);
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(k), to_k, key_off, step_off, 0);
+      } else {
+        __builtin_amdgcn_raw_buffer_store_b16(to_bf16(q), to_q, key_off, step_off, 0);
+        __builtin_amdgcn_raw_buffer_store_b16(to_bf16(k), to_k, key_off, step_off, 0);
+      }
+    }
+}
+
 // Bound by the time and the bytes of its loads (a compute unit holds one workgroup): a thread's part of the next 64 columns, of this head or of the next
 // one, is loaded into the registers that this one's have left.
-template <class E, int C, int DK>
+// SPLIT: few chunks, whose heads are workgroups of their own; delta_keys_kernel adds up what they leave.
+template <class E, int C, int DK, bool SPLIT>
 __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
   static_assert(C == 64, "two steps of a sum over steps");
   typedef DeltaSizes<C, DK> Z;
@@ -940,14 +972,17 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kt = kBoth ? wave & 3 : wave, mt0 = wave / Z::kKeyTiles * kMine;
   // Of M and N a wave has the tiles (mt, nt) of its rows mt, which it reads anyway, and one column nt <= mt (the two waves of a SIMD have about as many).
   const int wave_what = wave >> 2, nt = kBoth || wave_what == 0 ? wave & 3 : 3 - (wave & 3);
-  struct Item {  // a chunk of a key's head
+  struct Item {  // a chunk of a key's head, and which of its heads
     DeltaChunk at;
-    int hk;
+    int hk, first, end;
     int64_t step0, key0, head0;
     const E* d_o;
   };
   auto item_of = [&](int i) {
     Item x;
+    x.first = SPLIT ? i % (uint32_t)s.each : 0;
+    x.end = SPLIT ? x.first + 1 : s.each;
+    if (SPLIT) i /= (uint32_t)s.each;
     x.hk = i % (uint32_t)s.n_hk;
     const int at_chunk = i / (uint32_t)s.n_hk, c = at_chunk % s.chunks, b = at_chunk / s.chunks;
     x.at = delta_chunk(s, b, c);
@@ -1018,11 +1053,11 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
     return size;
   };
 
-  const int items = s.n_b * s.chunks * s.n_hk;
+  const int items = s.n_b * s.chunks * s.n_hk * (SPLIT ? s.each : 1);
   Item it = item_of(blockIdx.x);
   {
-    const uint32_t size = load_first(it, 0, true);
-    load_states(it, 0, size);
+    const uint32_t size = load_first(it, it.first, true);
+    load_states(it, it.first, size);
   }
   for (int i = blockIdx.x; i < items; i += gridDim.x) {
   const bool another = i + (int)gridDim.x < items;
@@ -1033,27 +1068,27 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
   const DeltaTable w = table + at.p;
   E* const dq = (E*)w->dq, * const dk = (E*)w->dk, * const dv = (E*)w->dv;
   if (at.live == 0) {
-    for (int i = tid; i < at.n * s.d_k; i += 64 * W) {
+    const int heads = it.end - it.first, columns = heads * s.d_v;
+    for (int i = tid; i < (it.first == 0 ? at.n * s.d_k : 0); i += 64 * W) {
       const int64_t o = ((step0 + i / s.d_k) * s.n_hk + hk) * s.d_k + i % s.d_k;
       st(dq, (size_t)o, 0.f);
       st(dk, (size_t)o, 0.f);
     }
-    const int columns = s.each * s.d_v;
     for (int64_t i = tid; i < (int64_t)at.n * columns; i += 64 * W)
-      st(dv, (size_t)(((step0 + i / columns) * s.n_h + hk * s.each) * s.d_v + i % columns), 0.f);
-    for (int i = tid; i < at.n * s.each; i += 64 * W) {
-      const int64_t o = (step0 + i / s.each) * s.n_h + hk * s.each + i % s.each;
+      st(dv, (size_t)(((step0 + i / columns) * s.n_h + hk * s.each + it.first) * s.d_v + i % columns), 0.f);
+    for (int i = tid; i < at.n * heads; i += 64 * W) {
+      const int64_t o = (step0 + i / heads) * s.n_h + hk * s.each + it.first + i % heads;
       if (w->dg) w->dg[o] = 0.f;
       w->dbeta[o] = 0.f;
     }
-    const uint32_t size = load_first(next, 0, another);
-    load_states(next, 0, size);
+    const uint32_t size = load_first(next, next.first, another);
+    load_states(next, next.first, size);
     it = next;
     continue;
   }
   const int64_t key_at = it.key0 * Z::kKeyPiece * NI;
   const uint16_t *const ktf = s.ktf + key_at, *const qtf = s.qtf + key_at;
-  for (int e = 0; e < s.each; ++e) {
+  for (int e = it.first; e < it.end; ++e) {
     // (What is made of the thread's number is made again for each head: kept, it would not fit the registers.)
     asm volatile("" : "+v"(tid));
     const int lane = tid & 63, row = lane & 15, g = lane >> 4, key = kt * 16 + row;
@@ -1225,9 +1260,9 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
       tiles_of(std::integral_constant<int, 0>(), 0, 4);
     }
     // the next columns: of the next head, or of another chunk
-    const bool last = e + 1 == s.each;
+    const bool last = e + 1 == it.end;
     const Item& then = last ? next : it;
-    const int then_e = last ? 0 : e + 1;
+    const int then_e = last ? next.first : e + 1;
     const uint32_t then_size = load_first(then, then_e, !last || another);
 #pragma unroll
     for (int x = 0; x < (kBoth ? 2 : 1); ++x) {
@@ -1319,6 +1354,15 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
         w->dbeta[o] = for_beta;
       }
     }
+    if constexpr (SPLIT) {
+      f32x4* const to = (f32x4*)s.keys + (head0 + e) * 2 * kMine * 512 + tid;
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        to[i * 512] = sum_q[i];
+        to[(kMine + i) * 512] = sum_k[i];
+      }
+      continue;
+    }
     if (e > 0) {
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
@@ -1334,32 +1378,32 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
       }
       continue;
     }
-    // rows of the keys' gradients: a lane's key in step 16 mt0 + 4 g of the chunk, and steps behind it; what does not exist fails the checks
-    const uint32_t hop = (uint32_t)(s.n_hk * s.d_k) * (uint32_t)sizeof(E);
-    const uint32_t key_off = key < s.d_k ? (uint32_t)(mt0 * 16 + 4 * g) * hop + (uint32_t)key * (uint32_t)sizeof(E) : kOob;
-    auto key_rows = [&](void* array, int n) {
-      n = __builtin_amdgcn_readfirstlane(n);
-      return rsrc_of((const E*)array + (step0 * s.n_hk + hk) * s.d_k, (uint32_t)(n - 1) * hop + (uint32_t)s.d_k * (uint32_t)sizeof(E));
-    };
-    const __amdgpu_buffer_rsrc_t to_q = key_rows(dq, at.n), to_k = key_rows(dk, at.n);
-#pragma unroll
-    for (int i = 0; i < kMine; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const bool in = (mt0 + i) * 16 + 4 * g + r < at.live;
-        const uint32_t step_off = (uint32_t)(i * 16 + r) * hop;
-        const float q = in ? sum_q[i][r] : 0.f, k = in ? sum_k[i][r] : 0.f;
-        if constexpr (sizeof(E) == 4) {
-          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(q), to_q, key_off, step_off, 0);
-          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(k), to_k, key_off, step_off, 0);
-        } else {
-          __builtin_amdgcn_raw_buffer_store_b16(to_bf16(q), to_q, key_off, step_off, 0);
-          __builtin_amdgcn_raw_buffer_store_b16(to_bf16(k), to_k, key_off, step_off, 0);
-        }
-      }
+    delta_store_keys<E>(s, (step0 * s.n_hk + hk) * s.d_k, dq, dk, at, mt0, key, sum_q, sum_k);
   }
   it = next;
   }
+}
+
+// dq and dk of a chunk of a key's head, whose heads' parts lie as the threads of delta_grad_kernel had them: added up in order.
+template <class E, int C, int DK>
+__global__ __launch_bounds__(512) void delta_keys_kernel(DeltaArgs s) {
+  constexpr int kKeyTiles = DK / 16, kMine = C / 16 * kKeyTiles / 8;
+  const DeltaTable table = DELTA_TABLE(s);
+  const int hk = blockIdx.x % (uint32_t)s.n_hk, at_chunk = blockIdx.x / (uint32_t)s.n_hk, c = at_chunk % s.chunks, b = at_chunk / s.chunks;
+  const DeltaChunk at = delta_chunk(s, b, c);
+  if (at.live == 0) return;  // (zeros are there)
+  const int tid = threadIdx.x, wave = tid >> 6, kt = kMine == 2 ? wave & 3 : wave, mt0 = wave / kKeyTiles * kMine;
+  const f32x4* from = (const f32x4*)s.keys + (int64_t)blockIdx.x * s.each * 2 * kMine * 512 + tid;
+  f32x4 sum_q[kMine] = {}, sum_k[kMine] = {};
+  for (int e = 0; e < s.each; ++e, from += 2 * kMine * 512) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      sum_q[i] += from[i * 512];
+      sum_k[i] += from[(kMine + i) * 512];
+    }
+  }
+  const int64_t step0 = (int64_t)b * at.steps + at.first;
+  delta_store_keys<E>(s, (step0 * s.n_hk + hk) * s.d_k, (E*)table[at.p].dq, (E*)table[at.p].dk, at, mt0, kt * 16 + (tid & 15), sum_q, sum_k);
 }
 
 // ---- single tokens --------------------------------------------------------
@@ -1505,6 +1549,10 @@ static int delta_args(distdl_delta_plan* p, const std::vector<DeltaWorker>& w, h
   return DISTDL_OK;
 }
 
+// Whether the heads of a chunk's keys are workgroups of their own for its gradients: where the chunks leave half of the compute units without work.  54 chunks of
+// keys with three heads, fp32: 45 us one head behind the other, 19 and 4 for their sum; a round of workgroups more than that would cost what it gives.
+static bool delta_heads_apart(size_t chunks, int each) { return each > 1 && chunks <= 128; }
+
 // The scratch of a call, one array behind the other at multiples of 256 bytes.
 template <class E, int DK>
 static int delta_scratch(distdl_delta_plan* p, bool back, hipStream_t st, DeltaArgs* s) {
@@ -1519,7 +1567,8 @@ static int delta_scratch(distdl_delta_plan* p, bool back, hipStream_t st, DeltaA
   } parts[] = {{(void**)&s->kf, key}, {(void**)&s->ktf, back || !delta_turned<E>() ? key : 0}, {(void**)&s->qf, back ? 0 : key}, {(void**)&s->qtf, back ? key : 0},
                {(void**)&s->tf, step}, {(void**)&s->pf, back ? 0 : step / kInner * delta_rounded<E>()}, {(void**)&s->ttf, back ? step : 0}, {(void**)&s->ptf, back ? step : 0},
                {(void**)&s->tiles, back ? heads * 2 * Z::kLower * 1024 : 0}, {(void**)&s->steps, heads * kStepNumbers * C * 4}, {(void**)&s->states, back ? state : 0}, {(void**)&s->dstates, back ? state : 0},
-               {(void**)&s->u, back ? rows : 0}, {(void**)&s->dr, back ? rows : 0}};
+               {(void**)&s->u, back ? rows : 0}, {(void**)&s->dr, back ? rows : 0},
+               {(void**)&s->keys, back && delta_heads_apart(keys, s->each) ? heads * 2 * C * DK * 4 : 0}};
   size_t all = 0;
   for (const Part& v : parts) all += (v.bytes + 255) / 256 * 256;
   bool is_new = true;
@@ -1549,7 +1598,10 @@ static int launch_delta(distdl_delta_plan* p, DeltaArgs& s, hipStream_t st) {
   constexpr auto prepare = delta_prepare_kernel<E, C, DK, BACK>;
   if ((rc = allow_large_lds<prepare>())) return rc;
   const dim3 chunks((unsigned)((int64_t)s.n_b * s.chunks * s.n_hk));
-  hipLaunchKernelGGL(prepare, chunks, dim3(256), sizeof(DeltaPrepareShared<E, C, DK>), st, s);
+  // A key's heads are shared out among workgroups that still fit one to a compute unit (54 chunks of keys with three heads, fp32, adjoint: 24 -> 14 us; more
+  // than that make K K^T again for nothing, 135 chunks with two heads, fp32: 23 -> 28).
+  const unsigned shares = std::min((unsigned)s.each, std::max(1u, 256u / chunks.x));
+  hipLaunchKernelGGL(prepare, dim3(chunks.x, shares), dim3(256), sizeof(DeltaPrepareShared<E, C, DK>), st, s);
   // A workgroup, of which a compute unit holds one, takes 32 columns where those of 16 would be more than a round.
   const int64_t chains = (int64_t)s.n_b * s.n_h;
   const bool two = s.d_v > 16 && chains * ((s.d_v + 15) / 16) > 256;
@@ -1560,9 +1612,16 @@ static int launch_delta(distdl_delta_plan* p, DeltaArgs& s, hipStream_t st) {
   if constexpr (BACK) {
     if (two) hipLaunchKernelGGL((delta_bwd_kernel<E, DK, 2>), groups, dim3(512), 0, st, s);
     else hipLaunchKernelGGL((delta_bwd_kernel<E, DK, 1>), groups, dim3(512), 0, st, s);
-    constexpr auto grad = delta_grad_kernel<E, C, DK>;
-    if ((rc = allow_large_lds<grad>())) return rc;
-    hipLaunchKernelGGL(grad, dim3(std::min(chunks.x, 256u)), dim3(512), sizeof(DeltaGradShared<E, C, DK>), st, s);
+    if (s.keys) {
+      constexpr auto grad = delta_grad_kernel<E, C, DK, true>;
+      if ((rc = allow_large_lds<grad>())) return rc;
+      hipLaunchKernelGGL(grad, dim3(std::min(chunks.x * s.each, 256u)), dim3(512), sizeof(DeltaGradShared<E, C, DK>), st, s);
+      hipLaunchKernelGGL((delta_keys_kernel<E, C, DK>), chunks, dim3(512), 0, st, s);
+    } else {
+      constexpr auto grad = delta_grad_kernel<E, C, DK, false>;
+      if ((rc = allow_large_lds<grad>())) return rc;
+      hipLaunchKernelGGL(grad, dim3(std::min(chunks.x, 256u)), dim3(512), sizeof(DeltaGradShared<E, C, DK>), st, s);
+    }
   }
   return DISTDL_OK;
 }

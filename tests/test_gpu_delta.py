@@ -138,6 +138,15 @@ def test_many_chains_take_two_tiles_of_columns():
         check(make(4, 70, 256, 64, 32, 40, dtype, 3), lengths_of(4, 70, 3), 2)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [(33, 70, 6, 2, 24, 20, 2), (65, 40, 4, 2, 100, 40, 1)])
+def test_heads_of_many_chunks_are_added_up_in_one_workgroup(size, dtype):
+    """More chunks of keys than 128, each with several heads (the sizes above have few, whose heads are workgroups of their own)."""
+    require_gpu()
+    n_b, T, n_h, n_hk, d_k, d_v, parts = size
+    check(make(n_b, T, n_h, n_hk, d_k, d_v, dtype, seed=5), lengths_of(n_b, T, 5), parts)
+
+
 def test_lengths_out_of_range_are_cut():
     require_gpu()
     x = make(3, 50, 2, 1, 32, 32, F32, 4)
