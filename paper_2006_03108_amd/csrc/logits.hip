@@ -239,6 +239,7 @@ struct LogitsSums {
   template <int WAVES>
   __device__ __forceinline__ void join_waves(float4* shared, float c) {
     join_lanes(c);
+    if (WAVES == 1) return;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = make_float4(m, mc, s, w);
     __syncthreads();
@@ -418,12 +419,12 @@ __device__ __forceinline__ void logits_finish(const LogitsArgs& s, int64_t row, 
   }
 }
 
-// A row, or one of its splits, to a workgroup.
-template <class E, bool ENTROPY, bool TOP, bool FEW, bool TINY>
-__global__ __launch_bounds__(kLogitsThreads, 8) void logits_fwd_kernel(LogitsArgs s) {
-  constexpr int B = logits_batch<E>() / (TOP ? 2 : 1);
-  __shared__ float4 sums[kLogitsWaves];
-  __shared__ uint64_t buffers[TOP ? kLogitsWaves * kTopRoom : 1];
+// A row, or one of its splits, to a workgroup.  THREADS: 64 for short rows, whose waves have nothing to join.
+template <class E, bool ENTROPY, bool TOP, bool FEW, bool TINY, int THREADS>
+__global__ __launch_bounds__(THREADS, 8) void logits_fwd_kernel(LogitsArgs s) {
+  constexpr int B = logits_batch<E>() / (TOP ? 2 : 1), kWaves = THREADS / 64;
+  __shared__ float4 sums[kWaves];
+  __shared__ uint64_t buffers[TOP ? kWaves * kTopRoom : 1];
   const LogitsTable table = LOGITS_TABLE(s);
   const int64_t row = blockIdx.x / (uint32_t)s.splits;
   const int split = blockIdx.x % (uint32_t)s.splits, tid = threadIdx.x, wave = tid >> 6;
@@ -443,19 +444,19 @@ __global__ __launch_bounds__(kLogitsThreads, 8) void logits_fwd_kernel(LogitsArg
       const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
       Vector next[B];
 #pragma unroll
-      for (int b = 0; b < B; ++b) next[b].load(x, p.n, from + tid + b * kLogitsThreads);
-      for (int base = from; base < to; base += B * kLogitsThreads) {
-        const int v0 = base + tid, end = base + B * kLogitsThreads;
+      for (int b = 0; b < B; ++b) next[b].load(x, p.n, from + tid + b * THREADS);
+      for (int base = from; base < to; base += B * THREADS) {
+        const int v0 = base + tid, end = base + B * THREADS;
         Vector v[B];
 #pragma unroll
         for (int b = 0; b < B; ++b) {
           v[b] = next[b];
-          next[b].load(x, p.n, v0 + (b + B) * kLogitsThreads);
+          next[b].load(x, p.n, v0 + (b + B) * THREADS);
         }
         float f[B * 8], most[B], all = -INFINITY;
 #pragma unroll
         for (int b = 0; b < B; ++b) {
-          v[b].values(f + 8 * b, p.n, v0 + b * kLogitsThreads, to, end > to, p.n % 8 != 0 && end >= p.vecs);
+          v[b].values(f + 8 * b, p.n, v0 + b * THREADS, to, end > to, p.n % 8 != 0 && end >= p.vecs);
           most[b] = max8(f + 8 * b);
           all = fmaxf(all, most[b]);
         }
@@ -477,23 +478,23 @@ __global__ __launch_bounds__(kLogitsThreads, 8) void logits_fwd_kernel(LogitsArg
               for (int i = 0; i < 8; ++i) g[i] = b == c ? f[8 * c + i] : g[i];
               of = b == c ? most[c] : of;
             }
-            const int i = v0 + b * kLogitsThreads;
+            const int i = v0 + b * THREADS;
             list.take(buffer, g, of, p.first + Vector::place(p.n, i), i < to ? Vector::first_of(p.n, i) : 8, p.n, s.n_top);
           }
         }
       }
     }
   } else {
-    logits_each<B, kLogitsThreads>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
+    logits_each<B, THREADS>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
       const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
       Vector v[B];
       float f[B * 8], all = -INFINITY;
-      const int v0 = base + tid, end = base + B * kLogitsThreads;
+      const int v0 = base + tid, end = base + B * THREADS;
 #pragma unroll
-      for (int b = 0; b < B; ++b) v[b].load(x, p.n, v0 + b * kLogitsThreads);
+      for (int b = 0; b < B; ++b) v[b].load(x, p.n, v0 + b * THREADS);
 #pragma unroll
       for (int b = 0; b < B; ++b) {
-        v[b].values(f + 8 * b, p.n, v0 + b * kLogitsThreads, to, end > to, p.n % 8 != 0 && end >= p.vecs);
+        v[b].values(f + 8 * b, p.n, v0 + b * THREADS, to, end > to, p.n % 8 != 0 && end >= p.vecs);
         all = fmaxf(all, max8(f + 8 * b));
       }
       logits_add<B * 8, ENTROPY>(a, f, all, s.c);
@@ -503,10 +504,10 @@ __global__ __launch_bounds__(kLogitsThreads, 8) void logits_fwd_kernel(LogitsArg
     list.flush(buffer, s.n_top);
     buffer[tid & 63] = list.best;
   }
-  a.join_waves<kLogitsWaves>(sums, s.c);
+  a.template join_waves<kWaves>(sums, s.c);
   if constexpr (TOP) {
     if (wave == 0)
-      for (int i = 1; i < kLogitsWaves; ++i) list.best = merged_lanes<FEW>(list.best, buffers[i * kTopRoom + tid]);
+      for (int i = 1; i < kWaves; ++i) list.best = merged_lanes<FEW>(list.best, buffers[i * kTopRoom + tid]);
   }
   if (s.splits == 1) {
     logits_finish(s, row, a, list.best, x_target);
@@ -578,8 +579,8 @@ __device__ __forceinline__ void logits_store(E* row, const float* f, int at, int
   }
 }
 
-template <class E, bool ENTROPY, bool TINY>
-__global__ __launch_bounds__(kLogitsThreads) void logits_bwd_kernel(LogitsArgs s) {
+template <class E, bool ENTROPY, bool TINY, int THREADS>
+__global__ __launch_bounds__(THREADS) void logits_bwd_kernel(LogitsArgs s) {
   constexpr int B = logits_batch<E>();
   const LogitsTable table = LOGITS_TABLE(s);
   const int64_t row = blockIdx.x / (uint32_t)s.splits;
@@ -592,20 +593,20 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_bwd_kernel(LogitsArgs s
   const bool nothing = (weight == 0.f && back == 0.f) || lse < -kFar;  // such rows are not read
   const bool far = lse >= kFar;
   const float lc = lse * (1.f / kLn2), at_target = weight * s.inv_t;
-  logits_each<B, kLogitsThreads>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
+  logits_each<B, THREADS>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
     const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
     E* const dx = (E*)table[j].dx + row * p.n;
     typedef LogitsVector<E, TINY> Vector;
     Vector v[B];
-    const bool edge = base + B * kLogitsThreads >= to;  // (a last vector, or none)
+    const bool edge = base + B * THREADS >= to;  // (a last vector, or none)
     if (!nothing) {
 #pragma unroll
-      for (int b = 0; b < B; ++b) v[b].load(x, p.n, base + b * kLogitsThreads + tid);
+      for (int b = 0; b < B; ++b) v[b].load(x, p.n, base + b * THREADS + tid);
     }
 #pragma unroll
     for (int b = 0; b < B; ++b) {
       float f[8] = {};
-      const int i0 = base + b * kLogitsThreads + tid;
+      const int i0 = base + b * THREADS + tid;
       const int at = Vector::place(p.n, i0), from = i0 < to ? Vector::first_of(p.n, i0) : 8;
       if (!nothing) {
         v[b].values(f, p.n, i0, to, false, false);
@@ -952,18 +953,46 @@ static int logits_aligned(const char* call, std::initializer_list<const void*> a
   return DISTDL_OK;
 }
 
+// Rounds of `threads` threads with `batch` vectors each over a row.
+static int64_t logits_rounds(const LogitsArgs& s, int threads, int batch) {
+  const int64_t each = (int64_t)threads * batch, wide = (s.vec_wide + each - 1) / each, rest = (s.vec_rest + each - 1) / each;
+  return s.extra * wide + (s.P - s.extra) * rest;
+}
+// Whether a row is one wave's: nothing to join, and where a worker's part is short, no waves without work.  us for 8192 rows, bf16, workgroup / wave:
+//   sums                   8192 entries on 1 worker 31 / 26, 16384 on 1 52 / 54, 16384 on 8 140 / 52
+//   with 20 alternatives   512 on 1 52 / 19, 16384 on 1 146 / 103 (600 rows: 1024 on 1 12.6 / 9.9, 8192 on 1 18 / 29)
+//   adjoint                4096 on 1 32 / 27, 8192 on 1 52 / 57, 2048 on 8 203 / 61
+//   distillation           4096 on 1 62 / 48, 8192 on 1 88 / 91, 16384 on 8 143 / 166
+static bool logits_wave_sums(const LogitsArgs& s, int batch) {
+  return s.splits == 1 && logits_rounds(s, 64, batch) <= std::max<int64_t>(4, 2 * logits_rounds(s, kLogitsThreads, batch));
+}
+static int64_t logits_vectors(const LogitsArgs& s) { return s.extra * s.vec_wide + (int64_t)(s.P - s.extra) * s.vec_rest; }
+// (at most 512 numbers of a lane one behind the other in a sum, as a workgroup has of 131072)
+static bool logits_wave_top(const LogitsArgs& s) { return s.splits == 1 && logits_vectors(s) <= (s.rows >= 4096 ? 4096 : 256); }
+static bool logits_wave_adjoint(const LogitsArgs& s, int batch) {
+  return s.splits == 1 && logits_rounds(s, 64, batch) <= 2 * logits_rounds(s, kLogitsThreads, batch);
+}
+static bool logits_wave_distill(const LogitsArgs& s, int batch) { return s.splits == 1 && logits_vectors(s) <= 128 * batch; }
+
 template <class E, bool ENTROPY, bool TINY>
 static void launch_logits_fwd(const LogitsArgs& s, hipStream_t st) {
   const dim3 grid((unsigned)(s.rows * s.splits)), block(kLogitsThreads);
-  if (s.n_top > 0 && s.splits > 1) hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, true, true, TINY>), grid, block, 0, st, s);
-  else if (s.n_top > 0) hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, true, false, TINY>), grid, block, 0, st, s);
-  else hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, false, false, TINY>), grid, block, 0, st, s);
+  if (s.n_top > 0) {
+    if (logits_wave_top(s)) hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, true, false, TINY, 64>), grid, dim3(64), 0, st, s);
+    else if (s.splits > 1) hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, true, true, TINY, kLogitsThreads>), grid, block, 0, st, s);
+    else hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, true, false, TINY, kLogitsThreads>), grid, block, 0, st, s);
+  } else {
+    if (logits_wave_sums(s, logits_batch<E>())) hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, false, false, TINY, 64>), grid, dim3(64), 0, st, s);
+    else hipLaunchKernelGGL((logits_fwd_kernel<E, ENTROPY, false, false, TINY, kLogitsThreads>), grid, block, 0, st, s);
+  }
   if (s.splits > 1) hipLaunchKernelGGL((logits_join_kernel<E>), dim3((unsigned)s.rows), block, 0, st, s);
 }
 
 template <class E, bool ENTROPY, bool TINY>
 static void launch_logits_bwd(const LogitsArgs& s, hipStream_t st) {
-  hipLaunchKernelGGL((logits_bwd_kernel<E, ENTROPY, TINY>), dim3((unsigned)(s.rows * s.splits)), dim3(kLogitsThreads), 0, st, s);
+  const dim3 grid((unsigned)(s.rows * s.splits));
+  if (logits_wave_adjoint(s, logits_batch<E>())) hipLaunchKernelGGL((logits_bwd_kernel<E, ENTROPY, TINY, 64>), grid, dim3(64), 0, st, s);
+  else hipLaunchKernelGGL((logits_bwd_kernel<E, ENTROPY, TINY, kLogitsThreads>), grid, dim3(kLogitsThreads), 0, st, s);
 }
 
 // Threads of a workgroup that keeps a row in its registers; 0: none does.
@@ -979,6 +1008,10 @@ static int distill_threads(const LogitsArgs& s, int slots) {
 template <class E, bool TINY>
 static void launch_distill(const LogitsArgs& s, bool gradient, hipStream_t st) {
   const dim3 grid((unsigned)(s.rows * s.splits)), block(kLogitsThreads);
+  if (logits_wave_distill(s, logits_batch<E>())) {
+    hipLaunchKernelGGL((distill_kernel<E, false, TINY, 64>), grid, dim3(64), 0, st, s);
+    return;
+  }
   const int kept = s.splits == 1 && gradient ? distill_threads(s, distill_slots<E>()) : 0;
   if (kept == 256) hipLaunchKernelGGL((distill_kept_kernel<E, 256>), grid, dim3(256), 0, st, s);
   else if (kept == 512) hipLaunchKernelGGL((distill_kept_kernel<E, 512>), grid, dim3(512), 0, st, s);
