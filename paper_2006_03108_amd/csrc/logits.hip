@@ -806,7 +806,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(LogitsArgs s) {
 }
 
 // Rows that fit a workgroup's registers (up to 65536 entries of bf16, 32768 of fp32) are read once.  Slot by slot: a slot has a vector for each thread, of one
-// worker.  Longer ones would leave a compute unit one workgroup, which reads, computes and writes in turn: 4096 x 131072, bf16, 648 us that way, 640 us read
+// worker.  Longer ones would leave a compute unit one workgroup, which reads, computes and writes in turn: 4096 x 131072, bf16, 648 us that way, 483 us read
 // twice.
 template <class E>
 constexpr int distill_slots() { return sizeof(E) == 2 ? 16 : 8; }
