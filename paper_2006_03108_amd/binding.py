@@ -724,13 +724,18 @@ def distdl_delta_bwd(plan, q, k, v, g, beta, h0, lengths, do, dhT, dq, dk, dv, d
 def distdl_delta_step(q, k, v, g, beta, state, slots, o, scale):
     """q, k: [rows, n_hk, d_k], v, o: [rows, n_h, d_v]; g (or None), beta: fp32 [rows, n_h]; state: fp32 [n_slots, n_h, d_k, d_v]; slots: int32
     [rows], or None for state i of row i."""
-    if q.dim() != 3 or v.dim() != 3 or state.dim() != 4 or q.shape[0] != v.shape[0] or state.shape[1:] != (v.shape[1], q.shape[2], v.shape[2]):
+    try:
+        (rows, n_hk, d_k), (rows_v, n_h, d_v), (n_slots, *of_state) = q.shape, v.shape, state.shape
+        fits = rows_v == rows and of_state == [n_h, d_k, d_v]
+    except ValueError:
+        fits = False
+    if not fits:
         raise DistdlError(ERR_INVALID_ARG, f"delta_step: queries of shape {tuple(q.shape)}, values of shape {tuple(v.shape)}, "
                                            f"states of shape {tuple(state.shape)}")
-    (rows, n_hk, d_k), (_, n_h, d_v), kind = q.shape, v.shape, (q.dtype,)
+    kind = (q.dtype,)
     _check(lib.distdl_delta_step(_one("q", q, kind, q.numel()), _one("k", k, kind, q.numel()), _one("v", v, kind, v.numel()),
                                  _maybe("g", g, _F32, rows * n_h), _one("beta", beta, _F32, rows * n_h), _one("state", state, _F32, state.numel()),
-                                 state.shape[0], _maybe("slots", slots, _I32, rows), _one("o", o, kind, v.numel()), rows, n_h, n_hk, d_k, d_v, scale,
+                                 n_slots, _maybe("slots", slots, _I32, rows), _one("o", o, kind, v.numel()), rows, n_h, n_hk, d_k, d_v, scale,
                                  _dtype_code(q.dtype), _stream()))
 
 

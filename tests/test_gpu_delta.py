@@ -139,9 +139,10 @@ def test_many_chains_take_two_tiles_of_columns():
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("size", [(33, 70, 6, 2, 24, 20, 2), (65, 40, 4, 2, 100, 40, 1)])
-def test_heads_of_many_chunks_are_added_up_in_one_workgroup(size, dtype):
-    """More chunks of keys than 128, each with several heads (the sizes above have few, whose heads are workgroups of their own)."""
+@pytest.mark.parametrize("size", [(33, 70, 6, 2, 24, 20, 2), (65, 40, 4, 2, 100, 40, 1), (2, 70, 140, 1, 20, 16, 1)])
+def test_heads_of_many_chunks_and_many_heads_of_few(size, dtype):
+    """More chunks of keys than 128, each with several heads, which one workgroup adds up; and few with more heads than there are workgroups for them (the sizes above
+    have few of both)."""
     require_gpu()
     n_b, T, n_h, n_hk, d_k, d_v, parts = size
     check(make(n_b, T, n_h, n_hk, d_k, d_v, dtype, seed=5), lengths_of(n_b, T, 5), parts)
