@@ -623,12 +623,19 @@ __global__ __launch_bounds__(THREADS) void logits_bwd_kernel(LogitsArgs s) {
 }
 
 // ---- divergence from a teacher's top logits -------------------------------
-struct Stored {
-  int32_t id[kStoredMost];
-  float p[kStoredMost];  // the teacher's probabilities
-  float x[kStoredMost];  // the student's logits
+constexpr int kStoredFew = 64;
+template <int N>
+struct Stored {  // a row's, N at most
+  static constexpr int kTable = N > kStoredFew ? 2 * N : 1;
+  int32_t id[N];
+  float p[N];  // the teacher's probabilities
+  float x[N];  // the student's logits
   float red[16];
+  int32_t table[kTable], twice;
 };
+// One to a lane where a wave has the row.
+template <int THREADS>
+constexpr int stored_most() { return THREADS == 64 ? kStoredFew : kStoredMost; }
 template <int WAVES>
 __device__ __forceinline__ float group_max(float v, float* red) {
 #pragma unroll
@@ -653,8 +660,8 @@ __device__ __forceinline__ float group_sum(float v, float* red) {
   return v;
 }
 // The teacher's probabilities of a row: false if it has stored nothing.  total: log2 of their sum relative to `most`.
-template <int THREADS>
-__device__ __forceinline__ bool stored_load(const LogitsArgs& s, int64_t row, Stored& t, float& mc, float& total) {
+template <int THREADS, int N>
+__device__ __forceinline__ bool stored_load(const LogitsArgs& s, int64_t row, Stored<N>& t, float& mc, float& total) {
   float most = -INFINITY;
   bool odd = false;
   for (int k = threadIdx.x; k < s.n_top; k += THREADS) {
@@ -676,8 +683,8 @@ __device__ __forceinline__ bool stored_load(const LogitsArgs& s, int64_t row, St
   return true;
 }
 // The row's loss, and the teacher's logits in t.p become probabilities.  a, stotal: the student's.
-template <int THREADS>
-__device__ __forceinline__ float stored_loss(const LogitsArgs& s, Stored& t, float mc, float total, const LogitsSums& a, float stotal) {
+template <int THREADS, int N>
+__device__ __forceinline__ float stored_loss(const LogitsArgs& s, Stored<N>& t, float mc, float total, const LogitsSums& a, float stotal) {
   float loss = 0.f;
   const float inv = __builtin_amdgcn_exp2f(-total);
   for (int k = threadIdx.x; k < s.n_top; k += THREADS) {
@@ -688,10 +695,35 @@ __device__ __forceinline__ float stored_loss(const LogitsArgs& s, Stored& t, flo
   return kLn2 * group_sum<THREADS / 64>(loss, t.red);
 }
 
-// The teacher's places among a split's vectors lo .. hi - 1 are written once more.  off: log2 of the sum, and its reference.
-template <class E, int THREADS>
-__device__ __forceinline__ void stored_places(const LogitsArgs& s, LogitsTable table, int64_t row, const Stored& t, const LogitsSums& a, float stotal, float scale,
+// Whether a place comes twice: they go into a table of twice their number, by a hash of the place.  (All threads of the workgroup.)
+template <int THREADS, int N>
+__device__ __forceinline__ bool stored_twice(const LogitsArgs& s, Stored<N>& t) {
+  const int bits = 32 - __builtin_clz((uint32_t)(2 * s.n_top - 1));  // (n_top is above 1)
+  for (int i = threadIdx.x; i < 1 << bits; i += THREADS) t.table[i] = -1;
+  if (threadIdx.x == 0) t.twice = 0;
+  __syncthreads();
+  for (int k = threadIdx.x; k < s.n_top; k += THREADS) {
+    const int id = t.id[k];
+    if (id < 0) continue;
+    for (uint32_t at = (uint32_t)id * 2654435769u >> (32 - bits);; at = (at + 1) & ((1u << bits) - 1)) {  // (half of the table stays free)
+      const int before = atomicCAS(&t.table[at], -1, id);
+      if (before == id) t.twice = 1;
+      if (before == -1 || before == id) break;
+    }
+  }
+  __syncthreads();
+  return t.twice != 0;
+}
+
+// The teacher's places among a split's vectors lo .. hi - 1 are written once more.  off: log2 of the sum, and its reference.  Looking through all of a row's places for
+// each of them is left for rows where one comes twice: 8192 x 1024 with 256 places, bf16, 167 us else.
+template <class E, int THREADS, int N>
+__device__ __forceinline__ void stored_places(const LogitsArgs& s, LogitsTable table, int64_t row, Stored<N>& t, const LogitsSums& a, float stotal, float scale,
                                               int lo, int hi) {
+  bool search = true;
+  if constexpr (N > kStoredFew) {
+    if (s.n_top > kStoredFew) search = stored_twice<THREADS>(s, t);
+  }
   for (int k = threadIdx.x; k < s.n_top; k += THREADS) {
     const int id = t.id[k];
     if (id < 0) continue;
@@ -700,8 +732,8 @@ __device__ __forceinline__ void stored_places(const LogitsArgs& s, LogitsTable t
     const int v = p.vec0 + (id - p.first) / 8;
     if (v < lo || v >= hi) continue;
     bool is_first = true;
-    float sum = 0.f;
-    for (int i = 0; i < s.n_top; ++i) {  // (a place that is stored twice has the sum, and its first one writes it)
+    float sum = search ? 0.f : t.p[k];
+    for (int i = 0; search && i < s.n_top; ++i) {  // (a place that is stored twice has the sum, and its first one writes it)
       const bool same = t.id[i] == id;
       sum += same ? t.p[i] : 0.f;
       if (same && i < k) is_first = false;
@@ -716,7 +748,7 @@ template <class E, bool FIRST, bool TINY, int THREADS>
 __global__ __launch_bounds__(THREADS) void distill_kernel(LogitsArgs s) {
   constexpr int B = logits_batch<E>();
   __shared__ float4 sums[THREADS / 64];
-  __shared__ Stored t;
+  __shared__ Stored<stored_most<THREADS>()> t;
   const LogitsTable table = LOGITS_TABLE(s);
   const int64_t row = blockIdx.x / (uint32_t)s.splits;
   const int split = blockIdx.x % (uint32_t)s.splits, tid = threadIdx.x;
@@ -815,7 +847,7 @@ __global__ __launch_bounds__(THREADS) void distill_kept_kernel(LogitsArgs s) {
   constexpr int S = distill_slots<E>();
   typedef LogitsVector<E, false> Vector;
   __shared__ float4 sums[THREADS / 64];
-  __shared__ Stored t;
+  __shared__ Stored<kStoredMost> t;
   const LogitsTable table = LOGITS_TABLE(s);
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x;
@@ -972,7 +1004,7 @@ static bool logits_wave_top(const LogitsArgs& s) { return s.splits == 1 && logit
 static bool logits_wave_adjoint(const LogitsArgs& s, int batch) {
   return s.splits == 1 && logits_rounds(s, 64, batch) <= 2 * logits_rounds(s, kLogitsThreads, batch);
 }
-static bool logits_wave_distill(const LogitsArgs& s, int batch) { return s.splits == 1 && logits_vectors(s) <= 128 * batch; }
+static bool logits_wave_distill(const LogitsArgs& s, int batch) { return s.splits == 1 && logits_vectors(s) <= 128 * batch && s.n_top <= kStoredFew; }
 
 template <class E, bool ENTROPY, bool TINY>
 static void launch_logits_fwd(const LogitsArgs& s, hipStream_t st) {

@@ -83,9 +83,11 @@ def test_adjoint(rows, n_v, parts, dtype):
 
 
 @TYPES
-@pytest.mark.parametrize("rows, n_v, parts, k", [(520, 1001, 1, 17), (520, 1990, 3, 64), (513, 9001, 2, 17), (512, 36001, 1, 5), (512, 70001, 1, 64), (520, 9001, 9, 33), (600, 100, 33, 9)])
-def test_distill(rows, n_v, parts, k, dtype):
-    """Rows of one wave, rows that a workgroup keeps, and rows that it reads twice."""
+@pytest.mark.parametrize("rows, n_v, parts, k", [(520, 1001, 1, 17), (520, 1990, 3, 64), (513, 9001, 2, 17), (512, 36001, 1, 5), (512, 70001, 1, 64), (520, 9001, 9, 33), (600, 100, 33, 9),
+                                                 (520, 1001, 1, 65), (512, 3001, 2, 300), (3, 5003, 2, 1024), (520, 1001, 1, 1000)])
+@pytest.mark.parametrize("twice", [False, True])
+def test_distill(rows, n_v, parts, k, twice, dtype):
+    """Rows of one wave, rows that a workgroup keeps, and rows that it reads twice; places that come twice in one row, and in all."""
     require_gpu()
     x, _, g = make(rows, n_v, dtype, 4, masked=0.0)
     ids, teacher = teacher_of(rows, n_v, k, g)
@@ -93,7 +95,9 @@ def test_distill(rows, n_v, parts, k, dtype):
     ids[0, k // 2:] = -1
     ids[1] = ids[1, torch.arange(k) // 2]  # every place twice
     ids[2, 0], weight[2] = n_v, 0.0
-    ids[3] = -1
+    if twice:
+        ids[:, -1] = ids[:, 0]
+    ids[3 % rows] = -1
     want_loss, want = tokens.distill(x.double().numpy(), ids.numpy(), teacher.double().numpy(), weight.double().numpy(), 1.5)
     plan, x_ = dd.distdl_logits_plan_create(rows, n_v, parts, dtype), cut(x.cuda(), parts)
     loss, dx = torch.full((rows,), 7.0, device="cuda"), [torch.full_like(t, 7.0) for t in x_]
