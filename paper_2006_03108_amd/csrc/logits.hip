@@ -623,19 +623,18 @@ __global__ __launch_bounds__(THREADS) void logits_bwd_kernel(LogitsArgs s) {
 }
 
 // ---- divergence from a teacher's top logits -------------------------------
-constexpr int kStoredFew = 64;
+constexpr int kStoredFew = 64;    // they are compared with each other
+constexpr int kStoredWave = 256;  // of a row that a wave has: 5 KiB of LDS, for 32 of them on a compute unit
 template <int N>
 struct Stored {  // a row's, N at most
-  static constexpr int kTable = N > kStoredFew ? 2 * N : 1;
   int32_t id[N];
   float p[N];  // the teacher's probabilities
   float x[N];  // the student's logits
   float red[16];
-  int32_t table[kTable], twice;
+  int32_t table[2 * N], twice;
 };
-// One to a lane where a wave has the row.
 template <int THREADS>
-constexpr int stored_most() { return THREADS == 64 ? kStoredFew : kStoredMost; }
+constexpr int stored_most() { return THREADS == 64 ? kStoredWave : kStoredMost; }
 template <int WAVES>
 __device__ __forceinline__ float group_max(float v, float* red) {
 #pragma unroll
@@ -720,10 +719,7 @@ __device__ __forceinline__ bool stored_twice(const LogitsArgs& s, Stored<N>& t) 
 template <class E, int THREADS, int N>
 __device__ __forceinline__ void stored_places(const LogitsArgs& s, LogitsTable table, int64_t row, Stored<N>& t, const LogitsSums& a, float stotal, float scale,
                                               int lo, int hi) {
-  bool search = true;
-  if constexpr (N > kStoredFew) {
-    if (s.n_top > kStoredFew) search = stored_twice<THREADS>(s, t);
-  }
+  const bool search = s.n_top <= kStoredFew || stored_twice<THREADS>(s, t);
   for (int k = threadIdx.x; k < s.n_top; k += THREADS) {
     const int id = t.id[k];
     if (id < 0) continue;
@@ -927,13 +923,15 @@ struct distdl_logits_plan {
 
 namespace distdl {
 
-// Workgroups of a row.  A row is one workgroup's where rows fill the card; else it is cut, down to half a batch of a workgroup.
-static int logits_splits(int64_t rows, int vecs, int batch) {
-  const int64_t wanted = (1024 + rows - 1) / rows, most = std::max(1, vecs / (batch * kLogitsThreads / 2));
-  return rows >= 512 ? 1 : (int)std::min(wanted, most);
+// Workgroups of a row.  A row is one workgroup's where rows fill the card; else it is cut, down to half a batch of a workgroup, or to one worker's part of `parts`, of which a
+// workgroup reads one behind the other (16 rows of 32000 bf16 on 8 workers with 20 alternatives 32 -> 16 us; not so the distillation, whose workgroups all look at
+// all of a row's places: 200 rows of 20000 on 8 with 32 places 26 -> 32).
+static int logits_splits(int64_t rows, int vecs, int batch, int parts) {
+  const int64_t wanted = (1024 + rows - 1) / rows, halves = vecs / (batch * kLogitsThreads / 2);
+  return rows >= 512 || halves < 2 ? 1 : (int)std::min(wanted, std::max<int64_t>(halves, std::min(parts, vecs)));
 }
 
-static int logits_args(distdl_logits_plan* p, const void* const x_dev[], void* const dx_dev[], double temperature, hipStream_t st, LogitsArgs* s) {
+static int logits_args(distdl_logits_plan* p, const void* const x_dev[], void* const dx_dev[], double temperature, int parts, hipStream_t st, LogitsArgs* s) {
   if (!(temperature >= 1e-6 && temperature <= 1e6)) return set_error(DISTDL_ERR_INVALID_ARG, "logits: temperature %g", temperature);
   const size_t size = dtype_size(p->dtype);
   std::vector<LogitsWorker> w((size_t)p->P);
@@ -961,7 +959,7 @@ static int logits_args(distdl_logits_plan* p, const void* const x_dev[], void* c
   s->c = (float)(1.4426950408889634 / temperature);
   s->inv_t = (float)(1.0 / temperature);
   const int vecs = s->extra * s->vec_wide + (s->P - s->extra) * s->vec_rest;
-  s->splits = logits_splits(p->rows, vecs, size == 2 ? logits_batch<uint16_t>() : logits_batch<float>());
+  s->splits = logits_splits(p->rows, vecs, size == 2 ? logits_batch<uint16_t>() : logits_batch<float>(), parts);
   s->per = (vecs + s->splits - 1) / s->splits;
   return DISTDL_OK;
 }
@@ -1004,7 +1002,11 @@ static bool logits_wave_top(const LogitsArgs& s) { return s.splits == 1 && logit
 static bool logits_wave_adjoint(const LogitsArgs& s, int batch) {
   return s.splits == 1 && logits_rounds(s, 64, batch) <= 2 * logits_rounds(s, kLogitsThreads, batch);
 }
-static bool logits_wave_distill(const LogitsArgs& s, int batch) { return s.splits == 1 && logits_vectors(s) <= 128 * batch && s.n_top <= kStoredFew; }
+// (256 places: 8192 rows of 1024 on 1 57 / 37, of 4096 on 1 72 / 79, 600 of 1000, fp32, 10 / 14)
+static bool logits_wave_distill(const LogitsArgs& s, int batch) {
+  const bool many = s.n_top > kStoredFew;
+  return s.splits == 1 && s.n_top <= kStoredWave && logits_vectors(s) <= (many ? 64 : 128) * batch && (!many || s.rows >= 4096);
+}
 
 template <class E, bool ENTROPY, bool TINY>
 static void launch_logits_fwd(const LogitsArgs& s, hipStream_t st) {
@@ -1118,7 +1120,7 @@ int distdl_logprob_fwd(distdl_logits_plan* p, const void* const x_dev[], const i
     LogitsArgs s;
     int rc;
     if ((rc = logits_aligned("logprob_fwd", {targets_dev, logp_dev, lse_dev, entropy_dev, top_ids_dev, top_logp_dev}))) return rc;
-    if ((rc = logits_args(p, x_dev, nullptr, temperature, st_, &s))) return rc;
+    if ((rc = logits_args(p, x_dev, nullptr, temperature, p->P, st_, &s))) return rc;
     s.targets = targets_dev;
     s.logp = logp_dev;
     s.lse = lse_dev;
@@ -1156,7 +1158,7 @@ int distdl_logprob_bwd(distdl_logits_plan* p, const void* const x_dev[], const i
     LogitsArgs s;
     int rc;
     if ((rc = logits_aligned("logprob_bwd", {targets_dev, lse_dev, entropy_dev, dlogp_dev, dentropy_dev}))) return rc;
-    if ((rc = logits_args(p, x_dev, dx_dev, temperature, st_, &s))) return rc;
+    if ((rc = logits_args(p, x_dev, dx_dev, temperature, p->P, st_, &s))) return rc;
     s.targets = dlogp_dev ? targets_dev : nullptr;
     s.lse = const_cast<float*>(lse_dev);
     s.entropy = const_cast<float*>(entropy_dev);
@@ -1184,7 +1186,7 @@ int distdl_distill_fwd_bwd(distdl_logits_plan* p, const void* const x_dev[], con
     LogitsArgs s;
     int rc;
     if ((rc = logits_aligned("distill", {ids_dev, teacher_dev, weight_dev, loss_dev}))) return rc;
-    if ((rc = logits_args(p, x_dev, dx_dev, temperature, st_, &s))) return rc;
+    if ((rc = logits_args(p, x_dev, dx_dev, temperature, 1, st_, &s))) return rc;
     s.stored_ids = ids_dev;
     s.stored = teacher_dev;
     s.n_top = n_top;

@@ -84,7 +84,7 @@ def test_adjoint(rows, n_v, parts, dtype):
 
 @TYPES
 @pytest.mark.parametrize("rows, n_v, parts, k", [(520, 1001, 1, 17), (520, 1990, 3, 64), (513, 9001, 2, 17), (512, 36001, 1, 5), (512, 70001, 1, 64), (520, 9001, 9, 33), (600, 100, 33, 9),
-                                                 (520, 1001, 1, 65), (512, 3001, 2, 300), (3, 5003, 2, 1024), (520, 1001, 1, 1000)])
+                                                 (520, 1001, 1, 65), (513, 999, 2, 256), (512, 3001, 2, 300), (3, 5003, 2, 1024), (520, 1001, 1, 1000)])
 @pytest.mark.parametrize("twice", [False, True])
 def test_distill(rows, n_v, parts, k, twice, dtype):
     """Rows of one wave, rows that a workgroup keeps, and rows that it reads twice; places that come twice in one row, and in all."""
