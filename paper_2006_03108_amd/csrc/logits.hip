@@ -993,12 +993,12 @@ static int64_t logits_rounds(const LogitsArgs& s, int threads, int batch) {
 //   with 20 alternatives   512 on 1 52 / 19, 16384 on 1 146 / 103 (600 rows: 1024 on 1 12.6 / 9.9, 8192 on 1 18 / 29)
 //   adjoint                4096 on 1 32 / 27, 8192 on 1 52 / 57, 2048 on 8 203 / 61
 //   distillation           4096 on 1 62 / 48, 8192 on 1 88 / 91, 16384 on 8 143 / 166
-static bool logits_wave_sums(const LogitsArgs& s, int batch) {
-  return s.splits == 1 && logits_rounds(s, 64, batch) <= std::max<int64_t>(4, 2 * logits_rounds(s, kLogitsThreads, batch));
-}
 static int64_t logits_vectors(const LogitsArgs& s) { return s.extra * s.vec_wide + (int64_t)(s.P - s.extra) * s.vec_rest; }
-// (at most 512 numbers of a lane one behind the other in a sum, as a workgroup has of 131072)
-static bool logits_wave_top(const LogitsArgs& s) { return s.splits == 1 && logits_vectors(s) <= (s.rows >= 4096 ? 4096 : 256); }
+constexpr int kWaveVectors = 4096;  // at most 512 numbers of a lane one behind the other in a sum, as a workgroup has of 131072
+static bool logits_wave_sums(const LogitsArgs& s, int batch) {
+  return s.splits == 1 && logits_vectors(s) <= kWaveVectors && logits_rounds(s, 64, batch) <= std::max<int64_t>(4, 2 * logits_rounds(s, kLogitsThreads, batch));
+}
+static bool logits_wave_top(const LogitsArgs& s) { return s.splits == 1 && logits_vectors(s) <= (s.rows >= 4096 ? kWaveVectors : 256); }
 static bool logits_wave_adjoint(const LogitsArgs& s, int batch) {
   return s.splits == 1 && logits_rounds(s, 64, batch) <= 2 * logits_rounds(s, kLogitsThreads, batch);
 }
