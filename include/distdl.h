@@ -545,7 +545,7 @@ int distdl_scan_step(const void* a_dev, const void* x_dev, float* state_dev, int
  *   call must differ.
  * Outputs must not overlap inputs.  A factor below exp(-200) is 0.  The
  * numbers between (states, what a step adds) have 24 bits in every product;
- * of what bf16 tensors alone depend on, 16.
+ * of what dq and dk of bf16 alone depend on, 16.
  * fwd and bwd keep what chunks of steps need in the plan's scratch, bwd two
  * states for each 64 steps: calls and recorded graphs
  * of one plan and stream share it, they run one after another.

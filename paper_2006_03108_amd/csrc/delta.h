@@ -163,13 +163,6 @@ __device__ __forceinline__ Pieces<3> split_tiles(f32x4 a, f32x4 b) {
   const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
   return split8(v);
 }
-template <int M, int N>
-__device__ __forceinline__ Pieces<M> first_pieces(const Pieces<N>& a) {
-  Pieces<M> o;
-#pragma unroll
-  for (int i = 0; i < M; ++i) o.p[i] = a.p[i];
-  return o;
-}
 // Eight numbers of the tensors' type: one piece of bf16, three of fp32.
 template <class E>
 constexpr int delta_pieces() { return sizeof(E) == 2 ? 1 : 3; }

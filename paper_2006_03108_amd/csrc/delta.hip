@@ -25,7 +25,7 @@ __device__ __forceinline__ float bounded(float g) { return g < -200.f ? -200.f :
 // beta's gradient is dR U / beta, what beta multiplies being U / beta.  So a beta of 0 counts as 2^-100: what it adds to a state does not show.
 __device__ __forceinline__ float nonzero(float beta) { return fabsf(beta) < 0x1p-100f ? 0x1p-100f : beta; }
 
-// Pieces of a product whose results the tensors' type rounds to bf16: what lies below 16 bits does not show there.
+// Pieces of a product whose results the tensors' type rounds to bf16 (adjoint): what lies below 16 bits does not show there.
 template <class E>
 constexpr int delta_rounded() { return sizeof(E) == 2 ? 2 : 3; }
 
@@ -114,7 +114,7 @@ template <class E, int C, int DK, bool BACK>
 __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
   typedef DeltaSizes<C, DK> Z;
   typedef DeltaPrepareShared<E, C, DK> Shared;
-  constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>();
+  constexpr int NI = delta_pieces<E>();
   extern __shared__ char delta_lds[];
   Shared& m = *(Shared*)delta_lds;
   const DeltaTable table = DELTA_TABLE(s);
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
           return split_tiles(*(const f32x4*)&from[i][32 * ts + 4 * g], *(const f32x4*)&from[i][32 * ts + 16 + 4 * g]);
         };
         store_fragment(s.tf + o, across(m.t));
-        if constexpr (!BACK) store_fragment(s.pf + head * Z::kStepPiece * NO + (int64_t)f * NO * kFragment, first_pieces<NO>(across(m.p)));
+        if constexpr (!BACK) store_fragment(s.pf + o, across(m.p));
       }
       if (BACK && mt / 2 <= ts) {
         auto down = [&](const float (*from)[Shared::kLine]) {
@@ -524,11 +524,11 @@ template <class E, int DK, int NT, bool STORE>
 __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaArgs s) {
   typedef DeltaSizes<kChunk, DK> Z;
   typedef DeltaColumns<E, NT> Columns;
-  constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>(), KT = DK / 64, KS = Z::kKeySteps;
+  constexpr int NI = delta_pieces<E>(), KT = DK / 64, KS = Z::kKeySteps;
   __shared__ DeltaTiles<16, NT> of_keys;  // K S: tile of steps, wave
-  __shared__ DeltaShared<STORE ? 1 : KS, NT, NO> for_queries;
+  __shared__ DeltaShared<STORE ? 1 : KS, NT, 3> for_queries;
   __shared__ DeltaShared<2, NT, 3> for_inner, for_state;
-  __shared__ DeltaShared<2, NT, STORE ? 1 : NO> for_out;
+  __shared__ DeltaShared<2, NT, STORE ? 1 : 3> for_out;
   const DeltaTable table = DELTA_TABLE(s);
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, tile = wave & 3;
   const DeltaChain chain = delta_chain<NT>(s);
@@ -541,11 +541,11 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
   if (!STORE && wave >= 4) {  // O = scale exp(G) (Q S) + P U
     auto outputs = [&](int p) { return table[p].o; };
     DeltaFragments<KS, NI, NI> qf;
-    DeltaFragments<2, NO, NO> pf;
+    DeltaFragments<2, kInner, kInner> pf;
     const int steps_in = tile < 2 ? 1 : 2;  // of the sums over steps, those that are not all zeros
     DeltaSteps steps;
     qf.start(s.qf, chunk0, s.n_hk, hk, Z::kKeyPiece * NI, 0, tile * KS * NI);
-    pf.start(s.pf, chunk0, s.n_h, h, Z::kStepPiece * NO, 0, tile * 2 * NO);
+    pf.start(s.pf, chunk0, s.n_h, h, Z::kStepPiece * kInner, 0, tile * 2 * kInner);
     steps.start(s, chunk0, h, 0);
     walk.start(s, 0, outputs);
     if (chunks > 0) {
@@ -637,7 +637,7 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int k = 0; k < NO; ++k) {
+        for (int k = 0; k < 3; ++k) {
           if constexpr (KT == 2) {
             for_queries.v[wave][n][k][lane] = own[n].p[k];
           } else {
@@ -1565,7 +1565,7 @@ static int delta_scratch(distdl_delta_plan* p, bool back, hipStream_t st, DeltaA
     void** at;
     size_t bytes;
   } parts[] = {{(void**)&s->kf, key}, {(void**)&s->ktf, back || !delta_turned<E>() ? key : 0}, {(void**)&s->qf, back ? 0 : key}, {(void**)&s->qtf, back ? key : 0},
-               {(void**)&s->tf, step}, {(void**)&s->pf, back ? 0 : step / kInner * delta_rounded<E>()}, {(void**)&s->ttf, back ? step : 0}, {(void**)&s->ptf, back ? step : 0},
+               {(void**)&s->tf, step}, {(void**)&s->pf, back ? 0 : step}, {(void**)&s->ttf, back ? step : 0}, {(void**)&s->ptf, back ? step : 0},
                {(void**)&s->tiles, back ? heads * 2 * Z::kLower * 1024 : 0}, {(void**)&s->steps, heads * kStepNumbers * C * 4}, {(void**)&s->states, back ? state : 0}, {(void**)&s->dstates, back ? state : 0},
                {(void**)&s->u, back ? rows : 0}, {(void**)&s->dr, back ? rows : 0},
                {(void**)&s->keys, back && delta_heads_apart(keys, s->each) ? heads * 2 * C * DK * 4 : 0}};
