@@ -755,7 +755,7 @@ __global__ __launch_bounds__(512, 2) void delta_bwd_kernel(DeltaArgs s) {
     steps.load(tile);
     __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);  // (so that the loop's waits count its own loads alone)
     // Three barriers a chunk, one chunk before the other waves.
-    for (int i = chunks; i >= 0; --i) {
+    for (; c >= 0; --c) {
       const bool more = c > 0;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -786,8 +786,11 @@ __global__ __launch_bounds__(512, 2) void delta_bwd_kernel(DeltaArgs s) {
       qtf.load();
       lds_barrier();
       lds_barrier();
-      c -= more;
     }
+    // (the other waves' last chunk: nothing is written while they read what was made for it)
+    lds_barrier();
+    lds_barrier();
+    lds_barrier();
     return;
   }
 
