@@ -544,8 +544,7 @@ int distdl_scan_step(const void* a_dev, const void* x_dev, float* state_dev, int
  *   0 .. n_slots - 1 is idle: its o is 0 and no state changes.  Slots of one
  *   call must differ.
  * Outputs must not overlap inputs.  A factor below exp(-200) is 0.  The
- * numbers between (states, what a step adds) have 24 bits in every product;
- * of what dq and dk of bf16 alone depend on, 16.
+ * numbers between (states, what a step adds) have 24 bits in every product.
  * fwd and bwd keep what chunks of steps need in the plan's scratch, bwd two
  * states for each 64 steps: calls and recorded graphs
  * of one plan and stream share it, they run one after another.

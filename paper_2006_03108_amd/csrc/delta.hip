@@ -25,10 +25,6 @@ __device__ __forceinline__ float bounded(float g) { return g < -200.f ? -200.f :
 // beta's gradient is dR U / beta, what beta multiplies being U / beta.  So a beta of 0 counts as 2^-100: what it adds to a state does not show.
 __device__ __forceinline__ float nonzero(float beta) { return fabsf(beta) < 0x1p-100f ? 0x1p-100f : beta; }
 
-// Pieces of a product whose results the tensors' type rounds to bf16 (adjoint): what lies below 16 bits does not show there.
-template <class E>
-constexpr int delta_rounded() { return sizeof(E) == 2 ? 2 : 3; }
-
 // Whether K^T is made of K where it is used.
 template <class E>
 constexpr bool delta_turned() { return sizeof(E) == 2; }
@@ -901,7 +897,7 @@ struct DeltaGradShared {
     struct {
       uint16_t dr[3][C][kRow], u[3][C][kRow], d_o[delta_pieces<E>()][C][kRow];
     };
-    uint16_t inner[3][delta_rounded<E>()][C][kRow];  // M + M^T, N, N^T; in a row, a lane's eight numbers of a step of the sum one behind the other
+    uint16_t inner[3][3][C][kRow];  // pieces of M + M^T, N, N^T; in a row, a lane's eight numbers of a step of the sum one behind the other
   };
   float row_sum[2][kTiles][C], col_sum[2][2][C];
   float dots[kKeyTiles][C], ends[kKeyTiles][C], us[C], both[kKeyTiles];
@@ -965,7 +961,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
   static_assert(C == 64, "two steps of a sum over steps");
   typedef DeltaSizes<C, DK> Z;
   typedef DeltaGradShared<E, C, DK> Shared;
-  constexpr int NI = delta_pieces<E>(), NO = delta_rounded<E>(), W = 8;
+  constexpr int NI = delta_pieces<E>(), W = 8;
   constexpr int kMine = Z::kTiles * Z::kKeyTiles / W;  // tiles of a wave: one column of keys, some rows of steps
   constexpr bool kBoth = kMine == 2;  // with 64 keys a wave has tiles of M and of N, with 128 of one of them
   extern __shared__ char delta_lds[];
@@ -1221,7 +1217,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
       if (row < 4) m.row_sum[what][nt][i0 + row] = across_of;
       const Pieces<3> p = split_tiles(mine, f32x4{});
 #pragma unroll
-      for (int k = 0; k < NO; ++k) {
+      for (int k = 0; k < 3; ++k) {
         const u32x2 v = {p.p[k][0], p.p[k][1]};
         if constexpr (what) {
           *(u32x2*)&m.inner[2][k][j][place_of(i0)] = v;
@@ -1313,9 +1309,9 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
       for (int i = 0; i < kMine; ++i) {
         const int mt = mt0 + i;
         auto across = [&](int what) {
-          Pieces<NO> o;
+          Pieces<3> o;
 #pragma unroll
-          for (int x = 0; x < NO; ++x) {
+          for (int x = 0; x < 3; ++x) {
             o.p[x] = *(const u32x4*)&m.inner[what][x][mt * 16 + row][32 * k + 8 * g];
           }
           return o;
