@@ -64,9 +64,9 @@ def log_softmax(x, temperature=1.0):
     most = z.max(1, keepdims=True)
     most = np.where(np.isneginf(most), 0.0, most)
     with np.errstate(divide="ignore"):
-        lse = most + np.log(np.exp(z - most).sum(1, keepdims=True))
-    with np.errstate(invalid="ignore"):
-        return np.where(np.isneginf(lse), -np.inf, z - lse), lse[:, 0]
+        total = np.log(np.exp(z - most).sum(1, keepdims=True))
+    with np.errstate(invalid="ignore"):  # (a maximum of -1e20 plus a logarithm is -1e20, so log p is not z - lse)
+        return np.where(np.isneginf(total), -np.inf, (z - most) - total), (most + total)[:, 0]
 
 
 def _plogp(log_p):

@@ -199,21 +199,22 @@ __device__ __forceinline__ T other_lane(T v) {
 }
 
 // ---- sums -----------------------------------------------------------------
-// Where the maximum is so far from 0 that m c may be no number (masks of the type's lowest value that leave nothing else), d is (x - m) c,
-// which costs an operation more and is 0 or out of exp2's range.
-constexpr float kFar = 1e30f;
+// The largest entry's own d is what rounding has left of m c: up to 2^-5 where m c is below 2^20, beyond what exp2 takes from 2^31 on (masks of -1e10, alone in a lane or a row), and m c is no
+// number at last.  From 2^20 on d is (x - m) c, of the reference m c itself: an operation more, and exact where entries are near the maximum.
+constexpr float kFar = 0x1p20f;
 
 struct LogitsSums {
   float m = -INFINITY, mc = 0.f, s = 0.f, w = 0.f;
-  __device__ __forceinline__ bool far() const { return fabsf(m) >= kFar && m != -INFINITY; }
+  __device__ __forceinline__ bool far() const { return fabsf(mc) >= kFar; }
   // d of an entry
   __device__ __forceinline__ float of(float x, float c) const { return far() ? (x - m) * c : fmaf(x, c, -mc); }
   __device__ __forceinline__ bool none() const { return m == -INFINITY && s == 0.f; }  // every entry is -inf
   // the reference moves up to the maximum m1
   __device__ __forceinline__ void raise(float m1, float c) {
     const float mc1 = m1 == -INFINITY ? 0.f : m1 * c;
-    // (where there is nothing to move, nowhere)
-    const float shift = m == -INFINITY ? 0.f : fmaxf(fabsf(m) >= kFar || fabsf(m1) >= kFar ? (m - m1) * c : mc - mc1, -kFar);
+    const bool far0 = far(), far1 = fabsf(mc1) >= kFar;
+    const float by = far1 ? far0 ? (m - m1) * c : fmaf(-m1, c, mc) : far0 ? fmaf(m, c, -mc1) : mc - mc1;
+    const float shift = m == -INFINITY ? 0.f : fmaxf(by, -200.f);  // (where there is nothing to move, nowhere)
     const float f = __builtin_amdgcn_exp2f(shift);
     w = f * fmaf(s, shift, w);
     s *= f;
@@ -244,7 +245,8 @@ struct LogitsSums {
     if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = make_float4(m, mc, s, w);
     __syncthreads();
     LogitsSums all;
-#pragma unroll
+    constexpr int kAtOnce = WAVES > 4 ? 2 : WAVES;  // (sixteen places in registers at once would leave a compute unit one workgroup: 480 -> 537 us for 4096 x 131072)
+#pragma unroll kAtOnce
     for (int i = 0; i < WAVES; ++i) {
       const float4 v = shared[i];
       LogitsSums one;
@@ -579,6 +581,8 @@ __device__ __forceinline__ void logits_store(E* row, const float* f, int at, int
   }
 }
 
+constexpr float kLseFar = 1e30f;
+
 template <class E, bool ENTROPY, bool TINY, int THREADS>
 __global__ __launch_bounds__(THREADS) void logits_bwd_kernel(LogitsArgs s) {
   constexpr int B = logits_batch<E>();
@@ -590,8 +594,8 @@ __global__ __launch_bounds__(THREADS) void logits_bwd_kernel(LogitsArgs s) {
   const float lse = s.lse[row], weight = live ? s.dlogp[row] : 0.f, back = ENTROPY ? s.dentropy[row] : 0.f;
   // dx = p (one + two log2 p) / temperature, and the target's dlogp
   const float one = (-weight - (ENTROPY ? back * s.entropy[row] : 0.f)) * s.inv_t, two = -back * kLn2 * s.inv_t;
-  const bool nothing = (weight == 0.f && back == 0.f) || lse < -kFar;  // such rows are not read
-  const bool far = lse >= kFar;
+  const bool nothing = (weight == 0.f && back == 0.f) || lse < -kLseFar;  // such rows are not read
+  const bool far = lse >= kLseFar;
   const float lc = lse * (1.f / kLn2), at_target = weight * s.inv_t;
   logits_each<B, THREADS>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
     const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));

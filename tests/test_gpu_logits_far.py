@@ -1,0 +1,99 @@
+"""Rows of logits with numbers far from 0: masks that are numbers (-1e9, -1e10, -1e20), alone or beside entries of ordinary size, at several
+temperatures; rows that are shifted as a whole.  Against the oracle in fp64.
+
+Tolerances as in test_gpu_logits.py where what counts is of ordinary size (z is, at every temperature): differences of numbers near each other are exact.  An lse, or a log
+probability of a masked entry, of size a is rounded a few times at that size: 2^-22 a.  A loss is a sum of t (log t - log p), and t is off by TOL of itself as p is there: where log p is
+a mask's of size a, by TOL t a.  A gradient scale (p - t) is off by TOL scale (p + t), whatever is left of it."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2006_03108_amd as dd
+from gpu_util import require_gpu
+from oracle import tokens
+from test_gpu_logits import BF16, F32, TOL, cut, forward, near
+
+pytestmark = pytest.mark.gpu
+TYPES = pytest.mark.parametrize("dtype", [F32, BF16])
+MASKS = pytest.mark.parametrize("mask", [-1e9, -1e10, -1e20])
+SIZE = 2.0 ** -22
+# rows, entries, workers: cut rows, a workgroup's, a wave's, tiny parts
+SHAPES = [(7, 20011, 3), (2, 90000, 1), (520, 9001, 2), (520, 1203, 3), (600, 100, 33)]
+
+
+def masked(rows, n_v, dtype, mask, temperature, seed=0):
+    """Seven kinds of rows by turns: nothing but the mask, one entry left, a masked front, a masked end, a masked middle, every other entry masked, no mask."""
+    g = torch.Generator().manual_seed(seed)
+    x = (3 * temperature * torch.randn(rows, n_v, generator=g)).to(dtype)
+    at = torch.arange(n_v)
+    kinds = [at >= 0, at != n_v // 3, at < n_v * 3 // 4, at >= n_v // 4, (at >= n_v // 5) & (at < n_v - 2), at % 2 == 0, at < 0]
+    for r in range(rows):
+        x[r, kinds[r % 7]] = mask
+    targets = torch.randint(0, n_v, (rows,), generator=g, dtype=torch.int32)
+    if rows > 1:
+        targets[1] = n_v // 3
+    return x, targets, g
+
+
+def check_forward(x, targets, parts, k, temperature):
+    _, (logp, lse, entropy, ids, top) = forward(x, targets, parts, k, temperature)
+    want = tokens.logprob_forward(x.double().numpy(), targets.numpy(), k, temperature)
+    for got, w, what in ((logp, want[0], "logp"), (lse, want[1], "lse"), (entropy, want[2], "entropy")) + (((top, want[4], "top"),) if k else ()):
+        near(got, w, TOL + SIZE * np.abs(w), what)
+    if k:
+        assert np.array_equal(ids.cpu().numpy(), want[3])
+
+
+@TYPES
+@MASKS
+@pytest.mark.parametrize("rows, n_v, parts", SHAPES)
+def test_masks_that_are_numbers(rows, n_v, parts, mask, dtype):
+    require_gpu()
+    for temperature in (1.0, 0.3, 0.1, 2.0):
+        x, targets, _ = masked(rows, n_v, dtype, mask, temperature)
+        for k in (0, 9):
+            check_forward(x, targets, parts, k, temperature)
+
+
+@pytest.mark.parametrize("shift", [726817.0, -726817.0, 1e6, -1e6, 1e7])
+@pytest.mark.parametrize("rows, n_v, parts", SHAPES)
+def test_shifted_rows(rows, n_v, parts, shift):
+    """A row that is shifted has the same log probabilities.  In units of log 2 the first shifts are 2^20, so some entries are below it and some above."""
+    require_gpu()
+    g = torch.Generator().manual_seed(1)
+    x = shift + 4 * torch.randn(rows, n_v, generator=g)
+    check_forward(x, torch.randint(0, n_v, (rows,), generator=g, dtype=torch.int32), parts, 9, 1.0)
+
+
+@pytest.mark.parametrize("temperature", [1e-6, 1e-3, 1e6])
+def test_all_temperatures(temperature):
+    """Logits of 5000 at the lowest temperature are 7e9 in units of log 2; neighbouring numbers are so far apart there that the largest has everything."""
+    require_gpu()
+    for rows in (5, 520):
+        g = torch.Generator().manual_seed(2)
+        x = 5000 + torch.randn(rows, 3001, generator=g)
+        x[1], x[2, :2000] = 5000.0, 5000.0
+        check_forward(x, torch.randint(0, 3001, (rows,), generator=g, dtype=torch.int32), 2, 5, temperature)
+
+
+@TYPES
+@MASKS
+@pytest.mark.parametrize("rows, n_v, parts, k", [(7, 20011, 3, 9), (520, 1001, 1, 9), (520, 9001, 2, 9), (512, 70001, 1, 9), (520, 1203, 3, 70), (600, 100, 33, 9)])
+def test_distillation_of_a_masked_student(rows, n_v, parts, k, mask, dtype):
+    """One wave's rows, kept ones, ones that are read twice and cut ones.  The teacher has places that the mask leaves, where it leaves enough."""
+    require_gpu()
+    for temperature in (1.0, 0.1):
+        x, _, g = masked(rows, n_v, dtype, mask, temperature, 3)
+        order = torch.argsort(-x.float(), dim=1, stable=True)
+        ids = torch.stack([o[torch.randperm(k + 15, generator=g)[:k]] for o in order]).to(torch.int32)
+        ids[1], ids[1, 0] = -1, n_v // 3
+        teacher, weight = 2 * temperature * torch.randn(rows, k, generator=g), 0.5 + torch.rand(rows, generator=g)
+        want_loss, want = tokens.distill(x.double().numpy(), ids.numpy(), teacher.double().numpy(), weight.double().numpy(), temperature)
+        plan, x_ = dd.distdl_logits_plan_create(rows, n_v, parts, dtype), cut(x.cuda(), parts)
+        loss, dx = torch.full((rows,), 7.0, device="cuda"), [torch.full_like(t, 7.0) for t in x_]
+        dd.distdl_distill_fwd_bwd(plan, x_, ids.cuda(), teacher.cuda(), weight.cuda(), loss, dx, temperature)
+        near(loss, want_loss, 2 * TOL + TOL * np.abs(want_loss), "loss")
+        scale = weight.double().numpy()[:, None] / temperature
+        p = np.exp(tokens.log_softmax(x.double().numpy(), temperature)[0])
+        size = p + np.abs(p - want / scale)  # p + t
+        near(torch.cat(dx, 1), want, TOL * scale * size + 1e-12 + (2.0 ** -8 * np.abs(want) if dtype == BF16 else 0), "dx")
