@@ -662,10 +662,11 @@ __device__ __forceinline__ float group_sum(float v, float* red) {
   for (int i = 1; i < WAVES; ++i) v += red[i];
   return v;
 }
-// The teacher's probabilities of a row: false if it has stored nothing.  total: log2 of their sum relative to `most`.
+// The teacher's probabilities of a row: false if it has stored nothing.  total: log2 of their sum relative to the largest, `most`.  (Differences from it first: any finite
+// numbers have probabilities, masks of the lowest value too.)
 template <int THREADS, int N>
-__device__ __forceinline__ bool stored_load(const LogitsArgs& s, int64_t row, Stored<N>& t, float& mc, float& total) {
-  float most = -INFINITY;
+__device__ __forceinline__ bool stored_load(const LogitsArgs& s, int64_t row, Stored<N>& t, float& most, float& total) {
+  most = -INFINITY;
   bool odd = false;
   for (int k = threadIdx.x; k < s.n_top; k += THREADS) {
     const int id = s.stored_ids[row * s.n_top + k];
@@ -678,20 +679,19 @@ __device__ __forceinline__ bool stored_load(const LogitsArgs& s, int64_t row, St
   }
   most = group_max<THREADS / 64>(odd ? INFINITY : most, t.red);  // (a NaN ends as NaN: inf - inf)
   if (most == -INFINITY) return false;
-  mc = most * s.c;
   float sum = 0.f;
-  for (int k = threadIdx.x; k < s.n_top; k += THREADS) sum += __builtin_amdgcn_exp2f(fmaf(t.p[k], s.c, -mc));
+  for (int k = threadIdx.x; k < s.n_top; k += THREADS) sum += __builtin_amdgcn_exp2f((t.p[k] - most) * s.c);
   sum = group_sum<THREADS / 64>(sum, t.red);
   total = __builtin_amdgcn_logf(sum);
   return true;
 }
 // The row's loss, and the teacher's logits in t.p become probabilities.  a, stotal: the student's.
 template <int THREADS, int N>
-__device__ __forceinline__ float stored_loss(const LogitsArgs& s, Stored<N>& t, float mc, float total, const LogitsSums& a, float stotal) {
+__device__ __forceinline__ float stored_loss(const LogitsArgs& s, Stored<N>& t, float most, float total, const LogitsSums& a, float stotal) {
   float loss = 0.f;
   const float inv = __builtin_amdgcn_exp2f(-total);
   for (int k = threadIdx.x; k < s.n_top; k += THREADS) {
-    const float d = fmaf(t.p[k], s.c, -mc), p = __builtin_amdgcn_exp2f(d) * inv;
+    const float d = (t.p[k] - most) * s.c, p = __builtin_amdgcn_exp2f(d) * inv;
     if (!(p == 0.f)) loss = fmaf(p, (d - total) - (a.of(t.x[k], s.c) - stotal), loss);
     t.p[k] = p;
   }
@@ -752,7 +752,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(LogitsArgs s) {
   const LogitsTable table = LOGITS_TABLE(s);
   const int64_t row = blockIdx.x / (uint32_t)s.splits;
   const int split = blockIdx.x % (uint32_t)s.splits, tid = threadIdx.x;
-  float weight = s.weight ? s.weight[row] : 1.f, mc = 0.f, total = 0.f;
+  float weight = s.weight ? s.weight[row] : 1.f, most = 0.f, total = 0.f;
   LogitsSums a;
   bool any = false;
   if (FIRST) {
@@ -765,7 +765,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(LogitsArgs s) {
       if (v >= lo && v < hi) s.stored_x[row * s.n_top + k] = logits_at<E>(s, table, row, id);
     }
   } else {
-    any = stored_load<THREADS>(s, row, t, mc, total);
+    any = stored_load<THREADS>(s, row, t, most, total);
     if (!any) weight = 0.f;
     if (any)
       for (int k = tid; k < s.n_top; k += THREADS)
@@ -799,7 +799,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(LogitsArgs s) {
     if (tid == 0 && split == 0 && s.loss) s.loss[row] = INFINITY;
     weight = 0.f;
   } else if (any) {
-    const float loss = stored_loss<THREADS>(s, t, mc, total, a, stotal);
+    const float loss = stored_loss<THREADS>(s, t, most, total, a, stotal);
     if (tid == 0 && split == 0 && s.loss) s.loss[row] = loss;
   } else if (tid == 0 && split == 0 && s.loss) {
     s.loss[row] = 0.f;
@@ -870,8 +870,8 @@ __global__ __launch_bounds__(THREADS) void distill_kept_kernel(LogitsArgs s) {
   };
   Vector v[S];
   slots([&](int i, int j, const LogitsPart& p, int base) { v[i].load(logits_row(table[j].x, row, p.n, sizeof(E)), p.n, base + tid); });
-  float weight = s.weight ? s.weight[row] : 1.f, mc = 0.f, total = 0.f;
-  const bool any = stored_load<THREADS>(s, row, t, mc, total);
+  float weight = s.weight ? s.weight[row] : 1.f, most = 0.f, total = 0.f;
+  const bool any = stored_load<THREADS>(s, row, t, most, total);
   if (any) {
     for (int k = tid; k < s.n_top; k += THREADS) t.x[k] = t.id[k] < 0 ? 0.f : logits_at<E>(s, table, row, t.id[k]);
   } else {
@@ -892,7 +892,7 @@ __global__ __launch_bounds__(THREADS) void distill_kept_kernel(LogitsArgs s) {
     loss = INFINITY;
     weight = 0.f;
   } else if (any) {
-    loss = stored_loss<THREADS>(s, t, mc, total, a, stotal);
+    loss = stored_loss<THREADS>(s, t, most, total, a, stotal);
   }
   if (tid == 0 && s.loss) s.loss[row] = loss;
   const float scale = weight * s.inv_t, off = a.mc + stotal;

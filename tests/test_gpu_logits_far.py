@@ -97,3 +97,41 @@ def test_distillation_of_a_masked_student(rows, n_v, parts, k, mask, dtype):
         p = np.exp(tokens.log_softmax(x.double().numpy(), temperature)[0])
         size = p + np.abs(p - want / scale)  # p + t
         near(torch.cat(dx, 1), want, TOL * scale * size + 1e-12 + (2.0 ** -8 * np.abs(want) if dtype == BF16 else 0), "dx")
+
+
+@TYPES
+@pytest.mark.parametrize("rows, n_v, parts, k", [(9, 20011, 3, 9), (520, 1001, 1, 9), (520, 9001, 2, 9), (512, 36001, 1, 9), (520, 1203, 3, 70), (600, 100, 33, 9)])
+def test_distillation_from_a_teacher_of_large_numbers(rows, n_v, parts, k, dtype):
+    """By turns: the lowest number at all places, at place 0 again and again (padding), one place with it, with -1e10, 1e10 and the largest number, equal large ones, ordinary ones
+    beside the lowest, ordinary ones.  One place with any finite logit is the cross entropy."""
+    require_gpu()
+    low = torch.finfo(F32).min
+    for temperature in (1.0, 0.25, 4.0):
+        g = torch.Generator().manual_seed(5)
+        x = (3 * temperature * torch.randn(rows, n_v, generator=g)).to(dtype)
+        ids = torch.stack([torch.randperm(n_v, generator=g)[:k] for _ in range(rows)]).to(torch.int32)
+        teacher, weight = 2 * temperature * torch.randn(rows, k, generator=g), 0.5 + torch.rand(rows, generator=g)
+        for r in range(rows):
+            kind = r % 9
+            if kind in (0, 1):
+                teacher[r] = low
+                ids[r] = ids[r] if kind == 0 else 0
+            elif kind < 6:
+                ids[r, 1:], teacher[r, 0] = -1, (low, -1e10, 1e10, -low)[kind - 2]
+            elif kind == 6:
+                teacher[r] = 1e20
+            elif kind == 7:
+                teacher[r, ::2] = low
+        weight[1] = 0.0  # (its loss is a number too)
+        want_loss, want = tokens.distill(x.double().numpy(), ids.numpy(), teacher.double().numpy(), weight.double().numpy(), temperature)
+        plan, x_ = dd.distdl_logits_plan_create(rows, n_v, parts, dtype), cut(x.cuda(), parts)
+        loss, dx = torch.full((rows,), 7.0, device="cuda"), [torch.full_like(t, 7.0) for t in x_]
+        dd.distdl_distill_fwd_bwd(plan, x_, ids.cuda(), teacher.cuda(), weight.cuda(), loss, dx, temperature)
+        near(loss, want_loss, 2 * TOL, "loss")
+        scale = weight.double().numpy()[:, None] / temperature
+        p = np.exp(tokens.log_softmax(x.double().numpy(), temperature)[0])
+        size = p * scale + np.abs(p * scale - want)  # of p and t
+        near(torch.cat(dx, 1), want, TOL * size + 1e-12 + (2.0 ** -8 * np.abs(want) if dtype == BF16 else 0), "dx")
+        log_p = tokens.log_softmax(x.double().numpy(), temperature)[0]
+        alone = [r for r in range(rows) if 2 <= r % 9 < 6]
+        near(loss[alone], [-log_p[r, ids[r, 0]] for r in alone], 2 * TOL, "cross entropy")
