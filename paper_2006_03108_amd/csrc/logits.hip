@@ -718,7 +718,7 @@ __device__ __forceinline__ bool stored_twice(const LogitsArgs& s, Stored<N>& t) 
   return t.twice != 0;
 }
 
-// The teacher's places among a split's vectors lo .. hi - 1 are written once more.  off: log2 of the sum, and its reference.  Looking through all of a row's places for
+// The teacher's places among a split's vectors lo .. hi - 1 are written once more.  stotal: log2 of the sum.  Looking through all of a row's places for
 // each of them is left for rows where one comes twice: 8192 x 1024 with 256 places, bf16, 167 us else.
 template <class E, int THREADS, int N>
 __device__ __forceinline__ void stored_places(const LogitsArgs& s, LogitsTable table, int64_t row, Stored<N>& t, const LogitsSums& a, float stotal, float scale,
@@ -805,7 +805,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(LogitsArgs s) {
     s.loss[row] = 0.f;
   }
   if (!table[0].dx) return;
-  const float scale = weight * s.inv_t, off = a.mc + stotal;
+  const float scale = weight * s.inv_t;
   const bool far = a.far();
   const bool nothing = weight == 0.f;  // such rows are not read
   __syncthreads();
@@ -827,7 +827,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(LogitsArgs s) {
       if (!nothing) {
         v[b].values(f, p.n, i0, to, false, false);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = scale * __builtin_amdgcn_exp2f(far ? a.of(f[i], s.c) - stotal : fmaf(f[i], s.c, -off));
+        for (int i = 0; i < 8; ++i) f[i] = scale * __builtin_amdgcn_exp2f((far ? (f[i] - a.m) * s.c : fmaf(f[i], s.c, -a.mc)) - stotal);  // (mc + stotal, rounded, would be off by what a row is shifted)
       }
       logits_store(dx, f, at, from, p.n, edge);
     }
@@ -895,7 +895,7 @@ __global__ __launch_bounds__(THREADS) void distill_kept_kernel(LogitsArgs s) {
     loss = stored_loss<THREADS>(s, t, most, total, a, stotal);
   }
   if (tid == 0 && s.loss) s.loss[row] = loss;
-  const float scale = weight * s.inv_t, off = a.mc + stotal;
+  const float scale = weight * s.inv_t;
   const bool nothing = weight == 0.f, far = a.far();
   __syncthreads();  // (places of the row are read above, of dx on x)
   slots([&](int i, int j, const LogitsPart& p, int base) {
@@ -904,7 +904,7 @@ __global__ __launch_bounds__(THREADS) void distill_kept_kernel(LogitsArgs s) {
     if (!nothing) {
       v[i].values(f, p.n, base + tid, p.vecs, false, false);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) f[k] = scale * __builtin_amdgcn_exp2f(far ? a.of(f[k], s.c) - stotal : fmaf(f[k], s.c, -off));
+      for (int k = 0; k < 8; ++k) f[k] = scale * __builtin_amdgcn_exp2f((far ? (f[k] - a.m) * s.c : fmaf(f[k], s.c, -a.mc)) - stotal);
     }
     const int at = Vector::place(p.n, base + tid), from = base + tid < p.vecs ? Vector::first_of(p.n, base + tid) : 8;
     logits_store(dx, f, at, from, p.n, base + THREADS >= p.vecs);

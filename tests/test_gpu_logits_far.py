@@ -135,3 +135,40 @@ def test_distillation_from_a_teacher_of_large_numbers(rows, n_v, parts, k, dtype
         log_p = tokens.log_softmax(x.double().numpy(), temperature)[0]
         alone = [r for r in range(rows) if 2 <= r % 9 < 6]
         near(loss[alone], [-log_p[r, ids[r, 0]] for r in alone], 2 * TOL, "cross entropy")
+
+
+@pytest.mark.parametrize("shift", [0.0, 1e3, -1e5, 5e5, 7e5, 1e6])
+@pytest.mark.parametrize("rows, n_v, parts, k", [(7, 20011, 3, 9), (520, 1001, 1, 9), (520, 9001, 2, 9), (512, 36001, 1, 9)])
+def test_gradients_of_shifted_rows(rows, n_v, parts, k, shift):
+    """x is rounded once it is shifted, the oracle has it as it is.  What a shift would cost were it in a number of its size: 2^-24 of 1e6 / ln 2, 9 % of p."""
+    require_gpu()
+    g = torch.Generator().manual_seed(6)
+    x = shift + 3 * torch.randn(rows, n_v, generator=g)
+    ids = torch.stack([torch.randperm(n_v, generator=g)[:k] for _ in range(rows)]).to(torch.int32)
+    teacher, weight = 2 * torch.randn(rows, k, generator=g), 0.5 + torch.rand(rows, generator=g)
+    want_loss, want = tokens.distill(x.double().numpy(), ids.numpy(), teacher.double().numpy(), weight.double().numpy())
+    plan, x_ = dd.distdl_logits_plan_create(rows, n_v, parts, F32), cut(x.cuda(), parts)
+    loss, dx = torch.full((rows,), 7.0, device="cuda"), [torch.full_like(t, 7.0) for t in x_]
+    dd.distdl_distill_fwd_bwd(plan, x_, ids.cuda(), teacher.cuda(), weight.cuda(), loss, dx)
+    near(loss, want_loss, 2 * TOL, "loss")
+    scale = weight.double().numpy()[:, None]
+    p = np.exp(tokens.log_softmax(x.double().numpy())[0])
+    size = p * scale + np.abs(p * scale - want)
+    near(torch.cat(dx, 1), want, TOL * size + 1e-12, "dx")
+
+
+def test_gradients_are_as_near_as_the_rounding_of_differences():
+    """Rows of ordinary logits, |z - lse| up to 25, 36 in units of log 2.  p = exp2(d) with d = (x c - m c) - log2 s: its two differences are rounded by up to 36 u each, half of that
+    as a rule, log2 s and exp2 by u of 12 and of p: less than 36 u ln 2 = 1.5e-6 of p by root mean square, and with most of the sum of squares in entries with d above -20 some 4e-7."""
+    require_gpu()
+    g = torch.Generator().manual_seed(7)
+    x = 3 * torch.randn(64, 10007, generator=g) + 11
+    ids, teacher = torch.randint(0, 10007, (64, 17), generator=g, dtype=torch.int32), torch.randn(64, 17, generator=g)
+    want = tokens.distill(x.double().numpy(), ids.numpy(), teacher.double().numpy(), np.ones(64))[1]
+    plan, x_ = dd.distdl_logits_plan_create(64, 10007, 3, F32), cut(x.cuda(), 3)
+    dx = [torch.empty_like(t) for t in x_]
+    dd.distdl_distill_fwd_bwd(plan, x_, ids.cuda(), teacher.cuda(), None, None, dx)
+    got = torch.cat(dx, 1).double().cpu().numpy()
+    rest = np.ones(got.shape, bool)  # (without the teacher's places, which are computed for themselves)
+    np.put_along_axis(rest, ids.numpy(), False, 1)
+    assert np.linalg.norm((got - want)[rest]) <= 4e-7 * np.linalg.norm(want[rest])
