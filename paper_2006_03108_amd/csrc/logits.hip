@@ -208,6 +208,11 @@ struct LogitsSums {
   __device__ __forceinline__ bool far() const { return fabsf(mc) >= kFar; }
   // d of an entry
   __device__ __forceinline__ float of(float x, float c) const { return far() ? (x - m) * c : fmaf(x, c, -mc); }
+  // log p of an entry, total: log2 s.  In units of log 2 the lowest numbers have none, so where d says -inf it is the difference over the temperature.
+  __device__ __forceinline__ float log_p(float x, float c, float inv_t, float total) const {
+    const float d = of(x, c);
+    return d == -INFINITY ? fmaf(x - m, inv_t, -kLn2 * total) : kLn2 * (d - total);
+  }
   __device__ __forceinline__ bool none() const { return m == -INFINITY && s == 0.f; }  // every entry is -inf
   // the reference moves up to the maximum m1
   __device__ __forceinline__ void raise(float m1, float c) {
@@ -410,14 +415,14 @@ __device__ __forceinline__ void logits_finish(const LogitsArgs& s, int64_t row, 
     if (s.logp) {
       const int t = s.targets[row];
       float v = 0.f;
-      if (t >= 0 && t < s.n_v) v = none ? -INFINITY : kLn2 * (a.of(x_target, s.c) - total);
+      if (t >= 0 && t < s.n_v) v = none ? -INFINITY : a.log_p(x_target, s.c, s.inv_t, total);
       s.logp[row] = v;
     }
   }
   if (s.n_top > 0 && threadIdx.x < s.n_top) {
     const int64_t o = row * s.n_top + threadIdx.x;
     if (s.ids) s.ids[o] = best ? (int32_t)~(uint32_t)best : -1;
-    if (s.top) s.top[o] = none || !best ? -INFINITY : kLn2 * (a.of(value_of(best), s.c) - total);
+    if (s.top) s.top[o] = none || !best ? -INFINITY : a.log_p(value_of(best), s.c, s.inv_t, total);
   }
 }
 
@@ -692,10 +697,10 @@ __device__ __forceinline__ float stored_loss(const LogitsArgs& s, Stored<N>& t, 
   const float inv = __builtin_amdgcn_exp2f(-total);
   for (int k = threadIdx.x; k < s.n_top; k += THREADS) {
     const float d = (t.p[k] - most) * s.c, p = __builtin_amdgcn_exp2f(d) * inv;
-    if (!(p == 0.f)) loss = fmaf(p, (d - total) - (a.of(t.x[k], s.c) - stotal), loss);
+    if (!(p == 0.f)) loss = fmaf(p, kLn2 * (d - total) - a.log_p(t.x[k], s.c, s.inv_t, stotal), loss);
     t.p[k] = p;
   }
-  return kLn2 * group_sum<THREADS / 64>(loss, t.red);
+  return group_sum<THREADS / 64>(loss, t.red);
 }
 
 // Whether a place comes twice: they go into a table of twice their number, by a hash of the place.  (All threads of the workgroup.)

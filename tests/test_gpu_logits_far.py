@@ -172,3 +172,29 @@ def test_gradients_are_as_near_as_the_rounding_of_differences():
     rest = np.ones(got.shape, bool)  # (without the teacher's places, which are computed for themselves)
     np.put_along_axis(rest, ids.numpy(), False, 1)
     assert np.linalg.norm((got - want)[rest]) <= 4e-7 * np.linalg.norm(want[rest])
+
+
+@TYPES
+@pytest.mark.parametrize("rows, n_v, parts", [(7, 20011, 3), (520, 9001, 2), (520, 1203, 3), (600, 100, 33)])
+def test_log_probabilities_of_the_lowest_value(rows, n_v, parts, dtype):
+    """Masks of the type's lowest value are numbers, and so are their log probabilities: -3.4e38, where it is in the range of 32 bits over the temperature."""
+    require_gpu()
+    for temperature in (1.0, 1.7):
+        x, _, g = masked(rows, n_v, dtype, torch.finfo(dtype).min, temperature, 8)
+        targets = torch.randint(0, n_v, (rows,), generator=g, dtype=torch.int32)
+        for r in range(rows):
+            if r % 7 in (1, 2, 5):
+                targets[r] = 0  # masked
+        check_forward(x, targets, parts, 9, temperature)
+        ids = targets[:, None].repeat(1, 2).contiguous()
+        ids[:, 1] = (ids[:, 0] + 1) % n_v
+        teacher = torch.tensor([[0.0, 1.0]]).repeat(rows, 1).contiguous()
+        loss = torch.full((rows,), 7.0, device="cuda")
+        plan, x_ = dd.distdl_logits_plan_create(rows, n_v, parts, dtype), cut(x.cuda(), parts)
+        dd.distdl_distill_fwd_bwd(plan, x_, ids.cuda(), teacher.cuda(), None, loss, None, temperature)
+        want = tokens.distill(x.double().numpy(), ids.numpy(), teacher.double().numpy(), np.ones(rows), temperature)[0]
+        near(loss, want, 2 * TOL + TOL * np.abs(want), "loss")
+        dx = [torch.full_like(t, 7.0) for t in x_]
+        again = torch.full((rows,), 7.0, device="cuda")
+        dd.distdl_distill_fwd_bwd(plan, x_, ids.cuda(), teacher.cuda(), None, again, dx, temperature)
+        near(again, want, 2 * TOL + TOL * np.abs(want), "loss beside a gradient")
