@@ -610,8 +610,7 @@ int distdl_adamw_step(distdl_adamw_plan* plan, void* const p_dev[], const void* 
  * gradients.  A row of nothing else has lse -inf, log probabilities -inf,
  * entropy 0 and gradients 0.  A row with +inf or a NaN answers NaN.  Masks of
  * the type's lowest value are numbers: a row of them alone is an even one (but
- * logprob_bwd, whose lse cannot hold how many they are, gives gradients 0 to
- * rows with an lse below -1e30).
+ * logprob_bwd gives gradients 0 to rows with an lse below -1e30).
  *
  * logprob_fwd: lse = log sum exp z;  logp = z[target] - lse, and 0 where the
  *   target is not in 0 .. n_v - 1 (targets are int32 [rows]);  entropy =
@@ -622,7 +621,8 @@ int distdl_adamw_step(distdl_adamw_plan* plan, void* const p_dev[], const void* 
  * logprob_bwd: dx = (dlogp (1[target] - p) - dentropy p (log p + entropy)) /
  *   temperature, from the lse and entropy that fwd wrote.  dlogp (with the
  *   targets) or dentropy (with the entropy) may be NULL; rows without a target
- *   have no part in dlogp.  A row whose gradients are 0 gets zeros without
+ *   have no part in dlogp.  Rows with an lse beyond -256 .. 256, which 24 bits
+ *   do not hold well enough, are read once more for it.  A row whose gradients are 0 gets zeros without
  *   being read.  dx may lie on x.
  * distill_fwd_bwd: a teacher's n_top (1 to 1024) logits or log probabilities
  *   for each row, fp32 [rows][n_top], at the places ids (int32); a place that

@@ -147,15 +147,21 @@ struct LogitsVector {
 template <class E>
 constexpr int logits_batch() { return sizeof(E) == 2 ? 4 : 2; }  // vectors of a lane under way: 64 bytes
 
-// f(worker, part, first vector of the workgroup's batch, end) for the batches of the split's vectors
+// f(worker, part, first vector of the workgroup's batch, end) for the batches of a row's vectors lo .. hi - 1
+__device__ __forceinline__ int logits_row_vectors(const LogitsArgs& s) { return s.extra * s.vec_wide + (s.P - s.extra) * s.vec_rest; }
 template <int B, int THREADS, class F>
-__device__ __forceinline__ void logits_each(const LogitsArgs& s, int split, F f) {
-  const int lo = split * s.per, hi = min(lo + s.per, s.extra * s.vec_wide + (s.P - s.extra) * s.vec_rest);
+__device__ __forceinline__ void logits_between(const LogitsArgs& s, int lo, int hi, F f) {
   for (int j = 0; j < s.P; ++j) {
     const LogitsPart p = logits_part(s, j);
     const int from = max(0, lo - p.vec0), to = min(p.vecs, hi - p.vec0);
     for (int base = from; base < to; base += THREADS * B) f(j, p, base, to);
   }
+}
+// ... of the split's
+template <int B, int THREADS, class F>
+__device__ __forceinline__ void logits_each(const LogitsArgs& s, int split, F f) {
+  const int lo = split * s.per;
+  logits_between<B, THREADS>(s, lo, min(lo + s.per, logits_row_vectors(s)), f);
 }
 
 // ---- lanes ----------------------------------------------------------------
@@ -426,6 +432,26 @@ __device__ __forceinline__ void logits_finish(const LogitsArgs& s, int64_t row, 
   }
 }
 
+// Sums of a row's vectors lo .. hi - 1.
+template <class E, bool ENTROPY, bool TINY, int THREADS>
+__device__ __forceinline__ void logits_sum(const LogitsArgs& s, LogitsTable table, int64_t row, int lo, int hi, LogitsSums& a) {
+  constexpr int B = logits_batch<E>();
+  logits_between<B, THREADS>(s, lo, hi, [&](int j, const LogitsPart& p, int base, int to) {
+    const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
+    LogitsVector<E, TINY> v[B];
+    float f[B * 8], all = -INFINITY;
+    const int v0 = base + threadIdx.x, end = base + B * THREADS;
+#pragma unroll
+    for (int b = 0; b < B; ++b) v[b].load(x, p.n, v0 + b * THREADS);
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      v[b].values(f + 8 * b, p.n, v0 + b * THREADS, to, end > to, p.n % 8 != 0 && end >= p.vecs);
+      all = fmaxf(all, max8(f + 8 * b));
+    }
+    logits_add<B * 8, ENTROPY>(a, f, all, s.c);
+  });
+}
+
 // A row, or one of its splits, to a workgroup.  THREADS: 64 for short rows, whose waves have nothing to join.
 template <class E, bool ENTROPY, bool TOP, bool FEW, bool TINY, int THREADS>
 __global__ __launch_bounds__(THREADS, 8) void logits_fwd_kernel(LogitsArgs s) {
@@ -443,7 +469,7 @@ __global__ __launch_bounds__(THREADS, 8) void logits_fwd_kernel(LogitsArgs s) {
   typedef LogitsVector<E, TINY> Vector;
   if constexpr (TOP) {
     // The next vectors are under way while these are looked through; one place in the code for both, and for what is rarely done.
-    const int lo = split * s.per, hi = min(lo + s.per, s.extra * s.vec_wide + (s.P - s.extra) * s.vec_rest);
+    const int lo = split * s.per, hi = min(lo + s.per, logits_row_vectors(s));
     for (int j = 0; j < s.P; ++j) {
       const LogitsPart p = logits_part(s, j);
       const int from = max(0, lo - p.vec0), to = min(p.vecs, hi - p.vec0);
@@ -492,20 +518,7 @@ __global__ __launch_bounds__(THREADS, 8) void logits_fwd_kernel(LogitsArgs s) {
       }
     }
   } else {
-    logits_each<B, THREADS>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
-      const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
-      Vector v[B];
-      float f[B * 8], all = -INFINITY;
-      const int v0 = base + tid, end = base + B * THREADS;
-#pragma unroll
-      for (int b = 0; b < B; ++b) v[b].load(x, p.n, v0 + b * THREADS);
-#pragma unroll
-      for (int b = 0; b < B; ++b) {
-        v[b].values(f + 8 * b, p.n, v0 + b * THREADS, to, end > to, p.n % 8 != 0 && end >= p.vecs);
-        all = fmaxf(all, max8(f + 8 * b));
-      }
-      logits_add<B * 8, ENTROPY>(a, f, all, s.c);
-    });
+    logits_sum<E, ENTROPY, TINY, THREADS>(s, table, row, split * s.per, min(split * s.per + s.per, logits_row_vectors(s)), a);
   }
   if constexpr (TOP) {
     list.flush(buffer, s.n_top);
@@ -586,7 +599,9 @@ __device__ __forceinline__ void logits_store(E* row, const float* f, int at, int
   }
 }
 
-constexpr float kLseFar = 1e30f;
+// An lse has 24 bits: of a shifted or masked row little or nothing of what exp needs.  Up to 256 it leaves p right to 4e-5; beyond, the row is read for its sums again, by its
+// first workgroup alone where it is cut (the gradient may lie on it).
+constexpr float kLseFar = 256.f, kLseNone = 1e30f;
 
 template <class E, bool ENTROPY, bool TINY, int THREADS>
 __global__ __launch_bounds__(THREADS) void logits_bwd_kernel(LogitsArgs s) {
@@ -599,10 +614,21 @@ __global__ __launch_bounds__(THREADS) void logits_bwd_kernel(LogitsArgs s) {
   const float lse = s.lse[row], weight = live ? s.dlogp[row] : 0.f, back = ENTROPY ? s.dentropy[row] : 0.f;
   // dx = p (one + two log2 p) / temperature, and the target's dlogp
   const float one = (-weight - (ENTROPY ? back * s.entropy[row] : 0.f)) * s.inv_t, two = -back * kLn2 * s.inv_t;
-  const bool nothing = (weight == 0.f && back == 0.f) || lse < -kLseFar;  // such rows are not read
-  const bool far = lse >= kLseFar;
+  const bool nothing = (weight == 0.f && back == 0.f) || lse < -kLseNone;  // such rows are not read
+  const bool far = !nothing && fabsf(lse) >= kLseFar;
   const float lc = lse * (1.f / kLn2), at_target = weight * s.inv_t;
-  logits_each<B, THREADS>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
+  int lo = split * s.per, hi = min(lo + s.per, logits_row_vectors(s));
+  LogitsSums a;
+  float stotal = 0.f;
+  if (far) {
+    if (split > 0) return;
+    hi = logits_row_vectors(s);
+    __shared__ float4 sums[THREADS / 64];
+    logits_sum<E, false, TINY, THREADS>(s, table, row, lo, hi, a);
+    a.template join_waves<THREADS / 64>(sums, s.c);
+    stotal = __builtin_amdgcn_logf(a.s);
+  }
+  logits_between<B, THREADS>(s, lo, hi, [&](int j, const LogitsPart& p, int base, int to) {
     const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
     E* const dx = (E*)table[j].dx + row * p.n;
     typedef LogitsVector<E, TINY> Vector;
@@ -621,7 +647,7 @@ __global__ __launch_bounds__(THREADS) void logits_bwd_kernel(LogitsArgs s) {
         v[b].values(f, p.n, i0, to, false, false);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float d = far ? fmaf(f[i], s.inv_t, -lse) * (1.f / kLn2) : fmaf(f[i], s.c, -lc), e = __builtin_amdgcn_exp2f(d);
+          const float d = far ? a.of(f[i], s.c) - stotal : fmaf(f[i], s.c, -lc), e = __builtin_amdgcn_exp2f(d);
           f[i] = ENTROPY ? e * fmaf(two, fmaxf(d, -200.f), one) : e * one;
           if (live && p.first + at + i == target) f[i] += at_target;
         }
@@ -778,20 +804,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(LogitsArgs s) {
   }
   const bool sum_here = FIRST || s.splits == 1;
   if (sum_here && (FIRST || any)) {
-    logits_each<B, THREADS>(s, split, [&](int j, const LogitsPart& p, int base, int to) {
-      const __amdgpu_buffer_rsrc_t x = logits_row(table[j].x, row, p.n, sizeof(E));
-      LogitsVector<E, TINY> v[B];
-      float f[B * 8], all = -INFINITY;
-      const int v0 = base + tid, end = base + B * THREADS;
-#pragma unroll
-      for (int b = 0; b < B; ++b) v[b].load(x, p.n, v0 + b * THREADS);
-#pragma unroll
-      for (int b = 0; b < B; ++b) {
-        v[b].values(f + 8 * b, p.n, v0 + b * THREADS, to, end > to, p.n % 8 != 0 && end >= p.vecs);
-        all = fmaxf(all, max8(f + 8 * b));
-      }
-      logits_add<B * 8, false>(a, f, all, s.c);
-    });
+    logits_sum<E, false, TINY, THREADS>(s, table, row, split * s.per, min(split * s.per + s.per, logits_row_vectors(s)), a);
     a.join_waves<THREADS / 64>(sums, s.c);
   }
   if (FIRST) {

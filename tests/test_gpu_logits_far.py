@@ -198,3 +198,48 @@ def test_log_probabilities_of_the_lowest_value(rows, n_v, parts, dtype):
         again = torch.full((rows,), 7.0, device="cuda")
         dd.distdl_distill_fwd_bwd(plan, x_, ids.cuda(), teacher.cuda(), None, again, dx, temperature)
         near(again, want, 2 * TOL + TOL * np.abs(want), "loss beside a gradient")
+
+
+def check_adjoint(x, targets, parts, temperature, g):
+    """p is off by TOL of itself and log p + H by 2 TOL; in place gives the same bits."""
+    rows, dtype = x.shape[0], x.dtype
+    dlogp, dent = torch.randn(rows, generator=g), torch.randn(rows, generator=g)
+    plan, (_, lse, entropy, _, _) = forward(x, targets, parts, 0, temperature)
+    n, w, e = x.double().numpy(), dlogp.double().numpy()[:, None], dent.double().numpy()[:, None]
+    log_p = tokens.log_softmax(n, temperature)[0]
+    p, live = np.exp(log_p), ((targets >= 0) & (targets < x.shape[1])).numpy()
+    hit = np.zeros(n.shape)
+    hit[live, targets.numpy()[live]] = 1
+    for what in ("logp", "entropy", "both"):
+        with_w, with_e = w * (what != "entropy") * live[:, None], e * (what != "logp")
+        want = tokens.logprob_adjoint(n, targets.numpy(), with_w[:, 0], with_e[:, 0], temperature)
+        size = np.abs(with_w) * (hit + p) + np.abs(with_e) * p * (np.maximum(np.abs(log_p), -200) + np.log(x.shape[1]) + 2)
+        x_ = cut(x.cuda(), parts)
+        args = (targets.cuda(), lse, entropy if what != "logp" else None, dlogp.cuda() if what != "entropy" else None, dent.cuda() if what != "logp" else None)
+        dx = [torch.full_like(t, 7.0) for t in x_]
+        dd.distdl_logprob_bwd(plan, x_, *args, dx, temperature)
+        got = torch.cat(dx, 1)
+        near(got, want, TOL * size / temperature + 1e-12 + (2.0 ** -8 * np.abs(want) if dtype == BF16 else 0), what)
+        dd.distdl_logprob_bwd(plan, x_, *args, x_, temperature)
+        assert torch.equal(torch.cat(x_, 1), got)
+
+
+@TYPES
+@MASKS
+@pytest.mark.parametrize("rows, n_v, parts", [(7, 20011, 3), (2, 70001, 1), (520, 3001, 2), (520, 9001, 1), (600, 100, 33)])
+def test_adjoint_of_masks_that_are_numbers(rows, n_v, parts, mask, dtype):
+    """A row of nothing but the mask is an even one, though its lse cannot hold how many entries it has."""
+    require_gpu()
+    for temperature in (1.0, 0.3):
+        x, targets, g = masked(rows, n_v, dtype, mask, temperature, 9)
+        check_adjoint(x, targets, parts, temperature, g)
+
+
+@pytest.mark.parametrize("shift", [200.0, -300.0, 5e3, -1e5, 1e6, 1e7])
+@pytest.mark.parametrize("rows, n_v, parts", [(7, 20011, 3), (520, 1203, 3), (520, 9001, 1)])
+def test_adjoint_of_shifted_rows(rows, n_v, parts, shift):
+    require_gpu()
+    g = torch.Generator().manual_seed(10)
+    x = shift + 3 * torch.randn(rows, n_v, generator=g)
+    targets = torch.randint(-1, n_v, (rows,), generator=g, dtype=torch.int32)
+    check_adjoint(x, targets, parts, 1.0, g)
