@@ -48,10 +48,10 @@ struct DeltaArgs {
   uint16_t *kf, *ktf, *qf, *qtf;      // fragments of K, K^T, Q, Q^T
   // ... and for each sequence, chunk and head
   uint16_t *tf, *pf, *ttf, *ptf;      // fragments of T and P, and of their transposes
-  float* tiles;                       // A and P, tiles on and below the diagonal as they lie in the lanes
+  float* tiles;                       // A / beta and P, tiles on and below the diagonal as they lie in the lanes
   float* steps;                       // of each step: kStepNumbers of them, [C] each
   float *states, *dstates;            // [DK][dvp] at a chunk's start; the gradient at its end
-  float *u, *dr;                      // [C][dvp]
+  float *u, *dr;                      // [C][dvp]; in u X where beta is 0
   float* keys;                        // parts of dq and dk, where a chunk's heads are workgroups of their own
 };
 

@@ -22,8 +22,8 @@ namespace distdl {
 // A factor of exp(-200) is 0 in 32 bits, and so is what it stands between.
 __device__ __forceinline__ float bounded(float g) { return g < -200.f ? -200.f : g; }
 
-// beta's gradient is dR U / beta, what beta multiplies being U / beta.  So a beta of 0 counts as 2^-100: what it adds to a state does not show.
-__device__ __forceinline__ float nonzero(float beta) { return fabsf(beta) < 0x1p-100f ? 0x1p-100f : beta; }
+// The adjoint has what beta multiplies as U / beta, where beta is no less than 2^-64: below, it is 0, which adds nothing to a state, and X is kept in U's place.
+__device__ __forceinline__ float divisor(float beta) { return fabsf(beta) < 0x1p-64f ? 0.f : beta; }
 
 // Whether K^T is made of K where it is used.
 template <class E>
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
     const int64_t head = ((int64_t)b * s.chunks + c) * s.n_h + h;
     const bool live = lane < at.live;
     const int64_t o = (step0 + lane) * s.n_h + h;
-    const float beta = live ? nonzero(w->beta[o]) : 0.f;
+    const float beta = !live ? 0.f : BACK ? divisor(w->beta[o]) : w->beta[o];
     double sum = live && w->g ? (double)bounded(w->g[o]) * 1.4426950408889634 : 0.0;
 #pragma unroll
     for (int d = 1; d < C; d *= 2) {
@@ -233,14 +233,14 @@ __global__ __launch_bounds__(256, 2) void delta_prepare_kernel(DeltaArgs s) {
       const DeltaLower at_tile = delta_lower(wave + 4 * x);
       const int j = at_tile.nt * 16 + row;
       const float whole = m.whole[slot][j], rest = m.rest[slot][j];
-      f32x4 a, p;
+      f32x4 a, p;  // (a: A / beta)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int i = at_tile.mt * 16 + 4 * g + r;
         const float decay = i >= j ? __builtin_amdgcn_exp2f((m.whole[slot][i] - whole) + (m.rest[slot][i] - rest)) : 0.f;
-        a[r] = i > j ? m.beta[slot][i] * decay * kk[x][r] : 0.f;
+        a[r] = i > j ? decay * kk[x][r] : 0.f;
         p[r] = i >= j ? s.scale * decay * qk[x][r] : 0.f;
-        m.a[i][j] = a[r];
+        m.a[i][j] = m.beta[slot][i] * a[r];
         m.p[i][j] = p[r];
         if (at_tile.mt != at_tile.nt) m.p[at_tile.nt * 16 + 4 * g + r][at_tile.mt * 16 + row] = 0.f;
       }
@@ -678,7 +678,7 @@ __global__ __launch_bounds__(STORE ? 256 : 512, 2) void delta_fwd_kernel(DeltaAr
       if (!STORE) for_out.write(wave, n, u[n]);
       if (STORE && col + 16 * n < s.dvp) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s.u[(head * kChunk + 16 * wave + 4 * g + r) * s.dvp + col + 16 * n] = u[n][r];
+        for (int r = 0; r < 4; ++r) s.u[(head * kChunk + 16 * wave + 4 * g + r) * s.dvp + col + 16 * n] = steps.beta[r] == 0.f ? x[n][r] : u[n][r];
       }
     }
 #pragma unroll
@@ -887,7 +887,7 @@ __global__ __launch_bounds__(512, 2) void delta_bwd_kernel(DeltaArgs s) {
 //   dA = -strictly lower (dR U^T),  dP = lower (dO U^T),  M = dA beta D,  N = scale D dP,  M and N of k_i k_j and q_i k_j
 //   dq = N K + scale exp(G) (dO S^T)
 //   dk = N^T Q + (M + M^T) K - exp(G) beta (dR S^T) + Y,  Y = exp(G_C - G) (U dS'^T)
-//   dv = beta dR,  dbeta_i = dR_i U_i / beta_i  (u = beta r, and dbeta = du r, of the step itself)
+//   dv = beta dR,  dbeta_i = dR_i U_i / beta_i  (u = beta r, and dbeta = du r, of the step itself; with beta of 0, r_i = X_i - sum_j A_ij / beta_i u_j)
 //   dG_i = sums of (M k k + N q k) over row i less those over column i, and the rows' products of q, k with what they were multiplied by; what
 //   exp(G_C) multiplies goes to the last step;  dg_t = sum of dG from t on
 template <class E, int C, int DK>
@@ -1111,6 +1111,12 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
         float r[8], u[8], out[8];
         numbers(r8, r);
         numbers(u8, u);
+        const float beta = m.steps[kBeta][t8], inverse = beta == 0.f ? 1.f : 1.f / beta;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          udot = fmaf(r[i], u[i] * inverse, udot);
+          u[i] = beta == 0.f ? 0.f : u[i];
+        }
         const Pieces<3> rp = split8(r), up = split8(u);
 #pragma unroll
         for (int k = 0; k < 3; ++k) {
@@ -1127,12 +1133,8 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
 #pragma unroll
           for (int k = 0; k < 3; ++k) *(u32x4*)&m.d_o[k][t8][col8] = op.p[k];
         }
-        const float beta = m.steps[kBeta][t8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          udot = fmaf(r[i], u[i], udot);
-          out[i] = t8 < at.live ? beta * r[i] : 0.f;
-        }
+        for (int i = 0; i < 8; ++i) out[i] = t8 < at.live ? beta * r[i] : 0.f;
         const int v = v0 + col8;
         if (t8 < at.n && v < s.d_v) store8(dv + ((step0 + t8) * s.n_h + h) * s.d_v + v, out, min(8, s.d_v - v));
       }
@@ -1194,7 +1196,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
       kk[k] = load_pieces(ktf, (kt * Z::kSteps + k) * NI * kFragment * 2);
       qq[k] = load_pieces(qtf, (kt * Z::kSteps + k) * NI * kFragment * 2);
     }
-    // M and N, in pieces; what A and P were made of is in them still: M k k = -dA A, and N q k = dP P
+    // M and N, in pieces; what A and P were made of is in them still: M k k = -dA A, of which beta is left out along the rows, and N q k = dP P
     const int j = nt * 16 + row;
     const float whole = m.steps[kWhole][j], rest = m.steps[kRest][j];
     float down[2] = {};
@@ -1210,7 +1212,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
         const float all = decay * acc[x][r] * (what ? s.scale : -beta_i[r]), part = what ? acc[x][r] * made[x][r] : -acc[x][r] * made[x][r];
         mine[r] = in ? all : 0.f;
         const float mine_part = below ? part : 0.f;
-        down[kBoth ? x / 2 : 0] += mine_part;
+        down[kBoth ? x / 2 : 0] += what ? mine_part : mine_part * beta_i[r];
         across[r] = sum16(mine_part);
       }
       const float across_of = row < 2 ? row ? across[1] : across[0] : row == 2 ? across[2] : across[3];
@@ -1323,14 +1325,16 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
     }
     if (wave == 0) {
       const int tile = lane >> 4;
-      float d = 0.f, end = 0.f, for_beta = lane < at.live ? m.us[lane] / m.steps[kBeta][lane] : 0.f, all = 0.f;
+      float d = 0.f, end = 0.f, all = 0.f, rows[2] = {};
+      const float beta = m.steps[kBeta][lane];
 #pragma unroll
       for (int what = 0; what < 2; ++what) {
 #pragma unroll
         for (int i = 0; i < Z::kTiles; ++i) {
           const float v = m.row_sum[what][i][lane];  // (what no wave wrote is not used)
-          d += i <= tile ? v : 0.f;
+          rows[what] += i <= tile ? v : 0.f;
         }
+        d += what ? rows[what] : beta * rows[what];
 #pragma unroll
         for (int i = 0; i < Z::kTiles / kMine; ++i) d -= m.col_sum[what][i][lane];
       }
@@ -1350,7 +1354,7 @@ __global__ __launch_bounds__(512, 2) void delta_grad_kernel(DeltaArgs s) {
       if (lane < at.n) {
         const int64_t o = (step0 + lane) * s.n_h + h;
         if (w->dg) w->dg[o] = lane < at.live ? d : 0.f;
-        w->dbeta[o] = for_beta;
+        w->dbeta[o] = lane < at.live ? m.us[lane] + (beta == 0.f ? rows[0] : 0.f) : 0.f;
       }
     }
     if constexpr (SPLIT) {
