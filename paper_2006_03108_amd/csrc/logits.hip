@@ -494,6 +494,15 @@ __global__ __launch_bounds__(THREADS, 8) void logits_fwd_kernel(LogitsArgs s) {
           all = fmaxf(all, most[b]);
         }
         logits_add<B * 8, ENTROPY>(a, f, all, s.c);
+        if (__any(a.s != a.s)) {  // (a signalling NaN was the maximum of it and a number: made quiet, it is not)
+          asm volatile("");
+#pragma unroll
+          for (int b = 0; b < B; ++b) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[8 * b + i] = __builtin_canonicalizef(f[8 * b + i]);
+            most[b] = max8(f + 8 * b);
+          }
+        }
         if (first) list.start(all, s.n_top);
         first = false;
         bool any = false;

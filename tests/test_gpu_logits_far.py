@@ -243,3 +243,25 @@ def test_adjoint_of_shifted_rows(rows, n_v, parts, shift):
     x = shift + 3 * torch.randn(rows, n_v, generator=g)
     targets = torch.randint(-1, n_v, (rows,), generator=g, dtype=torch.int32)
     check_adjoint(x, targets, parts, 1.0, g)
+
+
+@pytest.mark.parametrize("dtype, bits", [(F32, 0x7f800001), (F32, -1), (BF16, 0x7f81), (BF16, -1)])
+@pytest.mark.parametrize("rows", [3, 520, 4100])
+def test_nans_of_all_kinds_are_no_alternatives(rows, dtype, bits):
+    """Signalling NaNs too, beside the best entries: a maximum of one and a number is the NaN.  Half of the rows have none."""
+    require_gpu()
+    g = torch.Generator().manual_seed(11)
+    x = torch.randn(rows, 3001, generator=g).to(dtype)
+    top = x.float().argsort(dim=1, descending=True, stable=True)[:, :8]
+    clean = x.clone()
+    raw = x.view(torch.int32 if dtype == F32 else torch.int16)
+    for r in range(0, rows, 2):
+        at = int(top[r, r // 2 % 8])
+        for j in range(at // 8 * 8, min(at // 8 * 8 + 8, 3001)):
+            if j not in top[r].tolist() and (j + r // 2) % 2:
+                raw[r, j] = bits
+    _, (_, lse, _, ids, _) = forward(x, torch.zeros(rows, dtype=torch.int32), 1, 8)
+    want = torch.nan_to_num(x.float(), nan=-torch.inf).argsort(dim=1, descending=True, stable=True)[:, :8]
+    assert torch.equal(ids.cpu().long(), want)
+    assert torch.equal(lse.isnan().cpu(), x.float().isnan().any(1))
+    assert torch.equal(x[1::2], clean[1::2])
