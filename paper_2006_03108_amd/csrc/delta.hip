@@ -371,12 +371,6 @@ struct DeltaShared {
 #pragma unroll
     for (int i = 0; i < N; ++i) ((u32x2*)&v[tile >> 1][n][i][threadIdx.x & 63])[tile & 1] = u32x2{p.p[i][0], p.p[i][1]};
   }
-  // tiles 2 k and 2 k + 1
-  __device__ __forceinline__ void write(int k, int n, f32x4 x, f32x4 y) {
-    const Pieces<3> p = split_tiles(x, y);
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[k][n][i][threadIdx.x & 63] = p.p[i];
-  }
 };
 // Every STRIDE-th piece from piece `from` on begins a fragment.  `at`: the first one's place, `hop`: from chunk to chunk.
 template <int COUNT, int N, int STRIDE>
@@ -445,8 +439,6 @@ struct DeltaTurn {
         turned[i * 2 + mt / 2].p[0][mt % 2 * 2 + 1] = to_bf16(v[2], v[3]);
       }
   }
-  template <int N, int M>
-  __device__ __forceinline__ void operator()(const Pieces<N>&, Pieces<M>&) const {}
 };
 // Tiles of results in fp32, as they lie in the lanes.
 template <int TILES, int NT>
