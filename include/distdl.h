@@ -548,7 +548,13 @@ int distdl_scan_step(const void* a_dev, const void* x_dev, float* state_dev, int
  * fwd and bwd keep what chunks of steps need in the plan's scratch, bwd two
  * states for each 64 steps: calls and recorded graphs
  * of one plan and stream share it, they run one after another.
- * UNSUPPORTED: d_k from 129 on, n_h d_v from 2^22 on. */
+ * Where an input of a live step is no finite number, the outputs of its chunk
+ * of 64 steps may be NaN, those in front of it too; so may they be where the
+ * factors of a chunk multiply to more than 32 bits hold.
+ * UNSUPPORTED: d_k above 128; n_h d_v or n_hk d_k above 2^22, n_h or d_v above
+ * 2^20; plans with T from 2^30 on, n_b from 2^20 on, n_b n_hk (T / 64 + P) or
+ * n_b n_h (d_v + 15) / 16 from 2^23 on (quotients rounded down); steps with
+ * rows n_h (d_v + 31) / 32 from 2^24 on. */
 typedef struct distdl_delta_plan distdl_delta_plan;
 int distdl_delta_plan_create(distdl_delta_plan** out, int64_t n_b, int64_t T, int64_t n_h, int64_t n_hk, int64_t d_k,
                              int64_t d_v, int P, double scale, distdl_dtype dtype);
@@ -622,8 +628,8 @@ int distdl_adamw_step(distdl_adamw_plan* plan, void* const p_dev[], const void* 
  *   temperature, from the lse and entropy that fwd wrote.  dlogp (with the
  *   targets) or dentropy (with the entropy) may be NULL; rows without a target
  *   have no part in dlogp.  Rows with an lse beyond -256 .. 256, which 24 bits
- *   do not hold well enough, are read once more for it.  A row whose gradients are 0 gets zeros without
- *   being read.  dx may lie on x.
+ *   do not hold well enough, are read once more for it.  A row whose gradients
+ *   are 0 gets zeros without being read.  dx may lie on x.
  * distill_fwd_bwd: a teacher's n_top (1 to 1024) logits or log probabilities
  *   for each row, fp32 [rows][n_top], at the places ids (int32); a place that
  *   is not in 0 .. n_v - 1 is not used, one that comes twice counts twice.
