@@ -1021,7 +1021,8 @@ static int64_t logits_rounds(const LogitsArgs& s, int threads, int batch) {
 }
 // Whether a row is one wave's: nothing to join, and where a worker's part is short, no waves without work.  us for 8192 rows, bf16, workgroup / wave:
 //   sums                   8192 entries on 1 worker 31 / 26, 16384 on 1 52 / 54, 16384 on 8 140 / 52
-//   with 20 alternatives   512 on 1 52 / 19, 16384 on 1 146 / 103 (600 rows: 1024 on 1 12.6 / 9.9, 8192 on 1 18 / 29)
+//   with 20 alternatives   512 on 1 48 / 16, 16384 on 1 133 / 94; 4096 rows: 512 27 / 11, 16384 73 / 60; 2048 rows: 2048 19 / 14, 4096 20 / 21, 8192 28 / 32;
+//                          1024 rows: 1024 12.6 / 9.4, 2048 13.2 / 13.4, 4096 14 / 20; 600 rows: 1024 11.6 / 9.2, 2048 12.0 / 13.4, 8192 18 / 29
 //   adjoint                4096 on 1 32 / 27, 8192 on 1 52 / 57, 2048 on 8 203 / 61
 //   distillation           4096 on 1 62 / 48, 8192 on 1 88 / 91, 16384 on 8 143 / 166
 static int64_t logits_vectors(const LogitsArgs& s) { return s.extra * s.vec_wide + (int64_t)(s.P - s.extra) * s.vec_rest; }
