@@ -415,8 +415,8 @@ struct DeltaSteps {
   }
 };
 // K^T of a wave's keys from K of the same: a product of tiles of steps with a matrix of zeros and ones has K's numbers where a lane of the left operand K^T
-// wants them.  With bf16 keys that is 8 products and 16 other instructions in the time of the partial sums' reads, and 16 of 62 KiB less to load for a
-// chunk (222 us instead of 238 for 8192 steps of 32 heads); with the three pieces of fp32 keys it is three times that, and fragments are loaded.
+// wants them.  With bf16 keys that is 8 products and 16 other instructions in the time of the partial sums' reads, and 16 KiB less to load for a
+// chunk and to make in front (the call 290 us instead of 316 for 8192 steps of 32 heads); with the three pieces of fp32 keys it is three times that, and fragments are loaded.
 template <int KT>
 struct DeltaTurn {
   u32x4 ones[KT];  // (16 keys of the 32) of a fragment

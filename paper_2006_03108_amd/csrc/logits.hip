@@ -256,7 +256,7 @@ struct LogitsSums {
     if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = make_float4(m, mc, s, w);
     __syncthreads();
     LogitsSums all;
-    constexpr int kAtOnce = WAVES > 4 ? 2 : WAVES;  // (sixteen places in registers at once would leave a compute unit one workgroup: 480 -> 537 us for 4096 x 131072)
+    constexpr int kAtOnce = WAVES > 4 ? 2 : WAVES;  // (sixteen places in registers at once would leave a compute unit one workgroup: 537 us for 4096 x 131072 distilled, 490 so)
 #pragma unroll kAtOnce
     for (int i = 0; i < WAVES; ++i) {
       const float4 v = shared[i];
@@ -865,7 +865,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(LogitsArgs s) {
 }
 
 // Rows that fit a workgroup's registers (up to 65536 entries of bf16, 32768 of fp32) are read once.  Slot by slot: a slot has a vector for each thread, of one
-// worker.  Longer ones would leave a compute unit one workgroup, which reads, computes and writes in turn: 4096 x 131072, bf16, 648 us that way, 483 us read
+// worker.  Longer ones would leave a compute unit one workgroup, which reads, computes and writes in turn: 4096 x 131072, bf16, 648 us that way, 490 us read
 // twice.
 template <class E>
 constexpr int distill_slots() { return sizeof(E) == 2 ? 16 : 8; }
