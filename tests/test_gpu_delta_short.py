@@ -30,3 +30,12 @@ def test_adjoint_of_one_chunk_of_many_keys(heads):
         for _ in range(4):
             got = run(x, None, 1, 0.3)
             assert all(torch.equal(got[n], want[n]) for n in want)
+
+
+@pytest.mark.parametrize("T, parts", [(700, 2), (1100, 3)])
+def test_many_chunks_within_the_limit_of_chunks_of_64(T, parts):
+    """In fp32, by the argument of test_gpu_delta.py for the chunks of 64 steps that the kernels have: 48 u for a chunk and one more, 48 u (1 + T / 64), of which its limit for
+    chunks of 32 is up to twice as much."""
+    require_gpu()
+    x = make(2, T, 4, 2, 64, 48, F32, T)
+    check(x, torch.tensor([T, T - 70], dtype=torch.int32), parts, factor=(1 + T / 64) / (1 + T / 32))
